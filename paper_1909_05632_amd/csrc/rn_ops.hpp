@@ -1,0 +1,108 @@
+// Internal declarations of the operators in include/reuse_ops.h: kernel
+// launchers (rn_norm.hip, rn_sample.hip, rn_delta.hip, rn_delta_bwd.hip) and
+// device helpers they share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "reuse_ops.h"
+
+namespace rn {
+
+// ------------------------------------------------------------------ launchers
+
+struct NormArgs {
+    int64_t rows;
+    int width;
+    const void *x, *dy;           // dy: backward only
+    void *y;                      // dx in the backward call
+    int64_t xs, dys, ys;          // row strides in elements
+    const float *weight, *bias;
+    float eps;
+    float *stats;                 // [rows][2]; read by the backward call
+    float *part;                  // [blocks][2][width] partial weight and bias gradients, or NULL
+    int blocks;                   // row strips of the backward call
+    float *dweight, *dbias;
+    int accumulate;
+};
+int norm_blocks(int64_t rows, int width);
+hipError_t launch_norm(const NormArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_norm_backward(const NormArgs &a, bool bf16, hipStream_t s);
+
+struct SampleArgs {
+    int n, vocab;
+    const void *logits;
+    int64_t stride;
+    const float *u;
+    rn_sample_params p;
+    int32_t *tokens;
+    float *logprobs;
+};
+hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t s);
+
+struct DeltaArgs {
+    int n, hk, hv, dk, dv;
+    int64_t tokens;
+    float scale;
+    int64_t qs, ks, vs;
+    const void *q, *k, *v;
+    const float *g, *beta;
+    const int32_t *off;           // [n+1], or NULL: even lengths
+    const int32_t *ids;           // step: slots, or NULL
+    int slots;
+    const float *state;           // first states, or NULL
+    float *final_state;           // last states, or NULL (step: the state pool)
+    void *out;
+    // Per chunk slot (delta_chunk_slots) and value head:
+    float *inv;                   // [64][64] (I + A)^-1
+    float *score;                 // [64][64] scale e^(ci - cj) q_i . k_j, j <= i
+    float *before;                // [dk][dv] states before the chunk, or NULL (not kept)
+    // Backward call:
+    const void *dout;
+    const float *dfinal;
+    float *after;                 // [slots][hv][dk][dv] gradients of the states after each chunk
+    float *dwrite;                // [tokens][hv][dv] gradients of beta (v - S^T k)
+    void *dq, *dkey, *dval;
+    float *dg, *dbeta, *dstate;
+};
+// Chunk slots of a call: chunk c of sequence i has slot off[i] / 64 + i + c, so
+// every slot is below tokens / 64 + n and no two chunks share one.
+inline int64_t delta_chunk_slots(int64_t tokens, int n) { return tokens / RN_DELTA_CHUNK + n; }
+hipError_t launch_delta_step(const DeltaArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_delta_forward(const DeltaArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_delta_backward(const DeltaArgs &a, bool bf16, hipStream_t s);
+
+// Allows a kernel the dynamic LDS of its launch (more than the default 64 KiB).
+template <class K>
+inline hipError_t allow_lds(K *kernel, size_t bytes) {
+    if (bytes <= 64 * 1024) return hipSuccess;
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                               (int)bytes);
+}
+
+// ------------------------------------------------------------------ device helpers
+
+namespace ops {
+
+// bf16 as raw 16 bits, so that loads and conversions are explicit.
+struct bf16_t {
+    uint16_t bits;
+};
+__device__ inline float to_float(float v) { return v; }
+__device__ inline float to_float(bf16_t v) { return __uint_as_float((uint32_t)v.bits << 16); }
+template <class T> __device__ inline T from_float(float v);
+template <> __device__ inline float from_float<float>(float v) { return v; }
+// Rounded to nearest even; NaN stays NaN.
+template <> __device__ inline bf16_t from_float<bf16_t>(float v) {
+    return __builtin_bit_cast(bf16_t, static_cast<__bf16>(v));
+}
+
+// VEC consecutive elements in one access; the caller has checked alignment.
+template <class T, int VEC>
+struct alignas(sizeof(T) * VEC) Pack {
+    T v[VEC];
+};
+
+}  // namespace ops
+}  // namespace rn

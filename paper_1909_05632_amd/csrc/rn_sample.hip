@@ -1,0 +1,484 @@
+// Sampling with temperature, top-k, min-p and top-p from given random numbers.
+//
+// With m a row's largest logit and c = log2(e) / temperature,
+//   w_i = rint(2^31 2^((l_i - m) c)),
+// whole numbers, so that sums over them are exact and do not depend on their
+// order: parallel sums and histograms by atomics give the answer of the
+// definition, bit by bit.  2^31 leaves room for 2^22 of them in a double's 53
+// bits; the last bit of a weight is 2^-31 of the largest logit's share.  The
+// filters keep a prefix of the logits in descending order (equal ones by
+// index), so each is a threshold: a logit, and how many of its equals stay.
+#include "rn_ops.hpp"
+
+namespace rn {
+namespace {
+
+using namespace ops;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kOne = 0x1p31f;
+constexpr float kInf = __builtin_huge_valf();
+
+// A row's settings, resolved.
+struct Row {
+    bool greedy;
+    float c, min_p, top_p;
+    int top_k;                    // 0: all
+};
+
+__device__ inline Row row_settings(const rn_sample_params &p, int r) {
+    Row q;
+    const float t = p.dev_temperature ? p.dev_temperature[r] : p.temperature;
+    q.c = kLog2e / t;
+    q.greedy = !(t > 0.f) || !(q.c < kInf);
+    const int k = p.dev_top_k ? p.dev_top_k[r] : p.top_k;
+    q.top_k = k > 0 ? k : 0;
+    const float tp = p.dev_top_p ? p.dev_top_p[r] : p.top_p;
+    q.top_p = tp > 0.f ? tp : 0.f;
+    const float mp = p.dev_min_p ? p.dev_min_p[r] : p.min_p;
+    q.min_p = mp > 0.f ? fminf(mp, 1.f) : 0.f;
+    return q;
+}
+
+// NaN counts as -infinity, -0 as +0, so that order and equality are those of the key.
+__device__ inline float canonical(float l) { return l == l ? l + 0.f : -kInf; }
+__device__ inline uint32_t key_of(float l) {
+    const uint32_t b = __float_as_uint(l);
+    return b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u);
+}
+__device__ inline float of_key(uint32_t k) {
+    return __uint_as_float(k ^ ((int32_t)k < 0 ? 0x80000000u : 0xffffffffu));
+}
+
+// log2 of the weight's share of the largest, exactly as rounded in float32.
+// With a largest logit of +infinity its equals have share 1, the rest none.
+__device__ inline float z_of(float l, float m, float c) {
+    if (m == kInf) return l == kInf ? 0.f : -kInf;
+    return (l - m) * c;
+}
+// Below z = -33 a weight rounds to 0 (and the hardware's exp2, exact in its
+// normal range, would meet denormals).
+__device__ inline uint32_t weight_of(float z, float min_p) {
+    if (!(z > -33.f)) return 0;
+    const float e = __builtin_amdgcn_exp2f(z);
+    return e >= min_p ? (uint32_t)rintf(e * kOne) : 0;
+}
+__device__ inline float log_share(float z, uint64_t total) {
+    return (z - log2f((float)((double)total * 0x1p-31))) * kLn2;
+}
+// floor(u total), below total.
+__device__ inline uint64_t target_of(float u, uint64_t total) {
+    const double t = (double)u * (double)total;
+    if (!(t > 0.0)) return 0;
+    return t < (double)total ? min((uint64_t)t, total - 1) : total - 1;
+}
+
+__device__ inline uint64_t shfl_up64(uint64_t v, int d) { return __shfl_up((unsigned long long)v, d); }
+__device__ inline uint64_t shfl_xor64(uint64_t v, int d) { return __shfl_xor((unsigned long long)v, d); }
+__device__ inline uint64_t shfl64(uint64_t v, int s) { return __shfl((unsigned long long)v, s); }
+__device__ inline uint64_t wave_sum(uint64_t v) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += shfl_xor64(v, d);
+    return v;
+}
+__device__ inline uint64_t wave_scan(uint64_t v) {      // inclusive
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint64_t t = shfl_up64(v, d);
+        if (lane >= d) v += t;
+    }
+    return v;
+}
+
+// ------------------------------------------------------------------ up to 64 choices
+
+// One wave a row, one lane a choice.  Each lane counts the choices before its
+// own in descending order and adds their weights in one walk over the row, whose
+// keys and weights the wave broadcasts from its registers: no sort, no LDS.
+template <class T>
+__global__ __launch_bounds__(256) void k_sample_wave(SampleArgs a) {
+    const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (r >= a.n) return;
+    const Row q = row_settings(a.p, r);
+    const bool live = lane < a.vocab;
+    const float l = live ? canonical(to_float(static_cast<const T *>(a.logits)[r * a.stride + lane])) : -kInf;
+    float m = l;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    int token = -1;
+    float logp = -kInf;
+    if (m > -kInf) {
+        if (q.greedy) {
+            token = __ffsll((unsigned long long)__ballot(live && l == m)) - 1;
+            logp = 0.f;
+        } else {
+            const float z = z_of(l, m, q.c);
+            const uint32_t w = live ? weight_of(z, q.min_p) : 0, key = live ? key_of(l) : 0;
+            int rank = 0;
+            uint64_t before = 0;
+            for (int j = 0; j < a.vocab; ++j) {
+                const uint32_t kj = __builtin_amdgcn_readlane(key, j), wj = __builtin_amdgcn_readlane(w, j);
+                const bool ahead = kj > key || (kj == key && j < lane);
+                rank += ahead;
+                before += ahead ? wj : 0;
+            }
+            const bool in_k = q.top_k == 0 || rank < q.top_k;
+            const double limit = (double)q.top_p * (double)wave_sum(in_k ? w : 0);
+            const uint64_t mine = in_k && (rank == 0 || (double)before < limit) ? w : 0;
+            const uint64_t upto = wave_scan(mine), total = shfl64(upto, 63);
+            const uint64_t t = target_of(a.u[r], total);
+            token = __ffsll((unsigned long long)__ballot(upto > t)) - 1;
+            logp = log_share(__shfl(z, token), total);
+        }
+    }
+    if (lane == 0) {
+        a.tokens[r] = token;
+        if (a.logprobs) a.logprobs[r] = logp;
+    }
+}
+
+// ------------------------------------------------------------------ more choices
+
+constexpr int kBins = 1024;
+
+// One block of NT threads a row; the row is streamed from memory (from the
+// caches after the first time) once for each question asked of it:
+//   the largest logit;
+//   the histogram of z in steps of 1/32 (counts for top-k, weights for top-p),
+//     which gives the bin a threshold lies in;
+//   histograms of the keys within that bin, 1024 steps at a time, until a step
+//     is one key: one or two more;
+//   the weights that stay, by contiguous parts of the row, then of the part the
+//     draw falls into, down to one wave's vector.
+template <class T, int VEC, int NT>
+struct Block {
+    static constexpr int NW = NT / 64;
+    const T *x;
+    int vocab;
+    uint64_t (&hw)[kBins];
+    uint32_t (&hc)[kBins];
+    uint64_t (&part)[NW + 2];
+    uint32_t (&ties)[NW + 2];
+
+    // f(index, logit) for the elements [lo, hi), thread by thread in vectors.
+    template <class F>
+    __device__ void each(int lo, int hi, int first, int step, F &&f) const {
+        for (int i = lo + first * VEC; i < hi; i += step * VEC) {
+            if (VEC > 1 && i + VEC <= hi) {
+                const Pack<T, VEC> p = *reinterpret_cast<const Pack<T, VEC> *>(x + i);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) f(i + j, canonical(to_float(p.v[j])));
+            } else {
+                for (int j = 0; j < VEC && i + j < hi; ++j) f(i + j, canonical(to_float(x[i + j])));
+            }
+        }
+    }
+    template <class F>
+    __device__ void all(F &&f) const { each(0, vocab, threadIdx.x, NT, f); }
+
+    __device__ void clear() const {
+        for (int i = threadIdx.x; i < kBins; i += NT) hw[i] = 0, hc[i] = 0;
+        __syncthreads();
+    }
+
+    // The first bin at which `upto(before count, before weight, count, weight)`
+    // holds of the bins in order, and what lies before it; kBins if there is none.
+    struct Found {
+        int bin;
+        uint32_t count, in_count;
+        uint64_t weight, in_weight;
+    };
+    template <class P>
+    __device__ Found find(P &&reached) const {
+        constexpr int PER = kBins / NT;
+        __syncthreads();
+        uint64_t w = 0;
+        uint32_t c = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) w += hw[threadIdx.x * PER + j], c += hc[threadIdx.x * PER + j];
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const uint64_t sw = wave_scan(w), sc = wave_scan(c);
+        if (lane == 63) part[wave] = sw, ties[wave] = (uint32_t)sc;
+        __syncthreads();
+        uint64_t bw = sw - w;
+        uint32_t bc = (uint32_t)sc - c;
+        for (int k = 0; k < wave; ++k) bw += part[k], bc += ties[k];
+        int hit = kBins;
+        for (int j = 0; j < PER; ++j) {
+            const int b = threadIdx.x * PER + j;
+            if (reached(bc + hc[b], bw + hw[b])) {
+                hit = b;
+                break;
+            }
+            bc += hc[b], bw += hw[b];
+        }
+        // The conditions are monotone in the running sums: the lowest hit is it.
+        int low = hit;
+#pragma unroll
+        for (int d = 32; d; d >>= 1) low = min(low, __shfl_xor(low, d));
+        __syncthreads();
+        if (lane == 0) ties[wave] = low;
+        __syncthreads();
+        for (int k = 0; k < NW; ++k) low = min(low, (int)ties[k]);
+        __syncthreads();
+        if (hit == low && hit < kBins) part[NW] = bw, ties[NW] = bc, part[NW + 1] = hw[hit], ties[NW + 1] = hc[hit];
+        __syncthreads();
+        Found f{low, 0, 0, 0, 0};
+        if (low < kBins) f = Found{low, ties[NW], ties[NW + 1], part[NW], part[NW + 1]};
+        __syncthreads();
+        return f;
+    }
+};
+
+template <class T, int VEC, int NT>
+__global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
+    using B = Block<T, VEC, NT>;
+    constexpr int NW = NT / 64;
+    __shared__ uint64_t hw[kBins], part[NW + 2];
+    __shared__ uint32_t hc[kBins], ties[NW + 2], bound[2];
+    const int r = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Row q = row_settings(a.p, r);
+    const B b{static_cast<const T *>(a.logits) + r * a.stride, a.vocab, hw, hc, part, ties};
+
+    // the largest logit
+    float m = -kInf;
+    b.all([&](int, float l) { m = fmaxf(m, l); });
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    if (lane == 0) ties[wave] = __float_as_uint(m);
+    __syncthreads();
+    for (int k = 0; k < NW; ++k) m = fmaxf(m, __uint_as_float(ties[k]));
+    __syncthreads();
+    if (!(m > -kInf)) {                             // nothing to choose from
+        if (threadIdx.x == 0) {
+            a.tokens[r] = -1;
+            if (a.logprobs) a.logprobs[r] = -kInf;
+        }
+        return;
+    }
+    if (q.greedy) {
+        int at = a.vocab;
+        b.all([&](int i, float l) { at = l == m ? min(at, i) : at; });
+#pragma unroll
+        for (int d = 32; d; d >>= 1) at = min(at, __shfl_xor(at, d));
+        if (lane == 0) ties[wave] = at;
+        __syncthreads();
+        for (int k = 0; k < NW; ++k) at = min(at, (int)ties[k]);
+        if (threadIdx.x == 0) {
+            a.tokens[r] = at;
+            if (a.logprobs) a.logprobs[r] = 0.f;
+        }
+        return;
+    }
+
+    // What stays: logits above `cut`, and the first `equals` of those equal to it.
+    float cut = -kInf;
+    uint32_t equals = 0, equal_weight = 0;
+    const bool use_k = q.top_k > 0 && q.top_k < a.vocab, use_p = q.top_p < 1.f;
+    if (use_k || use_p) {
+        const auto bin_of = [&](float l) {          // descending logits have ascending bins
+            const float z = z_of(l, m, q.c);
+            return z > -32.f ? (int)(z * -32.f) : kBins;   // kBins: no weight
+        };
+        // Narrows a bin down to one key: the first key, from the largest down, at
+        // which the running count and weight satisfy `reached`.
+        struct Cut {
+            float logit;
+            uint32_t count, in_count;               // before it, and of its equals
+            uint64_t weight;
+        };
+        const auto narrow = [&](typename B::Found f, float above, auto &&reached) {
+            // The keys of the bin: binary search of its two edges, by two threads.
+            if (threadIdx.x < 2) {
+                uint32_t lo = key_of(-kInf), hi = key_of(m);       // the least key with a bin <= f.bin - edge
+                const int most = f.bin - (int)threadIdx.x;
+                while (lo < hi) {
+                    const uint32_t mid = lo + (hi - lo) / 2;
+                    if (bin_of(of_key(mid)) <= most) hi = mid;
+                    else lo = mid + 1;
+                }
+                // thread 0: the bin's least key; thread 1: the least key of the bins before
+                // it, or, where there is none, key_of(m), which belongs to this bin.
+                bound[threadIdx.x] = threadIdx.x && f.bin > 0 ? lo - 1 : threadIdx.x ? key_of(m) : lo;
+            }
+            __syncthreads();
+            uint32_t lo = bound[0], hi = bound[1];
+            uint32_t count = f.count;
+            uint64_t weight = f.weight;
+            for (;;) {
+                int shift = 0;
+                while (((hi - lo) >> shift) >= kBins) ++shift;
+                b.clear();
+                b.all([&](int, float l) {
+                    const uint32_t key = key_of(l);
+                    if (key >= lo && key <= hi && l > above) {
+                        const int s = (int)((hi - key) >> shift);
+                        atomicAdd(&hc[s], 1u);
+                        const uint32_t w = weight_of(z_of(l, m, q.c), q.min_p);
+                        if (w) atomicAdd((unsigned long long *)&hw[s], (unsigned long long)w);
+                    }
+                });
+                const typename B::Found g = b.find([&](uint32_t c, uint64_t w) { return reached(count + c, weight + w); });
+                count += g.count, weight += g.weight;
+                hi -= (uint32_t)g.bin << shift;
+                if (shift == 0) return Cut{of_key(hi), count, g.in_count, weight};
+                const uint32_t span = (1u << shift) - 1;
+                lo = hi - lo > span ? hi - span : lo;
+            }
+        };
+
+        b.clear();
+        b.all([&](int, float l) {
+            const float z = z_of(l, m, q.c);
+            if (z > -32.f) {
+                const int s = (int)(z * -32.f);
+                if (use_k) atomicAdd(&hc[s], 1u);
+                const uint32_t w = weight_of(z, q.min_p);
+                if (w) atomicAdd((unsigned long long *)&hw[s], (unsigned long long)w);
+            }
+        });
+        __syncthreads();
+        // The histogram is needed again for top-p: its bins are kept in registers.
+        constexpr int PER = kBins / NT;
+        uint64_t keep_w[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) keep_w[j] = hw[threadIdx.x * PER + j];
+        uint64_t total = 0, above_weight = 0;       // of what stays, and of that above `cut`
+        int k_bin = kBins;
+        bool cut_by_k = false;
+        if (use_k) {
+            const typename B::Found f = b.find([&](uint32_t c, uint64_t) { return c >= (uint32_t)q.top_k; });
+            if (f.bin < kBins) {
+                const Cut k = narrow(f, -kInf, [&](uint32_t c, uint64_t) { return c >= (uint32_t)q.top_k; });
+                cut = k.logit, equals = q.top_k - k.count, cut_by_k = true, k_bin = f.bin;
+                equal_weight = weight_of(z_of(cut, m, q.c), q.min_p);
+                above_weight = k.weight;
+                total = above_weight + (uint64_t)equals * equal_weight;
+            }
+        }
+        if (use_p) {
+            __syncthreads();
+            if (!cut_by_k) {
+                uint64_t s = 0;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) s += keep_w[j];
+                s = wave_sum(s);
+                if (lane == 0) part[wave] = s;
+                __syncthreads();
+                for (int k = 0; k < NW; ++k) total += part[k];
+                __syncthreads();
+            }
+            // Elements before which less than `limit` lies stay; the first has nothing before it.
+            const double limit = fmax((double)q.top_p * (double)total, 0.5);
+            const auto fill = [&](float logit, uint32_t count, uint64_t before) {
+                cut = logit, equal_weight = weight_of(z_of(cut, m, q.c), q.min_p);
+                const double each = (double)equal_weight;
+                uint32_t e = (uint32_t)fmin(ceil((limit - (double)before) / fmax(each, 1.0)), (double)count);
+                while (e > 0 && (double)(before + (uint64_t)(e - 1) * equal_weight) >= limit) --e;
+                while (e < count && (double)(before + (uint64_t)e * equal_weight) < limit) ++e;
+                equals = e;
+            };
+            if (cut_by_k && (double)above_weight < limit) {
+                fill(cut, equals, above_weight);    // it lies among the last of the top k
+            } else {
+                // The bins again, without those below the top k's last (whose bin's own
+                // weight below the cut cannot be reached: above_weight >= limit).
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const int s = threadIdx.x * PER + j;
+                    hw[s] = s <= k_bin ? keep_w[j] : 0, hc[s] = 0;
+                }
+                const auto reached = [&](uint32_t, uint64_t w) { return (double)w >= limit; };
+                const typename B::Found f = b.find(reached);
+                const Cut p = narrow(f, cut, reached);
+                fill(p.logit, p.in_count, p.weight);
+            }
+        }
+    }
+
+    // The draw.  Parts of the row in order: NW contiguous ones, then the part the
+    // target falls into in the same way, until a part is one vector a lane.
+    int lo = 0, hi = a.vocab;
+    uint64_t before = 0, target = 0, total = 0;     // weight before lo
+    uint32_t seen = 0;                              // equals before lo
+    const auto stays = [&](uint32_t had, uint32_t n) { return min(had + n, equals) - min(had, equals); };
+    for (bool first = true; first || hi - lo > 64 * VEC; first = false) {
+        const int grain = 64 * VEC;
+        const int step = ((hi - lo + NW - 1) / NW + grain - 1) / grain * grain;
+        const int from = lo + wave * step, to = min(hi, from + step);
+        uint64_t w = 0;
+        uint32_t e = 0;
+        b.each(from, to, lane, 64, [&](int, float l) {
+            if (l > cut) w += weight_of(z_of(l, m, q.c), q.min_p);
+            else if (l == cut) ++e;
+        });
+        w = wave_sum(w), e = (uint32_t)wave_sum(e);
+        if (lane == 0) part[wave] = w, ties[wave] = e;
+        __syncthreads();
+        if (first) {
+            uint32_t s = 0;
+            for (int k = 0; k < NW; ++k) total += part[k] + (uint64_t)stays(s, ties[k]) * equal_weight, s += ties[k];
+            target = target_of(a.u[r], total);
+        }
+        int k = 0;
+        for (; k < NW - 1; ++k) {
+            const uint64_t in = part[k] + (uint64_t)stays(seen, ties[k]) * equal_weight;
+            if (before + in > target) break;
+            before += in, seen += ties[k];
+        }
+        lo += k * step, hi = min(hi, lo + step);
+        __syncthreads();
+    }
+    if (wave == 0) {
+        uint64_t w = 0;
+        uint32_t e = 0;
+        b.each(lo, hi, lane, 64, [&](int, float l) {
+            if (l > cut) w += weight_of(z_of(l, m, q.c), q.min_p);
+            else if (l == cut) ++e;
+        });
+        const uint32_t had = seen + (uint32_t)wave_scan(e) - e;
+        const uint64_t mine = w + (uint64_t)stays(had, e) * equal_weight;
+        const uint64_t upto = before + wave_scan(mine);
+        const int owner = __ffsll((unsigned long long)__ballot(upto > target)) - 1;
+        if (lane == owner) {
+            uint64_t run = upto - mine;
+            uint32_t s = had;
+            int token = -1;
+            float z = 0.f;
+            b.each(lo, hi, lane, 64, [&](int i, float l) {
+                const float zi = z_of(l, m, q.c);
+                if (l > cut) run += weight_of(zi, q.min_p);
+                else if (l == cut) run += (uint64_t)stays(s++, 1) * equal_weight;
+                if (token < 0 && run > target) token = i, z = zi;
+            });
+            a.tokens[r] = token;
+            if (a.logprobs) a.logprobs[r] = log_share(z, total);
+        }
+    }
+}
+
+template <class T, int VEC>
+void launch_block(const SampleArgs &a, hipStream_t s) {
+    // A row of up to 4096 leaves most of 1024 threads without work; a longer one
+    // is worth all the waves a CU takes.
+    if (a.vocab <= 4096) k_sample_block<T, VEC, 256><<<a.n, 256, 0, s>>>(a);
+    else k_sample_block<T, VEC, 1024><<<a.n, 1024, 0, s>>>(a);
+}
+
+template <class T>
+hipError_t run(const SampleArgs &a, hipStream_t s) {
+    constexpr int VEC = 16 / sizeof(T);
+    if (a.vocab <= 64) k_sample_wave<T><<<(a.n + 3) / 4, 256, 0, s>>>(a);
+    else if (reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && a.stride % VEC == 0) launch_block<T, VEC>(a, s);
+    else launch_block<T, 1>(a, s);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t s) {
+    return bf16 ? run<bf16_t>(a, s) : run<float>(a, s);
+}
+
+}  // namespace rn
