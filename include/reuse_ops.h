@@ -164,8 +164,8 @@ size_t reuse_ops_delta_backward_scratch_bytes(const rn_delta_shape *shape);
  *                dev_state.
  *   dev_out:     [tokens][heads_v][dv] dtype, contiguous.
  *   dev_saved:   NULL, or reuse_ops_delta_saved_bytes bytes for the backward call.
- *   dev_scratch: reuse_ops_delta_scratch_bytes bytes, or NULL with dev_saved,
- *                which then has room for it; both are 256-byte aligned. */
+ *   dev_scratch: reuse_ops_delta_scratch_bytes bytes; saved and scratch are
+ *                256-byte aligned. */
 rn_status reuse_ops_delta_forward(const rn_delta_shape *shape, const void *dev_q, const void *dev_k,
                                   const void *dev_v, const float *dev_g, const float *dev_beta,
                                   const int32_t *dev_seq_off, const float *dev_state, float *dev_final, void *dev_out,

@@ -175,113 +175,410 @@ __global__ __launch_bounds__(256) void k_delta_prepare(DeltaArgs a) {
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void k_delta_walk(DeltaArgs a) {
+// The chunk operands of k_delta_walk, in fragment order: K, Q and K^T of a chunk
+// and key head, and for each value head that shares it (I + A)^-1, P and the
+// decays.  A block takes a chunk slot and a key head, a wave 16 of its tokens.
+//
+// The inverse by blocks of 16: the four on the diagonal by forward substitution,
+// a column a lane; then the 32s and the 64 from
+//   [L11 0; L21 L22]^-1 = [X11 0; -X22 L21 X11  X22]
+// on the float32 matrix cores.  Substitution of the blocks alone keeps this as
+// stable as that of the whole, with a chain of 16 rows in place of 64.
+template <class T, int KS>
+__global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
+    constexpr int NP = sizeof(T) == 2 ? 1 : 3, NPP = sizeof(T) == 2 ? 2 : 3;
+    constexpr int kKeys = 4 * KS * NP * kFrag;          // bf16 of one of kf, qf, kt
     extern __shared__ float lds[];
-    const int kp = (a.dk + 15) / 16 * 16, ld = kp + 4;
-    constexpr int ldv = kVT + 1;
-    float *sk = lds, *sq = sk + kC * ld, *m = sq + kC * ld, *p = m + kC * kLd;
-    float *S = p + kC * kLd, *w = S + kp * ldv;
+    float *kk = lds, *qk = kk + kC * kLd, *x = qk + kC * kLd;
+    uint16_t *skf = reinterpret_cast<uint16_t *>(x + kC * kLd);
     __shared__ double cs[kC];
     __shared__ float beta[kC];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int seq = blockIdx.x / a.hv, h = blockIdx.x % a.hv, hk = h / (a.hv / a.hk);
-    const int v0 = blockIdx.y * kVT;
-    const Span span = span_of(a, seq);
-    const int64_t sbase = ((int64_t)seq * a.hv + h) * a.dk * a.dv;
-    for (int i = threadIdx.x; i < kp * kVT; i += 256) {
-        const int d = i / kVT, v = i % kVT;
-        S[d * ldv + v] = a.state && d < a.dk && v0 + v < a.dv ? a.state[sbase + d * a.dv + v0 + v] : 0.f;
-    }
-    const int r0 = wave * 16, row4 = r0 + (lane >> 4) * 4, colv = lane & 15;
-    for (int at = 0, chunk = 0; at < span.len; at += kC, ++chunk) {
-        const Chunk c{seq, span.begin + at, min(kC, span.len - at)};
-        const int64_t ch = (int64_t)slot_of(span, seq, chunk) * a.hv + h;
-        __syncthreads();
-        if (wave == 0) {
-            cs[lane] = decay_sums(a, c, h);
-            beta[lane] = lane < c.len ? a.beta[(int64_t)(c.begin + lane) * a.hv + h] : 0.f;
-        }
-        for (int i = threadIdx.x; i < kC * kp; i += 256) {
-            const int t = i / kp, d = i % kp;
-            const bool in = t < c.len && d < a.dk;
-            sk[t * ld + d] = in ? load<T>(a.k, (c.begin + t) * a.ks + hk * a.dk + d) : 0.f;
-            sq[t * ld + d] = in ? load<T>(a.q, (c.begin + t) * a.qs + hk * a.dk + d) * a.scale : 0.f;
-        }
-        for (int i = threadIdx.x; i < kC * kC; i += 256) {
-            m[i / kC * kLd + i % kC] = a.inv[ch * kC * kC + i];
-            p[i / kC * kLd + i % kC] = a.score[ch * kC * kC + i];
-        }
-        if (a.before)
-            for (int i = threadIdx.x; i < a.dk * kVT; i += 256) {
-                const int d = i / kVT, v = i % kVT;
-                if (v0 + v < a.dv) a.before[(ch * a.dk + d) * a.dv + v0 + v] = S[d * ldv + v];
-            }
-        __syncthreads();
-        // beta (V - e^c K S), then V', then out: the wave's 16 tokens each.
-        const auto sb = [&](int k, int j) { return S[k * ldv + j]; };
-        const f32x4 held = tile_mm(kp, [&](int i, int k) { return sk[(r0 + i) * ld + k]; }, sb, f32x4{});
-        f32x4 o = tile_mm(kp, [&](int i, int k) { return sq[(r0 + i) * ld + k]; }, sb, f32x4{});
+    const int slot = blockIdx.x, hk = blockIdx.y, group = a.hv / a.hk;
+    const Chunk c = chunk_of(a, slot);
+    if (c.len == 0) return;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int64_t keys = ((int64_t)slot * a.hk + hk) * kKeys;
+    // K and Q as rows: the wave's 16 tokens.
+    const int token = wave * 16 + r;
+    bf16x8 qa[KS][NP];
+    const auto row = [&](const void *p, int64_t stride, int ks, bf16x8 (&f)[NP]) {
+        const int64_t at = (int64_t)(c.begin + token) * stride + hk * a.dk;
+        uint32_t w[4][NP];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int t = row4 + j;
-            const bool in = t < c.len && v0 + colv < a.dv;
-            const float v = in ? load<T>(a.v, (c.begin + t) * a.vs + (int64_t)h * a.dv + v0 + colv) : 0.f;
-            const float grown = expf((float)cs[t]);
-            w[t * ldv + colv] = beta[t] * (v - grown * held[j]);
-            o[j] *= grown;
+        for (int e = 0; e < 8; e += 2) {
+            const int d = ks * 32 + g * 8 + e;
+            const bool in = token < c.len;
+            split_pair<NP>(in && d < a.dk ? load<T>(p, at + d) : 0.f, in && d + 1 < a.dk ? load<T>(p, at + d + 1) : 0.f,
+                           w[e / 2]);
         }
-        __syncthreads();
-        const auto wb = [&](int k, int j) { return w[k * ldv + j]; };
-        const f32x4 nv = tile_mm(r0 + 16, [&](int i, int k) { return m[(r0 + i) * kLd + k]; }, wb, f32x4{});
-        __syncthreads();
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[(row4 + j) * ldv + colv] = nv[j];
-        __syncthreads();
-        o = tile_mm(r0 + 16, [&](int i, int k) { return p[(r0 + i) * kLd + k]; }, wb, o);
+        for (int i = 0; i < NP; ++i) f[i] = __builtin_bit_cast(bf16x8, u32x4{w[0][i], w[1][i], w[2][i], w[3][i]});
+    };
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int t = row4 + j;
-            if (t < c.len && v0 + colv < a.dv)
-                static_cast<T *>(a.out)[((int64_t)(c.begin + t) * a.hv + h) * a.dv + v0 + colv] = from_float<T>(o[j]);
-        }
-        // the memory after the chunk: rows of S, a wave every fourth 16
-        __syncthreads();
-        const double last = cs[kC - 1];
-        const float whole = expf((float)last);
-        for (int d0 = wave * 16; d0 < kp; d0 += 64) {
-            const f32x4 add = tile_mm(
-                kC, [&](int i, int k) { return sk[k * ld + d0 + i] * expf((float)(last - cs[k])); }, wb, f32x4{});
+    for (int ks = 0; ks < KS; ++ks) {
+        bf16x8 f[NP];
+        const int at = ((wave * KS + ks) * NP) * kFrag + lane * 8;
+        row(a.k, a.ks, ks, f);
+        row(a.q, a.qs, ks, qa[ks]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float &s = S[(d0 + (lane >> 4) * 4 + j) * ldv + colv];
-                s = fmaf(whole, s, add[j]);
-            }
+        for (int i = 0; i < NP; ++i) {
+            *reinterpret_cast<bf16x8 *>(skf + at + i * kFrag) = f[i];
+            *reinterpret_cast<bf16x8 *>(a.kf + keys + at + i * kFrag) = f[i];
+            *reinterpret_cast<bf16x8 *>(a.qf + keys + at + i * kFrag) = qa[ks][i];
         }
     }
     __syncthreads();
-    if (a.final_state)
-        for (int i = threadIdx.x; i < a.dk * kVT; i += 256) {
-            const int d = i / kVT, v = i % kVT;
-            if (v0 + v < a.dv) a.final_state[sbase + d * a.dv + v0 + v] = S[d * ldv + v];
+    // K K^T and Q K^T, the wave's rows of them.
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        f32x4 u{}, w{};
+        if (n <= wave) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                bf16x8 ka[NP], kb[NP];
+                load_frags<NP>(skf + ((wave * KS + ks) * NP) * kFrag + lane * 8, ka);
+                load_frags<NP>(skf + ((n * KS + ks) * NP) * kFrag + lane * 8, kb);
+                u = mm<NP, NP>(ka, kb, u);
+                w = mm<NP, NP>(qa[ks], kb, w);
+            }
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            kk[(wave * 16 + g * 4 + j) * kLd + n * 16 + r] = u[j];
+            qk[(wave * 16 + g * 4 + j) * kLd + n * 16 + r] = w[j] * a.scale;
+        }
+    }
+    // K^T as rows: element (d, token) from K's fragments.
+    for (int i = wave; i < 2 * KS * 2; i += 4) {
+        const int rt = i / 2, ks = i % 2, d = rt * 16 + r;
+        const int from = ((d / 32) * NP) * kFrag + (d % 32 / 8) * 16 * 8 + d % 8;    // of row block 0, token 0
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+            u16x8 v;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int t = ks * 32 + g * 8 + e;
+                v[e] = skf[from + (t / 16) * KS * NP * kFrag + p * kFrag + (t % 16) * 8];
+            }
+            *reinterpret_cast<u16x8 *>(a.kt + keys + (i * NP + p) * kFrag + lane * 8) = v;
+        }
+    }
+    for (int h = hk * group; h < (hk + 1) * group; ++h) {
+        const int64_t ch = (int64_t)slot * a.hv + h;
+        __syncthreads();
+        if (wave == 0) {
+            const double s = decay_sums(a, c, h), last = __shfl(s, 63);
+            const float b = lane < c.len ? a.beta[(int64_t)(c.begin + lane) * a.hv + h] : 0.f;
+            cs[lane] = s;
+            beta[lane] = b;
+            a.dec[ch * 3 * kC + lane] = expf((float)s);
+            a.dec[ch * 3 * kC + kC + lane] = expf((float)(last - s));
+            a.dec[ch * 3 * kC + 2 * kC + lane] = b;
+        }
+        __syncthreads();
+        // A into x, P into fragments: a lane's eight columns of a row.
+        for (int i = wave; i < kTri; i += 4) {
+            const int rb = i < 2 ? i : i / 2 + 1, ks = i < 2 ? 0 : i & 1;
+            const int t = rb * 16 + r;
+            uint32_t w[4][NPP];
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                float p[2];
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    const int u = ks * 32 + g * 8 + e + o;
+                    const float d = u <= t ? expf((float)(cs[t] - cs[u])) : 0.f;
+                    p[o] = u <= t ? d * qk[t * kLd + u] : 0.f;
+                    x[t * kLd + u] = u < t ? beta[t] * d * kk[t * kLd + u] : 0.f;
+                }
+                split_pair<NPP>(p[0], p[1], w[e / 2]);
+            }
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+            for (int p = 0; p < NPP; ++p)
+                *reinterpret_cast<u32x4 *>(a.pf + (ch * kTri + i) * NPP * kFrag + p * kFrag + lane * 8) =
+                    u32x4{w[0][p], w[1][p], w[2][p], w[3][p]};
+        }
+        __syncthreads();
+        if (wave == 0) {                                // the diagonal blocks, one a quarter wave
+            const float *d = x + g * 16 * kLd + g * 16;
+            float col[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float s = i == r ? 1.f : 0.f;
+#pragma unroll
+                for (int l = 0; l < i; ++l) s = fmaf(-d[i * kLd + l], col[l], s);
+                col[i] = s;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[(g * 16 + i) * kLd + g * 16 + r] = col[i];
+        }
+        __syncthreads();
+        // The 32s: -X11 (A10 X00) for the pairs (0, 1) and (2, 3), a wave each.
+        const auto put = [&](float *to, f32x4 v, float sign) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to[(g * 4 + j) * kLd + r] = sign * v[j];
+        };
+        if (wave < 2) {
+            float *b = x + wave * 32 * kLd + wave * 32, *l = b + 16 * kLd;
+            const f32x4 t = tile_mm(16, [&](int i, int k) { return l[i * kLd + k]; },
+                                    [&](int k, int j) { return b[k * kLd + j]; }, f32x4{});
+            // through the upper block, which the inverse leaves empty
+            put(b + 16, t, 1.f);
+            const f32x4 v = tile_mm(16, [&](int i, int k) { return l[i * kLd + 16 + k]; },
+                                    [&](int k, int j) { return b[k * kLd + 16 + j]; }, f32x4{});
+            put(l, v, -1.f);
+            put(b + 16, f32x4{}, 1.f);
+        }
+        __syncthreads();
+        {   // the 64: -X22 (A21 X11), a 16 x 16 tile a wave
+            const int ti = wave / 2 * 16, tj = wave % 2 * 16;
+            float *l = x + 32 * kLd, *up = x + 32;
+            const f32x4 t = tile_mm(32, [&](int i, int k) { return l[(ti + i) * kLd + k]; },
+                                    [&](int k, int j) { return x[k * kLd + tj + j]; }, f32x4{});
+            put(up + ti * kLd + tj, t, 1.f);
+            __syncthreads();
+            const f32x4 v = tile_mm(32, [&](int i, int k) { return l[(ti + i) * kLd + 32 + k]; },
+                                    [&](int k, int j) { return up[k * kLd + tj + j]; }, f32x4{});
+            put(l + ti * kLd + tj, v, -1.f);
+        }
+        __syncthreads();
+        for (int i = wave; i < kTri; i += 4) {
+            const int rb = i < 2 ? i : i / 2 + 1, ks = i < 2 ? 0 : i & 1;
+            const int t = rb * 16 + r;
+            uint32_t w[4][3];
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const int u = ks * 32 + g * 8 + e;
+                split_pair<3>(u <= t ? x[t * kLd + u] : 0.f, u + 1 <= t ? x[t * kLd + u + 1] : 0.f, w[e / 2]);
+            }
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+                *reinterpret_cast<u32x4 *>(a.mf + (ch * kTri + i) * 3 * kFrag + p * kFrag + lane * 8) =
+                    u32x4{w[0][p], w[1][p], w[2][p], w[3][p]};
+        }
+    }
+}
+
+// A sequence's chunks in order.  A block takes 16 CT columns of a head's memory,
+// wave w the tokens 16 w .. + 15 of a chunk and the memory's row tiles w, w + 4;
+// the memory stays in its owners' registers in float32, and goes through LDS as
+// bf16 planes to the waves that multiply by it, as do beta (V - e^c K S) and V'.
+// The left operands are read from memory in fragment order, straight into
+// registers, each for the next chunk as soon as this one's use of it is over.
+template <class T, int KS, int CT>
+__global__ __launch_bounds__(256) void k_delta_walk(DeltaArgs a) {
+    constexpr int NP = sizeof(T) == 2 ? 1 : 3, NPP = sizeof(T) == 2 ? 2 : 3;
+    constexpr int KP = KS * 32, RT = KP > 64 ? KP / 64 : 1;        // row tiles of the memory a wave owns
+    constexpr int VT = 16 * CT, ldS = KP + 8, ldT = kC + 8;
+    constexpr int kKeys = 4 * KS * NP * kFrag;
+    __shared__ __align__(16) uint16_t sS[3 * VT * ldS], sR[3 * VT * ldT], sV[NPP * VT * ldT], sL[3 * VT * ldT];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int seq = blockIdx.x / a.hv, h = blockIdx.x % a.hv, hk = h / (a.hv / a.hk);
+    const int v0 = blockIdx.y * VT;
+    const Span span = span_of(a, seq);
+    const int chunks = (span.len + kC - 1) / kC;
+    const int64_t slot0 = slot_of(span, seq, 0);
+    const int64_t sbase = ((int64_t)seq * a.hv + h) * a.dk * a.dv + v0;
+    const bool owner = wave * 16 < KP;
+
+    f32x4 S[RT][CT];
+    const auto put_state = [&] {
+        if (owner)
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int n = 0; n < CT; ++n)
+                    put4<3>(sS, VT * ldS, (n * 16 + r) * ldS + (wave + 4 * i) * 16 + g * 4, S[i][n]);
+    };
+    const auto write_state = [&](float *to) {                       // to: [dk][dv] from column v0
+        if (owner)
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int n = 0; n < CT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int d = (wave + 4 * i) * 16 + g * 4 + j;
+                        if (d < a.dk && v0 + n * 16 + r < a.dv) to[(int64_t)d * a.dv + n * 16 + r] = S[i][n][j];
+                    }
+    };
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int n = 0; n < CT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int d = (wave + 4 * i) * 16 + g * 4 + j;
+                const bool in = a.state && owner && d < a.dk && v0 + n * 16 + r < a.dv;
+                S[i][n][j] = in ? a.state[sbase + (int64_t)d * a.dv + n * 16 + r] : 0.f;
+            }
+
+    bf16x8 kf[KS][NP], qf[KS][NP], kt[RT][2][NP], mf[2][3], pf[2][NPP];
+    float vv[CT][4];
+    const auto load_rows = [&](int64_t slot) {
+        const int64_t at = (slot * a.hk + hk) * kKeys + wave * KS * NP * kFrag + lane * 8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            load_frags<NP>(a.kf + at + ks * NP * kFrag, kf[ks]);
+            load_frags<NP>(a.qf + at + ks * NP * kFrag, qf[ks]);
+        }
+    };
+    const auto load_kt = [&](int64_t slot) {
+        const int64_t at = (slot * a.hk + hk) * kKeys + lane * 8;
+        if (owner)
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    load_frags<NP>(a.kt + at + ((wave + 4 * i) * 2 + ks) * NP * kFrag, kt[i][ks]);
+    };
+    const auto load_tri = [&](int64_t slot) {
+        const int64_t ch = slot * a.hv + h;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+            if (ks <= wave / 2) {
+                load_frags<3>(a.mf + (ch * kTri + tri(wave, ks)) * 3 * kFrag + lane * 8, mf[ks]);
+                load_frags<NPP>(a.pf + (ch * kTri + tri(wave, ks)) * NPP * kFrag + lane * 8, pf[ks]);
+            }
+    };
+    const auto load_v = [&](int chunk) {
+#pragma unroll
+        for (int n = 0; n < CT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int t = chunk * kC + wave * 16 + g * 4 + j;
+                const bool in = t < span.len && v0 + n * 16 + r < a.dv;
+                vv[n][j] = in ? load<T>(a.v, (span.begin + t) * a.vs + (int64_t)h * a.dv + v0 + n * 16 + r) : 0.f;
+            }
+    };
+    if (chunks > 0) load_rows(slot0), load_tri(slot0), load_kt(slot0), load_v(0);
+    put_state();
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        const int64_t slot = slot0 + chunk, ch = slot * a.hv + h;
+        const int len = min(kC, span.len - chunk * kC);
+        const bool busy = wave * 16 < len;              // any token of this wave
+        const bool more = chunk + 1 < chunks;
+        const int half = len > 32 ? 2 : 1;              // 32-wide steps over the tokens
+        const f32x4 grown = *reinterpret_cast<const f32x4 *>(a.dec + ch * 3 * kC + wave * 16 + g * 4);
+        const f32x4 left = *reinterpret_cast<const f32x4 *>(a.dec + ch * 3 * kC + kC + wave * 16 + g * 4);
+        const f32x4 beta = *reinterpret_cast<const f32x4 *>(a.dec + ch * 3 * kC + 2 * kC + wave * 16 + g * 4);
+        const float whole = a.dec[ch * 3 * kC + kC - 1];
+        if (a.before) write_state(a.before + ch * a.dk * a.dv + v0);
+        dev::lds_barrier();                             // the memory's planes are there
+        f32x4 o[CT];
+#pragma unroll
+        for (int n = 0; n < CT; ++n) {
+            f32x4 held{};
+            o[n] = f32x4{};
+            if (busy)
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    bf16x8 s[3], s2[NPP];
+                    get8<3>(sS, VT * ldS, (n * 16 + r) * ldS + ks * 32 + g * 8, s);
+#pragma unroll
+                    for (int i = 0; i < NPP; ++i) s2[i] = s[i];
+                    held = mm<NP, 3>(kf[ks], s, held);
+                    o[n] = mm<NP, NPP>(qf[ks], s2, o[n]);
+                }
+            f32x4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                w[j] = beta[j] * (vv[n][j] - grown[j] * held[j]);
+                o[n][j] *= grown[j] * a.scale;
+            }
+            put4<3>(sR, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
+        }
+        if (more) load_rows(slot + 1), load_v(chunk + 1);
+        dev::lds_barrier();
+#pragma unroll
+        for (int n = 0; n < CT; ++n) {
+            f32x4 w{};
+            if (busy)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    if (ks <= wave / 2) {
+                        bf16x8 b[3];
+                        get8<3>(sR, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
+                        w = mm<3, 3>(mf[ks], b, w);
+                    }
+            put4<NPP>(sV, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] *= left[j];
+            put4<3>(sL, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
+        }
+        dev::lds_barrier();
+        if (owner)
+#pragma unroll
+            for (int n = 0; n < CT; ++n)
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) S[i][n][j] *= whole;
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks)
+                        if (ks < half) {
+                            bf16x8 b[3];
+                            get8<3>(sL, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
+                            S[i][n] = mm<NP, 3>(kt[i][ks], b, S[i][n]);
+                        }
+                }
+        if (more) {
+            put_state();                                // every wave is past its reads of the planes
+            load_kt(slot + 1);
+        }
+        if (busy)
+#pragma unroll
+            for (int n = 0; n < CT; ++n) {
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    if (ks <= wave / 2) {
+                        bf16x8 b[NPP];
+                        get8<NPP>(sV, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
+                        o[n] = mm<NPP, NPP>(pf[ks], b, o[n]);
+                    }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int t = wave * 16 + g * 4 + j;
+                    if (t < len && v0 + n * 16 + r < a.dv)
+                        static_cast<T *>(a.out)[((int64_t)(span.begin + chunk * kC + t) * a.hv + h) * a.dv + v0 +
+                                                n * 16 + r] = from_float<T>(o[n][j]);
+                }
+            }
+        if (more) load_tri(slot + 1);
+    }
+    if (a.final_state) write_state(a.final_state + sbase);
+}
+
+template <class T, int KS>
+hipError_t forward_ks(const DeltaArgs &a, hipStream_t s) {
+    constexpr int NP = sizeof(T) == 2 ? 1 : 3;
+    const int slots = (int)delta_chunk_slots(a.tokens, a.n);
+    if (a.tokens > 0) {
+        if (a.before) {
+            const int ld = (a.dk + 3) / 4 * 4 + 4;
+            const size_t bytes = sizeof(float) * (2 * kC * ld + 3 * kC * kLd);
+            if (hipError_t e = allow_lds(k_delta_prepare<T>, bytes)) return e;
+            k_delta_prepare<T><<<dim3(slots, a.hk), 256, bytes, s>>>(a);
+            if (hipError_t e = hipGetLastError()) return e;
+        }
+        constexpr size_t bytes = sizeof(float) * 3 * kC * kLd + 2 * 4 * KS * NP * kFrag;
+        if (hipError_t e = allow_lds(k_delta_operands<T, KS>, bytes)) return e;
+        k_delta_operands<T, KS><<<dim3(slots, a.hk), 256, bytes, s>>>(a);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    if (a.dv <= 16) k_delta_walk<T, KS, 1><<<dim3(a.n * a.hv, 1), 256, 0, s>>>(a);
+    else k_delta_walk<T, KS, 2><<<dim3(a.n * a.hv, (a.dv + 31) / 32), 256, 0, s>>>(a);
+    return hipGetLastError();
 }
 
 template <class T>
 hipError_t forward(const DeltaArgs &a, hipStream_t s) {
-    const int slots = (int)delta_chunk_slots(a.tokens, a.n);
-    if (a.tokens > 0) {
-        const int ld = (a.dk + 3) / 4 * 4 + 4;
-        const size_t bytes = sizeof(float) * (2 * kC * ld + 3 * kC * kLd);
-        if (hipError_t e = allow_lds(k_delta_prepare<T>, bytes)) return e;
-        k_delta_prepare<T><<<dim3(slots, a.hk), 256, bytes, s>>>(a);
-        if (hipError_t e = hipGetLastError()) return e;
-    }
-    const int kp = (a.dk + 15) / 16 * 16;
-    const size_t bytes = sizeof(float) * (2 * kC * (kp + 4) + 2 * kC * kLd + (kp + kC) * (kVT + 1));
-    if (hipError_t e = allow_lds(k_delta_walk<T>, bytes)) return e;
-    k_delta_walk<T><<<dim3(a.n * a.hv, (a.dv + kVT - 1) / kVT), 256, bytes, s>>>(a);
-    return hipGetLastError();
+    const int ks = delta_ksteps(a.dk);
+    return ks == 1 ? forward_ks<T, 1>(a, s) : ks == 2 ? forward_ks<T, 2>(a, s) : forward_ks<T, 4>(a, s);
 }
 
 }  // namespace

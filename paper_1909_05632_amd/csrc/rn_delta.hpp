@@ -2,6 +2,7 @@
 #pragma once
 
 #include "rn_ops.hpp"
+#include "rn_split.hpp"
 
 namespace rn {
 namespace ops {
@@ -74,6 +75,68 @@ template <class T>
 __device__ inline float load(const void *p, int64_t i) {
     return to_float(static_cast<const T *>(p)[i]);
 }
+
+// ---- products on the bf16 matrix cores
+//
+// A float32 operand is a sum of bf16 planes (rn_split.hpp), three for the bits
+// of float32; a bfloat16 input is one plane exactly.  A product of operands of
+// NA and NB planes takes the terms (i, j) with i + j < max(NA, NB): what is
+// dropped is below the last plane kept.
+//
+// Fragment order: a 16 x 32 piece of an operand is 64 lanes x 8 bf16, lane l
+// holding row (B operand: column) l % 16 at k = 8 (l / 16) .. + 7, so one
+// 16-byte access a lane reads or writes it.  The result's lane l holds rows
+// 4 (l / 16) .. + 3 of column l % 16.
+using dev::bf16x8;
+constexpr int kFrag = 512;           // bf16 of a fragment
+
+template <int NA, int NB>
+__device__ inline f32x4 mm(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], f32x4 acc) {
+    constexpr int N = NA > NB ? NA : NB;
+#pragma unroll
+    for (int s = N - 1; s >= 0; --s)             // small terms first
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if (s - i >= 0 && s - i < NB) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[s - i], acc, 0, 0, 0);
+    return acc;
+}
+
+template <int N>
+__device__ inline void load_frags(const uint16_t *p, bf16x8 (&f)[N]) {      // p: this lane's part of plane 0
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = *reinterpret_cast<const bf16x8 *>(p + i * kFrag);
+}
+
+// The N planes of a pair of float32 values, each plane's pair in one word.
+template <int N>
+__device__ inline void split_pair(float x, float y, uint32_t (&p)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        p[i] = dev::round_pair(x, y);
+        if (i + 1 < N) x -= dev::pair_lo(p[i]), y -= dev::pair_hi(p[i]);
+    }
+}
+
+// Four consecutive k of one column into N planes of an LDS operand [column][ld].
+template <int N>
+__device__ inline void put4(uint16_t *lds, int plane, int at, const f32x4 v) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    uint32_t a[N], b[N];
+    split_pair<N>(v[0], v[1], a);
+    split_pair<N>(v[2], v[3], b);
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<u32x2 *>(lds + i * plane + at) = u32x2{a[i], b[i]};
+}
+template <int N>
+__device__ inline void get8(const uint16_t *lds, int plane, int at, bf16x8 (&f)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = *reinterpret_cast<const bf16x8 *>(lds + i * plane + at);
+}
+
+// The 16 x 32 pieces of a lower triangular 64 x 64 operand that hold anything:
+// piece (row block, k step) -> 0..5.
+__device__ inline int tri(int rb, int ks) { return rb < 2 ? rb : rb * 2 - 2 + ks; }
+constexpr int kTri = 6;
 
 }  // namespace ops
 }  // namespace rn

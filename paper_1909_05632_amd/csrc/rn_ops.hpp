@@ -54,7 +54,13 @@ struct DeltaArgs {
     const float *state;           // first states, or NULL
     float *final_state;           // last states, or NULL (step: the state pool)
     void *out;
-    // Per chunk slot (delta_chunk_slots) and value head:
+    // Per chunk slot (delta_chunk_slots) and key head, in fragment order (rn_delta.hpp):
+    uint16_t *kf, *qf;            // K and Q as rows
+    uint16_t *kt;                 // K^T as rows
+    // Per chunk slot and value head:
+    uint16_t *mf;                 // (I + A)^-1, three planes
+    uint16_t *pf;                 // P
+    float *dec;                   // [3][64] e^c, e^(c64 - c), beta
     float *inv;                   // [64][64] (I + A)^-1
     float *score;                 // [64][64] scale e^(ci - cj) q_i . k_j, j <= i
     float *before;                // [dk][dv] states before the chunk, or NULL (not kept)
@@ -69,6 +75,11 @@ struct DeltaArgs {
 // Chunk slots of a call: chunk c of sequence i has slot off[i] / 64 + i + c, so
 // every slot is below tokens / 64 + n and no two chunks share one.
 inline int64_t delta_chunk_slots(int64_t tokens, int n) { return tokens / RN_DELTA_CHUNK + n; }
+// 32-wide steps of dk in the chunk kernels (powers of two).
+inline int delta_ksteps(int dk) { return dk <= 32 ? 1 : dk <= 64 ? 2 : 4; }
+// bf16 planes of an input, and of P.
+inline int delta_planes(bool bf16) { return bf16 ? 1 : 3; }
+inline int delta_score_planes(bool bf16) { return bf16 ? 2 : 3; }
 hipError_t launch_delta_step(const DeltaArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_delta_forward(const DeltaArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_delta_backward(const DeltaArgs &a, bool bf16, hipStream_t s);

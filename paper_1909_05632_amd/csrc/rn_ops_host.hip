@@ -57,12 +57,17 @@ bool too_wide(const rn_delta_shape *s) { return s->dk > RN_DELTA_MAX_DIM || s->d
 
 struct DeltaSizes {
     size_t pairs, states, tokens;   // bytes of a [64][64] set, a set of states, [tokens][hv][dv]
+    size_t keys, inverse, score, decay;   // of kf, qf or kt; mf; pf; dec
 };
 
 DeltaSizes sizes(const rn_delta_shape *s) {
     const size_t slots = (size_t)delta_chunk_slots(s->tokens, s->n), heads = s->heads_v;
+    const bool bf16 = s->dtype == RN_BF16;
     return {round_up(slots * heads * RN_DELTA_CHUNK * RN_DELTA_CHUNK * 4), round_up(slots * heads * s->dk * s->dv * 4),
-            round_up((size_t)s->tokens * heads * s->dv * 4)};
+            round_up((size_t)s->tokens * heads * s->dv * 4),
+            round_up(slots * s->heads_k * 4 * delta_ksteps(s->dk) * delta_planes(bf16) * 1024),
+            round_up(slots * heads * 6 * 3 * 1024), round_up(slots * heads * 6 * delta_score_planes(bf16) * 1024),
+            round_up(slots * heads * 3 * RN_DELTA_CHUNK * 4)};
 }
 
 DeltaArgs delta_args(const rn_delta_shape *s, const void *q, const void *k, const void *v, const float *g,
@@ -74,6 +79,17 @@ DeltaArgs delta_args(const rn_delta_shape *s, const void *q, const void *k, cons
     a.qs = s->q_stride, a.ks = s->k_stride, a.vs = s->v_stride;
     a.q = q, a.k = k, a.v = v, a.g = g, a.beta = beta;
     return a;
+}
+
+// The chunk operands' places in a scratch buffer; the first byte after them.
+char *lay_out(DeltaArgs &a, const DeltaSizes &z, char *at) {
+    a.kf = reinterpret_cast<uint16_t *>(at);
+    a.qf = reinterpret_cast<uint16_t *>(at += z.keys);
+    a.kt = reinterpret_cast<uint16_t *>(at += z.keys);
+    a.mf = reinterpret_cast<uint16_t *>(at += z.keys);
+    a.pf = reinterpret_cast<uint16_t *>(at += z.inverse);
+    a.dec = reinterpret_cast<float *>(at += z.score);
+    return at + z.decay;
 }
 
 rn_status check_delta(const rn_delta_shape *s, const void *q, const void *k, const void *v, const float *g,
@@ -178,7 +194,8 @@ size_t reuse_ops_delta_saved_bytes(const rn_delta_shape *shape) {
 
 size_t reuse_ops_delta_scratch_bytes(const rn_delta_shape *shape) {
     if (bad_shape(shape) || too_wide(shape)) return 0;
-    return 2 * sizes(shape).pairs + kAlign;
+    const DeltaSizes z = sizes(shape);
+    return 3 * z.keys + z.inverse + z.score + z.decay + kAlign;
 }
 
 size_t reuse_ops_delta_backward_scratch_bytes(const rn_delta_shape *shape) {
@@ -197,20 +214,21 @@ rn_status reuse_ops_delta_forward(const rn_delta_shape *shape, const void *q, co
     if (shape->n == 0) return RN_OK;
     if (shape->tokens > 0 && !out) return fail(RN_EINVAL, "out must not be NULL");
     if (misaligned(saved) || misaligned(scratch)) return fail(RN_EINVAL, "saved and scratch must be 256-byte aligned");
-    const size_t need = saved ? reuse_ops_delta_saved_bytes(shape) : reuse_ops_delta_scratch_bytes(shape);
-    if (saved) {
-        if (saved_bytes < need) return need_bytes("saved", need);
-    } else {
-        if (!scratch) return fail(RN_EINVAL, "scratch is NULL");
-        if (scratch_bytes < need) return need_bytes("scratch", need);
-    }
+    if (saved && saved_bytes < reuse_ops_delta_saved_bytes(shape))
+        return need_bytes("saved", reuse_ops_delta_saved_bytes(shape));
+    if (!scratch) return fail(RN_EINVAL, "scratch is NULL");
+    const size_t need = reuse_ops_delta_scratch_bytes(shape);
+    if (scratch_bytes < need) return need_bytes("scratch", need);
     const DeltaSizes z = sizes(shape);
-    char *at = static_cast<char *>(saved ? saved : scratch);
+    char *kept = static_cast<char *>(saved), *at = static_cast<char *>(scratch);
     DeltaArgs a = delta_args(shape, q, k, v, g, beta);
     a.off = seq_off, a.state = state, a.final_state = final_state, a.out = out;
-    a.inv = reinterpret_cast<float *>(at);
-    a.score = reinterpret_cast<float *>(at + z.pairs);
-    a.before = saved ? reinterpret_cast<float *>(at + 2 * z.pairs) : nullptr;
+    lay_out(a, z, at);
+    if (saved) {
+        a.inv = reinterpret_cast<float *>(kept);
+        a.score = reinterpret_cast<float *>(kept + z.pairs);
+        a.before = reinterpret_cast<float *>(kept + 2 * z.pairs);
+    }
     return launched(launch_delta_forward(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
 }
 

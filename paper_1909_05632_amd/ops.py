@@ -359,21 +359,24 @@ def delta_forward(q, k, v, g, beta, seq_off=None, n=None, state=None, final=None
     dims = (n, shape.heads_v, shape.dk, shape.dv)
     sp = _opt(state, "state", torch.float32, dev, dims)
     L = load_ops()
-    size = L.reuse_ops_delta_saved_bytes if save else L.reuse_ops_delta_scratch_bytes
-    need = _supported(size(ctypes.byref(shape)), L.reuse_ops_delta_forward, shape)
+    need = _supported(L.reuse_ops_delta_scratch_bytes(ctypes.byref(shape)), L.reuse_ops_delta_forward, shape)
     if final is None:
         final = torch.empty(dims, dtype=torch.float32, device=dev)
     fp = _like(final, "final", torch.float32, dev, dims)
     if out is None:
         out = torch.empty((shape.tokens, shape.heads_v, shape.dv), dtype=q.dtype, device=dev)
     op = _like(out, "out", q.dtype, dev, (shape.tokens, shape.heads_v, shape.dv))
-    buf = torch.empty(need, dtype=torch.uint8, device=dev)
-    held = (buf.data_ptr(), need, None, 0) if save else (None, 0, buf.data_ptr(), need)
+    scratch = torch.empty(need, dtype=torch.uint8, device=dev)
+    saved, kept, size = None, None, 0
+    if save:
+        size = L.reuse_ops_delta_saved_bytes(ctypes.byref(shape))
+        saved = torch.empty(size, dtype=torch.uint8, device=dev)
+        kept = saved.data_ptr()
     _launch(dev, stream, L.reuse_ops_delta_forward, ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp,
-            bp, off, sp, fp, op, *held)
+            bp, off, sp, fp, op, kept, size, scratch.data_ptr(), need)
     if stream is not None:
-        buf.record_stream(stream)
-    return (out, final, buf) if save else (out, final)
+        scratch.record_stream(stream)
+    return (out, final, saved) if save else (out, final)
 
 
 def delta_backward(dout, q, k, v, g, beta, seq_off=None, n=None, saved=None, dfinal=None, scale=None,
