@@ -133,7 +133,7 @@ typedef struct {
     rn_dtype dtype;               /* of q, k, v and out */
     float scale;
     /* Elements from a token to the next; heads are contiguous within a token
-     * (q, k: [heads_k][dk], v: [heads_v][dv]). */
+     * (q, k: [heads_k][dk], v: [heads_v][dv]).  Below 2^23. */
     int64_t q_stride, k_stride, v_stride;
 } rn_delta_shape;
 

@@ -370,13 +370,14 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
 // The left operands are read from memory in fragment order, straight into
 // registers, each for the next chunk as soon as this one's use of it is over.
 template <class T, int KS, int CT>
-__global__ __launch_bounds__(256) void k_delta_walk(DeltaArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delta_walk(DeltaArgs a) {
     constexpr int NP = sizeof(T) == 2 ? 1 : 3, NPP = sizeof(T) == 2 ? 2 : 3;
     constexpr int KP = KS * 32, RT = KP > 64 ? KP / 64 : 1;        // row tiles of the memory a wave owns
     constexpr int VT = 16 * CT, ldS = KP + 8, ldT = kC + 8;
     constexpr int kKeys = 4 * KS * NP * kFrag;
     __shared__ __align__(16) uint16_t sS[3 * VT * ldS], sR[3 * VT * ldT], sV[NPP * VT * ldT], sL[3 * VT * ldT];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int seq = blockIdx.x / a.hv, h = blockIdx.x % a.hv, hk = h / (a.hv / a.hk);
     const int v0 = blockIdx.y * VT;
     const Span span = span_of(a, seq);
@@ -384,6 +385,10 @@ __global__ __launch_bounds__(256) void k_delta_walk(DeltaArgs a) {
     const int64_t slot0 = slot_of(span, seq, 0);
     const int64_t sbase = ((int64_t)seq * a.hv + h) * a.dk * a.dv + v0;
     const bool owner = wave * 16 < KP;
+    const bool all_cols = v0 + VT <= a.dv, all_rows = a.dk == KP;
+    bool col_in[CT];
+#pragma unroll
+    for (int n = 0; n < CT; ++n) col_in[n] = v0 + n * 16 + (int)r < a.dv;
 
     f32x4 S[RT][CT];
     const auto put_state = [&] {
@@ -395,16 +400,16 @@ __global__ __launch_bounds__(256) void k_delta_walk(DeltaArgs a) {
                     put4<3>(sS, VT * ldS, (n * 16 + r) * ldS + (wave + 4 * i) * 16 + g * 4, S[i][n]);
     };
     const auto write_state = [&](float *to) {                       // to: [dk][dv] from column v0
-        if (owner)
+        if (!owner) return;
+        const uint32_t at = (wave * 16 + g * 4) * a.dv + r;
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
+        for (int i = 0; i < RT; ++i)
 #pragma unroll
-                for (int n = 0; n < CT; ++n)
+            for (int n = 0; n < CT; ++n)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int d = (wave + 4 * i) * 16 + g * 4 + j;
-                        if (d < a.dk && v0 + n * 16 + r < a.dv) to[(int64_t)d * a.dv + n * 16 + r] = S[i][n][j];
-                    }
+                for (int j = 0; j < 4; ++j)
+                    if ((all_cols || col_in[n]) && (all_rows || (wave + 4 * i) * 16 + (int)g * 4 + j < a.dk))
+                        to[at + (64 * i + j) * a.dv + n * 16] = S[i][n][j];
     };
 #pragma unroll
     for (int i = 0; i < RT; ++i)
@@ -413,60 +418,76 @@ __global__ __launch_bounds__(256) void k_delta_walk(DeltaArgs a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int d = (wave + 4 * i) * 16 + g * 4 + j;
-                const bool in = a.state && owner && d < a.dk && v0 + n * 16 + r < a.dv;
+                const bool in = a.state && owner && d < a.dk && col_in[n];
                 S[i][n][j] = in ? a.state[sbase + (int64_t)d * a.dv + n * 16 + r] : 0.f;
             }
 
+    // Loads are unconditional, from places clamped into the arrays, so that the
+    // compiler can count them and wait for each only where it is used.
     bf16x8 kf[KS][NP], qf[KS][NP], kt[RT][2][NP], mf[2][3], pf[2][NPP];
-    float vv[CT][4];
+    T vv[CT][4];
     const auto load_rows = [&](int64_t slot) {
-        const int64_t at = (slot * a.hk + hk) * kKeys + wave * KS * NP * kFrag + lane * 8;
+        const int64_t at = (slot * a.hk + hk) * kKeys + wave * KS * NP * kFrag;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            load_frags<NP>(a.kf + at + ks * NP * kFrag, kf[ks]);
-            load_frags<NP>(a.qf + at + ks * NP * kFrag, qf[ks]);
+            load_frags<NP>(a.kf + at + (lane * 8 + ks * NP * kFrag), kf[ks]);
+            load_frags<NP>(a.qf + at + (lane * 8 + ks * NP * kFrag), qf[ks]);
         }
     };
     const auto load_kt = [&](int64_t slot) {
-        const int64_t at = (slot * a.hk + hk) * kKeys + lane * 8;
-        if (owner)
+        const int64_t at = (slot * a.hk + hk) * kKeys + (wave % (2 * KS)) * 2 * NP * kFrag;
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
+        for (int i = 0; i < RT; ++i)
 #pragma unroll
-                for (int ks = 0; ks < 2; ++ks)
-                    load_frags<NP>(a.kt + at + ((wave + 4 * i) * 2 + ks) * NP * kFrag, kt[i][ks]);
+            for (int ks = 0; ks < 2; ++ks) load_frags<NP>(a.kt + at + (lane * 8 + (8 * i + ks) * NP * kFrag), kt[i][ks]);
     };
-    const auto load_tri = [&](int64_t slot) {
-        const int64_t ch = slot * a.hv + h;
+    const auto load_inv = [&](int64_t slot) {
+        const int64_t at = (slot * a.hv + h) * kTri * 3 * kFrag;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) load_frags<3>(a.mf + (at + tri(wave, min(ks, wave / 2)) * 3 * kFrag) + lane * 8, mf[ks]);
+    };
+    const auto load_score = [&](int64_t slot) {
+        const int64_t at = (slot * a.hv + h) * kTri * NPP * kFrag;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
-            if (ks <= wave / 2) {
-                load_frags<3>(a.mf + (ch * kTri + tri(wave, ks)) * 3 * kFrag + lane * 8, mf[ks]);
-                load_frags<NPP>(a.pf + (ch * kTri + tri(wave, ks)) * NPP * kFrag + lane * 8, pf[ks]);
-            }
+            load_frags<NPP>(a.pf + (at + tri(wave, min(ks, wave / 2)) * NPP * kFrag) + lane * 8, pf[ks]);
     };
+    f32x4 grown{}, left{}, beta{}, next_grown{}, next_left{}, next_beta{};
+    float whole = 0.f, next_whole = 0.f;
+    const auto load_decays = [&](int64_t slot) {
+        const float *d = a.dec + (slot * a.hv + h) * 3 * kC + wave * 16;
+        next_grown = *reinterpret_cast<const f32x4 *>(d + g * 4);
+        next_left = *reinterpret_cast<const f32x4 *>(d + (kC + g * 4));
+        next_beta = *reinterpret_cast<const f32x4 *>(d + (2 * kC + g * 4));
+        next_whole = a.dec[(slot * a.hv + h) * 3 * kC + kC - 1];
+    };
+    // Tokens past the end have beta 0; columns past dv are not written.  Offsets
+    // within a chunk fit 32 bits (token strides are below 2^23).
+    uint32_t col[CT], voff[4];
+#pragma unroll
+    for (int n = 0; n < CT; ++n) col[n] = min(n * 16 + (int)r, a.dv - 1 - v0);
     const auto load_v = [&](int chunk) {
+        const T *base = static_cast<const T *>(a.v) + (int64_t)(span.begin + chunk * kC) * a.vs + (h * a.dv + v0);
+        const int last = span.len - chunk * kC - 1;
 #pragma unroll
-        for (int n = 0; n < CT; ++n)
+        for (int j = 0; j < 4; ++j) voff[j] = min(wave * 16 + (int)g * 4 + j, last) * (uint32_t)a.vs;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int t = chunk * kC + wave * 16 + g * 4 + j;
-                const bool in = t < span.len && v0 + n * 16 + r < a.dv;
-                vv[n][j] = in ? load<T>(a.v, (span.begin + t) * a.vs + (int64_t)h * a.dv + v0 + n * 16 + r) : 0.f;
-            }
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int n = 0; n < CT; ++n) vv[n][j] = base[voff[j] + col[n]];
     };
-    if (chunks > 0) load_rows(slot0), load_tri(slot0), load_kt(slot0), load_v(0);
+    const uint32_t ooff = (wave * 16 + g * 4) * (uint32_t)(a.hv * a.dv) + r;
+    if (chunks > 0)
+        load_decays(slot0), load_rows(slot0), load_v(0), load_inv(slot0), load_kt(slot0), load_score(slot0);
     put_state();
-    for (int chunk = 0; chunk < chunks; ++chunk) {
-        const int64_t slot = slot0 + chunk, ch = slot * a.hv + h;
-        const int len = min(kC, span.len - chunk * kC);
-        const bool busy = wave * 16 < len;              // any token of this wave
-        const bool more = chunk + 1 < chunks;
-        const int half = len > 32 ? 2 : 1;              // 32-wide steps over the tokens
-        const f32x4 grown = *reinterpret_cast<const f32x4 *>(a.dec + ch * 3 * kC + wave * 16 + g * 4);
-        const f32x4 left = *reinterpret_cast<const f32x4 *>(a.dec + ch * 3 * kC + kC + wave * 16 + g * 4);
-        const f32x4 beta = *reinterpret_cast<const f32x4 *>(a.dec + ch * 3 * kC + 2 * kC + wave * 16 + g * 4);
-        const float whole = a.dec[ch * 3 * kC + kC - 1];
+
+    const auto step = [&](int chunk, auto more_) {
+        constexpr bool more = decltype(more_)::value;   // every chunk but the last: 64 tokens, and one follows
+        const int64_t next = slot0 + chunk + 1, ch = (slot0 + chunk) * a.hv + h;
+        const int len = more ? kC : span.len - chunk * kC;
+        const bool busy = more || wave * 16 < len;      // any token of this wave
+        const bool half2 = more || len > 32;            // tokens in the second 32
+        grown = next_grown, left = next_left, beta = next_beta, whole = next_whole;
         if (a.before) write_state(a.before + ch * a.dk * a.dv + v0);
         dev::lds_barrier();                             // the memory's planes are there
         f32x4 o[CT];
@@ -487,12 +508,13 @@ __global__ __launch_bounds__(256) void k_delta_walk(DeltaArgs a) {
             f32x4 w;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                w[j] = beta[j] * (vv[n][j] - grown[j] * held[j]);
+                const float gap = to_float(vv[n][j]) - grown[j] * held[j];
+                w[j] = beta[j] * (more || beta[j] != 0.f ? gap : 0.f);
                 o[n][j] *= grown[j] * a.scale;
             }
             put4<3>(sR, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
         }
-        if (more) load_rows(slot + 1), load_v(chunk + 1);
+        if constexpr (more) load_decays(next), load_rows(next), load_v(chunk + 1);
         dev::lds_barrier();
 #pragma unroll
         for (int n = 0; n < CT; ++n) {
@@ -510,27 +532,29 @@ __global__ __launch_bounds__(256) void k_delta_walk(DeltaArgs a) {
             for (int j = 0; j < 4; ++j) w[j] *= left[j];
             put4<3>(sL, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
         }
+        if constexpr (more) load_inv(next);
         dev::lds_barrier();
         if (owner)
 #pragma unroll
-            for (int n = 0; n < CT; ++n)
+            for (int n = 0; n < CT; ++n) {
+                bf16x8 b[2][3];
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    get8<3>(sL, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b[ks]);
 #pragma unroll
                 for (int i = 0; i < RT; ++i) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) S[i][n][j] *= whole;
-#pragma unroll
-                    for (int ks = 0; ks < 2; ++ks)
-                        if (ks < half) {
-                            bf16x8 b[3];
-                            get8<3>(sL, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
-                            S[i][n] = mm<NP, 3>(kt[i][ks], b, S[i][n]);
-                        }
+                    S[i][n] = mm<NP, 3>(kt[i][0], b[0], S[i][n]);
+                    if (half2) S[i][n] = mm<NP, 3>(kt[i][1], b[1], S[i][n]);
                 }
-        if (more) {
+            }
+        if constexpr (more) {
             put_state();                                // every wave is past its reads of the planes
-            load_kt(slot + 1);
+            load_kt(next);
         }
-        if (busy)
+        if (busy) {
+            T *out = static_cast<T *>(a.out) + ((int64_t)(span.begin + chunk * kC) * a.hv + h) * a.dv + v0;
 #pragma unroll
             for (int n = 0; n < CT; ++n) {
 #pragma unroll
@@ -540,16 +564,19 @@ __global__ __launch_bounds__(256) void k_delta_walk(DeltaArgs a) {
                         get8<NPP>(sV, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
                         o[n] = mm<NPP, NPP>(pf[ks], b, o[n]);
                     }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int t = wave * 16 + g * 4 + j;
-                    if (t < len && v0 + n * 16 + r < a.dv)
-                        static_cast<T *>(a.out)[((int64_t)(span.begin + chunk * kC + t) * a.hv + h) * a.dv + v0 +
-                                                n * 16 + r] = from_float<T>(o[n][j]);
-                }
             }
-        if (more) load_tri(slot + 1);
-    }
+#pragma unroll
+            for (int n = 0; n < CT; ++n)
+                if (all_cols || col_in[n])
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (more || wave * 16 + (int)g * 4 + j < len)
+                            out[ooff + j * a.hv * a.dv + n * 16] = from_float<T>(o[n][j]);
+        }
+        if constexpr (more) load_score(next);
+    };
+    for (int chunk = 0; chunk + 1 < chunks; ++chunk) step(chunk, std::true_type{});
+    if (chunks > 0) step(chunks - 1, std::false_type{});
     if (a.final_state) write_state(a.final_state + sbase);
 }
 

@@ -101,6 +101,23 @@ __device__ inline f32x4 mm(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], f32x4 a
     return acc;
 }
 
+// The same into three sums, by the terms' size: a matrix op waits for the one
+// before it on the same sum, so a wave that has few tiles needs more sums.
+struct Acc3 {
+    f32x4 v[3] = {};
+    __device__ f32x4 sum() const { return v[0] + (v[1] + v[2]); }
+};
+template <int NA, int NB>
+__device__ inline void mm(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], Acc3 &acc) {
+    constexpr int N = NA > NB ? NA : NB;
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int s = 0; s < N; ++s)
+            if (s - i >= 0 && s - i < NB)
+                acc.v[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[s - i], acc.v[s], 0, 0, 0);
+}
+
 template <int N>
 __device__ inline void load_frags(const uint16_t *p, bf16x8 (&f)[N]) {      // p: this lane's part of plane 0
 #pragma unroll

@@ -33,7 +33,7 @@ size_t round_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 bool known(rn_dtype d) { return d == RN_F32 || d == RN_BF16; }
 bool misaligned(const void *p) { return reinterpret_cast<uintptr_t>(p) % kAlign != 0; }
 
-constexpr int64_t kMaxRows = int64_t(1) << 40;
+constexpr int64_t kMaxRows = int64_t(1) << 40, kMaxStride = 1 << 23;
 constexpr int kMaxWidth = 1 << 30, kMaxHeads = 1024, kMaxSequences = 65535;
 
 // ------------------------------------------------------------------ delta rule
@@ -50,6 +50,8 @@ const char *bad_shape(const rn_delta_shape *s) {
     if (s->tokens > 1 && (s->q_stride < (int64_t)s->heads_k * s->dk || s->k_stride < (int64_t)s->heads_k * s->dk ||
                           s->v_stride < (int64_t)s->heads_v * s->dv))
         return "a token stride is smaller than its token";
+    if (s->tokens > 1 && (s->q_stride >= kMaxStride || s->k_stride >= kMaxStride || s->v_stride >= kMaxStride))
+        return "token strides must be below 2^23";
     return nullptr;
 }
 
