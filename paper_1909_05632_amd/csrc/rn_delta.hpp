@@ -150,6 +150,19 @@ __device__ inline void get8(const uint16_t *lds, int plane, int at, bf16x8 (&f)[
     for (int i = 0; i < N; ++i) f[i] = *reinterpret_cast<const bf16x8 *>(lds + i * plane + at);
 }
 
+// A store that is dropped where `in` is false, without a branch: the compiler
+// can then count what is in flight and wait for no more than it needs.  Offsets
+// are in bytes from a base that the wave shares.
+__device__ inline __amdgpu_buffer_rsrc_t rsrc_of(void *base) {
+    return __builtin_amdgcn_make_buffer_rsrc(base, 0, 0x7fffffff, 0x00027000);
+}
+template <class T>
+__device__ inline void store_if(bool in, __amdgpu_buffer_rsrc_t to, uint32_t at, T v) {
+    const uint32_t off = in ? at : 0xfffffff0u;
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), to, off, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), to, off, 0, 0);
+}
+
 // The 16 x 32 pieces of a lower triangular 64 x 64 operand that hold anything:
 // piece (row block, k step) -> 0..5.
 __device__ inline int tri(int rb, int ks) { return rb < 2 ? rb : rb * 2 - 2 + ks; }
