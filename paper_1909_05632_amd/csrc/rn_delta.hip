@@ -363,120 +363,32 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     }
 }
 
-// A sequence's chunks in order.  A block takes 16 CT columns of a head's memory.
-// Waves 0..3 carry the memory from chunk to chunk: wave w has the tokens 16 w ..
-// + 15 of a chunk and the memory's row tiles w, w + 4.  The memory stays in its
-// owners' registers in float32, and goes through LDS as bf16 planes to the waves
-// that multiply by it, as do beta (V - e^c K S) and V'.  Waves 4..7 read the
-// same planes and make the outputs, so that those stay out of the chain from one
-// memory to the next, which is what a long sequence waits for.  The left
-// operands are read from memory in fragment order, straight into registers, each
-// for the next chunk as soon as this one's use of it is over.
+// A sequence's chunks in order.  A block takes 16 CT columns of a head's memory,
+// wave w the tokens 16 w .. + 15 of a chunk and the memory's row tiles w, w + 4;
+// the memory stays in its owners' registers in float32, and goes through LDS as
+// bf16 planes to the waves that multiply by it, as do beta (V - e^c K S) and V'.
+// The left operands are read from memory in fragment order, straight into
+// registers, each for the next chunk as soon as this one's use of it is over.
 template <class T, int KS, int CT, bool SAVE>
-__global__ __launch_bounds__(512, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delta_walk(DeltaArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delta_walk(DeltaArgs a) {
     constexpr int NP = sizeof(T) == 2 ? 1 : 3, NPP = sizeof(T) == 2 ? 2 : 3;
     constexpr int KP = KS * 32, RT = KP > 64 ? KP / 64 : 1;        // row tiles of the memory a wave owns
     constexpr int VT = 16 * CT, ldS = KP + 8, ldT = kC + 8;
     constexpr int kKeys = 4 * KS * NP * kFrag;
     __shared__ __align__(16) uint16_t sS[3 * VT * ldS], sR[3 * VT * ldT], sV[NPP * VT * ldT], sL[3 * VT * ldT];
-    const int role = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int seq = blockIdx.x / a.hv, h = blockIdx.x % a.hv, hk = h / (a.hv / a.hk);
     const int v0 = blockIdx.y * VT;
     const Span span = span_of(a, seq);
     const int chunks = (span.len + kC - 1) / kC;
     const int64_t slot0 = slot_of(span, seq, 0);
+    const int64_t sbase = ((int64_t)seq * a.hv + h) * a.dk * a.dv + v0;
+    const bool owner = KP >= 64 || wave * 16 < KP;
     bool col_in[CT];
 #pragma unroll
     for (int n = 0; n < CT; ++n) col_in[n] = v0 + n * 16 + (int)r < a.dv;
-    // Loads are unconditional, from places clamped into the arrays, so that the
-    // compiler can count them and wait for each only where it is used.
-    const auto load_pair = [&](const uint16_t *base, int planes, int64_t slot) {   // pieces of row block `wave`
-        return base + (slot * a.hv + h) * kTri * planes * kFrag;
-    };
 
-    if (role == 1) {
-        bf16x8 qf[KS][NP], pf[2][NPP];
-        f32x4 grown{}, next_grown{};
-        const auto load_q = [&](int64_t slot, int ks) {
-            load_frags<NP>(a.qf + ((slot * a.hk + hk) * kKeys + wave * KS * NP * kFrag) + (lane * 8 + ks * NP * kFrag), qf[ks]);
-        };
-        const auto load_score = [&](int64_t slot) {
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks)
-                load_frags<NPP>(load_pair(a.pf, NPP, slot) + tri(wave, min(ks, wave / 2)) * NPP * kFrag + lane * 8, pf[ks]);
-        };
-        const auto load_grown = [&](int64_t slot) {
-            next_grown = *reinterpret_cast<const f32x4 *>(a.dec + ((slot * a.hv + h) * 3 * kC + wave * 16) + g * 4);
-        };
-        const uint32_t at = (wave * 16 + g * 4) * (uint32_t)(a.hv * a.dv) + r;
-        if (chunks > 0) {
-            load_grown(slot0);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) load_q(slot0, ks);
-            load_score(slot0);
-        }
-        const auto step = [&](int chunk, auto more_) {
-            constexpr bool more = decltype(more_)::value;
-            const int64_t next = slot0 + chunk + 1;
-            const int len = more ? kC : span.len - chunk * kC;
-            const bool busy = more || wave * 16 < len;
-            grown = next_grown;
-            dev::lds_barrier();                         // the memory's planes are there
-            Acc3 read[CT];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                if (busy) {
-                    bf16x8 s[CT][NPP];
-#pragma unroll
-                    for (int n = 0; n < CT; ++n) get8<NPP>(sS, VT * ldS, (n * 16 + r) * ldS + ks * 32 + g * 8, s[n]);
-#pragma unroll
-                    for (int n = 0; n < CT; ++n) mm<NP, NPP>(qf[ks], s[n], read[n]);
-                }
-                if constexpr (more) load_q(next, ks);
-            }
-            f32x4 o[CT];
-#pragma unroll
-            for (int n = 0; n < CT; ++n) {
-                o[n] = read[n].sum();
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[n][j] *= grown[j] * a.scale;
-            }
-            if constexpr (more) load_grown(next);
-            dev::lds_barrier();
-            dev::lds_barrier();                         // V' is there
-            if (busy) {
-                Acc3 acc[CT];
-                const auto part = [&](int ks) {
-                    bf16x8 b[CT][NPP];
-#pragma unroll
-                    for (int n = 0; n < CT; ++n) get8<NPP>(sV, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b[n]);
-#pragma unroll
-                    for (int n = 0; n < CT; ++n) mm<NPP, NPP>(pf[ks], b[n], acc[n]);
-                };
-                part(0);
-                if (wave >= 2) part(1);
-                const __amdgpu_buffer_rsrc_t rs = rsrc_of(static_cast<T *>(a.out) +
-                                                          ((int64_t)(span.begin + chunk * kC) * a.hv + h) * a.dv + v0);
-#pragma unroll
-                for (int n = 0; n < CT; ++n) {
-                    o[n] += acc[n].sum();
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        store_if(col_in[n] && (more || wave * 16 + (int)g * 4 + j < len), rs,
-                                 sizeof(T) * (at + j * a.hv * a.dv + n * 16), from_float<T>(o[n][j]));
-                }
-            }
-            if constexpr (more) load_score(next);
-        };
-        for (int chunk = 0; chunk + 1 < chunks; ++chunk) step(chunk, std::true_type{});
-        if (chunks > 0) step(chunks - 1, std::false_type{});
-        return;
-    }
-
-    const int64_t sbase = ((int64_t)seq * a.hv + h) * a.dk * a.dv + v0;
-    const bool owner = KP >= 64 || wave * 16 < KP;
     f32x4 S[RT][CT];
     const auto put_state = [&] {
         if (owner)
@@ -510,10 +422,17 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
                 S[i][n][j] = in ? a.state[sbase + (int64_t)d * a.dv + n * 16 + r] : 0.f;
             }
 
-    bf16x8 kf[KS][NP], kt[RT][2][NP], mf[2][3];
+    // Loads are unconditional, from places clamped into the arrays, so that the
+    // compiler can count them and wait for each only where it is used.
+    bf16x8 kf[KS][NP], qf[KS][NP], kt[RT][2][NP], mf[2][3], pf[2][NPP];
     T vv[CT][4];
-    const auto load_k = [&](int64_t slot, int ks) {
-        load_frags<NP>(a.kf + ((slot * a.hk + hk) * kKeys + wave * KS * NP * kFrag) + (lane * 8 + ks * NP * kFrag), kf[ks]);
+    const auto load_rows = [&](int64_t slot) {
+        const int64_t at = (slot * a.hk + hk) * kKeys + wave * KS * NP * kFrag;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            load_frags<NP>(a.kf + at + (lane * 8 + ks * NP * kFrag), kf[ks]);
+            load_frags<NP>(a.qf + at + (lane * 8 + ks * NP * kFrag), qf[ks]);
+        }
     };
     const auto load_kt = [&](int64_t slot) {
         const int64_t at = (slot * a.hk + hk) * kKeys + (wave % (2 * KS)) * 2 * NP * kFrag;
@@ -523,9 +442,15 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
             for (int ks = 0; ks < 2; ++ks) load_frags<NP>(a.kt + at + (lane * 8 + (8 * i + ks) * NP * kFrag), kt[i][ks]);
     };
     const auto load_inv = [&](int64_t slot) {
+        const int64_t at = (slot * a.hv + h) * kTri * 3 * kFrag;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) load_frags<3>(a.mf + (at + tri(wave, min(ks, wave / 2)) * 3 * kFrag) + lane * 8, mf[ks]);
+    };
+    const auto load_score = [&](int64_t slot) {
+        const int64_t at = (slot * a.hv + h) * kTri * NPP * kFrag;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
-            load_frags<3>(load_pair(a.mf, 3, slot) + tri(wave, min(ks, wave / 2)) * 3 * kFrag + lane * 8, mf[ks]);
+            load_frags<NPP>(a.pf + (at + tri(wave, min(ks, wave / 2)) * NPP * kFrag) + lane * 8, pf[ks]);
     };
     f32x4 grown{}, left{}, beta{}, next_grown{}, next_left{}, next_beta{};
     float whole = 0.f, next_whole = 0.f;
@@ -551,12 +476,9 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
 #pragma unroll
             for (int n = 0; n < CT; ++n) vv[n][j] = base[voff[j] + col[n]];
     };
-    if (chunks > 0) {
-        load_decays(slot0);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) load_k(slot0, ks);
-        load_v(0), load_inv(slot0), load_kt(slot0);
-    }
+    const uint32_t ooff = (wave * 16 + g * 4) * (uint32_t)(a.hv * a.dv) + r;
+    if (chunks > 0)
+        load_decays(slot0), load_rows(slot0), load_v(0), load_inv(slot0), load_kt(slot0), load_score(slot0);
     put_state();
 
     const auto step = [&](int chunk, auto more_) {
@@ -568,77 +490,90 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
         grown = next_grown, left = next_left, beta = next_beta, whole = next_whole;
         if constexpr (SAVE) write_state(a.before + ch * a.dk * a.dv + v0);
         dev::lds_barrier();                             // the memory's planes are there
-        {
-            Acc3 held[CT];
+        f32x4 o[CT];
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                if (busy) {
-                    bf16x8 s[CT][3];
+        for (int n = 0; n < CT; ++n) {
+            f32x4 held{};
+            o[n] = f32x4{};
+            if (busy)
 #pragma unroll
-                    for (int n = 0; n < CT; ++n) get8<3>(sS, VT * ldS, (n * 16 + r) * ldS + ks * 32 + g * 8, s[n]);
+                for (int ks = 0; ks < KS; ++ks) {
+                    bf16x8 s[3], s2[NPP];
+                    get8<3>(sS, VT * ldS, (n * 16 + r) * ldS + ks * 32 + g * 8, s);
 #pragma unroll
-                    for (int n = 0; n < CT; ++n) mm<NP, 3>(kf[ks], s[n], held[n]);
+                    for (int i = 0; i < NPP; ++i) s2[i] = s[i];
+                    held = mm<NP, 3>(kf[ks], s, held);
+                    o[n] = mm<NP, NPP>(qf[ks], s2, o[n]);
                 }
-                if constexpr (more) load_k(next, ks);
+            f32x4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float gap = to_float(vv[n][j]) - grown[j] * held[j];
+                w[j] = beta[j] * (more || beta[j] != 0.f ? gap : 0.f);
+                o[n][j] *= grown[j] * a.scale;
             }
+            put4<3>(sR, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
+        }
+        if constexpr (more) load_decays(next), load_rows(next), load_v(chunk + 1);
+        dev::lds_barrier();
+#pragma unroll
+        for (int n = 0; n < CT; ++n) {
+            f32x4 w{};
+            if (busy)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    if (ks <= wave / 2) {
+                        bf16x8 b[3];
+                        get8<3>(sR, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
+                        w = mm<3, 3>(mf[ks], b, w);
+                    }
+            put4<NPP>(sV, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] *= left[j];
+            put4<3>(sL, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
+        }
+        if constexpr (more) load_inv(next);
+        dev::lds_barrier();
+        if (owner)
 #pragma unroll
             for (int n = 0; n < CT; ++n) {
-                const f32x4 x = held[n].sum();
-                f32x4 w;
+                bf16x8 b[2][3];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float gap = to_float(vv[n][j]) - grown[j] * x[j];
-                    w[j] = beta[j] * (more || beta[j] != 0.f ? gap : 0.f);
+                for (int ks = 0; ks < 2; ++ks)
+                    get8<3>(sL, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b[ks]);
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) S[i][n][j] *= whole;
+                    S[i][n] = mm<NP, 3>(kt[i][0], b[0], S[i][n]);
+                    if (half2) S[i][n] = mm<NP, 3>(kt[i][1], b[1], S[i][n]);
                 }
-                put4<3>(sR, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
             }
-        }
-        dev::lds_barrier();
-        {
-            Acc3 acc[CT];
-            const auto part = [&](int ks) {
-                bf16x8 b[CT][3];
-#pragma unroll
-                for (int n = 0; n < CT; ++n) get8<3>(sR, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b[n]);
-#pragma unroll
-                for (int n = 0; n < CT; ++n) mm<3, 3>(mf[ks], b[n], acc[n]);
-            };
-            if (busy) {
-                part(0);
-                if (wave >= 2) part(1);
-            }
-            if constexpr (more) load_decays(next), load_v(chunk + 1), load_inv(next);
-#pragma unroll
-            for (int n = 0; n < CT; ++n) {
-                f32x4 w = acc[n].sum();
-                put4<NPP>(sV, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] *= left[j];
-                put4<3>(sL, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
-            }
-        }
-        dev::lds_barrier();
-        if (owner) {
-            bf16x8 b[2][CT][3];
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-                for (int n = 0; n < CT; ++n) get8<3>(sL, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b[ks][n]);
-#pragma unroll
-            for (int i = 0; i < RT; ++i)
-#pragma unroll
-                for (int n = 0; n < CT; ++n) {
-                    f32x4 x{};
-                    x = mm<NP, 3>(kt[i][0], b[0][n], x);
-                    if (half2) x = mm<NP, 3>(kt[i][1], b[1][n], x);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) S[i][n][j] = fmaf(whole, S[i][n][j], x[j]);
-                }
-        }
         if constexpr (more) {
-            load_kt(next);
             put_state();                                // every wave is past its reads of the planes
+            load_kt(next);
         }
+        if (busy) {
+            T *out = static_cast<T *>(a.out) + ((int64_t)(span.begin + chunk * kC) * a.hv + h) * a.dv + v0;
+#pragma unroll
+            for (int n = 0; n < CT; ++n) {
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    if (ks <= wave / 2) {
+                        bf16x8 b[NPP];
+                        get8<NPP>(sV, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
+                        o[n] = mm<NPP, NPP>(pf[ks], b, o[n]);
+                    }
+            }
+            const __amdgpu_buffer_rsrc_t rs = rsrc_of(out);
+#pragma unroll
+            for (int n = 0; n < CT; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    store_if(col_in[n] && (more || wave * 16 + (int)g * 4 + j < len), rs,
+                             sizeof(T) * (ooff + j * a.hv * a.dv + n * 16), from_float<T>(o[n][j]));
+        }
+        if constexpr (more) load_score(next);
     };
     for (int chunk = 0; chunk + 1 < chunks; ++chunk) step(chunk, std::true_type{});
     if (chunks > 0) step(chunks - 1, std::false_type{});
@@ -665,10 +600,14 @@ hipError_t forward_ks(const DeltaArgs &a, hipStream_t s) {
     const auto walk = [&](auto ct) {
         constexpr int CT = decltype(ct)::value;
         const dim3 grid(a.n * a.hv, (a.dv + 16 * CT - 1) / (16 * CT));
-        if (a.before) k_delta_walk<T, KS, CT, true><<<grid, 512, 0, s>>>(a);
-        else k_delta_walk<T, KS, CT, false><<<grid, 512, 0, s>>>(a);
+        if (a.before) k_delta_walk<T, KS, CT, true><<<grid, 256, 0, s>>>(a);
+        else k_delta_walk<T, KS, CT, false><<<grid, 256, 0, s>>>(a);
     };
-    if (a.dv <= 16) walk(std::integral_constant<int, 1>{});
+    // Two column tiles a block share the left operands' loads; with too few
+    // blocks for the CUs one tile's shorter chain counts more.  7 ragged sequences
+    // of 8 heads (224 blocks of two tiles): 132 us with two, 105 with one; 256 of 4
+    // heads: 41 us with two, 71 with one.
+    if (a.dv <= 16 || a.n * a.hv * ((a.dv + 31) / 32) <= 256) walk(std::integral_constant<int, 1>{});
     else walk(std::integral_constant<int, 2>{});
     return hipGetLastError();
 }
