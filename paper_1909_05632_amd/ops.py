@@ -90,7 +90,8 @@ def _check(status: int) -> None:
         raise B.ReuseNetError(status, reuse_ops_last_error())
 
 
-_CODES = {torch.float32: B.RN_F32, torch.bfloat16: B.RN_BF16}
+_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
+_CODES = {_F32: B.RN_F32, _BF16: B.RN_BF16}
 
 
 # The C ABI takes raw pointers and sizes: whatever does not match what the
@@ -111,15 +112,15 @@ def _like(x, what: str, dtype, device, shape) -> int:
     """The pointer of a contiguous tensor that has to be just so."""
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"{what} must be a torch tensor")
+    if x.dtype is dtype and x.device == device and x.shape == shape and x.is_contiguous():
+        return x.data_ptr()
     if x.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, got {x.dtype}")
     if x.device != device:
         raise ValueError(f"{what} must be on {device}, got {x.device}")
     if x.shape != shape:
         raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(x.shape)}")
-    if not x.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
-    return x.data_ptr()
+    raise ValueError(f"{what} must be contiguous")
 
 
 def _opt(x, what: str, dtype, device, shape) -> Optional[int]:
@@ -144,14 +145,30 @@ def _rows(x, what: str):
     raise ValueError(f"{what} must have contiguous rows at one stride, got strides {x.stride()}")
 
 
+# The small calls' time is the host's: the current stream's handle without a
+# Stream object around it, where torch has that (1.9 -> 0.1 us).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _launch(device, stream, call, *args) -> None:
     """The call on `stream`, with the tensors' GPU current."""
-    s = (stream or torch.cuda.current_stream(device)).cuda_stream
-    if torch.cuda.current_device() == device.index:
-        _check(call(*args, s))
+    index = device.index
+    s = _raw_stream(index) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == index:
+        status = call(*args, s)
     else:
         with torch.cuda.device(device):
-            _check(call(*args, s))
+            status = call(*args, s)
+    if status:
+        raise B.ReuseNetError(status, reuse_ops_last_error())
+
+
+def _empty(like, shape=None, dtype=None):
+    """A contiguous tensor of `like`'s device (and shape and dtype)."""
+    if shape is None:
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
+    return like.new_empty(shape, dtype=dtype)
 
 
 # ------------------------------------------------------------------ layer norm
@@ -168,12 +185,14 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, with_stats: bool = 
         raise ValueError("x must have a last axis of 1 or more")
     dev, width = x.device, x.shape[-1]
     rows, stride = _rows(x, "x")
-    w = _opt(weight, "weight", torch.float32, dev, (width,))
-    b = _opt(bias, "bias", torch.float32, dev, (width,))
+    w = None if weight is None else _like(weight, "weight", _F32, dev, (width,))
+    b = None if bias is None else _like(bias, "bias", _F32, dev, (width,))
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-    y = _like(out, "out", x.dtype, dev, x.shape)
-    stats = torch.empty((rows, 2), dtype=torch.float32, device=dev) if with_stats else None
+        out = _empty(x)
+        y = out.data_ptr()
+    else:
+        y = _like(out, "out", x.dtype, dev, x.shape)
+    stats = _empty(x, (rows, 2), _F32) if with_stats else None
     _launch(dev, stream, load_ops().reuse_ops_layer_norm, rows, width, x.data_ptr(), stride, code, w, b, eps, y, width,
             None if stats is None else stats.data_ptr())
     return (out, stats) if with_stats else out
@@ -195,11 +214,13 @@ def layer_norm_backward(dy, x, weight, stats, dx=None, dweight=None, dbias=None,
     dev, width = x.device, x.shape[-1]
     rows, xs = _rows(x, "x")
     _, dys = _rows(dy, "dy")
-    w = _opt(weight, "weight", torch.float32, dev, (width,))
-    st = _like(stats, "stats", torch.float32, dev, (rows, 2))
+    w = _opt(weight, "weight", _F32, dev, (width,))
+    st = _like(stats, "stats", _F32, dev, (rows, 2))
     if dx is None:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
-    d = _like(dx, "dx", x.dtype, dev, x.shape)
+        dx = _empty(x)
+        d = dx.data_ptr()
+    else:
+        d = _like(dx, "dx", x.dtype, dev, x.shape)
     L = load_ops()
     dw = db = sc = None
     need = 0
@@ -207,13 +228,13 @@ def layer_norm_backward(dy, x, weight, stats, dx=None, dweight=None, dbias=None,
         if accumulate and (dweight is None or dbias is None):
             raise ValueError("accumulate needs dweight and dbias")
         if dweight is None:
-            dweight = torch.empty(width, dtype=torch.float32, device=dev)
+            dweight = _empty(x, width, _F32)
         if dbias is None:
-            dbias = torch.empty(width, dtype=torch.float32, device=dev)
-        dw = _like(dweight, "dweight", torch.float32, dev, (width,))
-        db = _like(dbias, "dbias", torch.float32, dev, (width,))
+            dbias = _empty(x, width, _F32)
+        dw = _like(dweight, "dweight", _F32, dev, (width,))
+        db = _like(dbias, "dbias", _F32, dev, (width,))
         need = L.reuse_ops_layer_norm_backward_scratch_bytes(rows, width)
-        scratch = torch.empty(need, dtype=torch.uint8, device=dev)
+        scratch = _empty(x, need, torch.uint8)
         sc = scratch.data_ptr()
     _launch(dev, stream, L.reuse_ops_layer_norm_backward, rows, width, dy.data_ptr(), dys, x.data_ptr(), xs, code, w,
             st, d, width, dw, db, int(accumulate), sc, need)
@@ -240,37 +261,45 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=Non
     if not 1 <= vocab <= RN_SAMPLE_MAX_VOCAB:
         raise ValueError(f"vocab must be 1..{RN_SAMPLE_MAX_VOCAB}, got {vocab}")
     rows, stride = _rows(logits, "logits")
-    up = _like(u, "u", torch.float32, dev, (n,))
-    p = rn_sample_params(1.0, 0, 1.0, 0.0)
-    for name, value, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
-                               ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+    up = _like(u, "u", _F32, dev, (n,))
+    def setting(value, name, dtype):
+        """(number, pointer): one of the two is what counts."""
         if isinstance(value, torch.Tensor):
-            setattr(p, "dev_" + name, _like(value, name, dtype, dev, (n,)))
-        else:
-            setattr(p, name, int(value) if dtype is torch.int32 else float(value))
+            return 0, _like(value, name, dtype, dev, (n,))
+        return value, None
+
+    t, tp = setting(temperature, "temperature", _F32)
+    k, kp = setting(top_k, "top_k", _I32)
+    p, pp = setting(top_p, "top_p", _F32)
+    m, mp = setting(min_p, "min_p", _F32)
+    params = rn_sample_params(t, k, p, m, tp, kp, pp, mp)
     if tokens is None:
-        tokens = torch.empty(n, dtype=torch.int32, device=dev)
+        tokens = _empty(logits, n, _I32)
     if logprobs is None:
-        logprobs = torch.empty(n, dtype=torch.float32, device=dev)
-    t = _like(tokens, "tokens", torch.int32, dev, (n,))
-    lp = _like(logprobs, "logprobs", torch.float32, dev, (n,))
-    _launch(dev, stream, load_ops().reuse_ops_sample, n, vocab, logits.data_ptr(), stride, code, up, ctypes.byref(p), t,
-            lp)
+        logprobs = _empty(logits, n, _F32)
+    ids = _like(tokens, "tokens", _I32, dev, (n,))
+    lp = _like(logprobs, "logprobs", _F32, dev, (n,))
+    _launch(dev, stream, load_ops().reuse_ops_sample, n, vocab, logits.data_ptr(), stride, code, up,
+            ctypes.byref(params), ids, lp)
     return tokens, logprobs
 
 
 # ------------------------------------------------------------------ gated delta rule
 
-def _tokens(x, what: str, code: int, tokens: int, device):
+def _tokens(x, what: str, dtype, tokens: int, device):
     """(heads, size, token stride) of [tokens][heads][size] data whose heads are contiguous."""
-    if _data(x, what) != code or x.device != device:
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{what} must be a torch tensor")
+    if x.dtype is not dtype or x.device != device:
         raise ValueError(f"{what} must have q's dtype and device")
     if x.dim() != 3 or x.shape[0] != tokens:
         raise ValueError(f"{what} must have shape ({tokens}, heads, size), got {tuple(x.shape)}")
     _, heads, size = x.shape
-    st = x.stride()
     if heads < 1 or size < 1:
         raise ValueError(f"{what} must have heads and elements")
+    if x.is_contiguous():
+        return heads, size, heads * size
+    st = x.stride()
     if (size > 1 and st[2] != 1) or (heads > 1 and st[1] != size):
         raise ValueError(f"{what} must be contiguous within a token, got strides {st}")
     if tokens > 1 and st[0] < heads * size:
@@ -282,18 +311,18 @@ def _delta_shape(q, k, v, g, beta, n: int, scale):
     code = _data(q, "q")
     if q.dim() != 3:
         raise ValueError(f"q must have shape (tokens, heads, dk), got {tuple(q.shape)}")
-    tokens, dev = q.shape[0], q.device
-    hk, dk, qs = _tokens(q, "q", code, tokens, dev)
-    hk2, dk2, ks = _tokens(k, "k", code, tokens, dev)
-    hv, dv, vs = _tokens(v, "v", code, tokens, dev)
+    tokens, dev, dtype = q.shape[0], q.device, q.dtype
+    hk, dk, qs = _tokens(q, "q", dtype, tokens, dev)
+    hk2, dk2, ks = _tokens(k, "k", dtype, tokens, dev)
+    hv, dv, vs = _tokens(v, "v", dtype, tokens, dev)
     if (hk2, dk2) != (hk, dk):
         raise ValueError("k must have q's shape")
     if hv % hk:
         raise ValueError(f"{hv} value heads cannot share {hk} key heads")
     shape = rn_delta_shape(n, hk, hv, dk, dv, tokens, code, dk ** -0.5 if scale is None else scale, qs, ks, vs)
-    gp = _like(g, "g", torch.float32, dev, (tokens, hv))
-    bp = _like(beta, "beta", torch.float32, dev, (tokens, hv))
-    return shape, gp, bp, dev
+    gp = _like(g, "g", _F32, dev, (tokens, hv))
+    bp = _like(beta, "beta", _F32, dev, (tokens, hv))
+    return shape, gp, bp, dev, hv, dk, dv
 
 
 def _sequences(seq_off, n, tokens: int, device):
@@ -304,7 +333,7 @@ def _sequences(seq_off, n, tokens: int, device):
         m = seq_off.shape[0] - 1
         if n is not None and n != m:
             raise ValueError(f"n is {n}, seq_off has {m} sequences")
-        return m, _like(seq_off, "seq_off", torch.int32, device, (m + 1,))
+        return m, _like(seq_off, "seq_off", _I32, device, (m + 1,))
     if n is None:
         raise ValueError("give seq_off, or n for even sequences")
     if n < 0 or (n and tokens % n) or (not n and tokens):
@@ -321,15 +350,15 @@ def delta_step(q, k, v, g, beta, state, stream_ids=None, scale=None, out=None, s
     Returns out [n][heads_v][dv].
     """
     n = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() else 0
-    shape, gp, bp, dev = _delta_shape(q, k, v, g, beta, n, scale)
+    shape, gp, bp, dev, hv, dk, dv = _delta_shape(q, k, v, g, beta, n, scale)
     slots = state.shape[0] if isinstance(state, torch.Tensor) and state.dim() else 0
-    sp = _like(state, "state", torch.float32, dev, (slots, shape.heads_v, shape.dk, shape.dv))
-    ids = _opt(stream_ids, "stream_ids", torch.int32, dev, (n,))
+    sp = _like(state, "state", _F32, dev, (slots, hv, dk, dv))
+    ids = _opt(stream_ids, "stream_ids", _I32, dev, (n,))
     if ids is None and slots < n:
         raise ValueError(f"{n} streams need as many slots, state has {slots}")
     if out is None:
-        out = torch.empty((n, shape.heads_v, shape.dv), dtype=q.dtype, device=dev)
-    op = _like(out, "out", q.dtype, dev, (n, shape.heads_v, shape.dv))
+        out = _empty(v)
+    op = _like(out, "out", q.dtype, dev, (n, hv, dv))
     _launch(dev, stream, load_ops().reuse_ops_delta_step, ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(),
             gp, bp, ids, slots, sp, op)
     return out
@@ -355,22 +384,22 @@ def delta_forward(q, k, v, g, beta, seq_off=None, n=None, state=None, final=None
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor of shape (tokens, heads, dk)")
     n, off = _sequences(seq_off, n, q.shape[0], q.device)
-    shape, gp, bp, dev = _delta_shape(q, k, v, g, beta, n, scale)
-    dims = (n, shape.heads_v, shape.dk, shape.dv)
-    sp = _opt(state, "state", torch.float32, dev, dims)
+    shape, gp, bp, dev, hv, dk, dv = _delta_shape(q, k, v, g, beta, n, scale)
+    dims = (n, hv, dk, dv)
+    sp = _opt(state, "state", _F32, dev, dims)
     L = load_ops()
     need = _supported(L.reuse_ops_delta_scratch_bytes(ctypes.byref(shape)), L.reuse_ops_delta_forward, shape)
     if final is None:
-        final = torch.empty(dims, dtype=torch.float32, device=dev)
-    fp = _like(final, "final", torch.float32, dev, dims)
+        final = _empty(q, dims, _F32)
+    fp = _like(final, "final", _F32, dev, dims)
     if out is None:
-        out = torch.empty((shape.tokens, shape.heads_v, shape.dv), dtype=q.dtype, device=dev)
-    op = _like(out, "out", q.dtype, dev, (shape.tokens, shape.heads_v, shape.dv))
-    scratch = torch.empty(need, dtype=torch.uint8, device=dev)
+        out = _empty(v)
+    op = _like(out, "out", q.dtype, dev, v.shape)
+    scratch = _empty(q, need, torch.uint8)
     saved, kept, size = None, None, 0
     if save:
         size = L.reuse_ops_delta_saved_bytes(ctypes.byref(shape))
-        saved = torch.empty(size, dtype=torch.uint8, device=dev)
+        saved = _empty(q, size, torch.uint8)
         kept = saved.data_ptr()
     _launch(dev, stream, L.reuse_ops_delta_forward, ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp,
             bp, off, sp, fp, op, kept, size, scratch.data_ptr(), need)
@@ -389,24 +418,21 @@ def delta_backward(dout, q, k, v, g, beta, seq_off=None, n=None, saved=None, dfi
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor of shape (tokens, heads, dk)")
     n, off = _sequences(seq_off, n, q.shape[0], q.device)
-    shape, gp, bp, dev = _delta_shape(q, k, v, g, beta, n, scale)
-    dims = (n, shape.heads_v, shape.dk, shape.dv)
-    do = _like(dout, "dout", q.dtype, dev, (shape.tokens, shape.heads_v, shape.dv))
-    df = _opt(dfinal, "dfinal", torch.float32, dev, dims)
+    shape, gp, bp, dev, hv, dk, dv = _delta_shape(q, k, v, g, beta, n, scale)
+    dims = (n, hv, dk, dv)
+    do = _like(dout, "dout", q.dtype, dev, v.shape)
+    df = _opt(dfinal, "dfinal", _F32, dev, dims)
     L = load_ops()
     need = _supported(L.reuse_ops_delta_backward_scratch_bytes(ctypes.byref(shape)), L.reuse_ops_delta_backward, shape)
     if not isinstance(saved, torch.Tensor):
         raise TypeError("saved must be the buffer of delta_forward(..., save=True)")
     sp = _like(saved, "saved", torch.uint8, dev, (L.reuse_ops_delta_saved_bytes(ctypes.byref(shape)),))
-    dq = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    dk = torch.empty(k.shape, dtype=q.dtype, device=dev)
-    dv = torch.empty(v.shape, dtype=q.dtype, device=dev)
-    dg, dbeta = torch.empty_like(g), torch.empty_like(beta)
-    dstate = torch.empty(dims, dtype=torch.float32, device=dev) if want_dstate else None
-    scratch = torch.empty(need, dtype=torch.uint8, device=dev)
+    gq, gk, gv, dg, dbeta = _empty(q), _empty(k), _empty(v), _empty(g), _empty(beta)
+    dstate = _empty(q, dims, _F32) if want_dstate else None
+    scratch = _empty(q, need, torch.uint8)
     _launch(dev, stream, L.reuse_ops_delta_backward, ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp,
-            bp, off, sp, saved.numel(), do, df, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dg.data_ptr(),
+            bp, off, sp, saved.numel(), do, df, gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), dg.data_ptr(),
             dbeta.data_ptr(), None if dstate is None else dstate.data_ptr(), scratch.data_ptr(), need)
     if stream is not None:
         scratch.record_stream(stream)
-    return dq, dk, dv, dg, dbeta, dstate
+    return gq, gk, gv, dg, dbeta, dstate
