@@ -1,6 +1,8 @@
 // Device code that the gated delta rule's kernels share.
 #pragma once
 
+#include <type_traits>
+
 #include "rn_ops.hpp"
 #include "rn_split.hpp"
 
@@ -8,7 +10,7 @@ namespace rn {
 namespace ops {
 
 constexpr int kC = RN_DELTA_CHUNK;   // tokens of a chunk
-constexpr int kVT = 16;              // value columns of a block of the walks over chunks
+constexpr int kLd = kC + 4;          // row length of a 64-wide LDS tile, off the banks' stride
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -101,23 +103,6 @@ __device__ inline f32x4 mm(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], f32x4 a
     return acc;
 }
 
-// The same into three sums, by the terms' size: a matrix op waits for the one
-// before it on the same sum, so a wave that has few tiles needs more sums.
-struct Acc3 {
-    f32x4 v[3] = {};
-    __device__ f32x4 sum() const { return v[0] + (v[1] + v[2]); }
-};
-template <int NA, int NB>
-__device__ inline void mm(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], Acc3 &acc) {
-    constexpr int N = NA > NB ? NA : NB;
-#pragma unroll
-    for (int i = 0; i < NA; ++i)
-#pragma unroll
-        for (int s = 0; s < N; ++s)
-            if (s - i >= 0 && s - i < NB)
-                acc.v[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[s - i], acc.v[s], 0, 0, 0);
-}
-
 template <int N>
 __device__ inline void load_frags(const uint16_t *p, bf16x8 (&f)[N]) {      // p: this lane's part of plane 0
 #pragma unroll
@@ -167,6 +152,234 @@ __device__ inline void store_if(bool in, __amdgpu_buffer_rsrc_t to, uint32_t at,
 // piece (row block, k step) -> 0..5.
 __device__ inline int tri(int rb, int ks) { return rb < 2 ? rb : rb * 2 - 2 + ks; }
 constexpr int kTri = 6;
+// The same of its transpose.
+__device__ inline int tri_t(int rb, int ks) { return rb < 2 ? rb * 2 + ks : rb + 2; }
+
+// ---- the operands
+
+// The chunk operands of the walks, in fragment order: the triangular inverse, P
+// and the decays of a chunk and value head, and with the first of the value heads
+// that share a key head its K, Q and K^T.  The forward walk multiplies by
+// (I + A)^-1 with A_ij = e^(ci - cj) k_i . k_j beta_j and by P; the backward walk
+// (BWD) by the transposes of P and of (I + A)^-1 with beta_i in beta_j's place,
+// and by Q^T in place of Q.  A block takes a chunk slot and a value
+// head, a wave 16 of its tokens; what lies past the chunk's last 16 is not made.
+//
+// The inverse by blocks of 16: the four on the diagonal by forward substitution,
+// a column a lane; then the 32s and the 64 from
+//   [L11 0; L21 L22]^-1 = [X11 0; -X22 L21 X11  X22]
+// on the float32 matrix cores.  Substitution of the blocks alone keeps this as
+// stable as that of the whole, with a chain of 16 rows in place of 64.  (A power
+// series of the nilpotent A would be shorter, and loses all its bits where keys
+// are nearly parallel, as those of neighbouring frames are.)
+//
+// A chain of small steps with barriers between them: bound by their latency, so
+// the LDS is kept small (four blocks a CU in bfloat16) and the blocks many.
+template <class T, int KS, bool VEC, bool BWD>
+__global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
+    constexpr int NP = sizeof(T) == 2 ? 1 : 3, NPP = sizeof(T) == 2 && !BWD ? 2 : 3;
+    constexpr int kKeys = 4 * KS * NP * kFrag;          // bf16 of one of kf, qf, kt
+    extern __shared__ __align__(16) float lds[];
+    float *x = lds, *y = x + kC * kLd;                  // A, then its inverse; P, over K's fragments
+    uint16_t *skf = reinterpret_cast<uint16_t *>(y), *sqf = skf + kKeys;
+    __shared__ double cs[kC];
+    __shared__ float beta[kC];
+    const int slot = blockIdx.x, h = blockIdx.y, group = a.hv / a.hk, hk = h / group;
+    const Chunk c = chunk_of(a, slot);
+    if (c.len == 0) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int blocks = (c.len + 15) / 16;               // 16s of tokens
+    const bool first = h % group == 0, busy = wave < blocks;
+    const int64_t keys = ((int64_t)slot * a.hk + hk) * kKeys, ch = (int64_t)slot * a.hv + h;
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    // K and Q as rows: the wave's 16 tokens.
+    const int token = wave * 16 + r;
+    bf16x8 ka[KS][NP], qa[KS][NP];
+    const auto row = [&](const void *p, int64_t stride, int ks, bf16x8 (&f)[NP]) {
+        const int64_t at = (int64_t)(c.begin + token) * stride + hk * a.dk;
+        const int d0 = ks * 32 + g * 8;
+        float v[8];
+        if constexpr (VEC) {                            // rows on 16 bytes, dk a multiple of 8
+            constexpr int PER = 16 / sizeof(T);
+#pragma unroll
+            for (int e = 0; e < 8; e += PER) {
+                Pack<T, PER> q{};
+                if (token < c.len && d0 < a.dk) q = *reinterpret_cast<const Pack<T, PER> *>(static_cast<const T *>(p) + at + d0 + e);
+#pragma unroll
+                for (int o = 0; o < PER; ++o) v[e + o] = to_float(q.v[o]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = token < c.len && d0 + e < a.dk ? load<T>(p, at + d0 + e) : 0.f;
+        }
+        uint32_t w[4][NP];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split_pair<NP>(v[2 * e], v[2 * e + 1], w[e]);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) f[i] = __builtin_bit_cast(bf16x8, u32x4{w[0][i], w[1][i], w[2][i], w[3][i]});
+    };
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        row(a.k, a.ks, ks, ka[ks]);
+        row(a.q, a.qs, ks, qa[ks]);
+    }
+    if (wave == 0) {
+        const double s = decay_sums(a, c, h), last = __shfl(s, 63);
+        const float b = lane < c.len ? a.beta[(int64_t)(c.begin + lane) * a.hv + h] : 0.f;
+        cs[lane] = s;
+        beta[lane] = b;
+        a.dec[ch * 3 * kC + lane] = expf((float)s);
+        a.dec[ch * 3 * kC + kC + lane] = expf((float)(last - s));
+        a.dec[ch * 3 * kC + 2 * kC + lane] = b;
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int at = ((wave * KS + ks) * NP + i) * kFrag + lane * 8;
+            *reinterpret_cast<bf16x8 *>(skf + at) = ka[ks][i];
+            if constexpr (BWD) *reinterpret_cast<bf16x8 *>(sqf + at) = qa[ks][i];
+            if (first && busy) {
+                *reinterpret_cast<bf16x8 *>(a.kf + keys + at) = ka[ks][i];
+                if constexpr (!BWD) *reinterpret_cast<bf16x8 *>(a.qf + keys + at) = qa[ks][i];
+            }
+        }
+    __syncthreads();
+    // K K^T and Q K^T, the wave's rows of them.
+    f32x4 u[4] = {}, w[4] = {};
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+        if (busy && n <= wave)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                bf16x8 kb[NP];
+                load_frags<NP>(skf + ((n * KS + ks) * NP) * kFrag + lane * 8, kb);
+                u[n] = mm<NP, NP>(ka[ks], kb, u[n]);
+                w[n] = mm<NP, NP>(qa[ks], kb, w[n]);
+            }
+    // K^T (and Q^T) as rows: element (d, token) from K's fragments.
+    const auto transpose = [&](const uint16_t *from, uint16_t *to) {
+        for (int i = wave; i < 2 * KS * 2; i += 4) {
+            const int rt = i / 2, ks = i % 2, d = rt * 16 + r;
+            if (ks * 32 >= c.len) continue;
+            const int at = ((d / 32) * NP) * kFrag + (d % 32 / 8) * 16 * 8 + d % 8;      // of row block 0, token 0
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+                u16x8 v;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int t = ks * 32 + g * 8 + e;
+                    v[e] = from[at + (t / 16) * KS * NP * kFrag + p * kFrag + (t % 16) * 8];
+                }
+                *reinterpret_cast<u16x8 *>(to + keys + (i * NP + p) * kFrag + lane * 8) = v;
+            }
+        }
+    };
+    if (first) transpose(skf, a.kt);
+    if constexpr (BWD)
+        if (first) transpose(sqf, a.qt);
+    __syncthreads();                                    // K's fragments have been read
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const int col = n * 16 + r;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int t = wave * 16 + g * 4 + j;
+            const float d = busy && n <= wave && col <= t ? expf((float)(cs[t] - cs[col])) : 0.f;
+            y[t * kLd + col] = col <= t ? d * w[n][j] * a.scale : 0.f;
+            x[t * kLd + col] = col < t ? beta[BWD ? t : col] * d * u[n][j] : 0.f;
+        }
+    }
+    __syncthreads();
+    // A triangular matrix's pieces into fragments, a lane's eight columns of a row
+    // (BWD: of the transpose).
+    const auto pieces = [&](auto n_, const float *m, uint16_t *to, int start, int stride) {
+        constexpr int M = decltype(n_)::value;
+        for (int i = start; i < kTri; i += stride) {
+            const int rb = BWD ? (i < 4 ? i / 2 : i - 2) : i < 2 ? i : i / 2 + 1, ks = BWD ? (i < 4 ? i & 1 : 1) : i < 2 ? 0 : i & 1;
+            if (rb >= blocks || ks * 32 >= c.len) continue;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[e] = BWD ? m[(ks * 32 + g * 8 + e) * kLd + rb * 16 + r] : m[(rb * 16 + r) * kLd + ks * 32 + g * 8 + e];
+            uint32_t q[4][M];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split_pair<M>(v[2 * e], v[2 * e + 1], q[e]);
+#pragma unroll
+            for (int o = 0; o < M; ++o)
+                *reinterpret_cast<u32x4 *>(to + (ch * kTri + i) * M * kFrag + o * kFrag + lane * 8) =
+                    u32x4{q[0][o], q[1][o], q[2][o], q[3][o]};
+        }
+    };
+    if (wave == 0) {                                    // the diagonal blocks, one a quarter wave
+        const float *d = x + g * 16 * kLd + g * 16;
+        float col[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float s = i == r ? 1.f : 0.f;
+#pragma unroll
+            for (int l = 0; l < i; l += 4) {
+                const f32x4 v = *reinterpret_cast<const f32x4 *>(d + i * kLd + l);
+#pragma unroll
+                for (int o = 0; o < 4; ++o)
+                    if (l + o < i) s = fmaf(-v[o], col[l + o], s);
+            }
+            col[i] = s;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[(g * 16 + i) * kLd + g * 16 + r] = col[i];
+    } else {
+        pieces(std::integral_constant<int, NPP>{}, y, a.pf, wave - 1, 3);      // P meanwhile
+    }
+    __syncthreads();
+    const auto put = [&](float *to, f32x4 v, float sign) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[(g * 4 + j) * kLd + r] = sign * v[j];
+    };
+    // The 32s: -X11 (A10 X00) for the pairs (0, 1) and (2, 3), a wave each.
+    if (blocks > 1) {
+        if (wave < 2) {
+            float *b = x + wave * 32 * kLd + wave * 32, *l = b + 16 * kLd;
+            const f32x4 t = tile_mm(16, [&](int i, int k) { return l[i * kLd + k]; },
+                                    [&](int k, int j) { return b[k * kLd + j]; }, f32x4{});
+            put(y + wave * 16 * kLd, t, 1.f);           // y's first rows: P is out of them
+            const f32x4 v = tile_mm(16, [&](int i, int k) { return l[i * kLd + 16 + k]; },
+                                    [&](int k, int j) { return y[(wave * 16 + k) * kLd + j]; }, f32x4{});
+            put(l, v, -1.f);
+        }
+        __syncthreads();
+    }
+    // The 64: -X22 (A21 X11), a 16 x 16 tile a wave.
+    if (blocks > 2) {
+        const int ti = wave / 2 * 16, tj = wave % 2 * 16;
+        float *l = x + 32 * kLd;
+        const f32x4 t = tile_mm(32, [&](int i, int k) { return l[(ti + i) * kLd + k]; },
+                                [&](int k, int j) { return x[k * kLd + tj + j]; }, f32x4{});
+        put(y + ti * kLd + tj, t, 1.f);
+        __syncthreads();
+        const f32x4 v = tile_mm(32, [&](int i, int k) { return l[(ti + i) * kLd + 32 + k]; },
+                                [&](int k, int j) { return y[k * kLd + tj + j]; }, f32x4{});
+        put(l + ti * kLd + tj, v, -1.f);
+        __syncthreads();
+    }
+    pieces(std::integral_constant<int, 3>{}, x, a.mf, wave, 4);
+}
+
+template <class T, int KS, bool BWD>
+hipError_t launch_operands(const DeltaArgs &a, hipStream_t s) {
+    constexpr int NP = sizeof(T) == 2 ? 1 : 3;
+    constexpr size_t tile = sizeof(float) * kC * kLd, frags = (BWD ? 2 : 1) * 2 * 4 * KS * NP * kFrag;
+    constexpr size_t bytes = tile + (frags > tile ? frags : tile);
+    const auto even = [&](const void *p, int64_t stride) {
+        return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * sizeof(T) % 16 == 0;
+    };
+    const bool vec = a.dk % 8 == 0 && even(a.q, a.qs) && even(a.k, a.ks);
+    auto *kernel = vec ? k_delta_operands<T, KS, true, BWD> : k_delta_operands<T, KS, false, BWD>;
+    if (hipError_t e = allow_lds(kernel, bytes)) return e;
+    kernel<<<dim3((int)delta_chunk_slots(a.tokens, a.n), a.hv), 256, bytes, s>>>(a);
+    return hipGetLastError();
+}
 
 }  // namespace ops
 }  // namespace rn

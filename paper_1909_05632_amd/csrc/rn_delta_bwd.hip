@@ -1,17 +1,17 @@
 // Gradients of the gated delta rule over whole sequences.
 //
 // With the chunk quantities of rn_delta.hip (S and S' the memories before and
-// after a chunk, M = I + A, P, c) and dS' = dJ/dS':
-//   dV' = P^T dO + (e^(c64 - c) K) dS',      dR = M^-T dV'    (R = beta (V - e^c K S)),
-//   dS  = e^(c64) dS' + (scale e^c Q)^T dO - (beta e^c K)^T dR:
-// k_delta_bwd_walk takes the chunks of a sequence from the last to the first,
-// 16 columns of S a block, and leaves dS' and dR.  Then every chunk by itself
-// (k_delta_bwd_chunk), with dP = dO V'^T, dA = -dR V'^T and e = c_i - c_j:
-//   dv = beta dR,
-//   dq = scale (e^c dO S^T + (dP e^e) K),
-//   dk = [-beta e^c dR S^T + (beta dA e^e) K]  (k as the row: reads)
-//      + [e^(c64 - c) V' dS'^T + (dP e^e)^T scale Q + (beta dA e^e)^T K]  (as the column: writes),
-//   dbeta_i = sum dR (V - e^c K S) + sum_j dA_ij A_ij / beta_i,
+// after a chunk, E the errors, V' = beta E, P, c), M = I + A for
+// A_ij = beta_i e^(ci - cj) k_i . k_j, and dS' = dJ/dS':
+//   dV' = M^-T (P^T dO + (e^(c64 - c) K) dS'),
+//   dS  = e^(c64) dS' + (scale e^c Q)^T dO - (beta e^c K)^T dV':
+// k_delta_bwd_walk takes the chunks of a sequence from the last to the first and
+// leaves dS' and dV'.  Then every chunk by itself (k_delta_bwd_chunk), with
+// dP = dO V'^T, dL = -beta dV' V'^T and e = e^(ci - cj) for j <= i:
+//   dv = beta dV',  dbeta_i = dV'_i . E_i,
+//   dq = scale (e^c dO S^T + (dP e) K),
+//   dk = [-beta e^c dV' S^T + (dL e) K]                        (reads: k_i as the row)
+//      + [e^(c64 - c) V' dS'^T + scale (dP e)^T Q + (dL e)^T K]  (writes: k_j as the column),
 //   dc_i = q_i . dq_i + k_i . dk_i(reads) - k_i . dk_i(writes): every term of
 //     these products holds e^(c_i) or e^(-c_i) once,
 //   dc_64 also has sum_i e^(c64 - ci) k_i . (V' dS'^T)_i + e^(c64) <S, dS'>,
@@ -23,117 +23,265 @@ namespace {
 
 using namespace ops;
 
-constexpr int kLd = kC + 4;
-constexpr int kLdV = kVT + 1;
-
-template <class T>
-__global__ __launch_bounds__(256) void k_delta_bwd_walk(DeltaArgs a) {
-    extern __shared__ float lds[];
-    const int kp = (a.dk + 15) / 16 * 16, ld = kp + 4;
-    float *sk = lds, *sq = sk + kC * ld, *m = sq + kC * ld, *p = m + kC * kLd;
-    float *dS = p + kC * kLd, *w = dS + kp * kLdV, *od = w + kC * kLdV;
-    __shared__ double cs[kC];
-    __shared__ float beta[kC];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+// Laid out as the forward walk: 16 CT columns a block, wave w the tokens
+// 16 w .. + 15 and the gradient's row tiles w, w + 4, which stay in registers in
+// float32 and go through LDS as planes, as do dO, scale e^c dO, the right side of
+// the triangular system and -beta e^c dV'.
+template <class T, int KS, int CT>
+__global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delta_bwd_walk(DeltaArgs a) {
+    constexpr int NP = sizeof(T) == 2 ? 1 : 3;
+    constexpr int KP = KS * 32, RT = KP > 64 ? KP / 64 : 1;        // row tiles of the gradient a wave owns
+    constexpr int VT = 16 * CT, ldS = KP + 8, ldT = kC + 8;
+    constexpr int kKeys = 4 * KS * NP * kFrag;
+    __shared__ __align__(16) uint16_t sS[3 * VT * ldS], sO[NP * VT * ldT], sG[3 * VT * ldT], sX[3 * VT * ldT], sL[3 * VT * ldT];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int seq = blockIdx.x / a.hv, h = blockIdx.x % a.hv, hk = h / (a.hv / a.hk);
-    const int v0 = blockIdx.y * kVT;
+    const int v0 = blockIdx.y * VT;
     const Span span = span_of(a, seq);
-    const int64_t sbase = ((int64_t)seq * a.hv + h) * a.dk * a.dv;
-    for (int i = threadIdx.x; i < kp * kVT; i += 256) {
-        const int d = i / kVT, v = i % kVT;
-        dS[d * kLdV + v] = a.dfinal && d < a.dk && v0 + v < a.dv ? a.dfinal[sbase + d * a.dv + v0 + v] : 0.f;
-    }
-    const int r0 = wave * 16, row4 = r0 + (lane >> 4) * 4, colv = lane & 15;
-    for (int chunk = (span.len + kC - 1) / kC - 1; chunk >= 0; --chunk) {
-        const int at = chunk * kC;
-        const Chunk c{seq, span.begin + at, min(kC, span.len - at)};
-        const int64_t ch = (int64_t)slot_of(span, seq, chunk) * a.hv + h;
-        __syncthreads();
-        if (wave == 0) {
-            cs[lane] = decay_sums(a, c, h);
-            beta[lane] = lane < c.len ? a.beta[(int64_t)(c.begin + lane) * a.hv + h] : 0.f;
-        }
-        for (int i = threadIdx.x; i < kC * kp; i += 256) {
-            const int t = i / kp, d = i % kp;
-            const bool in = t < c.len && d < a.dk;
-            sk[t * ld + d] = in ? load<T>(a.k, (c.begin + t) * a.ks + hk * a.dk + d) : 0.f;
-            sq[t * ld + d] = in ? load<T>(a.q, (c.begin + t) * a.qs + hk * a.dk + d) * a.scale : 0.f;
-        }
-        for (int i = threadIdx.x; i < kC * kC; i += 256) {
-            m[i / kC * kLd + i % kC] = a.inv[ch * kC * kC + i];
-            p[i / kC * kLd + i % kC] = a.score[ch * kC * kC + i];
-        }
-        for (int i = threadIdx.x; i < kC * kVT; i += 256) {
-            const int t = i / kVT, v = i % kVT;
-            const bool in = t < c.len && v0 + v < a.dv;
-            od[t * kLdV + v] = in ? load<T>(a.dout, ((int64_t)(c.begin + t) * a.hv + h) * a.dv + v0 + v) : 0.f;
-        }
-        for (int i = threadIdx.x; i < a.dk * kVT; i += 256) {
-            const int d = i / kVT, v = i % kVT;
-            if (v0 + v < a.dv) a.after[(ch * a.dk + d) * a.dv + v0 + v] = dS[d * kLdV + v];
-        }
-        __syncthreads();
-        const double last = cs[kC - 1];
-        const auto ob = [&](int k, int j) { return od[k * kLdV + j]; };
-        const auto wb = [&](int k, int j) { return w[k * kLdV + j]; };
-        f32x4 x = tile_mm(kp, [&](int i, int k) { return sk[(r0 + i) * ld + k]; },
-                          [&](int k, int j) { return dS[k * kLdV + j]; }, f32x4{});
+    const int chunks = (span.len + kC - 1) / kC;
+    const int64_t slot0 = slot_of(span, seq, 0);
+    const int64_t sbase = ((int64_t)seq * a.hv + h) * a.dk * a.dv + v0;
+    const bool owner = KP >= 64 || wave * 16 < KP;
+    bool col_in[CT];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] *= expf((float)(last - cs[row4 + j]));
-        x = tile_mm(kC, [&](int i, int k) { return p[k * kLd + r0 + i]; }, ob, x);
+    for (int n = 0; n < CT; ++n) col_in[n] = v0 + n * 16 + (int)r < a.dv;
+
+    f32x4 S[RT][CT];                                    // the gradient of the memory
+    const auto put_state = [&] {
+        if (owner)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[(row4 + j) * kLdV + colv] = x[j];
-        __syncthreads();
-        x = tile_mm(kC, [&](int i, int k) { return m[k * kLd + r0 + i]; }, wb, f32x4{});
-        __syncthreads();
+            for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int t = row4 + j;
-            w[t * kLdV + colv] = x[j];
-            if (t < c.len && v0 + colv < a.dv)
-                a.dwrite[((int64_t)(c.begin + t) * a.hv + h) * a.dv + v0 + colv] = x[j];
-        }
-        __syncthreads();
-        const float whole = expf((float)last);
-        for (int d0 = wave * 16; d0 < kp; d0 += 64) {
-            f32x4 y = tile_mm(kC, [&](int i, int k) { return sq[k * ld + d0 + i] * expf((float)cs[k]); }, ob, f32x4{});
-            y = tile_mm(kC, [&](int i, int k) { return -beta[k] * expf((float)cs[k]) * sk[k * ld + d0 + i]; }, wb, y);
+                for (int n = 0; n < CT; ++n)
+                    put4<3>(sS, VT * ldS, (n * 16 + r) * ldS + (wave + 4 * i) * 16 + g * 4, S[i][n]);
+    };
+    const auto write_state = [&](float *to) {                       // to: [dk][dv] from column v0
+        if (!owner) return;
+        const __amdgpu_buffer_rsrc_t rs = rsrc_of(to);
+        const uint32_t at = (wave * 16 + g * 4) * a.dv + r;
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int n = 0; n < CT; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    store_if(col_in[n] && (wave + 4 * i) * 16 + (int)g * 4 + j < a.dk, rs,
+                             4 * (at + (64 * i + j) * a.dv + n * 16), (float)S[i][n][j]);
+    };
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int n = 0; n < CT; ++n)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                float &s = dS[(d0 + (lane >> 4) * 4 + j) * kLdV + colv];
-                s = fmaf(whole, s, y[j]);
+                const int d = (wave + 4 * i) * 16 + g * 4 + j;
+                const bool in = a.dfinal && owner && d < a.dk && col_in[n];
+                S[i][n][j] = in ? a.dfinal[sbase + (int64_t)d * a.dv + n * 16 + r] : 0.f;
             }
+
+    // Loads are unconditional, as in the forward walk.
+    bf16x8 kf[KS][NP], kt[RT][2][NP], qt[RT][2][NP], mf[2][3], pf[2][3];
+    T od[CT][4];
+    const auto load_k = [&](int64_t slot) {
+        const int64_t at = (slot * a.hk + hk) * kKeys + wave * KS * NP * kFrag;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) load_frags<NP>(a.kf + at + (lane * 8 + ks * NP * kFrag), kf[ks]);
+    };
+    const auto load_kq = [&](int64_t slot) {
+        const int64_t at = (slot * a.hk + hk) * kKeys + (wave % (2 * KS)) * 2 * NP * kFrag;
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                load_frags<NP>(a.kt + at + (lane * 8 + (8 * i + ks) * NP * kFrag), kt[i][ks]);
+                load_frags<NP>(a.qt + at + (lane * 8 + (8 * i + ks) * NP * kFrag), qt[i][ks]);
+            }
+    };
+    const auto load_tri = [&](const uint16_t *p, int64_t slot, bf16x8 (&f)[2][3]) {
+        const uint16_t *at = p + (slot * a.hv + h) * kTri * 3 * kFrag;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+            load_frags<3>(at + tri_t(wave, wave < 2 ? ks : 1) * 3 * kFrag + lane * 8, f[ks]);
+    };
+    f32x4 grown{}, left{}, beta{}, next_grown{}, next_left{}, next_beta{};
+    float whole = 0.f, next_whole = 0.f;
+    const auto load_decays = [&](int64_t slot) {
+        const float *d = a.dec + (slot * a.hv + h) * 3 * kC + wave * 16;
+        next_grown = *reinterpret_cast<const f32x4 *>(d + g * 4);
+        next_left = *reinterpret_cast<const f32x4 *>(d + (kC + g * 4));
+        next_beta = *reinterpret_cast<const f32x4 *>(d + (2 * kC + g * 4));
+        next_whole = a.dec[(slot * a.hv + h) * 3 * kC + kC - 1];
+    };
+    uint32_t col[CT];
+#pragma unroll
+    for (int n = 0; n < CT; ++n) col[n] = min(n * 16 + (int)r, a.dv - 1 - v0);
+    const uint32_t ooff = (wave * 16 + g * 4) * (uint32_t)(a.hv * a.dv) + r;
+    const auto load_o = [&](int chunk) {
+        const T *base = static_cast<const T *>(a.dout) + ((int64_t)(span.begin + chunk * kC) * a.hv + h) * a.dv + v0;
+        const int last = span.len - chunk * kC - 1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t t = min(wave * 16 + (int)g * 4 + j, last) * (uint32_t)(a.hv * a.dv);
+#pragma unroll
+            for (int n = 0; n < CT; ++n) od[n][j] = base[t + col[n]];
         }
+    };
+    if (chunks > 0) {
+        const int64_t slot = slot0 + chunks - 1;
+        load_decays(slot), load_o(chunks - 1), load_k(slot), load_tri(a.pf, slot, pf), load_tri(a.mf, slot, mf), load_kq(slot);
     }
-    __syncthreads();
-    if (a.dstate)
-        for (int i = threadIdx.x; i < a.dk * kVT; i += 256) {
-            const int d = i / kVT, v = i % kVT;
-            if (v0 + v < a.dv) a.dstate[sbase + d * a.dv + v0 + v] = dS[d * kLdV + v];
+    put_state();
+
+    const auto step = [&](int chunk, auto more_) {
+        constexpr bool more = decltype(more_)::value;   // a chunk comes before this one
+        const int64_t next = slot0 + chunk - 1, ch = (slot0 + chunk) * a.hv + h;
+        const int len = min(kC, span.len - chunk * kC);
+        const bool busy = wave * 16 < len;              // any token of this wave
+        const bool half2 = len > 32;                    // tokens in the second 32
+        grown = next_grown, left = next_left, beta = next_beta, whole = next_whole;
+        write_state(a.after + ch * a.dk * a.dv + v0);
+        f32x4 o[CT];
+#pragma unroll
+        for (int n = 0; n < CT; ++n) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[n][j] = wave * 16 + (int)g * 4 + j < len ? to_float(od[n][j]) : 0.f;
+            put4<NP>(sO, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, o[n]);
         }
+        dev::lds_barrier();                             // planes of dS' and dO are there
+        f32x4 x[CT];
+#pragma unroll
+        for (int n = 0; n < CT; ++n) {
+            x[n] = f32x4{};
+            if (busy) {
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    bf16x8 s[3];
+                    get8<3>(sS, VT * ldS, (n * 16 + r) * ldS + ks * 32 + g * 8, s);
+                    x[n] = mm<NP, 3>(kf[ks], s, x[n]);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[n][j] *= left[j];
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    if (wave < 2 ? ks == 0 || half2 : ks == 1) {
+                        bf16x8 b[NP];
+                        get8<NP>(sO, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
+                        x[n] = mm<3, NP>(pf[ks], b, x[n]);
+                    }
+            }
+            put4<3>(sX, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, x[n]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[n][j] *= grown[j] * a.scale;
+            put4<3>(sG, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, o[n]);
+        }
+        if constexpr (more) load_decays(next), load_o(chunk - 1), load_k(next), load_tri(a.pf, next, pf);
+        dev::lds_barrier();
+        const __amdgpu_buffer_rsrc_t rs = rsrc_of(a.dwrite + ((int64_t)(span.begin + chunk * kC) * a.hv + h) * a.dv + v0);
+#pragma unroll
+        for (int n = 0; n < CT; ++n) {
+            f32x4 w{};
+            if (busy)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    if (wave < 2 ? ks == 0 || half2 : ks == 1) {
+                        bf16x8 b[3];
+                        get8<3>(sX, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
+                        w = mm<3, 3>(mf[ks], b, w);
+                    }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                store_if(col_in[n] && wave * 16 + (int)g * 4 + j < len, rs, 4 * (ooff + j * a.hv * a.dv + n * 16), (float)w[j]);
+                w[j] *= -beta[j] * grown[j];
+            }
+            put4<3>(sL, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
+        }
+        if constexpr (more) load_tri(a.mf, next, mf);
+        dev::lds_barrier();
+        if (owner)
+#pragma unroll
+            for (int n = 0; n < CT; ++n) {
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) S[i][n][j] *= whole;
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+                    if (ks == 0 || half2) {
+                        bf16x8 b[3], c[3];
+                        get8<3>(sG, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
+                        get8<3>(sL, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, c);
+#pragma unroll
+                        for (int i = 0; i < RT; ++i) {
+                            S[i][n] = mm<NP, 3>(qt[i][ks], b, S[i][n]);
+                            S[i][n] = mm<NP, 3>(kt[i][ks], c, S[i][n]);
+                        }
+                    }
+            }
+        if constexpr (more) {
+            put_state();                                // every wave is past its reads of the planes
+            load_kq(next);
+        }
+    };
+    for (int chunk = chunks - 1; chunk > 0; --chunk) step(chunk, std::true_type{});
+    if (chunks > 0) step(0, std::false_type{});
+    if (a.dstate) write_state(a.dstate + sbase);
+}
+
+// ------------------------------------------------------------------ a chunk by itself
+
+// Eight consecutive elements of a row of `count`, zeros where there are none.
+template <class T, bool VEC>
+__device__ inline void load8(const T *p, bool in, int from, int count, float (&v)[8]) {
+    if constexpr (VEC) {                                // count a multiple of 8, rows on 16 bytes
+        constexpr int PER = 16 / sizeof(T);
+#pragma unroll
+        for (int e = 0; e < 8; e += PER) {
+            Pack<T, PER> q{};
+            if (in && from < count) q = *reinterpret_cast<const Pack<T, PER> *>(p + from + e);
+#pragma unroll
+            for (int o = 0; o < PER; ++o) v[e + o] = to_float(q.v[o]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = in && from + e < count ? to_float(p[from + e]) : 0.f;
+    }
+}
+template <int N>
+__device__ inline void planes8(const float (&v)[8], bf16x8 (&f)[N]) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    uint32_t w[4][N];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) split_pair<N>(v[2 * e], v[2 * e + 1], w[e]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = __builtin_bit_cast(bf16x8, u32x4{w[0][i], w[1][i], w[2][i], w[3][i]});
 }
 
 // A block takes a chunk slot and a key head and adds the value heads that share
-// it; a wave owns 16 tokens.  KT: 16-wide tiles of dk that a wave's registers hold.
-template <class T, int KT>
-__global__ __launch_bounds__(256) void k_delta_bwd_chunk(DeltaArgs a) {
-    extern __shared__ float lds[];
-    constexpr int kp = KT * 16, ld = kp + 4;
-    float *sk = lds, *sq = sk + kC * ld, *m = sq + kC * ld, *x = m + kC * kLd, *y = x + kC * kLd;
-    float *S = y + kC * kLd, *dS = S + kp * kLdV, *od = dS + kp * kLdV, *dr = od + kC * kLdV, *w = dr + kC * kLdV;
+// it; a wave owns 16 tokens, with dq, dk(reads) and dk(writes) of them in its
+// registers.  All big products sum over the values, 32 at a time: rows of dO,
+// dV', E, S and dS' are operands as they lie in memory.  The waves split S, dS'
+// and V' into planes once for all, through LDS; what is left of a block's time
+// is the matrix ops and those planes' reads.
+template <class T, int KS, bool VEC>
+__global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaArgs a) {
+    constexpr int NP = sizeof(T) == 2 ? 1 : 3, KT = 2 * KS;
+    constexpr int kKeys = 4 * KS * NP * kFrag;
+    constexpr int kStep = (2 * KT + 4) * 3 * kFrag * 2, kPairs = 2 * kC * kLd * 4;       // bytes of the two uses
+    __shared__ __align__(16) char lds[kStep > kPairs ? kStep : kPairs];
+    uint16_t *fS = reinterpret_cast<uint16_t *>(lds), *fD = fS + KT * 3 * kFrag, *fV = fD + KT * 3 * kFrag;
+    float *x = reinterpret_cast<float *>(lds), *y = x + kC * kLd;   // [i][j] of dP e and dL e
     __shared__ double cs[kC];
-    __shared__ float beta[kC], dc[kC], extra[4];
+    __shared__ float beta_s[kC], dc[kC], extra[4];
     const int slot = blockIdx.x, hk = blockIdx.y, group = a.hv / a.hk;
     const Chunk c = chunk_of(a, slot);
     if (c.len == 0) return;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int r0 = wave * 16, row4 = r0 + (lane >> 4) * 4, col = lane & 15;
-    for (int i = threadIdx.x; i < kC * kp; i += 256) {
-        const int t = i / kp, d = i % kp;
-        const bool in = t < c.len && d < a.dk;
-        sk[t * ld + d] = in ? load<T>(a.k, (c.begin + t) * a.ks + hk * a.dk + d) : 0.f;
-        sq[t * ld + d] = in ? load<T>(a.q, (c.begin + t) * a.qs + hk * a.dk + d) * a.scale : 0.f;
-    }
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int blocks = (c.len + 15) / 16, half = (c.len + 31) / 32;
+    const bool busy = wave < blocks;
+    const int token = wave * 16 + r;                    // as an operand's row
+    const int row4 = wave * 16 + g * 4;                 // as a result's rows
+    const int64_t keys = ((int64_t)slot * a.hk + hk) * kKeys;
     // Sum over the 16 lanes that hold a row's columns.
     const auto across = [&](float v) {
 #pragma unroll
@@ -148,102 +296,132 @@ __global__ __launch_bounds__(256) void k_delta_bwd_chunk(DeltaArgs a) {
         __syncthreads();
         if (wave == 0) {
             cs[lane] = decay_sums(a, c, h);
-            beta[lane] = lane < c.len ? a.beta[(int64_t)(c.begin + lane) * a.hv + h] : 0.f;
+            beta_s[lane] = lane < c.len ? a.beta[(int64_t)(c.begin + lane) * a.hv + h] : 0.f;
         }
-        for (int i = threadIdx.x; i < kC * kC; i += 256) m[i / kC * kLd + i % kC] = a.inv[ch * kC * kC + i];
-        f32x4 gq[KT], gr[KT], gw[KT], dp[4], da[4];
+        __syncthreads();
+        f32x4 gq[KT], gr[KT], gw[KT], dp[4], dl[4];
 #pragma unroll
         for (int n = 0; n < KT; ++n) gq[n] = gr[n] = gw[n] = f32x4{};
 #pragma unroll
-        for (int n = 0; n < 4; ++n) dp[n] = da[n] = f32x4{};
-        float db[4] = {0.f, 0.f, 0.f, 0.f}, dot = 0.f;
-        for (int v0 = 0; v0 < a.dv; v0 += kVT) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < kp * kVT; i += 256) {
-                const int d = i / kVT, v = i % kVT;
-                const bool in = d < a.dk && v0 + v < a.dv;
-                const int64_t at = (ch * a.dk + d) * a.dv + v0 + v;
-                const float s = in ? a.before[at] : 0.f, t = in ? a.after[at] : 0.f;
-                S[d * kLdV + v] = s;
-                dS[d * kLdV + v] = t;
-                dot = fmaf(s, t, dot);
-            }
-            for (int i = threadIdx.x; i < kC * kVT; i += 256) {
-                const int t = i / kVT, v = i % kVT;
-                const bool in = t < c.len && v0 + v < a.dv;
-                const int64_t at = ((int64_t)(c.begin + t) * a.hv + h) * a.dv + v0 + v;
-                od[t * kLdV + v] = in ? load<T>(a.dout, at) : 0.f;
-                dr[t * kLdV + v] = in ? a.dwrite[at] : 0.f;
-            }
-            __syncthreads();
-            const f32x4 held = tile_mm(kp, [&](int i, int k) { return sk[(r0 + i) * ld + k]; },
-                                       [&](int k, int j) { return S[k * kLdV + j]; }, f32x4{});
+        for (int n = 0; n < 4; ++n) dp[n] = dl[n] = f32x4{};
+        float db = 0.f, dot = 0.f;
+        const float b = beta_s[token];
+        const int64_t row = ((int64_t)(c.begin + token) * a.hv + h) * a.dv;
+        const bool in = token < c.len;
+        for (int v0 = 0; v0 < a.dv; v0 += 32) {
+            const int v = v0 + g * 8;
+            // S and dS', two or fewer of their row tiles a wave
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int t = row4 + j;
-                const bool in = t < c.len && v0 + col < a.dv;
-                const float v = in ? load<T>(a.v, (c.begin + t) * a.vs + (int64_t)h * a.dv + v0 + col) : 0.f;
-                const float gap = v - expf((float)cs[t]) * held[j], g = dr[t * kLdV + col];
-                db[j] += across(g * gap);
-                w[t * kLdV + col] = beta[t] * gap;
-                if (in)
-                    static_cast<T *>(a.dval)[((int64_t)(c.begin + t) * a.hv + h) * a.dv + v0 + col] =
-                        from_float<T>(beta[t] * g);
+            for (int i = 0; i < (KT + 3) / 4; ++i) {
+                const int n = wave + 4 * i, d = n * 16 + r;
+                if (KT % 4 == 0 || n < KT) {
+                    float s[8], t[8];
+                    load8<float, VEC>(a.before + (ch * a.dk + d) * a.dv, d < a.dk, v, a.dv, s);
+                    load8<float, VEC>(a.after + (ch * a.dk + d) * a.dv, d < a.dk, v, a.dv, t);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dot = fmaf(s[e], t[e], dot);
+                    bf16x8 f[3];
+                    planes8<3>(s, f);
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8 *>(fS + (n * 3 + p) * kFrag + lane * 8) = f[p];
+                    planes8<3>(t, f);
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8 *>(fD + (n * 3 + p) * kFrag + lane * 8) = f[p];
+                }
+            }
+            bf16x8 fo[NP], fr[3], fv[3];
+            if (busy) {
+                float o[8], w[8], e[8];
+                load8<T, VEC>(static_cast<const T *>(a.dout) + row, in, v, a.dv, o);
+                load8<float, VEC>(a.dwrite + row, in, v, a.dv, w);
+                load8<float, VEC>(a.err + row, in, v, a.dv, e);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    db = fmaf(w[i], e[i], db);
+                    e[i] *= b;
+                    w[i] *= b;
+                }
+                planes8<NP>(o, fo);
+                planes8<3>(w, fr);                      // beta dV', which is dv
+                planes8<3>(e, fv);                      // V'
+                T *dv = static_cast<T *>(a.dval) + row;
+                if (in) {
+                    if constexpr (VEC) {
+                        constexpr int PER = 16 / sizeof(T);
+#pragma unroll
+                        for (int i = 0; i < 8; i += PER) {
+                            Pack<T, PER> q;
+#pragma unroll
+                            for (int j = 0; j < PER; ++j) q.v[j] = from_float<T>(w[i + j]);
+                            if (v < a.dv) *reinterpret_cast<Pack<T, PER> *>(dv + v + i) = q;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (v + i < a.dv) dv[v + i] = from_float<T>(w[i]);
+                    }
+                }
+#pragma unroll
+                for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8 *>(fV + (wave * 3 + p) * kFrag + lane * 8) = fv[p];
             }
             __syncthreads();
-            const f32x4 nv = tile_mm(r0 + 16, [&](int i, int k) { return m[(r0 + i) * kLd + k]; },
-                                     [&](int k, int j) { return w[k * kLdV + j]; }, f32x4{});
-            __syncthreads();
+            if (busy) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[(row4 + j) * kLdV + col] = nv[j];
-            __syncthreads();
-            const auto oa = [&](int i, int k) { return od[(r0 + i) * kLdV + k]; };
-            const auto ra = [&](int i, int k) { return dr[(r0 + i) * kLdV + k]; };
-            const auto wa = [&](int i, int k) { return w[(r0 + i) * kLdV + k]; };
+                for (int n = 0; n < 4; ++n)
+                    if (n <= wave) {
+                        bf16x8 f[3];
+                        load_frags<3>(fV + n * 3 * kFrag + lane * 8, f);
+                        dp[n] = mm<NP, 3>(fo, f, dp[n]);
+                        dl[n] = mm<3, 3>(fr, f, dl[n]);
+                    }
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const auto wt = [&](int k, int j) { return w[(n * 16 + j) * kLdV + k]; };
-                dp[n] = tile_mm(kVT, oa, wt, dp[n]);
-                da[n] = tile_mm(kVT, ra, wt, da[n]);
+                for (int n = 0; n < KT; ++n) {
+                    bf16x8 f[3];
+                    load_frags<3>(fS + n * 3 * kFrag + lane * 8, f);
+                    gq[n] = mm<NP, 3>(fo, f, gq[n]);
+                    gr[n] = mm<3, 3>(fr, f, gr[n]);
+                    load_frags<3>(fD + n * 3 * kFrag + lane * 8, f);
+                    gw[n] = mm<3, 3>(fv, f, gw[n]);
+                }
             }
-#pragma unroll
-            for (int n = 0; n < KT; ++n) {
-                const auto st = [&](int k, int j) { return S[(n * 16 + j) * kLdV + k]; };
-                const auto dt = [&](int k, int j) { return dS[(n * 16 + j) * kLdV + k]; };
-                gq[n] = tile_mm(kVT, oa, st, gq[n]);
-                gr[n] = tile_mm(kVT, ra, st, gr[n]);
-                gw[n] = tile_mm(kVT, wa, dt, gw[n]);
-            }
+            __syncthreads();
         }
+        // dbeta: a row's four lanes
+        db += __shfl_xor(db, 16);
+        db += __shfl_xor(db, 32);
+        if (g == 0 && in) a.dbeta[(int64_t)(c.begin + token) * a.hv + h] = db;
         const double last = cs[kC - 1];
-        // k_i . k_j and the pairs' weights; dbeta's share of A.
+        // the pairs' weights
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            const f32x4 kk = tile_mm(kp, [&](int i, int k) { return sk[(r0 + i) * ld + k]; },
-                                     [&](int k, int j) { return sk[(n * 16 + j) * ld + k]; }, f32x4{});
+        for (int n = 0; n < 4; ++n)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int t = row4 + j, u = n * 16 + col;
-                const float d = u <= t ? expf((float)(cs[t] - cs[u])) : 0.f;
-                const float pa = u < t ? -da[n][j] * d : 0.f;
-                x[t * kLd + u] = u <= t ? dp[n][j] * d : 0.f;
-                y[t * kLd + u] = beta[t] * pa;
-                db[j] += across(u < t ? pa * kk[j] : 0.f);
+                const int t = row4 + j, u = n * 16 + r;
+                const float d = u <= t && n <= wave ? expf((float)(cs[t] - cs[u])) : 0.f;
+                x[t * kLd + u] = u <= t ? dp[n][j] * d * a.scale : 0.f;
+                y[t * kLd + u] = u < t ? -dl[n][j] * d : 0.f;
             }
-        }
-        // the memory's part of the sums, before the pairs' is added
+        // The memory's part of the sums, before the pairs' is added.  k and q: this
+        // wave's rows of the results' columns.
         float wsum = 0.f;
+        float kr[4][KT], qr[4][KT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int t = row4 + j;
+#pragma unroll
+            for (int n = 0; n < KT; ++n) {
+                const bool there = t < c.len && n * 16 + r < a.dk;
+                kr[j][n] = there ? load<T>(a.k, (int64_t)(c.begin + t) * a.ks + hk * a.dk + n * 16 + r) : 0.f;
+                qr[j][n] = there ? load<T>(a.q, (int64_t)(c.begin + t) * a.qs + hk * a.dk + n * 16 + r) : 0.f;
+            }
             const float grown = expf((float)cs[t]), left = expf((float)(last - cs[t]));
             float s = 0.f;
 #pragma unroll
             for (int n = 0; n < KT; ++n) {
-                gq[n][j] *= grown;
-                gr[n][j] *= -beta[t] * grown;
+                gq[n][j] *= grown * a.scale;
+                gr[n][j] *= -grown;
                 gw[n][j] *= left;
-                s = fmaf(gw[n][j], sk[t * ld + n * 16 + col], s);
+                s = fmaf(gw[n][j], kr[j][n], s);
             }
             wsum += across(s);
         }
@@ -254,31 +432,55 @@ __global__ __launch_bounds__(256) void k_delta_bwd_chunk(DeltaArgs a) {
         for (int s = 1; s < 64; s <<= 1) all += __shfl_xor(all, s);
         if (lane == 0) extra[wave] = all + wsum;
         __syncthreads();
+        if (busy)
 #pragma unroll
-        for (int n = 0; n < KT; ++n) {
-            const auto kb = [&](int k, int j) { return sk[k * ld + n * 16 + j]; };
-            const auto qb = [&](int k, int j) { return sq[k * ld + n * 16 + j]; };
-            gq[n] = tile_mm(r0 + 16, [&](int i, int k) { return x[(r0 + i) * kLd + k]; }, kb, gq[n]);
-            gr[n] = tile_mm(r0 + 16, [&](int i, int k) { return y[(r0 + i) * kLd + k]; }, kb, gr[n]);
-            gw[n] = tile_mm(kC, [&](int i, int k) { return x[k * kLd + r0 + i]; }, qb, gw[n]);
-            gw[n] = tile_mm(kC, [&](int i, int k) { return y[k * kLd + r0 + i]; }, kb, gw[n]);
-        }
+            for (int ks = 0; ks < 2; ++ks)
+                if (ks < half) {
+                    // rows i of dP e and dL e for the reads, columns for the writes
+                    bf16x8 fx[3], fy[3], fxt[3], fyt[3];
+                    const bool lower = ks <= wave / 2, upper = ks >= wave / 2;
+                    float v[8], w[8];
+                    const float *px = x + token * kLd + ks * 32 + g * 8, *py = px + kC * kLd;
+                    if (lower) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = px[e], w[e] = py[e];
+                        planes8<3>(v, fx);
+                        planes8<3>(w, fy);
+                    }
+                    if (upper) {
+                        const float *tx = x + (ks * 32 + g * 8) * kLd + token, *ty = tx + kC * kLd;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = tx[e * kLd], w[e] = ty[e * kLd];
+                        planes8<3>(v, fxt);
+                        planes8<3>(w, fyt);
+                    }
+#pragma unroll
+                    for (int n = 0; n < KT; ++n) {
+                        bf16x8 fk[NP], fq[NP];
+                        load_frags<NP>(a.kt + keys + (n * 2 + ks) * NP * kFrag + lane * 8, fk);
+                        load_frags<NP>(a.qt + keys + (n * 2 + ks) * NP * kFrag + lane * 8, fq);
+                        if (lower) {
+                            gq[n] = mm<3, NP>(fx, fk, gq[n]);
+                            gr[n] = mm<3, NP>(fy, fk, gr[n]);
+                        }
+                        if (upper) {
+                            gw[n] = mm<3, NP>(fxt, fq, gw[n]);
+                            gw[n] = mm<3, NP>(fyt, fk, gw[n]);
+                        }
+                    }
+                }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int t = row4 + j;
             float s = 0.f;
 #pragma unroll
             for (int n = 0; n < KT; ++n) {
-                s = fmaf(gq[n][j], sq[t * ld + n * 16 + col], s);
-                s = fmaf(gr[n][j] - gw[n][j], sk[t * ld + n * 16 + col], s);
+                s = fmaf(gq[n][j], qr[j][n], s);
+                s = fmaf(gr[n][j] - gw[n][j], kr[j][n], s);
                 tq[n][j] += gq[n][j];
                 tk[n][j] += gr[n][j] + gw[n][j];
             }
             s = across(s);
-            if (col == 0) {
-                dc[t] = s;
-                if (t < c.len) a.dbeta[(int64_t)(c.begin + t) * a.hv + h] = db[j];
-            }
+            if (r == 0) dc[row4 + j] = s;
         }
         __syncthreads();
         if (wave == 0) {
@@ -299,33 +501,34 @@ __global__ __launch_bounds__(256) void k_delta_bwd_chunk(DeltaArgs a) {
         const int64_t at = ((int64_t)(c.begin + t) * a.hk + hk) * a.dk;
 #pragma unroll
         for (int n = 0; n < KT; ++n)
-            if (n * 16 + col < a.dk) {
-                static_cast<T *>(a.dq)[at + n * 16 + col] = from_float<T>(tq[n][j] * a.scale);
-                static_cast<T *>(a.dkey)[at + n * 16 + col] = from_float<T>(tk[n][j]);
+            if (n * 16 + r < a.dk) {
+                static_cast<T *>(a.dq)[at + n * 16 + r] = from_float<T>(tq[n][j]);
+                static_cast<T *>(a.dkey)[at + n * 16 + r] = from_float<T>(tk[n][j]);
             }
     }
 }
 
-template <class T, int KT>
-hipError_t chunks(const DeltaArgs &a, hipStream_t s) {
-    constexpr int kp = KT * 16;
-    const size_t bytes = sizeof(float) * (2 * kC * (kp + 4) + 3 * kC * kLd + (2 * kp + 3 * kC) * kLdV);
-    if (hipError_t e = allow_lds(k_delta_bwd_chunk<T, KT>, bytes)) return e;
-    k_delta_bwd_chunk<T, KT><<<dim3((int)delta_chunk_slots(a.tokens, a.n), a.hk), 256, bytes, s>>>(a);
+template <class T, int KS>
+hipError_t backward_ks(const DeltaArgs &a, hipStream_t s) {
+    if (a.tokens > 0)
+        if (hipError_t e = launch_operands<T, KS, true>(a, s)) return e;
+    // One column tile a block or two, as in the forward walk.
+    if (a.dv <= 16 || a.n * a.hv * ((a.dv + 31) / 32) <= 256)
+        k_delta_bwd_walk<T, KS, 1><<<dim3(a.n * a.hv, (a.dv + 15) / 16), 256, 0, s>>>(a);
+    else k_delta_bwd_walk<T, KS, 2><<<dim3(a.n * a.hv, (a.dv + 31) / 32), 256, 0, s>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (a.tokens == 0) return hipSuccess;
+    const dim3 grid((int)delta_chunk_slots(a.tokens, a.n), a.hk);
+    const auto even = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+    if (a.dv % 8 == 0 && even(a.dout) && even(a.dval)) k_delta_bwd_chunk<T, KS, true><<<grid, 256, 0, s>>>(a);
+    else k_delta_bwd_chunk<T, KS, false><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
 template <class T>
 hipError_t backward(const DeltaArgs &a, hipStream_t s) {
-    const int kp = (a.dk + 15) / 16 * 16;
-    const size_t bytes = sizeof(float) * (2 * kC * (kp + 4) + 2 * kC * kLd + (kp + 2 * kC) * kLdV);
-    if (hipError_t e = allow_lds(k_delta_bwd_walk<T>, bytes)) return e;
-    k_delta_bwd_walk<T><<<dim3(a.n * a.hv, (a.dv + kVT - 1) / kVT), 256, bytes, s>>>(a);
-    if (hipError_t e = hipGetLastError()) return e;
-    if (a.tokens == 0) return hipSuccess;
-    if (a.dk <= 32) return chunks<T, 2>(a, s);
-    if (a.dk <= 64) return chunks<T, 4>(a, s);
-    return chunks<T, 8>(a, s);
+    const int ks = delta_ksteps(a.dk);
+    return ks == 1 ? backward_ks<T, 1>(a, s) : ks == 2 ? backward_ks<T, 2>(a, s) : backward_ks<T, 4>(a, s);
 }
 
 }  // namespace

@@ -55,20 +55,19 @@ struct DeltaArgs {
     float *final_state;           // last states, or NULL (step: the state pool)
     void *out;
     // Per chunk slot (delta_chunk_slots) and key head, in fragment order (rn_delta.hpp):
-    uint16_t *kf, *qf;            // K and Q as rows
-    uint16_t *kt;                 // K^T as rows
+    uint16_t *kf, *qf;            // K and Q as rows (qf: forward only)
+    uint16_t *kt, *qt;            // K^T and Q^T as rows (qt: backward only)
     // Per chunk slot and value head:
-    uint16_t *mf;                 // (I + A)^-1, three planes
+    uint16_t *mf;                 // the triangular inverse, three planes
     uint16_t *pf;                 // P
     float *dec;                   // [3][64] e^c, e^(c64 - c), beta
-    float *inv;                   // [64][64] (I + A)^-1
-    float *score;                 // [64][64] scale e^(ci - cj) q_i . k_j, j <= i
     float *before;                // [dk][dv] states before the chunk, or NULL (not kept)
+    float *err;                   // [tokens][hv][dv] v - S^T k as each token met it, or NULL
     // Backward call:
     const void *dout;
     const float *dfinal;
     float *after;                 // [slots][hv][dk][dv] gradients of the states after each chunk
-    float *dwrite;                // [tokens][hv][dv] gradients of beta (v - S^T k)
+    float *dwrite;                // [tokens][hv][dv] gradients of what each token wrote, beta err
     void *dq, *dkey, *dval;
     float *dg, *dbeta, *dstate;
 };
@@ -77,7 +76,7 @@ struct DeltaArgs {
 inline int64_t delta_chunk_slots(int64_t tokens, int n) { return tokens / RN_DELTA_CHUNK + n; }
 // 32-wide steps of dk in the chunk kernels (powers of two).
 inline int delta_ksteps(int dk) { return dk <= 32 ? 1 : dk <= 64 ? 2 : 4; }
-// bf16 planes of an input, and of P.
+// bf16 planes of an input, and of P (the backward call has three of P).
 inline int delta_planes(bool bf16) { return bf16 ? 1 : 3; }
 inline int delta_score_planes(bool bf16) { return bf16 ? 2 : 3; }
 hipError_t launch_delta_step(const DeltaArgs &a, bool bf16, hipStream_t s);

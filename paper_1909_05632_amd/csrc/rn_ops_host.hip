@@ -58,14 +58,14 @@ const char *bad_shape(const rn_delta_shape *s) {
 bool too_wide(const rn_delta_shape *s) { return s->dk > RN_DELTA_MAX_DIM || s->dv > RN_DELTA_MAX_DIM; }
 
 struct DeltaSizes {
-    size_t pairs, states, tokens;   // bytes of a [64][64] set, a set of states, [tokens][hv][dv]
-    size_t keys, inverse, score, decay;   // of kf, qf or kt; mf; pf; dec
+    size_t states, tokens;                // bytes of a set of states, of [tokens][hv][dv] float32
+    size_t keys, inverse, score, decay;   // of kf, qf, kt or qt; mf; pf; dec
 };
 
 DeltaSizes sizes(const rn_delta_shape *s) {
     const size_t slots = (size_t)delta_chunk_slots(s->tokens, s->n), heads = s->heads_v;
     const bool bf16 = s->dtype == RN_BF16;
-    return {round_up(slots * heads * RN_DELTA_CHUNK * RN_DELTA_CHUNK * 4), round_up(slots * heads * s->dk * s->dv * 4),
+    return {round_up(slots * heads * s->dk * s->dv * 4),
             round_up((size_t)s->tokens * heads * s->dv * 4),
             round_up(slots * s->heads_k * 4 * delta_ksteps(s->dk) * delta_planes(bf16) * 1024),
             round_up(slots * heads * 6 * 3 * 1024), round_up(slots * heads * 6 * delta_score_planes(bf16) * 1024),
@@ -81,17 +81,6 @@ DeltaArgs delta_args(const rn_delta_shape *s, const void *q, const void *k, cons
     a.qs = s->q_stride, a.ks = s->k_stride, a.vs = s->v_stride;
     a.q = q, a.k = k, a.v = v, a.g = g, a.beta = beta;
     return a;
-}
-
-// The chunk operands' places in a scratch buffer; the first byte after them.
-char *lay_out(DeltaArgs &a, const DeltaSizes &z, char *at) {
-    a.kf = reinterpret_cast<uint16_t *>(at);
-    a.qf = reinterpret_cast<uint16_t *>(at += z.keys);
-    a.kt = reinterpret_cast<uint16_t *>(at += z.keys);
-    a.mf = reinterpret_cast<uint16_t *>(at += z.keys);
-    a.pf = reinterpret_cast<uint16_t *>(at += z.inverse);
-    a.dec = reinterpret_cast<float *>(at += z.score);
-    return at + z.decay;
 }
 
 rn_status check_delta(const rn_delta_shape *s, const void *q, const void *k, const void *v, const float *g,
@@ -191,7 +180,7 @@ rn_status reuse_ops_delta_step(const rn_delta_shape *shape, const void *q, const
 size_t reuse_ops_delta_saved_bytes(const rn_delta_shape *shape) {
     if (bad_shape(shape) || too_wide(shape)) return 0;
     const DeltaSizes z = sizes(shape);
-    return 2 * z.pairs + z.states + kAlign;
+    return z.states + z.tokens + kAlign;
 }
 
 size_t reuse_ops_delta_scratch_bytes(const rn_delta_shape *shape) {
@@ -203,7 +192,7 @@ size_t reuse_ops_delta_scratch_bytes(const rn_delta_shape *shape) {
 size_t reuse_ops_delta_backward_scratch_bytes(const rn_delta_shape *shape) {
     if (bad_shape(shape) || too_wide(shape)) return 0;
     const DeltaSizes z = sizes(shape);
-    return z.states + z.tokens + kAlign;
+    return 3 * z.keys + 2 * z.inverse + z.decay + z.states + z.tokens + kAlign;
 }
 
 rn_status reuse_ops_delta_forward(const rn_delta_shape *shape, const void *q, const void *k, const void *v,
@@ -225,11 +214,15 @@ rn_status reuse_ops_delta_forward(const rn_delta_shape *shape, const void *q, co
     char *kept = static_cast<char *>(saved), *at = static_cast<char *>(scratch);
     DeltaArgs a = delta_args(shape, q, k, v, g, beta);
     a.off = seq_off, a.state = state, a.final_state = final_state, a.out = out;
-    lay_out(a, z, at);
+    a.kf = reinterpret_cast<uint16_t *>(at);
+    a.qf = reinterpret_cast<uint16_t *>(at += z.keys);
+    a.kt = reinterpret_cast<uint16_t *>(at += z.keys);
+    a.mf = reinterpret_cast<uint16_t *>(at += z.keys);
+    a.pf = reinterpret_cast<uint16_t *>(at += z.inverse);
+    a.dec = reinterpret_cast<float *>(at += z.score);
     if (saved) {
-        a.inv = reinterpret_cast<float *>(kept);
-        a.score = reinterpret_cast<float *>(kept + z.pairs);
-        a.before = reinterpret_cast<float *>(kept + 2 * z.pairs);
+        a.before = reinterpret_cast<float *>(kept);
+        a.err = reinterpret_cast<float *>(kept + z.states);
     }
     return launched(launch_delta_forward(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
 }
@@ -254,12 +247,17 @@ rn_status reuse_ops_delta_backward(const rn_delta_shape *shape, const void *q, c
     char *kept = const_cast<char *>(static_cast<const char *>(saved)), *at = static_cast<char *>(scratch);
     DeltaArgs a = delta_args(shape, q, k, v, g, beta);
     a.off = seq_off;
-    a.inv = reinterpret_cast<float *>(kept);
-    a.score = reinterpret_cast<float *>(kept + z.pairs);
-    a.before = reinterpret_cast<float *>(kept + 2 * z.pairs);
+    a.before = reinterpret_cast<float *>(kept);
+    a.err = reinterpret_cast<float *>(kept + z.states);
     a.dout = dout, a.dfinal = dfinal;
-    a.after = reinterpret_cast<float *>(at);
-    a.dwrite = reinterpret_cast<float *>(at + z.states);
+    a.kf = reinterpret_cast<uint16_t *>(at);
+    a.kt = reinterpret_cast<uint16_t *>(at += z.keys);
+    a.qt = reinterpret_cast<uint16_t *>(at += z.keys);
+    a.mf = reinterpret_cast<uint16_t *>(at += z.keys);
+    a.pf = reinterpret_cast<uint16_t *>(at += z.inverse);
+    a.dec = reinterpret_cast<float *>(at += z.inverse);
+    a.after = reinterpret_cast<float *>(at += z.decay);
+    a.dwrite = reinterpret_cast<float *>(at += z.states);
     a.dq = dq, a.dkey = dk, a.dval = dv, a.dg = dg, a.dbeta = dbeta, a.dstate = dstate;
     return launched(launch_delta_backward(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
 }
