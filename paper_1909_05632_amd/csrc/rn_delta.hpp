@@ -57,14 +57,14 @@ __device__ inline Chunk chunk_of(const DeltaArgs &a, int slot) {
     return {lo, s.begin + (int)at, min(kC, s.len - (int)at)};
 }
 
-// Log decays summed up to each token of a chunk, in double: differences of far
-// tokens stay exact to float32 where the sums are large.  An empty memory
+// Log decays (base 2) summed up to each token of a chunk, in double: differences
+// of far tokens stay exact to float32 where the sums are large.  An empty memory
 // (g = -infinity) is a decay of e^-10^6 = 0, whose differences are finite.
 // Tokens past the end count as g = 0.  One wave calls it; lane = token.
 __device__ inline double decay_sums(const DeltaArgs &a, const Chunk &c, int head) {
     const int lane = threadIdx.x & 63;
     float g = lane < c.len ? a.g[(int64_t)(c.begin + lane) * a.hv + head] : 0.f;
-    double s = g < -1e6f ? -1e6 : (double)g;
+    double s = (g < -1e6f ? -1e6 : (double)g) * 1.4426950408889634;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const double t = __shfl_up(s, d);
@@ -72,6 +72,8 @@ __device__ inline double decay_sums(const DeltaArgs &a, const Chunk &c, int head
     }
     return s;
 }
+// 2^d: the hardware's, exact to an ulp where the result is a normal float32.
+__device__ inline float decay(double d) { return __builtin_amdgcn_exp2f((float)d); }
 
 template <class T>
 __device__ inline float load(const void *p, int64_t i) {
@@ -228,8 +230,8 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
         const float b = lane < c.len ? a.beta[(int64_t)(c.begin + lane) * a.hv + h] : 0.f;
         cs[lane] = s;
         beta[lane] = b;
-        a.dec[ch * 3 * kC + lane] = expf((float)s);
-        a.dec[ch * 3 * kC + kC + lane] = expf((float)(last - s));
+        a.dec[ch * 3 * kC + lane] = decay(s);
+        a.dec[ch * 3 * kC + kC + lane] = decay(last - s);
         a.dec[ch * 3 * kC + 2 * kC + lane] = b;
     }
 #pragma unroll
@@ -286,7 +288,7 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int t = wave * 16 + g * 4 + j;
-            const float d = busy && n <= wave && col <= t ? expf((float)(cs[t] - cs[col])) : 0.f;
+            const float d = busy && n <= wave && col <= t ? decay(cs[t] - cs[col]) : 0.f;
             y[t * kLd + col] = col <= t ? d * w[n][j] * a.scale : 0.f;
             x[t * kLd + col] = col < t ? beta[BWD ? t : col] * d * u[n][j] : 0.f;
         }

@@ -263,7 +263,7 @@ __device__ inline void planes8(const float (&v)[8], bf16x8 (&f)[N]) {
 // dV', E, S and dS' are operands as they lie in memory.  The waves split S, dS'
 // and V' into planes once for all, through LDS; what is left of a block's time
 // is the matrix ops and those planes' reads.
-template <class T, int KS, bool VEC>
+template <class T, int KS, bool VEC, bool SHARED>
 __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaArgs a) {
     constexpr int NP = sizeof(T) == 2 ? 1 : 3, KT = 2 * KS;
     constexpr int kKeys = 4 * KS * NP * kFrag;
@@ -276,11 +276,10 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
     const int slot = blockIdx.x, hk = blockIdx.y, group = a.hv / a.hk;
     const Chunk c = chunk_of(a, slot);
     if (c.len == 0) return;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lane_ = threadIdx.x & 63;
     const int blocks = (c.len + 15) / 16, half = (c.len + 31) / 32;
     const bool busy = wave < blocks;
-    const int token = wave * 16 + r;                    // as an operand's row
-    const int row4 = wave * 16 + g * 4;                 // as a result's rows
     const int64_t keys = ((int64_t)slot * a.hk + hk) * kKeys;
     // Sum over the 16 lanes that hold a row's columns.
     const auto across = [&](float v) {
@@ -288,15 +287,21 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
         for (int s = 1; s < 16; s <<= 1) v += __shfl_xor(v, s);
         return v;
     };
-    f32x4 tq[KT], tk[KT];
+    f32x4 tq[KT], tk[KT];                               // over the value heads (SHARED)
 #pragma unroll
     for (int n = 0; n < KT; ++n) tq[n] = tk[n] = f32x4{};
-    for (int h = hk * group; h < (hk + 1) * group; ++h) {
+    for (int h = hk * group;; ++h) {
+        // The lane anew for each head: offsets from it are not kept from head to
+        // head, which would cost more registers than there are.
+        uint32_t lane = lane_, r = lane & 15, g = lane >> 4;
+        asm volatile("" : "+v"(lane), "+v"(r), "+v"(g));
+        const int token = wave * 16 + (int)r;           // as an operand's row
+        const int row4 = wave * 16 + (int)g * 4;        // as a result's rows
         const int64_t ch = (int64_t)slot * a.hv + h;
         __syncthreads();
         if (wave == 0) {
             cs[lane] = decay_sums(a, c, h);
-            beta_s[lane] = lane < c.len ? a.beta[(int64_t)(c.begin + lane) * a.hv + h] : 0.f;
+            beta_s[lane] = (int)lane < c.len ? a.beta[(int64_t)(c.begin + lane) * a.hv + h] : 0.f;
         }
         __syncthreads();
         f32x4 gq[KT], gr[KT], gw[KT], dp[4], dl[4];
@@ -309,11 +314,11 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
         const int64_t row = ((int64_t)(c.begin + token) * a.hv + h) * a.dv;
         const bool in = token < c.len;
         for (int v0 = 0; v0 < a.dv; v0 += 32) {
-            const int v = v0 + g * 8;
+            const int v = v0 + (int)g * 8;
             // S and dS', two or fewer of their row tiles a wave
 #pragma unroll
             for (int i = 0; i < (KT + 3) / 4; ++i) {
-                const int n = wave + 4 * i, d = n * 16 + r;
+                const int n = wave + 4 * i, d = n * 16 + (int)r;
                 if (KT % 4 == 0 || n < KT) {
                     float s[8], t[8];
                     load8<float, VEC>(a.before + (ch * a.dk + d) * a.dv, d < a.dk, v, a.dv, s);
@@ -376,6 +381,7 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
                     }
 #pragma unroll
                 for (int n = 0; n < KT; ++n) {
+                    if (n % 2 == 0) __builtin_amdgcn_sched_barrier(0);
                     bf16x8 f[3];
                     load_frags<3>(fS + n * 3 * kFrag + lane * 8, f);
                     gq[n] = mm<NP, 3>(fo, f, gq[n]);
@@ -390,44 +396,49 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
         db += __shfl_xor(db, 16);
         db += __shfl_xor(db, 32);
         if (g == 0 && in) a.dbeta[(int64_t)(c.begin + token) * a.hv + h] = db;
+        // Where this lane's results lie in k and q: offsets from bases that the wave
+        // shares, clamped into the rows (results there are 0).
+        const T *kbase = static_cast<const T *>(a.k) + (int64_t)c.begin * a.ks + hk * a.dk;
+        const T *qbase = static_cast<const T *>(a.q) + (int64_t)c.begin * a.qs + hk * a.dk;
+        uint32_t krow[4], qrow[4], dcol[KT];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            krow[j] = min(row4 + j, c.len - 1) * (uint32_t)a.ks;
+            qrow[j] = min(row4 + j, c.len - 1) * (uint32_t)a.qs;
+        }
+#pragma unroll
+        for (int n = 0; n < KT; ++n) dcol[n] = min(n * 16 + (int)r, a.dk - 1);
         const double last = cs[kC - 1];
         // the pairs' weights
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int t = row4 + j, u = n * 16 + r;
-                const float d = u <= t && n <= wave ? expf((float)(cs[t] - cs[u])) : 0.f;
+                const int t = row4 + j, u = n * 16 + (int)r;
+                const float d = u <= t && n <= wave ? decay(cs[t] - cs[u]) : 0.f;
                 x[t * kLd + u] = u <= t ? dp[n][j] * d * a.scale : 0.f;
                 y[t * kLd + u] = u < t ? -dl[n][j] * d : 0.f;
             }
-        // The memory's part of the sums, before the pairs' is added.  k and q: this
-        // wave's rows of the results' columns.
+        // The memory's part of the sums, before the pairs' is added.
         float wsum = 0.f;
-        float kr[4][KT], qr[4][KT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int t = row4 + j;
-#pragma unroll
-            for (int n = 0; n < KT; ++n) {
-                const bool there = t < c.len && n * 16 + r < a.dk;
-                kr[j][n] = there ? load<T>(a.k, (int64_t)(c.begin + t) * a.ks + hk * a.dk + n * 16 + r) : 0.f;
-                qr[j][n] = there ? load<T>(a.q, (int64_t)(c.begin + t) * a.qs + hk * a.dk + n * 16 + r) : 0.f;
-            }
-            const float grown = expf((float)cs[t]), left = expf((float)(last - cs[t]));
+            const float grown = decay(cs[t]), left = decay(last - cs[t]);
             float s = 0.f;
 #pragma unroll
             for (int n = 0; n < KT; ++n) {
                 gq[n][j] *= grown * a.scale;
                 gr[n][j] *= -grown;
                 gw[n][j] *= left;
-                s = fmaf(gw[n][j], kr[j][n], s);
+                s = fmaf(gw[n][j], to_float(kbase[krow[j] + dcol[n]]), s);
             }
-            wsum += across(s);
+            wsum += s;
         }
+        wsum = across(wsum);
         wsum += __shfl_xor(wsum, 16);
         wsum += __shfl_xor(wsum, 32);
-        float all = dot * expf((float)last);
+        float all = dot * decay(last);
 #pragma unroll
         for (int s = 1; s < 64; s <<= 1) all += __shfl_xor(all, s);
         if (lane == 0) extra[wave] = all + wsum;
@@ -456,9 +467,10 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
                     }
 #pragma unroll
                     for (int n = 0; n < KT; ++n) {
+                        __builtin_amdgcn_sched_barrier(0);     // or all tiles' loads are hoisted, and spilled
                         bf16x8 fk[NP], fq[NP];
-                        load_frags<NP>(a.kt + keys + (n * 2 + ks) * NP * kFrag + lane * 8, fk);
-                        load_frags<NP>(a.qt + keys + (n * 2 + ks) * NP * kFrag + lane * 8, fq);
+                        load_frags<NP>(a.kt + keys + (lane * 8 + (n * 2 + ks) * NP * kFrag), fk);
+                        load_frags<NP>(a.qt + keys + (lane * 8 + (n * 2 + ks) * NP * kFrag), fq);
                         if (lower) {
                             gq[n] = mm<3, NP>(fx, fk, gq[n]);
                             gr[n] = mm<3, NP>(fy, fk, gr[n]);
@@ -474,10 +486,10 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
             float s = 0.f;
 #pragma unroll
             for (int n = 0; n < KT; ++n) {
-                s = fmaf(gq[n][j], qr[j][n], s);
-                s = fmaf(gr[n][j] - gw[n][j], kr[j][n], s);
-                tq[n][j] += gq[n][j];
-                tk[n][j] += gr[n][j] + gw[n][j];
+                s = fmaf(gq[n][j], to_float(qbase[qrow[j] + dcol[n]]), s);
+                s = fmaf(gr[n][j] - gw[n][j], to_float(kbase[krow[j] + dcol[n]]), s);
+                tq[n][j] = SHARED ? tq[n][j] + gq[n][j] : gq[n][j];
+                tk[n][j] = SHARED ? tk[n][j] + (gr[n][j] + gw[n][j]) : gr[n][j] + gw[n][j];
             }
             s = across(s);
             if (r == 0) dc[row4 + j] = s;
@@ -485,26 +497,30 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
         __syncthreads();
         if (wave == 0) {
             double s = dc[lane];
-            if (lane == kC - 1) s += ((double)extra[0] + extra[1]) + ((double)extra[2] + extra[3]);
+            if (lane == kC - 1u) s += ((double)extra[0] + extra[1]) + ((double)extra[2] + extra[3]);
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) {
                 const double u = __shfl_down(s, d);
-                if (lane + d < 64) s += u;
+                if ((int)lane + d < 64) s += u;
             }
-            if (lane < c.len) a.dg[(int64_t)(c.begin + lane) * a.hv + h] = (float)s;
+            if ((int)lane < c.len) a.dg[(int64_t)(c.begin + lane) * a.hv + h] = (float)s;
         }
+        if (!SHARED || h + 1 == (hk + 1) * group) break;
     }
+    const uint32_t r = lane_ & 15;
+    const int row4 = wave * 16 + (int)(lane_ >> 4) * 4;
+    const __amdgpu_buffer_rsrc_t rq = rsrc_of(static_cast<T *>(a.dq) + ((int64_t)c.begin * a.hk + hk) * a.dk);
+    const __amdgpu_buffer_rsrc_t rk = rsrc_of(static_cast<T *>(a.dkey) + ((int64_t)c.begin * a.hk + hk) * a.dk);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int t = row4 + j;
-        if (t >= c.len) continue;
-        const int64_t at = ((int64_t)(c.begin + t) * a.hk + hk) * a.dk;
+        const uint32_t at = t * (uint32_t)(a.hk * a.dk) + r;
 #pragma unroll
-        for (int n = 0; n < KT; ++n)
-            if (n * 16 + r < a.dk) {
-                static_cast<T *>(a.dq)[at + n * 16 + r] = from_float<T>(tq[n][j]);
-                static_cast<T *>(a.dkey)[at + n * 16 + r] = from_float<T>(tk[n][j]);
-            }
+        for (int n = 0; n < KT; ++n) {
+            const bool in = t < c.len && n * 16 + (int)r < a.dk;
+            store_if(in, rq, sizeof(T) * (at + n * 16), from_float<T>(tq[n][j]));
+            store_if(in, rk, sizeof(T) * (at + n * 16), from_float<T>(tk[n][j]));
+        }
     }
 }
 
@@ -520,8 +536,14 @@ hipError_t backward_ks(const DeltaArgs &a, hipStream_t s) {
     if (a.tokens == 0) return hipSuccess;
     const dim3 grid((int)delta_chunk_slots(a.tokens, a.n), a.hk);
     const auto even = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
-    if (a.dv % 8 == 0 && even(a.dout) && even(a.dval)) k_delta_bwd_chunk<T, KS, true><<<grid, 256, 0, s>>>(a);
-    else k_delta_bwd_chunk<T, KS, false><<<grid, 256, 0, s>>>(a);
+    const bool vec = a.dv % 8 == 0 && even(a.dout) && even(a.dval);
+    if (a.hv > a.hk) {
+        if (vec) k_delta_bwd_chunk<T, KS, true, true><<<grid, 256, 0, s>>>(a);
+        else k_delta_bwd_chunk<T, KS, false, true><<<grid, 256, 0, s>>>(a);
+    } else {
+        if (vec) k_delta_bwd_chunk<T, KS, true, false><<<grid, 256, 0, s>>>(a);
+        else k_delta_bwd_chunk<T, KS, false, false><<<grid, 256, 0, s>>>(a);
+    }
     return hipGetLastError();
 }
 
