@@ -230,23 +230,24 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
 
 // ------------------------------------------------------------------ a chunk by itself
 
-// Eight consecutive elements of a row of `count`, zeros where there are none.
+// Eight consecutive elements of a row of `count`, zeros where there are none; as
+// loaded, so that a later step's can be on their way while this one is computed.
 template <class T, bool VEC>
-__device__ inline void load8(const T *p, bool in, int from, int count, float (&v)[8]) {
-    if constexpr (VEC) {                                // count a multiple of 8, rows on 16 bytes
-        constexpr int PER = 16 / sizeof(T);
+struct Raw8 {
+    static constexpr int PER = VEC ? 16 / sizeof(T) : 1;            // VEC: count a multiple of 8, rows on 16 bytes
+    Pack<T, PER> v[8 / PER];
+    __device__ void load(const T *p, bool in, int from, int count) {
 #pragma unroll
-        for (int e = 0; e < 8; e += PER) {
-            Pack<T, PER> q{};
-            if (in && from < count) q = *reinterpret_cast<const Pack<T, PER> *>(p + from + e);
-#pragma unroll
-            for (int o = 0; o < PER; ++o) v[e + o] = to_float(q.v[o]);
+        for (int e = 0; e < 8 / PER; ++e) {
+            v[e] = Pack<T, PER>{};
+            if (in && from + e * PER < count) v[e] = *reinterpret_cast<const Pack<T, PER> *>(p + from + e * PER);
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = in && from + e < count ? to_float(p[from + e]) : 0.f;
     }
-}
+    __device__ void get(float (&f)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = to_float(v[e / PER].v[e % PER]);
+    }
+};
 template <int N>
 __device__ inline void planes8(const float (&v)[8], bf16x8 (&f)[N]) {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -313,16 +314,30 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
         const float b = beta_s[token];
         const int64_t row = ((int64_t)(c.begin + token) * a.hv + h) * a.dv;
         const bool in = token < c.len;
+        constexpr int RT = (KT + 3) / 4;                // row tiles of S and dS' a wave splits
+        Raw8<float, VEC> rs[RT], rt[RT], rw, re;
+        Raw8<T, VEC> ro;
+        const auto fetch = [&](int v) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const int d = (wave + 4 * i) * 16 + (int)r;
+                rs[i].load(a.before + (ch * a.dk + d) * a.dv, d < a.dk, v, a.dv);
+                rt[i].load(a.after + (ch * a.dk + d) * a.dv, d < a.dk, v, a.dv);
+            }
+            ro.load(static_cast<const T *>(a.dout) + row, in, v, a.dv);
+            rw.load(a.dwrite + row, in, v, a.dv);
+            re.load(a.err + row, in, v, a.dv);
+        };
+        fetch(g * 8);
         for (int v0 = 0; v0 < a.dv; v0 += 32) {
             const int v = v0 + (int)g * 8;
             // S and dS', two or fewer of their row tiles a wave
 #pragma unroll
-            for (int i = 0; i < (KT + 3) / 4; ++i) {
-                const int n = wave + 4 * i, d = n * 16 + (int)r;
+            for (int i = 0; i < RT; ++i) {
+                const int n = wave + 4 * i;
                 if (KT % 4 == 0 || n < KT) {
                     float s[8], t[8];
-                    load8<float, VEC>(a.before + (ch * a.dk + d) * a.dv, d < a.dk, v, a.dv, s);
-                    load8<float, VEC>(a.after + (ch * a.dk + d) * a.dv, d < a.dk, v, a.dv, t);
+                    rs[i].get(s), rt[i].get(t);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) dot = fmaf(s[e], t[e], dot);
                     bf16x8 f[3];
@@ -337,9 +352,7 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
             bf16x8 fo[NP], fr[3], fv[3];
             if (busy) {
                 float o[8], w[8], e[8];
-                load8<T, VEC>(static_cast<const T *>(a.dout) + row, in, v, a.dv, o);
-                load8<float, VEC>(a.dwrite + row, in, v, a.dv, w);
-                load8<float, VEC>(a.err + row, in, v, a.dv, e);
+                ro.get(o), rw.get(w), re.get(e);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     db = fmaf(w[i], e[i], db);
@@ -369,7 +382,8 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
 #pragma unroll
                 for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8 *>(fV + (wave * 3 + p) * kFrag + lane * 8) = fv[p];
             }
-            __syncthreads();
+            fetch(v + 32);                              // nothing past the last column
+            dev::lds_barrier();                         // which leaves those loads in flight
             if (busy) {
 #pragma unroll
                 for (int n = 0; n < 4; ++n)
@@ -390,7 +404,7 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
                     gw[n] = mm<3, 3>(fv, f, gw[n]);
                 }
             }
-            __syncthreads();
+            dev::lds_barrier();
         }
         // dbeta: a row's four lanes
         db += __shfl_xor(db, 16);
@@ -443,44 +457,55 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
         for (int s = 1; s < 64; s <<= 1) all += __shfl_xor(all, s);
         if (lane == 0) extra[wave] = all + wsum;
         __syncthreads();
-        if (busy)
+        if (busy) {
+            // K^T's and Q^T's pieces, a few ahead of their use.
+            constexpr int AHEAD = NP == 1 ? 4 : 2;
+            bf16x8 fk[AHEAD][NP], fq[AHEAD][NP];
+            const auto ask = [&](int i) {               // piece i: k step i / KT, row tile i % KT
+                const int at = (i % KT * 2 + i / KT) * NP * kFrag;
+                load_frags<NP>(a.kt + keys + (lane * 8 + at), fk[i % AHEAD]);
+                load_frags<NP>(a.qt + keys + (lane * 8 + at), fq[i % AHEAD]);
+            };
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks)
-                if (ks < half) {
-                    // rows i of dP e and dL e for the reads, columns for the writes
-                    bf16x8 fx[3], fy[3], fxt[3], fyt[3];
-                    const bool lower = ks <= wave / 2, upper = ks >= wave / 2;
-                    float v[8], w[8];
-                    const float *px = x + token * kLd + ks * 32 + g * 8, *py = px + kC * kLd;
-                    if (lower) {
+            for (int i = 0; i < AHEAD; ++i) ask(i);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = px[e], w[e] = py[e];
-                        planes8<3>(v, fx);
-                        planes8<3>(w, fy);
-                    }
-                    if (upper) {
-                        const float *tx = x + (ks * 32 + g * 8) * kLd + token, *ty = tx + kC * kLd;
+            for (int ks = 0; ks < 2; ++ks) {
+                // rows i of dP e and dL e for the reads, columns for the writes
+                bf16x8 fx[3], fy[3], fxt[3], fyt[3];
+                const bool lower = ks <= wave / 2, upper = ks >= wave / 2;
+                float v[8], w[8];
+                const float *px = x + token * kLd + ks * 32 + g * 8, *py = px + kC * kLd;
+                if (ks < half && lower) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = tx[e * kLd], w[e] = ty[e * kLd];
-                        planes8<3>(v, fxt);
-                        planes8<3>(w, fyt);
-                    }
+                    for (int e = 0; e < 8; ++e) v[e] = px[e], w[e] = py[e];
+                    planes8<3>(v, fx);
+                    planes8<3>(w, fy);
+                }
+                if (ks < half && upper) {
+                    const float *tx = x + (ks * 32 + g * 8) * kLd + token, *ty = tx + kC * kLd;
 #pragma unroll
-                    for (int n = 0; n < KT; ++n) {
-                        __builtin_amdgcn_sched_barrier(0);     // or all tiles' loads are hoisted, and spilled
-                        bf16x8 fk[NP], fq[NP];
-                        load_frags<NP>(a.kt + keys + (lane * 8 + (n * 2 + ks) * NP * kFrag), fk);
-                        load_frags<NP>(a.qt + keys + (lane * 8 + (n * 2 + ks) * NP * kFrag), fq);
+                    for (int e = 0; e < 8; ++e) v[e] = tx[e * kLd], w[e] = ty[e * kLd];
+                    planes8<3>(v, fxt);
+                    planes8<3>(w, fyt);
+                }
+#pragma unroll
+                for (int n = 0; n < KT; ++n) {
+                    const int i = ks * KT + n;
+                    __builtin_amdgcn_sched_barrier(0);  // or all pieces' loads are hoisted, and spilled
+                    if (ks < half) {
                         if (lower) {
-                            gq[n] = mm<3, NP>(fx, fk, gq[n]);
-                            gr[n] = mm<3, NP>(fy, fk, gr[n]);
+                            gq[n] = mm<3, NP>(fx, fk[i % AHEAD], gq[n]);
+                            gr[n] = mm<3, NP>(fy, fk[i % AHEAD], gr[n]);
                         }
                         if (upper) {
-                            gw[n] = mm<3, NP>(fxt, fq, gw[n]);
-                            gw[n] = mm<3, NP>(fyt, fk, gw[n]);
+                            gw[n] = mm<3, NP>(fxt, fq[i % AHEAD], gw[n]);
+                            gw[n] = mm<3, NP>(fyt, fk[i % AHEAD], gw[n]);
                         }
                     }
+                    if (i + AHEAD < 2 * KT) ask(i + AHEAD);
                 }
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float s = 0.f;
