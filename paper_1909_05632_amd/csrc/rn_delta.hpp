@@ -188,6 +188,7 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     __shared__ float beta[kC];
     const int slot = blockIdx.x, h = blockIdx.y, group = a.hv / a.hk, hk = h / group;
     const Chunk c = chunk_of(a, slot);
+    if (BWD && h == 0 && threadIdx.x == 0) a.map[2 * slot] = c.begin, a.map[2 * slot + 1] = c.len;
     if (c.len == 0) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int blocks = (c.len + 15) / 16;               // 16s of tokens

@@ -230,17 +230,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
 
 // ------------------------------------------------------------------ a chunk by itself
 
-// Eight consecutive elements of a row of `count`, zeros where there are none; as
-// loaded, so that a later step's can be on their way while this one is computed.
+// Elements from .. + 3 and from + 16 .. + 19 of a row of `count`, zeros where there
+// are none; as loaded, so that a later step's can be on their way while this one
+// is computed.  (Which of 32 elements a lane holds is free as long as both
+// operands of a product agree; four lanes read 64 bytes on end this way.)
 template <class T, bool VEC>
 struct Raw8 {
-    static constexpr int PER = VEC ? 16 / sizeof(T) : 1;            // VEC: count a multiple of 8, rows on 16 bytes
+    static constexpr int PER = VEC ? 4 : 1;             // VEC: count a multiple of 8, rows on 16 bytes
     Pack<T, PER> v[8 / PER];
     __device__ void load(const T *p, bool in, int from, int count) {
 #pragma unroll
-        for (int e = 0; e < 8 / PER; ++e) {
-            v[e] = Pack<T, PER>{};
-            if (in && from + e * PER < count) v[e] = *reinterpret_cast<const Pack<T, PER> *>(p + from + e * PER);
+        for (int e = 0; e < 8; e += PER) {
+            const int at = from + (e < 4 ? e : e + 12);
+            v[e / PER] = Pack<T, PER>{};
+            if (in && at < count) v[e / PER] = *reinterpret_cast<const Pack<T, PER> *>(p + at);
         }
     }
     __device__ void get(float (&f)[8]) const {
@@ -248,6 +251,18 @@ struct Raw8 {
         for (int e = 0; e < 8; ++e) f[e] = to_float(v[e / PER].v[e % PER]);
     }
 };
+template <class T, bool VEC>
+__device__ inline void store8(T *p, int from, int count, const float (&f)[8]) {
+    constexpr int PER = VEC ? 4 : 1;
+#pragma unroll
+    for (int e = 0; e < 8; e += PER) {
+        const int at = from + (e < 4 ? e : e + 12);
+        Pack<T, PER> q;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) q.v[j] = from_float<T>(f[e + j]);
+        if (at < count) *reinterpret_cast<Pack<T, PER> *>(p + at) = q;
+    }
+}
 template <int N>
 __device__ inline void planes8(const float (&v)[8], bf16x8 (&f)[N]) {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -259,25 +274,30 @@ __device__ inline void planes8(const float (&v)[8], bf16x8 (&f)[N]) {
 }
 
 // A block takes a chunk slot and a key head and adds the value heads that share
-// it; a wave owns 16 tokens, with dq, dk(reads) and dk(writes) of them in its
-// registers.  All big products sum over the values, 32 at a time: rows of dO,
-// dV', E, S and dS' are operands as they lie in memory.  The waves split S, dS'
-// and V' into planes once for all, through LDS; what is left of a block's time
-// is the matrix ops and those planes' reads.
+// it.  All big products sum over the values, 32 at a time: rows of dO, dV', E, S
+// and dS' are operands as they lie in memory.  The waves split them into planes
+// once for all, through LDS, while the next step's are on their way.  dk above 64
+// takes eight waves: w and w + 4 own 16 tokens, half of dk's row tiles of dq,
+// dk(reads) and dk(writes) in the registers of each (four waves that own all of
+// dk fill the registers with these sums, and no second wave a SIMD covers the
+// first one's waits: 274 us for 8192 ragged tokens of 8 heads, 182 with eight).
+// Up to 64 four waves do: for a chunk of 16 tokens one of four works.
 template <class T, int KS, bool VEC, bool SHARED>
-__global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaArgs a) {
-    constexpr int NP = sizeof(T) == 2 ? 1 : 3, KT = 2 * KS;
+__global__ __launch_bounds__(KS == 4 ? 512 : 256, 2) void k_delta_bwd_chunk(DeltaArgs a) {
+    constexpr int NP = sizeof(T) == 2 ? 1 : 3, KT = 2 * KS, PARTS = KS == 4 ? 2 : 1, HT = KT / PARTS;
     constexpr int kKeys = 4 * KS * NP * kFrag;
-    constexpr int kStep = (2 * KT + 4) * 3 * kFrag * 2, kPairs = 2 * kC * kLd * 4;       // bytes of the two uses
+    constexpr int kStep = (2 * KT * 3 + 4 * (6 + NP)) * kFrag * 2, kPairs = 2 * kC * kLd * 4;   // bytes of the two uses
     __shared__ __align__(16) char lds[kStep > kPairs ? kStep : kPairs];
-    uint16_t *fS = reinterpret_cast<uint16_t *>(lds), *fD = fS + KT * 3 * kFrag, *fV = fD + KT * 3 * kFrag;
+    uint16_t *fS = reinterpret_cast<uint16_t *>(lds), *fD = fS + KT * 3 * kFrag;
+    uint16_t *fV = fD + KT * 3 * kFrag, *fR = fV + 4 * 3 * kFrag, *fO = fR + 4 * 3 * kFrag;     // V', dv, dO by 16 tokens
     float *x = reinterpret_cast<float *>(lds), *y = x + kC * kLd;   // [i][j] of dP e and dL e
     __shared__ double cs[kC];
-    __shared__ float beta_s[kC], dc[kC], extra[4];
+    __shared__ float beta_s[kC], dc[PARTS][kC], extra[4 * PARTS];
     const int slot = blockIdx.x, hk = blockIdx.y, group = a.hv / a.hk;
-    const Chunk c = chunk_of(a, slot);
+    const Chunk c{0, a.map[2 * slot], a.map[2 * slot + 1]};
     if (c.len == 0) return;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave8 & 3;
+    const int part = PARTS > 1 ? wave8 >> 2 : 0;
     const uint32_t lane_ = threadIdx.x & 63;
     const int blocks = (c.len + 15) / 16, half = (c.len + 31) / 32;
     const bool busy = wave < blocks;
@@ -288,9 +308,9 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
         for (int s = 1; s < 16; s <<= 1) v += __shfl_xor(v, s);
         return v;
     };
-    f32x4 tq[KT], tk[KT];                               // over the value heads (SHARED)
+    f32x4 tq[HT], tk[HT];                               // over the value heads (SHARED)
 #pragma unroll
-    for (int n = 0; n < KT; ++n) tq[n] = tk[n] = f32x4{};
+    for (int n = 0; n < HT; ++n) tq[n] = tk[n] = f32x4{};
     for (int h = hk * group;; ++h) {
         // The lane anew for each head: offsets from it are not kept from head to
         // head, which would cost more registers than there are.
@@ -300,107 +320,105 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
         const int row4 = wave * 16 + (int)g * 4;        // as a result's rows
         const int64_t ch = (int64_t)slot * a.hv + h;
         __syncthreads();
-        if (wave == 0) {
+        if (wave8 == 0) {
             cs[lane] = decay_sums(a, c, h);
             beta_s[lane] = (int)lane < c.len ? a.beta[(int64_t)(c.begin + lane) * a.hv + h] : 0.f;
         }
         __syncthreads();
-        f32x4 gq[KT], gr[KT], gw[KT], dp[4], dl[4];
+        // pr: dP and dL (with two parts, dP with the one and dL with the other)
+        f32x4 gq[HT], gr[HT], gw[HT], pr[3 - PARTS][4];
 #pragma unroll
-        for (int n = 0; n < KT; ++n) gq[n] = gr[n] = gw[n] = f32x4{};
+        for (int n = 0; n < HT; ++n) gq[n] = gr[n] = gw[n] = f32x4{};
 #pragma unroll
-        for (int n = 0; n < 4; ++n) dp[n] = dl[n] = f32x4{};
+        for (int n = 0; n < 4; ++n) pr[0][n] = pr[2 - PARTS][n] = f32x4{};
         float db = 0.f, dot = 0.f;
         const float b = beta_s[token];
         const int64_t row = ((int64_t)(c.begin + token) * a.hv + h) * a.dv;
         const bool in = token < c.len;
-        constexpr int RT = (KT + 3) / 4;                // row tiles of S and dS' a wave splits
+        constexpr int W8 = 4 * PARTS, RT = KT > W8 ? KT / W8 : 1;       // row tiles of S and dS' a wave splits
         Raw8<float, VEC> rs[RT], rt[RT], rw, re;
         Raw8<T, VEC> ro;
         const auto fetch = [&](int v) {
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                const int d = (wave + 4 * i) * 16 + (int)r;
+                const int d = (wave8 + W8 * i) * 16 + (int)r;
                 rs[i].load(a.before + (ch * a.dk + d) * a.dv, d < a.dk, v, a.dv);
                 rt[i].load(a.after + (ch * a.dk + d) * a.dv, d < a.dk, v, a.dv);
             }
-            ro.load(static_cast<const T *>(a.dout) + row, in, v, a.dv);
+            if (part == 0) re.load(a.err + row, in, v, a.dv);
+            if (part == 0) ro.load(static_cast<const T *>(a.dout) + row, in, v, a.dv);
             rw.load(a.dwrite + row, in, v, a.dv);
-            re.load(a.err + row, in, v, a.dv);
         };
-        fetch(g * 8);
+        fetch(g * 4);
         for (int v0 = 0; v0 < a.dv; v0 += 32) {
-            const int v = v0 + (int)g * 8;
-            // S and dS', two or fewer of their row tiles a wave
+            const int v = v0 + (int)g * 4;
+            const auto put = [&](uint16_t *to, const auto &f) {
+#pragma unroll
+                for (int p = 0; p < (int)(sizeof(f) / sizeof(f[0])); ++p) *reinterpret_cast<bf16x8 *>(to + p * kFrag + lane * 8) = f[p];
+            };
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                const int n = wave + 4 * i;
-                if (KT % 4 == 0 || n < KT) {
+                const int n = wave8 + W8 * i;
+                if (n < KT) {
                     float s[8], t[8];
                     rs[i].get(s), rt[i].get(t);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) dot = fmaf(s[e], t[e], dot);
                     bf16x8 f[3];
                     planes8<3>(s, f);
-#pragma unroll
-                    for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8 *>(fS + (n * 3 + p) * kFrag + lane * 8) = f[p];
+                    put(fS + n * 3 * kFrag, f);
                     planes8<3>(t, f);
-#pragma unroll
-                    for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8 *>(fD + (n * 3 + p) * kFrag + lane * 8) = f[p];
+                    put(fD + n * 3 * kFrag, f);
                 }
             }
-            bf16x8 fo[NP], fr[3], fv[3];
             if (busy) {
-                float o[8], w[8], e[8];
-                ro.get(o), rw.get(w), re.get(e);
+                float w[8];
+                bf16x8 f[3];
+                rw.get(w);
+                if (part == 0) {
+                    float o[8], e[8];
+                    bf16x8 fo[NP];
+                    ro.get(o), re.get(e);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    db = fmaf(w[i], e[i], db);
-                    e[i] *= b;
-                    w[i] *= b;
-                }
-                planes8<NP>(o, fo);
-                planes8<3>(w, fr);                      // beta dV', which is dv
-                planes8<3>(e, fv);                      // V'
-                T *dv = static_cast<T *>(a.dval) + row;
-                if (in) {
-                    if constexpr (VEC) {
-                        constexpr int PER = 16 / sizeof(T);
-#pragma unroll
-                        for (int i = 0; i < 8; i += PER) {
-                            Pack<T, PER> q;
-#pragma unroll
-                            for (int j = 0; j < PER; ++j) q.v[j] = from_float<T>(w[i + j]);
-                            if (v < a.dv) *reinterpret_cast<Pack<T, PER> *>(dv + v + i) = q;
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (v + i < a.dv) dv[v + i] = from_float<T>(w[i]);
+                    for (int i = 0; i < 8; ++i) {
+                        db = fmaf(w[i], e[i], db);
+                        e[i] *= b;
                     }
+                    planes8<NP>(o, fo);
+                    put(fO + wave * NP * kFrag, fo);
+                    planes8<3>(e, f);                   // V'
+                    put(fV + wave * 3 * kFrag, f);
                 }
+                if (part == PARTS - 1) {
 #pragma unroll
-                for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8 *>(fV + (wave * 3 + p) * kFrag + lane * 8) = fv[p];
+                    for (int i = 0; i < 8; ++i) w[i] *= b;
+                    planes8<3>(w, f);                   // beta dV', which is dv
+                    put(fR + wave * 3 * kFrag, f);
+                    if (in) store8<T, VEC>(static_cast<T *>(a.dval) + row, v, a.dv, w);
+                }
             }
             fetch(v + 32);                              // nothing past the last column
             dev::lds_barrier();                         // which leaves those loads in flight
             if (busy) {
+                bf16x8 fo[NP], fr[3], fv[3];
+                load_frags<NP>(fO + wave * NP * kFrag + lane * 8, fo);
+                load_frags<3>(fR + wave * 3 * kFrag + lane * 8, fr);
+                load_frags<3>(fV + wave * 3 * kFrag + lane * 8, fv);
 #pragma unroll
                 for (int n = 0; n < 4; ++n)
                     if (n <= wave) {
                         bf16x8 f[3];
                         load_frags<3>(fV + n * 3 * kFrag + lane * 8, f);
-                        dp[n] = mm<NP, 3>(fo, f, dp[n]);
-                        dl[n] = mm<3, 3>(fr, f, dl[n]);
+                        if (part == 0) pr[0][n] = mm<NP, 3>(fo, f, pr[0][n]);
+                        if (part == PARTS - 1) pr[2 - PARTS][n] = mm<3, 3>(fr, f, pr[2 - PARTS][n]);
                     }
 #pragma unroll
-                for (int n = 0; n < KT; ++n) {
-                    if (n % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+                for (int n = 0; n < HT; ++n) {
                     bf16x8 f[3];
-                    load_frags<3>(fS + n * 3 * kFrag + lane * 8, f);
+                    load_frags<3>(fS + (part * HT + n) * 3 * kFrag + lane * 8, f);
                     gq[n] = mm<NP, 3>(fo, f, gq[n]);
                     gr[n] = mm<3, 3>(fr, f, gr[n]);
-                    load_frags<3>(fD + n * 3 * kFrag + lane * 8, f);
+                    load_frags<3>(fD + (part * HT + n) * 3 * kFrag + lane * 8, f);
                     gw[n] = mm<3, 3>(fv, f, gw[n]);
                 }
             }
@@ -409,19 +427,32 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
         // dbeta: a row's four lanes
         db += __shfl_xor(db, 16);
         db += __shfl_xor(db, 32);
-        if (g == 0 && in) a.dbeta[(int64_t)(c.begin + token) * a.hv + h] = db;
+        if (part == 0 && g == 0 && in) a.dbeta[(int64_t)(c.begin + token) * a.hv + h] = db;
+        // K^T's and Q^T's pieces of this wave, a few ahead of their use.
+        constexpr int AHEAD = 2;
+        bf16x8 fk[AHEAD][NP], fq[AHEAD][NP];
+        const auto ask = [&](int i) {                   // piece i: k step i / HT, row tile i % HT
+            const int at = ((part * HT + i % HT) * 2 + i / HT) * NP * kFrag;
+            load_frags<NP>(a.kt + (keys + at) + lane * 8, fk[i % AHEAD]);
+            load_frags<NP>(a.qt + (keys + at) + lane * 8, fq[i % AHEAD]);
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) ask(i);
         // Where this lane's results lie in k and q: offsets from bases that the wave
         // shares, clamped into the rows (results there are 0).
         const T *kbase = static_cast<const T *>(a.k) + (int64_t)c.begin * a.ks + hk * a.dk;
         const T *qbase = static_cast<const T *>(a.q) + (int64_t)c.begin * a.qs + hk * a.dk;
-        uint32_t krow[4], qrow[4], dcol[KT];
+        T kr[4][HT], qr[4][HT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            krow[j] = min(row4 + j, c.len - 1) * (uint32_t)a.ks;
-            qrow[j] = min(row4 + j, c.len - 1) * (uint32_t)a.qs;
-        }
+            const uint32_t t = min(row4 + j, c.len - 1);
 #pragma unroll
-        for (int n = 0; n < KT; ++n) dcol[n] = min(n * 16 + (int)r, a.dk - 1);
+            for (int n = 0; n < HT; ++n) {
+                const uint32_t d = min((part * HT + n) * 16 + (int)r, a.dk - 1);
+                kr[j][n] = kbase[t * (uint32_t)a.ks + d];
+                qr[j][n] = qbase[t * (uint32_t)a.qs + d];
+            }
+        }
         const double last = cs[kC - 1];
         // the pairs' weights
 #pragma unroll
@@ -430,8 +461,8 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
             for (int j = 0; j < 4; ++j) {
                 const int t = row4 + j, u = n * 16 + (int)r;
                 const float d = u <= t && n <= wave ? decay(cs[t] - cs[u]) : 0.f;
-                x[t * kLd + u] = u <= t ? dp[n][j] * d * a.scale : 0.f;
-                y[t * kLd + u] = u < t ? -dl[n][j] * d : 0.f;
+                if (part == 0) x[t * kLd + u] = u <= t ? pr[0][n][j] * d * a.scale : 0.f;
+                if (part == PARTS - 1) y[t * kLd + u] = u < t ? -pr[2 - PARTS][n][j] * d : 0.f;
             }
         // The memory's part of the sums, before the pairs' is added.
         float wsum = 0.f;
@@ -439,35 +470,20 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
         for (int j = 0; j < 4; ++j) {
             const int t = row4 + j;
             const float grown = decay(cs[t]), left = decay(last - cs[t]);
-            float s = 0.f;
 #pragma unroll
-            for (int n = 0; n < KT; ++n) {
+            for (int n = 0; n < HT; ++n) {
                 gq[n][j] *= grown * a.scale;
                 gr[n][j] *= -grown;
                 gw[n][j] *= left;
-                s = fmaf(gw[n][j], to_float(kbase[krow[j] + dcol[n]]), s);
+                wsum = fmaf(gw[n][j], to_float(kr[j][n]), wsum);
             }
-            wsum += s;
         }
-        wsum = across(wsum);
-        wsum += __shfl_xor(wsum, 16);
-        wsum += __shfl_xor(wsum, 32);
-        float all = dot * decay(last);
+        float all = fmaf(dot, decay(last), wsum);
 #pragma unroll
         for (int s = 1; s < 64; s <<= 1) all += __shfl_xor(all, s);
-        if (lane == 0) extra[wave] = all + wsum;
-        __syncthreads();
+        if (lane == 0) extra[wave8] = all;
+        dev::lds_barrier();
         if (busy) {
-            // K^T's and Q^T's pieces, a few ahead of their use.
-            constexpr int AHEAD = NP == 1 ? 4 : 2;
-            bf16x8 fk[AHEAD][NP], fq[AHEAD][NP];
-            const auto ask = [&](int i) {               // piece i: k step i / KT, row tile i % KT
-                const int at = (i % KT * 2 + i / KT) * NP * kFrag;
-                load_frags<NP>(a.kt + keys + (lane * 8 + at), fk[i % AHEAD]);
-                load_frags<NP>(a.qt + keys + (lane * 8 + at), fq[i % AHEAD]);
-            };
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) ask(i);
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
                 // rows i of dP e and dL e for the reads, columns for the writes
@@ -489,8 +505,8 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
                     planes8<3>(w, fyt);
                 }
 #pragma unroll
-                for (int n = 0; n < KT; ++n) {
-                    const int i = ks * KT + n;
+                for (int n = 0; n < HT; ++n) {
+                    const int i = ks * HT + n;
                     __builtin_amdgcn_sched_barrier(0);  // or all pieces' loads are hoisted, and spilled
                     if (ks < half) {
                         if (lower) {
@@ -502,7 +518,7 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
                             gw[n] = mm<3, NP>(fyt, fk[i % AHEAD], gw[n]);
                         }
                     }
-                    if (i + AHEAD < 2 * KT) ask(i + AHEAD);
+                    if (i + AHEAD < 2 * HT) ask(i + AHEAD);
                 }
             }
         }
@@ -510,19 +526,22 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
         for (int j = 0; j < 4; ++j) {
             float s = 0.f;
 #pragma unroll
-            for (int n = 0; n < KT; ++n) {
-                s = fmaf(gq[n][j], to_float(qbase[qrow[j] + dcol[n]]), s);
-                s = fmaf(gr[n][j] - gw[n][j], to_float(kbase[krow[j] + dcol[n]]), s);
+            for (int n = 0; n < HT; ++n) {
+                s = fmaf(gq[n][j], to_float(qr[j][n]), s);
+                s = fmaf(gr[n][j] - gw[n][j], to_float(kr[j][n]), s);
                 tq[n][j] = SHARED ? tq[n][j] + gq[n][j] : gq[n][j];
                 tk[n][j] = SHARED ? tk[n][j] + (gr[n][j] + gw[n][j]) : gr[n][j] + gw[n][j];
             }
             s = across(s);
-            if (r == 0) dc[row4 + j] = s;
+            if (r == 0) dc[part][row4 + j] = s;
         }
         __syncthreads();
-        if (wave == 0) {
-            double s = dc[lane];
-            if (lane == kC - 1u) s += ((double)extra[0] + extra[1]) + ((double)extra[2] + extra[3]);
+        if (wave8 == 0) {
+            double s = PARTS > 1 ? (double)dc[0][lane] + dc[PARTS - 1][lane] : (double)dc[0][lane];
+            if (lane == kC - 1u) {
+#pragma unroll
+                for (int i = 0; i < 4 * PARTS; ++i) s += extra[i];
+            }
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) {
                 const double u = __shfl_down(s, d);
@@ -539,12 +558,12 @@ __global__ __launch_bounds__(256, KS == 4 ? 1 : 2) void k_delta_bwd_chunk(DeltaA
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int t = row4 + j;
-        const uint32_t at = t * (uint32_t)(a.hk * a.dk) + r;
 #pragma unroll
-        for (int n = 0; n < KT; ++n) {
-            const bool in = t < c.len && n * 16 + (int)r < a.dk;
-            store_if(in, rq, sizeof(T) * (at + n * 16), from_float<T>(tq[n][j]));
-            store_if(in, rk, sizeof(T) * (at + n * 16), from_float<T>(tk[n][j]));
+        for (int n = 0; n < HT; ++n) {
+            const int d = (part * HT + n) * 16 + (int)r;
+            const uint32_t at = t * (uint32_t)(a.hk * a.dk) + d;
+            store_if(t < c.len && d < a.dk, rq, sizeof(T) * at, from_float<T>(tq[n][j]));
+            store_if(t < c.len && d < a.dk, rk, sizeof(T) * at, from_float<T>(tk[n][j]));
         }
     }
 }
@@ -563,11 +582,11 @@ hipError_t backward_ks(const DeltaArgs &a, hipStream_t s) {
     const auto even = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
     const bool vec = a.dv % 8 == 0 && even(a.dout) && even(a.dval);
     if (a.hv > a.hk) {
-        if (vec) k_delta_bwd_chunk<T, KS, true, true><<<grid, 256, 0, s>>>(a);
-        else k_delta_bwd_chunk<T, KS, false, true><<<grid, 256, 0, s>>>(a);
+        if (vec) k_delta_bwd_chunk<T, KS, true, true><<<grid, KS == 4 ? 512 : 256, 0, s>>>(a);
+        else k_delta_bwd_chunk<T, KS, false, true><<<grid, KS == 4 ? 512 : 256, 0, s>>>(a);
     } else {
-        if (vec) k_delta_bwd_chunk<T, KS, true, false><<<grid, 256, 0, s>>>(a);
-        else k_delta_bwd_chunk<T, KS, false, false><<<grid, 256, 0, s>>>(a);
+        if (vec) k_delta_bwd_chunk<T, KS, true, false><<<grid, KS == 4 ? 512 : 256, 0, s>>>(a);
+        else k_delta_bwd_chunk<T, KS, false, false><<<grid, KS == 4 ? 512 : 256, 0, s>>>(a);
     }
     return hipGetLastError();
 }

@@ -66,6 +66,7 @@ struct DeltaArgs {
     // Backward call:
     const void *dout;
     const float *dfinal;
+    int32_t *map;                 // [slots][2] each chunk slot's first token and length
     float *after;                 // [slots][hv][dk][dv] gradients of the states after each chunk
     float *dwrite;                // [tokens][hv][dv] gradients of what each token wrote, beta err
     void *dq, *dkey, *dval;

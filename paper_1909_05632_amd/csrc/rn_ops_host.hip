@@ -60,6 +60,7 @@ bool too_wide(const rn_delta_shape *s) { return s->dk > RN_DELTA_MAX_DIM || s->d
 struct DeltaSizes {
     size_t states, tokens;                // bytes of a set of states, of [tokens][hv][dv] float32
     size_t keys, inverse, score, decay;   // of kf, qf, kt or qt; mf; pf; dec
+    size_t map;
 };
 
 DeltaSizes sizes(const rn_delta_shape *s) {
@@ -69,7 +70,7 @@ DeltaSizes sizes(const rn_delta_shape *s) {
             round_up((size_t)s->tokens * heads * s->dv * 4),
             round_up(slots * s->heads_k * 4 * delta_ksteps(s->dk) * delta_planes(bf16) * 1024),
             round_up(slots * heads * 6 * 3 * 1024), round_up(slots * heads * 6 * delta_score_planes(bf16) * 1024),
-            round_up(slots * heads * 3 * RN_DELTA_CHUNK * 4)};
+            round_up(slots * heads * 3 * RN_DELTA_CHUNK * 4), round_up(slots * 8)};
 }
 
 DeltaArgs delta_args(const rn_delta_shape *s, const void *q, const void *k, const void *v, const float *g,
@@ -192,7 +193,7 @@ size_t reuse_ops_delta_scratch_bytes(const rn_delta_shape *shape) {
 size_t reuse_ops_delta_backward_scratch_bytes(const rn_delta_shape *shape) {
     if (bad_shape(shape) || too_wide(shape)) return 0;
     const DeltaSizes z = sizes(shape);
-    return 3 * z.keys + 2 * z.inverse + z.decay + z.states + z.tokens + kAlign;
+    return 3 * z.keys + 2 * z.inverse + z.decay + z.states + z.tokens + z.map + kAlign;
 }
 
 rn_status reuse_ops_delta_forward(const rn_delta_shape *shape, const void *q, const void *k, const void *v,
@@ -258,6 +259,7 @@ rn_status reuse_ops_delta_backward(const rn_delta_shape *shape, const void *q, c
     a.dec = reinterpret_cast<float *>(at += z.inverse);
     a.after = reinterpret_cast<float *>(at += z.decay);
     a.dwrite = reinterpret_cast<float *>(at += z.states);
+    a.map = reinterpret_cast<int32_t *>(at += z.tokens);
     a.dq = dq, a.dkey = dk, a.dval = dv, a.dg = dg, a.dbeta = dbeta, a.dstate = dstate;
     return launched(launch_delta_backward(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
 }
