@@ -180,7 +180,7 @@ rn_status reuse_ops_delta_forward(const rn_delta_shape *shape, const void *dev_q
  *   dev_dv:             [tokens][heads_v][dv] dtype, contiguous.
  *   dev_dg, dev_dbeta:  [tokens][heads_v] float32.
  *   dev_dstate:         [n][heads_v][dk][dv] float32, or NULL (not wanted).
- * dev_dstate may be dev_dfinal. */
+ * dev_dstate must not be dev_dfinal. */
 rn_status reuse_ops_delta_backward(const rn_delta_shape *shape, const void *dev_q, const void *dev_k,
                                    const void *dev_v, const float *dev_g, const float *dev_beta,
                                    const int32_t *dev_seq_off, const void *dev_saved, size_t saved_bytes,

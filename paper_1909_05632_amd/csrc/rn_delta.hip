@@ -126,6 +126,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
     const int seq = blockIdx.x / a.hv, h = blockIdx.x % a.hv, hk = h / (a.hv / a.hk);
     const int v0 = blockIdx.y * VT;
     const Span span = span_of(a, seq);
+    if (span.len <= a.short_len) return;                // taken token by token
     const int chunks = (span.len + kC - 1) / kC;
     const int64_t slot0 = slot_of(span, seq, 0);
     const int64_t sbase = ((int64_t)seq * a.hv + h) * a.dk * a.dv + v0;
@@ -336,8 +337,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
 
 template <class T, int KS>
 hipError_t forward_ks(const DeltaArgs &a, hipStream_t s) {
-    if (a.tokens > 0)
-        if (hipError_t e = launch_operands<T, KS, false>(a, s)) return e;
+    if (hipError_t e = launch_operands<T, KS, false>(a, s)) return e;
     const auto walk = [&](auto ct) {
         constexpr int CT = decltype(ct)::value;
         const dim3 grid(a.n * a.hv, (a.dv + 16 * CT - 1) / (16 * CT));
@@ -368,7 +368,13 @@ hipError_t launch_delta_step(const DeltaArgs &a, bool bf16, hipStream_t s) {
     return hipGetLastError();
 }
 
-hipError_t launch_delta_forward(const DeltaArgs &a, bool bf16, hipStream_t s) {
+hipError_t launch_delta_forward(const DeltaArgs &args, bool bf16, hipStream_t s) {
+    DeltaArgs a = args;
+    const DeltaWays w = delta_ways(a);
+    a.short_len = w.tokens ? kShort : -1;
+    if (w.tokens)
+        if (hipError_t e = launch_delta_short_forward(a, bf16, s)) return e;
+    if (!w.chunks) return hipSuccess;
     return bf16 ? forward<bf16_t>(a, s) : forward<float>(a, s);
 }
 

@@ -43,6 +43,8 @@ __device__ inline int slot_of(const Span &s, int i, int chunk) { return s.begin 
 // not beyond it.  Slots that no chunk has give len 0.
 struct Chunk {
     int seq, begin, len;          // tokens begin .. begin + len - 1, len <= 64
+    int whole;                    // tokens of the sequence
+    bool last;                    // the sequence's last chunk
 };
 __device__ inline Chunk chunk_of(const DeltaArgs &a, int slot) {
     int lo = 0, hi = a.n - 1;
@@ -53,8 +55,8 @@ __device__ inline Chunk chunk_of(const DeltaArgs &a, int slot) {
     }
     const Span s = span_of(a, lo);
     const int64_t at = (int64_t)(slot - slot_of(s, lo, 0)) * kC;
-    if (at < 0 || at >= s.len) return {lo, 0, 0};
-    return {lo, s.begin + (int)at, min(kC, s.len - (int)at)};
+    if (at < 0 || at >= s.len) return {lo, 0, 0, 0, false};
+    return {lo, s.begin + (int)at, min(kC, s.len - (int)at), s.len, at + kC >= s.len};
 }
 
 // Log decays (base 2) summed up to each token of a chunk, in double: differences
@@ -188,8 +190,14 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     __shared__ float beta[kC];
     const int slot = blockIdx.x, h = blockIdx.y, group = a.hv / a.hk, hk = h / group;
     const Chunk c = chunk_of(a, slot);
-    if (BWD && h == 0 && threadIdx.x == 0) a.map[2 * slot] = c.begin, a.map[2 * slot + 1] = c.len;
+    if (BWD && h == 0 && threadIdx.x == 0) {
+        int32_t *m = a.map + 4 * slot;
+        m[0] = c.begin, m[1] = c.len, m[2] = c.seq, m[3] = c.last;
+    }
     if (c.len == 0) return;
+    // A sequence that goes token by token needs K^T and Q^T only, for the chunks' gradients.
+    const bool keys_only = c.whole <= a.short_len;
+    if (keys_only && (!BWD || h % (a.hv / a.hk))) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int blocks = (c.len + 15) / 16;               // 16s of tokens
     const bool first = h % group == 0, busy = wave < blocks;
@@ -282,6 +290,7 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     if (first) transpose(skf, a.kt);
     if constexpr (BWD)
         if (first) transpose(sqf, a.qt);
+    if (keys_only) return;
     __syncthreads();                                    // K's fragments have been read
 #pragma unroll
     for (int n = 0; n < 4; ++n) {

@@ -39,6 +39,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
     const int seq = blockIdx.x / a.hv, h = blockIdx.x % a.hv, hk = h / (a.hv / a.hk);
     const int v0 = blockIdx.y * VT;
     const Span span = span_of(a, seq);
+    if (span.len <= a.short_len) return;                // taken token by token
     const int chunks = (span.len + kC - 1) / kC;
     const int64_t slot0 = slot_of(span, seq, 0);
     const int64_t sbase = ((int64_t)seq * a.hv + h) * a.dk * a.dv + v0;
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
         const bool busy = wave * 16 < len;              // any token of this wave
         const bool half2 = len > 32;                    // tokens in the second 32
         grown = next_grown, left = next_left, beta = next_beta, whole = next_whole;
-        write_state(a.after + ch * a.dk * a.dv + v0);
+        if (chunk + 1 < chunks) write_state(a.after + ch * a.dk * a.dv + v0);
         f32x4 o[CT];
 #pragma unroll
         for (int n = 0; n < CT; ++n) {
@@ -294,7 +295,7 @@ __global__ __launch_bounds__(KS == 4 ? 512 : 256, 2) void k_delta_bwd_chunk(Delt
     __shared__ double cs[kC];
     __shared__ float beta_s[kC], dc[PARTS][kC], extra[4 * PARTS];
     const int slot = blockIdx.x, hk = blockIdx.y, group = a.hv / a.hk;
-    const Chunk c{0, a.map[2 * slot], a.map[2 * slot + 1]};
+    const Chunk c{a.map[4 * slot + 2], a.map[4 * slot], a.map[4 * slot + 1], 0, a.map[4 * slot + 3] != 0};
     if (c.len == 0) return;
     const int wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = wave8 & 3;
     const int part = PARTS > 1 ? wave8 >> 2 : 0;
@@ -338,12 +339,15 @@ __global__ __launch_bounds__(KS == 4 ? 512 : 256, 2) void k_delta_bwd_chunk(Delt
         constexpr int W8 = 4 * PARTS, RT = KT > W8 ? KT / W8 : 1;       // row tiles of S and dS' a wave splits
         Raw8<float, VEC> rs[RT], rt[RT], rw, re;
         Raw8<T, VEC> ro;
+        // the gradient of the memory after the chunk: dfinal after a sequence's last
+        const float *after = c.last ? a.dfinal + ((int64_t)c.seq * a.hv + h) * a.dk * a.dv : a.after + ch * a.dk * a.dv;
+        const bool no_after = c.last && !a.dfinal;
         const auto fetch = [&](int v) {
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
                 const int d = (wave8 + W8 * i) * 16 + (int)r;
                 rs[i].load(a.before + (ch * a.dk + d) * a.dv, d < a.dk, v, a.dv);
-                rt[i].load(a.after + (ch * a.dk + d) * a.dv, d < a.dk, v, a.dv);
+                rt[i].load(after + (int64_t)d * a.dv, d < a.dk && !no_after, v, a.dv);
             }
             if (part == 0) re.load(a.err + row, in, v, a.dv);
             if (part == 0) ro.load(static_cast<const T *>(a.dout) + row, in, v, a.dv);
@@ -572,15 +576,17 @@ template <class T, int KS>
 hipError_t backward_ks(const DeltaArgs &a, hipStream_t s) {
     if (a.tokens > 0)
         if (hipError_t e = launch_operands<T, KS, true>(a, s)) return e;
-    // One column tile a block or two, as in the forward walk.
-    if (a.dv <= 16 || a.n * a.hv * ((a.dv + 31) / 32) <= 256)
-        k_delta_bwd_walk<T, KS, 1><<<dim3(a.n * a.hv, (a.dv + 15) / 16), 256, 0, s>>>(a);
-    else k_delta_bwd_walk<T, KS, 2><<<dim3(a.n * a.hv, (a.dv + 31) / 32), 256, 0, s>>>(a);
-    if (hipError_t e = hipGetLastError()) return e;
+    if (delta_ways(a).chunks) {
+        // One column tile a block or two, as in the forward walk.
+        if (a.dv <= 16 || a.n * a.hv * ((a.dv + 31) / 32) <= 256)
+            k_delta_bwd_walk<T, KS, 1><<<dim3(a.n * a.hv, (a.dv + 15) / 16), 256, 0, s>>>(a);
+        else k_delta_bwd_walk<T, KS, 2><<<dim3(a.n * a.hv, (a.dv + 31) / 32), 256, 0, s>>>(a);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
     if (a.tokens == 0) return hipSuccess;
     const dim3 grid((int)delta_chunk_slots(a.tokens, a.n), a.hk);
     const auto even = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
-    const bool vec = a.dv % 8 == 0 && even(a.dout) && even(a.dval);
+    const bool vec = a.dv % 8 == 0 && even(a.dout) && even(a.dval) && even(a.dfinal);
     if (a.hv > a.hk) {
         if (vec) k_delta_bwd_chunk<T, KS, true, true><<<grid, KS == 4 ? 512 : 256, 0, s>>>(a);
         else k_delta_bwd_chunk<T, KS, false, true><<<grid, KS == 4 ? 512 : 256, 0, s>>>(a);
@@ -599,7 +605,12 @@ hipError_t backward(const DeltaArgs &a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_delta_backward(const DeltaArgs &a, bool bf16, hipStream_t s) {
+hipError_t launch_delta_backward(const DeltaArgs &args, bool bf16, hipStream_t s) {
+    DeltaArgs a = args;
+    const DeltaWays w = delta_ways(a);
+    a.short_len = w.tokens ? kShort : -1;
+    if (w.tokens)
+        if (hipError_t e = launch_delta_short_backward(a, bf16, s)) return e;
     return bf16 ? backward<bf16_t>(a, s) : backward<float>(a, s);
 }
 

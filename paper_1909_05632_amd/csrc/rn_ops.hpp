@@ -1,6 +1,6 @@
 // Internal declarations of the operators in include/reuse_ops.h: kernel
-// launchers (rn_norm.hip, rn_sample.hip, rn_delta.hip, rn_delta_bwd.hip) and
-// device helpers they share.
+// launchers (rn_norm.hip, rn_sample.hip, rn_delta.hip, rn_delta_short.hip,
+// rn_delta_bwd.hip) and device helpers they share.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -50,6 +50,7 @@ struct DeltaArgs {
     const float *g, *beta;
     const int32_t *off;           // [n+1], or NULL: even lengths
     const int32_t *ids;           // step: slots, or NULL
+    int short_len;                // sequences up to this length go token by token (-1: none)
     int slots;
     const float *state;           // first states, or NULL
     float *final_state;           // last states, or NULL (step: the state pool)
@@ -66,8 +67,8 @@ struct DeltaArgs {
     // Backward call:
     const void *dout;
     const float *dfinal;
-    int32_t *map;                 // [slots][2] each chunk slot's first token and length
-    float *after;                 // [slots][hv][dk][dv] gradients of the states after each chunk
+    int32_t *map;                 // [slots][4] each chunk slot's first token, length, sequence, whether its last
+    float *after;                 // [slots][hv][dk][dv] gradients of the states after each chunk but a sequence's last
     float *dwrite;                // [tokens][hv][dv] gradients of what each token wrote, beta err
     void *dq, *dkey, *dval;
     float *dg, *dbeta, *dstate;
@@ -80,7 +81,27 @@ inline int delta_ksteps(int dk) { return dk <= 32 ? 1 : dk <= 64 ? 2 : 4; }
 // bf16 planes of an input, and of P (the backward call has three of P).
 inline int delta_planes(bool bf16) { return bf16 ? 1 : 3; }
 inline int delta_score_planes(bool bf16) { return bf16 ? 2 : 3; }
+// Token by token a sequence takes about 0.3 us a token and no scratch; by chunks
+// the operands and the walk cost as much as some 35 tokens whatever the chunk
+// holds (measured at dk 64 and 128), so short sequences go token by token.
+constexpr int kShort = 32;
+// Which of the two ways a call has sequences for; lengths are on the device, so
+// ragged calls of few tokens a sequence launch both, and each takes its own.
+struct DeltaWays {
+    bool tokens, chunks;
+};
+inline DeltaWays delta_ways(const DeltaArgs &a) {
+    if (a.tokens == 0 || !a.off) {
+        const bool t = a.tokens <= (int64_t)kShort * a.n;
+        return {t, !t};
+    }
+    if (a.tokens <= kShort) return {true, false};
+    const bool t = a.tokens <= (int64_t)kShort * a.n;
+    return {t, true};
+}
 hipError_t launch_delta_step(const DeltaArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_delta_short_forward(const DeltaArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_delta_short_backward(const DeltaArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_delta_forward(const DeltaArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_delta_backward(const DeltaArgs &a, bool bf16, hipStream_t s);
 

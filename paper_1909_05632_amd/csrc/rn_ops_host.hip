@@ -70,7 +70,7 @@ DeltaSizes sizes(const rn_delta_shape *s) {
             round_up((size_t)s->tokens * heads * s->dv * 4),
             round_up(slots * s->heads_k * 4 * delta_ksteps(s->dk) * delta_planes(bf16) * 1024),
             round_up(slots * heads * 6 * 3 * 1024), round_up(slots * heads * 6 * delta_score_planes(bf16) * 1024),
-            round_up(slots * heads * 3 * RN_DELTA_CHUNK * 4), round_up(slots * 8)};
+            round_up(slots * heads * 3 * RN_DELTA_CHUNK * 4), round_up(slots * 16)};
 }
 
 DeltaArgs delta_args(const rn_delta_shape *s, const void *q, const void *k, const void *v, const float *g,
@@ -239,6 +239,7 @@ rn_status reuse_ops_delta_backward(const rn_delta_shape *shape, const void *q, c
     if (shape->n == 0) return RN_OK;
     if (shape->tokens > 0 && (!dout || !dq || !dk || !dv || !dg || !dbeta))
         return fail(RN_EINVAL, "dout and the gradients must not be NULL");
+    if (dstate && dstate == dfinal) return fail(RN_EINVAL, "dstate must not be dfinal");
     if (!saved || !scratch) return fail(RN_EINVAL, "saved and scratch must not be NULL");
     if (misaligned(saved) || misaligned(scratch)) return fail(RN_EINVAL, "saved and scratch must be 256-byte aligned");
     if (saved_bytes < reuse_ops_delta_saved_bytes(shape)) return need_bytes("saved", reuse_ops_delta_saved_bytes(shape));

@@ -92,6 +92,15 @@ def test_odd_head_sizes(dk, dv):
         _compare(x, off, 0.3, (dk, dv, dtype))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("hk,hv,dk,dv", [(1, 2, 128, 128), (2, 2, 64, 70), (1, 1, 20, 16)])
+@pytest.mark.parametrize("lengths", [[3] * 11, [32, 33, 1, 0, 31, 2, 70, 5, 9, 4], [31, 1], [20]])
+def test_short_and_long_sequences_in_one_call(lengths, hk, hv, dk, dv, dtype):
+    """Sequences up to 32 tokens may go another way than longer ones; both in one batch."""
+    x, off = _inputs(lengths, hk, hv, dk, dv, dtype, seed=len(lengths))
+    _compare(x, off, dk ** -0.5, lengths)
+
+
 def test_long_sequence_of_near_equal_keys():
     """Frames that hardly change: keys almost parallel, so the triangular systems are far from the identity."""
     x, off = _inputs([600], 1, 2, 64, 64, F32, near=8.0, decay=(1e-4, 1e-2))

@@ -153,6 +153,7 @@ def test_delta_arguments():
     _err(back(saved_bytes=kept - 1), B.RN_ENOSPACE, "saved")
     _err(back(bytes=need - 1), B.RN_ENOSPACE, "scratch")
     _err(back(saved=P + 64), B.RN_EINVAL, "aligned")
+    _err(back(dfinal=2 * P, dstate=2 * P), B.RN_EINVAL, "dfinal")
     one = _shape(tokens=2)
     step = dict(shape=ctypes.byref(one), q=P, k=P, v=P, g=P, beta=P, ids=None, slots=2, state=P, out=P, stream=None)
 
