@@ -74,8 +74,8 @@ rn_status reuse_ops_layer_norm_backward(int64_t rows, int32_t width, const void 
 /* Settings of a sampling call: each is one value for every row, or an array on
  * the device with a value per row where the pointer is not NULL. */
 typedef struct {
-    float temperature;            /* > 0; 0 or less, NaN, or so small that log2(e) / temperature
-                                     overflows: greedy (the largest logit, the lowest index of equal ones) */
+    float temperature;            /* > 0; 0 or less, NaN, or below 1.4e-37: greedy (the largest logit, the
+                                     lowest index of equal ones) */
     int32_t top_k;                /* keep the k largest logits; 0 or less: all */
     float top_p;                  /* keep the fewest that hold this share of the probability, one at least */
     float min_p;                  /* keep those with at least this share of the largest one's probability */

@@ -30,7 +30,7 @@ __device__ inline Row row_settings(const rn_sample_params &p, int r) {
     Row q;
     const float t = p.dev_temperature ? p.dev_temperature[r] : p.temperature;
     q.c = kLog2e / t;
-    q.greedy = !(t > 0.f) || !(q.c < kInf);
+    q.greedy = !(t > 0.f) || !(q.c * 32.f < kInf);
     const int k = p.dev_top_k ? p.dev_top_k[r] : p.top_k;
     q.top_k = k > 0 ? k : 0;
     const float tp = p.dev_top_p ? p.dev_top_p[r] : p.top_p;
@@ -142,15 +142,25 @@ __global__ __launch_bounds__(256) void k_sample_wave(SampleArgs a) {
 
 constexpr int kBins = 1024;
 
-// One block of NT threads a row; the row is streamed from memory (from the
-// caches after the first time) once for each question asked of it:
+// One block of NT threads a row, which is streamed (from the caches after the first
+// time) once for each question asked of it:
 //   the largest logit;
-//   the histogram of z in steps of 1/32 (counts for top-k, weights for top-p),
-//     which gives the bin a threshold lies in;
-//   histograms of the keys within that bin, 1024 steps at a time, until a step
-//     is one key: one or two more;
+//   the histogram of z in steps of 1/32 (counts for top-k and min-p, weights for
+//     top-p), which gives the bin a threshold lies in.
+// Where kPairs logits or fewer lie down to that bin they are put into a list, in
+// index order, and each thread ranks one of them against all others: no further
+// reading.  Otherwise
+//   histograms of the keys within the bin, 1024 steps at a time, until a step is
+//     one key: one or two more;
 //   the weights that stay, by contiguous parts of the row, then of the part the
 //     draw falls into, down to one wave's vector.
+//
+// One CU works on a row, so a reading is bound by what it has in flight: four
+// vectors a thread are on their way while one is looked at (256 rows of 131072
+// bfloat16: 12 us for the first reading without, 5 with).
+constexpr int kPairs = 512;
+constexpr int kAhead = 4;
+
 template <class T, int VEC, int NT>
 struct Block {
     static constexpr int NW = NT / 64;
@@ -163,19 +173,26 @@ struct Block {
 
     // f(index, logit) for the elements [lo, hi), thread by thread in vectors.
     template <class F>
-    __device__ void each(int lo, int hi, int first, int step, F &&f) const {
-        for (int i = lo + first * VEC; i < hi; i += step * VEC) {
-            if (VEC > 1 && i + VEC <= hi) {
-                const Pack<T, VEC> p = *reinterpret_cast<const Pack<T, VEC> *>(x + i);
+    __device__ __forceinline__ void each(int lo, int hi, int first, int step, F &&f) const {
+        using P = Pack<T, VEC>;
+        const int stride = step * VEC;
+        int i = lo + first * VEC;
+        P p[kAhead];
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) f(i + j, canonical(to_float(p.v[j])));
-            } else {
-                for (int j = 0; j < VEC && i + j < hi; ++j) f(i + j, canonical(to_float(x[i + j])));
-            }
+        for (int u = 0; u < kAhead; ++u)
+            if (i + u * stride + VEC <= hi) p[u] = *reinterpret_cast<const P *>(x + i + u * stride);
+        for (; i + VEC <= hi; i += stride) {
+            const P now = p[0];
+#pragma unroll
+            for (int u = 0; u + 1 < kAhead; ++u) p[u] = p[u + 1];
+            if (i + kAhead * stride + VEC <= hi) p[kAhead - 1] = *reinterpret_cast<const P *>(x + i + kAhead * stride);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) f(i + j, canonical(to_float(now.v[j])));
         }
+        for (; i < hi; ++i) f(i, canonical(to_float(x[i])));      // a last vector's part: one thread's
     }
     template <class F>
-    __device__ void all(F &&f) const { each(0, vocab, threadIdx.x, NT, f); }
+    __device__ __forceinline__ void all(F &&f) const { each(0, vocab, threadIdx.x, NT, f); }
 
     __device__ void clear() const {
         for (int i = threadIdx.x; i < kBins; i += NT) hw[i] = 0, hc[i] = 0;
@@ -190,7 +207,7 @@ struct Block {
         uint64_t weight, in_weight;
     };
     template <class P>
-    __device__ Found find(P &&reached) const {
+    __device__ __forceinline__ Found find(P &&reached) const {
         constexpr int PER = kBins / NT;
         __syncthreads();
         uint64_t w = 0;
@@ -237,6 +254,8 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
     constexpr int NW = NT / 64;
     __shared__ uint64_t hw[kBins], part[NW + 2];
     __shared__ uint32_t hc[kBins], ties[NW + 2], bound[2];
+    __shared__ uint32_t pair_key[kPairs], pair_weight[kPairs];
+    __shared__ int pair_at[kPairs];
     const int r = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Row q = row_settings(a.p, r);
     const B b{static_cast<const T *>(a.logits) + r * a.stride, a.vocab, hw, hc, part, ties};
@@ -276,6 +295,148 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
     float cut = -kInf;
     uint32_t equals = 0, equal_weight = 0;
     const bool use_k = q.top_k > 0 && q.top_k < a.vocab, use_p = q.top_p < 1.f;
+    uint64_t all_weights = 0;
+    constexpr int PER = kBins / NT;
+    if (use_k || use_p || q.min_p > 0.f) {
+        b.clear();
+        b.all([&](int, float l) {
+            const float z = z_of(l, m, q.c);
+            if (z > -32.f) {
+                const int s = (int)(z * -32.f);
+                atomicAdd(&hc[s], 1u);
+                if (use_p) {
+                    const uint32_t w = weight_of(z, q.min_p);
+                    if (w) atomicAdd((unsigned long long *)&hw[s], (unsigned long long)w);
+                }
+            }
+        });
+        __syncthreads();
+        // The last bin that anything may stay of: min-p's, and one more for rounding
+        // (NaN and infinities of its logarithm do not occur, it is above 0 and at most 1) ...
+        int last = kBins - 1;
+        if (q.min_p > 0.f) last = min(last, (int)fminf(log2f(q.min_p) * -32.f, (float)kBins) + 1);
+        // ... the k-th largest's, or the one in which top-p's share is reached.
+        if (use_p) {
+            uint64_t w = 0;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) w += hw[threadIdx.x * PER + j];
+            w = wave_sum(w);
+            if (lane == 0) part[wave] = w;
+            __syncthreads();
+            for (int i = 0; i < NW; ++i) all_weights += part[i];
+            __syncthreads();
+        }
+        if (use_k) last = min(last, b.find([&](uint32_t c, uint64_t) { return c >= (uint32_t)q.top_k; }).bin);
+        else if (use_p) {
+            const double limit = fmax((double)q.top_p * (double)all_weights, 0.5);
+            last = min(last, b.find([&](uint32_t, uint64_t w) { return (double)w >= limit; }).bin);
+        }
+        uint32_t n = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if ((int)threadIdx.x * PER + j <= last) n += hc[threadIdx.x * PER + j];
+        n = (uint32_t)wave_sum(n);
+        if (lane == 0) ties[wave] = n;
+        __syncthreads();
+        n = 0;
+        for (int i = 0; i < NW; ++i) n += ties[i];
+        __syncthreads();
+        if (n <= kPairs) {
+            // The list, in index order: each wave's part of the row, counted first.
+            const auto chosen = [&](float l) {
+                const float z = z_of(l, m, q.c);
+                return z > -32.f && (int)(z * -32.f) <= last;
+            };
+            const int grain = 64 * VEC, share = ((a.vocab + NW - 1) / NW + grain - 1) / grain * grain;
+            const int from = min(a.vocab, wave * share), to = min(a.vocab, from + share);
+            uint32_t mine = 0;
+            b.each(from, to, lane, 64, [&](int, float l) { mine += chosen(l); });
+            mine = (uint32_t)wave_sum(mine);
+            if (lane == 0) ties[wave] = mine;
+            __syncthreads();
+            if (mine) {
+                uint32_t at = 0;
+                for (int i = 0; i < wave; ++i) at += ties[i];
+                for (int base = from; base < to; base += grain) {
+                    uint32_t here = 0;
+                    b.each(base, min(to, base + grain), lane, 64, [&](int, float l) { here += chosen(l); });
+                    if (!__ballot(here != 0)) continue;
+                    const uint32_t upto = (uint32_t)wave_scan(here);
+                    uint32_t place = at + upto - here;
+                    if (here)
+                        b.each(base, min(to, base + grain), lane, 64, [&](int i, float l) {
+                            if (!chosen(l)) return;
+                            pair_key[place] = key_of(l);
+                            pair_weight[place] = weight_of(z_of(l, m, q.c), q.min_p);
+                            pair_at[place++] = i;
+                        });
+                    at += __shfl(upto, 63);
+                }
+            }
+            __syncthreads();
+            // As in k_sample_wave: what comes before each in descending order.  Two a
+            // thread where there are fewer threads.
+            constexpr int TWO = kPairs > NT ? kPairs / NT : 1;
+            uint64_t kept[TWO];
+            bool in_k[TWO];
+            uint64_t before[TWO];
+            uint64_t sum = 0;
+#pragma unroll
+            for (int o = 0; o < TWO; ++o) {
+                const uint32_t i = threadIdx.x * TWO + o;   // neighbours, so that scans are in index order
+                before[o] = 0, in_k[o] = false, kept[o] = 0;
+                if (i < n) {
+                    const uint32_t key = pair_key[i];
+                    int rank = 0;
+                    for (uint32_t t = 0; t < n; ++t) {
+                        const uint32_t kt = pair_key[t];
+                        const bool ahead = kt > key || (kt == key && t < i);
+                        rank += ahead;
+                        before[o] += ahead ? pair_weight[t] : 0;
+                    }
+                    in_k[o] = !use_k || rank < q.top_k;
+                    kept[o] = in_k[o] ? pair_weight[i] : 0;
+                    sum += kept[o];
+                }
+            }
+            uint64_t total = all_weights;
+            if (use_k || !use_p) {                          // all that top-p takes its share of is in the list
+                sum = wave_sum(sum);
+                if (lane == 0) part[wave] = sum;
+                __syncthreads();
+                total = 0;
+                for (int i = 0; i < NW; ++i) total += part[i];
+                __syncthreads();
+            }
+            const double limit = (double)q.top_p * (double)total;
+            uint64_t mine_kept = 0;
+#pragma unroll
+            for (int o = 0; o < TWO; ++o) {
+                if (use_p && !(before[o] == 0 || (double)before[o] < limit)) kept[o] = 0;
+                mine_kept += kept[o];
+            }
+            uint64_t upto = wave_scan(mine_kept);
+            if (lane == 63) part[wave] = upto;
+            __syncthreads();
+            total = 0;
+            for (int i = 0; i < NW; ++i) {
+                if (i == wave) upto += total;
+                total += part[i];
+            }
+            const uint64_t target = target_of(a.u[r], total);
+            uint64_t run = upto - mine_kept;
+#pragma unroll
+            for (int o = 0; o < TWO; ++o) {
+                if (run <= target && run + kept[o] > target) {
+                    const uint32_t i = threadIdx.x * TWO + o;
+                    a.tokens[r] = pair_at[i];
+                    if (a.logprobs) a.logprobs[r] = log_share(z_of(of_key(pair_key[i]), m, q.c), total);
+                }
+                run += kept[o];
+            }
+            return;
+        }
+    }
     if (use_k || use_p) {
         const auto bin_of = [&](float l) {          // descending logits have ascending bins
             const float z = z_of(l, m, q.c);
@@ -289,18 +450,28 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
             uint64_t weight;
         };
         const auto narrow = [&](typename B::Found f, float above, auto &&reached) {
-            // The keys of the bin: binary search of its two edges, by two threads.
-            if (threadIdx.x < 2) {
-                uint32_t lo = key_of(-kInf), hi = key_of(m);       // the least key with a bin <= f.bin - edge
-                const int most = f.bin - (int)threadIdx.x;
-                while (lo < hi) {
-                    const uint32_t mid = lo + (hi - lo) / 2;
-                    if (bin_of(of_key(mid)) <= most) hi = mid;
-                    else lo = mid + 1;
+            // The keys of the bin: its two edges, each searched by one wave, 64 places at
+            // once.  Wave 0: the least key with a bin up to this one; wave 1: the least with
+            // a bin before it, whose neighbour below is the bin's greatest (key_of(m) for
+            // bin 0).
+            if (wave < 2) {
+                uint32_t lo = key_of(-kInf), hi = key_of(m);
+                const int most = f.bin - wave;
+                if (most >= 0) {
+                    while (lo < hi) {                      // the answer lies in [lo, hi]
+                        const uint32_t width = (hi - lo + 63) / 64;
+                        const uint32_t probe = lo + min(hi - lo, (uint32_t)lane * width);
+                        const uint64_t yes = __ballot(bin_of(of_key(probe)) <= most);
+                        const int first = yes ? __ffsll((unsigned long long)yes) - 1 : 64;
+                        if (first == 0) hi = lo;
+                        else {
+                            const uint32_t below = lo + min(hi - lo, (uint32_t)(first - 1) * width);
+                            if (first < 64) hi = lo + min(hi - lo, (uint32_t)first * width);
+                            lo = below + 1;
+                        }
+                    }
                 }
-                // thread 0: the bin's least key; thread 1: the least key of the bins before
-                // it, or, where there is none, key_of(m), which belongs to this bin.
-                bound[threadIdx.x] = threadIdx.x && f.bin > 0 ? lo - 1 : threadIdx.x ? key_of(m) : lo;
+                if (lane == 0) bound[wave] = wave == 0 ? lo : f.bin > 0 ? lo - 1 : key_of(m);
             }
             __syncthreads();
             uint32_t lo = bound[0], hi = bound[1];
@@ -328,19 +499,7 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
             }
         };
 
-        b.clear();
-        b.all([&](int, float l) {
-            const float z = z_of(l, m, q.c);
-            if (z > -32.f) {
-                const int s = (int)(z * -32.f);
-                if (use_k) atomicAdd(&hc[s], 1u);
-                const uint32_t w = weight_of(z, q.min_p);
-                if (w) atomicAdd((unsigned long long *)&hw[s], (unsigned long long)w);
-            }
-        });
-        __syncthreads();
         // The histogram is needed again for top-p: its bins are kept in registers.
-        constexpr int PER = kBins / NT;
         uint64_t keep_w[PER];
 #pragma unroll
         for (int j = 0; j < PER; ++j) keep_w[j] = hw[threadIdx.x * PER + j];
@@ -359,16 +518,7 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
         }
         if (use_p) {
             __syncthreads();
-            if (!cut_by_k) {
-                uint64_t s = 0;
-#pragma unroll
-                for (int j = 0; j < PER; ++j) s += keep_w[j];
-                s = wave_sum(s);
-                if (lane == 0) part[wave] = s;
-                __syncthreads();
-                for (int k = 0; k < NW; ++k) total += part[k];
-                __syncthreads();
-            }
+            if (!cut_by_k) total = all_weights;
             // Elements before which less than `limit` lies stay; the first has nothing before it.
             const double limit = fmax((double)q.top_p * (double)total, 0.5);
             const auto fill = [&](float logit, uint32_t count, uint64_t before) {
