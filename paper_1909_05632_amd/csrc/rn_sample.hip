@@ -42,11 +42,15 @@ __device__ inline Row row_settings(const rn_sample_params &p, int r) {
 
 // NaN counts as -infinity, -0 as +0, so that order and equality are those of the key.
 __device__ inline float canonical(float l) { return l == l ? l + 0.f : -kInf; }
+// Bfloat16's keys have 16 bits, for their lower half would tell nothing.
+template <class T>
 __device__ inline uint32_t key_of(float l) {
-    const uint32_t b = __float_as_uint(l);
-    return b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u);
+    const uint32_t b = __float_as_uint(canonical(l));
+    return (b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u)) >> (32 - 8 * sizeof(T));
 }
+template <class T>
 __device__ inline float of_key(uint32_t k) {
+    if (sizeof(T) == 2) k = k << 16 | (k & 0x8000u ? 0u : 0xffffu);
     return __uint_as_float(k ^ ((int32_t)k < 0 ? 0x80000000u : 0xffffffffu));
 }
 
@@ -81,6 +85,15 @@ __device__ inline uint64_t wave_sum(uint64_t v) {
     for (int d = 32; d; d >>= 1) v += shfl_xor64(v, d);
     return v;
 }
+__device__ inline uint32_t wave_scan32(uint32_t v) {    // inclusive
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t t = __shfl_up(v, d);
+        if (lane >= d) v += t;
+    }
+    return v;
+}
 __device__ inline uint64_t wave_scan(uint64_t v) {      // inclusive
     const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -102,7 +115,7 @@ __global__ __launch_bounds__(256) void k_sample_wave(SampleArgs a) {
     if (r >= a.n) return;
     const Row q = row_settings(a.p, r);
     const bool live = lane < a.vocab;
-    const float l = live ? canonical(to_float(static_cast<const T *>(a.logits)[r * a.stride + lane])) : -kInf;
+    const float l = live ? to_float(static_cast<const T *>(a.logits)[r * a.stride + lane]) : -kInf;
     float m = l;
 #pragma unroll
     for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
@@ -114,7 +127,7 @@ __global__ __launch_bounds__(256) void k_sample_wave(SampleArgs a) {
             logp = 0.f;
         } else {
             const float z = z_of(l, m, q.c);
-            const uint32_t w = live ? weight_of(z, q.min_p) : 0, key = live ? key_of(l) : 0;
+            const uint32_t w = live ? weight_of(z, q.min_p) : 0, key = live ? key_of<T>(l) : 0;
             int rank = 0;
             uint64_t before = 0;
             for (int j = 0; j < a.vocab; ++j) {
@@ -147,9 +160,10 @@ constexpr int kBins = 1024;
 //   the largest logit;
 //   the histogram of z in steps of 1/32 (counts for top-k and min-p, weights for
 //     top-p), which gives the bin a threshold lies in.
-// Where kPairs logits or fewer lie down to that bin they are put into a list, in
-// index order, and each thread ranks one of them against all others: no further
-// reading.  Otherwise
+// Where kPairs logits or fewer lie down to that bin they are put into a list, and
+// each thread compares one of them with all others: no further reading.  (The
+// list's order is that of an atomic counter and changes; nothing computed from it
+// does.)  Otherwise
 //   histograms of the keys within the bin, 1024 steps at a time, until a step is
 //     one key: one or two more;
 //   the weights that stay, by contiguous parts of the row, then of the part the
@@ -157,21 +171,23 @@ constexpr int kBins = 1024;
 //
 // One CU works on a row, so a reading is bound by what it has in flight: four
 // vectors a thread are on their way while one is looked at (256 rows of 131072
-// bfloat16: 12 us for the first reading without, 5 with).
+// bfloat16: 12 us for the first reading without, 7
+// with; with six the whole call is 4 us slower, for the registers it takes).
 constexpr int kPairs = 512;
-constexpr int kAhead = 4;
 
 template <class T, int VEC, int NT>
 struct Block {
-    static constexpr int NW = NT / 64;
+    static constexpr int NW = NT / 64, kAhead = 4;
     const T *x;
     int vocab;
     uint64_t (&hw)[kBins];
     uint32_t (&hc)[kBins];
     uint64_t (&part)[NW + 2];
     uint32_t (&ties)[NW + 2];
+    int &bin;
 
-    // f(index, logit) for the elements [lo, hi), thread by thread in vectors.
+    // f(index, logit) for the elements [lo, hi), thread by thread in vectors.  Logits
+    // come as they are: NaN fails every comparison below, and has no weight.
     template <class F>
     __device__ __forceinline__ void each(int lo, int hi, int first, int step, F &&f) const {
         using P = Pack<T, VEC>;
@@ -187,9 +203,9 @@ struct Block {
             for (int u = 0; u + 1 < kAhead; ++u) p[u] = p[u + 1];
             if (i + kAhead * stride + VEC <= hi) p[kAhead - 1] = *reinterpret_cast<const P *>(x + i + kAhead * stride);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) f(i + j, canonical(to_float(now.v[j])));
+            for (int j = 0; j < VEC; ++j) f(i + j, to_float(now.v[j]));
         }
-        for (; i < hi; ++i) f(i, canonical(to_float(x[i])));      // a last vector's part: one thread's
+        for (; i < hi; ++i) f(i, to_float(x[i]));      // a last vector's part: one thread's
     }
     template <class F>
     __device__ __forceinline__ void all(F &&f) const { each(0, vocab, threadIdx.x, NT, f); }
@@ -215,32 +231,25 @@ struct Block {
 #pragma unroll
         for (int j = 0; j < PER; ++j) w += hw[threadIdx.x * PER + j], c += hc[threadIdx.x * PER + j];
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const uint64_t sw = wave_scan(w), sc = wave_scan(c);
-        if (lane == 63) part[wave] = sw, ties[wave] = (uint32_t)sc;
+        const uint64_t sw = wave_scan(w);
+        const uint32_t sc = wave_scan32(c);
+        if (lane == 63) part[wave] = sw, ties[wave] = sc;
+        if (threadIdx.x == 0) bin = kBins;
         __syncthreads();
         uint64_t bw = sw - w;
-        uint32_t bc = (uint32_t)sc - c;
+        uint32_t bc = sc - c;
         for (int k = 0; k < wave; ++k) bw += part[k], bc += ties[k];
-        int hit = kBins;
+        // The conditions are monotone in the running sums: they turn true in one bin.
         for (int j = 0; j < PER; ++j) {
             const int b = threadIdx.x * PER + j;
-            if (reached(bc + hc[b], bw + hw[b])) {
-                hit = b;
-                break;
-            }
-            bc += hc[b], bw += hw[b];
+            const uint64_t iw = hw[b];
+            const uint32_t ic = hc[b];
+            if (!reached(bc, bw) && reached(bc + ic, bw + iw))
+                bin = b, part[NW] = bw, ties[NW] = bc, part[NW + 1] = iw, ties[NW + 1] = ic;
+            bc += ic, bw += iw;
         }
-        // The conditions are monotone in the running sums: the lowest hit is it.
-        int low = hit;
-#pragma unroll
-        for (int d = 32; d; d >>= 1) low = min(low, __shfl_xor(low, d));
         __syncthreads();
-        if (lane == 0) ties[wave] = low;
-        __syncthreads();
-        for (int k = 0; k < NW; ++k) low = min(low, (int)ties[k]);
-        __syncthreads();
-        if (hit == low && hit < kBins) part[NW] = bw, ties[NW] = bc, part[NW + 1] = hw[hit], ties[NW + 1] = hc[hit];
-        __syncthreads();
+        const int low = bin;
         Found f{low, 0, 0, 0, 0};
         if (low < kBins) f = Found{low, ties[NW], ties[NW + 1], part[NW], part[NW + 1]};
         __syncthreads();
@@ -255,10 +264,10 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
     __shared__ uint64_t hw[kBins], part[NW + 2];
     __shared__ uint32_t hc[kBins], ties[NW + 2], bound[2];
     __shared__ uint32_t pair_key[kPairs], pair_weight[kPairs];
-    __shared__ int pair_at[kPairs];
+    __shared__ int pair_at[kPairs], found, listed;
     const int r = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Row q = row_settings(a.p, r);
-    const B b{static_cast<const T *>(a.logits) + r * a.stride, a.vocab, hw, hc, part, ties};
+    const B b{static_cast<const T *>(a.logits) + r * a.stride, a.vocab, hw, hc, part, ties, found};
 
     // the largest logit
     float m = -kInf;
@@ -342,57 +351,39 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
         for (int i = 0; i < NW; ++i) n += ties[i];
         __syncthreads();
         if (n <= kPairs) {
-            // The list, in index order: each wave's part of the row, counted first.
-            const auto chosen = [&](float l) {
+            if (threadIdx.x == 0) listed = 0;
+            for (int i = threadIdx.x; i < kPairs; i += NT) pair_key[i] = 0, pair_weight[i] = 0, pair_at[i] = INT32_MAX;
+            __syncthreads();
+            b.all([&](int i, float l) {
                 const float z = z_of(l, m, q.c);
-                return z > -32.f && (int)(z * -32.f) <= last;
-            };
-            const int grain = 64 * VEC, share = ((a.vocab + NW - 1) / NW + grain - 1) / grain * grain;
-            const int from = min(a.vocab, wave * share), to = min(a.vocab, from + share);
-            uint32_t mine = 0;
-            b.each(from, to, lane, 64, [&](int, float l) { mine += chosen(l); });
-            mine = (uint32_t)wave_sum(mine);
-            if (lane == 0) ties[wave] = mine;
-            __syncthreads();
-            if (mine) {
-                uint32_t at = 0;
-                for (int i = 0; i < wave; ++i) at += ties[i];
-                for (int base = from; base < to; base += grain) {
-                    uint32_t here = 0;
-                    b.each(base, min(to, base + grain), lane, 64, [&](int, float l) { here += chosen(l); });
-                    if (!__ballot(here != 0)) continue;
-                    const uint32_t upto = (uint32_t)wave_scan(here);
-                    uint32_t place = at + upto - here;
-                    if (here)
-                        b.each(base, min(to, base + grain), lane, 64, [&](int i, float l) {
-                            if (!chosen(l)) return;
-                            pair_key[place] = key_of(l);
-                            pair_weight[place] = weight_of(z_of(l, m, q.c), q.min_p);
-                            pair_at[place++] = i;
-                        });
-                    at += __shfl(upto, 63);
+                if (z > -32.f && (int)(z * -32.f) <= last) {
+                    const int place = atomicAdd(&listed, 1);
+                    pair_key[place] = key_of<T>(l);
+                    pair_weight[place] = weight_of(z, q.min_p);
+                    pair_at[place] = i;
                 }
-            }
+            });
             __syncthreads();
-            // As in k_sample_wave: what comes before each in descending order.  Two a
-            // thread where there are fewer threads.
+            // As in k_sample_wave: what comes before each in descending order (equal ones
+            // by index), then in index order.  Entries past n weigh nothing and rank last.
             constexpr int TWO = kPairs > NT ? kPairs / NT : 1;
-            uint64_t kept[TWO];
+            uint64_t kept[TWO], sum = 0;
             bool in_k[TWO];
             uint64_t before[TWO];
-            uint64_t sum = 0;
 #pragma unroll
             for (int o = 0; o < TWO; ++o) {
-                const uint32_t i = threadIdx.x * TWO + o;   // neighbours, so that scans are in index order
+                const uint32_t i = threadIdx.x + o * NT;
                 before[o] = 0, in_k[o] = false, kept[o] = 0;
                 if (i < n) {
                     const uint32_t key = pair_key[i];
+                    const int mine = pair_at[i];
                     int rank = 0;
-                    for (uint32_t t = 0; t < n; ++t) {
-                        const uint32_t kt = pair_key[t];
-                        const bool ahead = kt > key || (kt == key && t < i);
+#pragma unroll 8
+                    for (uint32_t t = 0; t < (n + 7) / 8 * 8; ++t) {
+                        const uint32_t kt = pair_key[t], wt = pair_weight[t];
+                        const bool ahead = (kt > key) | ((kt == key) & (pair_at[t] < mine));
                         rank += ahead;
-                        before[o] += ahead ? pair_weight[t] : 0;
+                        before[o] += ahead ? wt : 0;
                     }
                     in_k[o] = !use_k || rank < q.top_k;
                     kept[o] = in_k[o] ? pair_weight[i] : 0;
@@ -406,33 +397,40 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
                 __syncthreads();
                 total = 0;
                 for (int i = 0; i < NW; ++i) total += part[i];
-                __syncthreads();
             }
             const double limit = (double)q.top_p * (double)total;
-            uint64_t mine_kept = 0;
+            sum = 0;
 #pragma unroll
             for (int o = 0; o < TWO; ++o) {
                 if (use_p && !(before[o] == 0 || (double)before[o] < limit)) kept[o] = 0;
-                mine_kept += kept[o];
+                sum += kept[o];
             }
-            uint64_t upto = wave_scan(mine_kept);
-            if (lane == 63) part[wave] = upto;
+            __syncthreads();                                // all have read the weights and the parts
+#pragma unroll
+            for (int o = 0; o < TWO; ++o)
+                if (threadIdx.x + o * NT < n) pair_weight[threadIdx.x + o * NT] = (uint32_t)kept[o];
+            sum = wave_sum(sum);
+            if (lane == 0) part[wave] = sum;
             __syncthreads();
             total = 0;
-            for (int i = 0; i < NW; ++i) {
-                if (i == wave) upto += total;
-                total += part[i];
-            }
+            for (int i = 0; i < NW; ++i) total += part[i];
             const uint64_t target = target_of(a.u[r], total);
-            uint64_t run = upto - mine_kept;
 #pragma unroll
             for (int o = 0; o < TWO; ++o) {
-                if (run <= target && run + kept[o] > target) {
-                    const uint32_t i = threadIdx.x * TWO + o;
-                    a.tokens[r] = pair_at[i];
-                    if (a.logprobs) a.logprobs[r] = log_share(z_of(of_key(pair_key[i]), m, q.c), total);
+                const uint32_t i = threadIdx.x + o * NT;
+                if (i < n && kept[o]) {
+                    const int mine = pair_at[i];
+                    uint64_t run = 0;
+#pragma unroll 8
+                    for (uint32_t t = 0; t < (n + 7) / 8 * 8; ++t) {
+                        const uint32_t wt = pair_weight[t];
+                        run += pair_at[t] < mine ? wt : 0;
+                    }
+                    if (run <= target && run + kept[o] > target) {
+                        a.tokens[r] = mine;
+                        if (a.logprobs) a.logprobs[r] = log_share(z_of(of_key<T>(pair_key[i]), m, q.c), total);
+                    }
                 }
-                run += kept[o];
             }
             return;
         }
@@ -452,16 +450,16 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
         const auto narrow = [&](typename B::Found f, float above, auto &&reached) {
             // The keys of the bin: its two edges, each searched by one wave, 64 places at
             // once.  Wave 0: the least key with a bin up to this one; wave 1: the least with
-            // a bin before it, whose neighbour below is the bin's greatest (key_of(m) for
+            // a bin before it, whose neighbour below is the bin's greatest (m's for
             // bin 0).
             if (wave < 2) {
-                uint32_t lo = key_of(-kInf), hi = key_of(m);
+                uint32_t lo = key_of<T>(-kInf), hi = key_of<T>(m);
                 const int most = f.bin - wave;
                 if (most >= 0) {
                     while (lo < hi) {                      // the answer lies in [lo, hi]
                         const uint32_t width = (hi - lo + 63) / 64;
                         const uint32_t probe = lo + min(hi - lo, (uint32_t)lane * width);
-                        const uint64_t yes = __ballot(bin_of(of_key(probe)) <= most);
+                        const uint64_t yes = __ballot(bin_of(of_key<T>(probe)) <= most);
                         const int first = yes ? __ffsll((unsigned long long)yes) - 1 : 64;
                         if (first == 0) hi = lo;
                         else {
@@ -471,7 +469,7 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
                         }
                     }
                 }
-                if (lane == 0) bound[wave] = wave == 0 ? lo : f.bin > 0 ? lo - 1 : key_of(m);
+                if (lane == 0) bound[wave] = wave == 0 ? lo : f.bin > 0 ? lo - 1 : key_of<T>(m);
             }
             __syncthreads();
             uint32_t lo = bound[0], hi = bound[1];
@@ -481,9 +479,11 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
                 int shift = 0;
                 while (((hi - lo) >> shift) >= kBins) ++shift;
                 b.clear();
+                const float from = of_key<T>(lo), to = of_key<T>(hi);
                 b.all([&](int, float l) {
-                    const uint32_t key = key_of(l);
-                    if (key >= lo && key <= hi && l > above) {
+                    if (l >= from && l <= to && l > above) {
+                        const uint32_t key = key_of<T>(l);     // -0 and 0 compare equal, and have one key
+                        if (key < lo || key > hi) return;
                         const int s = (int)((hi - key) >> shift);
                         atomicAdd(&hc[s], 1u);
                         const uint32_t w = weight_of(z_of(l, m, q.c), q.min_p);
@@ -493,7 +493,7 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
                 const typename B::Found g = b.find([&](uint32_t c, uint64_t w) { return reached(count + c, weight + w); });
                 count += g.count, weight += g.weight;
                 hi -= (uint32_t)g.bin << shift;
-                if (shift == 0) return Cut{of_key(hi), count, g.in_count, weight};
+                if (shift == 0) return Cut{of_key<T>(hi), count, g.in_count, weight};
                 const uint32_t span = (1u << shift) - 1;
                 lo = hi - lo > span ? hi - span : lo;
             }
