@@ -123,8 +123,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
     __shared__ __align__(16) uint16_t sS[3 * VT * ldS], sR[3 * VT * ldT], sV[NPP * VT * ldT], sL[3 * VT * ldT];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const int seq = blockIdx.x / a.hv, h = blockIdx.x % a.hv, hk = h / (a.hv / a.hk);
-    const int v0 = blockIdx.y * VT;
+    const WalkBlock at = walk_block(a, (a.dv + VT - 1) / VT);
+    const int seq = at.seq, h = at.head, hk = h / (a.hv / a.hk), v0 = at.tile * VT;
     const Span span = span_of(a, seq);
     if (span.len <= a.short_len) return;                // taken token by token
     const int chunks = (span.len + kC - 1) / kC;
@@ -340,15 +340,11 @@ hipError_t forward_ks(const DeltaArgs &a, hipStream_t s) {
     if (hipError_t e = launch_operands<T, KS, false>(a, s)) return e;
     const auto walk = [&](auto ct) {
         constexpr int CT = decltype(ct)::value;
-        const dim3 grid(a.n * a.hv, (a.dv + 16 * CT - 1) / (16 * CT));
+        const int grid = a.n * a.hv * ((a.dv + 16 * CT - 1) / (16 * CT));
         if (a.before) k_delta_walk<T, KS, CT, true><<<grid, 256, 0, s>>>(a);
         else k_delta_walk<T, KS, CT, false><<<grid, 256, 0, s>>>(a);
     };
-    // Two column tiles a block share the left operands' loads; with too few
-    // blocks for the CUs one tile's shorter chain counts more.  7 ragged sequences
-    // of 8 heads (224 blocks of two tiles): 132 us with two, 105 with one; 256 of 4
-    // heads: 41 us with two, 71 with one.
-    if (a.dv <= 16 || a.n * a.hv * ((a.dv + 31) / 32) <= 256) walk(std::integral_constant<int, 1>{});
+    if (walk_tiles(a) == 1) walk(std::integral_constant<int, 1>{});
     else walk(std::integral_constant<int, 2>{});
     return hipGetLastError();
 }

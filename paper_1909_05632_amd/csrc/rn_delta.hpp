@@ -59,6 +59,29 @@ __device__ inline Chunk chunk_of(const DeltaArgs &a, int slot) {
     return {lo, s.begin + (int)at, min(kC, s.len - (int)at), s.len, at + kC >= s.len};
 }
 
+// A walk's blocks take the sequences from the longest to the shortest, so that
+// no long chain begins when others have ended; within one the column tiles of a
+// head are 8 k blocks apart where heads are a multiple of 8, on one XCD, whose
+// cache then serves its operands to all of them.  Beyond 64 sequences (a lane each)
+// they stay in order: the more there are, the less the last one counts.
+struct WalkBlock {
+    int seq, head, tile;
+};
+__device__ inline WalkBlock walk_block(const DeltaArgs &a, int tiles) {
+    const int per = a.hv * tiles, i = blockIdx.x % per;
+    int seq = blockIdx.x / per;
+    if (a.off && a.n > 1 && a.n <= 64) {
+        const int lane = threadIdx.x & 63, len = lane < a.n ? span_of(a, lane).len : -1;
+        int before = 0;
+        for (int j = 0; j < a.n; ++j) {
+            const int l = __builtin_amdgcn_readlane(len, j);
+            before += l > len || (l == len && j < lane);
+        }
+        seq = __ffsll((unsigned long long)__ballot(before == seq)) - 1;
+    }
+    return {seq, i % a.hv, i / a.hv};
+}
+
 // Log decays (base 2) summed up to each token of a chunk, in double: differences
 // of far tokens stay exact to float32 where the sums are large.  An empty memory
 // (g = -infinity) is a decay of e^-10^6 = 0, whose differences are finite.
@@ -376,6 +399,18 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
         __syncthreads();
     }
     pieces(std::integral_constant<int, 3>{}, x, a.mf, wave, 4);
+}
+
+// Column tiles of a walk's block.  Two share the left operands' loads; one has the
+// shorter chain, and is taken while two of its blocks a CU hold all there are
+// (16384 tokens of 16 heads of 128 x 128: 4 even sequences, 512 blocks of one
+// tile, 264 us either way; 5, 640 blocks, 287 us with one, 267 with two; 8, 1024
+// blocks, 248 and 210).  Ragged sequences end at different times and leave room
+// for more of them (5: 320 us with one, 415 with two; 8: 281 and 344; 12: 266 and
+// 270).
+inline int walk_tiles(const DeltaArgs &a) {
+    const int64_t pairs = (int64_t)a.n * a.hv * ((a.dv + 31) / 32);
+    return a.dv <= 16 || pairs <= (a.off ? 512 : 256) ? 1 : 2;
 }
 
 template <class T, int KS, bool BWD>
