@@ -13,6 +13,8 @@ constexpr int kC = RN_DELTA_CHUNK;   // tokens of a chunk
 constexpr int kLd = kC + 4;          // row length of a 64-wide LDS tile, off the banks' stride
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // One 16x16 tile of A B on the float32 matrix cores, added to acc.  a(i, k) and
 // b(k, j) read the operands; kk (a multiple of 4) is the summed length.  Lane l
@@ -149,7 +151,6 @@ __device__ inline void split_pair(float x, float y, uint32_t (&p)[N]) {
 // Four consecutive k of one column into N planes of an LDS operand [column][ld].
 template <int N>
 __device__ inline void put4(uint16_t *lds, int plane, int at, const f32x4 v) {
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
     uint32_t a[N], b[N];
     split_pair<N>(v[0], v[1], a);
     split_pair<N>(v[2], v[3], b);
@@ -162,17 +163,27 @@ __device__ inline void get8(const uint16_t *lds, int plane, int at, bf16x8 (&f)[
     for (int i = 0; i < N; ++i) f[i] = *reinterpret_cast<const bf16x8 *>(lds + i * plane + at);
 }
 
-// A store that is dropped where `in` is false, without a branch: the compiler
-// can then count what is in flight and wait for no more than it needs.  Offsets
-// are in bytes from a base that the wave shares.
-__device__ inline __amdgpu_buffer_rsrc_t rsrc_of(void *base) {
-    return __builtin_amdgcn_make_buffer_rsrc(base, 0, 0x7fffffff, 0x00027000);
+// Loads that give 0 and stores that are dropped where `in` is false, without a
+// branch: the compiler can then count what is in flight and wait for no more than
+// it needs.  Offsets are in bytes from a base that the wave shares.
+__device__ inline __amdgpu_buffer_rsrc_t rsrc_of(const void *base) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, 0x7fffffff, 0x00027000);
+}
+template <class T>
+__device__ inline T load_if(bool in, __amdgpu_buffer_rsrc_t from, uint32_t at) {
+    const uint32_t off = in ? at : 0xfffffff0u;
+    if constexpr (sizeof(T) == 16) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b128(from, off, 0, 0));
+    else if constexpr (sizeof(T) == 8) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b64(from, off, 0, 0));
+    else if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(from, off, 0, 0));
+    else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(from, off, 0, 0));
 }
 template <class T>
 __device__ inline void store_if(bool in, __amdgpu_buffer_rsrc_t to, uint32_t at, T v) {
     const uint32_t off = in ? at : 0xfffffff0u;
-    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), to, off, 0, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), to, off, 0, 0);
+    if constexpr (sizeof(T) == 16) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), to, off, 0, 0);
+    else if constexpr (sizeof(T) == 8) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), to, off, 0, 0);
+    else if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), to, off, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), to, off, 0, 0);
 }
 
 // The 16 x 32 pieces of a lower triangular 64 x 64 operand that hold anything:
@@ -213,19 +224,16 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     __shared__ float beta[kC];
     const int slot = blockIdx.x, h = blockIdx.y, group = a.hv / a.hk, hk = h / group;
     const Chunk c = chunk_of(a, slot);
+    const bool none = c.whole <= a.short_len;           // no chunk, or one of a sequence taken token by token
     if (BWD && h == 0 && threadIdx.x == 0) {
         int32_t *m = a.map + 4 * slot;
-        m[0] = c.begin, m[1] = c.len, m[2] = c.seq, m[3] = c.last;
+        m[0] = c.begin, m[1] = none ? 0 : c.len, m[2] = c.seq, m[3] = c.last;
     }
-    if (c.len == 0) return;
-    // A sequence that goes token by token needs K^T and Q^T only, for the chunks' gradients.
-    const bool keys_only = c.whole <= a.short_len;
-    if (keys_only && (!BWD || h % (a.hv / a.hk))) return;
+    if (none || c.len == 0) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int blocks = (c.len + 15) / 16;               // 16s of tokens
     const bool first = h % group == 0, busy = wave < blocks;
     const int64_t keys = ((int64_t)slot * a.hk + hk) * kKeys, ch = (int64_t)slot * a.hv + h;
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     // K and Q as rows: the wave's 16 tokens.
     const int token = wave * 16 + r;
     bf16x8 ka[KS][NP], qa[KS][NP];
@@ -313,7 +321,6 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     if (first) transpose(skf, a.kt);
     if constexpr (BWD)
         if (first) transpose(sqf, a.qt);
-    if (keys_only) return;
     __syncthreads();                                    // K's fragments have been read
 #pragma unroll
     for (int n = 0; n < 4; ++n) {

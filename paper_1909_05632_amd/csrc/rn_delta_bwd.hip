@@ -6,7 +6,8 @@
 //   dV' = M^-T (P^T dO + (e^(c64 - c) K) dS'),
 //   dS  = e^(c64) dS' + (scale e^c Q)^T dO - (beta e^c K)^T dV':
 // k_delta_bwd_walk takes the chunks of a sequence from the last to the first and
-// leaves dS' and dV'.  Then every chunk by itself (k_delta_bwd_chunk), with
+// leaves dS' and dV'.  Then every chunk by itself (k_delta_bwd_chunk; short sequences:
+// k_delta_short_grad), with
 // dP = dO V'^T, dL = -beta dV' V'^T and e = e^(ci - cj) for j <= i:
 //   dv = beta dV',  dbeta_i = dV'_i . E_i,
 //   dq = scale (e^c dO S^T + (dP e) K),
@@ -234,39 +235,38 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
 // Elements from .. + 3 and from + 16 .. + 19 of a row of `count`, zeros where there
 // are none; as loaded, so that a later step's can be on their way while this one
 // is computed.  (Which of 32 elements a lane holds is free as long as both
-// operands of a product agree; four lanes read 64 bytes on end this way.)
+// operands of a product agree; four lanes read 64 bytes on end this way.)  `row`
+// is the row's offset in bytes from a base that the wave shares; nothing branches,
+// as in store_if, so that each wait is for no more than it needs.
 template <class T, bool VEC>
 struct Raw8 {
     static constexpr int PER = VEC ? 4 : 1;             // VEC: count a multiple of 8, rows on 16 bytes
     Pack<T, PER> v[8 / PER];
-    __device__ void load(const T *p, bool in, int from, int count) {
+    __device__ void load(__amdgpu_buffer_rsrc_t p, bool in, uint32_t row, int from, int count) {
 #pragma unroll
         for (int e = 0; e < 8; e += PER) {
             const int at = from + (e < 4 ? e : e + 12);
-            v[e / PER] = Pack<T, PER>{};
-            if (in && at < count) v[e / PER] = *reinterpret_cast<const Pack<T, PER> *>(p + at);
+            v[e / PER] = load_if<Pack<T, PER>>(in && at < count, p, row + sizeof(T) * at);
+        }
+    }
+    __device__ void store(__amdgpu_buffer_rsrc_t p, bool in, uint32_t row, int from, int count) const {
+#pragma unroll
+        for (int e = 0; e < 8; e += PER) {
+            const int at = from + (e < 4 ? e : e + 12);
+            store_if(in && at < count, p, row + sizeof(T) * at, v[e / PER]);
         }
     }
     __device__ void get(float (&f)[8]) const {
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = to_float(v[e / PER].v[e % PER]);
     }
-};
-template <class T, bool VEC>
-__device__ inline void store8(T *p, int from, int count, const float (&f)[8]) {
-    constexpr int PER = VEC ? 4 : 1;
+    __device__ void set(const float (&f)[8]) {
 #pragma unroll
-    for (int e = 0; e < 8; e += PER) {
-        const int at = from + (e < 4 ? e : e + 12);
-        Pack<T, PER> q;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) q.v[j] = from_float<T>(f[e + j]);
-        if (at < count) *reinterpret_cast<Pack<T, PER> *>(p + at) = q;
+        for (int e = 0; e < 8; ++e) v[e / PER].v[e % PER] = from_float<T>(f[e]);
     }
-}
+};
 template <int N>
 __device__ inline void planes8(const float (&v)[8], bf16x8 (&f)[N]) {
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     uint32_t w[4][N];
 #pragma unroll
     for (int e = 0; e < 4; ++e) split_pair<N>(v[2 * e], v[2 * e + 1], w[e]);
@@ -334,24 +334,29 @@ __global__ __launch_bounds__(KS == 4 ? 512 : 256, 2) void k_delta_bwd_chunk(Delt
         for (int n = 0; n < 4; ++n) pr[0][n] = pr[2 - PARTS][n] = f32x4{};
         float db = 0.f, dot = 0.f;
         const float b = beta_s[token];
-        const int64_t row = ((int64_t)(c.begin + token) * a.hv + h) * a.dv;
+        const int64_t row0 = ((int64_t)c.begin * a.hv + h) * a.dv;
+        const uint32_t row = token * (uint32_t)(a.hv * a.dv);
         const bool in = token < c.len;
         constexpr int W8 = 4 * PARTS, RT = KT > W8 ? KT / W8 : 1;       // row tiles of S and dS' a wave splits
         Raw8<float, VEC> rs[RT], rt[RT], rw, re;
-        Raw8<T, VEC> ro;
+        Raw8<T, VEC> ro, rv{};
         // the gradient of the memory after the chunk: dfinal after a sequence's last
-        const float *after = c.last ? a.dfinal + ((int64_t)c.seq * a.hv + h) * a.dk * a.dv : a.after + ch * a.dk * a.dv;
+        const int64_t mem = (int64_t)a.dk * a.dv;
         const bool no_after = c.last && !a.dfinal;
+        const __amdgpu_buffer_rsrc_t pS = rsrc_of(a.before + ch * mem), pE = rsrc_of(a.err + row0), pW = rsrc_of(a.dwrite + row0);
+        const __amdgpu_buffer_rsrc_t pD = rsrc_of(c.last && a.dfinal ? a.dfinal + ((int64_t)c.seq * a.hv + h) * mem : a.after + ch * mem);
+        const __amdgpu_buffer_rsrc_t pO = rsrc_of(static_cast<const T *>(a.dout) + row0);
+        const __amdgpu_buffer_rsrc_t pV = rsrc_of(static_cast<T *>(a.dval) + row0);
         const auto fetch = [&](int v) {
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
                 const int d = (wave8 + W8 * i) * 16 + (int)r;
-                rs[i].load(a.before + (ch * a.dk + d) * a.dv, d < a.dk, v, a.dv);
-                rt[i].load(after + (int64_t)d * a.dv, d < a.dk && !no_after, v, a.dv);
+                rs[i].load(pS, d < a.dk, d * a.dv * 4, v, a.dv);
+                rt[i].load(pD, d < a.dk && !no_after, d * a.dv * 4, v, a.dv);
             }
-            if (part == 0) re.load(a.err + row, in, v, a.dv);
-            if (part == 0) ro.load(static_cast<const T *>(a.dout) + row, in, v, a.dv);
-            rw.load(a.dwrite + row, in, v, a.dv);
+            rw.load(pW, in, row * 4, v, a.dv);
+            re.load(pE, in && part == 0, row * 4, v, a.dv);
+            ro.load(pO, in && part == 0, row * sizeof(T), v, a.dv);
         };
         fetch(g * 4);
         for (int v0 = 0; v0 < a.dv; v0 += 32) {
@@ -398,10 +403,11 @@ __global__ __launch_bounds__(KS == 4 ? 512 : 256, 2) void k_delta_bwd_chunk(Delt
                     for (int i = 0; i < 8; ++i) w[i] *= b;
                     planes8<3>(w, f);                   // beta dV', which is dv
                     put(fR + wave * 3 * kFrag, f);
-                    if (in) store8<T, VEC>(static_cast<T *>(a.dval) + row, v, a.dv, w);
+                    rv.set(w);
                 }
             }
             fetch(v + 32);                              // nothing past the last column
+            rv.store(pV, in && part == PARTS - 1, row * sizeof(T), v, a.dv);
             dev::lds_barrier();                         // which leaves those loads in flight
             if (busy) {
                 bf16x8 fo[NP], fr[3], fv[3];
@@ -574,25 +580,20 @@ __global__ __launch_bounds__(KS == 4 ? 512 : 256, 2) void k_delta_bwd_chunk(Delt
 
 template <class T, int KS>
 hipError_t backward_ks(const DeltaArgs &a, hipStream_t s) {
-    if (a.tokens > 0)
-        if (hipError_t e = launch_operands<T, KS, true>(a, s)) return e;
-    if (delta_ways(a).chunks) {
-        if (walk_tiles(a) == 1)
-            k_delta_bwd_walk<T, KS, 1><<<a.n * a.hv * ((a.dv + 15) / 16), 256, 0, s>>>(a);
-        else k_delta_bwd_walk<T, KS, 2><<<a.n * a.hv * ((a.dv + 31) / 32), 256, 0, s>>>(a);
-        if (hipError_t e = hipGetLastError()) return e;
-    }
-    if (a.tokens == 0) return hipSuccess;
+    if (hipError_t e = launch_operands<T, KS, true>(a, s)) return e;
+    if (walk_tiles(a) == 1) k_delta_bwd_walk<T, KS, 1><<<a.n * a.hv * ((a.dv + 15) / 16), 256, 0, s>>>(a);
+    else k_delta_bwd_walk<T, KS, 2><<<a.n * a.hv * ((a.dv + 31) / 32), 256, 0, s>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
     const dim3 grid((int)delta_chunk_slots(a.tokens, a.n), a.hk);
     const auto even = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
     const bool vec = a.dv % 8 == 0 && even(a.dout) && even(a.dval) && even(a.dfinal);
-    if (a.hv > a.hk) {
-        if (vec) k_delta_bwd_chunk<T, KS, true, true><<<grid, KS == 4 ? 512 : 256, 0, s>>>(a);
-        else k_delta_bwd_chunk<T, KS, false, true><<<grid, KS == 4 ? 512 : 256, 0, s>>>(a);
-    } else {
-        if (vec) k_delta_bwd_chunk<T, KS, true, false><<<grid, KS == 4 ? 512 : 256, 0, s>>>(a);
-        else k_delta_bwd_chunk<T, KS, false, false><<<grid, KS == 4 ? 512 : 256, 0, s>>>(a);
-    }
+    const auto chunk = [&](auto vec_) {
+        constexpr bool VEC = decltype(vec_)::value;
+        if (a.hv > a.hk) k_delta_bwd_chunk<T, KS, VEC, true><<<grid, KS == 4 ? 512 : 256, 0, s>>>(a);
+        else k_delta_bwd_chunk<T, KS, VEC, false><<<grid, KS == 4 ? 512 : 256, 0, s>>>(a);
+    };
+    if (vec) chunk(std::true_type{});
+    else chunk(std::false_type{});
     return hipGetLastError();
 }
 
@@ -610,6 +611,7 @@ hipError_t launch_delta_backward(const DeltaArgs &args, bool bf16, hipStream_t s
     a.short_len = w.tokens ? kShort : -1;
     if (w.tokens)
         if (hipError_t e = launch_delta_short_backward(a, bf16, s)) return e;
+    if (!w.chunks) return hipSuccess;
     return bf16 ? backward<bf16_t>(a, s) : backward<float>(a, s);
 }
 

@@ -5,8 +5,8 @@
 // Backward, with D the gradient of the memory, from the last token on:
 //   D <- D + scale q dout^T,  x = D^T k (the gradient of beta err),
 //   D <- a (D - k (beta x)^T).
-// The chunks' gradients (k_delta_bwd_chunk) follow from err, x and the first
-// memory, however those were made.
+// The inputs' gradients (k_delta_short_grad) follow from err, x and the first
+// memory by the sums over pairs of tokens that are written down in rn_delta_bwd.hip.
 //
 // A wave owns 16 columns: lane l column l % 16, rows R (l / 16) .. + R - 1, in its
 // registers from the first token to the last.  Sums over the rows are R
@@ -153,6 +153,246 @@ __global__ __launch_bounds__(kWaves * 64) void k_delta_short_bwd(DeltaArgs a) {
     if (a.dstate) store_memory<R>(a, a.dstate + mem, row0, col, D);
 }
 
+// The inputs' gradients of a sequence that is one chunk, all of it on the float32
+// matrix cores: operands of 16 or 32 tokens are too few for the split into bf16
+// planes to pay.  A block takes a sequence and a key head and adds the value heads
+// that share it; wave w owns the memory's row tiles w, w + 4.  The tokens' rows lie
+// in LDS, S and dS' are read once, as operands as they lie in memory.  Bound by
+// those bytes: 256 episodes of 16 tokens and 4 heads of 64 x 64, 16 us for 60 MB (56
+// us by chunks, whose operands it does without).
+template <class T, int NT, int TT, bool VEC>
+__global__ __launch_bounds__(kWaves * 64, NT * TT == 1 ? 4 : 2) void k_delta_short_grad(DeltaArgs a) {
+    constexpr int rows = 16 * TT;                       // tokens there is room for
+    extern __shared__ __align__(16) float lds[];
+    __shared__ double cs[64];
+    __shared__ float beta[64], dc[kWaves][kShort], extra[kWaves];
+    const int seq = blockIdx.x / a.hk, hk = blockIdx.x % a.hk, group = a.hv / a.hk;
+    const Span span = span_of(a, seq);
+    const int len = span.len;
+    if (len == 0 || len > a.short_len) return;
+    const int dvp = (a.dv + 31) / 32 * 32, ldV = dvp + 4, ldX = rows + 4;
+    constexpr int KP = NT * 64, ldK = KP + 4;
+    float *sO = lds, *sW = sO + rows * ldV, *sV = sW + rows * ldV;      // dO, dV', V'
+    float *sK = sV + rows * ldV, *sQ = sK + rows * ldK;
+    float *x = sQ + rows * ldK, *y = x + rows * ldX;                    // [i][j] of dP e and dL e
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int tiles = (len + 15) / 16;
+    const Chunk c{seq, span.begin, len, len, true};
+    for (int i = threadIdx.x; i < rows * KP; i += kWaves * 64) {
+        const int t = i / KP, d = i % KP;
+        const bool in = t < len && d < a.dk;
+        sK[t * ldK + d] = in ? load<T>(a.k, (int64_t)(c.begin + t) * a.ks + hk * a.dk + d) : 0.f;
+        sQ[t * ldK + d] = in ? load<T>(a.q, (int64_t)(c.begin + t) * a.qs + hk * a.dk + d) : 0.f;
+    }
+    constexpr int PER = VEC ? 4 : 1;                    // VEC: dv a multiple of 4, rows on that
+    const auto mfma = [](float u, float v, f32x4 &acc) { acc = __builtin_amdgcn_mfma_f32_16x16x4f32(u, v, acc, 0, 0, 0); };
+    f32x4 tq[TT][NT], tk[TT][NT];                         // over the value heads
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) tq[t][n] = tk[t][n] = f32x4{};
+    for (int h = hk * group; h < (hk + 1) * group; ++h) {
+        const int64_t mem = (int64_t)a.dk * a.dv, row0 = ((int64_t)c.begin * a.hv + h) * a.dv;
+        const __amdgpu_buffer_rsrc_t pS = rsrc_of(a.before + ((int64_t)slot_of(span, seq, 0) * a.hv + h) * mem);
+        const __amdgpu_buffer_rsrc_t pD = rsrc_of(a.dfinal ? a.dfinal + ((int64_t)seq * a.hv + h) * mem : a.before);
+        struct Step {                                   // 32 columns of S and of dS'
+            Pack<float, PER> s[NT][2][4 / PER], d[NT][2][4 / PER];
+        } next;
+        const auto fetch = [&](int v0) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int o = 0; o < 2; ++o)
+#pragma unroll
+                    for (int e = 0; e < 4; e += PER) {
+                        const int d = (wave + 4 * n) * 16 + r, v = v0 + o * 16 + g * 4 + e;
+                        const bool in = d < a.dk && v < a.dv;
+                        next.s[n][o][e / PER] = load_if<Pack<float, PER>>(in, pS, 4 * (d * a.dv + v));
+                        next.d[n][o][e / PER] = load_if<Pack<float, PER>>(in && a.dfinal, pD, 4 * (d * a.dv + v));
+                    }
+        };
+        fetch(0);
+        __syncthreads();                                // the last head's rows have been read
+        if (wave == 0) {
+            cs[lane] = decay_sums(a, c, h);
+            beta[lane] = lane < len ? a.beta[(int64_t)(c.begin + lane) * a.hv + h] : 0.f;
+        }
+        // Eight threads a token: the rows, dv and dbeta.
+        const int token = threadIdx.x >> 3;
+        if (token < rows) {
+            const __amdgpu_buffer_rsrc_t pO = rsrc_of(static_cast<const T *>(a.dout) + row0), pW = rsrc_of(a.dwrite + row0);
+            const __amdgpu_buffer_rsrc_t pE = rsrc_of(a.err + row0), pV = rsrc_of(static_cast<T *>(a.dval) + row0);
+            const uint32_t row = token * (uint32_t)(a.hv * a.dv);
+            const float b = token < len ? a.beta[(int64_t)(c.begin + token) * a.hv + h] : 0.f;
+            float db = 0.f;
+            for (int v = (threadIdx.x & 7) * 4; v < dvp; v += 32) {
+                f32x4 o, w, e;
+#pragma unroll
+                for (int i = 0; i < 4; i += PER) {
+                    const bool in = token < len && v + i < a.dv;
+                    const auto to = load_if<Pack<T, PER>>(in, pO, sizeof(T) * (row + v + i));
+                    const auto tw = load_if<Pack<float, PER>>(in, pW, 4 * (row + v + i));
+                    const auto te = load_if<Pack<float, PER>>(in, pE, 4 * (row + v + i));
+                    Pack<T, PER> dv;
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) {
+                        o[i + j] = to_float(to.v[j]), w[i + j] = tw.v[j], e[i + j] = te.v[j];
+                        db = fmaf(w[i + j], e[i + j], db);
+                        e[i + j] *= b;
+                        dv.v[j] = from_float<T>(w[i + j] * b);
+                    }
+                    store_if(in, pV, sizeof(T) * (row + v + i), dv);
+                }
+                *reinterpret_cast<f32x4 *>(sO + token * ldV + v) = o;
+                *reinterpret_cast<f32x4 *>(sW + token * ldV + v) = w;
+                *reinterpret_cast<f32x4 *>(sV + token * ldV + v) = e;
+            }
+#pragma unroll
+            for (int s = 1; s < 8; s <<= 1) db += __shfl_xor(db, s);
+            if ((threadIdx.x & 7) == 0 && token < len) a.dbeta[(int64_t)(c.begin + token) * a.hv + h] = db;
+        }
+        __syncthreads();
+        f32x4 gq[TT][NT], gr[TT][NT], gw[TT][NT];
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) gq[t][n] = gr[t][n] = gw[t][n] = f32x4{};
+        float dot = 0.f;
+        for (int v0 = 0; v0 < dvp; v0 += 32) {
+            const Step now = next;
+            fetch(v0 + 32);                             // nothing past the last column
+#pragma unroll
+            for (int o = 0; o < 2; ++o)
+#pragma unroll
+                for (int t = 0; t < TT; ++t)
+                    if (t < tiles) {
+                        const int at = (t * 16 + r) * ldV + v0 + o * 16 + g * 4;
+                        const f32x4 fo = *reinterpret_cast<const f32x4 *>(sO + at), fw = *reinterpret_cast<const f32x4 *>(sW + at);
+                        const f32x4 fv = *reinterpret_cast<const f32x4 *>(sV + at);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float s = now.s[n][o][e / PER].v[e % PER], d = now.d[n][o][e / PER].v[e % PER];
+                                mfma(fo[e], s, gq[t][n]);
+                                mfma(fw[e], s, gr[t][n]);
+                                mfma(fv[e], d, gw[t][n]);
+                                if (t == 0) dot = fmaf(s, d, dot);
+                            }
+                    }
+        }
+        // The pairs of tokens: a tile of dP or of dL a job.
+        for (int job = wave; job < (tiles == 1 ? 2 : 6); job += kWaves) {
+            const bool write = job & 1;
+            const int ti = job > 1, tj = job > 3;
+            const float *p = (write ? sW : sO) + (ti * 16 + r) * ldV + g * 4, *q = sV + (tj * 16 + r) * ldV + g * 4;
+            f32x4 acc{};
+            for (int v = 0; v < dvp; v += 16) {
+                const f32x4 u = *reinterpret_cast<const f32x4 *>(p + v), w = *reinterpret_cast<const f32x4 *>(q + v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mfma(u[e], w[e], acc);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int t = ti * 16 + g * 4 + j, u = tj * 16 + r;
+                const float d = u <= t ? decay(cs[t] - cs[u]) : 0.f;
+                if (write) y[t * ldX + u] = u < t ? -beta[t] * acc[j] * d : 0.f;
+                else x[t * ldX + u] = u <= t ? acc[j] * d * a.scale : 0.f;
+            }
+        }
+        // The memory's part of the sums, before the pairs' is added.
+        const double last = cs[len - 1];
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+            if (t < tiles)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = t * 16 + g * 4 + j;
+                    const float grown = decay(cs[i]), left = decay(last - cs[i]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        gq[t][n][j] *= grown * a.scale;
+                        gr[t][n][j] *= -beta[i] * grown;
+                        gw[t][n][j] *= left;
+                        sum = fmaf(gw[t][n][j], sK[i * ldK + (wave + 4 * n) * 16 + r], sum);
+                    }
+                }
+        sum = fmaf(dot, decay(last), sum);
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
+        if (lane == 0) extra[wave] = sum;
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int kt = 0; kt < TT; ++kt)
+                if (t < tiles && kt < tiles)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const int k = kt * 16 + e + g;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const int d = (wave + 4 * n) * 16 + r;
+                            const float fk = sK[k * ldK + d];
+                            if (kt <= t) {              // rows i: reads
+                                mfma(x[(t * 16 + r) * ldX + k], fk, gq[t][n]);
+                                mfma(y[(t * 16 + r) * ldX + k], fk, gr[t][n]);
+                            }
+                            if (kt >= t) {              // columns j: writes
+                                mfma(x[k * ldX + t * 16 + r], sQ[k * ldK + d], gw[t][n]);
+                                mfma(y[k * ldX + t * 16 + r], fk, gw[t][n]);
+                            }
+                        }
+                    }
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+            if (t < tiles)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = t * 16 + g * 4 + j;
+                    float s = 0.f;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const int at = i * ldK + (wave + 4 * n) * 16 + r;
+                        s = fmaf(gq[t][n][j], sQ[at], s);
+                        s = fmaf(gr[t][n][j] - gw[t][n][j], sK[at], s);
+                        tq[t][n][j] += gq[t][n][j];
+                        tk[t][n][j] += gr[t][n][j] + gw[t][n][j];
+                    }
+#pragma unroll
+                    for (int o = 1; o < 16; o <<= 1) s += __shfl_xor(s, o);
+                    if (r == 0) dc[wave][i] = s;
+                }
+        __syncthreads();
+        if (wave == 0) {
+            double s = 0.;
+            if (lane < len)
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) s += dc[w][lane] + (lane == len - 1 ? extra[w] : 0.f);
+#pragma unroll
+            for (int d = 1; d < kShort; d <<= 1) {
+                const double u = __shfl_down(s, d);
+                if (lane + d < kShort) s += u;
+            }
+            if (lane < len) a.dg[(int64_t)(c.begin + lane) * a.hv + h] = (float)s;
+        }
+    }
+    const __amdgpu_buffer_rsrc_t rq = rsrc_of(static_cast<T *>(a.dq) + ((int64_t)c.begin * a.hk + hk) * a.dk);
+    const __amdgpu_buffer_rsrc_t rk = rsrc_of(static_cast<T *>(a.dkey) + ((int64_t)c.begin * a.hk + hk) * a.dk);
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int i = t * 16 + g * 4 + j, d = (wave + 4 * n) * 16 + r;
+                const uint32_t at = i * (uint32_t)(a.hk * a.dk) + d;
+                store_if(i < len && d < a.dk, rq, sizeof(T) * at, from_float<T>(tq[t][n][j]));
+                store_if(i < len && d < a.dk, rk, sizeof(T) * at, from_float<T>(tk[t][n][j]));
+            }
+}
+
 template <class T, class F>
 hipError_t by_rows(const DeltaArgs &a, F &&go) {
     if (a.n == 0) return hipSuccess;
@@ -174,9 +414,28 @@ hipError_t forward(const DeltaArgs &a, hipStream_t s) {
 
 template <class T>
 hipError_t backward(const DeltaArgs &a, hipStream_t s) {
-    return by_rows<T>(a, [&](auto r, dim3 grid) {
+    const hipError_t walk = by_rows<T>(a, [&](auto r, dim3 grid) {
         k_delta_short_bwd<T, decltype(r)::value><<<grid, kWaves * 64, 0, s>>>(a);
     });
+    if (walk != hipSuccess || a.n == 0) return walk;
+    const auto even = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+    const bool vec = a.dv % 4 == 0 && even(a.dout) && even(a.dval) && even(a.dfinal);
+    const auto grad = [&](auto nt_, auto tt_, auto vec_) -> hipError_t {
+        constexpr int NT = decltype(nt_)::value, TT = decltype(tt_)::value, rows = 16 * TT;
+        const int dvp = (a.dv + 31) / 32 * 32;
+        const size_t bytes = sizeof(float) * rows * (3 * (dvp + 4) + 2 * (NT * 64 + 4) + 2 * (rows + 4));
+        auto *kernel = k_delta_short_grad<T, NT, TT, decltype(vec_)::value>;
+        if (hipError_t e = allow_lds(kernel, bytes)) return e;
+        kernel<<<a.n * a.hk, kWaves * 64, bytes, s>>>(a);
+        return hipGetLastError();
+    };
+    const auto by_vec = [&](auto nt, auto tt) { return vec ? grad(nt, tt, std::true_type{}) : grad(nt, tt, std::false_type{}); };
+    // Even sequences of up to 16 tokens need room for one tile of tokens.
+    const auto by_tokens = [&](auto nt) {
+        return !a.off && a.tokens <= (int64_t)16 * a.n ? by_vec(nt, std::integral_constant<int, 1>{})
+                                                       : by_vec(nt, std::integral_constant<int, 2>{});
+    };
+    return a.dk <= 64 ? by_tokens(std::integral_constant<int, 1>{}) : by_tokens(std::integral_constant<int, 2>{});
 }
 
 }  // namespace
