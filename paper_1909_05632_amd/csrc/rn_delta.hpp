@@ -50,10 +50,11 @@ struct Chunk {
 };
 __device__ inline Chunk chunk_of(const DeltaArgs &a, int slot) {
     int lo = 0, hi = a.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (offset_of(a, mid) / kC + mid <= slot) lo = mid;
-        else hi = mid - 1;
+    while (lo < hi) {                                   // 64 places at once
+        const int step = (hi - lo + 63) / 64, at = lo + ((int)(threadIdx.x & 63) + 1) * step;
+        const bool up = at <= hi && offset_of(a, min(at, hi)) / kC + at <= slot;
+        lo += __popcll(__ballot(up)) * step;
+        hi = min(hi, lo + step - 1);
     }
     const Span s = span_of(a, lo);
     const int64_t at = (int64_t)(slot - slot_of(s, lo, 0)) * kC;

@@ -38,23 +38,41 @@ struct Stage {
     float a[kShort], beta[kShort];
 };
 
-// A sequence's tokens: k, scale q, the values (forward) or
-// their gradients, e^g and beta.  Rows past dk and columns past dv are 0.
-template <class T, int R>
+// A sequence's tokens: k, scale q, the values (forward) or their gradients, e^g
+// and beta.  Rows past dk and columns past dv are 0.  A pass's loads are all on
+// their way before the first is waited for: one pass does for 16 tokens up to dk 64.
+// VEC: dk, dv and strides multiples of 4, rows on that.
+template <class T, int R, bool VEC>
 __device__ inline void fill(const DeltaArgs &a, Stage<R> &s, const void *v, int64_t vs, int h, int hk, int v0, Span span) {
-    const int at = span.begin, count = span.len;
-    for (int i = threadIdx.x; i < count * Stage<R>::K; i += kWaves * 64) {
-        const int t = i / Stage<R>::K, d = i % Stage<R>::K;
-        const bool in = d < a.dk;
-        s.k[t][d] = in ? load<T>(a.k, (int64_t)(at + t) * a.ks + hk * a.dk + d) : 0.f;
-        s.q[t][d] = in ? load<T>(a.q, (int64_t)(at + t) * a.qs + hk * a.dk + d) * a.scale : 0.f;
+    constexpr int PER = VEC ? 4 : 1, TP = kWaves * 64 / R;              // tokens of k and q a pass
+    const __amdgpu_buffer_rsrc_t pk = rsrc_of(static_cast<const T *>(a.k) + (int64_t)span.begin * a.ks + hk * a.dk);
+    const __amdgpu_buffer_rsrc_t pq = rsrc_of(static_cast<const T *>(a.q) + (int64_t)span.begin * a.qs + hk * a.dk);
+    const __amdgpu_buffer_rsrc_t pv = rsrc_of(static_cast<const T *>(v) + (int64_t)span.begin * vs + h * a.dv + v0);
+    const int d = threadIdx.x % R * 4, c = threadIdx.x % 16 * 4;
+    for (int p = 0; p * (TP < 16 ? TP : 16) < span.len; ++p) {
+        const int tk = p * TP + threadIdx.x / R, tv = p * 16 + threadIdx.x / 16;
+        Pack<T, PER> fk[4 / PER], fq[4 / PER], fv[4 / PER];
+#pragma unroll
+        for (int e = 0; e < 4; e += PER) {
+            const bool in = tk < span.len && d + e < a.dk;
+            fk[e / PER] = load_if<Pack<T, PER>>(in, pk, sizeof(T) * (tk * (uint32_t)a.ks + d + e));
+            fq[e / PER] = load_if<Pack<T, PER>>(in, pq, sizeof(T) * (tk * (uint32_t)a.qs + d + e));
+            fv[e / PER] = load_if<Pack<T, PER>>(tv < span.len && v0 + c + e < a.dv, pv, sizeof(T) * (tv * (uint32_t)vs + c + e));
+        }
+        f32x4 k, q, w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            k[e] = to_float(fk[e / PER].v[e % PER]), q[e] = to_float(fq[e / PER].v[e % PER]) * a.scale;
+            w[e] = to_float(fv[e / PER].v[e % PER]);
+        }
+        if (tk < kShort) {
+            *reinterpret_cast<f32x4 *>(&s.k[tk][d]) = k;
+            *reinterpret_cast<f32x4 *>(&s.q[tk][d]) = q;
+        }
+        if (tv < kShort) *reinterpret_cast<f32x4 *>(&s.v[tv][c]) = w;
     }
-    for (int i = threadIdx.x; i < count * kWaves * 16; i += kWaves * 64) {
-        const int t = i / (kWaves * 16), c = i % (kWaves * 16);
-        s.v[t][c] = v0 + c < a.dv ? load<T>(v, (int64_t)(at + t) * vs + h * a.dv + v0 + c) : 0.f;
-    }
-    if ((int)threadIdx.x < count) {
-        const int64_t i = (int64_t)(at + threadIdx.x) * a.hv + h;
+    if ((int)threadIdx.x < span.len) {
+        const int64_t i = (int64_t)(span.begin + threadIdx.x) * a.hv + h;
         s.a[threadIdx.x] = expf(a.g[i]);
         s.beta[threadIdx.x] = a.beta[i];
     }
@@ -78,21 +96,21 @@ __device__ inline float dot(const float (&x)[R], const float (&y)[R]) {
     return (p[0] + p[1]) + (p[2] + p[3]);
 }
 
-// A head's memory [dk][dv] at column v0 + r, this lane's R rows.
+// A head's memory [dk][dv] at one column, this lane's R rows.
 template <int R>
 __device__ inline void load_memory(const DeltaArgs &a, const float *m, int row0, int col, float (&S)[R]) {
+    const __amdgpu_buffer_rsrc_t p = rsrc_of(m);
 #pragma unroll
-    for (int i = 0; i < R; ++i) S[i] = m && row0 + i < a.dk && col < a.dv ? m[(row0 + i) * a.dv + col] : 0.f;
+    for (int i = 0; i < R; ++i) S[i] = load_if<float>(m && row0 + i < a.dk && col < a.dv, p, 4 * ((row0 + i) * a.dv + col));
 }
 template <int R>
 __device__ inline void store_memory(const DeltaArgs &a, float *m, int row0, int col, const float (&S)[R]) {
-    if (col < a.dv)
+    const __amdgpu_buffer_rsrc_t p = rsrc_of(m);
 #pragma unroll
-        for (int i = 0; i < R; ++i)
-            if (row0 + i < a.dk) m[(row0 + i) * a.dv + col] = S[i];
+    for (int i = 0; i < R; ++i) store_if(row0 + i < a.dk && col < a.dv, p, 4 * ((row0 + i) * a.dv + col), S[i]);
 }
 
-template <class T, int R, bool SAVE>
+template <class T, int R, bool SAVE, bool VEC>
 __global__ __launch_bounds__(kWaves * 64) void k_delta_short(DeltaArgs a) {
     __shared__ __align__(16) Stage<R> st;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
@@ -103,11 +121,11 @@ __global__ __launch_bounds__(kWaves * 64) void k_delta_short(DeltaArgs a) {
     const int64_t mem = ((int64_t)seq * a.hv + h) * a.dk * a.dv;
     float S[R];
     load_memory<R>(a, a.state ? a.state + mem : nullptr, row0, col, S);
+    fill<T, R, VEC>(a, st, a.v, a.vs, h, hk, v0, span);
+    __syncthreads();
     if constexpr (SAVE)
         if (span.len > 0)
             store_memory<R>(a, a.before + ((int64_t)slot_of(span, seq, 0) * a.hv + h) * a.dk * a.dv, row0, col, S);
-    fill<T, R>(a, st, a.v, a.vs, h, hk, v0, span);
-    __syncthreads();
     for (int t = 0; t < span.len; ++t) {
         float k[R], q[R];
         row_of<R>(&st.k[t][row0], k);
@@ -125,7 +143,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_delta_short(DeltaArgs a) {
     if (a.final_state) store_memory<R>(a, a.final_state + mem, row0, col, S);
 }
 
-template <class T, int R>
+template <class T, int R, bool VEC>
 __global__ __launch_bounds__(kWaves * 64) void k_delta_short_bwd(DeltaArgs a) {
     __shared__ __align__(16) Stage<R> st;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
@@ -136,7 +154,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_delta_short_bwd(DeltaArgs a) {
     const int64_t mem = ((int64_t)seq * a.hv + h) * a.dk * a.dv;
     float D[R];
     load_memory<R>(a, a.dfinal ? a.dfinal + mem : nullptr, row0, col, D);
-    fill<T, R>(a, st, a.dout, (int64_t)a.hv * a.dv, h, hk, v0, span);
+    fill<T, R, VEC>(a, st, a.dout, (int64_t)a.hv * a.dv, h, hk, v0, span);
     __syncthreads();
     for (int t = span.len - 1; t >= 0; --t) {
         float k[R], q[R];
@@ -394,28 +412,37 @@ __global__ __launch_bounds__(kWaves * 64, NT * TT == 1 ? 4 : 2) void k_delta_sho
 }
 
 template <class T, class F>
-hipError_t by_rows(const DeltaArgs &a, F &&go) {
+hipError_t by_rows(const DeltaArgs &a, const void *v, int64_t vs, F &&go) {
     if (a.n == 0) return hipSuccess;
     const dim3 grid(a.n * a.hv, (a.dv + kWaves * 16 - 1) / (kWaves * 16));
-    if (a.dk <= 32) go(std::integral_constant<int, 8>{}, grid);
-    else if (a.dk <= 64) go(std::integral_constant<int, 16>{}, grid);
-    else go(std::integral_constant<int, 32>{}, grid);
+    const auto even = [](const void *p, int64_t stride) {
+        return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0 && stride % 4 == 0;
+    };
+    const bool vec = a.dk % 4 == 0 && a.dv % 4 == 0 && even(a.k, a.ks) && even(a.q, a.qs) && even(v, vs);
+    const auto rows = [&](auto vec_) {
+        if (a.dk <= 32) go(std::integral_constant<int, 8>{}, vec_, grid);
+        else if (a.dk <= 64) go(std::integral_constant<int, 16>{}, vec_, grid);
+        else go(std::integral_constant<int, 32>{}, vec_, grid);
+    };
+    if (vec) rows(std::true_type{});
+    else rows(std::false_type{});
     return hipGetLastError();
 }
 
 template <class T>
 hipError_t forward(const DeltaArgs &a, hipStream_t s) {
-    return by_rows<T>(a, [&](auto r, dim3 grid) {
+    return by_rows<T>(a, a.v, a.vs, [&](auto r, auto vec, dim3 grid) {
         constexpr int R = decltype(r)::value;
-        if (a.before) k_delta_short<T, R, true><<<grid, kWaves * 64, 0, s>>>(a);
-        else k_delta_short<T, R, false><<<grid, kWaves * 64, 0, s>>>(a);
+        constexpr bool VEC = decltype(vec)::value;
+        if (a.before) k_delta_short<T, R, true, VEC><<<grid, kWaves * 64, 0, s>>>(a);
+        else k_delta_short<T, R, false, VEC><<<grid, kWaves * 64, 0, s>>>(a);
     });
 }
 
 template <class T>
 hipError_t backward(const DeltaArgs &a, hipStream_t s) {
-    const hipError_t walk = by_rows<T>(a, [&](auto r, dim3 grid) {
-        k_delta_short_bwd<T, decltype(r)::value><<<grid, kWaves * 64, 0, s>>>(a);
+    const hipError_t walk = by_rows<T>(a, a.dout, (int64_t)a.hv * a.dv, [&](auto r, auto vec, dim3 grid) {
+        k_delta_short_bwd<T, decltype(r)::value, decltype(vec)::value><<<grid, kWaves * 64, 0, s>>>(a);
     });
     if (walk != hipSuccess || a.n == 0) return walk;
     const auto even = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
