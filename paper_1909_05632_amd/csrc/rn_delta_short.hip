@@ -196,13 +196,28 @@ __global__ __launch_bounds__(kWaves * 64, NT * TT == 1 ? 4 : 2) void k_delta_sho
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int tiles = (len + 15) / 16;
     const Chunk c{seq, span.begin, len, len, true};
-    for (int i = threadIdx.x; i < rows * KP; i += kWaves * 64) {
-        const int t = i / KP, d = i % KP;
-        const bool in = t < len && d < a.dk;
-        sK[t * ldK + d] = in ? load<T>(a.k, (int64_t)(c.begin + t) * a.ks + hk * a.dk + d) : 0.f;
-        sQ[t * ldK + d] = in ? load<T>(a.q, (int64_t)(c.begin + t) * a.qs + hk * a.dk + d) : 0.f;
+    constexpr int PER = VEC ? 4 : 1;                    // VEC: dk, dv and strides multiples of 4, rows on that
+    {
+        const __amdgpu_buffer_rsrc_t pk = rsrc_of(static_cast<const T *>(a.k) + (int64_t)c.begin * a.ks + hk * a.dk);
+        const __amdgpu_buffer_rsrc_t pq = rsrc_of(static_cast<const T *>(a.q) + (int64_t)c.begin * a.qs + hk * a.dk);
+        constexpr int TP = kWaves * 64 * 4 / KP;        // tokens a pass
+        const int d = threadIdx.x % (KP / 4) * 4;
+#pragma unroll
+        for (int t0 = 0; t0 < rows; t0 += TP) {
+            const int t = t0 + threadIdx.x / (KP / 4);
+            f32x4 k, q;
+#pragma unroll
+            for (int e = 0; e < 4; e += PER) {
+                const bool in = t < len && d + e < a.dk;
+                const auto fk = load_if<Pack<T, PER>>(in, pk, sizeof(T) * (t * (uint32_t)a.ks + d + e));
+                const auto fq = load_if<Pack<T, PER>>(in, pq, sizeof(T) * (t * (uint32_t)a.qs + d + e));
+#pragma unroll
+                for (int j = 0; j < PER; ++j) k[e + j] = to_float(fk.v[j]), q[e + j] = to_float(fq.v[j]);
+            }
+            *reinterpret_cast<f32x4 *>(sK + t * ldK + d) = k;
+            *reinterpret_cast<f32x4 *>(sQ + t * ldK + d) = q;
+        }
     }
-    constexpr int PER = VEC ? 4 : 1;                    // VEC: dv a multiple of 4, rows on that
     const auto mfma = [](float u, float v, f32x4 &acc) { acc = __builtin_amdgcn_mfma_f32_16x16x4f32(u, v, acc, 0, 0, 0); };
     f32x4 tq[TT][NT], tk[TT][NT];                         // over the value heads
 #pragma unroll
@@ -243,27 +258,42 @@ __global__ __launch_bounds__(kWaves * 64, NT * TT == 1 ? 4 : 2) void k_delta_sho
             const uint32_t row = token * (uint32_t)(a.hv * a.dv);
             const float b = token < len ? a.beta[(int64_t)(c.begin + token) * a.hv + h] : 0.f;
             float db = 0.f;
-            for (int v = (threadIdx.x & 7) * 4; v < dvp; v += 32) {
-                f32x4 o, w, e;
+            for (int v0 = (threadIdx.x & 7) * 4; v0 < dvp; v0 += 64) {
+                Pack<T, PER> to[2][4 / PER];
+                Pack<float, PER> tw[2][4 / PER], te[2][4 / PER];
 #pragma unroll
-                for (int i = 0; i < 4; i += PER) {
-                    const bool in = token < len && v + i < a.dv;
-                    const auto to = load_if<Pack<T, PER>>(in, pO, sizeof(T) * (row + v + i));
-                    const auto tw = load_if<Pack<float, PER>>(in, pW, 4 * (row + v + i));
-                    const auto te = load_if<Pack<float, PER>>(in, pE, 4 * (row + v + i));
-                    Pack<T, PER> dv;
+                for (int u = 0; u < 2; ++u)             // all on their way before the first is used
 #pragma unroll
-                    for (int j = 0; j < PER; ++j) {
-                        o[i + j] = to_float(to.v[j]), w[i + j] = tw.v[j], e[i + j] = te.v[j];
-                        db = fmaf(w[i + j], e[i + j], db);
-                        e[i + j] *= b;
-                        dv.v[j] = from_float<T>(w[i + j] * b);
+                    for (int i = 0; i < 4; i += PER) {
+                        const int v = v0 + 32 * u + i;
+                        const bool in = token < len && v < a.dv;
+                        to[u][i / PER] = load_if<Pack<T, PER>>(in, pO, sizeof(T) * (row + v));
+                        tw[u][i / PER] = load_if<Pack<float, PER>>(in, pW, 4 * (row + v));
+                        te[u][i / PER] = load_if<Pack<float, PER>>(in, pE, 4 * (row + v));
                     }
-                    store_if(in, pV, sizeof(T) * (row + v + i), dv);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    f32x4 o, w, e;
+#pragma unroll
+                    for (int i = 0; i < 4; i += PER) {
+                        const int v = v0 + 32 * u + i;
+                        Pack<T, PER> dv;
+#pragma unroll
+                        for (int j = 0; j < PER; ++j) {
+                            o[i + j] = to_float(to[u][i / PER].v[j]), w[i + j] = tw[u][i / PER].v[j], e[i + j] = te[u][i / PER].v[j];
+                            db = fmaf(w[i + j], e[i + j], db);
+                            e[i + j] *= b;
+                            dv.v[j] = from_float<T>(w[i + j] * b);
+                        }
+                        store_if(token < len && v < a.dv, pV, sizeof(T) * (row + v), dv);
+                    }
+                    if (v0 + 32 * u < dvp) {
+                        const int at = token * ldV + v0 + 32 * u;
+                        *reinterpret_cast<f32x4 *>(sO + at) = o;
+                        *reinterpret_cast<f32x4 *>(sW + at) = w;
+                        *reinterpret_cast<f32x4 *>(sV + at) = e;
+                    }
                 }
-                *reinterpret_cast<f32x4 *>(sO + token * ldV + v) = o;
-                *reinterpret_cast<f32x4 *>(sW + token * ldV + v) = w;
-                *reinterpret_cast<f32x4 *>(sV + token * ldV + v) = e;
             }
 #pragma unroll
             for (int s = 1; s < 8; s <<= 1) db += __shfl_xor(db, s);
@@ -445,8 +475,8 @@ hipError_t backward(const DeltaArgs &a, hipStream_t s) {
         k_delta_short_bwd<T, decltype(r)::value, decltype(vec)::value><<<grid, kWaves * 64, 0, s>>>(a);
     });
     if (walk != hipSuccess || a.n == 0) return walk;
-    const auto even = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
-    const bool vec = a.dv % 4 == 0 && even(a.dout) && even(a.dval) && even(a.dfinal);
+    const auto even = [](const void *p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 4 == 0; };
+    const bool vec = a.dk % 4 == 0 && even(a.k, a.ks) && even(a.q, a.qs) && even(a.dout, a.dv) && even(a.dval, 0) && even(a.dfinal, 0);
     const auto grad = [&](auto nt_, auto tt_, auto vec_) -> hipError_t {
         constexpr int NT = decltype(nt_)::value, TT = decltype(tt_)::value, rows = 16 * TT;
         const int dvp = (a.dv + 31) / 32 * 32;
