@@ -213,7 +213,9 @@ __device__ inline int tri_t(int rb, int ks) { return rb < 2 ? rb * 2 + ks : rb +
 // are nearly parallel, as those of neighbouring frames are.)
 //
 // A chain of small steps with barriers between them: bound by their latency, so
-// the LDS is kept small (four blocks a CU in bfloat16) and the blocks many.
+// the LDS is kept small (four blocks a CU in bfloat16) and the blocks many: 81 us
+// for 16384 tokens of 16 value heads (4 key heads) of 128 bfloat16, which write 180
+// MB, 2.2 TB/s.
 template <class T, int KS, bool VEC, bool BWD>
 __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     constexpr int NP = sizeof(T) == 2 ? 1 : 3, NPP = sizeof(T) == 2 && !BWD ? 2 : 3;

@@ -13,7 +13,8 @@
 // multiply-adds and two swaps of lanes; nothing passes between waves but k and q,
 // which the block stages in LDS, all tokens at once.  Bound by those
 // multiply-adds (4 R a token and wave; 256 episodes of 16 tokens and 4 heads of
-// 64 x 64 take 9 us of them) and by the memories' bytes.
+// 64 x 64 take 9 us of them) and by the memories' bytes: those episodes take 20 us
+// for 50 MB forward and 19 back.
 #include "rn_delta.hpp"
 
 namespace rn {
@@ -176,8 +177,8 @@ __global__ __launch_bounds__(kWaves * 64) void k_delta_short_bwd(DeltaArgs a) {
 // planes to pay.  A block takes a sequence and a key head and adds the value heads
 // that share it; wave w owns the memory's row tiles w, w + 4.  The tokens' rows lie
 // in LDS, S and dS' are read once, as operands as they lie in memory.  Bound by
-// those bytes: 256 episodes of 16 tokens and 4 heads of 64 x 64, 16 us for 60 MB (56
-// us by chunks, whose operands it does without).
+// those bytes: 256 episodes of 16 tokens and 4 heads of 64 x 64, 24 us for 67 MB, 2.8
+// TB/s (56 us by chunks, whose operands it does without).
 template <class T, int NT, int TT, bool VEC>
 __global__ __launch_bounds__(kWaves * 64, NT * TT == 1 ? 4 : 2) void k_delta_short_grad(DeltaArgs a) {
     constexpr int rows = 16 * TT;                       // tokens there is room for
