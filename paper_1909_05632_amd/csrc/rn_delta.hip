@@ -133,7 +133,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
     __shared__ __align__(16) uint16_t sS[3 * VT * ldS], sR[3 * VT * ldT], sV[NPP * VT * ldT], sL[3 * VT * ldT];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const WalkBlock at = walk_block(a, (a.dv + VT - 1) / VT);
+    const WalkBlock at = walk_block(a);
     const int seq = at.seq, h = at.head, hk = h / (a.hv / a.hk), v0 = at.tile * VT;
     const Span span = span_of(a, seq);
     if (span.len <= a.short_len) return;                // taken token by token
@@ -350,7 +350,7 @@ hipError_t forward_ks(const DeltaArgs &a, hipStream_t s) {
     if (hipError_t e = launch_operands<T, KS, false>(a, s)) return e;
     const auto walk = [&](auto ct) {
         constexpr int CT = decltype(ct)::value;
-        const int grid = a.n * a.hv * ((a.dv + 16 * CT - 1) / (16 * CT));
+        const dim3 grid = walk_grid(a, 16 * CT);
         if (a.before) k_delta_walk<T, KS, CT, true><<<grid, 256, 0, s>>>(a);
         else k_delta_walk<T, KS, CT, false><<<grid, 256, 0, s>>>(a);
     };

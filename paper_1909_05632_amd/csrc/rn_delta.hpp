@@ -70,9 +70,9 @@ __device__ inline Chunk chunk_of(const DeltaArgs &a, int slot) {
 struct WalkBlock {
     int seq, head, tile;
 };
-__device__ inline WalkBlock walk_block(const DeltaArgs &a, int tiles) {
-    const int per = a.hv * tiles, i = blockIdx.x % per;
-    int seq = blockIdx.x / per;
+__device__ inline WalkBlock walk_block(const DeltaArgs &a) {
+    const int i = blockIdx.x;
+    int seq = blockIdx.y;
     if (a.off && a.n > 1 && a.n <= 64) {
         const int lane = threadIdx.x & 63, len = lane < a.n ? span_of(a, lane).len : -1;
         int before = 0;
@@ -84,6 +84,7 @@ __device__ inline WalkBlock walk_block(const DeltaArgs &a, int tiles) {
     }
     return {seq, i % a.hv, i / a.hv};
 }
+inline dim3 walk_grid(const DeltaArgs &a, int width) { return dim3(a.hv * ((a.dv + width - 1) / width), a.n); }
 
 // Log decays (base 2) summed up to each token of a chunk, in double: differences
 // of far tokens stay exact to float32 where the sums are large.  An empty memory

@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
     __shared__ __align__(16) uint16_t sS[3 * VT * ldS], sO[NP * VT * ldT], sG[3 * VT * ldT], sX[3 * VT * ldT], sL[3 * VT * ldT];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const WalkBlock at = walk_block(a, (a.dv + VT - 1) / VT);
+    const WalkBlock at = walk_block(a);
     const int seq = at.seq, h = at.head, hk = h / (a.hv / a.hk), v0 = at.tile * VT;
     const Span span = span_of(a, seq);
     if (span.len <= a.short_len) return;                // taken token by token
@@ -584,8 +584,8 @@ __global__ __launch_bounds__(KS == 4 ? 512 : 256, 2) void k_delta_bwd_chunk(Delt
 template <class T, int KS>
 hipError_t backward_ks(const DeltaArgs &a, hipStream_t s) {
     if (hipError_t e = launch_operands<T, KS, true>(a, s)) return e;
-    if (walk_tiles(a) == 1) k_delta_bwd_walk<T, KS, 1><<<a.n * a.hv * ((a.dv + 15) / 16), 256, 0, s>>>(a);
-    else k_delta_bwd_walk<T, KS, 2><<<a.n * a.hv * ((a.dv + 31) / 32), 256, 0, s>>>(a);
+    if (walk_tiles(a) == 1) k_delta_bwd_walk<T, KS, 1><<<walk_grid(a, 16), 256, 0, s>>>(a);
+    else k_delta_bwd_walk<T, KS, 2><<<walk_grid(a, 32), 256, 0, s>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
     const dim3 grid((int)delta_chunk_slots(a.tokens, a.n), a.hk);
     const auto even = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
