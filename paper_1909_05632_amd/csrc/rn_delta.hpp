@@ -195,6 +195,15 @@ constexpr int kTri = 6;
 // The same of its transpose.
 __device__ inline int tri_t(int rb, int ks) { return rb < 2 ? rb * 2 + ks : rb + 2; }
 
+// What lanes of this wave wrote to LDS before is there for its other lanes after:
+// the wave's LDS accesses run in order, so it is the compiler alone that must not move
+// one past another's.
+__device__ inline void wave_exchange() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // ---- the operands
 
 // The chunk operands of the walks, in fragment order: the triangular inverse, P
@@ -390,6 +399,7 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
             const f32x4 t = tile_mm(16, [&](int i, int k) { return l[i * kLd + k]; },
                                     [&](int k, int j) { return b[k * kLd + j]; }, f32x4{});
             put(y + wave * 16 * kLd, t, 1.f);           // y's first rows: P is out of them
+            wave_exchange();
             const f32x4 v = tile_mm(16, [&](int i, int k) { return l[i * kLd + 16 + k]; },
                                     [&](int k, int j) { return y[(wave * 16 + k) * kLd + j]; }, f32x4{});
             put(l, v, -1.f);

@@ -1,0 +1,37 @@
+"""Chunks of the gated delta rule where their triangular systems, their batches or
+their values are hard, on the GPU against the recurrence in 64 bits.  Inputs and
+tolerances are those of test_gpu_ops_delta.py unless a test derives its own."""
+import math
+
+import pytest
+import torch
+
+from tests import ops_ref as R
+from tests.conftest import gpu_available
+from tests.test_gpu_ops_delta import BF16, F32, NAMES, TOL, TOL_G, _inputs, _reference, _run
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not gpu_available(), reason="needs an MI355X GPU")]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("length", [33, 48, 49, 64, 65, 600])
+def test_write_strengths_up_to_two(length, dtype):
+    """Near-equal keys and beta up to 2, where the inverse's entries stay at 2 from the diagonal
+    to the corner: (I + A)^-1_ij = -beta (1 - beta)^(i-j-1).
+
+    Its 64 entries a row, each off by some 2^-24 of their size, no longer shrink: 64 x 2^-24 of a
+    chunk's errors E, four times that allowed, 1.5e-5, and as the memory hardly decays the chunks'
+    errors add up like their square root.  The gradients pass through two such systems, twice
+    that; those of g and beta are allowed more in the proportion of TOL_G to TOL."""
+    x, off = _inputs([length], 1, 2, 64, 64, dtype, near=8.0, decay=(1e-4, 1e-2), seed=length)
+    u = torch.rand(x["beta"].shape, generator=torch.Generator().manual_seed(5))
+    x["beta"] = 2.0 - 0.05 * u
+    x["beta"][:, 1] = 2.0
+    out, final, grads = _run(x, off, 0.125)
+    want, last, g = _reference(x, off, 0.125)
+    tol = 4 * 64 * 2.0 ** -24 * math.sqrt((length + 63) // 64)
+    own = 2.0 ** -9 if dtype is BF16 else 0.0
+    assert R.rel(out, want) <= tol + own and R.rel(final, last) <= tol
+    for got, name in zip(grads, NAMES + ("state",)):
+        more = TOL_G / TOL[F32] if name in ("g", "beta") else 1.0
+        assert R.rel(got, g[name]) <= 2 * tol * more + (own if got.dtype is BF16 else 0.0), name
