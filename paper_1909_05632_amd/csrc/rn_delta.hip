@@ -117,20 +117,17 @@ void step(const DeltaArgs &a, hipStream_t s) {
 // bf16 planes to the waves that multiply by it, as do V - e^c K S and V'.
 // The left operands are read from memory in fragment order, straight into
 // registers, each for the next chunk as soon as this one's use of it is over.
-// Bfloat16: S and V' have three planes in all that enters the memory, two, and P
-// two, in the output's products, which then drop what is below 2^-16 of an output
-// that is rounded to 2^-9.
 // Bound by a chunk's chain of four products with barriers between them, 2.6 us a
 // chunk (bfloat16, 128 x 128, two blocks a CU), of which matrix operations are a
 // sixth: 16384 tokens of 5 sequences and 16 heads in 230 us, 112 TFLOP/s of the
 // rule's own operations (25.8 GFLOP).
 template <class T, int KS, int CT, bool SAVE>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delta_walk(DeltaArgs a) {
-    constexpr int NP = sizeof(T) == 2 ? 1 : 3, NPP = sizeof(T) == 2 ? 2 : 3;
+    constexpr int NP = sizeof(T) == 2 ? 1 : 3;
     constexpr int KP = KS * 32, RT = KP > 64 ? KP / 64 : 1;        // row tiles of the memory a wave owns
     constexpr int VT = 16 * CT, ldS = KP + 8, ldT = kC + 8;
     constexpr int kKeys = 4 * KS * NP * kFrag;
-    __shared__ __align__(16) uint16_t sS[3 * VT * ldS], sR[3 * VT * ldT], sV[NPP * VT * ldT], sL[3 * VT * ldT];
+    __shared__ __align__(16) uint16_t sS[3 * VT * ldS], sR[3 * VT * ldT], sV[3 * VT * ldT], sL[3 * VT * ldT];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const WalkBlock at = walk_block(a);
@@ -180,7 +177,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
 
     // Loads are unconditional, from places clamped into the arrays, so that the
     // compiler can count them and wait for each only where it is used.
-    bf16x8 kf[KS][NP], qf[KS][NP], kt[RT][2][NP], mf[2][3], pf[2][NPP];
+    bf16x8 kf[KS][NP], qf[KS][NP], kt[RT][2][NP], mf[2][3], pf[2][3];
     T vv[CT][4];
     const auto load_rows = [&](int64_t slot) {
         const int64_t at = (slot * a.hk + hk) * kKeys + wave * KS * NP * kFrag;
@@ -203,10 +200,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
         for (int ks = 0; ks < 2; ++ks) load_frags<3>(a.mf + (at + tri(wave, min(ks, wave / 2)) * 3 * kFrag) + lane * 8, mf[ks]);
     };
     const auto load_score = [&](int64_t slot) {
-        const int64_t at = (slot * a.hv + h) * kTri * NPP * kFrag;
+        const int64_t at = (slot * a.hv + h) * kTri * 3 * kFrag;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
-            load_frags<NPP>(a.pf + (at + tri(wave, min(ks, wave / 2)) * NPP * kFrag) + lane * 8, pf[ks]);
+        for (int ks = 0; ks < 2; ++ks) load_frags<3>(a.pf + (at + tri(wave, min(ks, wave / 2)) * 3 * kFrag) + lane * 8, pf[ks]);
     };
     f32x4 grown{}, left{}, beta{}, next_grown{}, next_left{}, next_beta{};
     float whole = 0.f, next_whole = 0.f;
@@ -254,12 +250,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
             if (busy)
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    bf16x8 s[3], s2[NPP];
+                    bf16x8 s[3];
                     get8<3>(sS, VT * ldS, (n * 16 + r) * ldS + ks * 32 + g * 8, s);
-#pragma unroll
-                    for (int i = 0; i < NPP; ++i) s2[i] = s[i];
                     held = mm<NP, 3>(kf[ks], s, held);
-                    o[n] = mm<NP, NPP>(qf[ks], s2, o[n]);
+                    o[n] = mm<NP, 3>(qf[ks], s, o[n]);
                 }
             f32x4 w;
 #pragma unroll
@@ -292,7 +286,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] *= beta[j];
-            put4<NPP>(sV, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
+            put4<3>(sV, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] *= left[j];
             put4<3>(sL, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
@@ -325,9 +319,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks)
                     if (ks <= wave / 2) {
-                        bf16x8 b[NPP];
-                        get8<NPP>(sV, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
-                        o[n] = mm<NPP, NPP>(pf[ks], b, o[n]);
+                        bf16x8 b[3];
+                        get8<3>(sV, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
+                        o[n] = mm<3, 3>(pf[ks], b, o[n]);
                     }
             }
             const __amdgpu_buffer_rsrc_t rs = rsrc_of(out);

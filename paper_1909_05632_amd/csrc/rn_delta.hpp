@@ -228,7 +228,7 @@ __device__ inline void wave_exchange() {
 // MB, 2.2 TB/s.
 template <class T, int KS, bool VEC, bool BWD>
 __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
-    constexpr int NP = sizeof(T) == 2 ? 1 : 3, NPP = sizeof(T) == 2 && !BWD ? 2 : 3;
+    constexpr int NP = sizeof(T) == 2 ? 1 : 3;
     constexpr int kKeys = 4 * KS * NP * kFrag;          // bf16 of one of kf, qf, kt
     extern __shared__ __align__(16) float lds[];
     float *x = lds, *y = x + kC * kLd;                  // A, then its inverse; P, over K's fragments
@@ -349,8 +349,7 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     __syncthreads();
     // A triangular matrix's pieces into fragments, a lane's eight columns of a row
     // (BWD: of the transpose).
-    const auto pieces = [&](auto n_, const float *m, uint16_t *to, int start, int stride) {
-        constexpr int M = decltype(n_)::value;
+    const auto pieces = [&](const float *m, uint16_t *to, int start, int stride) {
         for (int i = start; i < kTri; i += stride) {
             const int rb = BWD ? (i < 4 ? i / 2 : i - 2) : i < 2 ? i : i / 2 + 1, ks = BWD ? (i < 4 ? i & 1 : 1) : i < 2 ? 0 : i & 1;
             if (rb >= blocks || ks * 32 >= c.len) continue;
@@ -358,12 +357,12 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 v[e] = BWD ? m[(ks * 32 + g * 8 + e) * kLd + rb * 16 + r] : m[(rb * 16 + r) * kLd + ks * 32 + g * 8 + e];
-            uint32_t q[4][M];
+            uint32_t q[4][3];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) split_pair<M>(v[2 * e], v[2 * e + 1], q[e]);
+            for (int e = 0; e < 4; ++e) split_pair<3>(v[2 * e], v[2 * e + 1], q[e]);
 #pragma unroll
-            for (int o = 0; o < M; ++o)
-                *reinterpret_cast<u32x4 *>(to + (ch * kTri + i) * M * kFrag + o * kFrag + lane * 8) =
+            for (int o = 0; o < 3; ++o)
+                *reinterpret_cast<u32x4 *>(to + (ch * kTri + i) * 3 * kFrag + o * kFrag + lane * 8) =
                     u32x4{q[0][o], q[1][o], q[2][o], q[3][o]};
         }
     };
@@ -385,7 +384,7 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[(g * 16 + i) * kLd + g * 16 + r] = col[i];
     } else {
-        pieces(std::integral_constant<int, NPP>{}, y, a.pf, wave - 1, 3);      // P meanwhile
+        pieces(y, a.pf, wave - 1, 3);                   // P meanwhile
     }
     __syncthreads();
     const auto put = [&](float *to, f32x4 v, float sign) {
@@ -419,7 +418,7 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
         put(l + ti * kLd + tj, v, -1.f);
         __syncthreads();
     }
-    pieces(std::integral_constant<int, 3>{}, x, a.mf, wave, 4);
+    pieces(x, a.mf, wave, 4);
 }
 
 // Column tiles of a walk's block.  Two share the left operands' loads; one has the

@@ -59,8 +59,7 @@ struct DeltaArgs {
     uint16_t *kf, *qf;            // K and Q as rows (qf: forward only)
     uint16_t *kt, *qt;            // K^T and Q^T as rows (qt: backward only)
     // Per chunk slot and value head:
-    uint16_t *mf;                 // the triangular inverse, three planes
-    uint16_t *pf;                 // P
+    uint16_t *mf, *pf;            // the triangular inverse and P, three planes each
     float *dec;                   // [3][64] e^c, e^(c64 - c), beta
     float *before;                // [dk][dv] states before the chunk, or NULL (not kept)
     float *err;                   // [tokens][hv][dv] v - S^T k as each token met it, or NULL
@@ -78,9 +77,8 @@ struct DeltaArgs {
 inline int64_t delta_chunk_slots(int64_t tokens, int n) { return tokens / RN_DELTA_CHUNK + n; }
 // 32-wide steps of dk in the chunk kernels (powers of two).
 inline int delta_ksteps(int dk) { return dk <= 32 ? 1 : dk <= 64 ? 2 : 4; }
-// bf16 planes of an input, and of P (the backward call has three of P).
+// bf16 planes of an input.
 inline int delta_planes(bool bf16) { return bf16 ? 1 : 3; }
-inline int delta_score_planes(bool bf16) { return bf16 ? 2 : 3; }
 // Token by token a sequence takes about 0.3 us a token and no scratch; by chunks
 // the operands and the walk cost as much as some 35 tokens whatever the chunk
 // holds (measured at dk 64 and 128), so short sequences go token by token.

@@ -59,7 +59,7 @@ bool too_wide(const rn_delta_shape *s) { return s->dk > RN_DELTA_MAX_DIM || s->d
 
 struct DeltaSizes {
     size_t states, tokens;                // bytes of a set of states, of [tokens][hv][dv] float32
-    size_t keys, inverse, score, decay;   // of kf, qf, kt or qt; mf; pf; dec
+    size_t keys, inverse, decay;          // of kf, qf, kt or qt; mf or pf; dec
     size_t map;
 };
 
@@ -69,8 +69,7 @@ DeltaSizes sizes(const rn_delta_shape *s) {
     return {round_up(slots * heads * s->dk * s->dv * 4),
             round_up((size_t)s->tokens * heads * s->dv * 4),
             round_up(slots * s->heads_k * 4 * delta_ksteps(s->dk) * delta_planes(bf16) * 1024),
-            round_up(slots * heads * 6 * 3 * 1024), round_up(slots * heads * 6 * delta_score_planes(bf16) * 1024),
-            round_up(slots * heads * 3 * RN_DELTA_CHUNK * 4), round_up(slots * 16)};
+            round_up(slots * heads * 6 * 3 * 1024), round_up(slots * heads * 3 * RN_DELTA_CHUNK * 4), round_up(slots * 16)};
 }
 
 DeltaArgs delta_args(const rn_delta_shape *s, const void *q, const void *k, const void *v, const float *g,
@@ -187,7 +186,7 @@ size_t reuse_ops_delta_saved_bytes(const rn_delta_shape *shape) {
 size_t reuse_ops_delta_scratch_bytes(const rn_delta_shape *shape) {
     if (bad_shape(shape) || too_wide(shape)) return 0;
     const DeltaSizes z = sizes(shape);
-    return 3 * z.keys + z.inverse + z.score + z.decay + kAlign;
+    return 3 * z.keys + 2 * z.inverse + z.decay + kAlign;
 }
 
 size_t reuse_ops_delta_backward_scratch_bytes(const rn_delta_shape *shape) {
@@ -220,7 +219,7 @@ rn_status reuse_ops_delta_forward(const rn_delta_shape *shape, const void *q, co
     a.kt = reinterpret_cast<uint16_t *>(at += z.keys);
     a.mf = reinterpret_cast<uint16_t *>(at += z.keys);
     a.pf = reinterpret_cast<uint16_t *>(at += z.inverse);
-    a.dec = reinterpret_cast<float *>(at += z.score);
+    a.dec = reinterpret_cast<float *>(at += z.inverse);
     if (saved) {
         a.before = reinterpret_cast<float *>(kept);
         a.err = reinterpret_cast<float *>(kept + z.states);
