@@ -7,6 +7,12 @@ give and passes pointers on: the work runs in the library's HIP kernels, on
 bfloat16 data are taken; statistics, memories, settings and the gradients of
 float32 arguments are float32.
 
+With ``stream`` a call does what it does under ``torch.cuda.stream(stream)``:
+results and scratch are that stream's memory, whose reuse is ordered on it.  As
+there, the caller orders the streams that write the arguments and read the
+results, and records (``Tensor.record_stream``) a tensor that another stream
+still uses when it is dropped.
+
 A policy that remembers, one frame of n streams at a time:
 
     x = layer_norm(features, w, b)
@@ -151,10 +157,17 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _launch(device, stream, call, *args) -> None:
-    """The call on `stream`, with the tensors' GPU current."""
+def _on(stream, x):
+    """`stream` as the current one, for the memory a call makes as well as for its launches."""
+    if isinstance(x, torch.Tensor) and x.is_cuda and x.device != stream.device:
+        raise ValueError(f"stream is on {stream.device}, the tensors are on {x.device}")
+    return torch.cuda.stream(stream)
+
+
+def _launch(device, call, *args) -> None:
+    """The call on the current stream, with the tensors' GPU current."""
     index = device.index
-    s = _raw_stream(index) if stream is None else stream.cuda_stream
+    s = _raw_stream(index)
     if torch.cuda.current_device() == index:
         status = call(*args, s)
     else:
@@ -180,6 +193,9 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, with_stats: bool = 
     weight, bias: [width] float32 or None.  Returns y in x's dtype, and with
     with_stats also the [rows][2] float32 mean and 1/sd for the backward call.
     """
+    if stream is not None:
+        with _on(stream, x):
+            return layer_norm(x, weight, bias, eps, with_stats, out)
     code = _data(x, "x")
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError("x must have a last axis of 1 or more")
@@ -193,7 +209,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, with_stats: bool = 
     else:
         y = _like(out, "out", x.dtype, dev, x.shape)
     stats = _empty(x, (rows, 2), _F32) if with_stats else None
-    _launch(dev, stream, load_ops().reuse_ops_layer_norm, rows, width, x.data_ptr(), stride, code, w, b, eps, y, width,
+    _launch(dev, load_ops().reuse_ops_layer_norm, rows, width, x.data_ptr(), stride, code, w, b, eps, y, width,
             None if stats is None else stats.data_ptr())
     return (out, stats) if with_stats else out
 
@@ -206,6 +222,9 @@ def layer_norm_backward(dy, x, weight, stats, dx=None, dweight=None, dbias=None,
     write, or to add to with accumulate; made here if None.  want_params =
     False: dx only, the other two are returned as given.
     """
+    if stream is not None:
+        with _on(stream, x):
+            return layer_norm_backward(dy, x, weight, stats, dx, dweight, dbias, accumulate, want_params)
     code = _data(x, "x")
     if not isinstance(dy, torch.Tensor) or dy.dtype is not x.dtype or dy.shape != x.shape or dy.device != x.device:
         raise ValueError("dy must have x's dtype, shape and device")
@@ -236,10 +255,8 @@ def layer_norm_backward(dy, x, weight, stats, dx=None, dweight=None, dbias=None,
         need = L.reuse_ops_layer_norm_backward_scratch_bytes(rows, width)
         scratch = _empty(x, need, torch.uint8)
         sc = scratch.data_ptr()
-    _launch(dev, stream, L.reuse_ops_layer_norm_backward, rows, width, dy.data_ptr(), dys, x.data_ptr(), xs, code, w,
+    _launch(dev, L.reuse_ops_layer_norm_backward, rows, width, dy.data_ptr(), dys, x.data_ptr(), xs, code, w,
             st, d, width, dw, db, int(accumulate), sc, need)
-    if sc and stream is not None:
-        scratch.record_stream(stream)             # its memory is not reused before the call has run
     return dx, dweight, dbias
 
 
@@ -253,6 +270,9 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=Non
     greedy, top_k 0 and top_p 1 leave the filter off.  Returns ([n] int32
     choices, [n] float32 log-probabilities among what the filters left).
     """
+    if stream is not None:
+        with _on(stream, logits):
+            return sample(logits, u, temperature, top_k, top_p, min_p, tokens, logprobs)
     code = _data(logits, "logits")
     if logits.dim() != 2:
         raise ValueError(f"logits must have shape (n, vocab), got {tuple(logits.shape)}")
@@ -279,7 +299,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=Non
         logprobs = _empty(logits, n, _F32)
     ids = _like(tokens, "tokens", _I32, dev, (n,))
     lp = _like(logprobs, "logprobs", _F32, dev, (n,))
-    _launch(dev, stream, load_ops().reuse_ops_sample, n, vocab, logits.data_ptr(), stride, code, up,
+    _launch(dev, load_ops().reuse_ops_sample, n, vocab, logits.data_ptr(), stride, code, up,
             ctypes.byref(params), ids, lp)
     return tokens, logprobs
 
@@ -349,6 +369,9 @@ def delta_step(q, k, v, g, beta, state, stream_ids=None, scale=None, out=None, s
     [n] int32 distinct slots (None: 0..n-1).  scale defaults to dk^-1/2.
     Returns out [n][heads_v][dv].
     """
+    if stream is not None:
+        with _on(stream, q):
+            return delta_step(q, k, v, g, beta, state, stream_ids, scale, out)
     n = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() else 0
     shape, gp, bp, dev, hv, dk, dv = _delta_shape(q, k, v, g, beta, n, scale)
     slots = state.shape[0] if isinstance(state, torch.Tensor) and state.dim() else 0
@@ -359,7 +382,7 @@ def delta_step(q, k, v, g, beta, state, stream_ids=None, scale=None, out=None, s
     if out is None:
         out = _empty(v)
     op = _like(out, "out", q.dtype, dev, (n, hv, dv))
-    _launch(dev, stream, load_ops().reuse_ops_delta_step, ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+    _launch(dev, load_ops().reuse_ops_delta_step, ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(),
             gp, bp, ids, slots, sp, op)
     return out
 
@@ -381,6 +404,9 @@ def delta_forward(q, k, v, g, beta, seq_off=None, n=None, state=None, final=None
     last ones go (made here if None; it may be state).  Returns (out, final),
     with save also the buffer that delta_backward reads.
     """
+    if stream is not None:
+        with _on(stream, q):
+            return delta_forward(q, k, v, g, beta, seq_off, n, state, final, scale, save, out)
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor of shape (tokens, heads, dk)")
     n, off = _sequences(seq_off, n, q.shape[0], q.device)
@@ -401,10 +427,8 @@ def delta_forward(q, k, v, g, beta, seq_off=None, n=None, state=None, final=None
         size = L.reuse_ops_delta_saved_bytes(ctypes.byref(shape))
         saved = _empty(q, size, torch.uint8)
         kept = saved.data_ptr()
-    _launch(dev, stream, L.reuse_ops_delta_forward, ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp,
+    _launch(dev, L.reuse_ops_delta_forward, ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp,
             bp, off, sp, fp, op, kept, size, scratch.data_ptr(), need)
-    if stream is not None:
-        scratch.record_stream(stream)
     return (out, final, saved) if save else (out, final)
 
 
@@ -415,6 +439,9 @@ def delta_backward(dout, q, k, v, g, beta, seq_off=None, n=None, saved=None, dfi
     The inputs are the forward call's, saved its buffer; dout: dJ/dout, dfinal:
     dJ/dfinal or None.  dstate is None without want_dstate.
     """
+    if stream is not None:
+        with _on(stream, q):
+            return delta_backward(dout, q, k, v, g, beta, seq_off, n, saved, dfinal, scale, want_dstate)
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor of shape (tokens, heads, dk)")
     n, off = _sequences(seq_off, n, q.shape[0], q.device)
@@ -430,9 +457,7 @@ def delta_backward(dout, q, k, v, g, beta, seq_off=None, n=None, saved=None, dfi
     gq, gk, gv, dg, dbeta = _empty(q), _empty(k), _empty(v), _empty(g), _empty(beta)
     dstate = _empty(q, dims, _F32) if want_dstate else None
     scratch = _empty(q, need, torch.uint8)
-    _launch(dev, stream, L.reuse_ops_delta_backward, ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp,
+    _launch(dev, L.reuse_ops_delta_backward, ctypes.byref(shape), q.data_ptr(), k.data_ptr(), v.data_ptr(), gp,
             bp, off, sp, saved.numel(), do, df, gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), dg.data_ptr(),
             dbeta.data_ptr(), None if dstate is None else dstate.data_ptr(), scratch.data_ptr(), need)
-    if stream is not None:
-        scratch.record_stream(stream)
     return gq, gk, gv, dg, dbeta, dstate
