@@ -135,6 +135,10 @@ typedef struct {
     /* Elements from a token to the next; heads are contiguous within a token
      * (q, k: [heads_k][dk], v: [heads_v][dv]).  Below 2^23. */
     int64_t q_stride, k_stride, v_stride;
+    /* Not 0: every sequence has tokens / n of them, and seq_off will be NULL.  The
+     * sizes below are then those of the way such sequences take; 0 allows for any
+     * lengths. */
+    int32_t even;
 } rn_delta_shape;
 
 /* One token for each of n streams (tokens = n), the memory updated in place.
@@ -149,7 +153,13 @@ rn_status reuse_ops_delta_step(const rn_delta_shape *shape, const void *dev_q, c
 
 /* Bytes of the buffer a forward call leaves for the backward call, and of the
  * scratch each call needs (0 if the shape is not supported; every size is at
- * least 256). */
+ * least 256).  Where a call has 32 tokens a sequence on average or fewer, sequences
+ * of up to 32 go token by token and take no scratch in the forward call.  All
+ * others are taken by chunks of RN_DELTA_CHUNK tokens, each of which takes 37 KiB a
+ * value head, and a key head 12 KiB (bfloat16) or 36 KiB (float32) for dk up to 32,
+ * twice that up to 64, four times above; in the backward call also a memory.
+ * seq_off is not known when the sizes are asked for: without `even` they allow for
+ * as many chunks as any lengths can have. */
 size_t reuse_ops_delta_saved_bytes(const rn_delta_shape *shape);
 size_t reuse_ops_delta_scratch_bytes(const rn_delta_shape *shape);
 size_t reuse_ops_delta_backward_scratch_bytes(const rn_delta_shape *shape);

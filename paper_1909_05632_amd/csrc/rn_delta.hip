@@ -135,7 +135,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
     const Span span = span_of(a, seq);
     if (span.len <= a.short_len) return;                // taken token by token
     const int chunks = (span.len + kC - 1) / kC;
-    const int64_t slot0 = slot_of(span, seq, 0);
+    const int64_t slot0 = slot_of(a, span.begin, seq);
     const int64_t sbase = ((int64_t)seq * a.hv + h) * a.dk * a.dv + v0;
     const bool owner = KP >= 64 || wave * 16 < KP;
     bool col_in[CT];
@@ -235,12 +235,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
 
     const auto step = [&](int chunk, auto more_) {
         constexpr bool more = decltype(more_)::value;   // every chunk but the last: 64 tokens, and one follows
-        const int64_t next = slot0 + chunk + 1, ch = (slot0 + chunk) * a.hv + h;
+        const int64_t next = slot0 + chunk + 1;
         const int len = more ? kC : span.len - chunk * kC;
         const bool busy = more || wave * 16 < len;      // any token of this wave
         const bool half2 = more || len > 32;            // tokens in the second 32
         grown = next_grown, left = next_left, beta = next_beta, whole = next_whole;
-        if constexpr (SAVE) write_state(a.before + ch * a.dk * a.dv + v0);
+        if constexpr (SAVE) {
+            const int64_t kept = kept_slot_of(span.begin, seq) + chunk;
+            write_state(a.before + (kept * a.hv + h) * a.dk * a.dv + v0);
+        }
         dev::lds_barrier();                             // the memory's planes are there
         f32x4 o[CT];
 #pragma unroll
@@ -370,7 +373,7 @@ hipError_t launch_delta_step(const DeltaArgs &a, bool bf16, hipStream_t s) {
 
 hipError_t launch_delta_forward(const DeltaArgs &args, bool bf16, hipStream_t s) {
     DeltaArgs a = args;
-    const DeltaWays w = delta_ways(a);
+    const DeltaWays w = delta_ways(a.tokens, a.n, !a.off);
     a.short_len = w.tokens ? kShort : -1;
     if (w.tokens)
         if (hipError_t e = launch_delta_short_forward(a, bf16, s)) return e;

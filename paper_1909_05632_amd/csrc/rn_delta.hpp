@@ -39,10 +39,16 @@ __device__ inline Span span_of(const DeltaArgs &a, int i) {
     const int b = offset_of(a, i), e = offset_of(a, i + 1);
     return {b, e > b ? e - b : 0};
 }
-__device__ inline int slot_of(const Span &s, int i, int chunk) { return s.begin / kC + i + chunk; }
+// The slot of sequence i's first chunk among the operands (delta_slots), and among
+// the memories kept (delta_kept_slots); the next chunks' follow.
+__device__ inline int slot_of(const DeltaArgs &a, int begin, int i) {
+    return a.short_len >= 0 ? begin / kShort : begin / kC + i;
+}
+__device__ inline int kept_slot_of(int begin, int i) { return begin / kC + i; }
 
 // The sequence and chunk of a chunk slot: the last sequence whose first slot is
-// not beyond it.  Slots that no chunk has give len 0.
+// not beyond it.  Slots that no chunk has give len 0, or a sequence taken token by
+// token.
 struct Chunk {
     int seq, begin, len;          // tokens begin .. begin + len - 1, len <= 64
     int whole;                    // tokens of the sequence
@@ -52,12 +58,12 @@ __device__ inline Chunk chunk_of(const DeltaArgs &a, int slot) {
     int lo = 0, hi = a.n - 1;
     while (lo < hi) {                                   // 64 places at once
         const int step = (hi - lo + 63) / 64, at = lo + ((int)(threadIdx.x & 63) + 1) * step;
-        const bool up = at <= hi && offset_of(a, min(at, hi)) / kC + at <= slot;
+        const bool up = at <= hi && slot_of(a, offset_of(a, min(at, hi)), at) <= slot;
         lo += __popcll(__ballot(up)) * step;
         hi = min(hi, lo + step - 1);
     }
     const Span s = span_of(a, lo);
-    const int64_t at = (int64_t)(slot - slot_of(s, lo, 0)) * kC;
+    const int64_t at = (int64_t)(slot - slot_of(a, s.begin, lo)) * kC;
     if (at < 0 || at >= s.len) return {lo, 0, 0, 0, false};
     return {lo, s.begin + (int)at, min(kC, s.len - (int)at), s.len, at + kC >= s.len};
 }
@@ -444,7 +450,7 @@ hipError_t launch_operands(const DeltaArgs &a, hipStream_t s) {
     const bool vec = a.dk % 8 == 0 && even(a.q, a.qs) && even(a.k, a.ks);
     auto *kernel = vec ? k_delta_operands<T, KS, true, BWD> : k_delta_operands<T, KS, false, BWD>;
     if (hipError_t e = allow_lds(kernel, bytes)) return e;
-    kernel<<<dim3((int)delta_chunk_slots(a.tokens, a.n), a.hv), 256, bytes, s>>>(a);
+    kernel<<<dim3((int)delta_slots(a.tokens, a.n, !a.off), a.hv), 256, bytes, s>>>(a);
     return hipGetLastError();
 }
 

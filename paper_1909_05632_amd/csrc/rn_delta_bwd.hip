@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
     const Span span = span_of(a, seq);
     if (span.len <= a.short_len) return;                // taken token by token
     const int chunks = (span.len + kC - 1) / kC;
-    const int64_t slot0 = slot_of(span, seq, 0);
+    const int64_t slot0 = slot_of(a, span.begin, seq);
     const int64_t sbase = ((int64_t)seq * a.hv + h) * a.dk * a.dv + v0;
     const bool owner = KP >= 64 || wave * 16 < KP;
     bool col_in[CT];
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(KS == 4 ? 512 : 256, 2) void k_delta_bwd_chunk(Delt
     const uint32_t lane_ = threadIdx.x & 63;
     const int blocks = (c.len + 15) / 16, half = (c.len + 31) / 32;
     const bool busy = wave < blocks;
-    const int64_t keys = ((int64_t)slot * a.hk + hk) * kKeys;
+    const int64_t keys = ((int64_t)slot * a.hk + hk) * kKeys, kept = kept_slot_of(c.begin, c.seq);
     // Sum over the 16 lanes that hold a row's columns.
     const auto across = [&](float v) {
 #pragma unroll
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(KS == 4 ? 512 : 256, 2) void k_delta_bwd_chunk(Delt
         // the gradient of the memory after the chunk: dfinal after a sequence's last
         const int64_t mem = (int64_t)a.dk * a.dv;
         const bool no_after = c.last && !a.dfinal;
-        const __amdgpu_buffer_rsrc_t pS = rsrc_of(a.before + ch * mem), pE = rsrc_of(a.err + row0), pW = rsrc_of(a.dwrite + row0);
+        const __amdgpu_buffer_rsrc_t pS = rsrc_of(a.before + (kept * a.hv + h) * mem), pE = rsrc_of(a.err + row0), pW = rsrc_of(a.dwrite + row0);
         const __amdgpu_buffer_rsrc_t pD = rsrc_of(c.last && a.dfinal ? a.dfinal + ((int64_t)c.seq * a.hv + h) * mem : a.after + ch * mem);
         const __amdgpu_buffer_rsrc_t pO = rsrc_of(static_cast<const T *>(a.dout) + row0);
         const __amdgpu_buffer_rsrc_t pV = rsrc_of(static_cast<T *>(a.dval) + row0);
@@ -587,7 +587,7 @@ hipError_t backward_ks(const DeltaArgs &a, hipStream_t s) {
     if (walk_tiles(a) == 1) k_delta_bwd_walk<T, KS, 1><<<walk_grid(a, 16), 256, 0, s>>>(a);
     else k_delta_bwd_walk<T, KS, 2><<<walk_grid(a, 32), 256, 0, s>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
-    const dim3 grid((int)delta_chunk_slots(a.tokens, a.n), a.hk);
+    const dim3 grid((int)delta_slots(a.tokens, a.n, !a.off), a.hk);
     const auto even = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
     const bool vec = a.dv % 8 == 0 && even(a.dout) && even(a.dval) && even(a.dfinal);
     const auto chunk = [&](auto vec_) {
@@ -610,7 +610,7 @@ hipError_t backward(const DeltaArgs &a, hipStream_t s) {
 
 hipError_t launch_delta_backward(const DeltaArgs &args, bool bf16, hipStream_t s) {
     DeltaArgs a = args;
-    const DeltaWays w = delta_ways(a);
+    const DeltaWays w = delta_ways(a.tokens, a.n, !a.off);
     a.short_len = w.tokens ? kShort : -1;
     if (w.tokens)
         if (hipError_t e = launch_delta_short_backward(a, bf16, s)) return e;

@@ -126,7 +126,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_delta_short(DeltaArgs a) {
     __syncthreads();
     if constexpr (SAVE)
         if (span.len > 0)
-            store_memory<R>(a, a.before + ((int64_t)slot_of(span, seq, 0) * a.hv + h) * a.dk * a.dv, row0, col, S);
+            store_memory<R>(a, a.before + ((int64_t)kept_slot_of(span.begin, seq) * a.hv + h) * a.dk * a.dv, row0, col, S);
     for (int t = 0; t < span.len; ++t) {
         float k[R], q[R];
         row_of<R>(&st.k[t][row0], k);
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(kWaves * 64, NT * TT == 1 ? 4 : 2) void k_delta_sho
         for (int n = 0; n < NT; ++n) tq[t][n] = tk[t][n] = f32x4{};
     for (int h = hk * group; h < (hk + 1) * group; ++h) {
         const int64_t mem = (int64_t)a.dk * a.dv, row0 = ((int64_t)c.begin * a.hv + h) * a.dv;
-        const __amdgpu_buffer_rsrc_t pS = rsrc_of(a.before + ((int64_t)slot_of(span, seq, 0) * a.hv + h) * mem);
+        const __amdgpu_buffer_rsrc_t pS = rsrc_of(a.before + ((int64_t)kept_slot_of(span.begin, seq) * a.hv + h) * mem);
         const __amdgpu_buffer_rsrc_t pD = rsrc_of(a.dfinal ? a.dfinal + ((int64_t)seq * a.hv + h) * mem : a.before);
         struct Step {                                   // 32 columns of S and of dS'
             Pack<float, PER> s[NT][2][4 / PER], d[NT][2][4 / PER];

@@ -55,13 +55,13 @@ struct DeltaArgs {
     const float *state;           // first states, or NULL
     float *final_state;           // last states, or NULL (step: the state pool)
     void *out;
-    // Per chunk slot (delta_chunk_slots) and key head, in fragment order (rn_delta.hpp):
+    // Per chunk slot (delta_slots) and key head, in fragment order (rn_delta.hpp):
     uint16_t *kf, *qf;            // K and Q as rows (qf: forward only)
     uint16_t *kt, *qt;            // K^T and Q^T as rows (qt: backward only)
     // Per chunk slot and value head:
     uint16_t *mf, *pf;            // the triangular inverse and P, three planes each
     float *dec;                   // [3][64] e^c, e^(c64 - c), beta
-    float *before;                // [dk][dv] states before the chunk, or NULL (not kept)
+    float *before;                // [delta_kept_slots][hv][dk][dv] states before each chunk, or NULL (not kept)
     float *err;                   // [tokens][hv][dv] v - S^T k as each token met it, or NULL
     // Backward call:
     const void *dout;
@@ -72,9 +72,6 @@ struct DeltaArgs {
     void *dq, *dkey, *dval;
     float *dg, *dbeta, *dstate;
 };
-// Chunk slots of a call: chunk c of sequence i has slot off[i] / 64 + i + c, so
-// every slot is below tokens / 64 + n and no two chunks share one.
-inline int64_t delta_chunk_slots(int64_t tokens, int n) { return tokens / RN_DELTA_CHUNK + n; }
 // 32-wide steps of dk in the chunk kernels (powers of two).
 inline int delta_ksteps(int dk) { return dk <= 32 ? 1 : dk <= 64 ? 2 : 4; }
 // bf16 planes of an input.
@@ -88,15 +85,25 @@ constexpr int kShort = 32;
 struct DeltaWays {
     bool tokens, chunks;
 };
-inline DeltaWays delta_ways(const DeltaArgs &a) {
-    if (a.tokens == 0 || !a.off) {
-        const bool t = a.tokens <= (int64_t)kShort * a.n;
-        return {t, !t};
-    }
-    if (a.tokens <= kShort) return {true, false};
-    const bool t = a.tokens <= (int64_t)kShort * a.n;
+inline DeltaWays delta_ways(int64_t tokens, int n, bool even) {
+    const bool t = tokens <= (int64_t)kShort * n;
+    if (even || tokens == 0) return {t, !t};
+    if (tokens <= kShort) return {true, false};
     return {t, true};
 }
+// Slots of what is kept for the backward call, whichever way a sequence goes: chunk
+// c of sequence i has slot off[i] / 64 + i + c, so every slot is below
+// tokens / 64 + n and no two chunks share one.
+inline int64_t delta_kept_slots(int64_t tokens, int n) { return tokens / RN_DELTA_CHUNK + n; }
+// Slots of the chunk kernels' operands: the same, unless sequences of up to kShort
+// tokens go token by token, which have none.  The others' chunks then have slots
+// off[i] / 32 + c: a sequence of 33 tokens or more moves off / 32 on by its chunks
+// at least.  (They would otherwise take operands of 64 tokens for every sequence.)
+inline int64_t delta_slots(int64_t tokens, int n, bool even) {
+    const DeltaWays w = delta_ways(tokens, n, even);
+    return !w.chunks ? 0 : w.tokens ? tokens / kShort : delta_kept_slots(tokens, n);
+}
+static_assert(2 * kShort == RN_DELTA_CHUNK);
 hipError_t launch_delta_step(const DeltaArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_delta_short_forward(const DeltaArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_delta_short_backward(const DeltaArgs &a, bool bf16, hipStream_t s);

@@ -46,6 +46,7 @@ const char *bad_shape(const rn_delta_shape *s) {
     if (s->dk < 1 || s->dv < 1) return "dk and dv must be 1 or more";
     if (s->tokens < 0 || s->tokens > INT32_MAX) return "tokens must be 0..2^31 - 1";
     if (s->n == 0 && s->tokens > 0) return "tokens without sequences";
+    if (s->even && s->n > 0 && s->tokens % s->n) return "of even sequences, tokens must be a multiple of n";
     if (!known(s->dtype)) return "dtype must be RN_F32 or RN_BF16";
     if (s->tokens > 1 && (s->q_stride < (int64_t)s->heads_k * s->dk || s->k_stride < (int64_t)s->heads_k * s->dk ||
                           s->v_stride < (int64_t)s->heads_v * s->dv))
@@ -58,18 +59,29 @@ const char *bad_shape(const rn_delta_shape *s) {
 bool too_wide(const rn_delta_shape *s) { return s->dk > RN_DELTA_MAX_DIM || s->dv > RN_DELTA_MAX_DIM; }
 
 struct DeltaSizes {
-    size_t states, tokens;                // bytes of a set of states, of [tokens][hv][dv] float32
+    size_t kept, states, tokens;          // bytes of before; after; [tokens][hv][dv] float32
     size_t keys, inverse, decay;          // of kf, qf, kt or qt; mf or pf; dec
     size_t map;
 };
 
-DeltaSizes sizes(const rn_delta_shape *s) {
-    const size_t slots = (size_t)delta_chunk_slots(s->tokens, s->n), heads = s->heads_v;
+DeltaSizes sizes(const rn_delta_shape *s, bool even) {
+    const size_t slots = (size_t)delta_slots(s->tokens, s->n, even), heads = s->heads_v;
     const bool bf16 = s->dtype == RN_BF16;
-    return {round_up(slots * heads * s->dk * s->dv * 4),
+    return {round_up((size_t)delta_kept_slots(s->tokens, s->n) * heads * s->dk * s->dv * 4),
+            round_up(slots * heads * s->dk * s->dv * 4),
             round_up((size_t)s->tokens * heads * s->dv * 4),
             round_up(slots * s->heads_k * 4 * delta_ksteps(s->dk) * delta_planes(bf16) * 1024),
             round_up(slots * heads * 6 * 3 * 1024), round_up(slots * heads * 3 * RN_DELTA_CHUNK * 4), round_up(slots * 16)};
+}
+
+size_t forward_bytes(const rn_delta_shape *s, bool even) {
+    const DeltaSizes z = sizes(s, even);
+    return 3 * z.keys + 2 * z.inverse + z.decay + kAlign;
+}
+
+size_t backward_bytes(const rn_delta_shape *s, bool even) {
+    const DeltaSizes z = sizes(s, even);
+    return 3 * z.keys + 2 * z.inverse + z.decay + z.states + z.tokens + z.map + kAlign;
 }
 
 DeltaArgs delta_args(const rn_delta_shape *s, const void *q, const void *k, const void *v, const float *g,
@@ -179,20 +191,18 @@ rn_status reuse_ops_delta_step(const rn_delta_shape *shape, const void *q, const
 
 size_t reuse_ops_delta_saved_bytes(const rn_delta_shape *shape) {
     if (bad_shape(shape) || too_wide(shape)) return 0;
-    const DeltaSizes z = sizes(shape);
-    return z.states + z.tokens + kAlign;
+    const DeltaSizes z = sizes(shape, shape->even);
+    return z.kept + z.tokens + kAlign;
 }
 
 size_t reuse_ops_delta_scratch_bytes(const rn_delta_shape *shape) {
     if (bad_shape(shape) || too_wide(shape)) return 0;
-    const DeltaSizes z = sizes(shape);
-    return 3 * z.keys + 2 * z.inverse + z.decay + kAlign;
+    return forward_bytes(shape, shape->even);
 }
 
 size_t reuse_ops_delta_backward_scratch_bytes(const rn_delta_shape *shape) {
     if (bad_shape(shape) || too_wide(shape)) return 0;
-    const DeltaSizes z = sizes(shape);
-    return 3 * z.keys + 2 * z.inverse + z.decay + z.states + z.tokens + z.map + kAlign;
+    return backward_bytes(shape, shape->even);
 }
 
 rn_status reuse_ops_delta_forward(const rn_delta_shape *shape, const void *q, const void *k, const void *v,
@@ -200,6 +210,7 @@ rn_status reuse_ops_delta_forward(const rn_delta_shape *shape, const void *q, co
                                   float *final_state, void *out, void *saved, size_t saved_bytes, void *scratch,
                                   size_t scratch_bytes, void *stream) {
     if (rn_status s = check_delta(shape, q, k, v, g, beta)) return s;
+    if (shape->even && seq_off) return fail(RN_EINVAL, "even sequences have no seq_off");
     if (!seq_off && shape->n > 0 && shape->tokens % shape->n)
         return fail(RN_EINVAL, "without seq_off, tokens must be a multiple of n");
     if (shape->n == 0) return RN_OK;
@@ -208,9 +219,9 @@ rn_status reuse_ops_delta_forward(const rn_delta_shape *shape, const void *q, co
     if (saved && saved_bytes < reuse_ops_delta_saved_bytes(shape))
         return need_bytes("saved", reuse_ops_delta_saved_bytes(shape));
     if (!scratch) return fail(RN_EINVAL, "scratch is NULL");
-    const size_t need = reuse_ops_delta_scratch_bytes(shape);
+    const size_t need = forward_bytes(shape, !seq_off);
     if (scratch_bytes < need) return need_bytes("scratch", need);
-    const DeltaSizes z = sizes(shape);
+    const DeltaSizes z = sizes(shape, !seq_off);
     char *kept = static_cast<char *>(saved), *at = static_cast<char *>(scratch);
     DeltaArgs a = delta_args(shape, q, k, v, g, beta);
     a.off = seq_off, a.state = state, a.final_state = final_state, a.out = out;
@@ -222,7 +233,7 @@ rn_status reuse_ops_delta_forward(const rn_delta_shape *shape, const void *q, co
     a.dec = reinterpret_cast<float *>(at += z.inverse);
     if (saved) {
         a.before = reinterpret_cast<float *>(kept);
-        a.err = reinterpret_cast<float *>(kept + z.states);
+        a.err = reinterpret_cast<float *>(kept + z.kept);
     }
     return launched(launch_delta_forward(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
 }
@@ -233,6 +244,7 @@ rn_status reuse_ops_delta_backward(const rn_delta_shape *shape, const void *q, c
                                    void *dv, float *dg, float *dbeta, float *dstate, void *scratch,
                                    size_t scratch_bytes, void *stream) {
     if (rn_status s = check_delta(shape, q, k, v, g, beta)) return s;
+    if (shape->even && seq_off) return fail(RN_EINVAL, "even sequences have no seq_off");
     if (!seq_off && shape->n > 0 && shape->tokens % shape->n)
         return fail(RN_EINVAL, "without seq_off, tokens must be a multiple of n");
     if (shape->n == 0) return RN_OK;
@@ -242,14 +254,14 @@ rn_status reuse_ops_delta_backward(const rn_delta_shape *shape, const void *q, c
     if (!saved || !scratch) return fail(RN_EINVAL, "saved and scratch must not be NULL");
     if (misaligned(saved) || misaligned(scratch)) return fail(RN_EINVAL, "saved and scratch must be 256-byte aligned");
     if (saved_bytes < reuse_ops_delta_saved_bytes(shape)) return need_bytes("saved", reuse_ops_delta_saved_bytes(shape));
-    const size_t need = reuse_ops_delta_backward_scratch_bytes(shape);
+    const size_t need = backward_bytes(shape, !seq_off);
     if (scratch_bytes < need) return need_bytes("scratch", need);
-    const DeltaSizes z = sizes(shape);
+    const DeltaSizes z = sizes(shape, !seq_off);
     char *kept = const_cast<char *>(static_cast<const char *>(saved)), *at = static_cast<char *>(scratch);
     DeltaArgs a = delta_args(shape, q, k, v, g, beta);
     a.off = seq_off;
     a.before = reinterpret_cast<float *>(kept);
-    a.err = reinterpret_cast<float *>(kept + z.states);
+    a.err = reinterpret_cast<float *>(kept + z.kept);
     a.dout = dout, a.dfinal = dfinal;
     a.kf = reinterpret_cast<uint16_t *>(at);
     a.kt = reinterpret_cast<uint16_t *>(at += z.keys);

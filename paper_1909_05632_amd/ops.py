@@ -54,7 +54,7 @@ class rn_delta_shape(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int32), ("heads_k", ctypes.c_int32), ("heads_v", ctypes.c_int32),
                 ("dk", ctypes.c_int32), ("dv", ctypes.c_int32), ("tokens", ctypes.c_int64), ("dtype", ctypes.c_int),
                 ("scale", ctypes.c_float), ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
-                ("v_stride", ctypes.c_int64)]
+                ("v_stride", ctypes.c_int64), ("even", ctypes.c_int32)]
 
 
 _ops = None
@@ -327,7 +327,7 @@ def _tokens(x, what: str, dtype, tokens: int, device):
     return heads, size, (st[0] if tokens > 1 else heads * size)
 
 
-def _delta_shape(q, k, v, g, beta, n: int, scale):
+def _delta_shape(q, k, v, g, beta, n: int, scale, even: bool = True):
     code = _data(q, "q")
     if q.dim() != 3:
         raise ValueError(f"q must have shape (tokens, heads, dk), got {tuple(q.shape)}")
@@ -339,7 +339,7 @@ def _delta_shape(q, k, v, g, beta, n: int, scale):
         raise ValueError("k must have q's shape")
     if hv % hk:
         raise ValueError(f"{hv} value heads cannot share {hk} key heads")
-    shape = rn_delta_shape(n, hk, hv, dk, dv, tokens, code, dk ** -0.5 if scale is None else scale, qs, ks, vs)
+    shape = rn_delta_shape(n, hk, hv, dk, dv, tokens, code, dk ** -0.5 if scale is None else scale, qs, ks, vs, even)
     gp = _like(g, "g", _F32, dev, (tokens, hv))
     bp = _like(beta, "beta", _F32, dev, (tokens, hv))
     return shape, gp, bp, dev, hv, dk, dv
@@ -410,7 +410,7 @@ def delta_forward(q, k, v, g, beta, seq_off=None, n=None, state=None, final=None
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor of shape (tokens, heads, dk)")
     n, off = _sequences(seq_off, n, q.shape[0], q.device)
-    shape, gp, bp, dev, hv, dk, dv = _delta_shape(q, k, v, g, beta, n, scale)
+    shape, gp, bp, dev, hv, dk, dv = _delta_shape(q, k, v, g, beta, n, scale, off is None)
     dims = (n, hv, dk, dv)
     sp = _opt(state, "state", _F32, dev, dims)
     L = load_ops()
@@ -445,7 +445,7 @@ def delta_backward(dout, q, k, v, g, beta, seq_off=None, n=None, saved=None, dfi
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor of shape (tokens, heads, dk)")
     n, off = _sequences(seq_off, n, q.shape[0], q.device)
-    shape, gp, bp, dev, hv, dk, dv = _delta_shape(q, k, v, g, beta, n, scale)
+    shape, gp, bp, dev, hv, dk, dv = _delta_shape(q, k, v, g, beta, n, scale, off is None)
     dims = (n, hv, dk, dv)
     do = _like(dout, "dout", q.dtype, dev, v.shape)
     df = _opt(dfinal, "dfinal", _F32, dev, dims)

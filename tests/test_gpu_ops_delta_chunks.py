@@ -2,13 +2,14 @@
 their values are hard, on the GPU against the recurrence in 64 bits.  Inputs and
 tolerances are those of test_gpu_ops_delta.py unless a test derives its own."""
 import math
+import random
 
 import pytest
 import torch
 
 from tests import ops_ref as R
 from tests.conftest import gpu_available
-from tests.test_gpu_ops_delta import BF16, F32, NAMES, TOL, TOL_G, _inputs, _reference, _run
+from tests.test_gpu_ops_delta import BF16, F32, NAMES, TOL, TOL_G, _compare, _inputs, _reference, _run
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not gpu_available(), reason="needs an MI355X GPU")]
 
@@ -72,3 +73,19 @@ def test_bfloat16_outputs_are_sums_in_float32(what):
     largest = want[2:].abs().max().item()
     off = ((out.double().cpu() - want)[2:].abs() - 2.0 ** -8 * want[2:].abs()).max().item()
     assert largest < 2.0 ** -13 and off <= bound
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [3, 40, 64, 65, 300])
+def test_long_ones_among_short_share_no_slot(n, dtype):
+    """32 tokens a sequence or fewer on average, so that short ones go token by token: the others lie
+    at every distance from the places where slots begin, some next to each other."""
+    rng = random.Random(n)
+    lengths = [rng.choice((0, 1, 2, 5, 16, 31, 32)) for _ in range(n)]
+    for at in range(0, n, 9):
+        lengths[at:at + 2] = [rng.choice((33, 34, 64, 65, 95, 96, 97, 129)), rng.choice((0, 33, 64))][:len(lengths[at:at + 2])]
+    while sum(lengths) > 32 * n:
+        lengths[lengths.index(max(lengths))] -= 7
+    assert any(m > 32 for m in lengths)
+    x, off = _inputs(lengths, 1, 2, 16, 24, dtype, seed=n)
+    _compare(x, off, 0.25, lengths)

@@ -55,3 +55,47 @@ def test_what_a_call_makes_is_memory_of_its_stream(calls, monkeypatch):
     made.clear(), launched.clear()
     _every_call(stream=side)
     assert len(made) == want and all(m == [side] for m in made) and launched == [[side]] * 6 and not inside
+
+
+def _delta_bytes(n, tokens, even, hk=8, hv=8, dk=64, dv=64, dtype=torch.float32):
+    import ctypes
+    L = ops.load_ops()
+    s = ops.rn_delta_shape(n, hk, hv, dk, dv, tokens, ops._CODES[dtype], 1.0, hk * dk, hk * dk, hv * dv, even)
+    return [f(ctypes.byref(s)) for f in (L.reuse_ops_delta_saved_bytes, L.reuse_ops_delta_scratch_bytes,
+                                         L.reuse_ops_delta_backward_scratch_bytes)]
+
+
+def test_scratch_is_what_the_call_uses():
+    """Even sequences of up to 32 tokens go token by token: nothing forward, a float32 row a token
+    backward.  Ragged ones of as few on average may hold no more chunks than tokens / 32."""
+    for n, length in ((16384, 16), (5, 32), (1000, 1)):
+        tokens = n * length
+        saved, fwd, bwd = _delta_bytes(n, tokens, 1)
+        rows, state = tokens * 8 * 64 * 4, 8 * 64 * 64 * 4
+        assert fwd == 256 and bwd <= rows + 512
+        assert saved <= rows + (n + tokens // 64) * state + 768
+    # the chunk operands of one slot: the planes of K, Q and K^T, the inverse, the scores, the decays
+    one = 3 * 8 * 4 * 2 * 3 * 1024 + 8 * (2 * 18 * 1024 + 768)
+    _, fwd, bwd = _delta_bytes(16384, 16384 * 16, 0)
+    assert fwd <= 8192 * one + 4096 and bwd <= 8192 * (one + 8 * 64 * 64 * 4 + 16) + 16384 * 16 * 8 * 64 * 4 + 4096
+    assert _delta_bytes(8, 20, 0)[1] == 256                      # no sequence above 32 among 20 tokens
+    _, long_even, _ = _delta_bytes(4, 4 * 640, 1)
+    assert _delta_bytes(4, 4 * 640, 0)[1] == long_even >= 40 * one
+
+
+def test_even_sequences_are_told_to_the_library(calls):
+    q, v, g = torch.zeros(96, 1, 8), torch.zeros(96, 2, 8), torch.zeros(96, 2)
+    off = torch.tensor([0, 90, 96], dtype=torch.int32)
+    out, _, saved = ops.delta_forward(q, q, v, g, g, n=4, save=True)
+    ops.delta_backward(out, q, q, v, g, g, n=4, saved=saved)
+    out, _, saved = ops.delta_forward(q, q, v, g, g, off, save=True)
+    ops.delta_backward(out, q, q, v, g, g, off, saved=saved)
+    assert [c[1]._obj.even for c in calls] == [1, 1, 0, 0]
+    with pytest.raises(ops.B.ReuseNetError, match="multiple"):
+        ops._check(ops.load_ops().reuse_ops_delta_forward(
+            ops.ctypes.byref(ops.rn_delta_shape(5, 1, 2, 8, 8, 96, 0, 1.0, 8, 8, 16, 1)), *[256] * 5, None, None, 256, 256,
+            None, 0, 256, 1 << 30, None))
+    with pytest.raises(ops.B.ReuseNetError, match="no seq_off"):
+        ops._check(ops.load_ops().reuse_ops_delta_forward(
+            ops.ctypes.byref(ops.rn_delta_shape(4, 1, 2, 8, 8, 96, 0, 1.0, 8, 8, 16, 1)), *[256] * 5, 256, None, 256, 256,
+            None, 0, 256, 1 << 30, None))
