@@ -30,7 +30,7 @@ template <class T, int VEC, int ROWS>
 __global__ __launch_bounds__(256) void k_delta_step(DeltaArgs a, int lanes) {
     __shared__ float sq[RN_DELTA_MAX_DIM], sk[RN_DELTA_MAX_DIM];
     __shared__ float red[256 * VEC];
-    const int head = blockIdx.x % a.hv, i = blockIdx.x / a.hv;
+    const int head = blockIdx.x, i = blockIdx.y;
     const int slot = a.ids ? a.ids[i] : i;
     const int hk = head / (a.hv / a.hk);
     const int col = threadIdx.x % lanes, grp = threadIdx.x / lanes, groups = 256 / lanes;
@@ -103,7 +103,7 @@ void step(const DeltaArgs &a, hipStream_t s) {
     int lanes = 1;
     while (lanes * VEC < a.dv) lanes *= 2;              // at most 32 (VEC 4) or 128 (VEC 1)
     const int rows = (a.dk * lanes + 255) / 256;
-    const int blocks = a.n * a.hv;
+    const dim3 blocks(a.hv, a.n);                       // one axis holds 2^32 threads, fewer than n hv blocks may have
     if (rows <= 4) k_delta_step<T, VEC, 4><<<blocks, 256, 0, s>>>(a, lanes);
     else if (rows <= 16) k_delta_step<T, VEC, 16><<<blocks, 256, 0, s>>>(a, lanes);
     else if constexpr (VEC == 1) k_delta_step<T, VEC, 64><<<blocks, 256, 0, s>>>(a, lanes);

@@ -90,6 +90,8 @@ __device__ inline WalkBlock walk_block(const DeltaArgs &a) {
     }
     return {seq, i % a.hv, i / a.hv};
 }
+// Sequences on an axis of their own: one axis holds no more than 2^32 threads, and
+// a larger grid is cut off without an error.
 inline dim3 walk_grid(const DeltaArgs &a, int width) { return dim3(a.hv * ((a.dv + width - 1) / width), a.n); }
 
 // Log decays (base 2) summed up to each token of a chunk, in double: differences

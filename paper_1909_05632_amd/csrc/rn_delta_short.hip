@@ -115,10 +115,10 @@ template <class T, int R, bool SAVE, bool VEC>
 __global__ __launch_bounds__(kWaves * 64) void k_delta_short(DeltaArgs a) {
     __shared__ __align__(16) Stage<R> st;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int seq = blockIdx.x / a.hv, h = blockIdx.x % a.hv, hk = h / (a.hv / a.hk);
+    const int seq = blockIdx.y, h = blockIdx.x % a.hv, hk = h / (a.hv / a.hk);
     const Span span = span_of(a, seq);
     if (span.len > a.short_len) return;
-    const int v0 = blockIdx.y * kWaves * 16, vc = wave * 16 + r, col = v0 + vc, row0 = g * R;
+    const int v0 = blockIdx.x / a.hv * kWaves * 16, vc = wave * 16 + r, col = v0 + vc, row0 = g * R;
     const int64_t mem = ((int64_t)seq * a.hv + h) * a.dk * a.dv;
     float S[R];
     load_memory<R>(a, a.state ? a.state + mem : nullptr, row0, col, S);
@@ -148,10 +148,10 @@ template <class T, int R, bool VEC>
 __global__ __launch_bounds__(kWaves * 64) void k_delta_short_bwd(DeltaArgs a) {
     __shared__ __align__(16) Stage<R> st;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int seq = blockIdx.x / a.hv, h = blockIdx.x % a.hv, hk = h / (a.hv / a.hk);
+    const int seq = blockIdx.y, h = blockIdx.x % a.hv, hk = h / (a.hv / a.hk);
     const Span span = span_of(a, seq);
     if (span.len > a.short_len) return;
-    const int v0 = blockIdx.y * kWaves * 16, vc = wave * 16 + r, col = v0 + vc, row0 = g * R;
+    const int v0 = blockIdx.x / a.hv * kWaves * 16, vc = wave * 16 + r, col = v0 + vc, row0 = g * R;
     const int64_t mem = ((int64_t)seq * a.hv + h) * a.dk * a.dv;
     float D[R];
     load_memory<R>(a, a.dfinal ? a.dfinal + mem : nullptr, row0, col, D);
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kWaves * 64, NT * TT == 1 ? 4 : 2) void k_delta_sho
     extern __shared__ __align__(16) float lds[];
     __shared__ double cs[64];
     __shared__ float beta[64], dc[kWaves][kShort], extra[kWaves];
-    const int seq = blockIdx.x / a.hk, hk = blockIdx.x % a.hk, group = a.hv / a.hk;
+    const int seq = blockIdx.y, hk = blockIdx.x, group = a.hv / a.hk;
     const Span span = span_of(a, seq);
     const int len = span.len;
     if (len == 0 || len > a.short_len) return;
@@ -445,7 +445,7 @@ __global__ __launch_bounds__(kWaves * 64, NT * TT == 1 ? 4 : 2) void k_delta_sho
 template <class T, class F>
 hipError_t by_rows(const DeltaArgs &a, const void *v, int64_t vs, F &&go) {
     if (a.n == 0) return hipSuccess;
-    const dim3 grid(a.n * a.hv, (a.dv + kWaves * 16 - 1) / (kWaves * 16));
+    const dim3 grid = walk_grid(a, kWaves * 16);
     const auto even = [](const void *p, int64_t stride) {
         return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0 && stride % 4 == 0;
     };
@@ -484,7 +484,7 @@ hipError_t backward(const DeltaArgs &a, hipStream_t s) {
         const size_t bytes = sizeof(float) * rows * (3 * (dvp + 4) + 2 * (NT * 64 + 4) + 2 * (rows + 4));
         auto *kernel = k_delta_short_grad<T, NT, TT, decltype(vec_)::value>;
         if (hipError_t e = allow_lds(kernel, bytes)) return e;
-        kernel<<<a.n * a.hk, kWaves * 64, bytes, s>>>(a);
+        kernel<<<dim3(a.hk, a.n), kWaves * 64, bytes, s>>>(a);
         return hipGetLastError();
     };
     const auto by_vec = [&](auto nt, auto tt) { return vec ? grad(nt, tt, std::true_type{}) : grad(nt, tt, std::false_type{}); };
