@@ -110,6 +110,13 @@ hipError_t launch_delta_short_backward(const DeltaArgs &a, bool bf16, hipStream_
 hipError_t launch_delta_forward(const DeltaArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_delta_backward(const DeltaArgs &a, bool bf16, hipStream_t s);
 
+// A grid of up to 2^31 blocks: one axis holds no more than 2^32 threads, and a
+// larger one is cut off without an error.  block_index() may run past the last.
+inline dim3 grid_of(int64_t blocks) {
+    constexpr int64_t kRow = 1 << 20;
+    return blocks <= kRow ? dim3((unsigned)blocks) : dim3((unsigned)kRow, (unsigned)((blocks + kRow - 1) / kRow));
+}
+
 // Allows a kernel the dynamic LDS of its launch (more than the default 64 KiB).
 template <class K>
 inline hipError_t allow_lds(K *kernel, size_t bytes) {
@@ -121,6 +128,8 @@ inline hipError_t allow_lds(K *kernel, size_t bytes) {
 // ------------------------------------------------------------------ device helpers
 
 namespace ops {
+
+__device__ inline uint32_t block_index() { return blockIdx.x + blockIdx.y * gridDim.x; }
 
 // bf16 as raw 16 bits, so that loads and conversions are explicit.
 struct bf16_t {

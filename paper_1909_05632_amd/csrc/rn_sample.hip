@@ -26,7 +26,7 @@ struct Row {
     int top_k;                    // 0: all
 };
 
-__device__ inline Row row_settings(const rn_sample_params &p, int r) {
+__device__ inline Row row_settings(const rn_sample_params &p, uint32_t r) {
     Row q;
     const float t = p.dev_temperature ? p.dev_temperature[r] : p.temperature;
     q.c = kLog2e / t;
@@ -112,8 +112,9 @@ __device__ inline uint64_t wave_scan(uint64_t v) {      // inclusive
 // that walk: 1024 rows of 18 in 4.9 us.
 template <class T>
 __global__ __launch_bounds__(256) void k_sample_wave(SampleArgs a) {
-    const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (r >= a.n) return;
+    const uint32_t r = block_index() * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (r >= (uint32_t)a.n) return;
     const Row q = row_settings(a.p, r);
     const bool live = lane < a.vocab;
     const float l = live ? to_float(static_cast<const T *>(a.logits)[r * a.stride + lane]) : -kInf;
@@ -268,7 +269,9 @@ __global__ __launch_bounds__(NT) void k_sample_block(SampleArgs a) {
     __shared__ uint32_t hc[kBins], ties[NW + 2], bound[2];
     __shared__ uint32_t pair_key[kPairs], pair_weight[kPairs];
     __shared__ int pair_at[kPairs], found, listed;
-    const int r = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t r = block_index();
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (r >= (uint32_t)a.n) return;
     const Row q = row_settings(a.p, r);
     const B b{static_cast<const T *>(a.logits) + r * a.stride, a.vocab, hw, hc, part, ties, found};
 
@@ -615,14 +618,14 @@ template <class T, int VEC>
 void launch_block(const SampleArgs &a, hipStream_t s) {
     // A row of up to 4096 leaves most of 1024 threads without work; a longer one
     // is worth all the waves a CU takes.
-    if (a.vocab <= 4096) k_sample_block<T, VEC, 256><<<a.n, 256, 0, s>>>(a);
-    else k_sample_block<T, VEC, 1024><<<a.n, 1024, 0, s>>>(a);
+    if (a.vocab <= 4096) k_sample_block<T, VEC, 256><<<grid_of(a.n), 256, 0, s>>>(a);
+    else k_sample_block<T, VEC, 1024><<<grid_of(a.n), 1024, 0, s>>>(a);
 }
 
 template <class T>
 hipError_t run(const SampleArgs &a, hipStream_t s) {
     constexpr int VEC = 16 / sizeof(T);
-    if (a.vocab <= 64) k_sample_wave<T><<<(a.n + 3) / 4, 256, 0, s>>>(a);
+    if (a.vocab <= 64) k_sample_wave<T><<<grid_of(((int64_t)a.n + 3) / 4), 256, 0, s>>>(a);
     else if (reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && a.stride % VEC == 0) launch_block<T, VEC>(a, s);
     else launch_block<T, 1>(a, s);
     return hipGetLastError();

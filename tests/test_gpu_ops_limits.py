@@ -42,3 +42,18 @@ def test_more_heads_of_streams_than_a_grid_axis_holds():
     want = (scale * DO * new, D * B * err - B * x * mid, B * x, after * mid, x * err, torch.exp(G) * after)
     for a, b, name in zip(grads, want, ("q", "k", "v", "g", "beta", "state")):
         assert R.rel(a.reshape(n, heads), b) <= tol, name
+
+
+@pytest.mark.parametrize("rows,vocab", [((1 << 26) + 100, 2), ((1 << 24) + 50, 65), ((1 << 22) + 50, 4097)])
+def test_more_rows_of_choices_than_a_grid_axis_holds(rows, vocab):
+    """One wave, 256 threads and 1024 threads a row: each row's draw is the one it has in a small batch."""
+    from paper_1909_05632_amd import ops
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.empty(rows, vocab, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    u = torch.rand(rows, generator=gen, device="cuda")
+    tokens, logprobs = torch.full((rows,), -5, dtype=torch.int32, device="cuda"), torch.full((rows,), 9.0, device="cuda")
+    ops.sample(x, u, 0.8, 30, 0.9, tokens=tokens, logprobs=logprobs)
+    for lo in (0, rows // 2 - 1000, rows - 5000, rows - 1):
+        t, p = ops.sample(x[lo:lo + 5000], u[lo:lo + 5000], 0.8, 30, 0.9)
+        assert bool((t == tokens[lo:lo + 5000]).all()) and bool((p == logprobs[lo:lo + 5000]).all()), lo
+    assert int(tokens.min()) >= 0 and int(tokens.max()) < vocab and float(logprobs.max()) <= 0
