@@ -304,19 +304,19 @@ __global__ __launch_bounds__(kThreads) void k_norm_cols(NormArgs a) {
 __global__ __launch_bounds__(1024) void k_norm_reduce(NormArgs a) {
     __shared__ float lds[64][17];
     const int col = threadIdx.x % 16, k = threadIdx.x / 16;
-    const int c = blockIdx.x * 16 + col;          // 0 .. 2 width - 1
+    const int64_t c = (int64_t)block_index() * 16 + col, columns = (int64_t)2 * a.width;
     float s = 0.f;
-    if (c < 2 * a.width)
-        for (int b = k; b < a.blocks; b += 64) s += a.part[(size_t)b * 2 * a.width + c];
+    if (c < columns)
+        for (int b = k; b < a.blocks; b += 64) s += a.part[b * columns + c];
     lds[k][col] = s;
     __syncthreads();
     for (int m = 32; m; m >>= 1) {
         if (k < m) lds[k][col] += lds[k + m][col];
         __syncthreads();
     }
-    if (k == 0 && c < 2 * a.width) {
+    if (k == 0 && c < columns) {
         float *out = c < a.width ? a.dweight : a.dbias;
-        const int i = c < a.width ? c : c - a.width;
+        const int64_t i = c < a.width ? c : c - a.width;
         if (out) out[i] = a.accumulate ? out[i] + lds[0][col] : lds[0][col];
     }
 }
@@ -391,7 +391,7 @@ hipError_t run_backward(const NormArgs &a, hipStream_t s) {
     }
     if (hipError_t e = hipGetLastError()) return e;
     if (a.part) {
-        k_norm_reduce<<<(2 * a.width + 15) / 16, 1024, 0, s>>>(a);
+        k_norm_reduce<<<grid_of(((int64_t)2 * a.width + 15) / 16), 1024, 0, s>>>(a);
         return hipGetLastError();
     }
     return hipSuccess;

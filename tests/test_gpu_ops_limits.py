@@ -57,3 +57,20 @@ def test_more_rows_of_choices_than_a_grid_axis_holds(rows, vocab):
         t, p = ops.sample(x[lo:lo + 5000], u[lo:lo + 5000], 0.8, 30, 0.9)
         assert bool((t == tokens[lo:lo + 5000]).all()) and bool((p == logprobs[lo:lo + 5000]).all()), lo
     assert int(tokens.min()) >= 0 and int(tokens.max()) < vocab and float(logprobs.max()) <= 0
+
+
+def test_weight_gradients_wider_than_a_grid_axis_holds():
+    """2^25 + 6 columns in 16s, 1024 threads each: with one row dweight is dy xh and dbias dy."""
+    from paper_1909_05632_amd import ops
+    width = (1 << 25) + 6
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x, dy = (torch.randn(1, width, generator=gen, device="cuda") for _ in range(2))
+    stats = torch.tensor([[0.25, 1.5]], device="cuda")
+    dw, db = torch.full((width,), 7.0, device="cuda"), torch.full((width,), 7.0, device="cuda")
+    dx, _, _ = ops.layer_norm_backward(dy, x, None, stats, dweight=dw, dbias=db)
+    assert bool((db == dy[0]).all())
+    xh = (x.double() - 0.25) * 1.5
+    assert R.rel(dw, (dy.double() * xh)[0]) <= 4e-6
+    # a thread adds 2^17 terms of random sign in a row: 2^8.5 roundings of their sum's size, which dx shares through two means
+    d = dy.double()
+    assert R.rel(dx, 1.5 * (d - d.mean() - xh * (d * xh).mean())) <= 2.0 ** -24 * 2 ** 8.5
