@@ -26,6 +26,7 @@ and over whole episodes ``delta_forward(..., save=True)`` with
 from __future__ import annotations
 
 import ctypes
+import operator
 from typing import Optional
 
 import torch
@@ -133,6 +134,13 @@ def _opt(x, what: str, dtype, device, shape) -> Optional[int]:
     return None if x is None else _like(x, what, dtype, device, shape)
 
 
+def _count(v: int, what: str) -> int:
+    """v as the C calls' 32-bit counts hold it: ctypes drops what is above them without a word."""
+    if v > 0x7fffffff:
+        raise ValueError(f"{what} must be below 2^31, got {v}")
+    return v
+
+
 def _rows(x, what: str):
     """(rows, row stride) of a tensor read as rows of its last axis."""
     width = x.shape[-1]
@@ -199,7 +207,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, with_stats: bool = 
     code = _data(x, "x")
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError("x must have a last axis of 1 or more")
-    dev, width = x.device, x.shape[-1]
+    dev, width = x.device, _count(x.shape[-1], "width")
     rows, stride = _rows(x, "x")
     w = None if weight is None else _like(weight, "weight", _F32, dev, (width,))
     b = None if bias is None else _like(bias, "bias", _F32, dev, (width,))
@@ -230,7 +238,7 @@ def layer_norm_backward(dy, x, weight, stats, dx=None, dweight=None, dbias=None,
         raise ValueError("dy must have x's dtype, shape and device")
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError("x must have a last axis of 1 or more")
-    dev, width = x.device, x.shape[-1]
+    dev, width = x.device, _count(x.shape[-1], "width")
     rows, xs = _rows(x, "x")
     _, dys = _rows(dy, "dy")
     w = _opt(weight, "weight", _F32, dev, (width,))
@@ -278,6 +286,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=Non
         raise ValueError(f"logits must have shape (n, vocab), got {tuple(logits.shape)}")
     n, vocab = logits.shape
     dev = logits.device
+    _count(n, "n")
     if not 1 <= vocab <= RN_SAMPLE_MAX_VOCAB:
         raise ValueError(f"vocab must be 1..{RN_SAMPLE_MAX_VOCAB}, got {vocab}")
     rows, stride = _rows(logits, "logits")
@@ -290,6 +299,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=Non
 
     t, tp = setting(temperature, "temperature", _F32)
     k, kp = setting(top_k, "top_k", _I32)
+    k = min(max(operator.index(k), 0), RN_SAMPLE_MAX_VOCAB)     # above the vocabulary and below 1: all
     p, pp = setting(top_p, "top_p", _F32)
     m, mp = setting(min_p, "min_p", _F32)
     params = rn_sample_params(t, k, p, m, tp, kp, pp, mp)
@@ -339,6 +349,7 @@ def _delta_shape(q, k, v, g, beta, n: int, scale, even: bool = True):
         raise ValueError("k must have q's shape")
     if hv % hk:
         raise ValueError(f"{hv} value heads cannot share {hk} key heads")
+    _count(max(hk, hv, dk, dv, n), "heads, dk, dv and n")
     shape = rn_delta_shape(n, hk, hv, dk, dv, tokens, code, dk ** -0.5 if scale is None else scale, qs, ks, vs, even)
     gp = _like(g, "g", _F32, dev, (tokens, hv))
     bp = _like(beta, "beta", _F32, dev, (tokens, hv))
@@ -375,7 +386,7 @@ def delta_step(q, k, v, g, beta, state, stream_ids=None, scale=None, out=None, s
     n = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() else 0
     shape, gp, bp, dev, hv, dk, dv = _delta_shape(q, k, v, g, beta, n, scale)
     slots = state.shape[0] if isinstance(state, torch.Tensor) and state.dim() else 0
-    sp = _like(state, "state", _F32, dev, (slots, hv, dk, dv))
+    sp = _like(state, "state", _F32, dev, (_count(slots, "slots"), hv, dk, dv))
     ids = _opt(stream_ids, "stream_ids", _I32, dev, (n,))
     if ids is None and slots < n:
         raise ValueError(f"{n} streams need as many slots, state has {slots}")

@@ -99,3 +99,35 @@ def test_even_sequences_are_told_to_the_library(calls):
         ops._check(ops.load_ops().reuse_ops_delta_forward(
             ops.ctypes.byref(ops.rn_delta_shape(4, 1, 2, 8, 8, 96, 0, 1.0, 8, 8, 16, 1)), *[256] * 5, 256, None, 256, 256,
             None, 0, 256, 1 << 30, None))
+
+
+def test_sizes_past_32_bits_are_refused(calls):
+    """The C calls take 32-bit counts, and ctypes drops the bits above them without a word."""
+    big = (1 << 32) + 8
+    meta = lambda *shape, **kw: torch.empty(*shape, device="meta", **kw)  # noqa: E731
+    with pytest.raises(ValueError, match="width"):
+        ops.layer_norm(meta(1, big))
+    with pytest.raises(ValueError, match="width"):
+        ops.layer_norm_backward(meta(1, big), meta(1, big), None, meta(1, 2))
+    with pytest.raises(ValueError, match="n must"):
+        ops.sample(meta(big, 2), meta(big))
+    q, g = meta(4, 1, 8), meta(4, 1)
+    with pytest.raises(ValueError, match="slots"):
+        ops.delta_step(q, q, q, g, g, meta(big, 1, 8, 8))
+    q, g = meta(big, 1, 8), meta(big, 1)
+    with pytest.raises(ValueError, match="n must"):
+        ops.delta_step(q, q, q, g, g, meta(big, 1, 8, 8))
+    with pytest.raises(ValueError, match="n must"):
+        ops.delta_forward(q, q, q, g, g, n=big)
+    assert not calls
+
+
+def test_top_k_of_any_size_keeps_its_meaning(calls):
+    """Above the vocabulary, and 0 or less: all."""
+    x, u = torch.zeros(2, 9), torch.zeros(2)
+    for k, want in ((5, 5), (0, 0), (-3, 0), ((1 << 32) + 5, None), (1 << 31, None), (-(1 << 32) + 5, 0), (1 << 40, None)):
+        ops.sample(x, u, top_k=k)
+        got = calls[-1][-3]._obj.top_k
+        assert max(got, 0) == want if want is not None else got >= 9, (k, got)
+    with pytest.raises(TypeError):
+        ops.sample(x, u, top_k=2.5)
