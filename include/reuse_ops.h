@@ -119,7 +119,15 @@ rn_status reuse_ops_sample(int32_t n, int32_t vocab, const void *dev_logits, int
  *   S <- exp(g) S;  S <- S + beta k (v - S^T k)^T;  out = scale S^T q.
  * Value head h uses key head h / (heads_v / heads_k).  Keys of unit length keep
  * the memory bounded for beta in [0, 2].  g = -infinity empties the memory (an
- * episode that begins).
+ * episode that begins), if what it holds is finite.
+ *
+ * Values that are not finite (in float32 also finite ones from 3.39e38 on, which
+ * round to infinity in bfloat16) reach what the rule makes of them, as NaN or
+ * infinity, and nothing else: a token's q its out; an element of its v, or of the
+ * first memory, that column of out and of the memory from there on; its k, g or
+ * beta all columns from there on.  The gradients of a sequence that has such a
+ * value, or gets one in dout or dfinal, may be NaN throughout; other sequences'
+ * are not touched.
  */
 
 #define RN_DELTA_MAX_DIM 128

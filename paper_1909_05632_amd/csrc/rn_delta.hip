@@ -128,6 +128,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
     constexpr int VT = 16 * CT, ldS = KP + 8, ldT = kC + 8;
     constexpr int kKeys = 4 * KS * NP * kFrag;
     __shared__ __align__(16) uint16_t sS[3 * VT * ldS], sR[3 * VT * ldT], sV[3 * VT * ldT], sL[3 * VT * ldT];
+    __shared__ int sBad[VT];                            // a column's first token in the chunk that is not finite
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const WalkBlock at = walk_block(a);
@@ -231,6 +232,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
     const uint32_t ooff = (wave * 16 + g * 4) * (uint32_t)(a.hv * a.dv) + r;
     if (chunks > 0)
         load_decays(slot0), load_rows(slot0), load_v(0), load_inv(slot0), load_kt(slot0), load_score(slot0);
+    if (threadIdx.x < VT) sBad[threadIdx.x] = kC;
     put_state();
 
     const auto step = [&](int chunk, auto more_) {
@@ -258,17 +260,35 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
                     held = mm<NP, 3>(kf[ks], s, held);
                     o[n] = mm<NP, 3>(qf[ks], s, o[n]);
                 }
+            // Where a gap (or k, g or beta: beta is NaN) is not finite, the column is
+            // NaN from that token on; its products are made with 0, so that the tokens
+            // before it keep theirs.  (The memory is then NaN, and so is every gap of the
+            // chunks that follow.)
             f32x4 w;
+            int bad = kC;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 3; j >= 0; --j) {
+                const int t = wave * 16 + (int)g * 4 + j;
                 const float gap = to_float(vv[n][j]) - grown[j] * held[j];
-                w[j] = more || wave * 16 + (int)g * 4 + j < len ? gap : 0.f;
+                const bool in = more || t < len, out = in && max(magnitude(gap), magnitude(beta[j])) >= kHuge;
+                bad = out ? t : bad;
+                w[j] = in && !out ? gap : 0.f;
                 o[n][j] *= grown[j] * a.scale;
             }
+            if (__any(bad < kC)) atomicMin(&sBad[n * 16 + r], bad);
             put4<3>(sR, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
         }
         if constexpr (more) load_decays(next), load_rows(next), load_v(chunk + 1);
         dev::lds_barrier();
+        int from[CT];                                   // the columns' first tokens of NaN
+        bool spoilt = false;
+#pragma unroll
+        for (int n = 0; n < CT; ++n) from[n] = sBad[n * 16 + r], spoilt = spoilt || from[n] < kC;
+        spoilt = __any(spoilt);
+        const auto spoil = [&](int n, f32x4 &v) {       // rows of this wave's tokens
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = wave * 16 + (int)g * 4 + j >= from[n] ? kNaN : v[j];
+        };
 #pragma unroll
         for (int n = 0; n < CT; ++n) {
             f32x4 w{};
@@ -281,14 +301,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
                         w = mm<3, 3>(mf[ks], b, w);
                     }
             if constexpr (SAVE) {
+                f32x4 e = w;
+                if (spoilt) spoil(n, e);
                 const __amdgpu_buffer_rsrc_t rs = rsrc_of(a.err + ((int64_t)(span.begin + chunk * kC) * a.hv + h) * a.dv + v0);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     store_if(col_in[n] && (more || wave * 16 + (int)g * 4 + j < len), rs,
-                             4 * (ooff + j * a.hv * a.dv + n * 16), (float)w[j]);
+                             4 * (ooff + j * a.hv * a.dv + n * 16), (float)e[j]);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] *= beta[j];
+            for (int j = 0; j < 4; ++j) w[j] *= beta[j] == beta[j] ? beta[j] : 0.f;
             put4<3>(sV, VT * ldT, (n * 16 + r) * ldT + wave * 16 + g * 4, w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] *= left[j];
@@ -309,6 +331,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
                     for (int j = 0; j < 4; ++j) S[i][n][j] *= whole;
                     S[i][n] = mm<NP, 3>(kt[i][0], b[0], S[i][n]);
                     if (half2) S[i][n] = mm<NP, 3>(kt[i][1], b[1], S[i][n]);
+                    if (spoilt && from[n] < kC) S[i][n] = f32x4{kNaN, kNaN, kNaN, kNaN};
                 }
             }
         if constexpr (more) {
@@ -326,6 +349,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delt
                         get8<3>(sV, VT * ldT, (n * 16 + r) * ldT + ks * 32 + g * 8, b);
                         o[n] = mm<3, 3>(pf[ks], b, o[n]);
                     }
+                if (spoilt) spoil(n, o[n]);
             }
             const __amdgpu_buffer_rsrc_t rs = rsrc_of(out);
 #pragma unroll

@@ -97,10 +97,12 @@ inline dim3 walk_grid(const DeltaArgs &a, int width) { return dim3(a.hv * ((a.dv
 // Log decays (base 2) summed up to each token of a chunk, in double: differences
 // of far tokens stay exact to float32 where the sums are large.  An empty memory
 // (g = -infinity) is a decay of e^-10^6 = 0, whose differences are finite.
-// Tokens past the end count as g = 0.  One wave calls it; lane = token.
-__device__ inline double decay_sums(const DeltaArgs &a, const Chunk &c, int head) {
+// Tokens past the end count as g = 0, and so do those of NaN or +infinity where `bad`
+// is there to be told of them.  One wave calls it; lane = token.
+__device__ inline double decay_sums(const DeltaArgs &a, const Chunk &c, int head, bool *bad = nullptr) {
     const int lane = threadIdx.x & 63;
     float g = lane < c.len ? a.g[(int64_t)(c.begin + lane) * a.hv + head] : 0.f;
+    if (bad && !(g < __builtin_huge_valf())) *bad = true, g = 0.f;
     double s = (g < -1e6f ? -1e6 : (double)g) * 1.4426950408889634;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -111,6 +113,14 @@ __device__ inline double decay_sums(const DeltaArgs &a, const Chunk &c, int head
 }
 // 2^d: the hardware's, exact to an ulp where the result is a normal float32.
 __device__ inline float decay(double d) { return __builtin_amdgcn_exp2f((float)d); }
+
+// What counts as infinite: the magnitudes that round to infinity as a bf16 plane, in
+// float32 those from 3.39e38 on.  A product with a plane of them is NaN, also where
+// the other factor is the 0 of a triangular operand, so that a token's would reach
+// the tokens before it.
+constexpr uint32_t kHuge = 0x7f7f8000;
+__device__ inline uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+constexpr float kNaN = __builtin_nanf("");
 
 template <class T>
 __device__ inline float load(const void *p, int64_t i) {
@@ -230,6 +240,10 @@ __device__ inline void wave_exchange() {
 // series of the nilpotent A would be shorter, and loses all its bits where keys
 // are nearly parallel, as those of neighbouring frames are.)
 //
+// Forward, a token whose k, g or beta is not finite goes into the operands as one
+// that writes nothing (k, g and beta 0), and is marked by a NaN in beta's place in
+// dec: the walk makes NaN of what it reaches.
+//
 // A chain of small steps with barriers between them: bound by their latency, so
 // the LDS is kept small (four blocks a CU in bfloat16) and the blocks many: 81 us
 // for 16384 tokens of 16 value heads (4 key heads) of 128 bfloat16, which write 180
@@ -243,6 +257,7 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     uint16_t *skf = reinterpret_cast<uint16_t *>(y), *sqf = skf + kKeys;
     __shared__ double cs[kC];
     __shared__ float beta[kC];
+    __shared__ uint32_t largest[kC];                    // magnitudes in k's rows
     const int slot = blockIdx.x, h = blockIdx.y, group = a.hv / a.hk, hk = h / group;
     const Chunk c = chunk_of(a, slot);
     const bool none = c.whole <= a.short_len;           // no chunk, or one of a sequence taken token by token
@@ -258,7 +273,8 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     // K and Q as rows: the wave's 16 tokens.
     const int token = wave * 16 + r;
     bf16x8 ka[KS][NP], qa[KS][NP];
-    const auto row = [&](const void *p, int64_t stride, int ks, bf16x8 (&f)[NP]) {
+    uint32_t most = 0;
+    const auto row = [&](const void *p, int64_t stride, int ks, bf16x8 (&f)[NP], bool key) {
         const int64_t at = (int64_t)(c.begin + token) * stride + hk * a.dk;
         const int d0 = ks * 32 + g * 8;
         float v[8];
@@ -275,6 +291,9 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = token < c.len && d0 + e < a.dk ? load<T>(p, at + d0 + e) : 0.f;
         }
+        if (!BWD && key)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max(most, magnitude(v[e]));
         uint32_t w[4][NP];
 #pragma unroll
         for (int e = 0; e < 4; ++e) split_pair<NP>(v[2 * e], v[2 * e + 1], w[e]);
@@ -283,17 +302,30 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     };
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-        row(a.k, a.ks, ks, ka[ks]);
-        row(a.q, a.qs, ks, qa[ks]);
+        row(a.k, a.ks, ks, ka[ks], true);
+        row(a.q, a.qs, ks, qa[ks], false);
     }
+    if constexpr (!BWD) {
+        most = max(most, __shfl_xor(most, 16));         // the row's four lanes
+        most = max(most, __shfl_xor(most, 32));
+        if (g == 0) largest[token] = most;
+        if (most >= kHuge)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int i = 0; i < NP; ++i) ka[ks][i] = bf16x8{};
+    }
+    float marked = 0.f;                                 // wave 0, by tokens: beta, or NaN
     if (wave == 0) {
-        const double s = decay_sums(a, c, h), last = __shfl(s, 63);
+        bool bad = false;
+        const double s = decay_sums(a, c, h, BWD ? nullptr : &bad), last = __shfl(s, 63);
         const float b = lane < c.len ? a.beta[(int64_t)(c.begin + lane) * a.hv + h] : 0.f;
+        bad = bad || (!BWD && magnitude(b) >= kHuge);
         cs[lane] = s;
-        beta[lane] = b;
+        beta[lane] = bad ? 0.f : b;
         a.dec[ch * 3 * kC + lane] = decay(s);
         a.dec[ch * 3 * kC + kC + lane] = decay(last - s);
-        a.dec[ch * 3 * kC + 2 * kC + lane] = b;
+        marked = bad ? kNaN : b;
     }
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
@@ -308,6 +340,7 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
             }
         }
     __syncthreads();
+    if (wave == 0) a.dec[ch * 3 * kC + 2 * kC + lane] = !BWD && largest[lane] >= kHuge ? kNaN : marked;
     // K K^T and Q K^T, the wave's rows of them.
     f32x4 u[4] = {}, w[4] = {};
 #pragma unroll

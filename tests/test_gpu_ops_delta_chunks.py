@@ -89,3 +89,68 @@ def test_long_ones_among_short_share_no_slot(n, dtype):
     assert any(m > 32 for m in lengths)
     x, off = _inputs(lengths, 1, 2, 16, 24, dtype, seed=n)
     _compare(x, off, 0.25, lengths)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lengths,even", [([150], False), ([40, 70], False), ([64, 64], True), ([20], False),
+                                          ([16] * 4, True), ([5, 32, 70, 1, 0, 9], False)])
+def test_values_that_are_not_finite_reach_later_tokens_only(lengths, even, dtype):
+    """NaN or infinity in a token leaves the bits of the tokens before it alone, of the other
+    columns (v), of the other tokens (q), of the other heads (g, beta) and of the other sequences."""
+    from paper_1909_05632_amd import ops
+    hk, hv, dk, dv = 2, 4, 64, 70
+    x, off = _inputs(lengths, hk, hv, dk, dv, dtype, seed=sum(lengths))
+    d = {k: v.cuda() for k, v in x.items()}
+    how = dict(n=len(lengths)) if even else dict(seq_off=torch.tensor(off, dtype=torch.int32).cuda())
+
+    def run(y, save):
+        got = ops.delta_forward(*(y[k] for k in NAMES), state=y["state"], scale=0.125, save=save, **how)
+        return got[0], got[1]
+
+    want, last = run(d, False)
+    longest = max(range(len(lengths)), key=lambda i: lengths[i])
+    begin, end = off[longest], off[longest + 1]
+    for step in (0, 1, 15, 17, 40, 63, 64, 100):
+        t = begin + step
+        if t >= end:
+            continue
+        for name in NAMES:
+            for value in (math.nan, math.inf, -math.inf):
+                if name == "g" and value == -math.inf:
+                    continue                         # that empties the memory
+                y = {k: v.clone() for k, v in d.items()}
+                head = 1 if name in ("q", "k") else 2
+                if name in ("g", "beta"):
+                    y[name][t, head] = value
+                else:
+                    y[name][t, head, 7] = value
+                for save in (False, True):
+                    out, final = run(y, save)
+                    reached, memory = torch.zeros_like(out, dtype=torch.bool), torch.zeros_like(final, dtype=torch.bool)
+                    heads = slice(2, 4) if name in ("q", "k") else slice(2, 3)
+                    cols = slice(7, 8) if name == "v" else slice(0, dv)
+                    reached[t:t + 1 if name == "q" else end, heads, cols] = True
+                    if name != "q":
+                        memory[longest, heads, :, cols] = True
+                    case = (step, name, value, save)
+                    assert torch.equal(out[~reached], want[~reached]), case
+                    assert torch.equal(final[~memory], last[~memory]), case
+                    assert not out[reached].isfinite().any() and not final[memory].isfinite().any(), case
+
+
+@pytest.mark.parametrize("length", [20, 150])
+def test_a_memory_that_is_not_finite_stays_in_its_column(length):
+    from paper_1909_05632_amd import ops
+    for dtype in (F32, BF16):
+        x, off = _inputs([length, length], 1, 2, 40, 33, dtype)
+        d = {k: v.cuda() for k, v in x.items()}
+        want, last = ops.delta_forward(*(d[k] for k in NAMES), n=2, state=d["state"], scale=0.125)
+        for value in (math.nan, math.inf):
+            bad = d["state"].clone()
+            bad[1, 0, 3, 20] = value
+            out, final = ops.delta_forward(*(d[k] for k in NAMES), n=2, state=bad, scale=0.125)
+            reached, memory = torch.zeros_like(out, dtype=torch.bool), torch.zeros_like(final, dtype=torch.bool)
+            reached[length:, 0, 20] = True
+            memory[1, 0, :, 20] = True
+            assert torch.equal(out[~reached], want[~reached]) and torch.equal(final[~memory], last[~memory])
+            assert not out[reached].isfinite().any() and not final[memory].isfinite().any()
