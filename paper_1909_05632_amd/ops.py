@@ -13,6 +13,10 @@ there, the caller orders the streams that write the arguments and read the
 results, and records (``Tensor.record_stream``) a tensor that another stream
 still uses when it is dropped.
 
+Nothing is recorded for autograd: where it is on, tensors that require grad are
+refused.  Call under ``torch.no_grad()``, or in a ``torch.autograd.Function``
+whose backward makes the ``_backward`` call (examples/recurrent_policy.py).
+
 A policy that remembers, one frame of n streams at a time:
 
     x = layer_norm(features, w, b)
@@ -165,6 +169,15 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+def _no_grad(*tensors) -> None:
+    """Refuses what autograd would have to follow through a call that it does not see."""
+    if torch.is_grad_enabled():
+        for x in tensors:
+            if getattr(x, "requires_grad", False):
+                raise ValueError("a tensor requires grad, which is not recorded here: call under torch.no_grad(), "
+                                 "or in a torch.autograd.Function with the backward call")
+
+
 def _on(stream, x):
     """`stream` as the current one, for the memory a call makes as well as for its launches."""
     if isinstance(x, torch.Tensor) and x.is_cuda and x.device != stream.device:
@@ -204,6 +217,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, with_stats: bool = 
     if stream is not None:
         with _on(stream, x):
             return layer_norm(x, weight, bias, eps, with_stats, out)
+    _no_grad(x, weight, bias)
     code = _data(x, "x")
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError("x must have a last axis of 1 or more")
@@ -233,6 +247,7 @@ def layer_norm_backward(dy, x, weight, stats, dx=None, dweight=None, dbias=None,
     if stream is not None:
         with _on(stream, x):
             return layer_norm_backward(dy, x, weight, stats, dx, dweight, dbias, accumulate, want_params)
+    _no_grad(dy, x, weight, stats)
     code = _data(x, "x")
     if not isinstance(dy, torch.Tensor) or dy.dtype is not x.dtype or dy.shape != x.shape or dy.device != x.device:
         raise ValueError("dy must have x's dtype, shape and device")
@@ -281,6 +296,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=Non
     if stream is not None:
         with _on(stream, logits):
             return sample(logits, u, temperature, top_k, top_p, min_p, tokens, logprobs)
+    _no_grad(logits)
     code = _data(logits, "logits")
     if logits.dim() != 2:
         raise ValueError(f"logits must have shape (n, vocab), got {tuple(logits.shape)}")
@@ -383,6 +399,7 @@ def delta_step(q, k, v, g, beta, state, stream_ids=None, scale=None, out=None, s
     if stream is not None:
         with _on(stream, q):
             return delta_step(q, k, v, g, beta, state, stream_ids, scale, out)
+    _no_grad(q, k, v, g, beta, state)
     n = q.shape[0] if isinstance(q, torch.Tensor) and q.dim() else 0
     shape, gp, bp, dev, hv, dk, dv = _delta_shape(q, k, v, g, beta, n, scale)
     slots = state.shape[0] if isinstance(state, torch.Tensor) and state.dim() else 0
@@ -418,6 +435,7 @@ def delta_forward(q, k, v, g, beta, seq_off=None, n=None, state=None, final=None
     if stream is not None:
         with _on(stream, q):
             return delta_forward(q, k, v, g, beta, seq_off, n, state, final, scale, save, out)
+    _no_grad(q, k, v, g, beta, state)
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor of shape (tokens, heads, dk)")
     n, off = _sequences(seq_off, n, q.shape[0], q.device)
@@ -453,6 +471,7 @@ def delta_backward(dout, q, k, v, g, beta, seq_off=None, n=None, saved=None, dfi
     if stream is not None:
         with _on(stream, q):
             return delta_backward(dout, q, k, v, g, beta, seq_off, n, saved, dfinal, scale, want_dstate)
+    _no_grad(dout, q, k, v, g, beta, dfinal)
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor of shape (tokens, heads, dk)")
     n, off = _sequences(seq_off, n, q.shape[0], q.device)

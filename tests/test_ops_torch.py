@@ -131,3 +131,31 @@ def test_top_k_of_any_size_keeps_its_meaning(calls):
         assert max(got, 0) == want if want is not None else got >= 9, (k, got)
     with pytest.raises(TypeError):
         ops.sample(x, u, top_k=2.5)
+
+
+def test_tensors_that_require_grad_are_refused_in_grad_mode(calls):
+    """The calls record nothing: a result would be cut off from its inputs without a word."""
+    x, w, u = torch.zeros(3, 8), torch.ones(8), torch.zeros(3)
+    q, v, g, s = torch.zeros(4, 1, 8), torch.zeros(4, 2, 8), torch.zeros(4, 2), torch.zeros(4, 2, 8, 8)
+    off, stats = torch.tensor([0, 4], dtype=torch.int32), torch.zeros(3, 2)
+    s1 = s[:1].clone()
+    saved = ops.delta_forward(q, q, v, g, g, off, save=True)[2]
+    temperature = torch.ones(3)
+    every = [(ops.layer_norm, (x, w, w), {}, 3), (ops.layer_norm_backward, (x, x, w, stats), {}, 4),
+             (ops.sample, (x, u, temperature), {}, 1), (ops.delta_step, (q, q, v, g, g, s), {}, 6),
+             (ops.delta_forward, (q, q, v, g, g, off, None, s1), {}, 5),
+             (ops.delta_backward, (v, q, q, v, g, g, off, None, saved, s1), {}, 6)]
+    calls.clear()
+    for call, args, kw, floats in every:
+        for i in [*range(floats)] + ([7] if call is ops.delta_forward else []) + ([9] if call is ops.delta_backward else []):
+            some = list(args)
+            some[i] = args[i].clone().requires_grad_()
+            with pytest.raises(ValueError, match="requires grad"):
+                call(*some, **kw)
+            assert not calls
+            with torch.no_grad():
+                call(*some, **kw)
+            some[i] = some[i].detach()
+            call(*some, **kw)
+            assert len(calls) == 2
+            calls.clear()
