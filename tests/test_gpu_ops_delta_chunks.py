@@ -154,3 +154,101 @@ def test_a_memory_that_is_not_finite_stays_in_its_column(length):
             memory[1, 0, :, 20] = True
             assert torch.equal(out[~reached], want[~reached]) and torch.equal(final[~memory], last[~memory])
             assert not out[reached].isfinite().any() and not final[memory].isfinite().any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dk", [64, 100])
+@pytest.mark.parametrize("lengths,even", [([70] * 9, True), ([40, 97, 0, 64, 33] + [50] * 12, False)])
+def test_batches_that_take_two_column_tiles_a_block(lengths, even, dk, dtype):
+    """More than 256 (ragged: 512) sequences x heads x 32s of columns: a walk's block then has two
+    tiles of 16 columns, the second one here in part past dv, for every size of keys."""
+    from paper_1909_05632_amd import ops
+    x, off = _inputs(lengths, 2, 16, dk, 33, dtype, seed=dk)
+    d = {k: v.cuda() for k, v in x.items()}
+    args = [d[k] for k in NAMES]
+    how = dict(n=len(lengths)) if even else dict(seq_off=torch.tensor(off, dtype=torch.int32).cuda())
+    want, last, g = _reference(x, off, 0.125)
+    tol = TOL[F32] if dtype is F32 else 2.0 ** -9 + TOL[F32]
+    out, final = ops.delta_forward(*args, state=d["state"], scale=0.125, **how)
+    assert R.rel(out, want) <= tol and R.rel(final, last) <= TOL[F32]
+    out2, final2, saved = ops.delta_forward(*args, state=d["state"], scale=0.125, save=True, **how)
+    assert torch.equal(out2, out) and torch.equal(final2, final)
+    grads = ops.delta_backward(d["dout"], *args, saved=saved, dfinal=d["dfinal"], scale=0.125, **how)
+    for got, name, bound in zip(grads, NAMES + ("state",), (tol,) * 3 + (TOL_G, TOL_G, TOL[F32])):
+        assert R.rel(got, g[name]) <= bound, name
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_training_batch_of_episodes(dtype):
+    """256 streams of 64 frames, 4 heads of 64 x 64: some of the episodes against the recurrence."""
+    from paper_1909_05632_amd import ops
+    x, off = _inputs([64] * 256, 4, 4, 64, 64, dtype, seed=7)
+    d = {k: v.cuda() for k, v in x.items()}
+    args = [d[k] for k in NAMES]
+    out, final, saved = ops.delta_forward(*args, n=256, state=d["state"], scale=0.125, save=True)
+    grads = ops.delta_backward(d["dout"], *args, n=256, saved=saved, dfinal=d["dfinal"], scale=0.125)
+    tol = TOL[F32] if dtype is F32 else 2.0 ** -9 + TOL[F32]
+    for i in (0, 1, 63, 64, 130, 255):
+        a, b = off[i], off[i + 1]
+        part = {k: v[i:i + 1] if k in ("state", "dfinal") else v[a:b] for k, v in x.items()}
+        want, last, g = _reference(part, [0, b - a], 0.125)
+        assert R.rel(out[a:b], want) <= tol and R.rel(final[i:i + 1], last) <= TOL[F32], i
+        for got, name, bound in zip(grads, NAMES, (tol,) * 3 + (TOL_G, TOL_G)):
+            assert R.rel(got[a:b], g[name]) <= bound, (i, name)
+        assert R.rel(grads[5][i:i + 1], g["state"]) <= TOL[F32], i
+
+
+@pytest.mark.parametrize("lengths,even", [([20], False), ([16] * 4, True), ([16] * 4, False), ([5, 32, 70, 1, 0, 9], False)])
+def test_memory_emptied_in_short_sequences(lengths, even):
+    """g = -infinity at a token of sequences that go token by token: what follows is a sequence of its own."""
+    from paper_1909_05632_amd import ops
+    x, off = _inputs(lengths, 1, 2, 64, 48, F32, seed=3)
+    cut = {i: m // 2 for i, m in enumerate(lengths) if m > 1}
+    x["g"][[off[i] + c for i, c in cut.items()]] = -math.inf
+    d = {k: v.cuda() for k, v in x.items()}
+    args = [d[k] for k in NAMES]
+    how = dict(n=len(lengths)) if even else dict(seq_off=torch.tensor(off, dtype=torch.int32).cuda())
+    out, final, saved = ops.delta_forward(*args, state=d["state"], scale=0.2, save=True, **how)
+    grads = ops.delta_backward(d["dout"], *args, saved=saved, dfinal=d["dfinal"], scale=0.2, **how)
+    parts, firsts = [0], []                          # each sequence as the two it falls into
+    split = {k: v.clone() for k, v in x.items()}
+    state, dfinal = [], []
+    for i, m in enumerate(lengths):
+        c = cut.get(i, 0)
+        if c:
+            parts.append(off[i] + c)
+            firsts.append(off[i] + c)
+            state += [x["state"][i], torch.zeros_like(x["state"][i])]
+            dfinal += [torch.zeros_like(x["dfinal"][i]), x["dfinal"][i]]
+        else:
+            state.append(x["state"][i]), dfinal.append(x["dfinal"][i])
+        parts.append(off[i] + m)
+    split["g"][firsts] = 0.0
+    split["state"], split["dfinal"] = torch.stack(state), torch.stack(dfinal)
+    want, last, g = _reference(split, parts, 0.2)
+    ends = [parts.index(off[i + 1], 1) - 1 if lengths[i] else None for i in range(len(lengths))]
+    assert R.rel(out, want) <= TOL[F32]
+    for i, e in enumerate(ends):
+        assert R.rel(final[i], last[e] if e is not None else x["state"][i]) <= TOL[F32], i
+    for got, name, tol in zip(grads, NAMES, (TOL[F32],) * 3 + (TOL_G, TOL_G)):
+        a, b = got.double().cpu(), g[name].clone()
+        if name == "g":
+            assert a[firsts].abs().max() <= TOL_G * b.norm() and torch.isfinite(a).all()
+            a[firsts] = b[firsts] = 0.0
+        assert R.rel(a, b) <= tol, name
+
+
+@pytest.mark.parametrize("lengths", [[20, 16, 9], [5, 32, 70, 1, 0, 9], [16] * 4])
+def test_a_sequence_of_nan_stays_alone_token_by_token(lengths):
+    x, off = _inputs(lengths, 1, 2, 64, 64, F32)
+    out, final, grads = _run(x, off, 0.125)
+    at = 1
+    bad = {k: v.clone() for k, v in x.items()}
+    for k in ("q", "k", "v", "g", "beta", "dout"):
+        bad[k][off[at]:off[at + 1]] = math.nan
+    out2, final2, grads2 = _run(bad, off, 0.125)
+    keep = [t for t in range(off[-1]) if not off[at] <= t < off[at + 1]]
+    rest = [i for i in range(len(lengths)) if i != at]
+    assert torch.equal(out2[keep], out[keep]) and torch.equal(final2[rest], final[rest])
+    assert all(torch.equal(a[keep], b[keep]) for a, b in zip(grads2[:5], grads[:5]))
+    assert torch.equal(grads2[5][rest], grads[5][rest]) and out2[off[at]:off[at + 1]].isnan().all()
