@@ -462,16 +462,20 @@ __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     pieces(x, a.mf, wave, 4);
 }
 
-// Column tiles of a walk's block.  Two share the left operands' loads; one has the
-// shorter chain, and is taken while two of its blocks a CU hold all there are
-// (16384 tokens of 16 heads of 128 x 128: 4 even sequences, 512 blocks of one
-// tile, 264 us either way; 5, 640 blocks, 287 us with one, 267 with two; 8, 1024
-// blocks, 248 and 210).  Ragged sequences end at different times and leave room
-// for more of them (5: 320 us with one, 415 with two; 8: 281 and 344; 12: 266 and
-// 270).
+// Column tiles of a walk's block.  Two share the left operands' loads and one
+// chain of barriers; one has the shorter chain, and more blocks, which is what counts
+// until two-tile blocks (pairs) reach every CU.  Ragged sequences end at different
+// times and leave room for more blocks.  Whole forward calls, us, one tile / two:
+//   16384 bfloat16 tokens, 16 heads of 128 x 128: even, 128 pairs 386 / 501, 256
+//     307 / 294, 512 295 / 246; ragged, 320 358 / 451, 512 317 / 360, 640 317 / 325,
+//     768 312 / 299, 1024 310 / 294;
+//   8192 float32 tokens, 8 heads of 128 x 128: even, 128 151 / 197, 256 156 / 135;
+//     ragged, 384 172 / 182, 512 173 / 181, 768 186 / 156;
+//   16384 float32 tokens, 4 heads of 64 x 64: even, 128 85 / 98, 256 85 / 87, 1024
+//     91 / 86; ragged, 512 102 / 121, 768 104 / 112, 1024 105 / 108, 2048 139 / 130.
 inline int walk_tiles(const DeltaArgs &a) {
     const int64_t pairs = (int64_t)a.n * a.hv * ((a.dv + 31) / 32);
-    return a.dv <= 16 || pairs <= (a.off ? 512 : 256) ? 1 : 2;
+    return a.dv <= 16 || pairs <= (a.off ? 512 : 255) ? 1 : 2;
 }
 
 template <class T, int KS, bool BWD>

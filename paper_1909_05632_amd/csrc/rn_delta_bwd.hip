@@ -286,6 +286,9 @@ __device__ inline void planes8(const float (&v)[8], bf16x8 (&f)[N]) {
 // first one's waits: 274 us for 8192 ragged tokens of 8 heads, 182 with eight;
 // 155 with loads that do not branch).
 // Up to 64 four waves do: for a chunk of 16 tokens one of four works.
+// SHARED keeps dq's and dk's sums over the heads in registers too, and from dk 33 on
+// does not fit into the 256 there are: 2 and 3 of them spill for bfloat16 above 64, 31
+// for float32, 22 to 71 for four waves of 33 to 64.
 template <class T, int KS, bool VEC, bool SHARED>
 __global__ __launch_bounds__(KS == 4 ? 512 : 256, 2) void k_delta_bwd_chunk(DeltaArgs a) {
     constexpr int NP = sizeof(T) == 2 ? 1 : 3, KT = 2 * KS, PARTS = KS == 4 ? 2 : 1, HT = KT / PARTS;
