@@ -117,10 +117,14 @@ void step(const DeltaArgs &a, hipStream_t s) {
 // bf16 planes to the waves that multiply by it, as do V - e^c K S and V'.
 // The left operands are read from memory in fragment order, straight into
 // registers, each for the next chunk as soon as this one's use of it is over.
-// Bound by a chunk's chain of four products with barriers between them, 2.6 us a
-// chunk (bfloat16, 128 x 128, two blocks a CU), of which matrix operations are a
-// sixth: 16384 tokens of 5 sequences and 16 heads in 230 us, 112 TFLOP/s of the
-// rule's own operations (25.8 GFLOP).
+// S, V' and P have three planes in all products: outputs of bfloat16 data too are
+// sums of float32 before they are rounded (with two planes in the output's products
+// those differ from float32's by 1.4e-4 after rounding in place of 4e-5, and
+// the walk below takes 230 us).
+// Bound by a chunk's chain of four products with barriers between them, 2.9 us a
+// chunk (bfloat16, 128 x 128, two blocks a CU), in which the matrix cores are busy a
+// fifth of the time: 16384 tokens of 5 sequences and 16 heads in 256 us, 101
+// TFLOP/s of the rule's own operations (25.8 GFLOP).
 template <class T, int KS, int CT, bool SAVE>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && KS == 4 ? 1 : 2) void k_delta_walk(DeltaArgs a) {
     constexpr int NP = sizeof(T) == 2 ? 1 : 3;

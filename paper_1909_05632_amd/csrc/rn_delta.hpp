@@ -244,10 +244,10 @@ __device__ inline void wave_exchange() {
 // that writes nothing (k, g and beta 0), and is marked by a NaN in beta's place in
 // dec: the walk makes NaN of what it reaches.
 //
-// A chain of small steps with barriers between them: bound by their latency, so
-// the LDS is kept small (four blocks a CU in bfloat16) and the blocks many: 81 us
-// for 16384 tokens of 16 value heads (4 key heads) of 128 bfloat16, which write 180
-// MB, 2.2 TB/s.
+// A chain of small steps with barriers between them, so the LDS is kept small (four
+// blocks a CU in bfloat16) and the blocks many; with enough of them bound by memory:
+// 83 us for 16384 tokens of 16 value heads (4 key heads) of 128 bfloat16, which write
+// 205 MB and read K and Q once a value head, 169 MB, 4.5 TB/s.
 template <class T, int KS, bool VEC, bool BWD>
 __global__ __launch_bounds__(256) void k_delta_operands(DeltaArgs a) {
     constexpr int NP = sizeof(T) == 2 ? 1 : 3;
