@@ -1,7 +1,8 @@
 /*
  * reuse_ops — operators around a policy net on MI355X (gfx950): layer norm, the
- * gated delta rule (a memory per stream that is carried from frame to frame)
- * and the sampling of actions, in the library of reuse_net.h.
+ * gated delta rule (a memory per stream that is carried from frame to frame), the
+ * sampling of actions, and the norm of a residual stream, in the library of
+ * reuse_net.h.
  *
  * A policy over many streams of frames (Sec. 1: multiple input frames; Sec. 2:
  * actions and REINFORCE) normalises each frame's features, carries a memory
@@ -205,6 +206,54 @@ rn_status reuse_ops_delta_backward(const rn_delta_shape *shape, const void *dev_
                                    const void *dev_dout, const float *dev_dfinal, void *dev_dq, void *dev_dk,
                                    void *dev_dv, float *dev_dg, float *dev_dbeta, float *dev_dstate, void *dev_scratch,
                                    size_t scratch_bytes, void *hip_stream);
+
+/* ---- residual norm ----
+ *
+ *   total_j = x_j + residual_j (float32, rounded to dtype; x_j itself without a residual),
+ *   rstd = 1 / sqrt(sum_j total_j^2 / width + eps),  y_j = total_j rstd weight_j,
+ * the norm being that of the rounded total, which is what the backward call and the
+ * next layer see.  In 8 bits (e4m3, largest value 448), with t_j = total_j weight_j
+ * rounded to float32 and m = max_j |t_j|:
+ *   q_j = t_j (448 / m) rounded to nearest even (0 where m is 0),  scale = m rstd / 448,
+ * so that y_j = q_j scale to half a step of e4m3, and q depends on no order of sums.
+ * A row that holds NaN or infinity (or so large values that its sum of squares is
+ * infinite) has the y of these formulas, a scale of NaN and any q.
+ */
+
+/* `rows` rows of `width` elements (rows >= 0, width >= 1); results are contiguous.
+ *   dev_residual: NULL, or rows at residual_stride.
+ *   dev_weight:   [width] float32, or NULL for 1.
+ *   dev_y:        [rows][width] dtype, or NULL (not wanted).
+ *   dev_q, dev_scales: [rows][width] e4m3 and [rows] float32, both or neither.
+ *   dev_total:    [rows][width] dtype, or NULL; NULL without a residual.
+ *   dev_rstd:     [rows] float32 for the backward call, or NULL.
+ * y or total may be x or the residual itself where that is contiguous. */
+rn_status reuse_ops_rms_norm(int64_t rows, int32_t width, const void *dev_x, int64_t x_stride, rn_dtype dtype,
+                             const void *dev_residual, int64_t residual_stride, const float *dev_weight, float eps,
+                             void *dev_y, void *dev_q, float *dev_scales, void *dev_total, float *dev_rstd,
+                             void *hip_stream);
+
+/* Device scratch bytes the backward call needs for these sizes when it writes
+ * weight gradients (0 if a size is out of range). */
+size_t reuse_ops_rms_norm_backward_scratch_bytes(int64_t rows, int32_t width);
+
+/* Gradients of J given dy = dJ/dy and dtotal = dJ/dtotal (NULL: 0), the latter by
+ * what else the total goes into: with t_j = dy_j weight_j and n_j = total_j rstd,
+ *   dx_j = dtotal_j + rstd (t_j - n_j mean(t n)),  dweight_j = sum over rows dy_j n_j;
+ * the residual's gradient is dx too.
+ *   dev_total:   x of a forward call without a residual, its total otherwise.
+ *   dev_rstd:    [rows] from the forward call.
+ *   dev_dx:      [rows][width] dtype, contiguous; may be dy, total or dtotal itself
+ *                where that is contiguous.
+ *   dev_dweight: [width] float32 or NULL (not wanted); accumulate = 0 overwrites it,
+ *                accumulate != 0 adds to it.  No rows: zeros.
+ *   dev_scratch: 256-byte aligned, at least the bytes above (NULL if dweight is not
+ *                wanted). */
+rn_status reuse_ops_rms_norm_backward(int64_t rows, int32_t width, const void *dev_dy, int64_t dy_stride,
+                                      const void *dev_total, int64_t total_stride, rn_dtype dtype,
+                                      const float *dev_weight, const float *dev_rstd, const void *dev_dtotal,
+                                      int64_t dtotal_stride, void *dev_dx, float *dev_dweight, int32_t accumulate,
+                                      void *dev_scratch, size_t scratch_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

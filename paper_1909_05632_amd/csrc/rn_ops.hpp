@@ -1,6 +1,6 @@
 // Internal declarations of the operators in include/reuse_ops.h: kernel
-// launchers (rn_norm.hip, rn_sample.hip, rn_delta.hip, rn_delta_short.hip,
-// rn_delta_bwd.hip) and device helpers they share.
+// launchers (rn_norm.hip, rn_rms.hip, rn_sample.hip, rn_delta.hip,
+// rn_delta_short.hip, rn_delta_bwd.hip) and device helpers they share.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -29,6 +29,26 @@ struct NormArgs {
 int norm_blocks(int64_t rows, int width);
 hipError_t launch_norm(const NormArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_norm_backward(const NormArgs &a, bool bf16, hipStream_t s);
+
+struct RmsArgs {
+    int64_t rows;
+    int width;
+    const void *x, *residual;     // x: the total in the backward call
+    const void *dy, *dtotal;      // backward only
+    int64_t xs, rs, dys, dts;     // row strides in elements; results are contiguous
+    const float *weight;
+    float eps;
+    void *y, *total;              // y: dx in the backward call; either may be NULL in the forward call
+    uint8_t *q;
+    float *scales;
+    float *rstd;                  // [rows]; read by the backward call
+    float *part;                  // [blocks][width] partial weight gradients, or NULL
+    int blocks;                   // row strips of the backward call (norm_blocks)
+    float *dweight;
+    int accumulate;
+};
+hipError_t launch_rms(const RmsArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_rms_backward(const RmsArgs &a, bool bf16, hipStream_t s);
 
 struct SampleArgs {
     int n, vocab;

@@ -162,6 +162,70 @@ rn_status reuse_ops_layer_norm_backward(int64_t rows, int32_t width, const void 
     return launched(launch_norm_backward(a, dtype == RN_BF16, static_cast<hipStream_t>(stream)));
 }
 
+rn_status reuse_ops_rms_norm(int64_t rows, int32_t width, const void *x, int64_t x_stride, rn_dtype dtype,
+                             const void *residual, int64_t residual_stride, const float *weight, float eps, void *y,
+                             void *q, float *scales, void *total, float *rstd, void *stream) {
+    if (rows < 0 || rows > kMaxRows || width < 1 || width > kMaxWidth)
+        return fail(RN_EINVAL, "rows must be 0..2^40 and width 1..2^30");
+    if (!known(dtype)) return fail(RN_EINVAL, "dtype must be RN_F32 or RN_BF16");
+    if (!(eps >= 0.f)) return fail(RN_EINVAL, "eps must be 0 or more");
+    if (total && !residual) return fail(RN_EINVAL, "without a residual there is no total: it must be NULL");
+    if (rows == 0) return RN_OK;
+    if (!x) return fail(RN_EINVAL, "x must not be NULL");
+    if (!y && !q) return fail(RN_EINVAL, "y and q must not both be NULL");
+    if (!q != !scales) return fail(RN_EINVAL, "q and scales go together: one of them is NULL");
+    if (rows > 1 && (x_stride < width || (residual && residual_stride < width)))
+        return fail(RN_EINVAL, "a row stride is smaller than its row");
+    if (y && y == total) return fail(RN_EINVAL, "y and total must be two arrays");
+    if (rows > 1 && (((y == x || total == x) && x_stride != width) ||
+                     (residual && (y == residual || total == residual) && residual_stride != width)))
+        return fail(RN_EINVAL, "a result lies over an input that is not contiguous");
+    RmsArgs a{};
+    a.rows = rows, a.width = width;
+    a.x = x, a.residual = residual;
+    a.xs = x_stride, a.rs = residual ? residual_stride : 0;
+    a.weight = weight, a.eps = eps;
+    a.y = y, a.q = static_cast<uint8_t *>(q), a.scales = scales, a.total = total, a.rstd = rstd;
+    return launched(launch_rms(a, dtype == RN_BF16, static_cast<hipStream_t>(stream)));
+}
+
+size_t reuse_ops_rms_norm_backward_scratch_bytes(int64_t rows, int32_t width) {
+    if (rows < 0 || rows > kMaxRows || width < 1 || width > kMaxWidth) return 0;
+    return round_up((size_t)norm_blocks(rows, width) * (size_t)width * 4);
+}
+
+rn_status reuse_ops_rms_norm_backward(int64_t rows, int32_t width, const void *dy, int64_t dy_stride,
+                                      const void *total, int64_t total_stride, rn_dtype dtype, const float *weight,
+                                      const float *rstd, const void *dtotal, int64_t dtotal_stride, void *dx,
+                                      float *dweight, int32_t accumulate, void *scratch, size_t scratch_bytes,
+                                      void *stream) {
+    if (rows < 0 || rows > kMaxRows || width < 1 || width > kMaxWidth)
+        return fail(RN_EINVAL, "rows must be 0..2^40 and width 1..2^30");
+    if (!known(dtype)) return fail(RN_EINVAL, "dtype must be RN_F32 or RN_BF16");
+    if (rows == 0 && !dweight) return RN_OK;
+    if (rows > 0 && (!dy || !total || !rstd || !dx)) return fail(RN_EINVAL, "dy, total, rstd and dx must not be NULL");
+    if (rows > 1 && (dy_stride < width || total_stride < width || (dtotal && dtotal_stride < width)))
+        return fail(RN_EINVAL, "a row stride is smaller than its row");
+    if (rows > 1 && ((dx == dy && dy_stride != width) || (dx == total && total_stride != width) ||
+                     (dx == dtotal && dtotal_stride != width)))
+        return fail(RN_EINVAL, "a result lies over an input that is not contiguous");
+    if (dweight) {
+        if (!scratch) return fail(RN_EINVAL, "scratch is NULL");
+        if (misaligned(scratch)) return fail(RN_EINVAL, "scratch must be 256-byte aligned");
+        const size_t need = reuse_ops_rms_norm_backward_scratch_bytes(rows, width);
+        if (scratch_bytes < need) return need_bytes("scratch", need);
+    }
+    RmsArgs a{};
+    a.rows = rows, a.width = width;
+    a.x = total, a.dy = dy, a.dtotal = dtotal, a.y = dx;
+    a.xs = total_stride, a.dys = dy_stride, a.dts = dtotal ? dtotal_stride : 0;
+    a.weight = weight, a.rstd = const_cast<float *>(rstd);
+    a.blocks = rows > 0 ? norm_blocks(rows, width) : 0;
+    a.part = dweight ? static_cast<float *>(scratch) : nullptr;
+    a.dweight = dweight, a.accumulate = accumulate;
+    return launched(launch_rms_backward(a, dtype == RN_BF16, static_cast<hipStream_t>(stream)));
+}
+
 rn_status reuse_ops_sample(int32_t n, int32_t vocab, const void *logits, int64_t stride, rn_dtype dtype,
                            const float *u, const rn_sample_params *params, int32_t *tokens, float *logprobs,
                            void *stream) {

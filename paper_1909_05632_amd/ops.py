@@ -45,7 +45,8 @@ EXPORTS = (
     "reuse_ops_last_error", "reuse_ops_layer_norm", "reuse_ops_layer_norm_backward_scratch_bytes",
     "reuse_ops_layer_norm_backward", "reuse_ops_sample", "reuse_ops_delta_step", "reuse_ops_delta_saved_bytes",
     "reuse_ops_delta_scratch_bytes", "reuse_ops_delta_backward_scratch_bytes", "reuse_ops_delta_forward",
-    "reuse_ops_delta_backward",
+    "reuse_ops_delta_backward", "reuse_ops_rms_norm", "reuse_ops_rms_norm_backward_scratch_bytes",
+    "reuse_ops_rms_norm_backward",
 )
 
 
@@ -79,6 +80,9 @@ def load_ops():
             ("layer_norm", st, [I64, I32, P, I64, st, P, P, F, P, I64, P, P]),
             ("layer_norm_backward_scratch_bytes", SZ, [I64, I32]),
             ("layer_norm_backward", st, [I64, I32, P, I64, P, I64, st, P, P, P, I64, P, P, I32, P, SZ, P]),
+            ("rms_norm", st, [I64, I32, P, I64, st, P, I64, P, F, P, P, P, P, P, P]),
+            ("rms_norm_backward_scratch_bytes", SZ, [I64, I32]),
+            ("rms_norm_backward", st, [I64, I32, P, I64, P, I64, st, P, P, P, I64, P, P, I32, P, SZ, P]),
             ("sample", st, [I32, I32, P, I64, st, P, ctypes.POINTER(rn_sample_params), P, P, P]),
             ("delta_step", st, [shape, P, P, P, P, P, P, I32, P, P, P]),
             ("delta_saved_bytes", SZ, [shape]),
@@ -101,7 +105,7 @@ def _check(status: int) -> None:
         raise B.ReuseNetError(status, reuse_ops_last_error())
 
 
-_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
+_F32, _BF16, _I32, _F8 = torch.float32, torch.bfloat16, torch.int32, torch.float8_e4m3fn
 _CODES = {_F32: B.RN_F32, _BF16: B.RN_BF16}
 
 
@@ -281,6 +285,116 @@ def layer_norm_backward(dy, x, weight, stats, dx=None, dweight=None, dbias=None,
     _launch(dev, L.reuse_ops_layer_norm_backward, rows, width, dy.data_ptr(), dys, x.data_ptr(), xs, code, w,
             st, d, width, dw, db, int(accumulate), sc, need)
     return dx, dweight, dbias
+
+
+# ------------------------------------------------------------------ residual norm
+
+def _same(x, like, what: str, of: str) -> None:
+    """x has the dtype, shape and device of `like`."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{what} must be a torch tensor")
+    if x.dtype is not like.dtype or x.shape != like.shape or x.device != like.device:
+        raise ValueError(f"{what} must have {of}'s dtype, shape and device")
+
+
+def rms_norm(x, weight=None, residual=None, eps: float = 1e-5, with_stats: bool = False, quantize: bool = False,
+             out=None, scales=None, total=None, stream=None):
+    """Norm by the root mean square over the last axis, of x or of x + residual (reuse_ops_rms_norm).
+
+    x, residual: [..., width] float32 or bfloat16, rows contiguous and at one
+    stride; weight: [width] float32 or None.  Returns y in x's dtype; with
+    quantize in its place y / scales as float8_e4m3fn and the [rows] float32
+    scales; then x + residual in x's dtype if there is a residual, and with
+    with_stats the [rows] float32 1/rms for the backward call.  One result
+    comes alone, more as a tuple.  out, total: where y and the sum go (they
+    may be x or the residual); made here if None.
+    """
+    if stream is not None:
+        with _on(stream, x):
+            return rms_norm(x, weight, residual, eps, with_stats, quantize, out, scales, total)
+    _no_grad(x, weight, residual)
+    code = _data(x, "x")
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x must have a last axis of 1 or more")
+    dev, width = x.device, _count(x.shape[-1], "width")
+    rows, stride = _rows(x, "x")
+    w = None if weight is None else _like(weight, "weight", _F32, dev, (width,))
+    r, rs, tp = None, 0, None
+    if residual is not None:
+        _same(residual, x, "residual", "x")
+        r, rs = residual.data_ptr(), _rows(residual, "residual")[1]
+        if total is None:
+            total = _empty(x)
+        tp = _like(total, "total", x.dtype, dev, x.shape)
+    elif total is not None:
+        raise ValueError("without a residual there is no total")
+    if out is None:
+        out = _empty(x, x.shape, _F8) if quantize else _empty(x)
+    o = _like(out, "out", _F8 if quantize else x.dtype, dev, x.shape)
+    got, sp = [out], None
+    if quantize:
+        if scales is None:
+            scales = _empty(x, rows, _F32)
+        sp = _like(scales, "scales", _F32, dev, (rows,))
+        got.append(scales)
+    elif scales is not None:
+        raise ValueError("scales are written with quantize only")
+    if residual is not None:
+        got.append(total)
+    stats = None
+    if with_stats:
+        stats = _empty(x, rows, _F32)
+        got.append(stats)
+    _launch(dev, load_ops().reuse_ops_rms_norm, rows, width, x.data_ptr(), stride, code, r, rs, w, eps,
+            None if quantize else o, o if quantize else None, sp, tp, None if stats is None else stats.data_ptr())
+    return got[0] if len(got) == 1 else tuple(got)
+
+
+def rms_norm_backward(dy, total, weight, stats, dtotal=None, dx=None, dweight=None, accumulate: bool = False,
+                      want_params: bool = True, stream=None):
+    """(dx, dweight) of rms_norm (reuse_ops_rms_norm_backward); dx is the residual's gradient too.
+
+    total, stats: from the forward call (x itself if it had no residual).
+    dtotal: the gradient that reaches the sum by another way, or None.
+    dweight: [width] float32 buffer to write, or to add to with accumulate;
+    made here if None.  want_params = False: dx only, dweight is returned as
+    given.
+    """
+    if stream is not None:
+        with _on(stream, total):
+            return rms_norm_backward(dy, total, weight, stats, dtotal, dx, dweight, accumulate, want_params)
+    _no_grad(dy, total, weight, stats, dtotal)
+    code = _data(total, "total")
+    if total.dim() < 1 or total.shape[-1] < 1:
+        raise ValueError("total must have a last axis of 1 or more")
+    _same(dy, total, "dy", "total")
+    dev, width = total.device, _count(total.shape[-1], "width")
+    rows, ts = _rows(total, "total")
+    _, dys = _rows(dy, "dy")
+    dt, dts = None, 0
+    if dtotal is not None:
+        _same(dtotal, total, "dtotal", "total")
+        dt, dts = dtotal.data_ptr(), _rows(dtotal, "dtotal")[1]
+    w = _opt(weight, "weight", _F32, dev, (width,))
+    st = _like(stats, "stats", _F32, dev, (rows,))
+    if dx is None:
+        dx = _empty(total)
+    d = _like(dx, "dx", total.dtype, dev, total.shape)
+    L = load_ops()
+    dw = sc = None
+    need = 0
+    if want_params:
+        if accumulate and dweight is None:
+            raise ValueError("accumulate needs dweight")
+        if dweight is None:
+            dweight = _empty(total, width, _F32)
+        dw = _like(dweight, "dweight", _F32, dev, (width,))
+        need = L.reuse_ops_rms_norm_backward_scratch_bytes(rows, width)
+        scratch = _empty(total, need, torch.uint8)
+        sc = scratch.data_ptr()
+    _launch(dev, L.reuse_ops_rms_norm_backward, rows, width, dy.data_ptr(), dys, total.data_ptr(), ts, code, w, st,
+            dt, dts, d, dw, int(accumulate), sc, need)
+    return dx, dweight
 
 
 # ------------------------------------------------------------------ sampling

@@ -1,0 +1,102 @@
+"""The C ABI and the torch functions of a recurrent block's operators: bad
+arguments are refused with a status and a text before any launch.  None of it
+needs a GPU: every call below ends in the checks (or has nothing to do)."""
+import pytest
+import torch
+
+from paper_1909_05632_amd import binding as B
+from paper_1909_05632_amd import ops
+
+P = 256          # a pointer that is not NULL; no call below gets as far as using it
+
+
+def _err(status, want, text):
+    assert status == want, (status, ops.reuse_ops_last_error())
+    assert text in ops.reuse_ops_last_error(), ops.reuse_ops_last_error()
+
+
+def _caller(call, **base):
+    return lambda **kw: call(*{**base, **kw}.values())
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The functions on CPU tensors; every call that would have been launched."""
+    seen = []
+    monkeypatch.setattr(ops, "_data", lambda x, what: ops._CODES[x.dtype])
+    monkeypatch.setattr(ops, "_launch", lambda device, *call: seen.append(call))
+    return seen
+
+
+# ------------------------------------------------------------------ residual norm
+
+def test_rms_norm_arguments():
+    L = ops.load_ops()
+    call = _caller(L.reuse_ops_rms_norm, rows=4, width=8, x=P, xs=8, dtype=B.RN_F32, residual=2 * P, rs=8, w=P, eps=1e-5,
+                   y=3 * P, q=None, scales=None, total=4 * P, rstd=None, stream=None)
+    _err(call(rows=-1), B.RN_EINVAL, "rows")
+    _err(call(width=0), B.RN_EINVAL, "width")
+    _err(call(dtype=B.RN_U8), B.RN_EINVAL, "dtype")
+    _err(call(x=None), B.RN_EINVAL, "NULL")
+    _err(call(y=None), B.RN_EINVAL, "NULL")
+    _err(call(q=P), B.RN_EINVAL, "go together")
+    _err(call(scales=P), B.RN_EINVAL, "go together")
+    _err(call(residual=None), B.RN_EINVAL, "no total")
+    _err(call(xs=7), B.RN_EINVAL, "stride")
+    _err(call(rs=7), B.RN_EINVAL, "stride")
+    _err(call(total=3 * P), B.RN_EINVAL, "two arrays")
+    _err(call(y=P, xs=9), B.RN_EINVAL, "not contiguous")
+    _err(call(total=2 * P, rs=9), B.RN_EINVAL, "not contiguous")
+    _err(call(eps=-1.0), B.RN_EINVAL, "eps")
+    _err(call(eps=float("nan")), B.RN_EINVAL, "eps")
+    assert call(rows=0, x=None, y=None) == B.RN_OK
+    need = L.reuse_ops_rms_norm_backward_scratch_bytes(4, 8)
+    assert need > 0 and need % 256 == 0
+    assert L.reuse_ops_rms_norm_backward_scratch_bytes(-1, 8) == L.reuse_ops_rms_norm_backward_scratch_bytes(4, 0) == 0
+    back = _caller(L.reuse_ops_rms_norm_backward, rows=4, width=8, dy=P, dys=8, total=2 * P, ts=8, dtype=B.RN_F32, w=None,
+                   rstd=P, dtotal=3 * P, dts=8, dx=4 * P, dw=P, acc=0, scratch=P, bytes=need, stream=None)
+    _err(back(rows=1 << 50), B.RN_EINVAL, "rows")
+    _err(back(dtype=9), B.RN_EINVAL, "dtype")
+    for name in ("dy", "total", "rstd", "dx"):
+        _err(back(**{name: None}), B.RN_EINVAL, "NULL")
+    for name in ("dys", "ts", "dts"):
+        _err(back(**{name: 7}), B.RN_EINVAL, "stride")
+    for name, p in (("dys", P), ("ts", 2 * P), ("dts", 3 * P)):
+        _err(back(**{name: 9, "dx": p}), B.RN_EINVAL, "not contiguous")
+    _err(back(scratch=None), B.RN_EINVAL, "scratch")
+    _err(back(scratch=P + 4), B.RN_EINVAL, "aligned")
+    _err(back(bytes=need - 1), B.RN_ENOSPACE, "need")
+    assert back(rows=0, dw=None) == B.RN_OK
+
+
+def test_rms_norm_tensors(calls):
+    x, w, f8 = torch.zeros(3, 8), torch.ones(8), torch.zeros(3, 8, dtype=torch.float8_e4m3fn)
+    stats = torch.zeros(3)
+    assert ops.rms_norm(x, w).shape == (3, 8)
+    assert [t.dtype for t in ops.rms_norm(x, w, x, with_stats=True, quantize=True)] == [
+        torch.float8_e4m3fn, torch.float32, torch.float32, torch.float32]
+    calls.clear()
+    for bad, kw in ((ValueError, dict(residual=x[:2])), (ValueError, dict(residual=x.bfloat16())), (TypeError, dict(residual=1.0)),
+                    (ValueError, dict(weight=w[:7])), (TypeError, dict(weight=w.double())), (ValueError, dict(total=x)),
+                    (ValueError, dict(scales=stats)), (TypeError, dict(out=f8)), (TypeError, dict(out=x, quantize=True)),
+                    (ValueError, dict(quantize=True, scales=stats[:2])), (ValueError, dict(out=torch.zeros(8, 3).t()))):
+        with pytest.raises(bad):
+            ops.rms_norm(x, **kw)
+    for bad, args, kw in ((ValueError, (x[:2], x, w, stats), {}), (ValueError, (x, x, w, stats[:2]), {}),
+                          (TypeError, (x, x, w, None), {}), (ValueError, (x, x, w, stats), dict(dtotal=x[:1])),
+                          (ValueError, (x, x, w, stats), dict(accumulate=True)), (TypeError, (x, x, w, stats), dict(dx=x.bfloat16()))):
+        with pytest.raises(bad):
+            ops.rms_norm_backward(*args, **kw)
+    with pytest.raises(ValueError, match="width"):
+        ops.rms_norm(torch.empty(1, (1 << 32) + 8, device="meta"))
+    for i in range(3):
+        some = [x, w, x]
+        some[i] = some[i].clone().requires_grad_()
+        with pytest.raises(ValueError, match="requires grad"):
+            ops.rms_norm(*some)
+    for i in range(5):
+        some = [x, x, w, stats, x]
+        some[i] = some[i].clone().requires_grad_()
+        with pytest.raises(ValueError, match="requires grad"):
+            ops.rms_norm_backward(*some)
+    assert not calls
