@@ -1,8 +1,8 @@
 /*
  * reuse_ops — operators around a policy net on MI355X (gfx950): layer norm, the
  * gated delta rule (a memory per stream that is carried from frame to frame), the
- * sampling of actions, and the norm of a residual stream, in the library of
- * reuse_net.h.
+ * sampling of actions, the norm of a residual stream and the log-probabilities a
+ * policy is trained on, in the library of reuse_net.h.
  *
  * A policy over many streams of frames (Sec. 1: multiple input frames; Sec. 2:
  * actions and REINFORCE) normalises each frame's features, carries a memory
@@ -254,6 +254,50 @@ rn_status reuse_ops_rms_norm_backward(int64_t rows, int32_t width, const void *d
                                       const float *dev_weight, const float *dev_rstd, const void *dev_dtotal,
                                       int64_t dtotal_stride, void *dev_dx, float *dev_dweight, int32_t accumulate,
                                       void *dev_scratch, size_t scratch_bytes, void *hip_stream);
+
+/* ---- log-probabilities of given choices ----
+ *
+ * For each of n rows of `vocab` logits l and the choice t that was made, with
+ *   p_i = exp(l_i / temperature) / sum_j exp(l_j / temperature):
+ *   logprob = log p_t,  entropy = -sum_i p_i log p_i (0 log 0 = 0),
+ * and the `top` choices of the largest logits with their log-probabilities, from the
+ * largest down, the lowest index first of equal ones.
+ *
+ * A logit of -infinity has p = 0: a choice that is not allowed.  A row of nothing
+ * else gives logprob -infinity, entropy 0 and gradients of 0.  A row with NaN or
+ * +infinity gives NaN everywhere but in top_tokens, where NaN ranks as -infinity.
+ * A t outside 0..vocab-1 gives logprob 0, without a gradient; the entropy is as ever.
+ */
+
+#define RN_LOGPROBS_MAX_TOP 64
+
+/* Device scratch bytes of the call for these sizes, whatever its dtype (0 if one is out of range, never less than
+ * 256 otherwise). */
+size_t reuse_ops_log_probs_scratch_bytes(int32_t n, int32_t vocab, int32_t top);
+
+/*   dev_logits:       n rows at `stride`; 1 <= vocab <= RN_SAMPLE_MAX_VOCAB, n >= 0.
+ *   dev_tokens:       [n] int32 choices.
+ *   temperature:      above 0 (4.3e-39 and more, so that 1.44 / temperature is finite), finite.
+ *   dev_logprobs, dev_entropy: [n] float32 or NULL (not wanted).
+ *   dev_top_tokens, dev_top_logprobs: [n][top] int32 and float32, 0 <= top <=
+ *                     min(vocab, RN_LOGPROBS_MAX_TOP); NULL if top is 0.
+ *   dev_stats:        NULL, or [n][4] float32 for the backward call: the largest
+ *                     logit, 1 / sum_j exp((l_j - largest) / temperature), the
+ *                     logarithm of that sum, the entropy.
+ *   dev_scratch:      256-byte aligned, at least the bytes above. */
+rn_status reuse_ops_log_probs(int32_t n, int32_t vocab, const void *dev_logits, int64_t stride, rn_dtype dtype,
+                              const int32_t *dev_tokens, float temperature, int32_t top, float *dev_logprobs,
+                              float *dev_entropy, int32_t *dev_top_tokens, float *dev_top_logprobs, float *dev_stats,
+                              void *dev_scratch, size_t scratch_bytes, void *hip_stream);
+
+/* Gradient of J given dJ/dlogprob and dJ/dentropy ([n] float32 each, NULL: 0):
+ *   dl_i = (dlogprob ([i = t] - p_i) - dentropy p_i (log p_i + entropy)) / temperature.
+ *   dev_stats:   from the forward call of the same logits and temperature.
+ *   dev_dlogits: [n][vocab] dtype at dlogits_stride; may be logits itself at its stride. */
+rn_status reuse_ops_log_probs_backward(int32_t n, int32_t vocab, const void *dev_logits, int64_t stride,
+                                       rn_dtype dtype, const int32_t *dev_tokens, float temperature,
+                                       const float *dev_stats, const float *dev_dlogprobs, const float *dev_dentropy,
+                                       void *dev_dlogits, int64_t dlogits_stride, void *hip_stream);
 
 #ifdef __cplusplus
 }

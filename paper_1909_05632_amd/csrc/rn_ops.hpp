@@ -1,10 +1,12 @@
 // Internal declarations of the operators in include/reuse_ops.h: kernel
-// launchers (rn_norm.hip, rn_rms.hip, rn_sample.hip, rn_delta.hip,
-// rn_delta_short.hip, rn_delta_bwd.hip) and device helpers they share.
+// launchers (rn_norm.hip, rn_rms.hip, rn_sample.hip, rn_logp.hip,
+// rn_delta.hip, rn_delta_short.hip, rn_delta_bwd.hip) and device helpers they share.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "reuse_ops.h"
 
@@ -60,6 +62,29 @@ struct SampleArgs {
     float *logprobs;
 };
 hipError_t launch_sample(const SampleArgs &a, bool bf16, hipStream_t s);
+
+struct LogpArgs {
+    int n, vocab;
+    const void *logits;
+    int64_t stride;
+    const int32_t *tokens;
+    float c, inv_t;               // log2(e) / temperature, 1 / temperature
+    int top;
+    float *logprobs, *entropy;    // each may be NULL
+    int32_t *top_tokens;
+    float *top_logprobs;
+    float *stats;                 // [n][4], or NULL; read by the backward call
+    int parts;                    // blocks a row (logp_parts)
+    float *part_sums;             // [n][parts][3]
+    uint64_t *part_keys;          // [n][parts][top]
+    // Backward call:
+    const float *dlogprobs, *dentropy;     // each may be NULL
+    void *dlogits;
+    int64_t dstride;
+};
+int logp_parts(int n, int vocab, int top, bool bf16);
+hipError_t launch_logp(const LogpArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_logp_backward(const LogpArgs &a, bool bf16, hipStream_t s);
 
 struct DeltaArgs {
     int n, hk, hv, dk, dv;

@@ -2,6 +2,7 @@
 // launches.  Nothing throws and nothing aborts.
 #include "rn_ops.hpp"
 
+#include <cmath>
 #include <cstdio>
 
 namespace {
@@ -101,6 +102,29 @@ rn_status check_delta(const rn_delta_shape *s, const void *q, const void *k, con
     if (too_wide(s)) return fail(RN_EUNSUPPORTED, "dk and dv above 128 have no kernel");
     if (s->tokens > 0 && (!q || !k || !v || !g || !beta)) return fail(RN_EINVAL, "q, k, v, g and beta must not be NULL");
     return RN_OK;
+}
+
+// ------------------------------------------------------------------ log-probabilities
+
+const char *bad_logp(int32_t n, int32_t vocab, int32_t top) {
+    if (n < 0) return "n must be 0 or more";
+    if (vocab < 1 || vocab > RN_SAMPLE_MAX_VOCAB) return "vocab must be 1..2^20";
+    if (top < 0 || top > RN_LOGPROBS_MAX_TOP || top > vocab) return "top must be 0..64 and no more than vocab";
+    return nullptr;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+bool bad_temperature(float t) { return !(t > 0.f) || !(t < HUGE_VALF) || !(kLog2e / t < HUGE_VALF); }
+
+LogpArgs logp_args(int32_t n, int32_t vocab, const void *logits, int64_t stride, const int32_t *tokens,
+                   float temperature, float *stats) {
+    LogpArgs a{};
+    a.n = n, a.vocab = vocab;
+    a.logits = logits, a.stride = stride, a.tokens = tokens;
+    a.c = kLog2e / temperature, a.inv_t = 1.f / temperature;
+    a.stats = stats;
+    return a;
 }
 
 }  // namespace
@@ -238,6 +262,60 @@ rn_status reuse_ops_sample(int32_t n, int32_t vocab, const void *logits, int64_t
     if (n > 1 && stride < vocab) return fail(RN_EINVAL, "the row stride is smaller than a row");
     SampleArgs a{n, vocab, logits, stride, u, *params, tokens, logprobs};
     return launched(launch_sample(a, dtype == RN_BF16, static_cast<hipStream_t>(stream)));
+}
+
+size_t reuse_ops_log_probs_scratch_bytes(int32_t n, int32_t vocab, int32_t top) {
+    if (bad_logp(n, vocab, top)) return 0;
+    size_t most = 0;
+    for (const bool bf16 : {false, true}) {
+        const size_t parts = (size_t)logp_parts(n, vocab, top, bf16);
+        const size_t need = parts > 1 ? round_up(n * parts * 12) + round_up(n * parts * top * 8) : 0;
+        if (need > most) most = need;
+    }
+    return most < kAlign ? kAlign : most;
+}
+
+rn_status reuse_ops_log_probs(int32_t n, int32_t vocab, const void *logits, int64_t stride, rn_dtype dtype,
+                              const int32_t *tokens, float temperature, int32_t top, float *logprobs, float *entropy,
+                              int32_t *top_tokens, float *top_logprobs, float *stats, void *scratch,
+                              size_t scratch_bytes, void *stream) {
+    if (const char *why = bad_logp(n, vocab, top)) return fail(RN_EINVAL, why);
+    if (!known(dtype)) return fail(RN_EINVAL, "dtype must be RN_F32 or RN_BF16");
+    if (bad_temperature(temperature)) return fail(RN_EINVAL, "temperature must be above 0 and finite");
+    if (n == 0) return RN_OK;
+    if (!logits || !tokens) return fail(RN_EINVAL, "logits and tokens must not be NULL");
+    if (top > 0 && (!top_tokens || !top_logprobs)) return fail(RN_EINVAL, "top_tokens and top_logprobs must not be NULL");
+    if (n > 1 && stride < vocab) return fail(RN_EINVAL, "the row stride is smaller than a row");
+    if (!scratch) return fail(RN_EINVAL, "scratch is NULL");
+    if (misaligned(scratch)) return fail(RN_EINVAL, "scratch must be 256-byte aligned");
+    const size_t need = reuse_ops_log_probs_scratch_bytes(n, vocab, top);
+    if (scratch_bytes < need) return need_bytes("scratch", need);
+    LogpArgs a = logp_args(n, vocab, logits, stride, tokens, temperature, stats);
+    a.top = top;
+    a.logprobs = logprobs, a.entropy = entropy, a.top_tokens = top_tokens, a.top_logprobs = top_logprobs;
+    a.parts = logp_parts(n, vocab, top, dtype == RN_BF16);
+    a.part_sums = static_cast<float *>(scratch);
+    a.part_keys = reinterpret_cast<uint64_t *>(static_cast<char *>(scratch) + round_up((size_t)n * a.parts * 12));
+    return launched(launch_logp(a, dtype == RN_BF16, static_cast<hipStream_t>(stream)));
+}
+
+rn_status reuse_ops_log_probs_backward(int32_t n, int32_t vocab, const void *logits, int64_t stride, rn_dtype dtype,
+                                       const int32_t *tokens, float temperature, const float *stats,
+                                       const float *dlogprobs, const float *dentropy, void *dlogits,
+                                       int64_t dlogits_stride, void *stream) {
+    if (const char *why = bad_logp(n, vocab, 0)) return fail(RN_EINVAL, why);
+    if (!known(dtype)) return fail(RN_EINVAL, "dtype must be RN_F32 or RN_BF16");
+    if (bad_temperature(temperature)) return fail(RN_EINVAL, "temperature must be above 0 and finite");
+    if (n == 0) return RN_OK;
+    if (!logits || !tokens || !stats || !dlogits)
+        return fail(RN_EINVAL, "logits, tokens, stats and dlogits must not be NULL");
+    if (n > 1 && (stride < vocab || dlogits_stride < vocab))
+        return fail(RN_EINVAL, "the row stride is smaller than a row");
+    if (n > 1 && dlogits == logits && dlogits_stride != stride)
+        return fail(RN_EINVAL, "dlogits over logits must have the same stride");
+    LogpArgs a = logp_args(n, vocab, logits, stride, tokens, temperature, const_cast<float *>(stats));
+    a.dlogprobs = dlogprobs, a.dentropy = dentropy, a.dlogits = dlogits, a.dstride = dlogits_stride;
+    return launched(launch_logp_backward(a, dtype == RN_BF16, static_cast<hipStream_t>(stream)));
 }
 
 rn_status reuse_ops_delta_step(const rn_delta_shape *shape, const void *q, const void *k, const void *v,

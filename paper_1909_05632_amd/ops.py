@@ -38,6 +38,7 @@ import torch
 from . import binding as B
 
 RN_SAMPLE_MAX_VOCAB = 1 << 20
+RN_LOGPROBS_MAX_TOP = 64
 RN_DELTA_MAX_DIM = 128
 
 # Every entry point include/reuse_ops.h declares.
@@ -46,7 +47,8 @@ EXPORTS = (
     "reuse_ops_layer_norm_backward", "reuse_ops_sample", "reuse_ops_delta_step", "reuse_ops_delta_saved_bytes",
     "reuse_ops_delta_scratch_bytes", "reuse_ops_delta_backward_scratch_bytes", "reuse_ops_delta_forward",
     "reuse_ops_delta_backward", "reuse_ops_rms_norm", "reuse_ops_rms_norm_backward_scratch_bytes",
-    "reuse_ops_rms_norm_backward",
+    "reuse_ops_rms_norm_backward", "reuse_ops_log_probs_scratch_bytes", "reuse_ops_log_probs",
+    "reuse_ops_log_probs_backward",
 )
 
 
@@ -84,6 +86,9 @@ def load_ops():
             ("rms_norm_backward_scratch_bytes", SZ, [I64, I32]),
             ("rms_norm_backward", st, [I64, I32, P, I64, P, I64, st, P, P, P, I64, P, P, I32, P, SZ, P]),
             ("sample", st, [I32, I32, P, I64, st, P, ctypes.POINTER(rn_sample_params), P, P, P]),
+            ("log_probs_scratch_bytes", SZ, [I32, I32, I32]),
+            ("log_probs", st, [I32, I32, P, I64, st, P, F, I32, P, P, P, P, P, P, SZ, P]),
+            ("log_probs_backward", st, [I32, I32, P, I64, st, P, F, P, P, P, P, I64, P]),
             ("delta_step", st, [shape, P, P, P, P, P, P, I32, P, P, P]),
             ("delta_saved_bytes", SZ, [shape]),
             ("delta_scratch_bytes", SZ, [shape]),
@@ -442,6 +447,77 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=Non
     _launch(dev, load_ops().reuse_ops_sample, n, vocab, logits.data_ptr(), stride, code, up,
             ctypes.byref(params), ids, lp)
     return tokens, logprobs
+
+
+# ------------------------------------------------------------------ log-probabilities
+
+def _choices(logits, tokens):
+    """(dtype code, n, vocab, row stride, the choices' pointer) of a row of logits and a choice each."""
+    code = _data(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError(f"logits must have shape (n, vocab), got {tuple(logits.shape)}")
+    n, vocab = logits.shape
+    _count(n, "n")
+    if not 1 <= vocab <= RN_SAMPLE_MAX_VOCAB:
+        raise ValueError(f"vocab must be 1..{RN_SAMPLE_MAX_VOCAB}, got {vocab}")
+    return code, n, vocab, _rows(logits, "logits")[1], _like(tokens, "tokens", _I32, logits.device, (n,))
+
+
+def log_probs(logits, tokens, temperature: float = 1.0, top: int = 0, with_stats: bool = False, stream=None):
+    """Log-probabilities of given choices, and the entropy of their rows (reuse_ops_log_probs).
+
+    logits: [n][vocab] float32 or bfloat16, tokens: [n] int32 choices; one
+    outside 0..vocab-1 has log-probability 0 and no gradient.  temperature: a
+    number above 0.  Returns ([n], [n]) float32; with top also the [n][top]
+    int32 likeliest choices and their float32 log-probabilities, from the
+    likeliest down; with with_stats also the [n][4] float32 that
+    log_probs_backward reads.
+    """
+    if stream is not None:
+        with _on(stream, logits):
+            return log_probs(logits, tokens, temperature, top, with_stats)
+    _no_grad(logits)
+    code, n, vocab, stride, ids = _choices(logits, tokens)
+    top = operator.index(top)
+    if not 0 <= top <= min(vocab, RN_LOGPROBS_MAX_TOP):
+        raise ValueError(f"top must be 0..{min(vocab, RN_LOGPROBS_MAX_TOP)}, got {top}")
+    L = load_ops()
+    need = L.reuse_ops_log_probs_scratch_bytes(n, vocab, top)
+    scratch = _empty(logits, need, torch.uint8)
+    got = [_empty(logits, n, _F32), _empty(logits, n, _F32)]
+    if top:
+        got += [_empty(logits, (n, top), _I32), _empty(logits, (n, top), _F32)]
+    if with_stats:
+        got.append(_empty(logits, (n, 4), _F32))
+    _launch(logits.device, L.reuse_ops_log_probs, n, vocab, logits.data_ptr(), stride, code, ids, temperature, top,
+            got[0].data_ptr(), got[1].data_ptr(), got[2].data_ptr() if top else None,
+            got[3].data_ptr() if top else None, got[-1].data_ptr() if with_stats else None, scratch.data_ptr(), need)
+    return tuple(got)
+
+
+def log_probs_backward(dlogprobs, dentropy, logits, tokens, stats, temperature: float = 1.0, dlogits=None, stream=None):
+    """dlogits of log_probs (reuse_ops_log_probs_backward).
+
+    dlogprobs, dentropy: [n] float32 gradients of the two, or None for 0;
+    logits, tokens, temperature: the forward call's, stats its result.
+    dlogits: [n][vocab] in logits' dtype, at any row stride; it may be logits
+    itself; made here if None.
+    """
+    if stream is not None:
+        with _on(stream, logits):
+            return log_probs_backward(dlogprobs, dentropy, logits, tokens, stats, temperature, dlogits)
+    _no_grad(dlogprobs, dentropy, logits, stats)
+    code, n, vocab, stride, ids = _choices(logits, tokens)
+    dev = logits.device
+    st = _like(stats, "stats", _F32, dev, (n, 4))
+    dp = _opt(dlogprobs, "dlogprobs", _F32, dev, (n,))
+    de = _opt(dentropy, "dentropy", _F32, dev, (n,))
+    if dlogits is None:
+        dlogits = _empty(logits)
+    _same(dlogits, logits, "dlogits", "logits")
+    _launch(dev, load_ops().reuse_ops_log_probs_backward, n, vocab, logits.data_ptr(), stride, code, ids, temperature,
+            st, dp, de, dlogits.data_ptr(), _rows(dlogits, "dlogits")[1])
+    return dlogits
 
 
 # ------------------------------------------------------------------ gated delta rule

@@ -100,3 +100,61 @@ def test_rms_norm_tensors(calls):
         with pytest.raises(ValueError, match="requires grad"):
             ops.rms_norm_backward(*some)
     assert not calls
+
+
+# ------------------------------------------------------------------ log-probabilities
+
+def test_log_probs_arguments():
+    L = ops.load_ops()
+    base = dict(n=2, vocab=6, logits=P, stride=6, dtype=B.RN_F32, tokens=P, temperature=1.0, top=2, lp=P, h=P, ids=P, tlp=P,
+                stats=None, scratch=P, bytes=256, stream=None)
+    call = _caller(L.reuse_ops_log_probs, **base)
+    for kw, text in ((dict(n=-1), "n must"), (dict(vocab=0), "vocab"), (dict(vocab=(1 << 20) + 1), "vocab"), (dict(top=-1), "top"),
+                     (dict(top=7), "top"), (dict(vocab=1000, top=65), "top"), (dict(dtype=B.RN_U8), "dtype"),
+                     (dict(temperature=0.0), "temperature"), (dict(temperature=-1.0), "temperature"),
+                     (dict(temperature=float("nan")), "temperature"), (dict(temperature=float("inf")), "temperature"),
+                     (dict(temperature=1e-39), "temperature"), (dict(logits=None), "NULL"), (dict(tokens=None), "NULL"),
+                     (dict(ids=None), "NULL"), (dict(tlp=None), "NULL"), (dict(stride=5), "stride"), (dict(scratch=None), "scratch"),
+                     (dict(scratch=P + 8), "aligned")):
+        _err(call(**kw), B.RN_EINVAL, text)
+    _err(call(bytes=255), B.RN_ENOSPACE, "need")
+    assert call(n=0, logits=None, tokens=None) == B.RN_OK
+    size = L.reuse_ops_log_probs_scratch_bytes
+    assert size(-1, 6, 0) == size(2, 0, 0) == size(2, 6, 7) == size(2, 1000, 65) == 0
+    assert size(2, 6, 2) == 256 == size(1 << 20, 1 << 20, 64) == size((1 << 31) - 1, 1 << 20, 0)
+    assert size(1, 1 << 20, 64) >= 32 * 12 and size(1, 1 << 20, 64) % 256 == 0
+    _err(_caller(L.reuse_ops_log_probs, **{**base, "vocab": 1 << 20, "stride": 1 << 20, "n": 1})(), B.RN_ENOSPACE, "need")
+    back = _caller(L.reuse_ops_log_probs_backward, n=2, vocab=6, logits=P, stride=6, dtype=B.RN_F32, tokens=P, temperature=1.0,
+                   stats=P, dlp=P, dh=P, dl=2 * P, ds=6, stream=None)
+    for kw, text in ((dict(n=-1), "n must"), (dict(vocab=0), "vocab"), (dict(dtype=7), "dtype"), (dict(temperature=0.0), "temperature"),
+                     (dict(logits=None), "NULL"), (dict(tokens=None), "NULL"), (dict(stats=None), "NULL"), (dict(dl=None), "NULL"),
+                     (dict(stride=5), "stride"), (dict(ds=5), "stride"), (dict(dl=P, ds=7), "same stride")):
+        _err(back(**kw), B.RN_EINVAL, text)
+    assert back(n=0, logits=None) == B.RN_OK
+
+
+def test_log_probs_tensors(calls):
+    x, t, one, st = torch.zeros(3, 8), torch.zeros(3, dtype=torch.int32), torch.ones(3), torch.zeros(3, 4)
+    assert [tuple(g.shape) for g in ops.log_probs(x, t, top=2, with_stats=True)] == [(3,), (3,), (3, 2), (3, 2), (3, 4)]
+    assert ops.log_probs_backward(one, None, x, t, st).shape == (3, 8)
+    calls.clear()
+    for bad, args, kw in ((ValueError, (x[0], t), {}), (ValueError, (x, t[:2]), {}), (TypeError, (x, t.long()), {}),
+                          (ValueError, (x, t), dict(top=9)), (ValueError, (x, t), dict(top=-1)), (TypeError, (x, t), dict(top=1.5)),
+                          (ValueError, (torch.zeros(8, 3).t(), t), {}), (ValueError, (torch.zeros(3, 0), t), {}),
+                          (ValueError, (torch.empty((1 << 32) + 2, 4, device="meta"), t), {})):
+        with pytest.raises(bad):
+            ops.log_probs(*args, **kw)
+    for bad, args, kw in ((ValueError, (one[:2], None, x, t, st), {}), (TypeError, (one, one.double(), x, t, st), {}),
+                          (ValueError, (one, one, x, t, st[:, :3]), {}), (TypeError, (one, one, x, t, None), {}),
+                          (ValueError, (one, one, x, t, st), dict(dlogits=x.bfloat16())),
+                          (ValueError, (one, one, x, t, st), dict(dlogits=torch.zeros(8, 3).t()))):
+        with pytest.raises(bad):
+            ops.log_probs_backward(*args, **kw)
+    with pytest.raises(ValueError, match="requires grad"):
+        ops.log_probs(x.clone().requires_grad_(), t)
+    for i in (0, 1, 2, 4):
+        some = [one, one, x, t, st]
+        some[i] = some[i].clone().requires_grad_()
+        with pytest.raises(ValueError, match="requires grad"):
+            ops.log_probs_backward(*some)
+    assert not calls
