@@ -1,8 +1,9 @@
 /*
  * reuse_ops — operators around a policy net on MI355X (gfx950): layer norm, the
  * gated delta rule (a memory per stream that is carried from frame to frame), the
- * sampling of actions, the norm of a residual stream and the log-probabilities a
- * policy is trained on, in the library of reuse_net.h.
+ * sampling of actions, the norm of a residual stream, the log-probabilities a
+ * policy is trained on, and a short convolution over a stream's last tokens, in the
+ * library of reuse_net.h.
  *
  * A policy over many streams of frames (Sec. 1: multiple input frames; Sec. 2:
  * actions and REINFORCE) normalises each frame's features, carries a memory
@@ -298,6 +299,62 @@ rn_status reuse_ops_log_probs_backward(int32_t n, int32_t vocab, const void *dev
                                        rn_dtype dtype, const int32_t *dev_tokens, float temperature,
                                        const float *dev_stats, const float *dev_dlogprobs, const float *dev_dentropy,
                                        void *dev_dlogits, int64_t dlogits_stride, void *hip_stream);
+
+/* ---- short causal convolution ----
+ *
+ * Each channel by itself, over a sequence's tokens x_t:
+ *   pre_t = bias + sum_(k < taps) weight_k x_(t - taps + 1 + k),
+ *   out_t = pre_t / (1 + exp(-pre_t)) (silu), or pre_t.
+ * What lies before the sequence's first token is its window: the taps - 1 inputs
+ * before, the oldest first.
+ */
+
+#define RN_CONV_MAX_TAPS 4
+
+typedef struct {
+    int32_t n;                    /* sequences (streams), 0..65535 */
+    int32_t channels;             /* 1..65536 */
+    int32_t taps;                 /* 1..RN_CONV_MAX_TAPS */
+    int64_t tokens;               /* tokens of all sequences, 0..2^31 - 1 */
+    rn_dtype dtype;               /* of x, out and the windows */
+    int32_t silu;                 /* not 0: out = silu(pre) */
+    int64_t x_stride;             /* elements from a token to the next, below 2^23 */
+} rn_conv_shape;
+
+/* One token for each of n streams (tokens = n), the windows updated in place.
+ *   dev_weight:     [channels][taps] float32;  dev_bias: [channels] float32 or NULL (0).
+ *   dev_window:     [slots][taps - 1][channels] dtype; not used where taps is 1.
+ *   dev_stream_ids: [n] distinct slots, or NULL for 0..n-1.  A stream whose id is
+ *                   outside 0..slots-1 is left out and its out is 0.
+ *   dev_out:        [n][channels] dtype, contiguous; may be x itself where that is. */
+rn_status reuse_ops_causal_conv_step(const rn_conv_shape *shape, const void *dev_x, const float *dev_weight,
+                                     const float *dev_bias, const int32_t *dev_stream_ids, int32_t slots,
+                                     void *dev_window, void *dev_out, void *hip_stream);
+
+/* All tokens of n sequences packed one after another, as reuse_ops_delta_forward's.
+ *   dev_seq_off: [n+1] int32, or NULL: every sequence has tokens / n.
+ *   dev_window:  [n][taps - 1][channels] dtype before the first token, or NULL for 0.
+ *   dev_final:   the same after the last token, or NULL; not dev_window.
+ *   dev_out:     [tokens][channels] dtype, contiguous; not x. */
+rn_status reuse_ops_causal_conv(const rn_conv_shape *shape, const void *dev_x, const float *dev_weight,
+                                const float *dev_bias, const int32_t *dev_seq_off, const void *dev_window,
+                                void *dev_final, void *dev_out, void *hip_stream);
+
+/* Device scratch bytes of the backward call (0 if the shape is out of range). */
+size_t reuse_ops_causal_conv_backward_scratch_bytes(const rn_conv_shape *shape);
+
+/* Gradients of J given dout = dJ/dout and dfinal = dJ/dfinal (NULL: 0).
+ *   dev_dout:    [tokens][channels] dtype, contiguous.
+ *   dev_dfinal:  [n][taps - 1][channels] dtype or NULL.
+ *   dev_dx:      [tokens][channels] dtype, contiguous; neither x nor dout.
+ *   dev_dweight, dev_dbias: [channels][taps] and [channels] float32.
+ *   dev_dwindow: [n][taps - 1][channels] dtype or NULL (not wanted); not dfinal.
+ *   dev_scratch: 256-byte aligned. */
+rn_status reuse_ops_causal_conv_backward(const rn_conv_shape *shape, const void *dev_x, const float *dev_weight,
+                                         const float *dev_bias, const int32_t *dev_seq_off, const void *dev_window,
+                                         const void *dev_dout, const void *dev_dfinal, void *dev_dx,
+                                         float *dev_dweight, float *dev_dbias, void *dev_dwindow, void *dev_scratch,
+                                         size_t scratch_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -1,6 +1,6 @@
 // Internal declarations of the operators in include/reuse_ops.h: kernel
 // launchers (rn_norm.hip, rn_rms.hip, rn_sample.hip, rn_logp.hip,
-// rn_delta.hip, rn_delta_short.hip, rn_delta_bwd.hip) and device helpers they share.
+// rn_sconv.hip, rn_delta.hip, rn_delta_short.hip, rn_delta_bwd.hip) and device helpers they share.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -85,6 +85,30 @@ struct LogpArgs {
 int logp_parts(int n, int vocab, int top, bool bf16);
 hipError_t launch_logp(const LogpArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_logp_backward(const LogpArgs &a, bool bf16, hipStream_t s);
+
+struct CausalArgs {
+    int n, channels, taps, silu;
+    int64_t tokens, xs;
+    const void *x;
+    const float *weight, *bias;
+    const int32_t *off;           // [n+1], or NULL: even lengths
+    const int32_t *ids;           // step: slots, or NULL
+    int slots;
+    const void *window;           // first windows, or NULL for 0
+    void *final_window;           // last windows, or NULL (step: the windows' pool)
+    void *out;
+    // Backward call:
+    const void *dout, *dfinal;
+    void *dx, *dwindow;
+    float *dweight, *dbias;
+    float *part;                  // [run_blocks][channels (taps + 1)], causal_parts(tokens) rows at most
+    // Set by the launcher: threads of a block over the channels, rows of blocks over the tokens.
+    int lanes, run_blocks;
+};
+int64_t causal_parts(int64_t tokens);
+hipError_t launch_causal(const CausalArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_causal_backward(const CausalArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_causal_step(const CausalArgs &a, bool bf16, hipStream_t s);
 
 struct DeltaArgs {
     int n, hk, hv, dk, dv;

@@ -35,7 +35,7 @@ bool known(rn_dtype d) { return d == RN_F32 || d == RN_BF16; }
 bool misaligned(const void *p) { return reinterpret_cast<uintptr_t>(p) % kAlign != 0; }
 
 constexpr int64_t kMaxRows = int64_t(1) << 40, kMaxStride = 1 << 23;
-constexpr int kMaxWidth = 1 << 30, kMaxHeads = 1024, kMaxSequences = 65535;
+constexpr int kMaxWidth = 1 << 30, kMaxHeads = 1024, kMaxSequences = 65535, kMaxChannels = 65536;
 
 // ------------------------------------------------------------------ delta rule
 
@@ -124,6 +124,29 @@ LogpArgs logp_args(int32_t n, int32_t vocab, const void *logits, int64_t stride,
     a.logits = logits, a.stride = stride, a.tokens = tokens;
     a.c = kLog2e / temperature, a.inv_t = 1.f / temperature;
     a.stats = stats;
+    return a;
+}
+
+// ------------------------------------------------------------------ short convolution
+
+const char *bad_conv(const rn_conv_shape *s) {
+    if (!s) return "shape is NULL";
+    if (s->n < 0 || s->n > kMaxSequences) return "n must be 0..65535";
+    if (s->channels < 1 || s->channels > kMaxChannels) return "channels must be 1..65536";
+    if (s->taps < 1 || s->taps > RN_CONV_MAX_TAPS) return "taps must be 1..4";
+    if (s->tokens < 0 || s->tokens > INT32_MAX) return "tokens must be 0..2^31 - 1";
+    if (s->n == 0 && s->tokens > 0) return "tokens without sequences";
+    if (!known(s->dtype)) return "dtype must be RN_F32 or RN_BF16";
+    if (s->tokens > 1 && s->x_stride < s->channels) return "a token stride is smaller than its token";
+    if (s->tokens > 1 && s->x_stride >= kMaxStride) return "token strides must be below 2^23";
+    return nullptr;
+}
+
+CausalArgs conv_args(const rn_conv_shape *s, const void *x, const float *weight, const float *bias) {
+    CausalArgs a{};
+    a.n = s->n, a.channels = s->channels, a.taps = s->taps, a.silu = s->silu;
+    a.tokens = s->tokens, a.xs = s->x_stride;
+    a.x = x, a.weight = weight, a.bias = bias;
     return a;
 }
 
@@ -316,6 +339,65 @@ rn_status reuse_ops_log_probs_backward(int32_t n, int32_t vocab, const void *log
     LogpArgs a = logp_args(n, vocab, logits, stride, tokens, temperature, const_cast<float *>(stats));
     a.dlogprobs = dlogprobs, a.dentropy = dentropy, a.dlogits = dlogits, a.dstride = dlogits_stride;
     return launched(launch_logp_backward(a, dtype == RN_BF16, static_cast<hipStream_t>(stream)));
+}
+
+rn_status reuse_ops_causal_conv_step(const rn_conv_shape *shape, const void *x, const float *weight, const float *bias,
+                                     const int32_t *ids, int32_t slots, void *window, void *out, void *stream) {
+    if (const char *why = bad_conv(shape)) return fail(RN_EINVAL, why);
+    if (shape->tokens != shape->n) return fail(RN_EINVAL, "a step takes one token a stream: tokens must be n");
+    if (slots < 0 || (!ids && slots < shape->n)) return fail(RN_EINVAL, "fewer slots than streams");
+    if (shape->n == 0) return RN_OK;
+    if (!x || !weight || !out || (shape->taps > 1 && !window))
+        return fail(RN_EINVAL, "x, weight, window and out must not be NULL");
+    if (out == x && shape->n > 1 && shape->x_stride != shape->channels)
+        return fail(RN_EINVAL, "a result lies over an input that is not contiguous");
+    if (out == window) return fail(RN_EINVAL, "out and the windows must be two arrays");
+    CausalArgs a = conv_args(shape, x, weight, bias);
+    a.ids = ids, a.slots = slots, a.final_window = window, a.out = out;
+    return launched(launch_causal_step(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
+}
+
+rn_status reuse_ops_causal_conv(const rn_conv_shape *shape, const void *x, const float *weight, const float *bias,
+                                const int32_t *seq_off, const void *window, void *final_window, void *out,
+                                void *stream) {
+    if (const char *why = bad_conv(shape)) return fail(RN_EINVAL, why);
+    if (!seq_off && shape->n > 0 && shape->tokens % shape->n)
+        return fail(RN_EINVAL, "without seq_off, tokens must be a multiple of n");
+    if (shape->n == 0) return RN_OK;
+    if (shape->tokens > 0 && (!x || !weight || !out)) return fail(RN_EINVAL, "x, weight and out must not be NULL");
+    if (out && out == x) return fail(RN_EINVAL, "out must not be x");
+    if (final_window && final_window == window) return fail(RN_EINVAL, "the final windows must not be the first ones");
+    CausalArgs a = conv_args(shape, x, weight, bias);
+    a.off = seq_off, a.window = window, a.final_window = final_window, a.out = out;
+    return launched(launch_causal(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
+}
+
+size_t reuse_ops_causal_conv_backward_scratch_bytes(const rn_conv_shape *shape) {
+    if (bad_conv(shape)) return 0;
+    return round_up((size_t)causal_parts(shape->tokens) * shape->channels * (shape->taps + 1) * 4) + kAlign;
+}
+
+rn_status reuse_ops_causal_conv_backward(const rn_conv_shape *shape, const void *x, const float *weight,
+                                         const float *bias, const int32_t *seq_off, const void *window,
+                                         const void *dout, const void *dfinal, void *dx, float *dweight, float *dbias,
+                                         void *dwindow, void *scratch, size_t scratch_bytes, void *stream) {
+    if (const char *why = bad_conv(shape)) return fail(RN_EINVAL, why);
+    if (!seq_off && shape->n > 0 && shape->tokens % shape->n)
+        return fail(RN_EINVAL, "without seq_off, tokens must be a multiple of n");
+    if (shape->tokens > 0 && (!x || !dout || !dx)) return fail(RN_EINVAL, "x, dout and dx must not be NULL");
+    if (!weight || !dweight || !dbias) return fail(RN_EINVAL, "weight, dweight and dbias must not be NULL");
+    if (dx && (dx == x || dx == dout)) return fail(RN_EINVAL, "dx must be neither x nor dout");
+    if (dwindow && (dwindow == dfinal || dwindow == window))
+        return fail(RN_EINVAL, "dwindow must be neither dfinal nor the windows");
+    if (!scratch) return fail(RN_EINVAL, "scratch is NULL");
+    if (misaligned(scratch)) return fail(RN_EINVAL, "scratch must be 256-byte aligned");
+    const size_t need = reuse_ops_causal_conv_backward_scratch_bytes(shape);
+    if (scratch_bytes < need) return need_bytes("scratch", need);
+    CausalArgs a = conv_args(shape, x, weight, bias);
+    a.off = seq_off, a.window = window;
+    a.dout = dout, a.dfinal = dfinal, a.dx = dx, a.dwindow = dwindow, a.dweight = dweight, a.dbias = dbias;
+    a.part = static_cast<float *>(scratch);
+    return launched(launch_causal_backward(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
 }
 
 rn_status reuse_ops_delta_step(const rn_delta_shape *shape, const void *q, const void *k, const void *v,

@@ -39,6 +39,7 @@ from . import binding as B
 
 RN_SAMPLE_MAX_VOCAB = 1 << 20
 RN_LOGPROBS_MAX_TOP = 64
+RN_CONV_MAX_TAPS = 4
 RN_DELTA_MAX_DIM = 128
 
 # Every entry point include/reuse_ops.h declares.
@@ -48,7 +49,8 @@ EXPORTS = (
     "reuse_ops_delta_scratch_bytes", "reuse_ops_delta_backward_scratch_bytes", "reuse_ops_delta_forward",
     "reuse_ops_delta_backward", "reuse_ops_rms_norm", "reuse_ops_rms_norm_backward_scratch_bytes",
     "reuse_ops_rms_norm_backward", "reuse_ops_log_probs_scratch_bytes", "reuse_ops_log_probs",
-    "reuse_ops_log_probs_backward",
+    "reuse_ops_log_probs_backward", "reuse_ops_causal_conv_step", "reuse_ops_causal_conv",
+    "reuse_ops_causal_conv_backward_scratch_bytes", "reuse_ops_causal_conv_backward",
 )
 
 
@@ -65,6 +67,12 @@ class rn_delta_shape(ctypes.Structure):
                 ("v_stride", ctypes.c_int64), ("even", ctypes.c_int32)]
 
 
+class rn_conv_shape(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("channels", ctypes.c_int32), ("taps", ctypes.c_int32),
+                ("tokens", ctypes.c_int64), ("dtype", ctypes.c_int), ("silu", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64)]
+
+
 _ops = None
 
 
@@ -76,7 +84,7 @@ def load_ops():
     L = B.load_library()
     P, I32, I64, SZ, F, st = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float,
                               ctypes.c_int)
-    shape = ctypes.POINTER(rn_delta_shape)
+    shape, conv = ctypes.POINTER(rn_delta_shape), ctypes.POINTER(rn_conv_shape)
     for name, res, args in (
             ("last_error", ctypes.c_char_p, []),
             ("layer_norm", st, [I64, I32, P, I64, st, P, P, F, P, I64, P, P]),
@@ -89,6 +97,10 @@ def load_ops():
             ("log_probs_scratch_bytes", SZ, [I32, I32, I32]),
             ("log_probs", st, [I32, I32, P, I64, st, P, F, I32, P, P, P, P, P, P, SZ, P]),
             ("log_probs_backward", st, [I32, I32, P, I64, st, P, F, P, P, P, P, I64, P]),
+            ("causal_conv_step", st, [conv, P, P, P, P, I32, P, P, P]),
+            ("causal_conv", st, [conv, P, P, P, P, P, P, P, P]),
+            ("causal_conv_backward_scratch_bytes", SZ, [conv]),
+            ("causal_conv_backward", st, [conv, P, P, P, P, P, P, P, P, P, P, P, P, SZ, P]),
             ("delta_step", st, [shape, P, P, P, P, P, P, I32, P, P, P]),
             ("delta_saved_bytes", SZ, [shape]),
             ("delta_scratch_bytes", SZ, [shape]),
@@ -681,3 +693,118 @@ def delta_backward(dout, q, k, v, g, beta, seq_off=None, n=None, saved=None, dfi
             bp, off, sp, saved.numel(), do, df, gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), dg.data_ptr(),
             dbeta.data_ptr(), None if dstate is None else dstate.data_ptr(), scratch.data_ptr(), need)
     return gq, gk, gv, dg, dbeta, dstate
+
+
+# ------------------------------------------------------------------ short convolution
+
+def _flat(x, what: str, dtype, tokens: int, channels: int, device):
+    """(pointer, token stride) of [tokens][channels] data whose channels are contiguous."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{what} must be a torch tensor")
+    if x.dtype is not dtype or x.device != device:
+        raise ValueError(f"{what} must be {dtype} on {device}")
+    if x.shape != (tokens, channels):
+        raise ValueError(f"{what} must have shape ({tokens}, {channels}), got {tuple(x.shape)}")
+    return x.data_ptr(), _rows(x, what)[1]
+
+
+def _conv_shape(x, weight, bias, n: int, silu):
+    """(shape, taps, pointers of x, weight and bias, device) of a convolution's checked arguments."""
+    code = _data(x, "x")
+    if x.dim() != 2 or x.shape[1] < 1:
+        raise ValueError(f"x must have shape (tokens, channels), got {tuple(x.shape)}")
+    tokens, channels = x.shape
+    dev = x.device
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2 or not 1 <= weight.shape[1] <= RN_CONV_MAX_TAPS:
+        raise ValueError(f"weight must have shape (channels, taps) with 1..{RN_CONV_MAX_TAPS} taps")
+    taps = weight.shape[1]
+    _count(max(channels, n), "channels and n")
+    xp, stride = _flat(x, "x", x.dtype, tokens, channels, dev)
+    w, b = _like(weight, "weight", _F32, dev, (channels, taps)), _opt(bias, "bias", _F32, dev, (channels,))
+    return rn_conv_shape(n, channels, taps, tokens, code, bool(silu), stride), taps, xp, w, b, dev
+
+
+def causal_conv_step(x, weight, state, bias=None, stream_ids=None, silu: bool = True, out=None, stream=None):
+    """One token for each of n streams, their windows updated in place (reuse_ops_causal_conv_step).
+
+    x: [n][channels] float32 or bfloat16; weight: [channels][taps] float32,
+    the last tap the token's own; state: [slots][taps - 1][channels] in x's
+    dtype, the inputs before, oldest first; bias: [channels] float32 or None;
+    stream_ids: [n] int32 distinct slots (None: 0..n-1).  Returns out
+    [n][channels], which may be x.
+    """
+    if stream is not None:
+        with _on(stream, x):
+            return causal_conv_step(x, weight, state, bias, stream_ids, silu, out)
+    _no_grad(x, weight, state, bias)
+    n = x.shape[0] if isinstance(x, torch.Tensor) and x.dim() else 0
+    shape, taps, xp, w, b, dev = _conv_shape(x, weight, bias, n, silu)
+    slots = state.shape[0] if isinstance(state, torch.Tensor) and state.dim() else 0
+    sp = _like(state, "state", x.dtype, dev, (_count(slots, "slots"), taps - 1, x.shape[1]))
+    ids = _opt(stream_ids, "stream_ids", _I32, dev, (n,))
+    if ids is None and slots < n:
+        raise ValueError(f"{n} streams need as many slots, state has {slots}")
+    if out is None:
+        out = _empty(x)
+    op = _like(out, "out", x.dtype, dev, x.shape)
+    _launch(dev, load_ops().reuse_ops_causal_conv_step, ctypes.byref(shape), xp, w, b, ids, slots, sp, op)
+    return out
+
+
+def causal_conv(x, weight, bias=None, seq_off=None, n=None, state=None, final=None, silu: bool = True, out=None,
+                stream=None):
+    """All tokens of n sequences (reuse_ops_causal_conv).
+
+    x: [tokens][channels], weight: [channels][taps], bias: [channels] or None,
+    as for causal_conv_step; seq_off or n as for delta_forward.  state:
+    [n][taps - 1][channels] in x's dtype, the inputs before each sequence
+    (None: zeros); final: where the last ones go (made here if None; not
+    state).  Returns (out, final).
+    """
+    if stream is not None:
+        with _on(stream, x):
+            return causal_conv(x, weight, bias, seq_off, n, state, final, silu, out)
+    _no_grad(x, weight, bias, state)
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a tensor of shape (tokens, channels)")
+    n, off = _sequences(seq_off, n, x.shape[0], x.device)
+    shape, taps, xp, w, b, dev = _conv_shape(x, weight, bias, n, silu)
+    dims = (n, taps - 1, x.shape[1])
+    sp = _opt(state, "state", x.dtype, dev, dims)
+    if final is None:
+        final = _empty(x, dims, x.dtype)
+    fp = _like(final, "final", x.dtype, dev, dims)
+    if out is None:
+        out = _empty(x)
+    op = _like(out, "out", x.dtype, dev, x.shape)
+    _launch(dev, load_ops().reuse_ops_causal_conv, ctypes.byref(shape), xp, w, b, off, sp, fp, op)
+    return out, final
+
+
+def causal_conv_backward(dout, x, weight, bias=None, seq_off=None, n=None, state=None, dfinal=None, silu: bool = True,
+                         want_dstate: bool = True, stream=None):
+    """Gradients (dx, dweight, dbias, dstate) of causal_conv (reuse_ops_causal_conv_backward).
+
+    The inputs are the forward call's; dout: dJ/dout, dfinal: dJ/dfinal in x's
+    dtype or None.  dstate is None without want_dstate.
+    """
+    if stream is not None:
+        with _on(stream, x):
+            return causal_conv_backward(dout, x, weight, bias, seq_off, n, state, dfinal, silu, want_dstate)
+    _no_grad(dout, x, weight, bias, state, dfinal)
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a tensor of shape (tokens, channels)")
+    n, off = _sequences(seq_off, n, x.shape[0], x.device)
+    shape, taps, xp, w, b, dev = _conv_shape(x, weight, bias, n, silu)
+    dims = (n, taps - 1, x.shape[1])
+    sp = _opt(state, "state", x.dtype, dev, dims)
+    do = _like(dout, "dout", x.dtype, dev, x.shape)
+    df = _opt(dfinal, "dfinal", x.dtype, dev, dims)
+    L = load_ops()
+    need = L.reuse_ops_causal_conv_backward_scratch_bytes(ctypes.byref(shape))
+    dx, dw, db = _empty(x), _empty(weight), _empty(x, x.shape[1], _F32)
+    dstate = _empty(x, dims, x.dtype) if want_dstate else None
+    scratch = _empty(x, need, torch.uint8)
+    _launch(dev, L.reuse_ops_causal_conv_backward, ctypes.byref(shape), xp, w, b, off, sp, do, df, dx.data_ptr(),
+            dw.data_ptr(), db.data_ptr(), None if dstate is None else dstate.data_ptr(), scratch.data_ptr(), need)
+    return dx, dw, db, dstate

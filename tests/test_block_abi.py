@@ -158,3 +158,91 @@ def test_log_probs_tensors(calls):
         with pytest.raises(ValueError, match="requires grad"):
             ops.log_probs_backward(*some)
     assert not calls
+
+
+# ------------------------------------------------------------------ short convolution
+
+def _conv(n=2, channels=8, taps=4, tokens=10, dtype=B.RN_F32, silu=1, stride=8):
+    return ops.rn_conv_shape(n, channels, taps, tokens, dtype, silu, stride)
+
+
+def test_causal_conv_arguments():
+    L, ref = ops.load_ops(), ops.ctypes.byref
+    bad = ((dict(n=-1), "n must"), (dict(n=65536), "n must"), (dict(channels=0), "channels"), (dict(channels=65537), "channels"),
+           (dict(taps=0), "taps"), (dict(taps=5), "taps"), (dict(tokens=-1), "tokens"), (dict(tokens=1 << 31), "tokens"),
+           (dict(n=0), "without sequences"), (dict(dtype=B.RN_U8), "dtype"), (dict(stride=7), "stride"), (dict(stride=1 << 23), "2^23"))
+    s = _conv()
+    need = L.reuse_ops_causal_conv_backward_scratch_bytes(ref(s))
+    assert need >= 8 * 5 * 4 and need % 256 == 0
+    fwd = _caller(L.reuse_ops_causal_conv, shape=ref(s), x=P, w=P, b=None, off=P, window=2 * P, final=3 * P, out=4 * P, stream=None)
+    back = _caller(L.reuse_ops_causal_conv_backward, shape=ref(s), x=P, w=P, b=None, off=P, window=2 * P, dout=3 * P, dfinal=4 * P,
+                   dx=5 * P, dw=P, db=P, dwindow=6 * P, scratch=P, bytes=need, stream=None)
+    one = _conv(tokens=2)
+    step = _caller(L.reuse_ops_causal_conv_step, shape=ref(one), x=P, w=P, b=None, ids=None, slots=2, window=2 * P, out=3 * P,
+                   stream=None)
+    for kw, text in bad:
+        t = _conv(**kw)
+        assert L.reuse_ops_causal_conv_backward_scratch_bytes(ref(t)) == 0
+        for call in (fwd, back, step):
+            _err(call(shape=ref(t)), B.RN_EINVAL, text)
+    for call in (fwd, back, step):
+        _err(call(shape=None), B.RN_EINVAL, "shape")
+    for call in (fwd, back):
+        t = _conv(n=3)
+        _err(call(shape=ref(t), off=None), B.RN_EINVAL, "multiple")
+    for name in ("x", "w", "out"):
+        _err(fwd(**{name: None}), B.RN_EINVAL, "NULL")
+    _err(fwd(out=P), B.RN_EINVAL, "out must not be x")
+    _err(fwd(final=2 * P), B.RN_EINVAL, "first ones")
+    for name in ("x", "w", "dout", "dx", "dw", "db", "scratch"):
+        _err(back(**{name: None}), B.RN_EINVAL, "NULL")
+    _err(back(dx=P), B.RN_EINVAL, "neither")
+    _err(back(dx=3 * P), B.RN_EINVAL, "neither")
+    _err(back(dwindow=4 * P), B.RN_EINVAL, "neither")
+    _err(back(scratch=P + 8), B.RN_EINVAL, "aligned")
+    _err(back(bytes=need - 1), B.RN_ENOSPACE, "need")
+    _err(step(shape=ref(s)), B.RN_EINVAL, "one token a stream")
+    _err(step(slots=1), B.RN_EINVAL, "slots")
+    _err(step(slots=-1, ids=P), B.RN_EINVAL, "slots")
+    for name in ("x", "w", "window", "out"):
+        _err(step(**{name: None}), B.RN_EINVAL, "NULL")
+    wide = _conv(tokens=2, stride=9)
+    _err(step(shape=ref(wide), out=P), B.RN_EINVAL, "not contiguous")
+    _err(step(out=2 * P), B.RN_EINVAL, "two arrays")
+    none = _conv(n=0, tokens=0)
+    assert fwd(shape=ref(none)) == step(shape=ref(none), slots=0) == B.RN_OK
+
+
+def test_causal_conv_tensors(calls):
+    x, w, b, s = torch.zeros(6, 8), torch.zeros(8, 4), torch.zeros(8), torch.zeros(2, 3, 8)
+    off = torch.tensor([0, 2, 6], dtype=torch.int32)
+    out, final = ops.causal_conv(x, w, b, off, state=s)
+    assert out.shape == (6, 8) and final.shape == (2, 3, 8)
+    assert [tuple(g.shape) for g in ops.causal_conv_backward(out, x, w, b, off, state=s)] == [(6, 8), (8, 4), (8,), (2, 3, 8)]
+    assert ops.causal_conv_step(x[:2], w, s, b).shape == (2, 8)
+    calls.clear()
+    for bad, args, kw in ((ValueError, (x[0], w), dict(n=1)), (ValueError, (x, w[:7]), dict(n=1)), (ValueError, (x, b), dict(n=1)),
+                          (ValueError, (x, torch.zeros(8, 5)), dict(n=1)), (TypeError, (x, w.double()), dict(n=1)),
+                          (ValueError, (x, w, b[:3]), dict(n=1)), (ValueError, (x, w), {}), (ValueError, (x, w), dict(n=4)),
+                          (ValueError, (x, w, b, off), dict(state=s[:1])), (TypeError, (x, w, b, off), dict(state=s.bfloat16())),
+                          (ValueError, (x, w, b, off), dict(final=s[:, :2])), (ValueError, (x, w, b, off), dict(out=x[:5])),
+                          (TypeError, (x, w, b, off.long()), {}), (ValueError, (torch.zeros(8, 6).t(), w), dict(n=1))):
+        with pytest.raises(bad):
+            ops.causal_conv(*args, **kw)
+    for bad, kw in ((ValueError, dict(state=s[:1])), (ValueError, dict(state=s[:, :2].contiguous())),
+                    (TypeError, dict(state=s, stream_ids=off.long())), (ValueError, dict(state=s, out=x))):
+        with pytest.raises(bad):
+            ops.causal_conv_step(x[:2], w, **kw)
+    with pytest.raises(ValueError, match="dout|shape"):
+        ops.causal_conv_backward(out[:3], x, w, b, off)
+    with pytest.raises(TypeError, match="dfinal"):
+        ops.causal_conv_backward(out, x, w, b, off, dfinal=s.bfloat16())
+    for call, args in ((ops.causal_conv, [x, w, b, off, None, s]), (ops.causal_conv_backward, [out, x, w, b, off, None, s, s]),
+                       (ops.causal_conv_step, [x[:2], w, s, b])):
+        for i, t in enumerate(args):
+            if isinstance(t, torch.Tensor) and t.is_floating_point():
+                some = list(args)
+                some[i] = t.clone().requires_grad_()
+                with pytest.raises(ValueError, match="requires grad"):
+                    call(*some)
+    assert not calls
