@@ -2,7 +2,8 @@
  * reuse_ops — operators around a policy net on MI355X (gfx950): layer norm, the
  * gated delta rule (a memory per stream that is carried from frame to frame), the
  * sampling of actions, the norm of a residual stream, the log-probabilities a
- * policy is trained on, and a short convolution over a stream's last tokens, in the
+ * policy is trained on, a short convolution over a stream's last tokens and the
+ * selective scan (a memory that decays by an amount of each token's own), in the
  * library of reuse_net.h.
  *
  * A policy over many streams of frames (Sec. 1: multiple input frames; Sec. 2:
@@ -355,6 +356,91 @@ rn_status reuse_ops_causal_conv_backward(const rn_conv_shape *shape, const void 
                                          const void *dev_dout, const void *dev_dfinal, void *dev_dx,
                                          float *dev_dweight, float *dev_dbias, void *dev_dwindow, void *dev_scratch,
                                          size_t scratch_bytes, void *hip_stream);
+
+/* ---- selective scan ----
+ *
+ * A channel c carries a state of `states` numbers h.  For each token, with its input
+ * u, its step size and, of the channel's group, b and c:
+ *   s = softplus(dt + dt_bias), or dt + dt_bias,
+ *   h_i <- exp(s a_i) h_i + s b_i u,
+ *   y = sum_i c_i h_i + d u,  out = y z / (1 + exp(-z)), or y without z.
+ * Group g has channels g channels / groups and on.  With a <= 0 the states stay
+ * bounded.  s = 0 leaves the state as it is.
+ *
+ * Values that are not finite reach what the rule makes of them, as NaN or infinity,
+ * and nothing else: u, dt and z of a channel that channel's out, and u and dt its
+ * state, from that token on; b and c those of all channels of the group.  A value
+ * in one sequence reaches no other's results; dA, dD and the bias' gradient, which
+ * are sums over all tokens, it does reach.
+ */
+
+#define RN_SCAN_MAX_STATES 64
+#define RN_SCAN_KEEP 16
+
+typedef struct {
+    int32_t n;                    /* sequences (streams), 0..65535 */
+    int32_t channels, groups;     /* channels 1..65536, a multiple of groups */
+    int32_t states;               /* 1..RN_SCAN_MAX_STATES */
+    int64_t tokens;               /* tokens of all sequences, 0..2^31 - 1 */
+    rn_dtype dtype;               /* of u, dt, b, c, z and out */
+    int32_t softplus;             /* not 0: s = softplus(dt + dt_bias) */
+    /* Elements from a token to the next, below 2^23 (z_stride: not used without z).
+     * Within a token elements are contiguous (u, dt, z: [channels], b, c:
+     * [groups][states]). */
+    int64_t u_stride, dt_stride, b_stride, c_stride, z_stride;
+} rn_scan_shape;
+
+/* What a scan reads beside the shape. */
+typedef struct {
+    const void *u, *dt, *b, *c;
+    const float *a;               /* [channels][states] */
+    const float *d;               /* [channels], or NULL for 0 */
+    const void *z;                /* or NULL: out = y */
+    const float *dt_bias;         /* [channels], or NULL for 0 */
+} rn_scan_inputs;
+
+/* One token for each of n streams (tokens = n), the states updated in place.
+ *   dev_state:      [slots][channels][states] float32.
+ *   dev_stream_ids: [n] distinct slots, or NULL for 0..n-1.  A stream whose id is
+ *                   outside 0..slots-1 is left out and its out is 0.
+ *   dev_out:        [n][channels] dtype, contiguous; may be u itself where that is. */
+rn_status reuse_ops_scan_step(const rn_scan_shape *shape, const rn_scan_inputs *in, const int32_t *dev_stream_ids,
+                              int32_t slots, float *dev_state, void *dev_out, void *hip_stream);
+
+/* Bytes of the buffer a forward call leaves for the backward call (a state per
+ * RN_SCAN_KEEP tokens and sequence), and of the scratch each call needs (0 if the
+ * shape is not supported; every size is at least 256). */
+size_t reuse_ops_scan_saved_bytes(const rn_scan_shape *shape);
+size_t reuse_ops_scan_scratch_bytes(const rn_scan_shape *shape);
+size_t reuse_ops_scan_backward_scratch_bytes(const rn_scan_shape *shape);
+
+/* All tokens of n sequences packed one after another, as reuse_ops_delta_forward's.
+ *   dev_seq_off: [n+1] int32, or NULL: every sequence has tokens / n.
+ *   dev_state:   [n][channels][states] float32 before the first token, or NULL for 0.
+ *   dev_final:   the same after the last token, or NULL; it may be dev_state.
+ *   dev_out:     [tokens][channels] dtype, contiguous.
+ *   dev_saved:   NULL, or reuse_ops_scan_saved_bytes bytes for the backward call.
+ *   dev_scratch: reuse_ops_scan_scratch_bytes bytes; saved and scratch are 256-byte
+ *                aligned. */
+rn_status reuse_ops_scan_forward(const rn_scan_shape *shape, const rn_scan_inputs *in, const int32_t *dev_seq_off,
+                                 const float *dev_state, float *dev_final, void *dev_out, void *dev_saved,
+                                 size_t saved_bytes, void *dev_scratch, size_t scratch_bytes, void *hip_stream);
+
+/* Where a backward call's gradients go: like what they are the gradients of, but
+ * contiguous.  dz, dd, ddt_bias and dstate may be NULL (not wanted); dz is NULL
+ * without z. */
+typedef struct {
+    void *du, *ddt, *db, *dc, *dz;
+    float *da, *dd, *ddt_bias, *dstate;
+} rn_scan_grads;
+
+/* Gradients of J given dout = dJ/dout ([tokens][channels] dtype, contiguous) and
+ * dfinal = dJ/dfinal (NULL: 0), for the inputs and the saved buffer of a forward
+ * call.  dstate must not be dfinal. */
+rn_status reuse_ops_scan_backward(const rn_scan_shape *shape, const rn_scan_inputs *in, const int32_t *dev_seq_off,
+                                  const void *dev_saved, size_t saved_bytes, const void *dev_dout,
+                                  const float *dev_dfinal, const rn_scan_grads *grads, void *dev_scratch,
+                                  size_t scratch_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

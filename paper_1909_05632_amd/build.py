@@ -15,8 +15,8 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libreuse_net.so")
 SOURCES = ["rn_host.hip", "rn_masks.hip", "rn_conv.hip", "rn_conv_split.hip", "rn_conv_bf16.hip", "rn_head.hip", "rn_train.hip",
-           "rn_ops_host.hip", "rn_norm.hip", "rn_rms.hip", "rn_sample.hip", "rn_logp.hip", "rn_sconv.hip", "rn_delta.hip",
-           "rn_delta_short.hip", "rn_delta_bwd.hip"]
+           "rn_ops_host.hip", "rn_norm.hip", "rn_rms.hip", "rn_sample.hip", "rn_logp.hip", "rn_sconv.hip", "rn_scan.hip",
+           "rn_scan_bwd.hip", "rn_delta.hip", "rn_delta_short.hip", "rn_delta_bwd.hip"]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++20", f"--offload-arch={ARCH}", "-fPIC", "-Wall",

@@ -1,6 +1,7 @@
 // Internal declarations of the operators in include/reuse_ops.h: kernel
 // launchers (rn_norm.hip, rn_rms.hip, rn_sample.hip, rn_logp.hip,
-// rn_sconv.hip, rn_delta.hip, rn_delta_short.hip, rn_delta_bwd.hip) and device helpers they share.
+// rn_sconv.hip, rn_scan.hip, rn_scan_bwd.hip, rn_delta.hip, rn_delta_short.hip,
+// rn_delta_bwd.hip) and device helpers they share.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -109,6 +110,50 @@ int64_t causal_parts(int64_t tokens);
 hipError_t launch_causal(const CausalArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_causal_backward(const CausalArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_causal_step(const CausalArgs &a, bool bf16, hipStream_t s);
+
+struct ScanArgs {
+    int n, channels, groups, states, softplus;
+    int64_t tokens;
+    const void *u, *dt, *b, *c, *z;        // z may be NULL
+    int64_t us, dts, bs, cs, zs;
+    const float *a, *d, *dt_bias;          // d and dt_bias may be NULL
+    const int32_t *off;           // [n+1], or NULL: even lengths
+    const int32_t *ids;           // step: slots, or NULL
+    int slots;
+    const float *state;           // first states, or NULL
+    float *final_state;           // last states, or NULL (step: the states' pool)
+    void *out;
+    float *kept;                  // [scan_kept_slots][channels][states] states before every tile, or NULL
+    bool quads, whole_states;     // vectors of four channels, and of four states, are on their size
+    int64_t blocks;               // over the channels (scan_blocks)
+    int64_t chunk, chunks;        // tokens of a chunk, slots of chunks: tokens / chunk + n
+    bool parts;                   // sequences may have several chunks
+    float *ends;                  // [scan_ends][channels][states] states chunks end with from 0, then begin with
+    float *sums;                  // [scan_ends][channels] summed step sizes
+    // Backward call:
+    const void *dout;
+    const float *dfinal;
+    void *du, *ddt, *db, *dc, *dz;         // dz may be NULL
+    float *da, *dd, *ddt_bias, *dstate;    // all but da may be NULL
+    int64_t walkers;              // blocks over the chunks (scan_walkers)
+    float *part_bc;               // [blocks][tokens][2][states]
+    float *part_a, *part_d;       // [walkers][channels][states], [walkers][2][channels]
+};
+// The kept state of tile k of sequence i, which begins at token `begin`, is at this + k.
+__host__ __device__ inline int64_t scan_kept_slot(int begin, int i) { return begin / RN_SCAN_KEEP + i; }
+inline int64_t scan_kept_slots(int64_t tokens, int n) { return tokens / RN_SCAN_KEEP + n; }
+// Chunk c of a sequence of several has slot scan_end_slot + c: of more than `chunk`
+// tokens it moves begin / (chunk / 2) on by its chunks at least.
+__host__ __device__ inline int64_t scan_end_slot(const ScanArgs &a, int begin) { return begin / (a.chunk / 2); }
+inline int64_t scan_ends(int64_t tokens, int64_t chunk) { return tokens / (chunk / 2); }
+int scan_lanes(int states);
+int64_t scan_blocks(int channels, int groups, int states);
+int scan_chunk(int64_t tokens, int channels, int groups, int states);
+int64_t scan_walkers(int64_t chunks, int64_t blocks);
+hipError_t launch_scan(const ScanArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_scan_step(const ScanArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_scan_join_back(const ScanArgs &a, hipStream_t s);
+hipError_t launch_scan_backward(const ScanArgs &a, bool bf16, hipStream_t s);
 
 struct DeltaArgs {
     int n, hk, hv, dk, dv;

@@ -150,6 +150,87 @@ CausalArgs conv_args(const rn_conv_shape *s, const void *x, const float *weight,
     return a;
 }
 
+// ------------------------------------------------------------------ selective scan
+
+const char *bad_scan(const rn_scan_shape *s) {
+    if (!s) return "shape is NULL";
+    if (s->n < 0 || s->n > kMaxSequences) return "n must be 0..65535";
+    if (s->channels < 1 || s->channels > kMaxChannels || s->groups < 1 || s->channels % s->groups)
+        return "channels must be 1..65536 and a multiple of groups";
+    if (s->states < 1) return "states must be 1 or more";
+    if (s->tokens < 0 || s->tokens > INT32_MAX) return "tokens must be 0..2^31 - 1";
+    if (s->n == 0 && s->tokens > 0) return "tokens without sequences";
+    if (!known(s->dtype)) return "dtype must be RN_F32 or RN_BF16";
+    const int64_t bc = (int64_t)s->groups * s->states;
+    if (s->tokens > 1 && (s->u_stride < s->channels || s->dt_stride < s->channels || s->b_stride < bc || s->c_stride < bc))
+        return "a token stride is smaller than its token";
+    if (s->tokens > 1 && (s->u_stride >= kMaxStride || s->dt_stride >= kMaxStride || s->b_stride >= kMaxStride ||
+                          s->c_stride >= kMaxStride))
+        return "token strides must be below 2^23";
+    return nullptr;
+}
+
+bool too_many_states(const rn_scan_shape *s) { return s->states > RN_SCAN_MAX_STATES; }
+
+struct ScanSizes {
+    int64_t blocks, chunk, chunks, walkers;
+    size_t kept, ends, sums;              // bytes
+    size_t part_bc, part_a, part_d;
+};
+
+ScanSizes scan_sizes(const rn_scan_shape *s) {
+    ScanSizes z;
+    const size_t row = (size_t)s->channels * 4, states = row * s->states;
+    z.blocks = scan_blocks(s->channels, s->groups, s->states);
+    z.chunk = scan_chunk(s->tokens, s->channels, s->groups, s->states);
+    z.chunks = s->tokens / z.chunk + s->n;
+    z.walkers = scan_walkers(z.chunks, z.blocks);
+    z.kept = round_up(scan_kept_slots(s->tokens, s->n) * states);
+    const bool parts = s->tokens > z.chunk;
+    const size_t ends = parts ? scan_ends(s->tokens, z.chunk) : 0;
+    z.ends = round_up(ends * states), z.sums = round_up(ends * row);
+    z.part_bc = round_up((size_t)z.blocks * s->tokens * 2 * s->states * 4);
+    z.part_a = round_up(z.walkers * states), z.part_d = round_up(z.walkers * 2 * row);
+    return z;
+}
+
+size_t scan_bytes(const ScanSizes &z, bool backward) {
+    return z.ends + z.sums + (backward ? z.part_bc + z.part_a + z.part_d : 0) + kAlign;
+}
+
+// Vectors of four elements are on their size in every row of every array.
+bool on_quads(const rn_scan_shape *s, const void *p, int64_t stride) {
+    const int size = s->dtype == RN_BF16 ? 2 : 4;
+    return reinterpret_cast<uintptr_t>(p) % (4 * size) == 0 && stride % 4 == 0;
+}
+bool on_16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+rn_status check_scan(const rn_scan_shape *s, const rn_scan_inputs *in) {
+    if (const char *why = bad_scan(s)) return fail(RN_EINVAL, why);
+    if (too_many_states(s)) return fail(RN_EUNSUPPORTED, "states above 64 have no kernel");
+    if (!in) return fail(RN_EINVAL, "the inputs are NULL");
+    if (s->tokens > 0 && (!in->u || !in->dt || !in->b || !in->c)) return fail(RN_EINVAL, "u, dt, b and c must not be NULL");
+    if (!in->a) return fail(RN_EINVAL, "a must not be NULL");
+    if (in->z && s->tokens > 1 && s->z_stride < s->channels) return fail(RN_EINVAL, "a token stride is smaller than its token");
+    if (in->z && s->tokens > 1 && s->z_stride >= kMaxStride) return fail(RN_EINVAL, "token strides must be below 2^23");
+    return RN_OK;
+}
+
+ScanArgs scan_args(const rn_scan_shape *s, const rn_scan_inputs *in, const int32_t *seq_off, const ScanSizes &z) {
+    ScanArgs a{};
+    a.n = s->n, a.channels = s->channels, a.groups = s->groups, a.states = s->states, a.softplus = s->softplus;
+    a.tokens = s->tokens;
+    a.u = in->u, a.dt = in->dt, a.b = in->b, a.c = in->c, a.z = in->z;
+    a.us = s->u_stride, a.dts = s->dt_stride, a.bs = s->b_stride, a.cs = s->c_stride, a.zs = in->z ? s->z_stride : 0;
+    a.a = in->a, a.d = in->d, a.dt_bias = in->dt_bias;
+    a.off = seq_off;
+    a.quads = s->channels / s->groups % 4 == 0 && on_quads(s, a.u, a.us) && on_quads(s, a.dt, a.dts) && on_quads(s, a.z, a.zs);
+    a.whole_states = s->states % 4 == 0 && on_16(a.a);
+    a.blocks = z.blocks, a.chunk = z.chunk, a.chunks = z.chunks, a.walkers = z.walkers;
+    a.parts = (seq_off || s->n == 0 ? s->tokens : s->tokens / s->n) > z.chunk;
+    return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -398,6 +479,95 @@ rn_status reuse_ops_causal_conv_backward(const rn_conv_shape *shape, const void 
     a.dout = dout, a.dfinal = dfinal, a.dx = dx, a.dwindow = dwindow, a.dweight = dweight, a.dbias = dbias;
     a.part = static_cast<float *>(scratch);
     return launched(launch_causal_backward(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
+}
+
+rn_status reuse_ops_scan_step(const rn_scan_shape *shape, const rn_scan_inputs *in, const int32_t *ids, int32_t slots,
+                              float *state, void *out, void *stream) {
+    if (rn_status s = check_scan(shape, in)) return s;
+    if (shape->tokens != shape->n) return fail(RN_EINVAL, "a step takes one token a stream: tokens must be n");
+    if (slots < 0 || (!ids && slots < shape->n)) return fail(RN_EINVAL, "fewer slots than streams");
+    if (shape->n == 0) return RN_OK;
+    if (!state || !out) return fail(RN_EINVAL, "state and out must not be NULL");
+    if (shape->n > 1 && out == in->u && shape->u_stride != shape->channels)
+        return fail(RN_EINVAL, "a result lies over an input that is not contiguous");
+    ScanArgs a = scan_args(shape, in, nullptr, scan_sizes(shape));
+    a.whole_states = a.whole_states && on_16(state);
+    a.ids = ids, a.slots = slots, a.final_state = state, a.out = out;
+    return launched(launch_scan_step(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
+}
+
+size_t reuse_ops_scan_saved_bytes(const rn_scan_shape *shape) {
+    if (bad_scan(shape) || too_many_states(shape)) return 0;
+    return scan_sizes(shape).kept + kAlign;
+}
+
+size_t reuse_ops_scan_scratch_bytes(const rn_scan_shape *shape) {
+    if (bad_scan(shape) || too_many_states(shape)) return 0;
+    return scan_bytes(scan_sizes(shape), false);
+}
+
+size_t reuse_ops_scan_backward_scratch_bytes(const rn_scan_shape *shape) {
+    if (bad_scan(shape) || too_many_states(shape)) return 0;
+    return scan_bytes(scan_sizes(shape), true);
+}
+
+rn_status reuse_ops_scan_forward(const rn_scan_shape *shape, const rn_scan_inputs *in, const int32_t *seq_off,
+                                 const float *state, float *final_state, void *out, void *saved, size_t saved_bytes,
+                                 void *scratch, size_t scratch_bytes, void *stream) {
+    if (rn_status s = check_scan(shape, in)) return s;
+    if (!seq_off && shape->n > 0 && shape->tokens % shape->n)
+        return fail(RN_EINVAL, "without seq_off, tokens must be a multiple of n");
+    if (shape->n == 0) return RN_OK;
+    if (shape->tokens > 0 && !out) return fail(RN_EINVAL, "out must not be NULL");
+    if (misaligned(saved) || misaligned(scratch)) return fail(RN_EINVAL, "saved and scratch must be 256-byte aligned");
+    const ScanSizes z = scan_sizes(shape);
+    if (saved && saved_bytes < z.kept + kAlign) return need_bytes("saved", z.kept + kAlign);
+    if (!scratch) return fail(RN_EINVAL, "scratch is NULL");
+    const size_t need = scan_bytes(z, false);
+    if (scratch_bytes < need) return need_bytes("scratch", need);
+    ScanArgs a = scan_args(shape, in, seq_off, z);
+    a.quads = a.quads && on_quads(shape, out, 0);
+    a.whole_states = a.whole_states && on_16(state) && on_16(final_state);
+    a.state = state, a.final_state = final_state, a.out = out, a.kept = static_cast<float *>(saved);
+    char *at = static_cast<char *>(scratch);
+    a.ends = reinterpret_cast<float *>(at), a.sums = reinterpret_cast<float *>(at + z.ends);
+    return launched(launch_scan(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
+}
+
+rn_status reuse_ops_scan_backward(const rn_scan_shape *shape, const rn_scan_inputs *in, const int32_t *seq_off,
+                                  const void *saved, size_t saved_bytes, const void *dout, const float *dfinal,
+                                  const rn_scan_grads *grads, void *scratch, size_t scratch_bytes, void *stream) {
+    if (rn_status s = check_scan(shape, in)) return s;
+    if (!seq_off && shape->n > 0 && shape->tokens % shape->n)
+        return fail(RN_EINVAL, "without seq_off, tokens must be a multiple of n");
+    if (!grads) return fail(RN_EINVAL, "the gradients are NULL");
+    if (shape->tokens > 0 && (!dout || !grads->du || !grads->ddt || !grads->db || !grads->dc))
+        return fail(RN_EINVAL, "dout and the gradients of u, dt, b and c must not be NULL");
+    if (!grads->da) return fail(RN_EINVAL, "da must not be NULL");
+    if (grads->dz && !in->z) return fail(RN_EINVAL, "dz without z");
+    if (grads->dstate && grads->dstate == dfinal) return fail(RN_EINVAL, "dstate must not be dfinal");
+    if (!saved || !scratch) return fail(RN_EINVAL, "saved and scratch must not be NULL");
+    if (misaligned(saved) || misaligned(scratch)) return fail(RN_EINVAL, "saved and scratch must be 256-byte aligned");
+    const ScanSizes z = scan_sizes(shape);
+    if (saved_bytes < z.kept + kAlign) return need_bytes("saved", z.kept + kAlign);
+    const size_t need = scan_bytes(z, true);
+    if (scratch_bytes < need) return need_bytes("scratch", need);
+    ScanArgs a = scan_args(shape, in, seq_off, z);
+    for (const void *p : {dout, static_cast<const void *>(grads->du), static_cast<const void *>(grads->ddt),
+                          static_cast<const void *>(grads->dz)})
+        a.quads = a.quads && on_quads(shape, p, 0);
+    a.whole_states = a.whole_states && on_16(dfinal) && on_16(grads->dstate);
+    a.kept = static_cast<float *>(const_cast<void *>(saved));
+    a.dout = dout, a.dfinal = dfinal;
+    a.du = grads->du, a.ddt = grads->ddt, a.db = grads->db, a.dc = grads->dc, a.dz = grads->dz;
+    a.da = grads->da, a.dd = grads->dd, a.ddt_bias = grads->ddt_bias, a.dstate = grads->dstate;
+    char *at = static_cast<char *>(scratch);
+    a.ends = reinterpret_cast<float *>(at);
+    a.sums = reinterpret_cast<float *>(at += z.ends);
+    a.part_bc = reinterpret_cast<float *>(at += z.sums);
+    a.part_a = reinterpret_cast<float *>(at += z.part_bc);
+    a.part_d = reinterpret_cast<float *>(at += z.part_a);
+    return launched(launch_scan_backward(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
 }
 
 rn_status reuse_ops_delta_step(const rn_delta_shape *shape, const void *q, const void *k, const void *v,

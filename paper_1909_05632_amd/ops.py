@@ -40,6 +40,7 @@ from . import binding as B
 RN_SAMPLE_MAX_VOCAB = 1 << 20
 RN_LOGPROBS_MAX_TOP = 64
 RN_CONV_MAX_TAPS = 4
+RN_SCAN_MAX_STATES = 64
 RN_DELTA_MAX_DIM = 128
 
 # Every entry point include/reuse_ops.h declares.
@@ -50,7 +51,9 @@ EXPORTS = (
     "reuse_ops_delta_backward", "reuse_ops_rms_norm", "reuse_ops_rms_norm_backward_scratch_bytes",
     "reuse_ops_rms_norm_backward", "reuse_ops_log_probs_scratch_bytes", "reuse_ops_log_probs",
     "reuse_ops_log_probs_backward", "reuse_ops_causal_conv_step", "reuse_ops_causal_conv",
-    "reuse_ops_causal_conv_backward_scratch_bytes", "reuse_ops_causal_conv_backward",
+    "reuse_ops_causal_conv_backward_scratch_bytes", "reuse_ops_causal_conv_backward", "reuse_ops_scan_step",
+    "reuse_ops_scan_saved_bytes", "reuse_ops_scan_scratch_bytes", "reuse_ops_scan_backward_scratch_bytes",
+    "reuse_ops_scan_forward", "reuse_ops_scan_backward",
 )
 
 
@@ -73,6 +76,21 @@ class rn_conv_shape(ctypes.Structure):
                 ("x_stride", ctypes.c_int64)]
 
 
+class rn_scan_shape(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("channels", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("states", ctypes.c_int32), ("tokens", ctypes.c_int64), ("dtype", ctypes.c_int),
+                ("softplus", ctypes.c_int32), ("u_stride", ctypes.c_int64), ("dt_stride", ctypes.c_int64),
+                ("b_stride", ctypes.c_int64), ("c_stride", ctypes.c_int64), ("z_stride", ctypes.c_int64)]
+
+
+class rn_scan_inputs(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("u", "dt", "b", "c", "a", "d", "z", "dt_bias")]
+
+
+class rn_scan_grads(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("du", "ddt", "db", "dc", "dz", "da", "dd", "ddt_bias", "dstate")]
+
+
 _ops = None
 
 
@@ -85,6 +103,7 @@ def load_ops():
     P, I32, I64, SZ, F, st = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float,
                               ctypes.c_int)
     shape, conv = ctypes.POINTER(rn_delta_shape), ctypes.POINTER(rn_conv_shape)
+    scan, given = ctypes.POINTER(rn_scan_shape), ctypes.POINTER(rn_scan_inputs)
     for name, res, args in (
             ("last_error", ctypes.c_char_p, []),
             ("layer_norm", st, [I64, I32, P, I64, st, P, P, F, P, I64, P, P]),
@@ -101,6 +120,12 @@ def load_ops():
             ("causal_conv", st, [conv, P, P, P, P, P, P, P, P]),
             ("causal_conv_backward_scratch_bytes", SZ, [conv]),
             ("causal_conv_backward", st, [conv, P, P, P, P, P, P, P, P, P, P, P, P, SZ, P]),
+            ("scan_step", st, [scan, given, P, I32, P, P, P]),
+            ("scan_saved_bytes", SZ, [scan]),
+            ("scan_scratch_bytes", SZ, [scan]),
+            ("scan_backward_scratch_bytes", SZ, [scan]),
+            ("scan_forward", st, [scan, given, P, P, P, P, P, SZ, P, SZ, P]),
+            ("scan_backward", st, [scan, given, P, P, SZ, P, P, ctypes.POINTER(rn_scan_grads), P, SZ, P]),
             ("delta_step", st, [shape, P, P, P, P, P, P, I32, P, P, P]),
             ("delta_saved_bytes", SZ, [shape]),
             ("delta_scratch_bytes", SZ, [shape]),
@@ -808,3 +833,135 @@ def causal_conv_backward(dout, x, weight, bias=None, seq_off=None, n=None, state
     _launch(dev, L.reuse_ops_causal_conv_backward, ctypes.byref(shape), xp, w, b, off, sp, do, df, dx.data_ptr(),
             dw.data_ptr(), db.data_ptr(), None if dstate is None else dstate.data_ptr(), scratch.data_ptr(), need)
     return dx, dw, db, dstate
+
+
+# ------------------------------------------------------------------ selective scan
+
+def _scan_shape(u, dt, a, b, c, d, z, dt_bias, softplus, n: int):
+    """(shape, inputs, channels, states, device) of a scan's checked arguments."""
+    code = _data(u, "u")
+    if u.dim() != 2 or u.shape[1] < 1:
+        raise ValueError(f"u must have shape (tokens, channels), got {tuple(u.shape)}")
+    tokens, channels = u.shape
+    dev, dtype = u.device, u.dtype
+    up, us = _flat(u, "u", dtype, tokens, channels, dev)
+    dtp, dts = _flat(dt, "dt", dtype, tokens, channels, dev)
+    zp, zs = (None, 0) if z is None else _flat(z, "z", dtype, tokens, channels, dev)
+    groups, states, bs = _tokens(b, "b", dtype, tokens, dev)
+    if channels % groups:
+        raise ValueError(f"{channels} channels cannot share {groups} groups")
+    if _tokens(c, "c", dtype, tokens, dev)[:2] != (groups, states):
+        raise ValueError("c must have b's shape")
+    cs = _tokens(c, "c", dtype, tokens, dev)[2]
+    _count(max(channels, states, n), "channels, states and n")
+    inputs = rn_scan_inputs(up, dtp, b.data_ptr(), c.data_ptr(), _like(a, "a", _F32, dev, (channels, states)),
+                            _opt(d, "d", _F32, dev, (channels,)), zp, _opt(dt_bias, "dt_bias", _F32, dev, (channels,)))
+    return (rn_scan_shape(n, channels, groups, states, tokens, code, bool(softplus), us, dts, bs, cs, zs), inputs,
+            channels, states, dev)
+
+
+def scan_step(u, dt, a, b, c, state, d=None, z=None, dt_bias=None, softplus: bool = True, stream_ids=None, out=None,
+              stream=None):
+    """One token for each of n streams, their states updated in place (reuse_ops_scan_step).
+
+    u, dt, z: [n][channels], b, c: [n][groups][states] float32 or bfloat16; a:
+    [channels][states], d, dt_bias: [channels] float32; d, z and dt_bias may be
+    None.  state: [slots][channels][states] float32; stream_ids: [n] int32
+    distinct slots (None: 0..n-1).  Returns out [n][channels], which may be u.
+    """
+    if stream is not None:
+        with _on(stream, u):
+            return scan_step(u, dt, a, b, c, state, d, z, dt_bias, softplus, stream_ids, out)
+    _no_grad(u, dt, a, b, c, state, d, z, dt_bias)
+    n = u.shape[0] if isinstance(u, torch.Tensor) and u.dim() else 0
+    shape, inputs, channels, states, dev = _scan_shape(u, dt, a, b, c, d, z, dt_bias, softplus, n)
+    slots = state.shape[0] if isinstance(state, torch.Tensor) and state.dim() else 0
+    sp = _like(state, "state", _F32, dev, (_count(slots, "slots"), channels, states))
+    ids = _opt(stream_ids, "stream_ids", _I32, dev, (n,))
+    if ids is None and slots < n:
+        raise ValueError(f"{n} streams need as many slots, state has {slots}")
+    if out is None:
+        out = _empty(u)
+    op = _like(out, "out", u.dtype, dev, u.shape)
+    _launch(dev, load_ops().reuse_ops_scan_step, ctypes.byref(shape), ctypes.byref(inputs), ids, slots, sp, op)
+    return out
+
+
+def _scan_supported(need: int, shape) -> int:
+    if need == 0:                                  # re-run the call's own checks to report why
+        _check(load_ops().reuse_ops_scan_step(ctypes.byref(shape), None, None, 0, None, None, None))
+    return need
+
+
+def scan_forward(u, dt, a, b, c, d=None, z=None, dt_bias=None, softplus: bool = True, seq_off=None, n=None, state=None,
+                 final=None, save: bool = False, out=None, stream=None):
+    """All tokens of n sequences (reuse_ops_scan_forward).
+
+    The inputs as for scan_step, over tokens; seq_off or n as for
+    delta_forward.  state: [n][channels][states] float32 before each sequence
+    (None: zeros); final: where the last ones go (made here if None; it may be
+    state).  Returns (out, final), with save also the buffer that scan_backward
+    reads.
+    """
+    if stream is not None:
+        with _on(stream, u):
+            return scan_forward(u, dt, a, b, c, d, z, dt_bias, softplus, seq_off, n, state, final, save, out)
+    _no_grad(u, dt, a, b, c, d, z, dt_bias, state)
+    if not isinstance(u, torch.Tensor) or u.dim() != 2:
+        raise ValueError("u must be a tensor of shape (tokens, channels)")
+    n, off = _sequences(seq_off, n, u.shape[0], u.device)
+    shape, inputs, channels, states, dev = _scan_shape(u, dt, a, b, c, d, z, dt_bias, softplus, n)
+    dims = (n, channels, states)
+    sp = _opt(state, "state", _F32, dev, dims)
+    L = load_ops()
+    need = _scan_supported(L.reuse_ops_scan_scratch_bytes(ctypes.byref(shape)), shape)
+    if final is None:
+        final = _empty(u, dims, _F32)
+    fp = _like(final, "final", _F32, dev, dims)
+    if out is None:
+        out = _empty(u)
+    op = _like(out, "out", u.dtype, dev, u.shape)
+    scratch = _empty(u, need, torch.uint8)
+    saved, kept, size = None, None, 0
+    if save:
+        size = L.reuse_ops_scan_saved_bytes(ctypes.byref(shape))
+        saved = _empty(u, size, torch.uint8)
+        kept = saved.data_ptr()
+    _launch(dev, L.reuse_ops_scan_forward, ctypes.byref(shape), ctypes.byref(inputs), off, sp, fp, op, kept, size,
+            scratch.data_ptr(), need)
+    return (out, final, saved) if save else (out, final)
+
+
+def scan_backward(dout, u, dt, a, b, c, d=None, z=None, dt_bias=None, softplus: bool = True, seq_off=None, n=None,
+                  saved=None, dfinal=None, want_dstate: bool = True, stream=None):
+    """Gradients (du, ddt, da, db, dc, dd, dz, ddt_bias, dstate) of scan_forward (reuse_ops_scan_backward).
+
+    The inputs are the forward call's, saved its buffer; dout: dJ/dout, dfinal:
+    dJ/dfinal or None.  dd, dz and ddt_bias are None where d, z and dt_bias
+    are, dstate without want_dstate.
+    """
+    if stream is not None:
+        with _on(stream, u):
+            return scan_backward(dout, u, dt, a, b, c, d, z, dt_bias, softplus, seq_off, n, saved, dfinal, want_dstate)
+    _no_grad(dout, u, dt, a, b, c, d, z, dt_bias, dfinal)
+    if not isinstance(u, torch.Tensor) or u.dim() != 2:
+        raise ValueError("u must be a tensor of shape (tokens, channels)")
+    n, off = _sequences(seq_off, n, u.shape[0], u.device)
+    shape, inputs, channels, states, dev = _scan_shape(u, dt, a, b, c, d, z, dt_bias, softplus, n)
+    dims = (n, channels, states)
+    do = _like(dout, "dout", u.dtype, dev, u.shape)
+    df = _opt(dfinal, "dfinal", _F32, dev, dims)
+    L = load_ops()
+    need = _scan_supported(L.reuse_ops_scan_backward_scratch_bytes(ctypes.byref(shape)), shape)
+    if not isinstance(saved, torch.Tensor):
+        raise TypeError("saved must be the buffer of scan_forward(..., save=True)")
+    sp = _like(saved, "saved", torch.uint8, dev, (L.reuse_ops_scan_saved_bytes(ctypes.byref(shape)),))
+    du, ddt, da, db, dc = _empty(u), _empty(u), _empty(a), _empty(b), _empty(c)
+    dd, dz, dbias = (None if t is None else _empty(t) for t in (d, z, dt_bias))
+    dstate = _empty(u, dims, _F32) if want_dstate else None
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    grads = rn_scan_grads(*map(ptr, (du, ddt, db, dc, dz, da, dd, dbias, dstate)))
+    scratch = _empty(u, need, torch.uint8)
+    _launch(dev, L.reuse_ops_scan_backward, ctypes.byref(shape), ctypes.byref(inputs), off, sp, saved.numel(), do, df,
+            ctypes.byref(grads), scratch.data_ptr(), need)
+    return du, ddt, da, db, dc, dd, dz, dbias, dstate

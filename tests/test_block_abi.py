@@ -246,3 +246,126 @@ def test_causal_conv_tensors(calls):
                 with pytest.raises(ValueError, match="requires grad"):
                     call(*some)
     assert not calls
+
+
+# ------------------------------------------------------------------ selective scan
+
+def _scan(n=2, channels=8, groups=2, states=4, tokens=10, dtype=B.RN_F32, softplus=1, u=8, dt=8, b=8, c=8, z=8):
+    return ops.rn_scan_shape(n, channels, groups, states, tokens, dtype, softplus, u, dt, b, c, z)
+
+
+def test_scan_arguments():
+    L, ref = ops.load_ops(), ops.ctypes.byref
+    sizes = (L.reuse_ops_scan_saved_bytes, L.reuse_ops_scan_scratch_bytes, L.reuse_ops_scan_backward_scratch_bytes)
+    s, one, none = _scan(), _scan(tokens=2), _scan(n=0, tokens=0)
+    given = {k: P for k in ("u", "dt", "b", "c", "a", "d", "z", "dt_bias")}
+    into = {k: P for k in ("du", "ddt", "db", "dc", "dz", "da", "dd", "ddt_bias", "dstate")}
+    inputs = lambda **kw: ref(ops.rn_scan_inputs(**{**given, **kw}))  # noqa: E731
+    grads = lambda **kw: ref(ops.rn_scan_grads(**{**into, **kw}))  # noqa: E731
+    saved, fwd_bytes, bwd_bytes = (f(ref(s)) for f in sizes)
+    assert all(x >= 256 and x % 256 == 0 for x in (saved, fwd_bytes, bwd_bytes)) and saved >= 2 * 8 * 4 * 4
+    fwd = _caller(L.reuse_ops_scan_forward, shape=ref(s), given=inputs(), off=P, state=None, final=None, out=P, saved=None,
+                  saved_bytes=0, scratch=P, bytes=fwd_bytes, stream=None)
+    back = _caller(L.reuse_ops_scan_backward, shape=ref(s), given=inputs(), off=P, saved=P, saved_bytes=saved, dout=P, dfinal=None,
+                   grads=grads(), scratch=P, bytes=bwd_bytes, stream=None)
+    step = _caller(L.reuse_ops_scan_step, shape=ref(one), given=inputs(), ids=None, slots=2, state=P, out=2 * P, stream=None)
+    for kw, text in ((dict(n=-1), "n must"), (dict(n=65536), "n must"), (dict(channels=0), "channels"), (dict(groups=0), "channels"),
+                     (dict(channels=65538), "channels"), (dict(groups=3), "channels"), (dict(states=0), "states"),
+                     (dict(tokens=-1), "tokens"), (dict(tokens=1 << 31), "tokens"), (dict(n=0), "without sequences"),
+                     (dict(dtype=B.RN_U8), "dtype"), (dict(u=7), "stride"), (dict(dt=7), "stride"), (dict(b=7), "stride"),
+                     (dict(c=7), "stride"), (dict(u=1 << 23), "2^23"), (dict(b=1 << 23), "2^23")):
+        t = _scan(**kw)
+        assert all(f(ref(t)) == 0 for f in sizes), kw
+        for call in (fwd, back, step):
+            _err(call(shape=ref(t)), B.RN_EINVAL, text)
+    wide = _scan(states=65, b=130, c=130)
+    assert all(f(ref(wide)) == 0 for f in sizes) and all(f(None) == 0 for f in sizes)
+    for call in (fwd, back, step):
+        _err(call(shape=ref(wide)), B.RN_EUNSUPPORTED, "64")
+        _err(call(shape=None), B.RN_EINVAL, "shape")
+        _err(call(given=None), B.RN_EINVAL, "inputs")
+        for name in ("u", "dt", "b", "c", "a"):
+            _err(call(given=inputs(**{name: None})), B.RN_EINVAL, "NULL")
+        for t in (_scan(tokens=2, z=7), _scan(tokens=2, z=1 << 23)):
+            _err(call(shape=ref(t)), B.RN_EINVAL, "stride")
+    odd = _scan(n=3)
+    for call in (fwd, back):
+        _err(call(shape=ref(odd), off=None), B.RN_EINVAL, "multiple")
+        _err(call(scratch=None), B.RN_EINVAL, "scratch")
+        _err(call(scratch=P + 8), B.RN_EINVAL, "aligned")
+        _err(call(bytes=255), B.RN_ENOSPACE, "scratch")
+    _err(fwd(out=None), B.RN_EINVAL, "NULL")
+    _err(fwd(saved=P, saved_bytes=saved - 1), B.RN_ENOSPACE, "saved")
+    for name in ("du", "ddt", "db", "dc", "da"):
+        _err(back(grads=grads(**{name: None})), B.RN_EINVAL, "NULL")
+    _err(back(grads=None), B.RN_EINVAL, "gradients")
+    _err(back(dout=None), B.RN_EINVAL, "NULL")
+    _err(back(saved=None), B.RN_EINVAL, "NULL")
+    _err(back(saved_bytes=saved - 1), B.RN_ENOSPACE, "saved")
+    _err(back(given=inputs(z=None)), B.RN_EINVAL, "dz without z")
+    _err(back(dfinal=P), B.RN_EINVAL, "dfinal")
+    _err(step(shape=ref(s)), B.RN_EINVAL, "one token a stream")
+    _err(step(slots=1), B.RN_EINVAL, "slots")
+    _err(step(slots=-1, ids=P), B.RN_EINVAL, "slots")
+    _err(step(state=None), B.RN_EINVAL, "NULL")
+    _err(step(out=None), B.RN_EINVAL, "NULL")
+    apart = _scan(tokens=2, u=9)
+    _err(step(shape=ref(apart), out=P), B.RN_EINVAL, "not contiguous")
+    assert fwd(shape=ref(none), scratch=None) == step(shape=ref(none), slots=0, state=None) == B.RN_OK
+
+
+def test_scan_sizes_stay_in_bounds():
+    """Scratch and saved bytes grow with the tokens, not with sequences times channels times states."""
+    L, ref = ops.load_ops(), ops.ctypes.byref
+    many = ops.rn_scan_shape(65535, 4096, 1, 16, 65535, B.RN_BF16, 1, 4096, 4096, 16, 16, 4096)
+    long = ops.rn_scan_shape(1, 4096, 1, 16, 1 << 20, B.RN_BF16, 1, 4096, 4096, 16, 16, 4096)
+    state = 4096 * 16 * 4
+    assert L.reuse_ops_scan_saved_bytes(ref(long)) <= ((1 << 16) + 1) * state + 512
+    assert L.reuse_ops_scan_scratch_bytes(ref(long)) <= 1 << 30
+    sums = 64 * 65535 * 2 * 16 * 4
+    # the sums of b's and c's gradients, and parts of a bounded number of blocks; ends of chunks that 65535 tokens can have
+    assert L.reuse_ops_scan_backward_scratch_bytes(ref(many)) <= sums + (1 << 28)
+
+
+def test_scan_tensors(calls):
+    t, n = 6, 2
+    u, b, a, d, s = torch.zeros(t, 8), torch.zeros(t, 2, 4), torch.zeros(8, 4), torch.zeros(8), torch.zeros(n, 8, 4)
+    off = torch.tensor([0, 2, 6], dtype=torch.int32)
+    out, final, saved = ops.scan_forward(u, u, a, b, b, d, u, d, seq_off=off, state=s, save=True)
+    got = ops.scan_backward(out, u, u, a, b, b, d, u, d, seq_off=off, saved=saved)
+    assert [tuple(g.shape) for g in got] == [(6, 8), (6, 8), (8, 4), (6, 2, 4), (6, 2, 4), (8,), (6, 8), (8,), (2, 8, 4)]
+    bare = ops.scan_backward(out, u, u, a, b, b, seq_off=off, saved=saved, want_dstate=False)
+    assert [g is None for g in bare] == [False] * 5 + [True] * 4
+    assert ops.scan_step(u[:2], u[:2], a, b[:2], b[:2], s).shape == (2, 8)
+    calls.clear()
+    for bad, args, kw in ((ValueError, (u[0], u, a, b, b), dict(n=1)), (ValueError, (u, u[:5], a, b, b), dict(n=1)),
+                          (ValueError, (u, u.bfloat16(), a, b, b), dict(n=1)), (ValueError, (u, u, a[:7], b, b), dict(n=1)),
+                          (TypeError, (u, u, a.bfloat16(), b, b), dict(n=1)), (ValueError, (u, u, a, b[:, :, :3], b), dict(n=1)),
+                          (ValueError, (u, u, a, torch.zeros(t, 3, 4), torch.zeros(t, 3, 4)), dict(n=1)),
+                          (ValueError, (u, u, a, b.transpose(1, 2), b), dict(n=1)), (ValueError, (u, u, a, b, b), {}),
+                          (ValueError, (u, u, a, b, b), dict(n=4)), (ValueError, (u, u, a, b, b, d[:3]), dict(n=1)),
+                          (ValueError, (u, u, a, b, b, d, u[:, :4]), dict(n=1)), (ValueError, (u, u, a, b, b), dict(n=1, state=s)),
+                          (ValueError, (u, u, a, b, b), dict(n=2, final=s[:1])), (ValueError, (u, u, a, b, b), dict(n=2, out=u[:5])),
+                          (ValueError, (u.t(), u, a, b, b), dict(n=1)), (TypeError, (u, u, a, b, b), dict(seq_off=off.long()))):
+        with pytest.raises(bad):
+            ops.scan_forward(*args, **kw)
+    big = torch.zeros(t, 1, 65)
+    for call, kw in ((ops.scan_forward, {}), (ops.scan_backward, dict(saved=saved))):
+        with pytest.raises(B.ReuseNetError, match="64"):
+            call(*([u] if call is ops.scan_backward else []), u, u, torch.zeros(8, 65), big, big, n=1, **kw)
+    with pytest.raises(TypeError, match="saved"):
+        ops.scan_backward(out, u, u, a, b, b, seq_off=off)
+    with pytest.raises(ValueError, match="saved"):
+        ops.scan_backward(out, u, u, a, b, b, seq_off=off, saved=saved[:-1])
+    with pytest.raises(ValueError, match="slots"):
+        ops.scan_step(u, u, a, b, b, s)
+    for call, args in ((ops.scan_forward, [u, u, a, b, b, d, u, d, True, off, None, s]),
+                       (ops.scan_backward, [out, u, u, a, b, b, d, u, d, True, off, None, saved, s]),
+                       (ops.scan_step, [u[:2], u[:2], a, b[:2], b[:2], s, d, u[:2], d])):
+        for i, x in enumerate(args):
+            if isinstance(x, torch.Tensor) and x.is_floating_point():
+                some = list(args)
+                some[i] = x.clone().requires_grad_()
+                with pytest.raises(ValueError, match="requires grad"):
+                    call(*some)
+    assert not calls
