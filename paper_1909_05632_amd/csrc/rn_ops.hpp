@@ -123,12 +123,13 @@ struct ScanArgs {
     const float *state;           // first states, or NULL
     float *final_state;           // last states, or NULL (step: the states' pool)
     void *out;
-    float *kept;                  // [scan_kept_slots][channels][states] states before every tile, or NULL
+    float *kept;                  // [scan_kept_slots] states before every tile, or NULL.  kept and ends are the
+                                  // library's own: [...][states / 4, rounded up][channels][4]
     bool quads, whole_states;     // vectors of four channels, and of four states, are on their size
     int64_t blocks;               // over the channels (scan_blocks)
     int64_t chunk, chunks;        // tokens of a chunk, slots of chunks: tokens / chunk + n
     bool parts;                   // sequences may have several chunks
-    float *ends;                  // [scan_ends][channels][states] states chunks end with from 0, then begin with
+    float *ends;                  // [scan_ends] states chunks end with from 0, then begin with
     float *sums;                  // [scan_ends][channels] summed step sizes
     // Backward call:
     const void *dout;
@@ -139,8 +140,8 @@ struct ScanArgs {
     float *part_bc;               // [blocks][tokens][2][states]
     float *part_a, *part_d;       // [walkers][channels][states], [walkers][2][channels]
 };
-// The kept state of tile k of sequence i, which begins at token `begin`, is at this + k.
-__host__ __device__ inline int64_t scan_kept_slot(int begin, int i) { return begin / RN_SCAN_KEEP + i; }
+// Tile k of sequence i, which begins at token `begin`, has kept slot
+// begin / RN_SCAN_KEEP + i + k: below this, and no two tiles share one.
 inline int64_t scan_kept_slots(int64_t tokens, int n) { return tokens / RN_SCAN_KEEP + n; }
 // Chunk c of a sequence of several has slot scan_end_slot + c: of more than `chunk`
 // tokens it moves begin / (chunk / 2) on by its chunks at least.

@@ -180,15 +180,15 @@ struct ScanSizes {
 
 ScanSizes scan_sizes(const rn_scan_shape *s) {
     ScanSizes z;
-    const size_t row = (size_t)s->channels * 4, states = row * s->states;
+    const size_t row = (size_t)s->channels * 4, states = row * s->states, own = row * ((s->states + 3) / 4 * 4);
     z.blocks = scan_blocks(s->channels, s->groups, s->states);
     z.chunk = scan_chunk(s->tokens, s->channels, s->groups, s->states);
     z.chunks = s->tokens / z.chunk + s->n;
     z.walkers = scan_walkers(z.chunks, z.blocks);
-    z.kept = round_up(scan_kept_slots(s->tokens, s->n) * states);
+    z.kept = round_up(scan_kept_slots(s->tokens, s->n) * own);
     const bool parts = s->tokens > z.chunk;
     const size_t ends = parts ? scan_ends(s->tokens, z.chunk) : 0;
-    z.ends = round_up(ends * states), z.sums = round_up(ends * row);
+    z.ends = round_up(ends * own), z.sums = round_up(ends * row);
     z.part_bc = round_up((size_t)z.blocks * s->tokens * 2 * s->states * 4);
     z.part_a = round_up(z.walkers * states), z.part_d = round_up(z.walkers * 2 * row);
     return z;

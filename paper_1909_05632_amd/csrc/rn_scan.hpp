@@ -40,6 +40,12 @@ __device__ inline ScanChunk scan_chunk_of(const ScanArgs &a, const Seqs &s, int6
             scan_end_slot(a, begin) + c};
 }
 
+// The kept state of the chunk's first tile; the next tiles' follow.
+__device__ inline int64_t scan_kept_slot(const ScanArgs &a, const Seqs &s, const ScanChunk &chunk) {
+    const int begin = s.offset(chunk.seq);
+    return begin / kTile + chunk.seq + (chunk.begin - begin) / kTile;
+}
+
 // The block's channels c0 .. c0 + CB - 1, of which those below c1 are there; all of one group.
 template <int L>
 struct ScanBlock {
@@ -68,22 +74,18 @@ __device__ inline float over_states(float v) {
     return v;
 }
 
-// log(1 + e^x), relative error a few 2^-24 throughout: with e = e^-|x| and
-// q = e / (2 + e) <= 1/3, log(1 + e) = 2 (q + q^3/3 + q^5/5 + ...); the first term
-// left out is below 2^-25 of the sum.  The exponent's product is taken in two parts.
+// log(1 + e^x): with e = e^-|x| and q = e / (2 + e) <= 1/3, log(1 + e) is
+// 2 artanh(q) = q P(q^2), P of degree 4 by least squares weighted towards its largest
+// error, 4.5e-9 of it.  Relative error |x| 2^-24 from the exponent's rounding (as much
+// as x, itself a rounded sum, brings along) and a few 2^-24.
 __device__ inline float softplus(float x) {
-    const float m = -fabsf(x), t = m * kLog2e;
-    const float rest = fmaf(m, kLog2e, -t) + m * 1.925963033500011e-08f;     // log2(e) - kLog2e
-    float e = __builtin_amdgcn_exp2f(t);
-    e = t > -1e30f ? fmaf(e * kLn2, rest, e) : e;                            // infinite: e is 0 (NaN: NaN)
+    const float e = __builtin_amdgcn_exp2f(-fabsf(x) * kLog2e);
     const float q = e * __builtin_amdgcn_rcpf(2.f + e), r = q * q;
-    float p = fmaf(r, 1.f / 13, 1.f / 11);
-    p = fmaf(r, p, 1.f / 9);
-    p = fmaf(r, p, 1.f / 7);
-    p = fmaf(r, p, 1.f / 5);
-    p = fmaf(r, p, 1.f / 3);
-    p = fmaf(r, p, 1.f);
-    return fmaf(2.f * q, p, x > 0.f ? x : 0.f);
+    float p = fmaf(r, 0.2801215648651123f, 0.2800177335739136f);
+    p = fmaf(r, p, 0.4002152979373932f);
+    p = fmaf(r, p, 0.666664183139801f);
+    p = fmaf(r, p, 2.f);
+    return fmaf(q, p, fmaxf(x, 0.f));
 }
 
 // A lane's states of channel c, number n0 and on, of an array [...][channels][states].
@@ -110,6 +112,18 @@ __device__ inline void store_states(const ScanArgs &a, float *p, int64_t row, in
         for (int i = 0; i < kStates; ++i)
             if (n0 + i < a.states) p[i] = v[i];
     }
+}
+
+// The same of an array of the library's own, [...][states / 4, rounded up][channels][4].
+__device__ inline f32x4 *own_states(const ScanArgs &a, float *p, int64_t row, int c, int quad) {
+    return reinterpret_cast<f32x4 *>(p) + (row * ((a.states + kStates - 1) / kStates) + quad) * a.channels + c;
+}
+__device__ inline f32x4 load_own(const ScanArgs &a, float *p, int64_t row, int c, int quad, bool live) {
+    if (!live || quad * kStates >= a.states) return f32x4{0.f, 0.f, 0.f, 0.f};
+    return *own_states(a, p, row, c, quad);
+}
+__device__ inline void store_own(const ScanArgs &a, float *p, int64_t row, int c, int quad, bool live, f32x4 v) {
+    if (live && quad * kStates < a.states) *own_states(a, p, row, c, quad) = v;
 }
 
 // Four channels of a token; those that are not there are not touched.

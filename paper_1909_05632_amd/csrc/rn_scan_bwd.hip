@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_back(ScanArgs a) {
             total += s;
         }
     }
-    store_states(a, a.ends, chunk.end, c, lane * kStates, live, g);
+    store_own(a, a.ends, chunk.end, c, lane, live, g);
     if (live && lane == 0) a.sums[chunk.end * a.channels + c] = total;
 }
 
@@ -175,15 +175,14 @@ __global__ __launch_bounds__(kScanThreads, 2) void k_scan_bwd(ScanArgs a) {
         const ScanChunk chunk = scan_chunk_of(a, seqs, slot);
         if (chunk.seq < 0) continue;
         f32x4 g = chunk.alone() ? load_states(a, a.dfinal, chunk.seq, c, lane * kStates, live)
-                                : load_states(a, a.ends, chunk.end, c, lane * kStates, live);
-        const int begin = seqs.offset(chunk.seq);
-        const int64_t kept = scan_kept_slot(begin, chunk.seq) + (chunk.begin - begin) / kTile;
+                                : load_own(a, a.ends, chunk.end, c, lane, live);
+        const int64_t kept = scan_kept_slot(a, seqs, chunk);
         Raw<T> raw[Q::PER], next[Q::PER];
         TileBC<T, L> bc;
         f32x4 next_h;
         const auto fetch = [&](int t0) {
             bc.load(a, where.group, chunk.begin + t0, chunk.len - t0);
-            next_h = load_states(a, a.kept, kept + t0 / kTile, c, lane * kStates, live);
+            next_h = load_own(a, a.kept, kept + t0 / kTile, c, lane, live);
             if (!there) return;
 #pragma unroll
             for (int i = 0; i < Q::PER; ++i)
@@ -222,7 +221,7 @@ __global__ __launch_bounds__(kScanThreads, 2) void k_scan_bwd(ScanArgs a) {
                 const f32x4 b = *reinterpret_cast<const f32x4 *>(&sb[t][lane * kStates]);
 #pragma unroll
                 for (int i = 0; i < kStates; ++i)
-                    h[t + 1][i] = fmaf(__builtin_amdgcn_exp2f(s * decay[i]), h[t][i], x * b[i]);
+                    h[t + 1][i] = fmaf(x, b[i], __builtin_amdgcn_exp2f(s * decay[i]) * h[t][i]);
                 if (a.z) {
                     const f32x4 cc = *reinterpret_cast<const f32x4 *>(&sc[t][lane * kStates]);
                     float y = 0.f;

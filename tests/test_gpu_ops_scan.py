@@ -219,7 +219,8 @@ def test_gradient_against_differences():
 
 
 def test_step_sizes_of_any_size():
-    """softplus far out on both sides: -infinity leaves the state as it is, large steps empty it."""
+    """softplus far out on both sides: -infinity leaves the state as it is, large steps empty it.  e^-|x| is
+    off by the rounding of its exponent, |x| 2^-24 of itself, and all else by a few 2^-24: 4e-7."""
     from paper_1909_05632_amd import ops
     raw = torch.tensor([-float("inf"), -200.0, -90.0, -30.0, -12.0, -3.0, -1e-3, 0.0, 1e-3, 0.7, 3.0, 12.0, 20.0, 90.0, 1e4])
     T = len(raw)
@@ -230,11 +231,12 @@ def test_step_sizes_of_any_size():
     out, final = ops.scan_forward(**g, n=1, state=state)
     s = torch.where(raw > 100, raw.double(), torch.log1p(torch.exp(raw.double())))
     want = torch.exp(-0.5 * s) * 2 + s
-    assert ((out.cpu().double()[0] - want).abs() <= 4e-7 * want).all() and out[0, 0] == 2 and torch.equal(final[0, :, 0], out[0])
+    tol = 4e-7 + raw.double().abs().clamp(max=200) * 2.0 ** -24
+    assert ((out.cpu().double()[0] - want).abs() <= tol * want).all() and out[0, 0] == 2 and torch.equal(final[0, :, 0], out[0])
     # the step alone, from a state of 0: relative to itself also where it is tiny (below 1e-38 it is 0)
     small = ops.scan_forward(**g, n=1)[0].cpu().double()[0]
     fine = s > 1e-37
-    assert ((small - s).abs()[fine] <= 4e-7 * s[fine]).all() and (small[~fine] <= 1e-37).all()
+    assert ((small - s).abs()[fine] <= (tol * s)[fine]).all() and (small[~fine] <= 1e-37).all()
 
 
 @pytest.mark.parametrize("tokens", [60, 700])
