@@ -125,8 +125,10 @@ struct ScanArgs {
     void *out;
     float *kept;                  // [scan_kept_slots] states before every tile, or NULL.  kept and ends are the
                                   // library's own: [...][states / 4, rounded up][channels][4]
-    bool quads, whole_states;     // vectors of four channels, and of four states, are on their size
-    int64_t blocks;               // over the channels (scan_blocks)
+    bool whole_states;            // vectors of four states are on their size in all arrays
+    int padded;                   // states rounded up to 4, 8, 16, 32 or 64
+    float *packed;                // [tokens][groups][padded / 4][b, c][4]
+    int64_t blocks;               // 64 channels each (scan_blocks)
     int64_t chunk, chunks;        // tokens of a chunk, slots of chunks: tokens / chunk + n
     bool parts;                   // sequences may have several chunks
     float *ends;                  // [scan_ends] states chunks end with from 0, then begin with
@@ -147,9 +149,10 @@ inline int64_t scan_kept_slots(int64_t tokens, int n) { return tokens / RN_SCAN_
 // tokens it moves begin / (chunk / 2) on by its chunks at least.
 __host__ __device__ inline int64_t scan_end_slot(const ScanArgs &a, int begin) { return begin / (a.chunk / 2); }
 inline int64_t scan_ends(int64_t tokens, int64_t chunk) { return tokens / (chunk / 2); }
-int scan_lanes(int states);
-int64_t scan_blocks(int channels, int groups, int states);
-int scan_chunk(int64_t tokens, int channels, int groups, int states);
+int64_t scan_blocks(int channels, int groups);
+int scan_chunk(int64_t tokens, int channels, int groups, bool backward);
+int scan_padded(int states);
+hipError_t launch_scan_pack(const ScanArgs &a, bool bf16, hipStream_t s);
 int64_t scan_walkers(int64_t chunks, int64_t blocks);
 hipError_t launch_scan(const ScanArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_scan_step(const ScanArgs &a, bool bf16, hipStream_t s);

@@ -174,35 +174,34 @@ bool too_many_states(const rn_scan_shape *s) { return s->states > RN_SCAN_MAX_ST
 
 struct ScanSizes {
     int64_t blocks, chunk, chunks, walkers;
-    size_t kept, ends, sums;              // bytes
+    size_t kept, packed, ends, sums;      // bytes
     size_t part_bc, part_a, part_d;
 };
 
-ScanSizes scan_sizes(const rn_scan_shape *s) {
-    ScanSizes z;
+ScanSizes scan_sizes(const rn_scan_shape *s, bool backward) {
+    ScanSizes z{};
     const size_t row = (size_t)s->channels * 4, states = row * s->states, own = row * ((s->states + 3) / 4 * 4);
-    z.blocks = scan_blocks(s->channels, s->groups, s->states);
-    z.chunk = scan_chunk(s->tokens, s->channels, s->groups, s->states);
+    z.blocks = scan_blocks(s->channels, s->groups);
+    z.chunk = scan_chunk(s->tokens, s->channels, s->groups, backward);
     z.chunks = s->tokens / z.chunk + s->n;
     z.walkers = scan_walkers(z.chunks, z.blocks);
     z.kept = round_up(scan_kept_slots(s->tokens, s->n) * own);
-    const bool parts = s->tokens > z.chunk;
-    const size_t ends = parts ? scan_ends(s->tokens, z.chunk) : 0;
+    // The forward call may need it by the address of bfloat16 b and c, which is not known here.
+    if (const int padded = scan_padded(s->states); backward || s->dtype == RN_BF16 || padded != s->states)
+        z.packed = round_up((size_t)s->tokens * s->groups * 2 * padded * 4);
+    const size_t ends = s->tokens > z.chunk ? scan_ends(s->tokens, z.chunk) : 0;
     z.ends = round_up(ends * own), z.sums = round_up(ends * row);
-    z.part_bc = round_up((size_t)z.blocks * s->tokens * 2 * s->states * 4);
-    z.part_a = round_up(z.walkers * states), z.part_d = round_up(z.walkers * 2 * row);
+    if (backward) {
+        z.part_bc = round_up((size_t)z.blocks * s->tokens * 2 * s->states * 4);
+        z.part_a = round_up(z.walkers * states), z.part_d = round_up(z.walkers * 2 * row);
+    }
     return z;
 }
 
-size_t scan_bytes(const ScanSizes &z, bool backward) {
-    return z.ends + z.sums + (backward ? z.part_bc + z.part_a + z.part_d : 0) + kAlign;
+size_t scan_bytes(const ScanSizes &z) {
+    return z.packed + z.ends + z.sums + z.part_bc + z.part_a + z.part_d + kAlign;
 }
 
-// Vectors of four elements are on their size in every row of every array.
-bool on_quads(const rn_scan_shape *s, const void *p, int64_t stride) {
-    const int size = s->dtype == RN_BF16 ? 2 : 4;
-    return reinterpret_cast<uintptr_t>(p) % (4 * size) == 0 && stride % 4 == 0;
-}
 bool on_16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 rn_status check_scan(const rn_scan_shape *s, const rn_scan_inputs *in) {
@@ -216,7 +215,8 @@ rn_status check_scan(const rn_scan_shape *s, const rn_scan_inputs *in) {
     return RN_OK;
 }
 
-ScanArgs scan_args(const rn_scan_shape *s, const rn_scan_inputs *in, const int32_t *seq_off, const ScanSizes &z) {
+ScanArgs scan_args(const rn_scan_shape *s, const rn_scan_inputs *in, const int32_t *seq_off, const ScanSizes &z,
+                   void *scratch) {
     ScanArgs a{};
     a.n = s->n, a.channels = s->channels, a.groups = s->groups, a.states = s->states, a.softplus = s->softplus;
     a.tokens = s->tokens;
@@ -224,10 +224,14 @@ ScanArgs scan_args(const rn_scan_shape *s, const rn_scan_inputs *in, const int32
     a.us = s->u_stride, a.dts = s->dt_stride, a.bs = s->b_stride, a.cs = s->c_stride, a.zs = in->z ? s->z_stride : 0;
     a.a = in->a, a.d = in->d, a.dt_bias = in->dt_bias;
     a.off = seq_off;
-    a.quads = s->channels / s->groups % 4 == 0 && on_quads(s, a.u, a.us) && on_quads(s, a.dt, a.dts) && on_quads(s, a.z, a.zs);
     a.whole_states = s->states % 4 == 0 && on_16(a.a);
     a.blocks = z.blocks, a.chunk = z.chunk, a.chunks = z.chunks, a.walkers = z.walkers;
     a.parts = (seq_off || s->n == 0 ? s->tokens : s->tokens / s->n) > z.chunk;
+    a.padded = scan_padded(s->states);
+    char *at = static_cast<char *>(scratch);
+    a.packed = reinterpret_cast<float *>(at);
+    a.ends = reinterpret_cast<float *>(at + z.packed);
+    a.sums = reinterpret_cast<float *>(at + z.packed + z.ends);
     return a;
 }
 
@@ -490,7 +494,7 @@ rn_status reuse_ops_scan_step(const rn_scan_shape *shape, const rn_scan_inputs *
     if (!state || !out) return fail(RN_EINVAL, "state and out must not be NULL");
     if (shape->n > 1 && out == in->u && shape->u_stride != shape->channels)
         return fail(RN_EINVAL, "a result lies over an input that is not contiguous");
-    ScanArgs a = scan_args(shape, in, nullptr, scan_sizes(shape));
+    ScanArgs a = scan_args(shape, in, nullptr, scan_sizes(shape, false), nullptr);
     a.whole_states = a.whole_states && on_16(state);
     a.ids = ids, a.slots = slots, a.final_state = state, a.out = out;
     return launched(launch_scan_step(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
@@ -498,17 +502,17 @@ rn_status reuse_ops_scan_step(const rn_scan_shape *shape, const rn_scan_inputs *
 
 size_t reuse_ops_scan_saved_bytes(const rn_scan_shape *shape) {
     if (bad_scan(shape) || too_many_states(shape)) return 0;
-    return scan_sizes(shape).kept + kAlign;
+    return scan_sizes(shape, false).kept + kAlign;
 }
 
 size_t reuse_ops_scan_scratch_bytes(const rn_scan_shape *shape) {
     if (bad_scan(shape) || too_many_states(shape)) return 0;
-    return scan_bytes(scan_sizes(shape), false);
+    return scan_bytes(scan_sizes(shape, false));
 }
 
 size_t reuse_ops_scan_backward_scratch_bytes(const rn_scan_shape *shape) {
     if (bad_scan(shape) || too_many_states(shape)) return 0;
-    return scan_bytes(scan_sizes(shape), true);
+    return scan_bytes(scan_sizes(shape, true));
 }
 
 rn_status reuse_ops_scan_forward(const rn_scan_shape *shape, const rn_scan_inputs *in, const int32_t *seq_off,
@@ -520,17 +524,14 @@ rn_status reuse_ops_scan_forward(const rn_scan_shape *shape, const rn_scan_input
     if (shape->n == 0) return RN_OK;
     if (shape->tokens > 0 && !out) return fail(RN_EINVAL, "out must not be NULL");
     if (misaligned(saved) || misaligned(scratch)) return fail(RN_EINVAL, "saved and scratch must be 256-byte aligned");
-    const ScanSizes z = scan_sizes(shape);
+    const ScanSizes z = scan_sizes(shape, false);
     if (saved && saved_bytes < z.kept + kAlign) return need_bytes("saved", z.kept + kAlign);
     if (!scratch) return fail(RN_EINVAL, "scratch is NULL");
-    const size_t need = scan_bytes(z, false);
+    const size_t need = scan_bytes(z);
     if (scratch_bytes < need) return need_bytes("scratch", need);
-    ScanArgs a = scan_args(shape, in, seq_off, z);
-    a.quads = a.quads && on_quads(shape, out, 0);
+    ScanArgs a = scan_args(shape, in, seq_off, z, scratch);
     a.whole_states = a.whole_states && on_16(state) && on_16(final_state);
     a.state = state, a.final_state = final_state, a.out = out, a.kept = static_cast<float *>(saved);
-    char *at = static_cast<char *>(scratch);
-    a.ends = reinterpret_cast<float *>(at), a.sums = reinterpret_cast<float *>(at + z.ends);
     return launched(launch_scan(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));
 }
 
@@ -548,23 +549,18 @@ rn_status reuse_ops_scan_backward(const rn_scan_shape *shape, const rn_scan_inpu
     if (grads->dstate && grads->dstate == dfinal) return fail(RN_EINVAL, "dstate must not be dfinal");
     if (!saved || !scratch) return fail(RN_EINVAL, "saved and scratch must not be NULL");
     if (misaligned(saved) || misaligned(scratch)) return fail(RN_EINVAL, "saved and scratch must be 256-byte aligned");
-    const ScanSizes z = scan_sizes(shape);
+    const ScanSizes z = scan_sizes(shape, true);
     if (saved_bytes < z.kept + kAlign) return need_bytes("saved", z.kept + kAlign);
-    const size_t need = scan_bytes(z, true);
+    const size_t need = scan_bytes(z);
     if (scratch_bytes < need) return need_bytes("scratch", need);
-    ScanArgs a = scan_args(shape, in, seq_off, z);
-    for (const void *p : {dout, static_cast<const void *>(grads->du), static_cast<const void *>(grads->ddt),
-                          static_cast<const void *>(grads->dz)})
-        a.quads = a.quads && on_quads(shape, p, 0);
+    ScanArgs a = scan_args(shape, in, seq_off, z, scratch);
     a.whole_states = a.whole_states && on_16(dfinal) && on_16(grads->dstate);
     a.kept = static_cast<float *>(const_cast<void *>(saved));
     a.dout = dout, a.dfinal = dfinal;
     a.du = grads->du, a.ddt = grads->ddt, a.db = grads->db, a.dc = grads->dc, a.dz = grads->dz;
     a.da = grads->da, a.dd = grads->dd, a.ddt_bias = grads->ddt_bias, a.dstate = grads->dstate;
-    char *at = static_cast<char *>(scratch);
-    a.ends = reinterpret_cast<float *>(at);
-    a.sums = reinterpret_cast<float *>(at += z.ends);
-    a.part_bc = reinterpret_cast<float *>(at += z.sums);
+    char *at = static_cast<char *>(scratch) + z.packed + z.ends + z.sums;
+    a.part_bc = reinterpret_cast<float *>(at);
     a.part_a = reinterpret_cast<float *>(at += z.part_bc);
     a.part_d = reinterpret_cast<float *>(at += z.part_a);
     return launched(launch_scan_backward(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));

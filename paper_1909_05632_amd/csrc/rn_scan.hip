@@ -4,8 +4,8 @@
 //   out = y silu(z).
 //
 // Bound by its arithmetic: for each token, channel and state an exponential and
-// four multiplications or multiply-adds.  A channel's states stay in the registers
-// of its lanes (rn_scan.hpp) from a chunk's first token to its last.  Where there
+// four multiplications or multiply-adds, 24 cycles a wave.  A channel's states stay
+// in the registers of its lane from a chunk's first token to its last.  Where there
 // are too few channels and sequences for the GPU, sequences are cut into chunks:
 // each chunk's end from a state of 0 (k_scan_seq<LOCAL>), then the states that the
 // chunks begin with, one after the other (k_scan_join: a chunk's decay is that of
@@ -17,119 +17,18 @@ namespace {
 
 using namespace ops;
 
-// LOCAL: of every chunk but a sequence's last, the state at its end from 0, and its
-// summed step sizes.
-template <class T, int L, bool LOCAL>
-__global__ __launch_bounds__(kScanThreads) void k_scan_seq(ScanArgs a) {
-    constexpr int N = kStates * L, CB = ScanBlock<L>::CB;
-    using Q = Quads<L>;
-    __shared__ float step[kTile][CB][2];                // s, s u
-    __shared__ __attribute__((aligned(16))) float sb[kTile][N], sc[kTile][N];
-    __shared__ float sy[LOCAL ? 1 : kTile][CB];
-    const uint32_t block = block_index();
-    const ScanBlock<L> where(a, (int)(block % a.blocks));
-    const int64_t slot = block / a.blocks;
-    if (slot >= a.chunks) return;
-    const Seqs seqs{a.off, a.n, a.tokens};
-    const ScanChunk chunk = scan_chunk_of(a, seqs, slot);
-    if (chunk.seq < 0 || (LOCAL && chunk.last)) return;
-
-    const int lane = threadIdx.x % L, mine = threadIdx.x / L, c = where.c0 + mine;
-    const bool live = c < where.c1;
-    f32x4 decay = load_states(a, a.a, 0, c, lane * kStates, live) * kLog2e;
-    f32x4 h = {0.f, 0.f, 0.f, 0.f};
-    if (!LOCAL) h = chunk.alone() ? load_states(a, a.state, chunk.seq, c, lane * kStates, live)
-                                  : load_own(a, a.ends, chunk.end, c, lane, live);
-    float total = 0.f;
-
-    // This thread's quad of channels.
-    const int q0 = where.c0 + Q::channel();
-    const bool there = q0 < where.c1 && Q::row(0) < kTile;
-    float bias[4], d[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const bool in = there && q0 + j < where.c1;
-        bias[j] = in && a.dt_bias ? a.dt_bias[q0 + j] : 0.f;
-        d[j] = in && a.d && !LOCAL ? a.d[q0 + j] : 0.f;
-    }
-    Pack<T, 4> u[Q::PER], dt[Q::PER], z[Q::PER], next_u[Q::PER], next_dt[Q::PER], next_z[Q::PER];
-    TileBC<T, L> bc;
-    const auto fetch = [&](int t0) {
-        bc.load(a, where.group, chunk.begin + t0, chunk.len - t0);
-        if (!there) return;
-#pragma unroll
-        for (int i = 0; i < Q::PER; ++i) {
-            const int64_t t = chunk.begin + min(t0 + Q::row(i), chunk.len - 1);
-            next_u[i] = load_quad<T>(a, a.u, a.us, t, q0, where.c1);
-            next_dt[i] = load_quad<T>(a, a.dt, a.dts, t, q0, where.c1);
-            if (!LOCAL && a.z) next_z[i] = load_quad<T>(a, a.z, a.zs, t, q0, where.c1);
-        }
-    };
-    if (chunk.len > 0) fetch(0);
-    const int64_t kept = scan_kept_slot(a, seqs, chunk);
-    for (int t0 = 0; t0 < chunk.len; t0 += kTile) {
-        if (!LOCAL && a.kept) store_own(a, a.kept, kept + t0 / kTile, c, lane, live, h);
-        bc.store(a, chunk.len - t0, sb, sc);
-#pragma unroll
-        for (int i = 0; i < Q::PER; ++i) {
-            u[i] = next_u[i], dt[i] = next_dt[i], z[i] = next_z[i];
-            const int t = Q::row(i);
-            if (t >= kTile) continue;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float s = 0.f, x = 0.f;                 // past the end, and where no channel is: nothing happens
-                if (there && t0 + t < chunk.len && q0 + j < where.c1) {
-                    s = to_float(dt[i].v[j]) + bias[j];
-                    if (a.softplus) s = softplus(s);
-                    x = s * to_float(u[i].v[j]);
-                }
-                step[t][Q::channel() + j][0] = s;
-                step[t][Q::channel() + j][1] = x;
-            }
-        }
-        __syncthreads();
-        if (t0 + kTile < chunk.len) fetch(t0 + kTile);
-        float kept_y = 0.f;
-#pragma unroll
-        for (int t = 0; t < kTile; ++t) {
-            const float s = step[t][mine][0], x = step[t][mine][1];
-            const f32x4 b = *reinterpret_cast<const f32x4 *>(&sb[t][lane * kStates]);
-            const f32x4 cc = *reinterpret_cast<const f32x4 *>(&sc[t][lane * kStates]);
-            float y = 0.f;
-#pragma unroll
-            for (int i = 0; i < kStates; ++i) {
-                h[i] = fmaf(x, b[i], __builtin_amdgcn_exp2f(s * decay[i]) * h[i]);
-                if (!LOCAL) y = fmaf(cc[i], h[i], y);
-            }
-            if (LOCAL) {
-                total += s;
-            } else {
-                y = over_states<L>(y);                  // lane i keeps token i's, of every L
-                kept_y = lane == t % L ? y : kept_y;
-                if (t % L == L - 1) sy[t - (L - 1) + lane][mine] = kept_y;
-            }
-        }
-        __syncthreads();
-        if (LOCAL || !there) continue;
-#pragma unroll
-        for (int i = 0; i < Q::PER; ++i) {
-            const int t = Q::row(i);
-            if (t >= kTile || t0 + t >= chunk.len) continue;
-            float o[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                o[j] = fmaf(d[j], to_float(u[i].v[j]), sy[t][Q::channel() + j]);
-                if (a.z) o[j] *= silu(to_float(z[i].v[j]));
-            }
-            store_quad<T>(a, a.out, chunk.begin + t0 + t, q0, where.c1, o);
-        }
-    }
-    if (LOCAL) {
-        store_own(a, a.ends, chunk.end, c, lane, live, h);
-        if (live && lane == 0) a.sums[chunk.end * a.channels + c] = total;
-    } else if (chunk.last) {
-        store_states(a, a.final_state, chunk.seq, c, lane * kStates, live, h);
-    }
+// b and c as Packed, where the kernels do not read the caller's own.
+template <class T>
+__global__ __launch_bounds__(kScanThreads) void k_scan_pack(ScanArgs a) {
+    const int64_t i = (int64_t)block_index() * kScanThreads + threadIdx.x, row = i / (2 * a.padded);
+    const int at = (int)(i % (2 * a.padded)), n = at / (2 * kStates) * kStates + at % kStates, group = (int)(row % a.groups);
+    const int64_t t = row / a.groups;
+    if (t >= a.tokens) return;
+    float v = 0.f;
+    if (n < a.states)
+        v = to_float(at % (2 * kStates) < kStates ? static_cast<const T *>(a.b)[t * a.bs + group * a.states + n]
+                                                  : static_cast<const T *>(a.c)[t * a.cs + group * a.states + n]);
+    a.packed[i] = v;
 }
 
 // A thread four states: what each chunk of a sequence begins with, in place of its
@@ -166,76 +65,41 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_join(ScanArgs a) {
     }
 }
 
-// ------------------------------------------------------------------ a lane a channel
+// ------------------------------------------------------------------ sequences
 
-// S states in the registers of one lane, for S = 4, 8, 16, 32 and 64: nothing passes
-// between lanes, and a token's b and c, the same for all of them, are scalars, which
-// the loads' own unit brings.  A wave takes 64 channels of a chunk by itself.
-constexpr int kBatch = 8;         // tokens whose loads are on their way at once
-
-template <class T, int S>
-struct Scalars {
-    uint32_t raw[S * sizeof(T) / 4];
-    __device__ void load(const T *p) {
-        typedef const __attribute__((address_space(4))) uint32_t *Constant;
-        const Constant q = (Constant)(uintptr_t)p;
-#pragma unroll
-        for (int i = 0; i < (int)(S * sizeof(T) / 4); ++i) raw[i] = q[i];
-    }
-    __device__ float operator[](int i) const {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(raw[i]);
-        else return __uint_as_float(i % 2 ? raw[i / 2] & 0xffff0000u : raw[i / 2] << 16);
-    }
-};
-
-// An array's rows from one on: a lane's element of them.
-template <class T>
-__device__ inline __amdgpu_buffer_rsrc_t rows_from(const void *p, int64_t stride, int64_t row) {
-    const char *base = static_cast<const char *>(p) + row * stride * (int)sizeof(T);
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, 0x7fffffff, 0x00027000);
-}
-template <class T>
-__device__ inline uint32_t row_load(__amdgpu_buffer_rsrc_t rows, uint32_t lane, int at) {
-    if constexpr (sizeof(T) == 2) return (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(rows, lane, at, 0) << 16;
-    else return __builtin_amdgcn_raw_buffer_load_b32(rows, lane, at, 0);
-}
-template <class T>
-__device__ inline void row_store(__amdgpu_buffer_rsrc_t rows, uint32_t lane, int at, T v) {
-    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), rows, lane, at, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), rows, lane, at, 0);
-}
-
-template <class T, int S, bool LOCAL>
-__global__ __launch_bounds__(64) void k_scan_lane(ScanArgs a) {
+// A wave takes 64 channels of a chunk by itself, all S states of a channel in the
+// registers of its lane.  LOCAL: of every chunk but a sequence's last, the state at
+// its end from 0, and its summed step sizes.
+template <class T, class BC, int S, bool LOCAL>
+__global__ __launch_bounds__(64) void k_scan_seq(ScanArgs a) {
     const uint32_t block = block_index();
-    const int of = a.channels / a.groups, per = (of + 63) / 64, cblock = (int)(block % (per * a.groups));
-    const int group = cblock / per, c = group * of + cblock % per * 64 + (int)threadIdx.x, c1 = (group + 1) * of;
-    const int64_t slot = block / (per * a.groups);
+    const int me = threadIdx.x;
+    const ScanChannels where(a, (int)(block % a.blocks), me);
+    const int64_t slot = block / a.blocks;
     if (slot >= a.chunks) return;
     const Seqs seqs{a.off, a.n, a.tokens};
     ScanChunk chunk = scan_chunk_of(a, seqs, slot);
     if (chunk.seq < 0 || (LOCAL && chunk.last)) return;
     chunk.begin = __builtin_amdgcn_readfirstlane(chunk.begin), chunk.len = __builtin_amdgcn_readfirstlane(chunk.len);
-    const bool live = c < c1;
-    const int at = live ? c : c1 - 1;                   // lanes without a channel go along with the last one
+    const bool live = where.live;
+    const int c = where.c;
     float decay[S], h[S];
 #pragma unroll
     for (int q = 0; q < S / kStates; ++q) {
-        const f32x4 d = load_states(a, a.a, 0, at, q * kStates, true) * kLog2e;
+        const f32x4 d = load_states(a, a.a, 0, c, q * kStates, true) * kLog2e;
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
-        if (!LOCAL) s = chunk.alone() ? load_states(a, a.state, chunk.seq, at, q * kStates, true)
-                                      : load_own(a, a.ends, chunk.end, at, q, true);
+        if (!LOCAL) s = chunk.alone() ? load_states(a, a.state, chunk.seq, c, q * kStates, true)
+                                      : load_own(a, a.ends, chunk.end, c, q, true);
 #pragma unroll
         for (int i = 0; i < kStates; ++i) decay[q * kStates + i] = d[i], h[q * kStates + i] = s[i];
     }
-    const float bias = a.dt_bias ? a.dt_bias[at] : 0.f, d = a.d && !LOCAL ? a.d[at] : 0.f;
+    const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, d = a.d && !LOCAL ? a.d[c] : 0.f;
     const int64_t kept = scan_kept_slot(a, seqs, chunk);
     float total = 0.f;
     // A lane's own numbers, put by so that the tokens' loop can be a loop: unrolled, it
     // would have the scalars of all its tokens at once.
     __shared__ float sx[kBatch][2][64];                 // s, then y; s u
-    const int me = threadIdx.x;
-    const uint32_t lane = (uint32_t)at * sizeof(T), to_lane = live ? lane : 0xfffffff0u;
+    const uint32_t lane = (uint32_t)c * sizeof(T), to_lane = live ? lane : 0xfffffff0u;
     uint32_t ru[kBatch], rdt[kBatch], rz[kBatch];
     const auto fetch = [&](int t0) {                    // tokens past the last are it
         const int64_t first = chunk.begin + t0;
@@ -248,9 +112,8 @@ __global__ __launch_bounds__(64) void k_scan_lane(ScanArgs a) {
             if (!LOCAL) rz[i] = row_load<T>(z, lane, r * (int)(a.z ? a.zs : a.us));
         }
     };
-    constexpr int AT = S * sizeof(T) <= 32 ? (LOCAL ? 4 : 2) : 1;    // tokens whose scalars are there at once (a wave has 100)
-    const T *b_at = static_cast<const T *>(a.b) + chunk.begin * a.bs + group * S;
-    const T *c_at = static_cast<const T *>(a.c) + chunk.begin * a.cs + group * S;
+    constexpr int AT = S * sizeof(BC) <= 32 ? (LOCAL ? 4 : 2) : 1;    // tokens whose scalars are there at once (a wave has 100)
+    TokenRows<BC> rows_b(a, 0, where.group, chunk.begin), rows_c(a, 1, where.group, chunk.begin);
     if (chunk.len > 0) fetch(0);
     for (int t0 = 0; t0 < chunk.len; t0 += kBatch) {
         // The step sizes of all tokens at once, for each is a long chain.
@@ -271,12 +134,12 @@ __global__ __launch_bounds__(64) void k_scan_lane(ScanArgs a) {
                 store_own(a, a.kept, kept + t0 / kTile, c, q, live, f32x4{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]});
 #pragma unroll 1
         for (int i = 0; i < m; i += AT) {
-            Scalars<T, S> b[AT], cc[AT];
+            Scalars<BC, S> b[AT], cc[AT];
 #pragma unroll
             for (int k = 0; k < AT; ++k) {
-                b[k].load(b_at);
-                if (!LOCAL) cc[k].load(c_at);
-                if (t0 + i + k + 1 < chunk.len) b_at += a.bs, c_at += a.cs;
+                b[k].load(rows_b.at);
+                if (!LOCAL) cc[k].load(rows_c.at);
+                if (t0 + i + k + 1 < chunk.len) rows_b.at += rows_b.stride, rows_c.at += rows_c.stride;
             }
 #pragma unroll
             for (int k = 0; k < AT; ++k) {
@@ -318,7 +181,19 @@ __global__ __launch_bounds__(64) void k_scan_lane(ScanArgs a) {
 
 // ------------------------------------------------------------------ one token
 
-// Blocks walk the streams with the grid's second axis; L lanes a channel.
+// Sum over a channel's L lanes: 1 and 2 apart, then the other four of eight, the
+// other eight of sixteen (which hold one value by then, so mirrored will do).
+template <int L>
+__device__ inline float over_states(float v) {
+    if constexpr (L >= 2) v += dpp<0xb1>(v);
+    if constexpr (L >= 4) v += dpp<0x4e>(v);
+    if constexpr (L >= 8) v += dpp<0x141>(v);
+    if constexpr (L >= 16) v += dpp<0x140>(v);
+    return v;
+}
+
+// Bound by the states' bytes.  L lanes carry a channel, four states each, so that a
+// wave's accesses are one piece; blocks walk the streams with the grid's second axis.
 template <class T, int L>
 __global__ __launch_bounds__(kScanThreads) void k_scan_step(ScanArgs a) {
     const int lane = threadIdx.x % L, n0 = lane * kStates;
@@ -365,46 +240,35 @@ inline dim3 join_grid(const ScanArgs &a) {
     return grid_of((a.n * quads * a.channels + kScanThreads - 1) / kScanThreads);
 }
 
-// A lane a channel: where all of its states are whole quads, a power of two of them,
-// and b and c are on the four bytes that scalar loads need.
-template <class T>
-bool by_lane(const ScanArgs &a) {
-    const auto on_4 = [](const void *p, int64_t stride) {
-        return reinterpret_cast<uintptr_t>(p) % 4 == 0 && stride * (int)sizeof(T) % 4 == 0;
-    };
-    return a.states >= 4 && (a.states & (a.states - 1)) == 0 && on_4(a.b, a.bs) && on_4(a.c, a.cs);
-}
-
-template <class T>
-hipError_t forward(const ScanArgs &a, hipStream_t s) {
-    if (by_lane<T>(a)) {
-        const dim3 grid = grid_of((int64_t)a.groups * ((a.channels / a.groups + 63) / 64) * a.chunks);
-        for_lanes_of(a.states, [&](auto l) {
-            constexpr int S = decltype(l)::value * kStates;
-            if (a.parts) {
-                k_scan_lane<T, S, true><<<grid, 64, 0, s>>>(a);
-                k_scan_join<false><<<join_grid(a), kScanThreads, 0, s>>>(a);
-            }
-            k_scan_lane<T, S, false><<<grid, 64, 0, s>>>(a);
-        });
-        return hipGetLastError();
-    }
+template <class T, class BC>
+hipError_t sequences(const ScanArgs &a, hipStream_t s) {
     const dim3 grid = grid_of(a.blocks * a.chunks);
-    for_lanes_of(a.states, [&](auto l) {
-        constexpr int L = decltype(l)::value;
+    for_states(a.states, [&](auto states) {
+        constexpr int S = decltype(states)::value;
         if (a.parts) {
-            k_scan_seq<T, L, true><<<grid, kScanThreads, 0, s>>>(a);
+            k_scan_seq<T, BC, S, true><<<grid, 64, 0, s>>>(a);
             k_scan_join<false><<<join_grid(a), kScanThreads, 0, s>>>(a);
         }
-        k_scan_seq<T, L, false><<<grid, kScanThreads, 0, s>>>(a);
+        k_scan_seq<T, BC, S, false><<<grid, 64, 0, s>>>(a);
     });
     return hipGetLastError();
 }
 
+// The caller's own b and c where their rows are on four bytes and of 4, 8, 16, 32 or 64.
+template <class T>
+hipError_t forward(const ScanArgs &a, hipStream_t s) {
+    const auto on_4 = [&](const void *p, int64_t stride) {
+        return reinterpret_cast<uintptr_t>(p) % 4 == 0 && (a.tokens < 2 || stride * (int)sizeof(T) % 4 == 0);
+    };
+    if (a.padded == a.states && on_4(a.b, a.bs) && on_4(a.c, a.cs)) return sequences<T, T>(a, s);
+    if (hipError_t e = launch_scan_pack(a, sizeof(T) == 2, s)) return e;
+    return sequences<T, Packed>(a, s);
+}
+
 template <class T>
 hipError_t step(const ScanArgs &a, hipStream_t s) {
-    for_lanes_of(a.states, [&](auto l) {
-        constexpr int L = decltype(l)::value, CB = kScanThreads / L;
+    for_states(a.states, [&](auto states) {
+        constexpr int L = decltype(states)::value / kStates, CB = kScanThreads / L;
         const int across = (a.channels + CB - 1) / CB, rows = (2048 + across - 1) / across;
         k_scan_step<T, L><<<dim3(across, a.n < rows ? a.n : rows), kScanThreads, 0, s>>>(a);
     });
@@ -413,22 +277,32 @@ hipError_t step(const ScanArgs &a, hipStream_t s) {
 
 }  // namespace
 
-int scan_lanes(int states) {
-    int l = 0;
-    ops::for_lanes_of(states, [&](auto x) { l = decltype(x)::value; });
-    return l;
-}
-int64_t scan_blocks(int channels, int groups, int states) {
-    const int cb = ops::kScanThreads / scan_lanes(states);
-    return (int64_t)groups * ((channels / groups + cb - 1) / cb);
-}
-// Chunks so long that all tokens' are kBlocks blocks, but no shorter than kShortest:
-// below, what the chunks' ends cost is more than what they free.
-int scan_chunk(int64_t tokens, int channels, int groups, int states) {
-    constexpr int64_t kBlocks = 8192, kShortest = 64;
-    int64_t c = (tokens * groups * ((channels / groups + 63) / 64) + kBlocks - 1) / kBlocks;
+int64_t scan_blocks(int channels, int groups) { return (int64_t)groups * ((channels / groups + 63) / 64); }
+
+// Chunks so long that all tokens' are as many blocks as fill the GPU (8 waves a SIMD
+// forward; 2048 blocks of as many waves as a channel has quads of states backward),
+// but no shorter than kShortest: below, what the chunks' ends cost is more than what
+// they free.
+int scan_chunk(int64_t tokens, int channels, int groups, bool backward) {
+    constexpr int64_t kShortest = 64;
+    const int64_t blocks = backward ? 2048 : 8192;
+    int64_t c = (tokens * scan_blocks(channels, groups) + blocks - 1) / blocks;
     c = (c + RN_SCAN_KEEP - 1) / RN_SCAN_KEEP * RN_SCAN_KEEP;
     return (int)(c < kShortest ? kShortest : c < (1 << 30) ? c : 1 << 30);
+}
+
+// States of a channel as the kernels see them.
+int scan_padded(int states) {
+    int p = 4;
+    while (p < states) p *= 2;
+    return p;
+}
+hipError_t launch_scan_pack(const ScanArgs &a, bool bf16, hipStream_t s) {
+    if (a.tokens == 0) return hipSuccess;
+    const dim3 grid = grid_of((a.tokens * a.groups * 2 * a.padded + ops::kScanThreads - 1) / ops::kScanThreads);
+    if (bf16) k_scan_pack<ops::bf16_t><<<grid, ops::kScanThreads, 0, s>>>(a);
+    else k_scan_pack<float><<<grid, ops::kScanThreads, 0, s>>>(a);
+    return hipGetLastError();
 }
 
 hipError_t launch_scan(const ScanArgs &a, bool bf16, hipStream_t s) {

@@ -1,10 +1,8 @@
 // Device code that the selective scan's kernels share.
 //
-// L lanes carry a channel's states, kStates each (states that are not there have
-// a = b = c = 0), so a wave has 64 / L channels and a block 256 / L.  Tokens go by
-// tiles of kTile.  What only a channel needs of a token, its step size and products
-// with it, is computed once, by the thread that loads it (quads of channels), and
-// read from LDS by the channel's lanes.
+// A lane carries a channel, 64 of one group a wave: nothing passes between lanes but
+// the gradients of b and c, and a token's b and c, the same for all lanes, are
+// scalars, which the loads' own unit brings.
 #pragma once
 
 #include "rn_seq.hpp"
@@ -13,6 +11,7 @@ namespace rn {
 namespace ops {
 
 constexpr int kScanThreads = 256, kStates = 4, kTile = RN_SCAN_KEEP;
+constexpr int kBatch = 8;         // tokens whose loads are on their way at once
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -46,32 +45,24 @@ __device__ inline int64_t scan_kept_slot(const ScanArgs &a, const Seqs &s, const
     return begin / kTile + chunk.seq + (chunk.begin - begin) / kTile;
 }
 
-// The block's channels c0 .. c0 + CB - 1, of which those below c1 are there; all of one group.
-template <int L>
-struct ScanBlock {
-    static constexpr int CB = kScanThreads / L;
-    int group, c0, c1;
-    __device__ ScanBlock(const ScanArgs &a, int i) {
-        const int of = a.channels / a.groups, per = (of + CB - 1) / CB;
-        group = i / per;
-        c0 = group * of + i % per * CB;
-        c1 = (group + 1) * of;
+// A wave's channels: 64 of a group, of which lane `me` has c, or goes along with the
+// group's last where there is none.
+struct ScanChannels {
+    int group, c;
+    bool live;
+    __device__ ScanChannels(const ScanArgs &a, int block, int me) {
+        const int of = a.channels / a.groups, per = (of + 63) / 64;
+        group = block / per;
+        const int at = group * of + block % per * 64 + me, last = (group + 1) * of - 1;
+        live = at <= last;
+        c = live ? at : last;
     }
 };
 
-template <int CTRL>
-__device__ inline float dpp(float v) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
-}
-// Sum over a channel's L lanes: 1 and 2 apart, then the other four of eight, the
-// other eight of sixteen (which hold one value by then, so mirrored will do).
-template <int L>
-__device__ inline float over_states(float v) {
-    if constexpr (L >= 2) v += dpp<0xb1>(v);
-    if constexpr (L >= 4) v += dpp<0x4e>(v);
-    if constexpr (L >= 8) v += dpp<0x141>(v);
-    if constexpr (L >= 16) v += dpp<0x140>(v);
-    return v;
+template <int CTRL, int BANKS = 0xf>
+__device__ inline float dpp(float v, float old = 0.f) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old), __builtin_bit_cast(int, v),
+                                                                 CTRL, 0xf, BANKS, BANKS == 0xf));
 }
 
 // log(1 + e^x): with e = e^-|x| and q = e / (2 + e) <= 1/3, log(1 + e) is
@@ -126,75 +117,77 @@ __device__ inline void store_own(const ScanArgs &a, float *p, int64_t row, int c
     if (live && quad * kStates < a.states) *own_states(a, p, row, c, quad) = v;
 }
 
-// Four channels of a token; those that are not there are not touched.
-template <class T>
-__device__ inline Pack<T, 4> load_quad(const ScanArgs &a, const void *p, int64_t stride, int64_t token, int c, int c1) {
-    const T *x = static_cast<const T *>(p) + token * stride + c;
-    if (a.quads) return *reinterpret_cast<const Pack<T, 4> *>(x);
-    Pack<T, 4> v;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v.v[j] = x[c + j < c1 ? j : 0];
-    return v;
-}
-template <class T>
-__device__ inline void store_quad(const ScanArgs &a, void *p, int64_t token, int c, int c1, const float (&v)[4]) {
-    T *x = static_cast<T *>(p) + token * a.channels + c;
-    if (a.quads) {
-        store_as<T, 4>(x, v);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (c + j < c1) x[j] = from_float<T>(v[j]);
-    }
-}
+// b and c in float32, as k_scan_pack leaves them: a token's and group's quads of
+// states, four of b and then four of c each, the last of them 0.
+struct Packed {
+    float v;
+};
 
-// b and c of a tile, [kTile][4 L] each: a thread's elements, in flight and then in LDS.
-template <class T, int L>
-struct TileBC {
-    static constexpr int N = kStates * L, PER = (kTile * N + kScanThreads - 1) / kScanThreads;
-    T b[PER], c[PER];
-    __device__ void load(const ScanArgs &a, int group, int begin, int len) {
+// S of a token's b or c.  The address is one for the wave and on four bytes.
+template <class BC, int S>
+struct Scalars {
+    uint32_t raw[sizeof(BC) == 2 ? S / 2 : S];
+    __device__ void load(const BC *p) {
+        typedef const __attribute__((address_space(4))) uint32_t *Constant;
+        const Constant q = (Constant)(uintptr_t)p;
+        if constexpr (std::is_same<BC, Packed>::value) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = threadIdx.x + i * kScanThreads, t = e / N, n = e % N;
-            if (e < kTile * N && t < len && n < a.states) {
-                const int64_t at = begin + t;
-                b[i] = static_cast<const T *>(a.b)[at * a.bs + group * a.states + n];
-                c[i] = static_cast<const T *>(a.c)[at * a.cs + group * a.states + n];
-            }
+            for (int i = 0; i < S; ++i) raw[i] = q[i / kStates * 2 * kStates + i % kStates];
+        } else {
+#pragma unroll
+            for (int i = 0; i < (int)(S * sizeof(BC) / 4); ++i) raw[i] = q[i];
         }
     }
-    __device__ void store(const ScanArgs &a, int len, float (&sb)[kTile][N], float (&sc)[kTile][N]) const {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = threadIdx.x + i * kScanThreads, t = e / N, n = e % N;
-            if (e < kTile * N) {
-                const bool in = t < len && n < a.states;
-                sb[t][n] = in ? to_float(b[i]) : 0.f;
-                sc[t][n] = in ? to_float(c[i]) : 0.f;
-            }
+    __device__ float operator[](int i) const {
+        if constexpr (sizeof(BC) == 4) return __uint_as_float(raw[i]);
+        else return __uint_as_float(i % 2 ? raw[i / 2] & 0xffff0000u : raw[i / 2] << 16);
+    }
+};
+
+// An array's rows from one on: a lane's element of them.
+template <class T>
+__device__ inline __amdgpu_buffer_rsrc_t rows_from(const void *p, int64_t stride, int64_t row) {
+    const char *base = static_cast<const char *>(p) + row * stride * (int)sizeof(T);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, 0x7fffffff, 0x00027000);
+}
+template <class T>
+__device__ inline uint32_t row_load(__amdgpu_buffer_rsrc_t rows, uint32_t lane, int at) {
+    if constexpr (sizeof(T) == 2) return (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(rows, lane, at, 0) << 16;
+    else return __builtin_amdgcn_raw_buffer_load_b32(rows, lane, at, 0);
+}
+template <class T>
+__device__ inline void row_store(__amdgpu_buffer_rsrc_t rows, uint32_t lane, int at, T v) {
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), rows, lane, at, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), rows, lane, at, 0);
+}
+
+// Where a group's b or c (kind 1) of token t is: the caller's own, or as packed.
+template <class BC>
+struct TokenRows {
+    const BC *at;
+    int64_t stride;
+    __device__ TokenRows(const ScanArgs &a, int kind, int group, int64_t t) {
+        if constexpr (std::is_same<BC, Packed>::value) {
+            at = reinterpret_cast<const Packed *>(a.packed) + kind * kStates;
+            stride = (int64_t)a.groups * 2 * a.padded;
+            at += t * stride + group * 2 * a.padded;
+        } else {
+            at = static_cast<const BC *>(kind ? a.c : a.b);
+            stride = kind ? a.cs : a.bs;
+            at += t * stride + group * a.states;
         }
     }
 };
 
-// Quads of a tile: thread i has quad i % (CB / 4) of token i / (CB / 4), and on.
-template <int L>
-struct Quads {
-    static constexpr int CB = kScanThreads / L, ACROSS = CB / 4, ROWS = kScanThreads / ACROSS;
-    static constexpr int PER = kTile / ROWS > 1 ? kTile / ROWS : 1;
-    static __device__ int channel() { return threadIdx.x % ACROSS * 4; }
-    static __device__ int row(int i) { return threadIdx.x / ACROSS + i * ROWS; }
-};
-
-// The lanes of a channel by its states.
+// f(states of a channel, rounded up to 4, 8, 16, 32 or 64).
 template <class F>
-inline void for_lanes_of(int states, F &&f) {
+inline void for_states(int states, F &&f) {
     using std::integral_constant;
-    if (states <= 4) f(integral_constant<int, 1>{});
-    else if (states <= 8) f(integral_constant<int, 2>{});
-    else if (states <= 16) f(integral_constant<int, 4>{});
-    else if (states <= 32) f(integral_constant<int, 8>{});
-    else f(integral_constant<int, 16>{});
+    if (states <= 4) f(integral_constant<int, 4>{});
+    else if (states <= 8) f(integral_constant<int, 8>{});
+    else if (states <= 16) f(integral_constant<int, 16>{});
+    else if (states <= 32) f(integral_constant<int, 32>{});
+    else f(integral_constant<int, 64>{});
 }
 
 }  // namespace ops

@@ -13,9 +13,9 @@
 // forward (k_scan_back: each chunk's g at its begin from 0).
 //
 // Bound by its arithmetic: for each token, channel and state two exponentials, 14
-// multiplications or multiply-adds, and a sixth of that again for the sums over
-// channels: those of a wave in registers (sum_channels), of a block in LDS, of all
-// blocks by another kernel, each in a fixed order.
+// multiplications or multiply-adds, and a third of that again for the sums over
+// channels: those of a wave in registers (over_channels), of all waves by another
+// kernel, each in a fixed order.
 #include "rn_rows.hpp"
 #include "rn_scan.hpp"
 
@@ -24,12 +24,10 @@ namespace {
 
 using namespace ops;
 
-// 32 values a lane, summed over the lanes of a wave that carry other channels (lane
-// bits log2(L)..5).  Every step joins two lanes: each keeps half of the values that
-// both have.  Then lane l has value i of all channels at v[i & (R - 1)], R = 32 / (64 / L),
-// for those i whose upper bits are its own channel bits, the highest first.
+// Two lanes whose numbers differ in one bit: the one without it gets a of both, the
+// one with it b of both.
 template <int BIT>
-__device__ inline float exchange(float a, float b) {    // lanes without the bit: a of both, with it: b of both
+__device__ inline float exchange(float a, float b) {
     if constexpr (BIT == 5 || BIT == 4) {
         const auto r = BIT == 5
             ? __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false)
@@ -37,309 +35,271 @@ __device__ inline float exchange(float a, float b) {    // lanes without the bit
         return __uint_as_float(r[0]) + __uint_as_float(r[1]);
     } else {
         const bool up = threadIdx.x >> BIT & 1;
-        const float keep = up ? b : a, give = up ? a : b;
-        if constexpr (BIT == 3) return keep + dpp<0x128>(give);                 // 8 on in a row of 16
-        else if constexpr (BIT == 2) return keep + __shfl_xor(give, 4);
-        else if constexpr (BIT == 1) return keep + dpp<0x4e>(give);
-        else return keep + dpp<0xb1>(give);
+        const float keep = up ? b : a;
+        if constexpr (BIT == 3) return keep + dpp<0x128>(up ? a : b);           // 8 on in a row of 16
+        else return keep + dpp<0x114, 0xa>(b, dpp<0x104, 0x5>(a));              // 4 on, and 4 back
     }
 }
-template <int L, int BIT = 5, int COUNT = 32>
-__device__ inline void sum_channels(float (&v)[32]) {
-    if constexpr ((1 << BIT) >= L && COUNT > 1) {
+// 16 values a lane, summed over the wave's lanes: of value i, the sum is with the lanes
+// 4 i .. 4 i + 3.  Every step joins two lanes, which keep half of the values each; the
+// last two add.
+__device__ inline float over_channels(float (&v)[16]) {
 #pragma unroll
-        for (int i = 0; i < COUNT / 2; ++i) v[i] = exchange<BIT>(v[i], v[i + COUNT / 2]);
-        if constexpr (BIT > 0) sum_channels<L, BIT - 1, COUNT / 2>(v);
-    } else if constexpr ((1 << BIT) >= L) {             // one value left: of both lanes
-        v[0] += dpp<0xb1>(v[0]);
-    }
+    for (int i = 0; i < 8; ++i) v[i] = exchange<5>(v[i], v[i + 8]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = exchange<4>(v[i], v[i + 4]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v[i] = exchange<3>(v[i], v[i + 2]);
+    float r = exchange<2>(v[0], v[1]);
+    r += dpp<0x4e>(r);
+    return r + dpp<0xb1>(r);
 }
 
-// What a quad of channels is at a token, as loaded.
-template <class T>
+// A channel's element of u, dt, z and dout at a token, as float32 bits.
 struct Raw {
-    Pack<T, 4> u, dt, z, dout;
+    uint32_t u, dt, z, dout;
 };
-
 template <class T>
-__device__ inline Raw<T> load_raw(const ScanArgs &a, int64_t t, int c, int c1) {
-    Raw<T> r;
-    r.u = load_quad<T>(a, a.u, a.us, t, c, c1);
-    r.dt = load_quad<T>(a, a.dt, a.dts, t, c, c1);
-    r.dout = load_quad<T>(a, a.dout, a.channels, t, c, c1);
-    if (a.z) r.z = load_quad<T>(a, a.z, a.zs, t, c, c1);
-    return r;
-}
+struct RawRows {
+    __amdgpu_buffer_rsrc_t u, dt, z, dout;
+    int us, dts, zs, os;
+    __device__ RawRows(const ScanArgs &a, int64_t t)    // without z, dout is read in its place
+        : u(rows_from<T>(a.u, a.us, t)), dt(rows_from<T>(a.dt, a.dts, t)),
+          z(rows_from<T>(a.z ? a.z : a.dout, a.z ? a.zs : a.channels, t)), dout(rows_from<T>(a.dout, a.channels, t)),
+          us((int)a.us), dts((int)a.dts), zs((int)(a.z ? a.zs : a.channels)), os(a.channels) {}
+    __device__ Raw load(uint32_t lane, int row) const {
+        const int r = row * (int)sizeof(T);
+        return {row_load<T>(u, lane, r * us), row_load<T>(dt, lane, r * dts), row_load<T>(z, lane, r * zs),
+                row_load<T>(dout, lane, r * os)};
+    }
+};
 
 // dJ/d(state before each chunk but a sequence's first), from 0 behind it, and the
 // chunk's summed step sizes.
-template <class T, int L>
-__global__ __launch_bounds__(kScanThreads) void k_scan_back(ScanArgs a) {
-    constexpr int N = kStates * L, CB = ScanBlock<L>::CB;
-    using Q = Quads<L>;
-    __shared__ float in[kTile][CB][2];                  // s, p
-    __shared__ __attribute__((aligned(16))) float sb[kTile][N], sc[kTile][N];
+template <class T, int S>
+__global__ __launch_bounds__(64) void k_scan_back(ScanArgs a) {
+    __shared__ float in[kBatch][2][64];                 // s, p
     const uint32_t block = block_index();
-    const ScanBlock<L> where(a, (int)(block % a.blocks));
+    const int me = threadIdx.x;
+    const ScanChannels where(a, (int)(block % a.blocks), me);
     const int64_t slot = block / a.blocks;
     if (slot >= a.chunks) return;
     const Seqs seqs{a.off, a.n, a.tokens};
-    const ScanChunk chunk = scan_chunk_of(a, seqs, slot);
+    ScanChunk chunk = scan_chunk_of(a, seqs, slot);
     if (chunk.seq < 0 || chunk.first) return;
-    const int lane = threadIdx.x % L, mine = threadIdx.x / L, c = where.c0 + mine;
-    const bool live = c < where.c1;
-    const f32x4 decay = load_states(a, a.a, 0, c, lane * kStates, live) * kLog2e;
-    f32x4 g = {0.f, 0.f, 0.f, 0.f};
+    chunk.begin = __builtin_amdgcn_readfirstlane(chunk.begin), chunk.len = __builtin_amdgcn_readfirstlane(chunk.len);
+    const int c = where.c;
+    float decay[S], g[S];
+#pragma unroll
+    for (int q = 0; q < S / kStates; ++q) {
+        const f32x4 d = load_states(a, a.a, 0, c, q * kStates, true) * kLog2e;
+#pragma unroll
+        for (int i = 0; i < kStates; ++i) decay[q * kStates + i] = d[i], g[q * kStates + i] = 0.f;
+    }
+    const float bias = a.dt_bias ? a.dt_bias[c] : 0.f;
+    const uint32_t lane = (uint32_t)c * sizeof(T);
     float total = 0.f;
-    const int q0 = where.c0 + Q::channel();
-    const bool there = q0 < where.c1 && Q::row(0) < kTile;
-    float bias[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) bias[j] = there && q0 + j < where.c1 && a.dt_bias ? a.dt_bias[q0 + j] : 0.f;
-    Raw<T> raw[Q::PER];
-    TileBC<T, L> bc;
+    Raw raw[kBatch];
     const auto fetch = [&](int t0) {
-        bc.load(a, where.group, chunk.begin + t0, chunk.len - t0);
-        if (!there) return;
+        const RawRows<T> rows(a, chunk.begin + t0);
 #pragma unroll
-        for (int i = 0; i < Q::PER; ++i)
-            raw[i] = load_raw<T>(a, chunk.begin + min(t0 + Q::row(i), chunk.len - 1), q0, where.c1);
+        for (int i = 0; i < kBatch; ++i) raw[i] = rows.load(lane, min(i, chunk.len - t0 - 1));
     };
-    const int last = (chunk.len - 1) / kTile * kTile;
+    const int last = (chunk.len - 1) / kBatch * kBatch;
+    TokenRows<Packed> rows_c(a, 1, where.group, chunk.begin + chunk.len - 1);
     fetch(last);
-    for (int t0 = last; t0 >= 0; t0 -= kTile) {
-        __syncthreads();                                // the last tile has been read
-        bc.store(a, chunk.len - t0, sb, sc);
+    for (int t0 = last; t0 >= 0; t0 -= kBatch) {
+        const int m = min(kBatch, chunk.len - t0);
 #pragma unroll
-        for (int i = 0; i < Q::PER; ++i) {
-            const int t = Q::row(i);
-            if (t >= kTile) continue;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float s = 0.f, p = 0.f;
-                if (there && t0 + t < chunk.len && q0 + j < where.c1) {
-                    s = to_float(raw[i].dt.v[j]) + bias[j];
-                    if (a.softplus) s = softplus(s);
-                    p = to_float(raw[i].dout.v[j]);
-                    if (a.z) p *= silu(to_float(raw[i].z.v[j]));
-                }
-                in[t][Q::channel() + j][0] = s;
-                in[t][Q::channel() + j][1] = p;
-            }
+        for (int i = 0; i < kBatch; ++i) {
+            float s = __uint_as_float(raw[i].dt) + bias, p = __uint_as_float(raw[i].dout);
+            if (a.softplus) s = softplus(s);
+            if (a.z) p *= silu(__uint_as_float(raw[i].z));
+            in[i][0][me] = s, in[i][1][me] = p;
         }
-        __syncthreads();
-        if (t0 > 0) fetch(t0 - kTile);
+        if (t0 > 0) fetch(t0 - kBatch);
+#pragma unroll 1
+        for (int i = m - 1; i >= 0; --i) {
+            Scalars<Packed, S> cc;
+            cc.load(rows_c.at);
+            if (t0 + i > 0) rows_c.at -= rows_c.stride;
+            const float s = in[i][0][me], p = in[i][1][me];
 #pragma unroll
-        for (int t = kTile - 1; t >= 0; --t) {
-            const float s = in[t][mine][0], p = in[t][mine][1];
-            const f32x4 cc = *reinterpret_cast<const f32x4 *>(&sc[t][lane * kStates]);
-#pragma unroll
-            for (int i = 0; i < kStates; ++i) g[i] = __builtin_amdgcn_exp2f(s * decay[i]) * fmaf(cc[i], p, g[i]);
+            for (int n = 0; n < S; ++n) g[n] = __builtin_amdgcn_exp2f(s * decay[n]) * fmaf(cc[n], p, g[n]);
             total += s;
         }
     }
-    store_own(a, a.ends, chunk.end, c, lane, live, g);
-    if (live && lane == 0) a.sums[chunk.end * a.channels + c] = total;
+#pragma unroll
+    for (int q = 0; q < S / kStates; ++q)
+        store_own(a, a.ends, chunk.end, c, q, where.live, f32x4{g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]});
+    if (where.live) a.sums[chunk.end * a.channels + c] = total;
 }
 
-template <class T, int L>
-__global__ __launch_bounds__(kScanThreads, 2) void k_scan_bwd(ScanArgs a) {
-    constexpr int N = kStates * L, CB = ScanBlock<L>::CB, WAVES = kScanThreads / 64;
-    using Q = Quads<L>;
-    // s, u and p of each token and channel; a channel's lanes, which are one wave's,
-    // replace them by sum g a k, sum g b and sum c h when they are done with a token.
-    __shared__ float io[kTile][3][CB];
-    __shared__ __attribute__((aligned(16))) float sb[kTile][N], sc[kTile][N];
-    __shared__ __attribute__((aligned(16))) float sums[WAVES][kTile][2][N];    // of db and dc, by wave
+// A block takes 64 channels, wave w their states 4 w .. 4 w + 3, and tokens by halves
+// of a tile; W waves.  A token is loaded, and its results are stored, by one of them.
+template <class T, int W>
+__global__ __launch_bounds__(64 * W, W == 4 ? 3 : W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a) {
+    constexpr int HALF = kTile / 2, OWN = W < HALF ? HALF / W : 1;             // a wave's tokens of a half
+    __shared__ float in[kTile][5][64];                  // of each token s, u, p, softplus', dout silu'(z)
+    __shared__ float sum_y[W][kTile][64];               // sum c h, by wave
+    __shared__ float sums[W][HALF][2][64];              // sum g a k, sum g b
     const uint32_t block = block_index();
-    const int cblock = (int)(block % a.blocks);
-    const ScanBlock<L> where(a, cblock);
+    const int cblock = (int)(block % a.blocks), me = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const ScanChannels where(a, cblock, me);
     const int64_t walker = block / a.blocks;
     if (walker >= a.walkers) return;
     const Seqs seqs{a.off, a.n, a.tokens};
-    const int lane = threadIdx.x % L, mine = threadIdx.x / L, c = where.c0 + mine, wave = threadIdx.x / 64;
-    const bool live = c < where.c1;
-    const f32x4 decay = load_states(a, a.a, 0, c, lane * kStates, live) * kLog2e;
+    const int c = where.c;
+    const f32x4 decay = load_states(a, a.a, 0, c, w * kStates, true) * kLog2e;
+    const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, d = a.d ? a.d[c] : 0.f;
+    const uint32_t lane = (uint32_t)c * sizeof(T), to_lane = where.live ? lane : 0xfffffff0u;
     f32x4 da = {0.f, 0.f, 0.f, 0.f};
-    const int q0 = where.c0 + Q::channel();
-    const bool there = q0 < where.c1 && Q::row(0) < kTile;
-    float bias[4], d[4], dd[4], dbias[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const bool in = there && q0 + j < where.c1;
-        bias[j] = in && a.dt_bias ? a.dt_bias[q0 + j] : 0.f;
-        d[j] = in && a.d ? a.d[q0 + j] : 0.f;
-        dd[j] = dbias[j] = 0.f;
-    }
+    float dd = 0.f, dbias = 0.f;
+    // Token j of this wave's in half k.
+    const auto token = [&](int k, int j) { return k * HALF + w * OWN + j; };
+    const bool helps = w * OWN < HALF;
     for (int64_t slot = walker; slot < a.chunks; slot += a.walkers) {
-        const ScanChunk chunk = scan_chunk_of(a, seqs, slot);
+        ScanChunk chunk = scan_chunk_of(a, seqs, slot);
         if (chunk.seq < 0) continue;
-        f32x4 g = chunk.alone() ? load_states(a, a.dfinal, chunk.seq, c, lane * kStates, live)
-                                : load_own(a, a.ends, chunk.end, c, lane, live);
+        chunk.begin = __builtin_amdgcn_readfirstlane(chunk.begin), chunk.len = __builtin_amdgcn_readfirstlane(chunk.len);
+        f32x4 g = chunk.alone() ? load_states(a, a.dfinal, chunk.seq, c, w * kStates, true)
+                                : load_own(a, a.ends, chunk.end, c, w, true);
         const int64_t kept = scan_kept_slot(a, seqs, chunk);
-        Raw<T> raw[Q::PER], next[Q::PER];
-        TileBC<T, L> bc;
+        Raw raw[2][OWN];
         f32x4 next_h;
         const auto fetch = [&](int t0) {
-            bc.load(a, where.group, chunk.begin + t0, chunk.len - t0);
-            next_h = load_own(a, a.kept, kept + t0 / kTile, c, lane, live);
-            if (!there) return;
+            next_h = load_own(a, a.kept, kept + t0 / kTile, c, w, true);
+            const RawRows<T> rows(a, chunk.begin + t0);
 #pragma unroll
-            for (int i = 0; i < Q::PER; ++i)
-                next[i] = load_raw<T>(a, chunk.begin + min(t0 + Q::row(i), chunk.len - 1), q0, where.c1);
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int j = 0; j < OWN; ++j)
+                    if (helps) raw[k][j] = rows.load(lane, min(token(k, j), chunk.len - t0 - 1));
         };
         const int last = chunk.len > 0 ? (chunk.len - 1) / kTile * kTile : -1;
         if (last >= 0) fetch(last);
         for (int t0 = last; t0 >= 0; t0 -= kTile) {
-            bc.store(a, chunk.len - t0, sb, sc);
+            const int m = min(kTile, chunk.len - t0);
 #pragma unroll
-            for (int i = 0; i < Q::PER; ++i) {
-                raw[i] = next[i];
-                const int t = Q::row(i);
-                if (t >= kTile) continue;
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float s = 0.f, u = 0.f, p = 0.f;
-                    if (there && t0 + t < chunk.len && q0 + j < where.c1) {
-                        s = to_float(raw[i].dt.v[j]) + bias[j];
-                        if (a.softplus) s = softplus(s);
-                        u = to_float(raw[i].u.v[j]);
-                        p = to_float(raw[i].dout.v[j]);
-                        if (a.z) p *= silu(to_float(raw[i].z.v[j]));
+                for (int j = 0; j < OWN; ++j) {
+                    if (!helps) continue;
+                    const int t = token(k, j);
+                    const float r = __uint_as_float(raw[k][j].dt) + bias, z = __uint_as_float(raw[k][j].z);
+                    float p = __uint_as_float(raw[k][j].dout);
+                    if (a.z) {
+                        const float gate = sigmoid(z);
+                        in[t][4][me] = p * gate * fmaf(z, 1.f - gate, 1.f);
+                        p *= z * gate;
                     }
-                    io[t][0][Q::channel() + j] = s, io[t][1][Q::channel() + j] = u, io[t][2][Q::channel() + j] = p;
+                    // Past the end, and where no channel is, nothing happens.
+                    const bool live = where.live && t < m;
+                    in[t][0][me] = t < m ? (a.softplus ? softplus(r) : r) : 0.f;
+                    in[t][1][me] = live ? __uint_as_float(raw[k][j].u) : 0.f;
+                    in[t][2][me] = live ? p : 0.f;
+                    in[t][3][me] = a.softplus ? sigmoid(r) : 1.f;
                 }
-            }
             f32x4 h[kTile + 1];                         // before each token, and after the last
             h[0] = next_h;
             __syncthreads();
             if (t0 > 0) fetch(t0 - kTile);
-            float kept_y[kTile / L > 0 ? kTile / L : 1];
+            // The scalars of token t, not before `after` is known: there are registers for
+            // those of two tokens, and left alone all of the tile's would come first.
+            const TokenRows<Packed> rows(a, 0, where.group, chunk.begin + t0);
+            const Packed *from = rows.at + w * 2 * kStates;
+            const int stride = (int)rows.stride;
+            struct BC {
+                Scalars<Packed, kStates> b, c;
+            };
+            const auto scalars = [&](int t, float after) {
+                asm volatile("" : "+s"(from) : "v"(after));
+                BC v;
+                v.b.load(from + min(t, m - 1) * stride), v.c.load(from + min(t, m - 1) * stride + kStates);
+                return v;
+            };
+            BC next = scalars(0, h[0][0]);
 #pragma unroll
             for (int t = 0; t < kTile; ++t) {
-                const float s = io[t][0][mine], x = s * io[t][1][mine];
-                const f32x4 b = *reinterpret_cast<const f32x4 *>(&sb[t][lane * kStates]);
+                const BC now = next;
+                next = scalars(t + 1 < kTile ? t + 1 : t, h[t][0]);
+                const float st = in[t][0][me], x = st * in[t][1][me];
+                float y = 0.f;
 #pragma unroll
-                for (int i = 0; i < kStates; ++i)
-                    h[t + 1][i] = fmaf(x, b[i], __builtin_amdgcn_exp2f(s * decay[i]) * h[t][i]);
-                if (a.z) {
-                    const f32x4 cc = *reinterpret_cast<const f32x4 *>(&sc[t][lane * kStates]);
-                    float y = 0.f;
-#pragma unroll
-                    for (int i = 0; i < kStates; ++i) y = fmaf(cc[i], h[t + 1][i], y);
-                    y = over_states<L>(y);
-                    kept_y[t / L] = t % L == 0 || lane == t % L ? y : kept_y[t / L];
+                for (int i = 0; i < kStates; ++i) {
+                    h[t + 1][i] = fmaf(x, now.b[i], __builtin_amdgcn_exp2f(st * decay[i]) * h[t][i]);
+                    y = fmaf(now.c[i], h[t + 1][i], y);
                 }
+                if (a.z) sum_y[w][t][me] = y;
             }
 #pragma unroll
-            for (int t4 = kTile - 4; t4 >= 0; t4 -= 4) {
-                float v[32];                            // [token][db, dc][state]
-                float ak[4], gb[4];
+            for (int half = 1; half >= 0; --half) {
 #pragma unroll
-                for (int t = t4 + 3; t >= t4; --t) {
-                    const float s = io[t][0][mine], x = s * io[t][1][mine], p = io[t][2][mine];
-                    const f32x4 b = *reinterpret_cast<const f32x4 *>(&sb[t][lane * kStates]);
-                    const f32x4 cc = *reinterpret_cast<const f32x4 *>(&sc[t][lane * kStates]);
-                    float *o = v + (t - t4) * 8;
-                    float sum_ak = 0.f, sum_gb = 0.f;
+                for (int t2 = half * HALF + HALF - 2; t2 >= half * HALF; t2 -= 2) {
+                    float v[16];                        // [token][db, dc][state]
 #pragma unroll
-                    for (int i = 0; i < kStates; ++i) {
-                        const float e = __builtin_amdgcn_exp2f(s * decay[i]);
-                        g[i] = fmaf(cc[i], p, g[i]);
-                        const float gk = g[i] * (e * h[t][i]);
-                        sum_ak = fmaf(gk, decay[i], sum_ak);
-                        da[i] = fmaf(gk, s, da[i]);
-                        sum_gb = fmaf(g[i], b[i], sum_gb);
-                        o[i] = g[i] * x;
-                        o[4 + i] = h[t + 1][i] * p;
-                        g[i] *= e;
-                    }
-                    ak[t - t4] = over_states<L>(sum_ak), gb[t - t4] = over_states<L>(sum_gb);
-                }
-                sum_channels<L>(v);
-                // Lane bits 5 and 4 are the token's where the channels have them (L <= 16).
-                {
-                    constexpr int R = L >= 2 ? L / 2 : 1;               // values a lane has now
-                    const int at = ((threadIdx.x & 63) / (L > 2 ? L : 2)) * R;
-                    float *to = &sums[wave][t4][0][0];
-                    // Value at + i is [token][kind][state].
-                    if constexpr (R >= 4) {
+                    for (int t = t2 + 1; t >= t2; --t) {
+                        const float st = in[t][0][me], x = st * in[t][1][me], pt = in[t][2][me];
+                        const BC now = next;
+                        next = scalars(t > 0 ? t - 1 : 0, g[0]);
+                        float *o = v + (t - t2) * 8, ak = 0.f, gb = 0.f;
 #pragma unroll
-                        for (int i = 0; i < R; i += 4)
-                            *reinterpret_cast<f32x4 *>(to + (at + i) / 4 * N + lane * kStates) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < R; ++i) to[(at + i) / 4 * N + lane * kStates + (at + i) % 4] = v[i];
-                    }
-                }
-                // Lanes of a channel write the tokens' sums in turn, over what they have all read.
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    if (lane == t % L) {
-                        io[t4 + t][0][mine] = ak[t] * kLn2;
-                        io[t4 + t][1][mine] = gb[t];
-                    }
-            }
-            if (a.z) {
-#pragma unroll
-                for (int i = 0; i < (kTile / L > 0 ? kTile / L : 1); ++i)
-                    if (L <= kTile) io[i * L + lane][2][mine] = kept_y[i];
-            }
-            __syncthreads();
-            if (there) {
-#pragma unroll
-                for (int i = 0; i < Q::PER; ++i) {
-                    const int t = Q::row(i);
-                    if (t >= kTile || t0 + t >= chunk.len) continue;
-                    float du[4], ddt[4], dz[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float r = to_float(raw[i].dt.v[j]) + bias[j], s = a.softplus ? softplus(r) : r;
-                        const float u = to_float(raw[i].u.v[j]), out = to_float(raw[i].dout.v[j]);
-                        float p = out;
-                        const float sum_gb = io[t][1][Q::channel() + j];
-                        if (a.z) {
-                            const float z = to_float(raw[i].z.v[j]);
-                            dz[j] = out * fmaf(d[j], u, io[t][2][Q::channel() + j]) * silu_slope(z);
-                            p *= silu(z);
+                        for (int i = 0; i < kStates; ++i) {
+                            const float e = __builtin_amdgcn_exp2f(st * decay[i]);
+                            g[i] = fmaf(now.c[i], pt, g[i]);
+                            const float gk = g[i] * (e * h[t][i]);
+                            ak = fmaf(gk, decay[i], ak);
+                            da[i] = fmaf(gk, st, da[i]);
+                            gb = fmaf(now.b[i], g[i], gb);
+                            o[i] = g[i] * x;
+                            o[4 + i] = h[t + 1][i] * pt;
+                            g[i] *= e;
                         }
-                        du[j] = fmaf(s, sum_gb, d[j] * p);
-                        ddt[j] = fmaf(u, sum_gb, io[t][0][Q::channel() + j]);
-                        if (a.softplus) ddt[j] *= sigmoid(r);
-                        if (q0 + j < where.c1) dd[j] = fmaf(p, u, dd[j]), dbias[j] += ddt[j];
+                        sums[w][t % HALF][0][me] = ak, sums[w][t % HALF][1][me] = gb;
                     }
-                    const int64_t at = chunk.begin + t0 + t;
-                    store_quad<T>(a, a.du, at, q0, where.c1, du);
-                    store_quad<T>(a, a.ddt, at, q0, where.c1, ddt);
-                    if (a.dz) store_quad<T>(a, a.dz, at, q0, where.c1, dz);
+                    const float r = over_channels(v);
+                    const int t = t2 + me / 32, n = w * kStates + me / 4 % 4;
+                    if (me % 4 == 0 && t < m && n < a.states)
+                        a.part_bc[(((int64_t)cblock * a.tokens + chunk.begin + t0 + t) * 2 + me / 16 % 2) * a.states + n] = r;
                 }
-            }
-            for (int i = threadIdx.x; i < kTile * 2 * N; i += kScanThreads) {
-                const int t = i / (2 * N), n = i % N;
-                if (t0 + t >= chunk.len || n >= a.states) continue;
-                float v = 0.f;
+                __syncthreads();
+                if (helps) {
+                    const int64_t first = chunk.begin + t0;
+                    const auto du = rows_from<T>(a.du, a.channels, first), ddt = rows_from<T>(a.ddt, a.channels, first);
+                    const auto dz = rows_from<T>(a.dz, a.channels, first);
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) v += (&sums[w][0][0][0])[i];
-                a.part_bc[(((int64_t)cblock * a.tokens + chunk.begin + t0 + t) * 2 + i / N % 2) * a.states + n] = v;
+                    for (int j = 0; j < OWN; ++j) {
+                        const int t = token(half, j);
+                        if (t >= m) break;
+                        float ak = 0.f, gb = 0.f, y = 0.f;
+#pragma unroll
+                        for (int k = 0; k < W; ++k) {
+                            ak += sums[k][t % HALF][0][me], gb += sums[k][t % HALF][1][me];
+                            if (a.dz) y += sum_y[k][t][me];
+                        }
+                        const float uj = in[t][1][me], pj = in[t][2][me], dr = fmaf(uj, gb, ak * kLn2) * in[t][3][me];
+                        dd = fmaf(pj, uj, dd), dbias += dr;
+                        const int at = t * a.channels * (int)sizeof(T);
+                        row_store<T>(du, to_lane, at, from_float<T>(fmaf(in[t][0][me], gb, d * pj)));
+                        row_store<T>(ddt, to_lane, at, from_float<T>(dr));
+                        if (a.dz) row_store<T>(dz, to_lane, at, from_float<T>(in[t][4][me] * fmaf(d, uj, y)));
+                    }
+                }
+                if (half) __syncthreads();              // sums is written again; after the other half the next tile's barrier is
             }
         }
-        if (chunk.first) store_states(a, a.dstate, chunk.seq, c, lane * kStates, live, g);
+        if (chunk.first) store_states(a, a.dstate, chunk.seq, c, w * kStates, where.live, g);
     }
-    store_states(a, a.part_a, walker, c, lane * kStates, live, da);
-    // dd and dbias: the quads of a channel are in threads ACROSS apart.
-    float *last = &io[0][0][0];
+    store_states(a, a.part_a, walker, c, w * kStates, where.live, da);
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (Q::row(0) < kTile) last[threadIdx.x * 8 + j] = dd[j], last[threadIdx.x * 8 + 4 + j] = dbias[j];
+    in[w % kTile][0][me] = dd, in[w % kTile][1][me] = dbias;
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * CB; i += kScanThreads) {
-        const int ch = i % CB, kind = i / CB;
-        if (where.c0 + ch >= where.c1) continue;
-        float v = 0.f;
-        for (int r = 0; r < (Q::ROWS < kTile ? Q::ROWS : kTile); ++r) v += last[(r * Q::ACROSS + ch / 4) * 8 + kind * 4 + ch % 4];
-        a.part_d[(walker * 2 + kind) * a.channels + where.c0 + ch] = v;
-    }
+    if (w < 2 && where.live)
+        for (int kind = w; kind < 2; kind += W < 2 ? W : 2) {
+            float v = 0.f;
+            for (int k = 0; k < W; ++k) v += in[k][kind][me];
+            a.part_d[(walker * 2 + kind) * a.channels + c] = v;
+        }
 }
 
 // db and dc of the blocks of a group's channels, in a fixed order.
@@ -369,14 +329,17 @@ __global__ __launch_bounds__(1024) void k_scan_sum_d(ScanArgs a) {
 
 template <class T>
 hipError_t backward(const ScanArgs &a, hipStream_t s) {
-    for_lanes_of(a.states, [&](auto l) {
-        constexpr int L = decltype(l)::value;
+    if (hipError_t e = launch_scan_pack(a, sizeof(T) == 2, s)) return e;
+    hipError_t joined = hipSuccess;
+    for_states(a.states, [&](auto states) {
+        constexpr int S = decltype(states)::value, W = S / kStates;
         if (a.parts) {
-            k_scan_back<T, L><<<grid_of(a.blocks * a.chunks), kScanThreads, 0, s>>>(a);
-            (void)launch_scan_join_back(a, s);
+            k_scan_back<T, S><<<grid_of(a.blocks * a.chunks), 64, 0, s>>>(a);
+            joined = launch_scan_join_back(a, s);
         }
-        k_scan_bwd<T, L><<<grid_of(a.blocks * a.walkers), kScanThreads, 0, s>>>(a);
+        k_scan_bwd<T, W><<<grid_of(a.blocks * a.walkers), 64 * W, 0, s>>>(a);
     });
+    if (joined) return joined;
     if (hipError_t e = hipGetLastError()) return e;
     if (a.tokens > 0)
         k_scan_bc<T><<<grid_of((2 * a.tokens * a.groups * a.states + kScanThreads - 1) / kScanThreads), kScanThreads, 0, s>>>(a);
