@@ -152,6 +152,7 @@ inline int64_t scan_ends(int64_t tokens, int64_t chunk) { return tokens / (chunk
 int64_t scan_blocks(int channels, int groups);
 int scan_chunk(int64_t tokens, int channels, int groups, bool backward);
 int scan_padded(int states);
+bool scan_direct(const ScanArgs &a, bool bf16);
 hipError_t launch_scan_pack(const ScanArgs &a, bool bf16, hipStream_t s);
 int64_t scan_walkers(int64_t chunks, int64_t blocks);
 hipError_t launch_scan(const ScanArgs &a, bool bf16, hipStream_t s);

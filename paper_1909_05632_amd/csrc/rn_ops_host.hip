@@ -186,8 +186,8 @@ ScanSizes scan_sizes(const rn_scan_shape *s, bool backward) {
     z.chunks = s->tokens / z.chunk + s->n;
     z.walkers = scan_walkers(z.chunks, z.blocks);
     z.kept = round_up(scan_kept_slots(s->tokens, s->n) * own);
-    // The forward call may need it by the address of bfloat16 b and c, which is not known here.
-    if (const int padded = scan_padded(s->states); backward || s->dtype == RN_BF16 || padded != s->states)
+    // Calls may need it by the address of bfloat16 b and c, which is not known here.
+    if (const int padded = scan_padded(s->states); s->dtype == RN_BF16 || padded != s->states)
         z.packed = round_up((size_t)s->tokens * s->groups * 2 * padded * 4);
     const size_t ends = s->tokens > z.chunk ? scan_ends(s->tokens, z.chunk) : 0;
     z.ends = round_up(ends * own), z.sums = round_up(ends * row);

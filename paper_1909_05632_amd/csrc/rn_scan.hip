@@ -121,9 +121,9 @@ __global__ __launch_bounds__(64) void k_scan_seq(ScanArgs a) {
         float v[kBatch], gate[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-            v[i] = __uint_as_float(ru[i]);
-            if (!LOCAL) gate[i] = a.z ? silu(__uint_as_float(rz[i])) : 1.f;
-            float s = __uint_as_float(rdt[i]) + bias;
+            v[i] = row_float<T>(ru[i]);
+            if (!LOCAL) gate[i] = a.z ? silu(row_float<T>(rz[i])) : 1.f;
+            float s = row_float<T>(rdt[i]) + bias;
             if (a.softplus) s = softplus(s);
             sx[i][0][me] = i < m ? s : 0.f, sx[i][1][me] = i < m ? s * v[i] : 0.f;     // past the end nothing happens
         }
@@ -254,13 +254,9 @@ hipError_t sequences(const ScanArgs &a, hipStream_t s) {
     return hipGetLastError();
 }
 
-// The caller's own b and c where their rows are on four bytes and of 4, 8, 16, 32 or 64.
 template <class T>
 hipError_t forward(const ScanArgs &a, hipStream_t s) {
-    const auto on_4 = [&](const void *p, int64_t stride) {
-        return reinterpret_cast<uintptr_t>(p) % 4 == 0 && (a.tokens < 2 || stride * (int)sizeof(T) % 4 == 0);
-    };
-    if (a.padded == a.states && on_4(a.b, a.bs) && on_4(a.c, a.cs)) return sequences<T, T>(a, s);
+    if (scan_direct(a, sizeof(T) == 2)) return sequences<T, T>(a, s);
     if (hipError_t e = launch_scan_pack(a, sizeof(T) == 2, s)) return e;
     return sequences<T, Packed>(a, s);
 }
@@ -296,6 +292,13 @@ int scan_padded(int states) {
     int p = 4;
     while (p < states) p *= 2;
     return p;
+}
+// Whether the caller's own rows of b and c do: on four bytes, and of as many states.
+bool scan_direct(const ScanArgs &a, bool bf16) {
+    const auto on_4 = [&](const void *p, int64_t stride) {
+        return reinterpret_cast<uintptr_t>(p) % 4 == 0 && (a.tokens < 2 || stride * (bf16 ? 2 : 4) % 4 == 0);
+    };
+    return a.padded == a.states && on_4(a.b, a.bs) && on_4(a.c, a.cs);
 }
 hipError_t launch_scan_pack(const ScanArgs &a, bool bf16, hipStream_t s) {
     if (a.tokens == 0) return hipSuccess;

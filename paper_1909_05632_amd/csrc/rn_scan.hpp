@@ -150,10 +150,15 @@ __device__ inline __amdgpu_buffer_rsrc_t rows_from(const void *p, int64_t stride
     const char *base = static_cast<const char *>(p) + row * stride * (int)sizeof(T);
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, 0x7fffffff, 0x00027000);
 }
+// The bits as loaded; as a float only where they are used, or each load would be waited for.
 template <class T>
 __device__ inline uint32_t row_load(__amdgpu_buffer_rsrc_t rows, uint32_t lane, int at) {
-    if constexpr (sizeof(T) == 2) return (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(rows, lane, at, 0) << 16;
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_raw_buffer_load_b16(rows, lane, at, 0);
     else return __builtin_amdgcn_raw_buffer_load_b32(rows, lane, at, 0);
+}
+template <class T>
+__device__ inline float row_float(uint32_t bits) {
+    return __uint_as_float(sizeof(T) == 2 ? bits << 16 : bits);
 }
 template <class T>
 __device__ inline void row_store(__amdgpu_buffer_rsrc_t rows, uint32_t lane, int at, T v) {

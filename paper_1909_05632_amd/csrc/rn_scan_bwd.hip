@@ -55,7 +55,7 @@ __device__ inline float over_channels(float (&v)[16]) {
     return r + dpp<0xb1>(r);
 }
 
-// A channel's element of u, dt, z and dout at a token, as float32 bits.
+// A channel's element of u, dt, z and dout at a token, as loaded.
 struct Raw {
     uint32_t u, dt, z, dout;
 };
@@ -76,7 +76,7 @@ struct RawRows {
 
 // dJ/d(state before each chunk but a sequence's first), from 0 behind it, and the
 // chunk's summed step sizes.
-template <class T, int S>
+template <class T, class BC, int S>
 __global__ __launch_bounds__(64) void k_scan_back(ScanArgs a) {
     __shared__ float in[kBatch][2][64];                 // s, p
     const uint32_t block = block_index();
@@ -106,27 +106,34 @@ __global__ __launch_bounds__(64) void k_scan_back(ScanArgs a) {
         for (int i = 0; i < kBatch; ++i) raw[i] = rows.load(lane, min(i, chunk.len - t0 - 1));
     };
     const int last = (chunk.len - 1) / kBatch * kBatch;
-    TokenRows<Packed> rows_c(a, 1, where.group, chunk.begin + chunk.len - 1);
+    constexpr int AT = S * sizeof(BC) <= 32 ? 4 : S <= 16 ? 2 : 1;          // tokens whose scalars are there at once
+    TokenRows<BC> rows_c(a, 1, where.group, chunk.begin + chunk.len - 1);
     fetch(last);
     for (int t0 = last; t0 >= 0; t0 -= kBatch) {
         const int m = min(kBatch, chunk.len - t0);
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-            float s = __uint_as_float(raw[i].dt) + bias, p = __uint_as_float(raw[i].dout);
+            float s = row_float<T>(raw[i].dt) + bias, p = row_float<T>(raw[i].dout);
             if (a.softplus) s = softplus(s);
-            if (a.z) p *= silu(__uint_as_float(raw[i].z));
-            in[i][0][me] = s, in[i][1][me] = p;
+            if (a.z) p *= silu(row_float<T>(raw[i].z));
+            in[i][0][me] = i < m ? s : 0.f, in[i][1][me] = i < m ? p : 0.f;           // past the end nothing happens
         }
         if (t0 > 0) fetch(t0 - kBatch);
 #pragma unroll 1
-        for (int i = m - 1; i >= 0; --i) {
-            Scalars<Packed, S> cc;
-            cc.load(rows_c.at);
-            if (t0 + i > 0) rows_c.at -= rows_c.stride;
-            const float s = in[i][0][me], p = in[i][1][me];
+        for (int i = (m + AT - 1) / AT * AT - 1; i >= 0; i -= AT) {
+            Scalars<BC, S> cc[AT];
 #pragma unroll
-            for (int n = 0; n < S; ++n) g[n] = __builtin_amdgcn_exp2f(s * decay[n]) * fmaf(cc[n], p, g[n]);
-            total += s;
+            for (int k = 0; k < AT; ++k) {
+                cc[k].load(rows_c.at);
+                if (i - k < m && t0 + i - k > 0) rows_c.at -= rows_c.stride;
+            }
+#pragma unroll
+            for (int k = 0; k < AT; ++k) {
+                const float s = in[i - k][0][me], p = in[i - k][1][me];
+#pragma unroll
+                for (int n = 0; n < S; ++n) g[n] = __builtin_amdgcn_exp2f(s * decay[n]) * fmaf(cc[k][n], p, g[n]);
+                total += s;
+            }
         }
     }
 #pragma unroll
@@ -135,14 +142,16 @@ __global__ __launch_bounds__(64) void k_scan_back(ScanArgs a) {
     if (where.live) a.sums[chunk.end * a.channels + c] = total;
 }
 
-// A block takes 64 channels, wave w their states 4 w .. 4 w + 3, and tokens by halves
-// of a tile; W waves.  A token is loaded, and its results are stored, by one of them.
+// A block takes 64 channels, wave w of W their states 4 w .. 4 w + 3.  A token is
+// loaded, and its results are stored, by one of them.
 template <class T, int W>
-__global__ __launch_bounds__(64 * W, W == 4 ? 3 : W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a) {
-    constexpr int HALF = kTile / 2, OWN = W < HALF ? HALF / W : 1;             // a wave's tokens of a half
+__global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a) {
+    // Tokens between barriers: sums of all waves for a whole tile of 64 states are more than the LDS.
+    constexpr int PART = W <= 8 ? kTile : kTile / 2;
+    constexpr int OWN = kTile / W, N = kStates * W, THREADS = 64 * W, PER = kTile * N / THREADS;
     __shared__ float in[kTile][5][64];                  // of each token s, u, p, softplus', dout silu'(z)
-    __shared__ float sum_y[W][kTile][64];               // sum c h, by wave
-    __shared__ float sums[W][HALF][2][64];              // sum g a k, sum g b
+    __shared__ float sums[W][PART][3][64];              // sum g a k, sum g b and sum c h, by wave
+    __shared__ __attribute__((aligned(16))) float sb[kTile][N], sc[kTile][N];
     const uint32_t block = block_index();
     const int cblock = (int)(block % a.blocks), me = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const ScanChannels where(a, cblock, me);
@@ -155,9 +164,6 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 3 : W == 16 ? 4 : 2) void k_scan_b
     const uint32_t lane = (uint32_t)c * sizeof(T), to_lane = where.live ? lane : 0xfffffff0u;
     f32x4 da = {0.f, 0.f, 0.f, 0.f};
     float dd = 0.f, dbias = 0.f;
-    // Token j of this wave's in half k.
-    const auto token = [&](int k, int j) { return k * HALF + w * OWN + j; };
-    const bool helps = w * OWN < HALF;
     for (int64_t slot = walker; slot < a.chunks; slot += a.walkers) {
         ScanChunk chunk = scan_chunk_of(a, seqs, slot);
         if (chunk.seq < 0) continue;
@@ -165,97 +171,87 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 3 : W == 16 ? 4 : 2) void k_scan_b
         f32x4 g = chunk.alone() ? load_states(a, a.dfinal, chunk.seq, c, w * kStates, true)
                                 : load_own(a, a.ends, chunk.end, c, w, true);
         const int64_t kept = scan_kept_slot(a, seqs, chunk);
-        Raw raw[2][OWN];
+        Raw raw[OWN];
+        T raw_b[PER], raw_c[PER];
         f32x4 next_h;
         const auto fetch = [&](int t0) {
             next_h = load_own(a, a.kept, kept + t0 / kTile, c, w, true);
             const RawRows<T> rows(a, chunk.begin + t0);
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int j = 0; j < OWN; ++j) raw[j] = rows.load(lane, min(w * OWN + j, chunk.len - t0 - 1));
 #pragma unroll
-                for (int j = 0; j < OWN; ++j)
-                    if (helps) raw[k][j] = rows.load(lane, min(token(k, j), chunk.len - t0 - 1));
+            for (int i = 0; i < PER; ++i) {
+                const int e = threadIdx.x + i * THREADS, n = min(e % N, a.states - 1);
+                const int64_t t = chunk.begin + min(t0 + e / N, chunk.len - 1);
+                raw_b[i] = static_cast<const T *>(a.b)[t * a.bs + where.group * a.states + n];
+                raw_c[i] = static_cast<const T *>(a.c)[t * a.cs + where.group * a.states + n];
+            }
         };
         const int last = chunk.len > 0 ? (chunk.len - 1) / kTile * kTile : -1;
         if (last >= 0) fetch(last);
         for (int t0 = last; t0 >= 0; t0 -= kTile) {
             const int m = min(kTile, chunk.len - t0);
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int j = 0; j < OWN; ++j) {
-                    if (!helps) continue;
-                    const int t = token(k, j);
-                    const float r = __uint_as_float(raw[k][j].dt) + bias, z = __uint_as_float(raw[k][j].z);
-                    float p = __uint_as_float(raw[k][j].dout);
-                    if (a.z) {
-                        const float gate = sigmoid(z);
-                        in[t][4][me] = p * gate * fmaf(z, 1.f - gate, 1.f);
-                        p *= z * gate;
-                    }
-                    // Past the end, and where no channel is, nothing happens.
-                    const bool live = where.live && t < m;
-                    in[t][0][me] = t < m ? (a.softplus ? softplus(r) : r) : 0.f;
-                    in[t][1][me] = live ? __uint_as_float(raw[k][j].u) : 0.f;
-                    in[t][2][me] = live ? p : 0.f;
-                    in[t][3][me] = a.softplus ? sigmoid(r) : 1.f;
+            for (int j = 0; j < OWN; ++j) {
+                const int t = w * OWN + j;
+                const float r = row_float<T>(raw[j].dt) + bias, z = row_float<T>(raw[j].z);
+                float p = row_float<T>(raw[j].dout);
+                if (a.z) {
+                    const float gate = sigmoid(z);
+                    in[t][4][me] = p * gate * fmaf(z, 1.f - gate, 1.f);
+                    p *= z * gate;
                 }
+                // Past the end, and where no channel is, nothing happens.
+                const bool live = where.live && t < m;
+                in[t][0][me] = t < m ? (a.softplus ? softplus(r) : r) : 0.f;
+                in[t][1][me] = live ? row_float<T>(raw[j].u) : 0.f;
+                in[t][2][me] = live ? p : 0.f;
+                in[t][3][me] = a.softplus ? sigmoid(r) : 1.f;
+            }
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int e = threadIdx.x + i * THREADS, t = e / N, n = e % N;
+                const bool there = t < m && n < a.states;
+                sb[t][n] = there ? to_float(raw_b[i]) : 0.f, sc[t][n] = there ? to_float(raw_c[i]) : 0.f;
+            }
             f32x4 h[kTile + 1];                         // before each token, and after the last
             h[0] = next_h;
             __syncthreads();
             if (t0 > 0) fetch(t0 - kTile);
-            // The scalars of token t, not before `after` is known: there are registers for
-            // those of two tokens, and left alone all of the tile's would come first.
-            const TokenRows<Packed> rows(a, 0, where.group, chunk.begin + t0);
-            const Packed *from = rows.at + w * 2 * kStates;
-            const int stride = (int)rows.stride;
-            struct BC {
-                Scalars<Packed, kStates> b, c;
-            };
-            const auto scalars = [&](int t, float after) {
-                asm volatile("" : "+s"(from) : "v"(after));
-                BC v;
-                v.b.load(from + min(t, m - 1) * stride), v.c.load(from + min(t, m - 1) * stride + kStates);
-                return v;
-            };
-            BC next = scalars(0, h[0][0]);
 #pragma unroll
             for (int t = 0; t < kTile; ++t) {
-                const BC now = next;
-                next = scalars(t + 1 < kTile ? t + 1 : t, h[t][0]);
                 const float st = in[t][0][me], x = st * in[t][1][me];
-                float y = 0.f;
+                const f32x4 b = *reinterpret_cast<const f32x4 *>(&sb[t][w * kStates]);
 #pragma unroll
-                for (int i = 0; i < kStates; ++i) {
-                    h[t + 1][i] = fmaf(x, now.b[i], __builtin_amdgcn_exp2f(st * decay[i]) * h[t][i]);
-                    y = fmaf(now.c[i], h[t + 1][i], y);
-                }
-                if (a.z) sum_y[w][t][me] = y;
+                for (int i = 0; i < kStates; ++i)
+                    h[t + 1][i] = fmaf(x, b[i], __builtin_amdgcn_exp2f(st * decay[i]) * h[t][i]);
             }
 #pragma unroll
-            for (int half = 1; half >= 0; --half) {
+            for (int part = kTile - PART; part >= 0; part -= PART) {
 #pragma unroll
-                for (int t2 = half * HALF + HALF - 2; t2 >= half * HALF; t2 -= 2) {
-                    float v[16];                        // [token][db, dc][state]
+                for (int t2 = part + PART - 2; t2 >= part; t2 -= 2) {
+                    float v[16];                            // [token][db, dc][state]
 #pragma unroll
                     for (int t = t2 + 1; t >= t2; --t) {
                         const float st = in[t][0][me], x = st * in[t][1][me], pt = in[t][2][me];
-                        const BC now = next;
-                        next = scalars(t > 0 ? t - 1 : 0, g[0]);
-                        float *o = v + (t - t2) * 8, ak = 0.f, gb = 0.f;
+                        const f32x4 b = *reinterpret_cast<const f32x4 *>(&sb[t][w * kStates]);
+                        const f32x4 cc = *reinterpret_cast<const f32x4 *>(&sc[t][w * kStates]);
+                        float *o = v + (t - t2) * 8, ak = 0.f, gb = 0.f, y = 0.f;
 #pragma unroll
                         for (int i = 0; i < kStates; ++i) {
                             const float e = __builtin_amdgcn_exp2f(st * decay[i]);
-                            g[i] = fmaf(now.c[i], pt, g[i]);
+                            g[i] = fmaf(cc[i], pt, g[i]);
                             const float gk = g[i] * (e * h[t][i]);
                             ak = fmaf(gk, decay[i], ak);
                             da[i] = fmaf(gk, st, da[i]);
-                            gb = fmaf(now.b[i], g[i], gb);
+                            gb = fmaf(b[i], g[i], gb);
+                            y = fmaf(cc[i], h[t + 1][i], y);
                             o[i] = g[i] * x;
                             o[4 + i] = h[t + 1][i] * pt;
                             g[i] *= e;
                         }
-                        sums[w][t % HALF][0][me] = ak, sums[w][t % HALF][1][me] = gb;
+                        sums[w][t - part][0][me] = ak, sums[w][t - part][1][me] = gb;
+                        if (a.dz) sums[w][t - part][2][me] = y;
                     }
                     const float r = over_channels(v);
                     const int t = t2 + me / 32, n = w * kStates + me / 4 % 4;
@@ -263,29 +259,27 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 3 : W == 16 ? 4 : 2) void k_scan_b
                         a.part_bc[(((int64_t)cblock * a.tokens + chunk.begin + t0 + t) * 2 + me / 16 % 2) * a.states + n] = r;
                 }
                 __syncthreads();
-                if (helps) {
-                    const int64_t first = chunk.begin + t0;
-                    const auto du = rows_from<T>(a.du, a.channels, first), ddt = rows_from<T>(a.ddt, a.channels, first);
-                    const auto dz = rows_from<T>(a.dz, a.channels, first);
+                const int64_t first = chunk.begin + t0;
+                const auto du = rows_from<T>(a.du, a.channels, first), ddt = rows_from<T>(a.ddt, a.channels, first);
+                const auto dz = rows_from<T>(a.dz, a.channels, first);
 #pragma unroll
-                    for (int j = 0; j < OWN; ++j) {
-                        const int t = token(half, j);
-                        if (t >= m) break;
-                        float ak = 0.f, gb = 0.f, y = 0.f;
+                for (int j = 0; j < OWN; ++j) {
+                    const int t = w * OWN + j;
+                    if (t < part || t >= min(m, part + PART)) continue;
+                    float ak = 0.f, gb = 0.f, y = 0.f;
 #pragma unroll
-                        for (int k = 0; k < W; ++k) {
-                            ak += sums[k][t % HALF][0][me], gb += sums[k][t % HALF][1][me];
-                            if (a.dz) y += sum_y[k][t][me];
-                        }
-                        const float uj = in[t][1][me], pj = in[t][2][me], dr = fmaf(uj, gb, ak * kLn2) * in[t][3][me];
-                        dd = fmaf(pj, uj, dd), dbias += dr;
-                        const int at = t * a.channels * (int)sizeof(T);
-                        row_store<T>(du, to_lane, at, from_float<T>(fmaf(in[t][0][me], gb, d * pj)));
-                        row_store<T>(ddt, to_lane, at, from_float<T>(dr));
-                        if (a.dz) row_store<T>(dz, to_lane, at, from_float<T>(in[t][4][me] * fmaf(d, uj, y)));
+                    for (int k = 0; k < W; ++k) {
+                        ak += sums[k][t - part][0][me], gb += sums[k][t - part][1][me];
+                        if (a.dz) y += sums[k][t - part][2][me];
                     }
+                    const float ut = in[t][1][me], pt = in[t][2][me], dr = fmaf(ut, gb, ak * kLn2) * in[t][3][me];
+                    dd = fmaf(pt, ut, dd), dbias += dr;
+                    const int at = t * a.channels * (int)sizeof(T);
+                    row_store<T>(du, to_lane, at, from_float<T>(fmaf(in[t][0][me], gb, d * pt)));
+                    row_store<T>(ddt, to_lane, at, from_float<T>(dr));
+                    if (a.dz) row_store<T>(dz, to_lane, at, from_float<T>(in[t][4][me] * fmaf(d, ut, y)));
                 }
-                if (half) __syncthreads();              // sums is written again; after the other half the next tile's barrier is
+                if (part) __syncthreads();              // sums is written again; behind the last part the next tile's barrier is
             }
         }
         if (chunk.first) store_states(a, a.dstate, chunk.seq, c, w * kStates, where.live, g);
@@ -329,18 +323,22 @@ __global__ __launch_bounds__(1024) void k_scan_sum_d(ScanArgs a) {
 
 template <class T>
 hipError_t backward(const ScanArgs &a, hipStream_t s) {
-    if (hipError_t e = launch_scan_pack(a, sizeof(T) == 2, s)) return e;
-    hipError_t joined = hipSuccess;
+    hipError_t e = hipSuccess;
+    const bool direct = scan_direct(a, sizeof(T) == 2);
+    if (a.parts && !direct) e = launch_scan_pack(a, sizeof(T) == 2, s);
+    if (e) return e;
     for_states(a.states, [&](auto states) {
-        constexpr int S = decltype(states)::value, W = S / kStates;
+        constexpr int S = decltype(states)::value;
+        const dim3 grid = grid_of(a.blocks * a.chunks);
         if (a.parts) {
-            k_scan_back<T, S><<<grid_of(a.blocks * a.chunks), 64, 0, s>>>(a);
-            joined = launch_scan_join_back(a, s);
+            if (direct) k_scan_back<T, T, S><<<grid, 64, 0, s>>>(a);
+            else k_scan_back<T, Packed, S><<<grid, 64, 0, s>>>(a);
+            e = launch_scan_join_back(a, s);
         }
-        k_scan_bwd<T, W><<<grid_of(a.blocks * a.walkers), 64 * W, 0, s>>>(a);
+        k_scan_bwd<T, S / kStates><<<grid_of(a.blocks * a.walkers), 64 * (S / kStates), 0, s>>>(a);
     });
-    if (joined) return joined;
-    if (hipError_t e = hipGetLastError()) return e;
+    if (e) return e;
+    if ((e = hipGetLastError())) return e;
     if (a.tokens > 0)
         k_scan_bc<T><<<grid_of((2 * a.tokens * a.groups * a.states + kScanThreads - 1) / kScanThreads), kScanThreads, 0, s>>>(a);
     k_scan_sum_a<<<column_grid((int64_t)a.channels * a.states), 1024, 0, s>>>(a);
@@ -352,7 +350,7 @@ hipError_t backward(const ScanArgs &a, hipStream_t s) {
 
 // Blocks over the chunks, each of which has a part of da, dd and the bias' gradient.
 int64_t scan_walkers(int64_t chunks, int64_t blocks) {
-    const int64_t w = (2048 + blocks - 1) / blocks;
+    const int64_t w = (4096 + blocks - 1) / blocks;
     return chunks < w ? (chunks > 0 ? chunks : 1) : w;
 }
 
