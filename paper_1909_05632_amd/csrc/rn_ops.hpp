@@ -90,6 +90,7 @@ hipError_t launch_logp_backward(const LogpArgs &a, bool bf16, hipStream_t s);
 struct CausalArgs {
     int n, channels, taps, silu;
     int64_t tokens, xs;
+    int even;                     // tokens / n
     const void *x;
     const float *weight, *bias;
     const int32_t *off;           // [n+1], or NULL: even lengths
@@ -114,6 +115,7 @@ hipError_t launch_causal_step(const CausalArgs &a, bool bf16, hipStream_t s);
 struct ScanArgs {
     int n, channels, groups, states, softplus;
     int64_t tokens;
+    int even;                     // tokens / n
     const void *u, *dt, *b, *c, *z;        // z may be NULL
     int64_t us, dts, bs, cs, zs;
     const float *a, *d, *dt_bias;          // d and dt_bias may be NULL
@@ -129,7 +131,8 @@ struct ScanArgs {
     int padded;                   // states rounded up to 4, 8, 16, 32 or 64
     float *packed;                // [tokens][groups][padded / 4][b, c][4]
     int64_t blocks;               // 64 channels each (scan_blocks)
-    int64_t chunk, chunks;        // tokens of a chunk, slots of chunks: tokens / chunk + n
+    int log_chunk;
+    int64_t chunks;               // slots of chunks: tokens / chunk + n
     bool parts;                   // sequences may have several chunks
     float *ends;                  // [scan_ends] states chunks end with from 0, then begin with
     float *sums;                  // [scan_ends][channels] summed step sizes
@@ -141,16 +144,18 @@ struct ScanArgs {
     int64_t walkers;              // blocks over the chunks (scan_walkers)
     float *part_bc;               // [blocks][tokens][2][states]
     float *part_a, *part_d;       // [walkers][channels][states], [walkers][2][channels]
+
+    __host__ __device__ int64_t chunk() const { return (int64_t)1 << log_chunk; }      // tokens of a chunk
 };
 // Tile k of sequence i, which begins at token `begin`, has kept slot
 // begin / RN_SCAN_KEEP + i + k: below this, and no two tiles share one.
 inline int64_t scan_kept_slots(int64_t tokens, int n) { return tokens / RN_SCAN_KEEP + n; }
 // Chunk c of a sequence of several has slot scan_end_slot + c: of more than `chunk`
 // tokens it moves begin / (chunk / 2) on by its chunks at least.
-__host__ __device__ inline int64_t scan_end_slot(const ScanArgs &a, int begin) { return begin / (a.chunk / 2); }
-inline int64_t scan_ends(int64_t tokens, int64_t chunk) { return tokens / (chunk / 2); }
+__host__ __device__ inline int64_t scan_end_slot(const ScanArgs &a, int begin) { return begin >> (a.log_chunk - 1); }
+inline int64_t scan_ends(int64_t tokens, int log_chunk) { return tokens >> log_chunk ? tokens >> (log_chunk - 1) : 0; }
 int64_t scan_blocks(int channels, int groups);
-int scan_chunk(int64_t tokens, int channels, int groups, bool backward);
+int scan_log_chunk(int64_t tokens, int channels, int groups, bool backward);
 int scan_padded(int states);
 bool scan_direct(const ScanArgs &a, bool bf16);
 hipError_t launch_scan_pack(const ScanArgs &a, bool bf16, hipStream_t s);

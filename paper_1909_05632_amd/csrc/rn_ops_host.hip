@@ -146,6 +146,7 @@ CausalArgs conv_args(const rn_conv_shape *s, const void *x, const float *weight,
     CausalArgs a{};
     a.n = s->n, a.channels = s->channels, a.taps = s->taps, a.silu = s->silu;
     a.tokens = s->tokens, a.xs = s->x_stride;
+    a.even = s->n > 0 ? (int)(s->tokens / s->n) : 0;
     a.x = x, a.weight = weight, a.bias = bias;
     return a;
 }
@@ -173,7 +174,8 @@ const char *bad_scan(const rn_scan_shape *s) {
 bool too_many_states(const rn_scan_shape *s) { return s->states > RN_SCAN_MAX_STATES; }
 
 struct ScanSizes {
-    int64_t blocks, chunk, chunks, walkers;
+    int64_t blocks, chunks, walkers;
+    int log_chunk;
     size_t kept, packed, ends, sums;      // bytes
     size_t part_bc, part_a, part_d;
 };
@@ -182,14 +184,14 @@ ScanSizes scan_sizes(const rn_scan_shape *s, bool backward) {
     ScanSizes z{};
     const size_t row = (size_t)s->channels * 4, states = row * s->states, own = row * ((s->states + 3) / 4 * 4);
     z.blocks = scan_blocks(s->channels, s->groups);
-    z.chunk = scan_chunk(s->tokens, s->channels, s->groups, backward);
-    z.chunks = s->tokens / z.chunk + s->n;
+    z.log_chunk = scan_log_chunk(s->tokens, s->channels, s->groups, backward);
+    z.chunks = (s->tokens >> z.log_chunk) + s->n;
     z.walkers = scan_walkers(z.chunks, z.blocks);
     z.kept = round_up(scan_kept_slots(s->tokens, s->n) * own);
     // Calls may need it by the address of bfloat16 b and c, which is not known here.
     if (const int padded = scan_padded(s->states); s->dtype == RN_BF16 || padded != s->states)
         z.packed = round_up((size_t)s->tokens * s->groups * 2 * padded * 4);
-    const size_t ends = s->tokens > z.chunk ? scan_ends(s->tokens, z.chunk) : 0;
+    const size_t ends = scan_ends(s->tokens, z.log_chunk);
     z.ends = round_up(ends * own), z.sums = round_up(ends * row);
     if (backward) {
         z.part_bc = round_up((size_t)z.blocks * s->tokens * 2 * s->states * 4);
@@ -225,8 +227,9 @@ ScanArgs scan_args(const rn_scan_shape *s, const rn_scan_inputs *in, const int32
     a.a = in->a, a.d = in->d, a.dt_bias = in->dt_bias;
     a.off = seq_off;
     a.whole_states = s->states % 4 == 0 && on_16(a.a);
-    a.blocks = z.blocks, a.chunk = z.chunk, a.chunks = z.chunks, a.walkers = z.walkers;
-    a.parts = (seq_off || s->n == 0 ? s->tokens : s->tokens / s->n) > z.chunk;
+    a.even = s->n > 0 ? (int)(s->tokens / s->n) : 0;
+    a.blocks = z.blocks, a.log_chunk = z.log_chunk, a.chunks = z.chunks, a.walkers = z.walkers;
+    a.parts = (seq_off || s->n == 0 ? s->tokens : a.even) > a.chunk();
     a.padded = scan_padded(s->states);
     char *at = static_cast<char *>(scratch);
     a.packed = reinterpret_cast<float *>(at);

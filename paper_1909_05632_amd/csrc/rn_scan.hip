@@ -41,9 +41,9 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_join(ScanArgs a) {
     const int64_t per = (int64_t)a.channels * quads, i = (int64_t)block_index() * kScanThreads + threadIdx.x;
     if (i >= per * a.n) return;
     const int seq = (int)(i / per), quad = (int)(i % per / a.channels), c = (int)(i % a.channels);
-    const Seqs seqs{a.off, a.n, a.tokens};
+    const Seqs seqs{a.off, a.n, a.tokens, a.even};
     const int begin = seqs.offset(seq), len = max(0, seqs.offset(seq + 1) - begin);
-    const int64_t slot = scan_end_slot(a, begin), count = (len + a.chunk - 1) / a.chunk;
+    const int64_t slot = scan_end_slot(a, begin), count = (len + a.chunk() - 1) >> a.log_chunk;
     if (count < 2) return;
     const f32x4 decay = load_states(a, a.a, 0, c, quad * kStates, true) * kLog2e;
     f32x4 h = load_states(a, BACK ? a.dfinal : a.state, seq, c, quad * kStates, true);
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(64) void k_scan_seq(ScanArgs a) {
     const ScanChannels where(a, (int)(block % a.blocks), me);
     const int64_t slot = block / a.blocks;
     if (slot >= a.chunks) return;
-    const Seqs seqs{a.off, a.n, a.tokens};
+    const Seqs seqs{a.off, a.n, a.tokens, a.even};
     ScanChunk chunk = scan_chunk_of(a, seqs, slot);
     if (chunk.seq < 0 || (LOCAL && chunk.last)) return;
     chunk.begin = __builtin_amdgcn_readfirstlane(chunk.begin), chunk.len = __builtin_amdgcn_readfirstlane(chunk.len);
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(64) void k_scan_seq(ScanArgs a) {
         const auto z = rows_from<T>(LOCAL || !a.z ? a.u : a.z, LOCAL || !a.z ? a.us : a.zs, first);
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-            const int r = min(i, chunk.len - t0 - 1) * (int)sizeof(T);
+            const int r = min(i, chunk.len - 1 - t0) * (int)sizeof(T);
             ru[i] = row_load<T>(u, lane, r * (int)a.us), rdt[i] = row_load<T>(dt, lane, r * (int)a.dts);
             if (!LOCAL) rz[i] = row_load<T>(z, lane, r * (int)(a.z ? a.zs : a.us));
         }
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(64) void k_scan_seq(ScanArgs a) {
             if (a.softplus) s = softplus(s);
             sx[i][0][me] = i < m ? s : 0.f, sx[i][1][me] = i < m ? s * v[i] : 0.f;     // past the end nothing happens
         }
-        if (t0 + kBatch < chunk.len) fetch(t0 + kBatch);
+        fetch(min(t0 + kBatch, chunk.len - 1));         // without a branch, so that nothing waits for it here
         if (!LOCAL && a.kept && t0 % kTile == 0)
 #pragma unroll
             for (int q = 0; q < S / kStates; ++q)
@@ -277,14 +277,14 @@ int64_t scan_blocks(int channels, int groups) { return (int64_t)groups * ((chann
 
 // Chunks so long that all tokens' are as many blocks as fill the GPU (8 waves a SIMD
 // forward; 2048 blocks of as many waves as a channel has quads of states backward),
-// but no shorter than kShortest: below, what the chunks' ends cost is more than what
-// they free.
-int scan_chunk(int64_t tokens, int channels, int groups, bool backward) {
-    constexpr int64_t kShortest = 64;
-    const int64_t blocks = backward ? 2048 : 8192;
-    int64_t c = (tokens * scan_blocks(channels, groups) + blocks - 1) / blocks;
-    c = (c + RN_SCAN_KEEP - 1) / RN_SCAN_KEEP * RN_SCAN_KEEP;
-    return (int)(c < kShortest ? kShortest : c < (1 << 30) ? c : 1 << 30);
+// but no shorter than 2^kShortest: below, what the chunks' ends cost is more than
+// what they free.
+int scan_log_chunk(int64_t tokens, int channels, int groups, bool backward) {
+    constexpr int kShortest = 6;
+    const int64_t blocks = backward ? 2048 : 8192, want = (tokens * scan_blocks(channels, groups) + blocks - 1) / blocks;
+    int l = kShortest;
+    while (l < 30 && ((int64_t)1 << l) < want) ++l;
+    return l;
 }
 
 // States of a channel as the kernels see them.

@@ -28,14 +28,14 @@ __device__ inline ScanChunk scan_chunk_of(const ScanArgs &a, const Seqs &s, int6
     int lo = 0, hi = a.n - 1;
     while (lo < hi) {                                   // 64 places at once; uniform within a wave
         const int step = (hi - lo + 63) / 64, at = lo + ((int)(threadIdx.x & 63) + 1) * step;
-        const bool up = at <= hi && (int64_t)s.offset(min(at, hi)) / a.chunk + at <= slot;
+        const bool up = at <= hi && (int64_t)(s.offset(min(at, hi)) >> a.log_chunk) + at <= slot;
         lo += __popcll(__ballot(up)) * step;
         hi = min(hi, lo + step - 1);
     }
     const int begin = s.offset(lo), len = max(0, s.offset(lo + 1) - begin);
-    const int64_t c = slot - (begin / a.chunk + lo), at = c * a.chunk;
+    const int64_t c = slot - ((begin >> a.log_chunk) + lo), at = c << a.log_chunk;
     if (c < 0 || (at >= len && c > 0)) return {-1, 0, 0, false, false, 0};
-    return {lo, begin + (int)at, (int)min((int64_t)a.chunk, len - at), c == 0, at + a.chunk >= len,
+    return {lo, begin + (int)at, (int)min(a.chunk(), len - at), c == 0, at + a.chunk() >= len,
             scan_end_slot(a, begin) + c};
 }
 

@@ -84,7 +84,7 @@ __global__ __launch_bounds__(64) void k_scan_back(ScanArgs a) {
     const ScanChannels where(a, (int)(block % a.blocks), me);
     const int64_t slot = block / a.blocks;
     if (slot >= a.chunks) return;
-    const Seqs seqs{a.off, a.n, a.tokens};
+    const Seqs seqs{a.off, a.n, a.tokens, a.even};
     ScanChunk chunk = scan_chunk_of(a, seqs, slot);
     if (chunk.seq < 0 || chunk.first) return;
     chunk.begin = __builtin_amdgcn_readfirstlane(chunk.begin), chunk.len = __builtin_amdgcn_readfirstlane(chunk.len);
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(64) void k_scan_back(ScanArgs a) {
             if (a.z) p *= silu(row_float<T>(raw[i].z));
             in[i][0][me] = i < m ? s : 0.f, in[i][1][me] = i < m ? p : 0.f;           // past the end nothing happens
         }
-        if (t0 > 0) fetch(t0 - kBatch);
+        fetch(max(t0 - kBatch, 0));                     // without a branch, so that nothing waits for it here
 #pragma unroll 1
         for (int i = (m + AT - 1) / AT * AT - 1; i >= 0; i -= AT) {
             Scalars<BC, S> cc[AT];
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
     const ScanChannels where(a, cblock, me);
     const int64_t walker = block / a.blocks;
     if (walker >= a.walkers) return;
-    const Seqs seqs{a.off, a.n, a.tokens};
+    const Seqs seqs{a.off, a.n, a.tokens, a.even};
     const int c = where.c;
     const f32x4 decay = load_states(a, a.a, 0, c, w * kStates, true) * kLog2e;
     const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, d = a.d ? a.d[c] : 0.f;
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
             f32x4 h[kTile + 1];                         // before each token, and after the last
             h[0] = next_h;
             __syncthreads();
-            if (t0 > 0) fetch(t0 - kTile);
+            fetch(max(t0 - kTile, 0));                  // without a branch, so that nothing waits for it here
 #pragma unroll
             for (int t = 0; t < kTile; ++t) {
                 const float st = in[t][0][me], x = st * in[t][1][me];

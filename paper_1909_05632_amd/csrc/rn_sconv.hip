@@ -114,7 +114,7 @@ template <class T, int VEC, int K>
 __global__ __launch_bounds__(kThreads) void k_conv_seq(CausalArgs a) {
     const Place p(a, VEC);
     if (p.c >= a.channels) return;
-    const Seqs s{a.off, a.n, a.tokens};
+    const Seqs s{a.off, a.n, a.tokens, a.even};
     if (p.ends) return final_row<T, VEC, K>(a, s, p);
     const int64_t from = p.run * kRun;
     if (from >= a.tokens) return;
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(CausalArgs a) {
     constexpr int N = (K + 1) * VEC;
     __shared__ float sum[N][kThreads];
     const Place p(a, VEC);
-    const Seqs s{a.off, a.n, a.tokens};
+    const Seqs s{a.off, a.n, a.tokens, a.even};
     if (p.ends) {
         if (p.c < a.channels) window_row<T, VEC, K>(a, s, p);
         return;

@@ -11,14 +11,15 @@ struct Seqs {
     const int32_t *off;           // [n+1], or NULL: even lengths
     int n;
     int64_t tokens;
+    int even;                     // tokens / n
     // Within the arrays whatever the offsets say.
     __device__ int offset(int i) const {
-        const int64_t t = off ? off[i] : tokens / n * i;
+        const int64_t t = off ? off[i] : (int64_t)even * i;
         return (int)(t < 0 ? 0 : t < tokens ? t : tokens);
     }
     // The sequence that owns token t: the last that does not begin behind it.
     __device__ int of(int t) const {
-        if (!off) return (int)(t / (tokens / n));
+        if (!off) return t / even;
         int lo = 0, hi = n - 1;
         while (lo < hi) {
             const int mid = lo + (hi - lo + 1) / 2;
