@@ -99,7 +99,7 @@ __global__ __launch_bounds__(64) void k_scan_seq(ScanArgs a) {
     // A lane's own numbers, put by so that the tokens' loop can be a loop: unrolled, it
     // would have the scalars of all its tokens at once.
     __shared__ float sx[kBatch][2][64];                 // s, then y; s u
-    const uint32_t lane = (uint32_t)c * sizeof(T), to_lane = live ? lane : 0xfffffff0u;
+    const uint32_t lane = (uint32_t)c * sizeof(T), to_lane = live ? lane : kNowhere;
     uint32_t ru[kBatch], rdt[kBatch], rz[kBatch];
     const auto fetch = [&](int t0) {                    // tokens past the last are it
         const int64_t first = chunk.begin + t0;
@@ -128,10 +128,11 @@ __global__ __launch_bounds__(64) void k_scan_seq(ScanArgs a) {
             sx[i][0][me] = i < m ? s : 0.f, sx[i][1][me] = i < m ? s * v[i] : 0.f;     // past the end nothing happens
         }
         fetch(min(t0 + kBatch, chunk.len - 1));         // without a branch, so that nothing waits for it here
-        if (!LOCAL && a.kept && t0 % kTile == 0)
+        if (!LOCAL)
 #pragma unroll
             for (int q = 0; q < S / kStates; ++q)
-                store_own(a, a.kept, kept + t0 / kTile, c, q, live, f32x4{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]});
+                store_own_if(live && t0 % kTile == 0, a, a.kept, kept + t0 / kTile, c, q,
+                             f32x4{h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]});
 #pragma unroll 1
         for (int i = 0; i < m; i += AT) {
             Scalars<BC, S> b[AT], cc[AT];
@@ -166,8 +167,8 @@ __global__ __launch_bounds__(64) void k_scan_seq(ScanArgs a) {
             const auto out = rows_from<T>(a.out, a.channels, chunk.begin + t0);
 #pragma unroll
             for (int i = 0; i < kBatch; ++i)
-                if (i < m)
-                    row_store<T>(out, to_lane, i * a.channels * (int)sizeof(T), from_float<T>(fmaf(d, v[i], sx[i][0][me]) * gate[i]));
+                row_store<T>(out, i < m ? to_lane : kNowhere, i * a.channels * (int)sizeof(T),
+                             from_float<T>(fmaf(d, v[i], sx[i][0][me]) * gate[i]));
         }
     }
 #pragma unroll
@@ -276,12 +277,12 @@ hipError_t step(const ScanArgs &a, hipStream_t s) {
 int64_t scan_blocks(int channels, int groups) { return (int64_t)groups * ((channels / groups + 63) / 64); }
 
 // Chunks so long that all tokens' are as many blocks as fill the GPU (8 waves a SIMD
-// forward; 2048 blocks of as many waves as a channel has quads of states backward),
+// forward; half of that backward, where what follows takes more of them),
 // but no shorter than 2^kShortest: below, what the chunks' ends cost is more than
 // what they free.
 int scan_log_chunk(int64_t tokens, int channels, int groups, bool backward) {
     constexpr int kShortest = 6;
-    const int64_t blocks = backward ? 2048 : 8192, want = (tokens * scan_blocks(channels, groups) + blocks - 1) / blocks;
+    const int64_t blocks = backward ? 4096 : 8192, want = (tokens * scan_blocks(channels, groups) + blocks - 1) / blocks;
     int l = kShortest;
     while (l < 30 && ((int64_t)1 << l) < want) ++l;
     return l;

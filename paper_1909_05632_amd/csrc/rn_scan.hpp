@@ -116,6 +116,13 @@ __device__ inline f32x4 load_own(const ScanArgs &a, float *p, int64_t row, int c
 __device__ inline void store_own(const ScanArgs &a, float *p, int64_t row, int c, int quad, bool live, f32x4 v) {
     if (live && quad * kStates < a.states) *own_states(a, p, row, c, quad) = v;
 }
+// Without a branch, p NULL or not.
+__device__ inline void store_own_if(bool in, const ScanArgs &a, float *p, int64_t row, int c, int quad, f32x4 v) {
+    const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(own_states(a, p, row, 0, 0), 0, 0x7fffffff, 0x00027000);
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const bool there = in && p && quad * kStates < a.states;
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rows, there ? (uint32_t)(quad * a.channels + c) * 16 : 0xfffffff0u, 0, 0);
+}
 
 // b and c in float32, as k_scan_pack leaves them: a token's and group's quads of
 // states, four of b and then four of c each, the last of them 0.
@@ -150,6 +157,9 @@ __device__ inline __amdgpu_buffer_rsrc_t rows_from(const void *p, int64_t stride
     const char *base = static_cast<const char *>(p) + row * stride * (int)sizeof(T);
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, 0x7fffffff, 0x00027000);
 }
+// Stores go without branches (what goes to kNowhere is past every array's end, and dropped), so
+// that the number of them in flight is known, and a wait for loads not one for stores.
+constexpr uint32_t kNowhere = 0xfffffff0u;
 // The bits as loaded; as a float only where they are used, or each load would be waited for.
 template <class T>
 __device__ inline uint32_t row_load(__amdgpu_buffer_rsrc_t rows, uint32_t lane, int at) {

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
     const int c = where.c;
     const f32x4 decay = load_states(a, a.a, 0, c, w * kStates, true) * kLog2e;
     const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, d = a.d ? a.d[c] : 0.f;
-    const uint32_t lane = (uint32_t)c * sizeof(T), to_lane = where.live ? lane : 0xfffffff0u;
+    const uint32_t lane = (uint32_t)c * sizeof(T), to_lane = where.live ? lane : kNowhere;
     f32x4 da = {0.f, 0.f, 0.f, 0.f};
     float dd = 0.f, dbias = 0.f;
     for (int64_t slot = walker; slot < a.chunks; slot += a.walkers) {
@@ -218,14 +218,27 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
             h[0] = next_h;
             __syncthreads();
             fetch(max(t0 - kTile, 0));                  // without a branch, so that nothing waits for it here
+            // What a token needs is on its way from LDS during the one before.
+            struct Token {
+                float s, u, p;
+                f32x4 b, c;
+            };
+            const auto token = [&](int t) {
+                return Token{in[t][0][me], in[t][1][me], in[t][2][me], *reinterpret_cast<const f32x4 *>(&sb[t][w * kStates]),
+                             *reinterpret_cast<const f32x4 *>(&sc[t][w * kStates])};
+            };
+            Token next = token(0);
 #pragma unroll
             for (int t = 0; t < kTile; ++t) {
-                const float st = in[t][0][me], x = st * in[t][1][me];
-                const f32x4 b = *reinterpret_cast<const f32x4 *>(&sb[t][w * kStates]);
+                const Token now = next;
+                next = token(t + 1 < kTile ? t + 1 : t);
+                __builtin_amdgcn_sched_barrier(0);
+                const float x = now.s * now.u;
 #pragma unroll
                 for (int i = 0; i < kStates; ++i)
-                    h[t + 1][i] = fmaf(x, b[i], __builtin_amdgcn_exp2f(st * decay[i]) * h[t][i]);
+                    h[t + 1][i] = fmaf(x, now.b[i], __builtin_amdgcn_exp2f(now.s * decay[i]) * h[t][i]);
             }
+            const auto part_bc = rows_from<float>(a.part_bc, 2 * a.states, (int64_t)cblock * a.tokens + chunk.begin + t0);
 #pragma unroll
             for (int part = kTile - PART; part >= 0; part -= PART) {
 #pragma unroll
@@ -233,9 +246,11 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
                     float v[16];                            // [token][db, dc][state]
 #pragma unroll
                     for (int t = t2 + 1; t >= t2; --t) {
-                        const float st = in[t][0][me], x = st * in[t][1][me], pt = in[t][2][me];
-                        const f32x4 b = *reinterpret_cast<const f32x4 *>(&sb[t][w * kStates]);
-                        const f32x4 cc = *reinterpret_cast<const f32x4 *>(&sc[t][w * kStates]);
+                        const Token now = next;
+                        if (t > 0) next = token(t - 1);
+                        __builtin_amdgcn_sched_barrier(0);
+                        const float st = now.s, x = st * now.u, pt = now.p;
+                        const f32x4 b = now.b, cc = now.c;
                         float *o = v + (t - t2) * 8, ak = 0.f, gb = 0.f, y = 0.f;
 #pragma unroll
                         for (int i = 0; i < kStates; ++i) {
@@ -251,12 +266,12 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
                             g[i] *= e;
                         }
                         sums[w][t - part][0][me] = ak, sums[w][t - part][1][me] = gb;
-                        if (a.dz) sums[w][t - part][2][me] = y;
+                        sums[w][t - part][2][me] = y;
                     }
                     const float r = over_channels(v);
                     const int t = t2 + me / 32, n = w * kStates + me / 4 % 4;
-                    if (me % 4 == 0 && t < m && n < a.states)
-                        a.part_bc[(((int64_t)cblock * a.tokens + chunk.begin + t0 + t) * 2 + me / 16 % 2) * a.states + n] = r;
+                    const bool there = me % 4 == 0 && t < m && n < a.states;
+                    row_store<float>(part_bc, there ? ((t * 2 + me / 16 % 2) * a.states + n) * 4 : kNowhere, 0, r);
                 }
                 __syncthreads();
                 const int64_t first = chunk.begin + t0;
@@ -265,19 +280,20 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
 #pragma unroll
                 for (int j = 0; j < OWN; ++j) {
                     const int t = w * OWN + j;
-                    if (t < part || t >= min(m, part + PART)) continue;
+                    if (t < part || t >= part + PART) continue;     // a wave's one token, where there are two parts
+                    const uint32_t to = t < m ? to_lane : kNowhere;
                     float ak = 0.f, gb = 0.f, y = 0.f;
 #pragma unroll
                     for (int k = 0; k < W; ++k) {
                         ak += sums[k][t - part][0][me], gb += sums[k][t - part][1][me];
-                        if (a.dz) y += sums[k][t - part][2][me];
+                        y += sums[k][t - part][2][me];
                     }
                     const float ut = in[t][1][me], pt = in[t][2][me], dr = fmaf(ut, gb, ak * kLn2) * in[t][3][me];
-                    dd = fmaf(pt, ut, dd), dbias += dr;
+                    dd = fmaf(pt, ut, dd), dbias += t < m ? dr : 0.f;
                     const int at = t * a.channels * (int)sizeof(T);
-                    row_store<T>(du, to_lane, at, from_float<T>(fmaf(in[t][0][me], gb, d * pt)));
-                    row_store<T>(ddt, to_lane, at, from_float<T>(dr));
-                    if (a.dz) row_store<T>(dz, to_lane, at, from_float<T>(in[t][4][me] * fmaf(d, ut, y)));
+                    row_store<T>(du, to, at, from_float<T>(fmaf(in[t][0][me], gb, d * pt)));
+                    row_store<T>(ddt, to, at, from_float<T>(dr));
+                    row_store<T>(dz, a.dz ? to : kNowhere, at, from_float<T>(in[t][4][me] * fmaf(d, ut, y)));
                 }
                 if (part) __syncthreads();              // sums is written again; behind the last part the next tile's barrier is
             }
@@ -307,6 +323,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_bc(ScanArgs a) {
     const float *p = a.part_bc + ((group * of * a.tokens + t) * 2 + kind) * a.states + n;
     const int64_t on = a.tokens * 2 * a.states;
     float v = 0.f;
+#pragma unroll 8
     for (int64_t k = 0; k < of; ++k) v += p[k * on];
     static_cast<T *>(kind ? a.dc : a.db)[t * per + group * a.states + n] = from_float<T>(v);
 }
