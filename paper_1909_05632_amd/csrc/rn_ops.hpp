@@ -103,11 +103,11 @@ struct CausalArgs {
     const void *dout, *dfinal;
     void *dx, *dwindow;
     float *dweight, *dbias;
-    float *part;                  // [run_blocks][channels (taps + 1)], causal_parts(tokens) rows at most
-    // Set by the launcher: threads of a block over the channels, rows of blocks over the tokens.
-    int lanes, run_blocks;
+    float *part;                  // [run_blocks][channels (taps + 1)], causal_parts rows at most
+    // Set by the launcher: threads of a block over the channels, rows of blocks over the tokens, tokens a thread.
+    int lanes, run_blocks, run;
 };
-int64_t causal_parts(int64_t tokens);
+int64_t causal_parts(int64_t tokens, int channels);
 hipError_t launch_causal(const CausalArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_causal_backward(const CausalArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_causal_step(const CausalArgs &a, bool bf16, hipStream_t s);

@@ -462,7 +462,7 @@ rn_status reuse_ops_causal_conv(const rn_conv_shape *shape, const void *x, const
 
 size_t reuse_ops_causal_conv_backward_scratch_bytes(const rn_conv_shape *shape) {
     if (bad_conv(shape)) return 0;
-    return round_up((size_t)causal_parts(shape->tokens) * shape->channels * (shape->taps + 1) * 4) + kAlign;
+    return round_up((size_t)causal_parts(shape->tokens, shape->channels) * shape->channels * (shape->taps + 1) * 4) + kAlign;
 }
 
 rn_status reuse_ops_causal_conv_backward(const rn_conv_shape *shape, const void *x, const float *weight,

@@ -71,7 +71,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_join(ScanArgs a) {
 // registers of its lane.  LOCAL: of every chunk but a sequence's last, the state at
 // its end from 0, and its summed step sizes.
 template <class T, class BC, int S, bool LOCAL>
-__global__ __launch_bounds__(64) void k_scan_seq(ScanArgs a) {
+__global__ __launch_bounds__(64, S <= 16 ? 5 : 1) void k_scan_seq(ScanArgs a) {
     const uint32_t block = block_index();
     const int me = threadIdx.x;
     const ScanChannels where(a, (int)(block % a.blocks), me);

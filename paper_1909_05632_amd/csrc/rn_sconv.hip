@@ -17,7 +17,6 @@ namespace {
 
 using namespace ops;
 
-constexpr int kRun = 32;          // tokens a thread
 constexpr int kAhead = 4;         // rows whose loads are on their way at once
 
 // The channels' weights, and their inputs at the last K - 1 tokens, oldest first.
@@ -79,7 +78,7 @@ struct Taps {
 };
 
 // Where a thread works: `lanes` threads side by side over the channels, 256 / lanes
-// runs a block.  The blocks behind the last run take the sequences' ends.
+// runs of a.run tokens a block.  The blocks behind the last run take the sequences' ends.
 struct Place {
     int c;                        // first channel, or beyond the last
     int64_t run;                  // run of tokens, or row of the sequences' ends
@@ -116,9 +115,9 @@ __global__ __launch_bounds__(kThreads) void k_conv_seq(CausalArgs a) {
     if (p.c >= a.channels) return;
     const Seqs s{a.off, a.n, a.tokens, a.even};
     if (p.ends) return final_row<T, VEC, K>(a, s, p);
-    const int64_t from = p.run * kRun;
+    const int64_t from = p.run * a.run;
     if (from >= a.tokens) return;
-    const int to = (int)min(from + kRun, a.tokens);
+    const int to = (int)min(from + a.run, a.tokens);
     int t = (int)from;
     At at(s, t);
     Taps<T, VEC, K> taps;
@@ -126,10 +125,20 @@ __global__ __launch_bounds__(kThreads) void k_conv_seq(CausalArgs a) {
     taps.before(a, at.seq, at.begin, t, p.c);
     const T *x = static_cast<const T *>(a.x) + p.c;
     T *out = static_cast<T *>(a.out) + p.c;
+    Pack<T, VEC> next[kAhead];
+    const auto fetch = [&](int from) {                  // the next rows are on their way while these are worked on
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            next[u] = *reinterpret_cast<const Pack<T, VEC> *>(x + (int64_t)min(from + u, to - 1) * a.xs);
+    };
+    fetch(t);
     for (; t < to; t += kAhead) {
         float now[kAhead][VEC];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) load_as<T, VEC>(x + (int64_t)min(t + u, to - 1) * a.xs, now[u]);
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) now[u][j] = to_float(next[u].v[j]);
+        fetch(t + kAhead);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (t + u >= to) break;
@@ -201,9 +210,9 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(CausalArgs a) {
 #pragma unroll
         for (int k = 0; k < K; ++k) dw[k][j] = 0.f;
     }
-    const int64_t from = p.run * kRun;
+    const int64_t from = p.run * a.run;
     if (from < a.tokens && p.c < a.channels) {
-        const int first = (int)from, to = (int)min(from + kRun, a.tokens);
+        const int first = (int)from, to = (int)min(from + a.run, a.tokens);
         int t = first;
         At at(s, t);
         Taps<T, VEC, K> taps;
@@ -219,14 +228,24 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(CausalArgs a) {
         // The tokens behind the run that its own are seen by.
         const auto stop_of = [&] { return max(to, min(to + K - 1, at.end)); };
         int stop = at.end < to ? to : stop_of();
+        // The next rows are on their way while these are worked on.
+        Pack<T, VEC> next_x[kAhead], next_g[kAhead];
+        const auto fetch = [&](int from) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t row = min((int64_t)from + u, a.tokens - 1);
+                next_x[u] = *reinterpret_cast<const Pack<T, VEC> *>(x + row * a.xs);
+                next_g[u] = *reinterpret_cast<const Pack<T, VEC> *>(dout + row * a.channels);
+            }
+        };
+        fetch(t);
         for (; t < stop; t += kAhead) {
             float now[kAhead][VEC], g[kAhead][VEC];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int64_t row = min((int64_t)t + u, a.tokens - 1);
-                load_as<T, VEC>(x + row * a.xs, now[u]);
-                load_as<T, VEC>(dout + row * a.channels, g[u]);
-            }
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) now[u][j] = to_float(next_x[u].v[j]), g[u][j] = to_float(next_g[u].v[j]);
+            fetch(t + kAhead);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int i = t + u;
@@ -364,12 +383,22 @@ int lanes_of(int channels, int vec) {
     return l;
 }
 
+// Tokens a thread: half as many where that leaves fewer than 2048 waves of 8 channels
+// a lane.  16384 x 4096 bfloat16 forward take 56 us with 32 and 59 with 64, backward 112
+// and 103; 2048 x 2048 forward 9 us with 8 and 17 with 32, backward 24 with 8 and 66 with 64.
+int run_of(int64_t tokens, int channels, bool backward) {
+    int r = backward ? 64 : 32;
+    while (r > 8 && tokens * channels / (8 * 64) / r < 2048) r /= 2;
+    return r;
+}
+
 template <class T, int VEC>
 hipError_t run(CausalArgs a, bool backward, hipStream_t s) {
     a.lanes = lanes_of(a.channels, VEC);
+    a.run = run_of(a.tokens, a.channels, backward);
     const int64_t per = kThreads / a.lanes;
     const bool ends = a.taps > 1 && (backward ? a.dwindow : a.final_window);
-    const int64_t runs = (a.tokens + kRun - 1) / kRun, rows = ends ? (int64_t)a.n * (a.taps - 1) : 0;
+    const int64_t runs = (a.tokens + a.run - 1) / a.run, rows = ends ? (int64_t)a.n * (a.taps - 1) : 0;
     a.run_blocks = (int)((runs + per - 1) / per);
     const int64_t across = (a.channels + a.lanes * VEC - 1) / (a.lanes * VEC);
     const int64_t blocks = across * (a.run_blocks + (rows + per - 1) / per);
@@ -402,7 +431,10 @@ hipError_t dispatch(const CausalArgs &a, bool backward, hipStream_t s) {
 
 // Rows of partial weight gradients: the most that a call of this size has, whatever
 // its alignment (kThreads / 64 runs of tokens a block, or more).
-int64_t causal_parts(int64_t tokens) { return (tokens + kRun * (kThreads / 64) - 1) / (kRun * (kThreads / 64)); }
+int64_t causal_parts(int64_t tokens, int channels) {
+    const int64_t per = (int64_t)run_of(tokens, channels, true) * (ops::kThreads / 64);
+    return (tokens + per - 1) / per;
+}
 
 hipError_t launch_causal(const CausalArgs &a, bool bf16, hipStream_t s) {
     return bf16 ? dispatch<bf16_t>(a, false, s) : dispatch<float>(a, false, s);
