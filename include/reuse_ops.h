@@ -332,8 +332,10 @@ rn_status reuse_ops_causal_conv_step(const rn_conv_shape *shape, const void *dev
                                      const float *dev_bias, const int32_t *dev_stream_ids, int32_t slots,
                                      void *dev_window, void *dev_out, void *hip_stream);
 
-/* All tokens of n sequences packed one after another, as reuse_ops_delta_forward's.
- *   dev_seq_off: [n+1] int32, or NULL: every sequence has tokens / n.
+/* All tokens of n sequences packed one after another.
+ *   dev_seq_off: [n+1] int32, ascending, or NULL: every sequence has tokens / n.  Tokens
+ *                behind seq_off[n] (a padded batch) are no sequence's: their results
+ *                are left as they were, and they have no part in any other's.
  *   dev_window:  [n][taps - 1][channels] dtype before the first token, or NULL for 0.
  *   dev_final:   the same after the last token, or NULL; not dev_window.
  *   dev_out:     [tokens][channels] dtype, contiguous; not x. */
@@ -414,11 +416,11 @@ size_t reuse_ops_scan_saved_bytes(const rn_scan_shape *shape);
 size_t reuse_ops_scan_scratch_bytes(const rn_scan_shape *shape);
 size_t reuse_ops_scan_backward_scratch_bytes(const rn_scan_shape *shape);
 
-/* All tokens of n sequences packed one after another, as reuse_ops_delta_forward's.
- *   dev_seq_off: [n+1] int32, or NULL: every sequence has tokens / n.
+/* All tokens of n sequences packed one after another.
+ *   dev_seq_off: as reuse_ops_causal_conv's.
  *   dev_state:   [n][channels][states] float32 before the first token, or NULL for 0.
  *   dev_final:   the same after the last token, or NULL; it may be dev_state.
- *   dev_out:     [tokens][channels] dtype, contiguous.
+ *   dev_out:     [tokens][channels] dtype, contiguous; not one of the inputs.
  *   dev_saved:   NULL, or reuse_ops_scan_saved_bytes bytes for the backward call.
  *   dev_scratch: reuse_ops_scan_scratch_bytes bytes; saved and scratch are 256-byte
  *                aligned. */
@@ -436,7 +438,7 @@ typedef struct {
 
 /* Gradients of J given dout = dJ/dout ([tokens][channels] dtype, contiguous) and
  * dfinal = dJ/dfinal (NULL: 0), for the inputs and the saved buffer of a forward
- * call.  dstate must not be dfinal. */
+ * call.  No gradient lies over dout or an input; dstate is not dfinal. */
 rn_status reuse_ops_scan_backward(const rn_scan_shape *shape, const rn_scan_inputs *in, const int32_t *dev_seq_off,
                                   const void *dev_saved, size_t saved_bytes, const void *dev_dout,
                                   const float *dev_dfinal, const rn_scan_grads *grads, void *dev_scratch,

@@ -204,6 +204,10 @@ size_t scan_bytes(const ScanSizes &z) {
     return z.packed + z.ends + z.sums + z.part_bc + z.part_a + z.part_d + kAlign;
 }
 
+bool is_input(const rn_scan_inputs *in, const void *p) {
+    return p && (p == in->u || p == in->dt || p == in->b || p == in->c || p == in->z);
+}
+
 bool on_16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 rn_status check_scan(const rn_scan_shape *s, const rn_scan_inputs *in) {
@@ -495,8 +499,11 @@ rn_status reuse_ops_scan_step(const rn_scan_shape *shape, const rn_scan_inputs *
     if (slots < 0 || (!ids && slots < shape->n)) return fail(RN_EINVAL, "fewer slots than streams");
     if (shape->n == 0) return RN_OK;
     if (!state || !out) return fail(RN_EINVAL, "state and out must not be NULL");
-    if (shape->n > 1 && out == in->u && shape->u_stride != shape->channels)
+    if (shape->n > 1 && ((out == in->u && shape->u_stride != shape->channels) ||
+                         (out == in->dt && shape->dt_stride != shape->channels) ||
+                         (out == in->z && shape->z_stride != shape->channels)))
         return fail(RN_EINVAL, "a result lies over an input that is not contiguous");
+    if (out == in->b || out == in->c) return fail(RN_EINVAL, "out must be neither b nor c");
     ScanArgs a = scan_args(shape, in, nullptr, scan_sizes(shape, false), nullptr);
     a.whole_states = a.whole_states && on_16(state);
     a.ids = ids, a.slots = slots, a.final_state = state, a.out = out;
@@ -532,6 +539,7 @@ rn_status reuse_ops_scan_forward(const rn_scan_shape *shape, const rn_scan_input
     if (!scratch) return fail(RN_EINVAL, "scratch is NULL");
     const size_t need = scan_bytes(z);
     if (scratch_bytes < need) return need_bytes("scratch", need);
+    if (shape->tokens > 0 && is_input(in, out)) return fail(RN_EINVAL, "out must not be one of the inputs");
     ScanArgs a = scan_args(shape, in, seq_off, z, scratch);
     a.whole_states = a.whole_states && on_16(state) && on_16(final_state);
     a.state = state, a.final_state = final_state, a.out = out, a.kept = static_cast<float *>(saved);
@@ -556,6 +564,9 @@ rn_status reuse_ops_scan_backward(const rn_scan_shape *shape, const rn_scan_inpu
     if (saved_bytes < z.kept + kAlign) return need_bytes("saved", z.kept + kAlign);
     const size_t need = scan_bytes(z);
     if (scratch_bytes < need) return need_bytes("scratch", need);
+    if (shape->tokens > 0)
+        for (const void *p : {grads->du, grads->ddt, grads->db, grads->dc, grads->dz})
+            if (is_input(in, p) || (p && p == dout)) return fail(RN_EINVAL, "a gradient lies over dout or an input");
     ScanArgs a = scan_args(shape, in, seq_off, z, scratch);
     a.whole_states = a.whole_states && on_16(dfinal) && on_16(grads->dstate);
     a.kept = static_cast<float *>(const_cast<void *>(saved));

@@ -319,6 +319,8 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_bc(ScanArgs a) {
     if (i >= 2 * per * a.tokens) return;
     const int n = (int)(i % a.states), group = (int)(i / a.states % a.groups), kind = (int)(i / per % 2);
     const int64_t t = i / per / 2;
+    const Seqs seqs{a.off, a.n, a.tokens, a.even};
+    if (t < seqs.offset(0) || t >= seqs.offset(a.n)) return;    // no sequence's
     const int64_t of = a.blocks / a.groups;
     const float *p = a.part_bc + ((group * of * a.tokens + t) * 2 + kind) * a.states + n;
     const int64_t on = a.tokens * 2 * a.states;

@@ -115,9 +115,9 @@ __global__ __launch_bounds__(kThreads) void k_conv_seq(CausalArgs a) {
     if (p.c >= a.channels) return;
     const Seqs s{a.off, a.n, a.tokens, a.even};
     if (p.ends) return final_row<T, VEC, K>(a, s, p);
-    const int64_t from = p.run * a.run;
-    if (from >= a.tokens) return;
-    const int to = (int)min(from + a.run, a.tokens);
+    const int64_t from = max(p.run * a.run, (int64_t)s.offset(0));
+    const int to = (int)min((p.run + 1) * a.run, (int64_t)s.offset(a.n));      // what no sequence owns is left alone
+    if (from >= to) return;
     int t = (int)from;
     At at(s, t);
     Taps<T, VEC, K> taps;
@@ -210,9 +210,10 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(CausalArgs a) {
 #pragma unroll
         for (int k = 0; k < K; ++k) dw[k][j] = 0.f;
     }
-    const int64_t from = p.run * a.run;
-    if (from < a.tokens && p.c < a.channels) {
-        const int first = (int)from, to = (int)min(from + a.run, a.tokens);
+    const int64_t from = max(p.run * a.run, (int64_t)s.offset(0));
+    const int to = (int)min((p.run + 1) * a.run, (int64_t)s.offset(a.n));
+    if (from < to && p.c < a.channels) {
+        const int first = (int)from;
         int t = first;
         At at(s, t);
         Taps<T, VEC, K> taps;

@@ -781,7 +781,8 @@ def causal_conv(x, weight, bias=None, seq_off=None, n=None, state=None, final=No
     """All tokens of n sequences (reuse_ops_causal_conv).
 
     x: [tokens][channels], weight: [channels][taps], bias: [channels] or None,
-    as for causal_conv_step; seq_off or n as for delta_forward.  state:
+    as for causal_conv_step; seq_off or n as for delta_forward, but tokens behind
+    seq_off[n] are no sequence's: their results are left as they were.  state:
     [n][taps - 1][channels] in x's dtype, the inputs before each sequence
     (None: zeros); final: where the last ones go (made here if None; not
     state).  Returns (out, final).
@@ -898,7 +899,7 @@ def scan_forward(u, dt, a, b, c, d=None, z=None, dt_bias=None, softplus: bool = 
     """All tokens of n sequences (reuse_ops_scan_forward).
 
     The inputs as for scan_step, over tokens; seq_off or n as for
-    delta_forward.  state: [n][channels][states] float32 before each sequence
+    causal_conv.  state: [n][channels][states] float32 before each sequence
     (None: zeros); final: where the last ones go (made here if None; it may be
     state).  Returns (out, final), with save also the buffer that scan_backward
     reads.

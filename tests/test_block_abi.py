@@ -311,6 +311,16 @@ def test_scan_arguments():
     _err(step(out=None), B.RN_EINVAL, "NULL")
     apart = _scan(tokens=2, u=9)
     _err(step(shape=ref(apart), out=P), B.RN_EINVAL, "not contiguous")
+    for t in (_scan(tokens=2, dt=9), _scan(tokens=2, z=9)):
+        _err(step(shape=ref(t), out=P), B.RN_EINVAL, "not contiguous")
+    for name in ("b", "c"):
+        _err(step(given=inputs(**{name: 2 * P})), B.RN_EINVAL, "neither b nor c")
+    for name in ("u", "dt", "b", "c", "z"):
+        _err(fwd(given=inputs(**{name: 2 * P}), out=2 * P), B.RN_EINVAL, "one of the inputs")
+        for grad in ("du", "ddt", "db", "dc", "dz"):
+            away = {k: 9 * P for k in ("du", "ddt", "db", "dc", "dz")}
+            _err(back(given=inputs(**{name: 2 * P}), dout=3 * P, grads=grads(**{**away, grad: 2 * P})), B.RN_EINVAL, "lies over")
+            _err(back(dout=3 * P, grads=grads(**{**away, grad: 3 * P})), B.RN_EINVAL, "lies over")
     assert fwd(shape=ref(none), scratch=None) == step(shape=ref(none), slots=0, state=None) == B.RN_OK
 
 

@@ -188,6 +188,30 @@ def test_no_tokens_and_empty_sequences():
     assert ops.causal_conv_step(x, w, window, b).shape == (0, 8)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("channels", [24, 7])
+def test_tokens_behind_the_last_sequence(channels, dtype):
+    """A padded batch: the rows behind are left as they were, whatever they hold, and reach no result."""
+    from paper_1909_05632_amd import ops
+    for held, off in ((5, [0, 3, 5]), (70, [0, 40, 40, 70]), (0, [0, 0])):
+        n = len(off) - 1
+        x, w, b, window, dout, dfinal = _inputs(held, channels, 4, n, dtype, seed=held)
+        want = _check(x, w, b, window, dout, dfinal, off) if held else None
+        pad = torch.full((100, channels), float("nan"), dtype=dtype)
+        px, pd = torch.cat([x, pad]).cuda(), torch.cat([dout, pad]).cuda()
+        kw = dict(seq_off=torch.tensor(off, dtype=torch.int32).cuda(), state=window.cuda())
+        out = torch.full_like(px, 7.0)
+        _, final = ops.causal_conv(px, w.cuda(), b.cuda(), out=out, **kw)
+        dx, dw, db, ds = ops.causal_conv_backward(pd, px, w.cuda(), b.cuda(), dfinal=dfinal.cuda(), **kw)
+        assert (out[held:] == 7).all()
+        if want is None:
+            assert torch.equal(final.cpu(), window) and torch.equal(ds.cpu(), dfinal) and not dw.any() and not db.any()
+            continue
+        assert R.rel(out[:held], want[0]) <= TOL[dtype] and torch.equal(final, want[1])
+        for got, ref, tol in zip((dx[:held], dw, db, ds), want[2], (TOL[dtype], 4e-6, 4e-6, TOL[dtype])):
+            assert R.rel(got, ref) <= tol
+
+
 def test_other_stream_same_bits_and_in_a_graph():
     from paper_1909_05632_amd import ops
     x, w, b, window, dout, dfinal = (t.cuda() for t in _inputs(2100, 136, 4, 7, BF16, seed=13))

@@ -281,6 +281,26 @@ def test_no_tokens_and_empty_sequences():
     assert ops.scan_step(**g, state=state).shape == (0, 8)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("states", [16, 6])
+def test_tokens_behind_the_last_sequence(states, dtype):
+    """A padded batch: the rows behind are left as they were, whatever they hold, and reach no result."""
+    from paper_1909_05632_amd import ops
+    for held, off in ((5, [0, 3, 5]), (300, [0, 40, 40, 300])):
+        x, dout, dfinal = S.inputs(held, 12, states, 2, len(off) - 1, dtype, seed=held)
+        out, final, grads = _check(x, dout, dfinal, off)
+        pad = lambda t: torch.cat([t, torch.full((700, *t.shape[1:]), float("nan"), dtype=dtype)]).cuda()  # noqa: E731
+        g = {k: pad(v) if k in ("u", "dt", "b", "c", "z") else v.cuda() for k, v in x.items()}
+        state, seqs = g.pop("state"), dict(seq_off=torch.tensor(off, dtype=torch.int32).cuda())
+        o2 = torch.full_like(g["u"], 7.0)
+        _, f2, saved = ops.scan_forward(**g, state=state, save=True, out=o2, **seqs)
+        assert (o2[held:] == 7).all() and R.rel(o2[:held], out) <= TOL[dtype] and R.rel(f2, final) <= TOL[F32]
+        g2 = dict(zip(S.GRADS, ops.scan_backward(pad(dout), **g, saved=saved, dfinal=dfinal.cuda(), **seqs)))
+        for k in S.GRADS:
+            got = g2[k][:held] if k in ("du", "ddt", "db", "dc", "dz") else g2[k]
+            assert R.rel(got, grads[k]) <= (TOL[F32] if k[1:] in WIDE else TOL[dtype]), k
+
+
 def test_other_stream_same_bits_and_in_a_graph():
     from paper_1909_05632_amd import ops
     side = torch.cuda.Stream()
