@@ -219,7 +219,8 @@ rn_status reuse_ops_delta_backward(const rn_delta_shape *shape, const void *dev_
  *   q_j = t_j (448 / m) rounded to nearest even (0 where m is 0),  scale = m rstd / 448,
  * so that y_j = q_j scale to half a step of e4m3, and q depends on no order of sums.
  * A row that holds NaN or infinity (or so large values that its sum of squares is
- * infinite) has the y of these formulas, a scale of NaN and any q.
+ * infinite) has the y of these formulas, a scale of NaN and any q.  Squares are float32:
+ * those of values below 2^-75 are 0, beside eps or not.
  */
 
 /* `rows` rows of `width` elements (rows >= 0, width >= 1); results are contiguous.

@@ -33,6 +33,15 @@ __device__ inline float row_max(float v, float *lds) {
     return v;
 }
 
+// What a row's |h w| are multiplied by, in two factors: 448 / largest, and a power of two
+// where that would be infinite.
+struct Steps {
+    float up, step;
+    __device__ explicit Steps(float largest) : up(largest < 0x1p-100f ? 0x1p60f : 1.f) {
+        step = largest > 0.f ? kE4m3Max / (largest * up) : 0.f;
+    }
+};
+
 // e4m3, to nearest even; two values' bits.
 __device__ inline uint32_t e4m3_pair(float x, float y) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false) & 0xffffu;
@@ -100,7 +109,7 @@ __global__ __launch_bounds__(kThreads) void k_rms(RmsArgs a) {
             largest = row_max<G>(largest, most);
         }
         if (!live) continue;
-        const float step = largest > 0.f ? kE4m3Max / largest : 0.f;
+        const Steps to_q(largest);
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int c = (lane + G * i) * VEC;
@@ -116,7 +125,7 @@ __global__ __launch_bounds__(kThreads) void k_rms(RmsArgs a) {
             if (a.q) {
                 float t[VEC];
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) t[j] = to_float(p[i].v[j]) * w[j] * step;
+                for (int j = 0; j < VEC; ++j) t[j] = to_float(p[i].v[j]) * w[j] * to_q.up * to_q.step;
                 store_e4m3<VEC>(a.q + r * a.width + c, t);
             }
         }
@@ -146,12 +155,12 @@ __global__ __launch_bounds__(kThreads) void k_rms_wide(RmsArgs a) {
         }
         const float rstd = 1.0f / sqrtf(row_sum<kThreads>(s, lds) * inv + a.eps);
         if (a.q) largest = row_max<kThreads>(largest, most);
-        const float step = largest > 0.f ? kE4m3Max / largest : 0.f;
+        const Steps to_q(largest);
         for (int c = threadIdx.x; c < a.width; c += kThreads) {
             const float h = to_float(total ? total[c] : a.residual ? from_float<T>(to_float(x[c]) + to_float(add[c])) : x[c]);
             const float w = a.weight ? a.weight[c] : 1.f;
             if (a.y) static_cast<T *>(a.y)[r * a.width + c] = from_float<T>(h * rstd * w);
-            if (a.q) a.q[r * a.width + c] = (uint8_t)e4m3_pair(h * w * step, 0.f);
+            if (a.q) a.q[r * a.width + c] = (uint8_t)e4m3_pair(h * w * to_q.up * to_q.step, 0.f);
         }
         if (threadIdx.x == 0) {
             if (a.rstd) a.rstd[r] = rstd;

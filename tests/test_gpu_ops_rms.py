@@ -200,3 +200,18 @@ def test_more_rows_than_a_grid_takes_at_once():
     for lo in (0, 16380, 65530, 70000):
         a, b = ops.rms_norm(x[lo:lo + 9], w, r[lo:lo + 9], EPS)
         assert torch.equal(a, y[lo:lo + 9]) and torch.equal(b, total[lo:lo + 9])
+
+
+def test_rows_of_tiny_values_in_8_bits():
+    """448 / m is infinite where m is below 1.3e-36; q and the scales are as they are for any other row.
+    (y is q scale to half a step of e4m3, 2^-4 of it or 2^-10 of 448, and a few 2^-24.)"""
+    from paper_1909_05632_amd import ops
+    for width in (96, 9000):
+        for size in (3e-36, 1e-36, 2.0 ** -121, 1e-37):
+            x = (size * torch.linspace(-1, 1, width)).expand(3, width).contiguous()
+            q, scales = ops.rms_norm(x.cuda(), eps=EPS, quantize=True)
+            y = x.double() / EPS ** 0.5
+            got = q.cpu().double() * scales.cpu().double()[:, None]
+            largest = y.abs().max()
+            assert ((got - y).abs() <= (y.abs() * 2.0 ** -4).clamp(min=largest / 448 * 2.0 ** -10) + 1e-5 * largest).all()
+            assert q.float().abs().max() == 448
