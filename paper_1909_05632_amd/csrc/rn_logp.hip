@@ -9,13 +9,15 @@
 //   p_i = 2^z_i / s,  dl_i = (dlogp ([i = t] - p_i) - dent p_i (log p_i + entropy)) / temperature.
 //
 // Alternatives rank by key: the logit's bits in an order of whole numbers, then the
-// lowest index, so that keys are distinct.  Each group of four threads knows the
-// largest of its logits; the top-th largest of those is a bound below which no
-// alternative lies, and only the groups above it have any: their logits are read once
-// more.  (A bound of every thread's largest is a little higher, but 256 keys take
-// 16 times the comparisons of 64: 64 rows of 131072 19 us, in place of 18.)
+// lowest index, so that keys are distinct.  Each pair of threads knows the largest of
+// its logits; the top-th largest of those is a bound below which no alternative lies,
+// and only the pairs above it have any: their logits are read once more.  (Fours of
+// threads: 4096 rows of 5000 with 20 alternatives 31 us and with 64 114, pairs 33 and
+// 41, every thread by itself 46 and 50, for 256 keys are ranked against 256.)
 //
 // Bound by HBM: a logit is read once forward (a few are, twice) and once backward.
+// 2048 rows of 131072 bfloat16, 537 MB: 112 us forward (4.8 TB/s), 178 with 20
+// alternatives; 208 backward (5.2 TB/s).  4096 rows of 18: 3.6 and 3.2 us.
 #include "rn_ops.hpp"
 
 namespace rn {
@@ -26,7 +28,8 @@ using namespace ops;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kGroup = 4, kGroups = kThreads / kGroup;       // RN_LOGPROBS_MAX_TOP groups, or more
+constexpr int kGroup = 2, kGroups = kThreads / kGroup;       // RN_LOGPROBS_MAX_TOP groups, or more
+constexpr int kAhead = 2;         // vectors a thread has on their way at once
 constexpr int kList = 1024;       // alternatives that are ranked at once
 static_assert(kGroups >= RN_LOGPROBS_MAX_TOP);
 // Smaller rows are in the registers of a wave or less (kWaveVocab / 64 logits a lane).
@@ -206,7 +209,9 @@ struct Part {
         return best;
     }
 
-    __device__ Sums sums(Lds &lds, float c, bool top) const {
+    // TOP is no argument, for what it needs costs the other calls 30% (registers).
+    template <bool TOP>
+    __device__ Sums sums(Lds &lds, float c) const {
         Sums s = kNone;
         uint64_t best = 0;
         float best_logit = -kInf;
@@ -219,27 +224,45 @@ struct Part {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) add(s, base, l[j], c);
             // Equal ones later on rank behind: only a larger one, or the first, is looked at.
-            if (top && (m > best_logit || best == 0)) {
+            if (TOP && (m > best_logit || best == 0)) {
                 best = max(best, largest_of(v, l, ~0ull));
                 best_logit = logit_of(best);
             }
         };
-        int v = lo + threadIdx.x;
-        for (; v + 3 * kThreads < hi; v += 4 * kThreads) {
-            float l[4][VEC];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) vec.load(v + u * kThreads, l[u]);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) take(v + u * kThreads, l[u]);
-        }
-        for (; v < hi; v += kThreads) {
+        const auto edge = [&](int v) {                  // the row's first or last vector, of which it has a part
             float l[VEC];
             vec.load(v, l);
             take(v, l);
+        };
+        int v = lo + threadIdx.x;
+        int had = -1;
+        if (v < hi && !vec.whole(v)) edge(v), had = v, v += kThreads;
+        const int end = hi > lo && !vec.whole(hi - 1) ? hi - 1 : hi;
+        if (v < end) {
+            // The next vectors are on their way while these are worked on.
+            Pack<T, VEC> next[kAhead];
+            const auto fetch = [&](int v) {
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+                    next[u] = *reinterpret_cast<const Pack<T, VEC> *>(vec.x + vec.first(min(v + u * kThreads, end - 1)));
+            };
+            fetch(v);
+            for (; v < end; v += kAhead * kThreads) {
+                float l[kAhead][VEC];
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) l[u][j] = to_float(next[u].v[j]);
+                fetch(v + kAhead * kThreads);
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+                    if (v + u * kThreads < end) take(v + u * kThreads, l[u]);
+            }
         }
+        if (end < hi && end != had && (end - lo) % kThreads == threadIdx.x) edge(end);
         s = over_lanes<64>(s, c);
         if ((threadIdx.x & 63) == 0) lds.sums[threadIdx.x >> 6] = s;
-        if (top) {
+        if constexpr (TOP) {
 #pragma unroll
             for (int d = 1; d < kGroup; d *= 2) best = max(best, (uint64_t)__shfl_xor((unsigned long long)best, d));
             lds.best[threadIdx.x / kGroup] = best;
@@ -324,14 +347,14 @@ struct Part {
 };
 
 // One block a row (parts = 1), or a part of one, whose sums and keys go to scratch.
-template <class T>
+template <class T, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_logp_part(LogpArgs a) {
     __shared__ typename Part<T>::Lds lds;
     const int64_t i = block_index(), r = i / a.parts;
     if (r >= a.n) return;
     const Part<T> part(a, r, (int)(i % a.parts));
-    const Sums s = part.sums(lds, a.c, a.top > 0);
-    if (a.top) part.top(lds, a.top);
+    const Sums s = part.template sums<TOP>(lds, a.c);
+    if constexpr (TOP) part.top(lds, a.top);
     if (a.parts > 1) {
         if (threadIdx.x == 0) a.part_sums[3 * i] = s.m, a.part_sums[3 * i + 1] = s.s, a.part_sums[3 * i + 2] = s.w;
         if ((int)threadIdx.x < a.top) a.part_keys[i * a.top + threadIdx.x] = lds.top[threadIdx.x];
@@ -458,7 +481,9 @@ hipError_t run_forward(const LogpArgs &a, hipStream_t s) {
         });
         return hipGetLastError();
     }
-    k_logp_part<T><<<grid_of((int64_t)a.n * a.parts), kThreads, 0, s>>>(a);
+    const dim3 grid = grid_of((int64_t)a.n * a.parts);
+    if (a.top) k_logp_part<T, true><<<grid, kThreads, 0, s>>>(a);
+    else k_logp_part<T, false><<<grid, kThreads, 0, s>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
     if (a.parts > 1) k_logp_join<T><<<grid_of(a.n), kThreads, 0, s>>>(a);
     return hipGetLastError();
@@ -483,6 +508,8 @@ hipError_t run_backward(const LogpArgs &a, hipStream_t s) {
 
 // Blocks a row: rows are shared where there are too few to fill the GPU, as long as
 // a part has four vectors a thread, its sums fit a wave and its keys the join's list.
+// 64 rows of 131072 with 20 alternatives: in 512 blocks 18 us and the join 5.5, in 1024
+// 21 and 12, in 2048 27 and 30.
 int logp_parts(int n, int vocab, int top, bool bf16) {
     if (vocab <= kWaveVocab || n <= 0 || n >= 512) return 1;
     const int vectors = vocab / (bf16 ? 8 : 4), want = (512 + n - 1) / n;

@@ -730,7 +730,8 @@ def _flat(x, what: str, dtype, tokens: int, channels: int, device):
         raise ValueError(f"{what} must be {dtype} on {device}")
     if x.shape != (tokens, channels):
         raise ValueError(f"{what} must have shape ({tokens}, {channels}), got {tuple(x.shape)}")
-    return x.data_ptr(), _rows(x, what)[1]
+    row, one = x.stride()
+    return x.data_ptr(), row if one == 1 and row >= channels else _rows(x, what)[1]
 
 
 def _conv_shape(x, weight, bias, n: int, silu):
@@ -851,9 +852,9 @@ def _scan_shape(u, dt, a, b, c, d, z, dt_bias, softplus, n: int):
     groups, states, bs = _tokens(b, "b", dtype, tokens, dev)
     if channels % groups:
         raise ValueError(f"{channels} channels cannot share {groups} groups")
-    if _tokens(c, "c", dtype, tokens, dev)[:2] != (groups, states):
+    groups_c, states_c, cs = _tokens(c, "c", dtype, tokens, dev)
+    if groups_c != groups or states_c != states:
         raise ValueError("c must have b's shape")
-    cs = _tokens(c, "c", dtype, tokens, dev)[2]
     _count(max(channels, states, n), "channels, states and n")
     inputs = rn_scan_inputs(up, dtp, b.data_ptr(), c.data_ptr(), _like(a, "a", _F32, dev, (channels, states)),
                             _opt(d, "d", _F32, dev, (channels,)), zp, _opt(dt_bias, "dt_bias", _F32, dev, (channels,)))
