@@ -10,6 +10,10 @@
 // each chunk's end from a state of 0 (k_scan_seq<LOCAL>), then the states that the
 // chunks begin with, one after the other (k_scan_join: a chunk's decay is that of
 // its summed step sizes), then every chunk with its state.
+//
+// 16384 ragged tokens of 4096 channels of 16 states, bfloat16: 205 us for the chunks'
+// ends, 19 for what they begin with, 290 for all tokens, vector instructions in 96% and
+// 91% of the cycles: a token's step size, gate and stores are a quarter of them.
 #include "rn_scan.hpp"
 
 namespace rn {
@@ -69,7 +73,8 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_join(ScanArgs a) {
 
 // A wave takes 64 channels of a chunk by itself, all S states of a channel in the
 // registers of its lane.  LOCAL: of every chunk but a sequence's last, the state at
-// its end from 0, and its summed step sizes.
+// its end from 0, and its summed step sizes.  Five waves a SIMD where the registers
+// allow (302 us without the bound, 290 with it, 10% more with one of six).
 template <class T, class BC, int S, bool LOCAL>
 __global__ __launch_bounds__(64, S <= 16 ? 5 : 1) void k_scan_seq(ScanArgs a) {
     const uint32_t block = block_index();
@@ -193,8 +198,9 @@ __device__ inline float over_states(float v) {
     return v;
 }
 
-// Bound by the states' bytes.  L lanes carry a channel, four states each, so that a
-// wave's accesses are one piece; blocks walk the streams with the grid's second axis.
+// Bound by the states' bytes: 1024 streams of 2048 channels of 16 states, 62 us, 4.6 TB/s.
+// L lanes carry a channel, four states each, so that a wave's accesses are one piece;
+// blocks walk the streams with the grid's second axis.
 template <class T, int L>
 __global__ __launch_bounds__(kScanThreads) void k_scan_step(ScanArgs a) {
     const int lane = threadIdx.x % L, n0 = lane * kStates;
@@ -277,9 +283,9 @@ hipError_t step(const ScanArgs &a, hipStream_t s) {
 int64_t scan_blocks(int channels, int groups) { return (int64_t)groups * ((channels / groups + 63) / 64); }
 
 // Chunks so long that all tokens' are as many blocks as fill the GPU (8 waves a SIMD
-// forward; half of that backward, where what follows takes more of them),
-// but no shorter than 2^kShortest: below, what the chunks' ends cost is more than
-// what they free.
+// forward; half of that backward, where each block has W waves), but no shorter than
+// 2^kShortest, 4 tiles.  16384 ragged tokens of 4096 channels forward, 8192 blocks:
+// the ends 208 us, the join 19, all tokens 300; 4096 blocks: 256, 13 and 322.
 int scan_log_chunk(int64_t tokens, int channels, int groups, bool backward) {
     constexpr int kShortest = 6;
     const int64_t blocks = backward ? 4096 : 8192, want = (tokens * scan_blocks(channels, groups) + blocks - 1) / blocks;

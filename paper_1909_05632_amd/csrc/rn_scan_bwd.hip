@@ -12,10 +12,12 @@
 // Where sequences are cut into chunks, what g is at their ends comes first, as
 // forward (k_scan_back: each chunk's g at its begin from 0).
 //
-// Bound by its arithmetic: for each token, channel and state two exponentials, 14
-// multiplications or multiply-adds, and a third of that again for the sums over
-// channels: those of a wave in registers (over_channels), of all waves by another
-// kernel, each in a fixed order.
+// Bound by its arithmetic: for each token, channel and state one and a half
+// exponentials, 15 multiplications or multiply-adds, and a third of that again for the
+// sums over channels: those of a wave in registers (over_channels), of all waves by
+// another kernel, each in a fixed order.  8192 ragged tokens of 2048 channels of 16
+// states, bfloat16: k_scan_bwd 270 us, vector instructions in 3 of 4 of its cycles;
+// k_scan_back 76, the joins 15, the sums 10 (a), 8 (b and c) and 5 us.
 #include "rn_rows.hpp"
 #include "rn_scan.hpp"
 
@@ -143,11 +145,14 @@ __global__ __launch_bounds__(64) void k_scan_back(ScanArgs a) {
 }
 
 // A block takes 64 channels, wave w of W their states 4 w .. 4 w + 3.  A token is
-// loaded, and its results are stored, by one of them.
+// loaded, and its results are stored, by one of them.  Two waves a SIMD: at three, the
+// states of a tile do not fit the registers.  As many of its tokens' decays as fit too
+// stay there for the way back (8 of 16: 270 us; none 289; 10, with a spill, 275).
 template <class T, int W>
 __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a) {
     // Tokens between barriers: sums of all waves for a whole tile of 64 states are more than the LDS.
     constexpr int PART = W <= 8 ? kTile : kTile / 2;
+    constexpr int SAVED = W == 1 || W == 16 ? 0 : W == 2 ? 6 : 8;
     constexpr int OWN = kTile / W, N = kStates * W, THREADS = 64 * W, PER = kTile * N / THREADS;
     __shared__ float in[kTile][5][64];                  // of each token s, u, p, softplus', dout silu'(z)
     __shared__ float sums[W][PART][3][64];              // sum g a k, sum g b and sum c h, by wave
@@ -214,6 +219,7 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
                 const bool there = t < m && n < a.states;
                 sb[t][n] = there ? to_float(raw_b[i]) : 0.f, sc[t][n] = there ? to_float(raw_c[i]) : 0.f;
             }
+            f32x4 e[kTile];                             // decays of the last SAVED tokens
             f32x4 h[kTile + 1];                         // before each token, and after the last
             h[0] = next_h;
             __syncthreads();
@@ -235,8 +241,11 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
                 __builtin_amdgcn_sched_barrier(0);
                 const float x = now.s * now.u;
 #pragma unroll
-                for (int i = 0; i < kStates; ++i)
-                    h[t + 1][i] = fmaf(x, now.b[i], __builtin_amdgcn_exp2f(now.s * decay[i]) * h[t][i]);
+                for (int i = 0; i < kStates; ++i) {
+                    const float now_e = __builtin_amdgcn_exp2f(now.s * decay[i]);
+                    if (t >= kTile - SAVED) e[t][i] = now_e;
+                    h[t + 1][i] = fmaf(x, now.b[i], now_e * h[t][i]);
+                }
             }
             const auto part_bc = rows_from<float>(a.part_bc, 2 * a.states, (int64_t)cblock * a.tokens + chunk.begin + t0);
 #pragma unroll
@@ -254,16 +263,16 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
                         float *o = v + (t - t2) * 8, ak = 0.f, gb = 0.f, y = 0.f;
 #pragma unroll
                         for (int i = 0; i < kStates; ++i) {
-                            const float e = __builtin_amdgcn_exp2f(st * decay[i]);
+                            const float te = t >= kTile - SAVED ? e[t][i] : __builtin_amdgcn_exp2f(st * decay[i]);
                             g[i] = fmaf(cc[i], pt, g[i]);
-                            const float gk = g[i] * (e * h[t][i]);
+                            const float gk = g[i] * (te * h[t][i]);
                             ak = fmaf(gk, decay[i], ak);
                             da[i] = fmaf(gk, st, da[i]);
                             gb = fmaf(b[i], g[i], gb);
                             y = fmaf(cc[i], h[t + 1][i], y);
                             o[i] = g[i] * x;
                             o[4 + i] = h[t + 1][i] * pt;
-                            g[i] *= e;
+                            g[i] *= te;
                         }
                         sums[w][t - part][0][me] = ak, sums[w][t - part][1][me] = gb;
                         sums[w][t - part][2][me] = y;

