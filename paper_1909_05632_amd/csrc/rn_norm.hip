@@ -255,7 +255,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_cols(NormArgs a) {
 
 // Sums the strips in a fixed order.
 __global__ __launch_bounds__(1024) void k_norm_reduce(NormArgs a) {
-    column_sums(a.part, (int64_t)2 * a.width, a.blocks, [&](int64_t c, float v) {
+    column_sums(a.part, (int64_t)2 * a.width, a.blocks, block_index(), [&](int64_t c, float v) {
         float *out = c < a.width ? a.dweight : a.dbias;
         const int64_t i = c < a.width ? c : c - a.width;
         if (out) out[i] = a.accumulate ? out[i] + v : v;

@@ -307,7 +307,7 @@ __global__ __launch_bounds__(kThreads) void k_rms_cols(RmsArgs a) {
 }
 
 __global__ __launch_bounds__(1024) void k_rms_reduce(RmsArgs a) {
-    column_sums(a.part, a.width, a.blocks, [&](int64_t c, float v) { a.dweight[c] = a.accumulate ? a.dweight[c] + v : v; });
+    column_sums(a.part, a.width, a.blocks, block_index(), [&](int64_t c, float v) { a.dweight[c] = a.accumulate ? a.dweight[c] + v : v; });
 }
 
 // 16-byte accesses where every row of every array allows them.

@@ -86,10 +86,10 @@ inline bool aligned(const void *p, int64_t stride, int size) {
 // out[c] (+)= the sum over b of part[b][c], in a fixed order: 16 columns a block, 64
 // threads a column each adding every 64th part, then a tree.
 template <class Out>
-__device__ inline void column_sums(const float *part, int64_t columns, int parts, Out &&out) {
+__device__ inline void column_sums(const float *part, int64_t columns, int parts, uint32_t block, Out &&out) {
     __shared__ float lds[64][17];
     const int col = threadIdx.x % 16, k = threadIdx.x / 16;
-    const int64_t c = (int64_t)block_index() * 16 + col;
+    const int64_t c = (int64_t)block * 16 + col;
     float s = 0.f;
     if (c < columns)
         for (int b = k; b < parts; b += 64) s += part[b * columns + c];
@@ -101,7 +101,8 @@ __device__ inline void column_sums(const float *part, int64_t columns, int parts
     }
     if (k == 0 && c < columns) out(c, lds[0][col]);
 }
-inline dim3 column_grid(int64_t columns) { return grid_of((columns + 15) / 16); }   // of 1024 threads
+inline int64_t column_blocks(int64_t columns) { return (columns + 15) / 16; }       // of 1024 threads
+inline dim3 column_grid(int64_t columns) { return grid_of(column_blocks(columns)); }
 
 }  // namespace ops
 }  // namespace rn

@@ -318,7 +318,7 @@ __global__ __launch_bounds__(kThreads) void k_conv_bwd(CausalArgs a) {
 
 __global__ __launch_bounds__(1024) void k_conv_reduce(CausalArgs a) {
     const int64_t weights = (int64_t)a.channels * a.taps;
-    column_sums(a.part, weights + a.channels, a.run_blocks, [&](int64_t c, float v) {
+    column_sums(a.part, weights + a.channels, a.run_blocks, block_index(), [&](int64_t c, float v) {
         if (c < weights) a.dweight[c] = v;
         else a.dbias[c - weights] = v;
     });
