@@ -317,7 +317,7 @@ typedef struct {
     int32_t n;                    /* sequences (streams), 0..65535 */
     int32_t channels;             /* 1..65536 */
     int32_t taps;                 /* 1..RN_CONV_MAX_TAPS */
-    int64_t tokens;               /* tokens of all sequences, 0..2^31 - 1 */
+    int64_t tokens;               /* tokens of all sequences, 0..2^31 - 64 */
     rn_dtype dtype;               /* of x, out and the windows */
     int32_t silu;                 /* not 0: out = silu(pre) */
     int64_t x_stride;             /* elements from a token to the next, below 2^23 */

@@ -134,7 +134,8 @@ const char *bad_conv(const rn_conv_shape *s) {
     if (s->n < 0 || s->n > kMaxSequences) return "n must be 0..65535";
     if (s->channels < 1 || s->channels > kMaxChannels) return "channels must be 1..65536";
     if (s->taps < 1 || s->taps > RN_CONV_MAX_TAPS) return "taps must be 1..4";
-    if (s->tokens < 0 || s->tokens > INT32_MAX) return "tokens must be 0..2^31 - 1";
+    // The kernels count some tokens past the last in 32 bits.
+    if (s->tokens < 0 || s->tokens > INT32_MAX - 63) return "tokens must be 0..2^31 - 64";
     if (s->n == 0 && s->tokens > 0) return "tokens without sequences";
     if (!known(s->dtype)) return "dtype must be RN_F32 or RN_BF16";
     if (s->tokens > 1 && s->x_stride < s->channels) return "a token stride is smaller than its token";

@@ -185,7 +185,11 @@ def test_causal_conv_arguments():
         assert L.reuse_ops_causal_conv_backward_scratch_bytes(ref(t)) == 0
         for call in (fwd, back, step):
             _err(call(shape=ref(t)), B.RN_EINVAL, text)
+    assert L.reuse_ops_causal_conv_backward_scratch_bytes(ref(_conv(tokens=(1 << 31) - 64))) > 0
+    most = _conv(tokens=(1 << 31) - 63)
+    assert L.reuse_ops_causal_conv_backward_scratch_bytes(ref(most)) == 0
     for call in (fwd, back, step):
+        _err(call(shape=ref(most)), B.RN_EINVAL, "2^31 - 64")
         _err(call(shape=None), B.RN_EINVAL, "shape")
     for call in (fwd, back):
         t = _conv(n=3)
