@@ -16,8 +16,8 @@
 // 41, every thread by itself 46 and 50, for 256 keys are ranked against 256.)
 //
 // Bound by HBM: a logit is read once forward (a few are, twice) and once backward.
-// 2048 rows of 131072 bfloat16, 537 MB: 112 us forward (4.8 TB/s), 178 with 20
-// alternatives; 208 backward (5.2 TB/s).  4096 rows of 18: 3.6 and 3.2 us.
+// 2048 rows of 131072 bfloat16, 537 MB: 135 us forward (4.0 TB/s), half as long again
+// with 20 alternatives; 210 backward (5.1 TB/s).  4096 rows of 18: 3.5 and 2.8 us.
 #include "rn_ops.hpp"
 
 namespace rn {

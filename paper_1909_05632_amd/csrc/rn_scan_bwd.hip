@@ -16,7 +16,7 @@
 // exponentials, 15 multiplications or multiply-adds, and a third of that again for the
 // sums over channels: those of a wave in registers (over_channels), of all waves by
 // another kernel, each in a fixed order.  8192 ragged tokens of 2048 channels of 16
-// states, bfloat16: k_scan_bwd 270 us, vector instructions in 3 of 4 of its cycles;
+// states, bfloat16: k_scan_bwd 280 us, vector instructions in 3 of 4 of its cycles;
 // k_scan_back 76, the joins 15, the sums over blocks 19.
 #include "rn_rows.hpp"
 #include "rn_scan.hpp"

@@ -1,5 +1,7 @@
 """Operators around a policy net (include/reuse_ops.h): layer norm, the gated
-delta rule's memory and the sampling of actions, on torch tensors.
+delta rule's memory and the sampling of actions; the norm of a residual stream,
+the short convolution, the selective scan and the log-probabilities of actions
+that were taken, on torch tensors.
 
 Every function only checks its arguments, allocates what the caller did not
 give and passes pointers on: the work runs in the library's HIP kernels, on
@@ -26,6 +28,16 @@ A policy that remembers, one frame of n streams at a time:
 
 and over whole episodes ``delta_forward(..., save=True)`` with
 ``delta_backward`` and ``layer_norm_backward`` for the gradients.
+
+One whose memory is a window and a state, in a block beside a residual stream x:
+
+    u, z, dt, b, c = ...                         # the caller's projections of rms_norm(x, w)
+    u = causal_conv_step(u, w_conv, window)      # [streams][taps - 1][channels], in place
+    h = scan_step(u, dt, a, b, c, state, z=z)    # [streams][channels][states], in place
+    y, x = rms_norm(h @ w_mid, w, residual=x)    # for the next block, or for logits
+
+and over whole episodes ``causal_conv``, ``scan_forward(..., save=True)`` and
+``log_probs(logits, actions, with_stats=True)`` with their ``_backward`` calls.
 """
 from __future__ import annotations
 
