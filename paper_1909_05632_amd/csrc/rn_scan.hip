@@ -198,10 +198,12 @@ __device__ inline float over_states(float v) {
     return v;
 }
 
-// Bound by the states' bytes: 1024 streams of 2048 channels of 16 states, 62 us, 4.6 TB/s.
+// Bound by the states' bytes: 1024 streams of 2048 channels of 16 states, 57 us (5.0
+// TB/s) where the pool is in the last-level cache, 88 otherwise.  (Loads and stores that
+// pass by the caches: 80 and 81.)
 // L lanes carry a channel, four states each, so that a wave's accesses are one piece;
 // blocks walk the streams with the grid's second axis.
-template <class T, int L>
+template <class T, int L, bool WHOLE>
 __global__ __launch_bounds__(kScanThreads) void k_scan_step(ScanArgs a) {
     const int lane = threadIdx.x % L, n0 = lane * kStates;
     const int c = (int)(blockIdx.x * (kScanThreads / L) + threadIdx.x / L);
@@ -209,36 +211,68 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_step(ScanArgs a) {
     const int group = c / (a.channels / a.groups);
     const f32x4 decay = load_states(a, a.a, 0, c, n0, true) * kLog2e;
     const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, d = a.d ? a.d[c] : 0.f;
+    if (a.slots == 0) {                                 // no state to read
+        for (int r = blockIdx.y; r < a.n; r += gridDim.y)
+            if (lane == 0) static_cast<T *>(a.out)[(int64_t)r * a.channels + c] = from_float<T>(0.f);
+        return;
+    }
+    // The next stream's numbers are on their way while this one's are worked on: loads
+    // without branches, from a place of the array where there is nothing to read.
+    struct Stream {
+        bool there;
+        int64_t slot;
+        float h[kStates];
+        T u, dt, z, b[kStates], c[kStates];
+    };
+    const T *z_rows = static_cast<const T *>(a.z ? a.z : a.u);
+    const int64_t zs = a.z ? a.zs : a.us;
+    const auto fetch = [&](int row) {
+        Stream s;
+        const int64_t r = min(row, a.n - 1), slot = a.ids ? a.ids[r] : r;
+        s.there = slot >= 0 && slot < a.slots;
+        s.slot = s.there ? slot : 0;
+        const float *p = a.final_state + (s.slot * a.channels + c) * a.states;
+        if constexpr (WHOLE) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(p + min(n0, a.states - kStates));
+#pragma unroll
+            for (int i = 0; i < kStates; ++i) s.h[i] = v[i];
+        }
+        const T *pb = static_cast<const T *>(a.b) + r * a.bs + group * a.states;
+        const T *pc = static_cast<const T *>(a.c) + r * a.cs + group * a.states;
+#pragma unroll
+        for (int i = 0; i < kStates; ++i) {
+            const int at = min(n0 + i, a.states - 1);
+            if constexpr (!WHOLE) s.h[i] = p[at];
+            s.b[i] = pb[at], s.c[i] = pc[at];
+        }
+        s.u = static_cast<const T *>(a.u)[r * a.us + c], s.dt = static_cast<const T *>(a.dt)[r * a.dts + c];
+        s.z = z_rows[r * zs + c];
+        return s;
+    };
+    Stream next = fetch(blockIdx.y);
     for (int r = blockIdx.y; r < a.n; r += gridDim.y) {
-        const int64_t slot = a.ids ? a.ids[r] : r;
+        const Stream now = next;
+        next = fetch(r + gridDim.y);
         T *out = static_cast<T *>(a.out) + (int64_t)r * a.channels + c;
-        if (slot < 0 || slot >= a.slots) {
+        if (!now.there) {
             if (lane == 0) *out = from_float<T>(0.f);
             continue;
         }
-        f32x4 h = load_states(a, a.final_state, slot, c, n0, true);
-        const float u = to_float(static_cast<const T *>(a.u)[r * a.us + c]);
-        float s = to_float(static_cast<const T *>(a.dt)[r * a.dts + c]) + bias;
-        const float z = a.z ? to_float(static_cast<const T *>(a.z)[r * a.zs + c]) : 0.f;
-        const T *pb = static_cast<const T *>(a.b) + r * a.bs + group * a.states + n0;
-        const T *pc = static_cast<const T *>(a.c) + r * a.cs + group * a.states + n0;
-        float b[kStates], cc[kStates];
-#pragma unroll
-        for (int i = 0; i < kStates; ++i) {
-            const bool in = n0 + i < a.states;
-            b[i] = in ? to_float(pb[i]) : 0.f, cc[i] = in ? to_float(pc[i]) : 0.f;
-        }
+        const float u = to_float(now.u);
+        float s = to_float(now.dt) + bias;
         if (a.softplus) s = softplus(s);
         const float x = s * u;
         float y = 0.f;
+        f32x4 h;
 #pragma unroll
         for (int i = 0; i < kStates; ++i) {
-            h[i] = fmaf(x, b[i], __builtin_amdgcn_exp2f(s * decay[i]) * h[i]);
-            y = fmaf(cc[i], h[i], y);
+            const bool in = n0 + i < a.states;
+            h[i] = fmaf(x, in ? to_float(now.b[i]) : 0.f, __builtin_amdgcn_exp2f(s * decay[i]) * (in ? now.h[i] : 0.f));
+            y = fmaf(in ? to_float(now.c[i]) : 0.f, h[i], y);
         }
-        store_states(a, a.final_state, slot, c, n0, true, h);
+        store_states(a, a.final_state, now.slot, c, n0, true, h);
         y = fmaf(d, u, over_states<L>(y));
-        if (lane == 0) *out = from_float<T>(a.z ? y * silu(z) : y);
+        if (lane == 0) *out = from_float<T>(a.z ? y * silu(to_float(now.z)) : y);
     }
 }
 
@@ -273,7 +307,9 @@ hipError_t step(const ScanArgs &a, hipStream_t s) {
     for_states(a.states, [&](auto states) {
         constexpr int L = decltype(states)::value / kStates, CB = kScanThreads / L;
         const int across = (a.channels + CB - 1) / CB, rows = (2048 + across - 1) / across;
-        k_scan_step<T, L><<<dim3(across, a.n < rows ? a.n : rows), kScanThreads, 0, s>>>(a);
+        const dim3 grid(across, a.n < rows ? a.n : rows);
+        if (a.whole_states) k_scan_step<T, L, true><<<grid, kScanThreads, 0, s>>>(a);
+        else k_scan_step<T, L, false><<<grid, kScanThreads, 0, s>>>(a);
     });
     return hipGetLastError();
 }

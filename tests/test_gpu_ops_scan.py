@@ -175,6 +175,22 @@ def test_steps_of_many_streams():
         assert torch.equal(y, out) and torch.equal(state, final)
 
 
+def test_steps_of_a_pool_without_slots():
+    """No id is a slot then: every out is 0, and nothing is read or written through the pool's pointer."""
+    from paper_1909_05632_amd import binding as B
+    from paper_1909_05632_amd import ops
+    L, ref = ops.load_ops(), ops.ctypes.byref
+    for states, channels in ((16, 70), (5, 9)):
+        x, a = torch.randn(3, channels, device="cuda"), torch.zeros(channels, states, device="cuda")
+        b, pool = torch.randn(3, 1, states, device="cuda"), torch.full((1, channels, states), 3.0, device="cuda")
+        ids, out = torch.tensor([0, -1, 7], dtype=torch.int32, device="cuda"), torch.ones(3, channels, device="cuda")
+        shape = ops.rn_scan_shape(3, channels, 1, states, 3, B.RN_F32, 1, channels, channels, states, states, 0)
+        given = ops.rn_scan_inputs(x.data_ptr(), x.data_ptr(), b.data_ptr(), b.data_ptr(), a.data_ptr(), None, None, None)
+        stream = torch.cuda.current_stream().cuda_stream
+        assert L.reuse_ops_scan_step(ref(shape), ref(given), ids.data_ptr(), 0, pool.data_ptr(), out.data_ptr(), stream) == B.RN_OK
+        assert not out.any() and (pool == 3).all()
+
+
 def test_views_odd_addresses_and_final_over_state():
     from paper_1909_05632_amd import ops
     for dtype, states in ((F32, 16), (BF16, 16), (BF16, 6)):
