@@ -2,7 +2,7 @@
 
 Tolerances (2-norm, relative).  pre is a chain of at most 5 roundings, silu's
 exponential and reciprocal are an ulp each: below 16 x 2^-24 = 1e-6; 4e-6 is
-asked for.  Weight gradients add up to 32 tokens in a row and then a tree, of
+asked for.  Weight gradients add up to 64 tokens in a row and then a tree, of
 terms of random sign: 4e-6 as well.  A result rounded once to bfloat16 is within
 2^-8 of it (half a step).  Windows are copies."""
 import pytest

@@ -132,3 +132,25 @@ def test_a_frame_in_a_graph():
             torch.cuda.synchronize()
             assert all(torch.equal(p, q) for p, q in zip(got, want[t])), t
         assert all(torch.equal(p, q) for p, q in zip(held, eager))
+
+
+def test_slots_past_32_bits():
+    """Pools of more than 2^31 elements: the last slots are stepped as those of a small pool are."""
+    from paper_1909_05632_amd import ops
+    n, channels, states, slots = 3, 4096, 16, 34000
+    gen = torch.Generator().manual_seed(6)
+    randn = lambda *s: torch.randn(*s, generator=gen).cuda()  # noqa: E731
+    x, conv_w, a, b = randn(n, channels), randn(channels, 4), -randn(channels, states).exp(), randn(n, 1, states)
+    far = torch.tensor([slots - 1, 0, slots - 2], dtype=torch.int32).cuda()
+    state, window = randn(n, channels, states), randn(n, 3, channels)
+    pool = torch.empty(slots, channels, states, device="cuda")
+    windows = torch.empty(6 * slots, 3, channels, device="cuda")
+    assert pool.numel() > 2 ** 31 and windows.numel() > 2 ** 31
+    wide = torch.tensor([6 * slots - 1, 0, 6 * slots - 2], dtype=torch.int32).cuda()
+    pool[far.long()], windows[wide.long()] = state, window
+    want = ops.causal_conv_step(x, conv_w, window), ops.scan_step(x, x, a, b, b, state)
+    got = ops.causal_conv_step(x, conv_w, windows, stream_ids=wide), ops.scan_step(x, x, a, b, b, pool, stream_ids=far)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert torch.equal(pool[far.long()], state) and torch.equal(windows[wide.long()], window)
+    del pool, windows
+    torch.cuda.empty_cache()
