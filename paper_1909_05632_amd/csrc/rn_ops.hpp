@@ -155,7 +155,7 @@ inline int64_t scan_kept_slots(int64_t tokens, int n) { return tokens / RN_SCAN_
 __host__ __device__ inline int64_t scan_end_slot(const ScanArgs &a, int begin) { return begin >> (a.log_chunk - 1); }
 inline int64_t scan_ends(int64_t tokens, int log_chunk) { return tokens >> log_chunk ? tokens >> (log_chunk - 1) : 0; }
 int64_t scan_blocks(int channels, int groups);
-int scan_log_chunk(int64_t tokens, int channels, int groups, bool backward);
+int scan_log_chunk(int64_t tokens, int n, int channels, int groups, bool backward);
 int scan_padded(int states);
 bool scan_direct(const ScanArgs &a, bool bf16);
 hipError_t launch_scan_pack(const ScanArgs &a, bool bf16, hipStream_t s);

@@ -185,7 +185,7 @@ ScanSizes scan_sizes(const rn_scan_shape *s, bool backward) {
     ScanSizes z{};
     const size_t row = (size_t)s->channels * 4, states = row * s->states, own = row * ((s->states + 3) / 4 * 4);
     z.blocks = scan_blocks(s->channels, s->groups);
-    z.log_chunk = scan_log_chunk(s->tokens, s->channels, s->groups, backward);
+    z.log_chunk = scan_log_chunk(s->tokens, s->n, s->channels, s->groups, backward);
     z.chunks = (s->tokens >> z.log_chunk) + s->n;
     z.walkers = scan_walkers(z.chunks, z.blocks);
     z.kept = round_up(scan_kept_slots(s->tokens, s->n) * own);
