@@ -81,7 +81,8 @@ struct Taps {
 };
 
 // Where a thread works: `lanes` threads side by side over the channels, 256 / lanes
-// runs of a.run tokens a block.  The blocks behind the last run take the sequences' ends.
+// runs of a.run tokens a block.  The blocks behind the last run take the sequences' ends,
+// where those are wanted: a large grid is rounded up, so there may be such blocks anyway.
 struct Place {
     int c;                        // first channel, or beyond the last
     int64_t run;                  // run of tokens, or row of the sequences' ends
@@ -103,7 +104,7 @@ struct Place {
 template <class T, int VEC, int K>
 __device__ inline void final_row(const CausalArgs &a, const Seqs &s, const Place &p) {
     if constexpr (K > 1) {
-        if (p.run >= (int64_t)a.n * (K - 1)) return;
+        if (!a.final_window || p.run >= (int64_t)a.n * (K - 1)) return;
         const int seq = (int)(p.run / (K - 1)), i = (int)(p.run % (K - 1));
         const int begin = s.offset(seq), end = max(begin, s.offset(seq + 1));
         float v[VEC];
@@ -166,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void k_conv_seq(CausalArgs a) {
 template <class T, int VEC, int K>
 __device__ inline void window_row(const CausalArgs &a, const Seqs &s, const Place &p) {
     if constexpr (K > 1) {
-        if (p.run >= (int64_t)a.n * (K - 1)) return;
+        if (!a.dwindow || p.run >= (int64_t)a.n * (K - 1)) return;
         const int seq = (int)(p.run / (K - 1)), i = (int)(p.run % (K - 1));
         const int begin = s.offset(seq), end = max(begin, s.offset(seq + 1)), len = end - begin;
         Taps<T, VEC, K> taps;

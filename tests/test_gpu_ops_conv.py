@@ -255,3 +255,34 @@ def test_offsets_past_32_bits():
     assert torch.equal(dx[-100:], dx2) and torch.isfinite(dw).all()
     del x, out, dx
     torch.cuda.empty_cache()
+
+
+def test_more_blocks_than_a_grid_axis_holds_and_no_windows():
+    """One block more than 2^20, whose grid is rounded up, in calls that want no last windows and no gradient of
+    the first ones: the tokens around the last blocks and the first ones are as they are alone."""
+    from paper_1909_05632_amd import binding as B
+    from paper_1909_05632_amd import ops
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    # single elements, 8 lanes: 32 runs of 32 tokens a block
+    tokens, ref = (1 << 30) + 1, ops.ctypes.byref
+    x = torch.empty(tokens, 1, dtype=BF16, device="cuda").normal_(generator=gen)
+    w, b = torch.randn(1, 4, generator=gen, device="cuda"), torch.randn(1, generator=gen, device="cuda")
+    out = torch.full_like(x, 7.0)
+    shape = ops.rn_conv_shape(1, 1, 4, tokens, B.RN_BF16, 1, 1)
+    assert ops.load_ops().reuse_ops_causal_conv(ref(shape), x.data_ptr(), w.data_ptr(), b.data_ptr(), None, None, None,
+                                                out.data_ptr(), torch.cuda.current_stream().cuda_stream) == B.RN_OK
+    assert torch.equal(out[:5000], ops.causal_conv(x[:5000], w, b, n=1)[0])
+    assert torch.equal(out[-5000:], ops.causal_conv(x[-5000:], w, b, n=1, state=x[None, -5003:-5000].contiguous())[0])
+    del x, out
+    # 33 channels, single elements, 64 lanes: 4 runs of 64 tokens a block
+    tokens, channels = (1 << 28) + 1, 33
+    x = torch.empty(tokens, channels, dtype=BF16, device="cuda").normal_(generator=gen)
+    w, b = torch.randn(channels, 4, generator=gen, device="cuda"), torch.randn(channels, generator=gen, device="cuda")
+    dx, dw, _, none = ops.causal_conv_backward(x, x, w, b, n=1, want_dstate=False)
+    assert none is None and torch.isfinite(dw).all()
+    head, tail = x[:5003].contiguous(), x[-5000:].contiguous()
+    assert torch.equal(dx[:5000], ops.causal_conv_backward(head, head, w, b, n=1)[0][:5000])
+    window = x[None, -5003:-5000].contiguous()
+    assert torch.equal(dx[-5000:], ops.causal_conv_backward(tail, tail, w, b, n=1, state=window)[0])
+    del x, dx
+    torch.cuda.empty_cache()
