@@ -44,6 +44,12 @@ struct Steps {
     }
 };
 
+// A row's scale.  NaN where the sum of its squares is infinite or NaN: finite values whose
+// squares overflow have an rstd of 0, and a scale of 0 would be that of a row of zeros.
+__device__ inline float scale_of(float squares, float largest, float rstd) {
+    return squares < __builtin_huge_valf() ? largest * rstd / kE4m3Max : __builtin_nanf("");
+}
+
 // e4m3, to nearest even; two values' bits.
 __device__ inline uint32_t e4m3_pair(float x, float y) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false) & 0xffffu;
@@ -97,7 +103,8 @@ __global__ __launch_bounds__(kThreads) void k_rms(RmsArgs a) {
             for (int i = 0; i < ITEMS; ++i)
                 if (lane + G * i < nv) *reinterpret_cast<Pack<T, VEC> *>(total + (lane + G * i) * VEC) = p[i];
         }
-        const float rstd = 1.0f / sqrtf(row_sum<G>(s, lds) * inv + a.eps);
+        s = row_sum<G>(s, lds);
+        const float rstd = 1.0f / sqrtf(s * inv + a.eps);
         float largest = 0.f;
         if (a.q) {
 #pragma unroll
@@ -133,7 +140,7 @@ __global__ __launch_bounds__(kThreads) void k_rms(RmsArgs a) {
         }
         if (lane == 0) {
             if (a.rstd) a.rstd[r] = rstd;
-            if (a.q) a.scales[r] = largest * rstd / kE4m3Max;
+            if (a.q) a.scales[r] = scale_of(s, largest, rstd);
         }
     }
 }
@@ -155,7 +162,8 @@ __global__ __launch_bounds__(kThreads) void k_rms_wide(RmsArgs a) {
             s = fmaf(to_float(h), to_float(h), s);
             if (a.q) largest = fmaxf(largest, fabsf(to_float(h) * (a.weight ? a.weight[c] : 1.f)));
         }
-        const float rstd = 1.0f / sqrtf(row_sum<kThreads>(s, lds) * inv + a.eps);
+        s = row_sum<kThreads>(s, lds);
+        const float rstd = 1.0f / sqrtf(s * inv + a.eps);
         if (a.q) largest = row_max<kThreads>(largest, most);
         const Steps to_q(largest);
         for (int c = threadIdx.x; c < a.width; c += kThreads) {
@@ -166,7 +174,7 @@ __global__ __launch_bounds__(kThreads) void k_rms_wide(RmsArgs a) {
         }
         if (threadIdx.x == 0) {
             if (a.rstd) a.rstd[r] = rstd;
-            if (a.q) a.scales[r] = largest * rstd / kE4m3Max;
+            if (a.q) a.scales[r] = scale_of(s, largest, rstd);
         }
     }
 }

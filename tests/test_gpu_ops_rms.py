@@ -215,3 +215,20 @@ def test_rows_of_tiny_values_in_8_bits():
             largest = y.abs().max()
             assert ((got - y).abs() <= (y.abs() * 2.0 ** -4).clamp(min=largest / 448 * 2.0 ** -10) + 1e-5 * largest).all()
             assert q.float().abs().max() == 448
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_whose_squares_overflow(dtype):
+    """Finite values above 2^64 have an infinite sum of squares: y is 0 by its formula, and the scale NaN, so that
+    such a row is not taken for one of zeros.  The rows beside it are as they were."""
+    from paper_1909_05632_amd import ops
+    for width in (160, 9001):
+        x, r, _, _, w = (t.cuda() for t in _inputs(6, width, dtype))
+        y, total, q, scales = *ops.rms_norm(x, w, r, EPS), *ops.rms_norm(x, w, r, EPS, quantize=True)[:2]
+        x2 = x.clone()
+        x2[1], x2[3, width // 2], x2[4] = 2e19, -1e30, 3e38
+        y2, total2, q2, scales2 = *ops.rms_norm(x2, w, r, EPS), *ops.rms_norm(x2, w, r, EPS, quantize=True)[:2]
+        rest, over = [0, 2, 5], [1, 3, 4]
+        assert torch.equal(y2[rest], y[rest]) and torch.equal(scales2[rest], scales[rest])
+        assert torch.equal(q2.view(torch.uint8)[rest], q.view(torch.uint8)[rest])
+        assert torch.isfinite(total2).all() and not y2[over].any() and scales2[over].isnan().all()
