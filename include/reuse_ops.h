@@ -368,7 +368,9 @@ rn_status reuse_ops_causal_conv_backward(const rn_conv_shape *shape, const void 
  *   h_i <- exp(s a_i) h_i + s b_i u,
  *   y = sum_i c_i h_i + d u,  out = y z / (1 + exp(-z)), or y without z.
  * Group g has channels g channels / groups and on.  With a <= 0 the states stay
- * bounded.  s = 0 leaves the state as it is.
+ * bounded.  s = 0 leaves the state as it is, whatever a is: an infinite a counts as the
+ * largest number of its sign, so that -infinity empties a state at every token whose s is
+ * above 0, with a da of 0 and no part in ds.
  *
  * Values that are not finite reach what the rule makes of them, as NaN or infinity,
  * and nothing else: u, dt and z of a channel that channel's out, and u and dt its

@@ -49,7 +49,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_join(ScanArgs a) {
     const int begin = seqs.offset(seq), len = max(0, seqs.offset(seq + 1) - begin);
     const int64_t slot = scan_end_slot(a, begin), count = (len + a.chunk() - 1) >> a.log_chunk;
     if (count < 2) return;
-    const f32x4 decay = load_states(a, a.a, 0, c, quad * kStates, true) * kLog2e;
+    const f32x4 decay = load_decay(a, c, quad * kStates);
     f32x4 h = load_states(a, BACK ? a.dfinal : a.state, seq, c, quad * kStates, true);
     for (int64_t k = 0; k < count; k += kJoin) {
         f32x4 end[kJoin];
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(64, S <= 16 ? 5 : 1) void k_scan_seq(ScanArgs a) {
     float decay[S], h[S];
 #pragma unroll
     for (int q = 0; q < S / kStates; ++q) {
-        const f32x4 d = load_states(a, a.a, 0, c, q * kStates, true) * kLog2e;
+        const f32x4 d = load_decay(a, c, q * kStates);
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
         if (!LOCAL) s = chunk.alone() ? load_states(a, a.state, chunk.seq, c, q * kStates, true)
                                       : load_own(a, a.ends, chunk.end, c, q, true);
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_step(ScanArgs a) {
     const int c = (int)(blockIdx.x * (kScanThreads / L) + threadIdx.x / L);
     if (c >= a.channels) return;                        // a channel's lanes at once
     const int group = c / (a.channels / a.groups);
-    const f32x4 decay = load_states(a, a.a, 0, c, n0, true) * kLog2e;
+    const f32x4 decay = load_decay(a, c, n0);
     const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, d = a.d ? a.d[c] : 0.f;
     if (a.slots == 0) {                                 // no state to read
         for (int r = blockIdx.y; r < a.n; r += gridDim.y)

@@ -93,6 +93,15 @@ __device__ inline f32x4 load_states(const ScanArgs &a, const float *p, int64_t r
     }
     return v;
 }
+// a log2(e) of a channel's states, finite where a is not NaN: exp(s a) is then 1 where s is 0, as
+// of the tokens past a sequence's end, and an infinite a is the largest of its sign.
+__device__ inline f32x4 load_decay(const ScanArgs &a, int c, int n0) {
+    constexpr float kMost = 3.4028234663852886e38f;
+    f32x4 v = load_states(a, a.a, 0, c, n0, true) * kLog2e;
+#pragma unroll
+    for (int i = 0; i < kStates; ++i) v[i] = v[i] < -kMost ? -kMost : v[i] > kMost ? kMost : v[i];
+    return v;
+}
 __device__ inline void store_states(const ScanArgs &a, float *p, int64_t row, int c, int n0, bool live, f32x4 v) {
     if (!live || !p) return;
     p += (row * a.channels + c) * a.states + n0;

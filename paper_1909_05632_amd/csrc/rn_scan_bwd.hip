@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64) void k_scan_back(ScanArgs a) {
     float decay[S], g[S];
 #pragma unroll
     for (int q = 0; q < S / kStates; ++q) {
-        const f32x4 d = load_states(a, a.a, 0, c, q * kStates, true) * kLog2e;
+        const f32x4 d = load_decay(a, c, q * kStates);
 #pragma unroll
         for (int i = 0; i < kStates; ++i) decay[q * kStates + i] = d[i], g[q * kStates + i] = 0.f;
     }
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
     if (walker >= a.walkers) return;
     const Seqs seqs{a.off, a.n, a.tokens, a.even};
     const int c = where.c;
-    const f32x4 decay = load_states(a, a.a, 0, c, w * kStates, true) * kLog2e;
+    const f32x4 decay = load_decay(a, c, w * kStates);
     const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, d = a.d ? a.d[c] : 0.f;
     const uint32_t lane = (uint32_t)c * sizeof(T), to_lane = where.live ? lane : kNowhere;
     f32x4 da = {0.f, 0.f, 0.f, 0.f};

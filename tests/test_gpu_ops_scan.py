@@ -365,3 +365,40 @@ def test_offsets_past_32_bits():
     assert R.rel(out[cut:], end) <= TOL[BF16] and R.rel(final, last) <= TOL[F32]
     del u, dt, out
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("states", [2, 5, 16, 40])
+@pytest.mark.parametrize("tokens", [1, 2, 3, 7, 16, 19, 130])
+def test_states_that_are_emptied_by_every_token(tokens, states, dtype):
+    """a of -infinity: exp(s a) is 0 for every s above 0, whatever the sequence's length.  (The gradients are those
+    of a very low finite a, whose da is 0 and whose part in ds is too.)"""
+    from paper_1909_05632_amd import ops
+    x, dout, dfinal = S.inputs(tokens, 6, states, 2, 1, dtype, seed=tokens)
+    some = torch.rand(6, states, generator=torch.Generator().manual_seed(1)) < 0.4
+    some[0, 0], x["a"][some] = True, -1e30
+    lowest = _check(x, dout, dfinal, [0, tokens])
+    x["a"][some] = -float("inf")
+    out, final, grads = _run(x, dout, dfinal, n=1)
+    assert torch.equal(out, lowest[0]) and torch.equal(final, lowest[1])
+    assert all(torch.equal(grads[k], lowest[2][k]) for k in S.GRADS)
+    g = _cuda(x)
+    pool = g.pop("state")
+    for t in range(min(tokens, 3)):
+        y = ops.scan_step(**{k: v[t:t + 1] if k in ("u", "dt", "b", "c", "z") else v for k, v in g.items()}, state=pool)
+        assert torch.equal(y, out[t:t + 1])
+
+
+def test_a_step_of_zero_leaves_the_state_whatever_a_is():
+    from paper_1909_05632_amd import ops
+    a = torch.tensor([[-3.4e38, -2.5e38, -1.0, 2.5e38, 3.4e38]], device="cuda")
+    for tokens in (1, 5, 100):
+        u, dt = torch.ones(tokens, 1, device="cuda"), torch.zeros(tokens, 1, device="cuda")
+        b = torch.ones(tokens, 1, 5, device="cuda")
+        state = torch.tensor([[[1.0, -2.0, 3.0, 4.0, -5.0]]], device="cuda")
+        out, final, saved = ops.scan_forward(u, dt, a, b, b, softplus=False, n=1, state=state, save=True)
+        assert (out == 1).all() and torch.equal(final, state)
+        dstate = ops.scan_backward(out, u, dt, a, b, b, softplus=False, n=1, saved=saved)[-1]
+        assert (dstate == tokens).all()
+        assert (ops.scan_step(u[:1], dt[:1], a, b[:1], b[:1], state, softplus=False) == 1).all()
+        assert torch.equal(final, state)
