@@ -154,7 +154,7 @@ typedef struct {
 
 /* One token for each of n streams (tokens = n), the memory updated in place.
  *   dev_g, dev_beta:  [n][heads_v] float32.
- *   dev_state:        [slots][heads_v][dk][dv] float32.
+ *   dev_state:        [slots][heads_v][dk][dv] float32 (NULL without slots).
  *   dev_stream_ids:   [n] distinct slots, or NULL for 0..n-1.  A stream whose id
  *                     is outside 0..slots-1 is left out and its out is 0.
  *   dev_out:          [n][heads_v][dv] dtype, contiguous. */
@@ -325,7 +325,8 @@ typedef struct {
 
 /* One token for each of n streams (tokens = n), the windows updated in place.
  *   dev_weight:     [channels][taps] float32;  dev_bias: [channels] float32 or NULL (0).
- *   dev_window:     [slots][taps - 1][channels] dtype; not used where taps is 1.
+ *   dev_window:     [slots][taps - 1][channels] dtype (NULL without slots); not used where
+ *                   taps is 1.
  *   dev_stream_ids: [n] distinct slots, or NULL for 0..n-1.  A stream whose id is
  *                   outside 0..slots-1 is left out and its out is 0.
  *   dev_out:        [n][channels] dtype, contiguous; may be x itself where that is. */
@@ -405,7 +406,7 @@ typedef struct {
 } rn_scan_inputs;
 
 /* One token for each of n streams (tokens = n), the states updated in place.
- *   dev_state:      [slots][channels][states] float32.
+ *   dev_state:      [slots][channels][states] float32 (NULL without slots).
  *   dev_stream_ids: [n] distinct slots, or NULL for 0..n-1.  A stream whose id is
  *                   outside 0..slots-1 is left out and its out is 0.
  *   dev_out:        [n][channels] dtype, contiguous; may be u itself where that is. */

@@ -440,7 +440,7 @@ rn_status reuse_ops_causal_conv_step(const rn_conv_shape *shape, const void *x, 
     if (shape->tokens != shape->n) return fail(RN_EINVAL, "a step takes one token a stream: tokens must be n");
     if (slots < 0 || (!ids && slots < shape->n)) return fail(RN_EINVAL, "fewer slots than streams");
     if (shape->n == 0) return RN_OK;
-    if (!x || !weight || !out || (shape->taps > 1 && !window))
+    if (!x || !weight || !out || (shape->taps > 1 && slots > 0 && !window))
         return fail(RN_EINVAL, "x, weight, window and out must not be NULL");
     if (out == x && shape->n > 1 && shape->x_stride != shape->channels)
         return fail(RN_EINVAL, "a result lies over an input that is not contiguous");
@@ -499,7 +499,7 @@ rn_status reuse_ops_scan_step(const rn_scan_shape *shape, const rn_scan_inputs *
     if (shape->tokens != shape->n) return fail(RN_EINVAL, "a step takes one token a stream: tokens must be n");
     if (slots < 0 || (!ids && slots < shape->n)) return fail(RN_EINVAL, "fewer slots than streams");
     if (shape->n == 0) return RN_OK;
-    if (!state || !out) return fail(RN_EINVAL, "state and out must not be NULL");
+    if ((slots > 0 && !state) || !out) return fail(RN_EINVAL, "state and out must not be NULL");
     if (shape->n > 1 && ((out == in->u && shape->u_stride != shape->channels) ||
                          (out == in->dt && shape->dt_stride != shape->channels) ||
                          (out == in->z && shape->z_stride != shape->channels)))
@@ -588,7 +588,7 @@ rn_status reuse_ops_delta_step(const rn_delta_shape *shape, const void *q, const
     if (shape->tokens != shape->n) return fail(RN_EINVAL, "a step takes one token a stream: tokens must be n");
     if (slots < 0 || (!ids && slots < shape->n)) return fail(RN_EINVAL, "fewer slots than streams");
     if (shape->n == 0) return RN_OK;
-    if (!state || !out) return fail(RN_EINVAL, "state and out must not be NULL");
+    if ((slots > 0 && !state) || !out) return fail(RN_EINVAL, "state and out must not be NULL");
     DeltaArgs a = delta_args(shape, q, k, v, g, beta);
     a.ids = ids, a.slots = slots, a.final_state = state, a.out = out;
     return launched(launch_delta_step(a, shape->dtype == RN_BF16, static_cast<hipStream_t>(stream)));

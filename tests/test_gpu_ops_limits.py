@@ -74,3 +74,22 @@ def test_weight_gradients_wider_than_a_grid_axis_holds():
     # a thread adds 2^17 terms of random sign in a row: 2^8.5 roundings of their sum's size, which dx shares through two means
     d = dy.double()
     assert R.rel(dx, 1.5 * (d - d.mean() - xh * (d * xh).mean())) <= 2.0 ** -24 * 2 ** 8.5
+
+
+def test_steps_of_an_empty_pool():
+    """No id is a slot of a pool of 0 slots: every out is 0."""
+    from paper_1909_05632_amd import ops
+    ids = torch.tensor([0, -1, 7], dtype=torch.int32, device="cuda")
+    for dtype in (torch.float32, torch.bfloat16):
+        for channels, states in ((70, 16), (9, 5)):
+            x, a = torch.randn(3, channels, device="cuda").to(dtype), torch.zeros(channels, states, device="cuda")
+            b, pool = torch.randn(3, 1, states, device="cuda").to(dtype), torch.empty(0, channels, states, device="cuda")
+            out = torch.ones(3, channels, dtype=dtype, device="cuda")
+            assert ops.scan_step(x, x, a, b, b, pool, stream_ids=ids, out=out) is out and not out.any()
+            for taps in (1, 4):
+                w, pool = torch.randn(channels, taps, device="cuda"), torch.empty(0, taps - 1, channels, dtype=dtype, device="cuda")
+                out = torch.ones(3, channels, dtype=dtype, device="cuda")
+                assert ops.causal_conv_step(x, w, pool, stream_ids=ids, out=out) is out and not out.any()
+        q, v = torch.randn(3, 2, 8, device="cuda").to(dtype), torch.randn(3, 4, 5, device="cuda").to(dtype)
+        g, pool, out = torch.zeros(3, 4, device="cuda"), torch.empty(0, 4, 8, 5, device="cuda"), torch.ones_like(v)
+        assert ops.delta_step(q, q, v, g, g, pool, stream_ids=ids, out=out) is out and not out.any()
