@@ -64,7 +64,12 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_join(ScanArgs a) {
             if (k + u >= count) break;
             *own_states(a, a.ends, slot + (BACK ? count - 1 - k - u : k + u), c, quad) = h;
 #pragma unroll
-            for (int n = 0; n < kStates; ++n) h[n] = fmaf(__builtin_amdgcn_exp2f(s[u] * decay[n]), h[n], end[u][n]);
+            for (int n = 0; n < kStates; ++n) {
+                // Where states grow, a chunk's factor may be past float32 and its product with the
+                // state not: then in two factors.  Of a state of 0 there is nothing to grow.
+                const float x = s[u] * decay[n], over = x > 126.f && h[n] != 0.f ? x - 126.f : 0.f;
+                h[n] = fmaf(__builtin_amdgcn_exp2f(x > 126.f ? 126.f : x), h[n] * __builtin_amdgcn_exp2f(over), end[u][n]);
+            }
         }
     }
 }

@@ -402,3 +402,25 @@ def test_a_step_of_zero_leaves_the_state_whatever_a_is():
         assert (dstate == tokens).all()
         assert (ops.scan_step(u[:1], dt[:1], a, b[:1], b[:1], state, softplus=False) == 1).all()
         assert torch.equal(final, state)
+
+
+def test_states_that_grow_across_chunks():
+    """a above 0: over a chunk exp(sum of s a) may be past float32 while the state is 0, or so small that the
+    product is not.  (Exponents of up to 140 are off by 140 2^-24 of the result at each of two roundings: 2e-5.)"""
+    from paper_1909_05632_amd import ops
+    gen = torch.Generator().manual_seed(4)
+    tokens, channels = 200, 3
+    for states in (2, 6):
+        a = 6 - 2 * torch.arange(states).float().remainder(2).expand(channels, states)
+        u, dout = torch.zeros(tokens, channels), torch.zeros(tokens, channels)
+        u[-5:], dout[:5] = torch.randn(5, channels, generator=gen), torch.randn(5, channels, generator=gen)
+        x = dict(u=u, dt=torch.ones(tokens, channels), a=a.contiguous(), b=torch.randn(tokens, 1, states, generator=gen),
+                 c=torch.randn(tokens, 1, states, generator=gen), d=None, z=None, dt_bias=None, state=None)
+        out, _, grads = _check(x, dout, None, [0, tokens], softplus=False)
+        assert out[-5:].all() and not out[:-5].any() and grads["du"][:5].all() and not grads["du"][5:].any()
+        # a state of 1e-30, over 16 tokens of growth, then held
+        x["dt"][16:], x["u"], x["state"] = 0, torch.zeros_like(u), torch.full((1, channels, states), 1e-30)
+        g = _cuda(x)
+        out, final = ops.scan_forward(**g, softplus=False, n=1)
+        y, last = S.scan({k: None if v is None else v.double() for k, v in x.items()}, [0, tokens], False)
+        assert R.rel(final, last) <= 4e-5 and R.rel(out, y) <= 4e-5
