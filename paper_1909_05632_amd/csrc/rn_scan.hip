@@ -49,29 +49,48 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_join(ScanArgs a) {
     const int begin = seqs.offset(seq), len = max(0, seqs.offset(seq + 1) - begin);
     const int64_t slot = scan_end_slot(a, begin), count = (len + a.chunk() - 1) >> a.log_chunk;
     if (count < 2) return;
-    const f32x4 decay = load_decay(a, c, quad * kStates);
+    const f32x4 decay = finite_decay(load_decay(a, c, quad * kStates));
     f32x4 h = load_states(a, BACK ? a.dfinal : a.state, seq, c, quad * kStates, true);
-    for (int64_t k = 0; k < count; k += kJoin) {
-        f32x4 end[kJoin];
-        float s[kJoin];
+    // The chunks of k, k + kJoin, .. one after the other.  GROWS: a chunk's factor may be past
+    // float32 and its product with the state not, so such go in factors that are not.
+    const auto walk = [&](auto grows) {
+        const float most = fmaxf(fmaxf(decay[0], decay[1]), fmaxf(decay[2], decay[3]));
+        const float least = fminf(fminf(decay[0], decay[1]), fminf(decay[2], decay[3]));
+        for (int64_t k = 0; k < count; k += kJoin) {
+            f32x4 end[kJoin];
+            float s[kJoin], lo = 0.f, hi = 0.f;
 #pragma unroll
-        for (int u = 0; u < kJoin; ++u) {               // past the last one: the last one's, not used
-            const int64_t m = min(k + u, count - 1), j = slot + (BACK ? count - 1 - m : m);
-            end[u] = *own_states(a, a.ends, j, c, quad), s[u] = a.sums[j * a.channels + c];
-        }
+            for (int u = 0; u < kJoin; ++u) {           // past the last one: the last one's, not used
+                const int64_t m = min(k + u, count - 1), j = slot + (BACK ? count - 1 - m : m);
+                end[u] = *own_states(a, a.ends, j, c, quad), s[u] = a.sums[j * a.channels + c];
+            }
+            if constexpr (decltype(grows)::value) {
 #pragma unroll
-        for (int u = 0; u < kJoin; ++u) {
-            if (k + u >= count) break;
-            *own_states(a, a.ends, slot + (BACK ? count - 1 - k - u : k + u), c, quad) = h;
+                for (int u = 0; u < kJoin; ++u) lo = fminf(lo, s[u]), hi = fmaxf(hi, s[u]);
+            }
+            const bool past = hi * most > 126.f || lo * least > 126.f;
 #pragma unroll
-            for (int n = 0; n < kStates; ++n) {
-                // Where states grow, a chunk's factor may be past float32 and its product with the
-                // state not: then in two factors.  Of a state of 0 there is nothing to grow.
-                const float x = s[u] * decay[n], over = x > 126.f && h[n] != 0.f ? x - 126.f : 0.f;
-                h[n] = fmaf(__builtin_amdgcn_exp2f(x > 126.f ? 126.f : x), h[n] * __builtin_amdgcn_exp2f(over), end[u][n]);
+            for (int u = 0; u < kJoin; ++u) {
+                if (k + u >= count) break;
+                *own_states(a, a.ends, slot + (BACK ? count - 1 - k - u : k + u), c, quad) = h;
+                f32x4 x = s[u] * decay;
+                if (decltype(grows)::value && past)
+#pragma unroll
+                    for (int n = 0; n < kStates; ++n) {   // 2^378: more than any state but 0 has room for
+                        h[n] *= __builtin_amdgcn_exp2f(fminf(fmaxf(x[n] - 126.f, 0.f), 126.f));
+                        h[n] *= __builtin_amdgcn_exp2f(fminf(fmaxf(x[n] - 252.f, 0.f), 126.f));
+                        x[n] = x[n] > 126.f ? 126.f : x[n];
+                    }
+#pragma unroll
+                for (int n = 0; n < kStates; ++n) h[n] = fmaf(__builtin_amdgcn_exp2f(x[n]), h[n], end[u][n]);
             }
         }
-    }
+    };
+    // With steps by softplus and no a above 0 (which is how such layers are made) states only
+    // decay, and nothing is looked at: 16384 tokens' joins 19 us, otherwise 21.
+    const bool may = !a.softplus || !(decay[0] <= 0.f && decay[1] <= 0.f && decay[2] <= 0.f && decay[3] <= 0.f);
+    if (may) walk(std::true_type{});
+    else walk(std::false_type{});
 }
 
 // ------------------------------------------------------------------ sequences
@@ -125,6 +144,8 @@ __global__ __launch_bounds__(64, S <= 16 ? 5 : 1) void k_scan_seq(ScanArgs a) {
     constexpr int AT = S * sizeof(BC) <= 32 ? (LOCAL ? 4 : 2) : 1;    // tokens whose scalars are there at once (a wave has 100)
     TokenRows<BC> rows_b(a, 0, where.group, chunk.begin), rows_c(a, 1, where.group, chunk.begin);
     if (chunk.len > 0) fetch(0);
+#pragma unroll
+    for (int n = 0; n < S; ++n) decay[n] = finite_decay(decay[n]);
     for (int t0 = 0; t0 < chunk.len; t0 += kBatch) {
         // The step sizes of all tokens at once, for each is a long chain.
         const int m = min(kBatch, chunk.len - t0);
@@ -214,7 +235,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_step(ScanArgs a) {
     const int c = (int)(blockIdx.x * (kScanThreads / L) + threadIdx.x / L);
     if (c >= a.channels) return;                        // a channel's lanes at once
     const int group = c / (a.channels / a.groups);
-    const f32x4 decay = load_decay(a, c, n0);
+    f32x4 decay = load_decay(a, c, n0);
     const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, d = a.d ? a.d[c] : 0.f;
     if (a.slots == 0) {                                 // no state to read
         for (int r = blockIdx.y; r < a.n; r += gridDim.y)
@@ -255,6 +276,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_step(ScanArgs a) {
         return s;
     };
     Stream next = fetch(blockIdx.y);
+    decay = finite_decay(decay);
     for (int r = blockIdx.y; r < a.n; r += gridDim.y) {
         const Stream now = next;
         next = fetch(r + gridDim.y);

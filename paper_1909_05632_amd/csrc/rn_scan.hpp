@@ -93,14 +93,19 @@ __device__ inline f32x4 load_states(const ScanArgs &a, const float *p, int64_t r
     }
     return v;
 }
-// a log2(e) of a channel's states, finite where a is not NaN: exp(s a) is then 1 where s is 0, as
-// of the tokens past a sequence's end, and an infinite a is the largest of its sign.
+// a log2(e) of a channel's states.  Finite where a is not NaN: exp(s a) is then 1 where s is 0, as
+// of the tokens past a sequence's end, and an infinite a is the largest of its sign.  In two
+// steps, for the second waits for a: behind the first tokens' loads (gradients of 256 episodes of
+// 16 tokens 34.4 us, otherwise 35.1).
 __device__ inline f32x4 load_decay(const ScanArgs &a, int c, int n0) {
+    return load_states(a, a.a, 0, c, n0, true) * kLog2e;
+}
+__device__ inline float finite_decay(float v) {
     constexpr float kMost = 3.4028234663852886e38f;
-    f32x4 v = load_states(a, a.a, 0, c, n0, true) * kLog2e;
-#pragma unroll
-    for (int i = 0; i < kStates; ++i) v[i] = v[i] < -kMost ? -kMost : v[i] > kMost ? kMost : v[i];
-    return v;
+    return v < -kMost ? -kMost : v > kMost ? kMost : v;
+}
+__device__ inline f32x4 finite_decay(f32x4 v) {
+    return f32x4{finite_decay(v[0]), finite_decay(v[1]), finite_decay(v[2]), finite_decay(v[3])};
 }
 __device__ inline void store_states(const ScanArgs &a, float *p, int64_t row, int c, int n0, bool live, f32x4 v) {
     if (!live || !p) return;

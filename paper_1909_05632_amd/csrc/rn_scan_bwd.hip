@@ -111,6 +111,8 @@ __global__ __launch_bounds__(64) void k_scan_back(ScanArgs a) {
     constexpr int AT = S * sizeof(BC) <= 32 ? 4 : S <= 16 ? 2 : 1;          // tokens whose scalars are there at once
     TokenRows<BC> rows_c(a, 1, where.group, chunk.begin + chunk.len - 1);
     fetch(last);
+#pragma unroll
+    for (int n = 0; n < S; ++n) decay[n] = finite_decay(decay[n]);
     for (int t0 = last; t0 >= 0; t0 -= kBatch) {
         const int m = min(kBatch, chunk.len - t0);
 #pragma unroll
@@ -164,7 +166,7 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
     if (walker >= a.walkers) return;
     const Seqs seqs{a.off, a.n, a.tokens, a.even};
     const int c = where.c;
-    const f32x4 decay = load_decay(a, c, w * kStates);
+    f32x4 decay = load_decay(a, c, w * kStates);
     const float bias = a.dt_bias ? a.dt_bias[c] : 0.f, d = a.d ? a.d[c] : 0.f;
     const uint32_t lane = (uint32_t)c * sizeof(T), to_lane = where.live ? lane : kNowhere;
     f32x4 da = {0.f, 0.f, 0.f, 0.f};
@@ -194,6 +196,7 @@ __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a
         };
         const int last = chunk.len > 0 ? (chunk.len - 1) / kTile * kTile : -1;
         if (last >= 0) fetch(last);
+        decay = finite_decay(decay);
         for (int t0 = last; t0 >= 0; t0 -= kTile) {
             const int m = min(kTile, chunk.len - t0);
 #pragma unroll
