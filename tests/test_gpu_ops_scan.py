@@ -424,3 +424,50 @@ def test_states_that_grow_across_chunks():
         out, final = ops.scan_forward(**g, softplus=False, n=1)
         y, last = S.scan({k: None if v is None else v.double() for k, v in x.items()}, [0, tokens], False)
         assert R.rel(final, last) <= 4e-5 and R.rel(out, y) <= 4e-5
+
+
+# Chunks of `chunk` tokens in the gradients: the least power of two, 32 or more, that
+# leaves no more than 4096 for all blocks of channels (64 of a group, or what it has).
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tokens,channels,states,groups,n,chunk", [
+    (1100, 130, 16, 130, 2, 64), (1200, 140, 64, 140, 3, 64), (1200, 300, 32, 150, 2, 64), (1000, 270, 4, 270, 1, 128),
+    (1300, 230, 7, 230, 3, 128), (1400, 390, 16, 390, 2, 256), (900, 600, 33, 600, 1, 256), (2100, 4160, 16, 1, 3, 64),
+    (2200, 4100, 8, 2, 2, 64), (1500, 6200, 4, 1, 2, 64)])
+def test_gradients_in_chunks_of_several_tiles(tokens, channels, states, groups, n, chunk, dtype):
+    blocks = groups * -(-(channels // groups) // 64)
+    assert max(32, 1 << (-(-tokens * blocks // 4096) - 1).bit_length()) == chunk and tokens / n > 2 * chunk
+    x, dout, dfinal = S.inputs(tokens, channels, states, groups, n, dtype, seed=tokens)
+    off = _cuts(tokens, n, seed=groups)
+    assert max(q - p for p, q in zip(off, off[1:])) > 2 * chunk
+    out, final, grads = _run(x, dout, dfinal, seq_off=torch.tensor(off, dtype=torch.int32).cuda())
+    leaves = {k: v.cuda().double().requires_grad_() for k, v in x.items()}
+    y, last = S.scan(leaves, off)
+    assert R.rel(out, y) <= TOL[dtype] and R.rel(final, last) <= TOL[F32]
+    loss = (y * dout.cuda().double()).sum() + (last * dfinal.cuda().double()).sum()
+    for k, want in zip(S.NAMES, torch.autograd.grad(loss, [leaves[k] for k in S.NAMES])):
+        assert R.rel(grads["d" + k], want) <= (TOL[F32] if k in WIDE else TOL[dtype]), k
+
+
+def test_gradients_past_32_bits():
+    """600000 tokens of 4096 channels in bfloat16 are 2.4e9 elements: the gradients of the last tokens, and of the
+    first, are those of calls of their own (decays are e^-0.02 a token at most: 2000 tokens on, nothing is left)."""
+    from paper_1909_05632_amd import ops
+    tokens, channels, states, part, far = 600000, 4096, 2, 512, 2000
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    u, dt = (torch.empty(tokens, channels, dtype=BF16, device="cuda").normal_(generator=gen) for _ in range(2))
+    b, c = (torch.empty(tokens, 1, states, dtype=BF16, device="cuda").normal_(generator=gen) for _ in range(2))
+    a = -torch.rand(channels, states, generator=gen, device="cuda") - 0.05
+    saved = ops.scan_forward(u, dt, a, b, c, n=1, save=True)[2]
+    grads = dict(zip(S.GRADS, ops.scan_backward(u, u, dt, a, b, c, n=1, saved=saved)))
+    del saved
+    for lo, hi, keep in ((0, part + far, slice(0, part)), (tokens - part - far, tokens, slice(far, part + far))):
+        x = [t[lo:hi] for t in (u, dt)] + [a] + [t[lo:hi] for t in (b, c)]
+        kept = ops.scan_forward(*x, n=1, save=True)[2]
+        alone = dict(zip(S.GRADS, ops.scan_backward(x[0].contiguous(), *x, n=1, saved=kept)))
+        for k in ("du", "ddt", "db", "dc"):
+            assert R.rel(grads[k][lo:hi][keep], alone[k][keep]) <= TOL[BF16], k
+        if lo == 0:
+            assert R.rel(grads["dstate"], alone["dstate"]) <= TOL[F32]
+    assert torch.isfinite(grads["da"]).all()
+    del u, dt, grads
+    torch.cuda.empty_cache()
