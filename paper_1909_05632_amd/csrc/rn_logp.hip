@@ -499,7 +499,9 @@ hipError_t run_backward(const LogpArgs &a, hipStream_t s) {
         return hipGetLastError();
     }
     constexpr int VEC = 16 / sizeof(T), PER = kTurns * kThreads;
-    const int pieces = ((a.vocab + VEC - 1) / VEC + 1 + PER - 1) / PER;      // a row may begin inside a vector
+    // A row may begin inside a vector.  (Where none does and vocab is a multiple of PER
+    // vectors, a block a row has nothing to do: one of 9 at 131072 bfloat16.)
+    const int pieces = ((a.vocab + VEC - 1) / VEC + 1 + PER - 1) / PER;
     k_logp_bwd<T><<<grid_of((int64_t)a.n * pieces), kThreads, 0, s>>>(a, pieces);
     return hipGetLastError();
 }

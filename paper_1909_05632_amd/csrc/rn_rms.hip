@@ -7,9 +7,9 @@
 // then a function of h and w alone, and enters the row's scale.
 //
 // A few operations per element: bound by HBM.  A row stays in the registers of the
-// G lanes that own it, so every input is read once.  16384 x 4096 bfloat16: forward 94 us
-// (5.7 TB/s), backward 109 and 5 for the sum over blocks (4.9 TB/s); 1024 x 8192 to 8
-// bits 18 us (3.3 TB/s: there is a tenth of the bytes to have on their way).
+// G lanes that own it, so every input is read once.  16384 x 4096 bfloat16: forward 92 us
+// (5.8 TB/s), backward 109 and 5 for the sum over blocks (4.9 TB/s); 1024 x 8192 to 8
+// bits 17 us (3.4 TB/s: there is a tenth of the bytes to have on their way).
 #include "rn_rows.hpp"
 
 namespace rn {

@@ -11,9 +11,10 @@
 // chunks begin with, one after the other (k_scan_join: a chunk's decay is that of
 // its summed step sizes), then every chunk with its state.
 //
-// 16384 ragged tokens of 4096 channels of 16 states, bfloat16: 205 us for the chunks'
-// ends, 19 for what they begin with, 290 for all tokens, vector instructions in 96% and
-// 91% of the cycles: a token's step size, gate and stores are a quarter of them.
+// 16384 ragged tokens of 4096 channels of 16 states, bfloat16: 190 to 213 us for the
+// chunks' ends, 18 to 20 for what they begin with, 270 to 298 for all tokens (by the card's
+// clock), vector instructions in 98% and 88% of the cycles: a token's step size, gate and
+// stores are a quarter of them.  The whole call 447 us; of 4 states 260, of 32 880, of 64 1793.
 #include "rn_scan.hpp"
 
 namespace rn {
@@ -37,7 +38,8 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_pack(ScanArgs a) {
 
 // A thread four states: what each chunk of a sequence begins with, in place of its
 // end.  BACK: the same from the last chunk to the first, for gradients (state:
-// dfinal).  Loads of kJoin chunks are on their way at once.
+// dfinal).  Loads of kJoin chunks are on their way at once (18 us for 16384 tokens; of 16
+// 19.5, of 32 24).
 constexpr int kJoin = 8;
 template <bool BACK>
 __global__ __launch_bounds__(kScanThreads) void k_scan_join(ScanArgs a) {
@@ -87,7 +89,7 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_join(ScanArgs a) {
         }
     };
     // With steps by softplus and no a above 0 (which is how such layers are made) states only
-    // decay, and nothing is looked at: 16384 tokens' joins 19 us, otherwise 21.
+    // decay, and nothing is looked at: 16384 tokens 19 us, otherwise 21.
     const bool may = !a.softplus || !(decay[0] <= 0.f && decay[1] <= 0.f && decay[2] <= 0.f && decay[3] <= 0.f);
     if (may) walk(std::true_type{});
     else walk(std::false_type{});
@@ -97,8 +99,11 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_join(ScanArgs a) {
 
 // A wave takes 64 channels of a chunk by itself, all S states of a channel in the
 // registers of its lane.  LOCAL: of every chunk but a sequence's last, the state at
-// its end from 0, and its summed step sizes.  Five waves a SIMD where the registers
-// allow (302 us without the bound, 290 with it, 10% more with one of six).
+// its end from 0, and its summed step sizes.  Five waves a SIMD up to 16 states (302 us
+// without the bound, 290 with it, 10% more with one of six); bfloat16 ones of 16 put two or
+// three registers by in scratch for that.  Of 32 and 64 states three and two waves fit, and
+// 28 to 90 of a token's scalars are kept in vector registers' lanes, from where vector
+// instructions fetch them.
 template <class T, class BC, int S, bool LOCAL>
 __global__ __launch_bounds__(64, S <= 16 ? 5 : 1) void k_scan_seq(ScanArgs a) {
     const uint32_t block = block_index();
@@ -224,9 +229,10 @@ __device__ inline float over_states(float v) {
     return v;
 }
 
-// Bound by the states' bytes: 1024 streams of 2048 channels of 16 states, 57 us (5.0
-// TB/s) where the pool is in the last-level cache, 88 otherwise.  (Loads and stores that
-// pass by the caches: 80 and 81.)
+// Bound by the states' bytes: 1024 streams of 2048 channels of 16 states, 58 us (4.9
+// TB/s) where the pool is in the last-level cache, 88 otherwise (3.2 TB/s: short of a copy's
+// 4.7, with one vector of states a lane on its way beside eleven small loads; not taken
+// further).  Loads and stores that pass by the caches: 80 and 81.
 // L lanes carry a channel, four states each, so that a wave's accesses are one piece;
 // blocks walk the streams with the grid's second axis.
 template <class T, int L, bool WHOLE>
@@ -355,6 +361,12 @@ int64_t scan_blocks(int channels, int groups) { return (int64_t)groups * ((chann
 // forward 52, 52 and 92, and training 3 of 2480 121, 103 and 120.  One chunk of four tiles
 // for all tokens where it holds them: no sequence has several, which is known here then
 // (training 9 of 5 tokens 60, otherwise 73).
+// Around the ends of the rule, chunks of one tile and of two, us: 2048 tokens of 256 channels
+// of 16 states forward, a mean of 56: 32 and 43, of 64: 32 and 43, of 1024: 43 and 47, of
+// 2048: 47 and 49; 4096 of 512: 50 and 56, 50 and 57, 64 and 60, 67 and 59; the same with
+// gradients 143 and 149, 139 and 145, 158 and 150, 170 and 154, of 64 states 741 and 711,
+// 723 and 690, 641 and 614, 639 and 606.  (Four tiles: slower in all of these.)
+// States and direction, which the rule does not look at, shift where the two meet.
 int scan_log_chunk(int64_t tokens, int n, int channels, int groups, bool backward) {
     const int64_t blocks = backward ? 4096 : 8192, want = (tokens * scan_blocks(channels, groups) + blocks - 1) / blocks;
     const int64_t mean = n > 0 ? tokens / n : 0;

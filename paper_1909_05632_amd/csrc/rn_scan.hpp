@@ -2,7 +2,8 @@
 //
 // A lane carries a channel, 64 of one group a wave: nothing passes between lanes but
 // the gradients of b and c, and a token's b and c, the same for all lanes, are
-// scalars, which the loads' own unit brings.
+// scalars, which the loads' own unit brings.  A group of fewer than 64 channels leaves
+// the wave's other lanes without work.
 #pragma once
 
 #include "rn_seq.hpp"

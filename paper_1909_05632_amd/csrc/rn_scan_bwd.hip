@@ -16,8 +16,8 @@
 // exponentials, 15 multiplications or multiply-adds, and a third of that again for the
 // sums over channels: those of a wave in registers (over_channels), of all waves by
 // another kernel, each in a fixed order.  8192 ragged tokens of 2048 channels of 16
-// states, bfloat16: k_scan_bwd 280 us, vector instructions in 3 of 4 of its cycles;
-// k_scan_back 76, the joins 15, the sums over blocks 19.
+// states, bfloat16: k_scan_bwd 276 to 293 us (by the card's clock), vector instructions
+// in 3 of 4 of its cycles; k_scan_back 75, its join 15, the sums over blocks 20.
 #include "rn_rows.hpp"
 #include "rn_scan.hpp"
 
@@ -149,7 +149,11 @@ __global__ __launch_bounds__(64) void k_scan_back(ScanArgs a) {
 // A block takes 64 channels, wave w of W their states 4 w .. 4 w + 3.  A token is
 // loaded, and its results are stored, by one of them.  Two waves a SIMD: at three, the
 // states of a tile do not fit the registers.  As many of its tokens' decays as fit too
-// stay there for the way back (8 of 16: 270 us; none 289; 10, with a spill, 275).
+// stay there for the way back (timed in turn: 8 of 16 286 us; none 300; 10, with a spill, 287).
+// Two sizes are off that, and slow for their work.  33 to 64 states (W = 16): sixteen waves
+// have 128 registers each, and 98 are put by in 328 bytes of scratch a lane, a tile's states
+// among them: 8192 tokens of 2048 channels of 64 states 2454 us, where those of 32 take 580.
+// 1 to 4 (W = 1): 33 KB of LDS a wave leave room for one a SIMD, 186 us.
 template <class T, int W>
 __global__ __launch_bounds__(64 * W, W == 16 ? 4 : 2) void k_scan_bwd(ScanArgs a) {
     // Tokens between barriers: sums of all waves for a whole tile of 64 states are more than the LDS.
